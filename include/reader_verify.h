@@ -18,7 +18,10 @@
  *   layers of a model in one launch), reader_kv_rearrange
  *   (Algorithm 4 on the paper's padded cache layout), reader_verify_attn_padded /
  *   reader_padded_append / reader_padded_rearrange (the padded cache of Sec. 4.3 run as a cache, to be
- *   measured against the paged one), reader_accept_noalloc.
+ *   measured against the paged one), reader_accept_noalloc;
+ *   and what comes before it: reader_prompt_append (head norms, position rotation and cache write of a prompt),
+ *   reader_prompt_attn (its causal attention over the paged cache) and reader_tree_rotate (the same norms and rotation
+ *   for draft nodes).
  *
  * Conventions common to every call
  *   - Every pointer named below is a DEVICE pointer owned by the caller unless it says "host".
@@ -389,6 +392,104 @@ reader_status reader_accept_noalloc(reader_ctx *ctx, const reader_tree *tree, co
                                     const float *logits, int32_t vocab, int32_t *target_ids,
                                     int32_t max_path, int32_t *path_out, int32_t *n_acc_out,
                                     int32_t *bonus_out, int32_t *status_out, void *stream);
+
+/*
+ * ---- From a prompt to a cache, from a projection to a tree --------------------------------------------------------
+ * The calls above start from a cache that holds the prompt and from tree tensors that hold rotated keys.  The calls
+ * below make both, in the same conventions:
+ *   prompt, per layer:   reader_prompt_append -> reader_prompt_attn          (whole prompts, pieces of prompts, and
+ *                                                                             single tokens without a draft)
+ *   step, per layer:     reader_tree_rotate -> reader_verify_attn -> ...
+ */
+
+/*
+ * New tokens of a batch, packed one sequence behind the other without padding.
+ *   token_start   i32 [batch + 1]: rows token_start[b] .. token_start[b+1]-1 of the packed tensors belong to
+ *                 sequence b (none when the two are equal); non-decreasing, within [0, total_tokens]
+ *   total_tokens  rows of the packed tensors; rows outside every sequence are neither read nor written, so a
+ *                 captured call may be given tensors larger than a step needs
+ * Token i of sequence b stands at position seq_lens[b] + i: seq_lens counts the tokens committed before this call.
+ * An array that breaks the convention gives READER_ERR_INVALID_ARG in every status word, and nothing else is written.
+ */
+typedef struct {
+    int32_t batch, total_tokens;
+    const int32_t *token_start;
+} reader_prompt;
+
+/*
+ * What happens to a head of queries or keys x[0 .. head_dim-1] before it is used.
+ *   q_weight, k_weight  bf16 [head_dim]: x := x * rsqrt(mean(x^2) + eps) * weight, per head; both NULL: no norm
+ *   rope           f32 [max_positions][2][rot_dim / 2]: cosines, then sines, of each position's angles (any scaling of
+ *                  the angles is the caller's); NULL: no rotation.  The first rot_dim elements of a head are rotated:
+ *                  pair j is (j, j + rot_dim/2), or (2j, 2j + 1) if interleaved != 0:
+ *                  (a, b) := (a cos - b sin, b cos + a sin)
+ *   rot_dim        a multiple of 16, at most head_dim
+ * fp32 arithmetic, one rounding (nearest even) to bf16 at the end.
+ */
+typedef struct {
+    const void *q_weight, *k_weight;
+    float eps;
+    const float *rope;
+    int32_t max_positions, rot_dim, interleaved;
+} reader_rotation;
+
+/*
+ * A projection's output into the cache: queries and keys of the new tokens are normalised and rotated, keys and
+ * values written to the pages of their positions seq_lens[b] + i, queries to q_out.  seq_lens is not changed (the last
+ * layer's reader_prompt_attn advances it).
+ *   q, k, v    bf16: head h of token t at q + t * q_stride + h * head_dim (strides in elements, multiples of 8): the
+ *              parts of one fused tensor or tensors of their own
+ *   q_out      bf16 [total_tokens][n_q_heads][head_dim]; may be q itself if q_stride = n_q_heads * head_dim
+ *   status_out i32 [batch]: READER_ERR_CAPACITY when the page table or the rope table cannot hold the new positions
+ *              or they begin below shared_prefix_len, READER_ERR_BAD_PAGE when a page that would be written is
+ *              outside the pool: nothing of that sequence is written to the cache, its rows of q_out are zero
+ * head_dim 64 or 128.  Sequences must not share a page that the call writes to.
+ */
+reader_status reader_prompt_append(reader_ctx *ctx, const void *q, const void *k, const void *v, int64_t q_stride,
+                                   int64_t k_stride, int64_t v_stride, int32_t n_q_heads, reader_kv_cache *cache,
+                                   const reader_prompt *prompt, const reader_rotation *rotation, void *q_out,
+                                   int32_t *status_out, void *stream);
+
+/*
+ * The same for the nodes of draft trees: node j of sequence b stands at position seq_lens[b] + (nodes above it).
+ *   q, k, v    as above, token row b * n_nodes + j
+ *   q_out bf16 [batch][n_nodes][n_q_heads][head_dim], k_tree_out, v_tree_out bf16
+ *              [batch][n_nodes][n_kv_heads][head_dim]: the q, k_tree, v_tree of reader_verify_attn and
+ *              reader_kv_commit.  q_out (k_tree_out, v_tree_out) may be q (k, v) itself if that is dense.
+ *   status_out i32 [batch]: READER_ERR_BAD_TREE; READER_ERR_CAPACITY when seq_lens[b] < 0 or the rope table is too
+ *              short for the tree: that sequence's rows are zero
+ * tree->anc_mask is not used.
+ */
+reader_status reader_tree_rotate(reader_ctx *ctx, const void *q, const void *k, const void *v, int64_t q_stride,
+                                 int64_t k_stride, int64_t v_stride, int32_t n_q_heads, int32_t n_kv_heads,
+                                 int32_t head_dim, const reader_tree *tree, const int32_t *seq_lens,
+                                 const reader_rotation *rotation, void *q_out, void *k_tree_out, void *v_tree_out,
+                                 int32_t *status_out, void *stream);
+
+/* Bytes of device scratch that reader_prompt_attn needs, whatever the batch.  Host call, no CUDA work; 0 on bad
+ * arguments. */
+size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
+
+/*
+ * Causal attention of the new tokens over the cache, which already holds their own keys and values (from
+ * reader_prompt_append): token i of sequence b attends to the positions 0 .. seq_lens[b] + i.  With seq_lens[b] = 0 it
+ * is a whole prompt, otherwise the next piece of one, with a single token plain decoding; a call may mix them.
+ *   q, out     bf16 [total_tokens][n_q_heads][head_dim]
+ *   lse_out    f32 [total_tokens][n_q_heads], natural log of the softmax denominator; nullable
+ *   update_seq_lens  non-zero: seq_lens[b] += new tokens afterwards (pass 0 for all but the last layer)
+ *   workspace  at least reader_prompt_workspace_bytes(...) bytes, 256-byte aligned; contents are scratch, calls that
+ *              share it must not overlap on the GPU
+ *   status_out i32 [batch]: READER_ERR_CAPACITY, READER_ERR_BAD_PAGE, READER_ERR_TIMEOUT: that sequence's rows of out and
+ *              lse_out are zero and its length is not advanced
+ * softmax_scale > 0, n_q_heads / n_kv_heads at most 128, batch at most 32768, else READER_ERR_UNSUPPORTED.  What the
+ * cache holds at positions a token does not see has no influence on its row, infinities and NaN included.
+ * Arithmetic: bf16 inputs, fp32 accumulation and softmax, probabilities rounded to bf16 before the value product, bf16
+ * (nearest-even) output.
+ */
+reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_heads, reader_kv_cache *cache,
+                                 const reader_prompt *prompt, float softmax_scale, int32_t update_seq_lens, void *out,
+                                 float *lse_out, void *workspace, size_t workspace_bytes, int32_t *status_out,
+                                 void *stream);
 
 #ifdef __cplusplus
 }

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_float, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_float, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass
 from typing import Optional
 
@@ -27,7 +27,8 @@ EXPORTS = ("reader_create", "reader_destroy", "reader_status_string", "reader_se
            "reader_workspace_bytes", "reader_tree_encode", "reader_verify_attn", "reader_accept",
            "reader_kv_commit", "reader_accept_noalloc", "reader_sample_targets", "reader_kv_rearrange", "reader_kv_commit_layers",
            "reader_accept_commit", "reader_verify_prepare", "reader_verify_attn_prepared",
-           "reader_padded_workspace_bytes", "reader_verify_attn_padded", "reader_padded_append", "reader_padded_rearrange")
+           "reader_padded_workspace_bytes", "reader_verify_attn_padded", "reader_padded_append", "reader_padded_rearrange",
+           "reader_prompt_append", "reader_tree_rotate", "reader_prompt_workspace_bytes", "reader_prompt_attn")
 
 
 class ReaderError(RuntimeError):
@@ -49,6 +50,15 @@ class _PaddedCache(Structure):
 
 class _Tree(Structure):
     _fields_ = [("batch", c_int32), ("n_nodes", c_int32), ("parent", c_void_p), ("anc_mask", c_void_p)]
+
+
+class _Prompt(Structure):
+    _fields_ = [("batch", c_int32), ("total_tokens", c_int32), ("token_start", c_void_p)]
+
+
+class _Rotation(Structure):
+    _fields_ = [("q_weight", c_void_p), ("k_weight", c_void_p), ("eps", c_float), ("rope", c_void_p),
+                ("max_positions", c_int32), ("rot_dim", c_int32), ("interleaved", c_int32)]
 
 
 _lib = None
@@ -121,6 +131,18 @@ def load_library() -> ctypes.CDLL:
     lib.reader_padded_append.restype = c_int32
     lib.reader_padded_rearrange.argtypes = [c_void_p, POINTER(_PaddedCache), c_int32, c_void_p, c_void_p]
     lib.reader_padded_rearrange.restype = c_int32
+    lib.reader_prompt_append.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int32,
+                                         POINTER(_KvCache), POINTER(_Prompt), POINTER(_Rotation), c_void_p, c_void_p, c_void_p]
+    lib.reader_prompt_append.restype = c_int32
+    lib.reader_tree_rotate.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int32, c_int32,
+                                       c_int32, POINTER(_Tree), c_void_p, POINTER(_Rotation), c_void_p, c_void_p, c_void_p,
+                                       c_void_p, c_void_p]
+    lib.reader_tree_rotate.restype = c_int32
+    lib.reader_prompt_workspace_bytes.argtypes = [c_void_p, c_int32]
+    lib.reader_prompt_workspace_bytes.restype = c_size_t
+    lib.reader_prompt_attn.argtypes = [c_void_p, c_void_p, c_int32, POINTER(_KvCache), POINTER(_Prompt), c_float, c_int32,
+                                       c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.reader_prompt_attn.restype = c_int32
     lib.reader_kv_commit.argtypes = [c_void_p, POINTER(_KvCache), c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                                      c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
     lib.reader_kv_commit.restype = c_int32
@@ -144,6 +166,26 @@ def _dev(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
 
 def _stream() -> c_void_p:
     return c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _rows(t: torch.Tensor, name: str, shape) -> int:
+    """Checks a bf16 tensor [..., heads, head_dim] whose heads are dense and whose tokens are evenly spaced (a tensor of its
+    own or a part of a fused projection's output) and returns the token stride in elements."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16):
+        raise TypeError(f"{name}: need a CUDA tensor of dtype {torch.bfloat16}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: need shape {tuple(shape)}, got {tuple(t.shape)}")
+    heads, d = shape[-2:]
+    if t.numel() == 0:
+        return heads * d
+    if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != d):
+        raise ValueError(f"{name}: the heads of a token must be dense")
+    if len(shape) == 4:
+        b, n = shape[:2]
+        if b > 1 and n > 1 and t.stride(0) != n * t.stride(1):
+            raise ValueError(f"{name}: the tokens must be evenly spaced")
+        return t.stride(1) if n > 1 else t.stride(0) if b > 1 else heads * d
+    return t.stride(0) if shape[0] > 1 else heads * d
 
 
 @dataclass
@@ -196,6 +238,7 @@ class Reader:
             raise ReaderError(st, "reader_create")
         self._h = h
         self._ws: Optional[torch.Tensor] = None
+        self._prompt_ws: Optional[torch.Tensor] = None
 
     def close(self):
         if getattr(self, "_h", None):
@@ -529,6 +572,116 @@ class Reader:
         if st != OK:
             raise ReaderError(st, "reader_kv_commit")
         return slots, status
+
+    # ---- from a prompt to a cache, from a projection to a tree
+    def _here(self, *tensors: Optional[torch.Tensor]) -> None:
+        for t in tensors:
+            if t is not None and t.device.index != self.device:
+                raise ValueError(f"a tensor is on {t.device}, this reader on cuda:{self.device}")
+
+    def _rotation(self, head_dim: int, rope, q_weight, k_weight, eps: float, interleaved: bool) -> _Rotation:
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None and _dev(w, torch.bfloat16, name).shape != (head_dim,):
+                raise ValueError(f"{name}: need shape ({head_dim},)")
+        positions = rot = 0
+        if rope is not None:
+            _dev(rope, torch.float32, "rope")
+            if rope.dim() != 3 or rope.shape[1] != 2:
+                raise ValueError("rope: need [max_positions, 2, rot_dim / 2]")
+            positions, rot = rope.shape[0], 2 * rope.shape[2]
+        self._here(rope, q_weight, k_weight)
+        return _Rotation(None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+                         float(eps), None if rope is None else rope.data_ptr(), positions, rot, int(bool(interleaved)))
+
+    def _prompt(self, cache: KvCache, token_start: torch.Tensor, tokens: int) -> _Prompt:
+        _dev(token_start, torch.int32, "token_start")
+        B = cache.page_table.shape[0]
+        if token_start.shape != (B + 1,) or cache.seq_lens.shape != (B,):
+            raise ValueError("token_start: one more entry than the cache has sequences; seq_lens: one for each")
+        self._here(token_start, cache.page_table, cache.k_pool, cache.v_pool, cache.seq_lens)
+        return _Prompt(B, tokens, token_start.data_ptr())
+
+    def prompt_append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: KvCache, token_start: torch.Tensor,
+                      rope: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                      out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        """Head norms, rotation and cache write of packed new tokens: q [tokens, Hq, D], k and v [tokens, Hkv, D] (views of
+        a fused projection are fine), rope f32 [max_positions, 2, rot_dim / 2].  Returns (rotated queries, status)."""
+        c = cache._c()
+        tokens, Hq, D = q.shape
+        qs, ks, vs = _rows(q, "q", q.shape), _rows(k, "k", (tokens, c.n_kv_heads, c.head_dim)), _rows(v, "v", (tokens, c.n_kv_heads, c.head_dim))
+        if D != c.head_dim:
+            raise ValueError("q: its head dimension is not the cache's")
+        p, r = self._prompt(cache, token_start, tokens), self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
+        out = torch.empty((tokens, Hq, D), dtype=torch.bfloat16, device=q.device) if out is None else _dev(out, torch.bfloat16, "out")
+        status = torch.empty(p.batch, dtype=torch.int32, device=q.device) if status is None else _dev(status, torch.int32, "status")
+        if out.shape != q.shape or status.shape != (p.batch,):
+            raise ValueError("out: the shape of q; status: one word for each sequence")
+        self._here(q, k, v, out, status)
+        st = self.lib.reader_prompt_append(self._h, _ptr(q), _ptr(k), _ptr(v), qs, ks, vs, Hq, ctypes.byref(c), ctypes.byref(p),
+                                           ctypes.byref(r), _ptr(out), _ptr(status), _stream())
+        if st != OK:
+            raise ReaderError(st, "reader_prompt_append")
+        return out, status
+
+    def tree_rotate(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_lens: torch.Tensor, parent: torch.Tensor,
+                    rope: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                    k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                    out: Optional[torch.Tensor] = None, k_tree: Optional[torch.Tensor] = None,
+                    v_tree: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        """The same for draft nodes: q [B, T, Hq, D], k and v [B, T, Hkv, D], parent [B, T].  Returns
+        (q, k_tree, v_tree, status) for verify_attn and kv_commit."""
+        _dev(parent, torch.int32, "parent"); _dev(seq_lens, torch.int32, "seq_lens")
+        B, T, Hq, D = q.shape
+        Hkv = k.shape[2]
+        qs, ks, vs = _rows(q, "q", q.shape), _rows(k, "k", (B, T, Hkv, D)), _rows(v, "v", (B, T, Hkv, D))
+        if parent.shape != (B, T) or seq_lens.shape != (B,):
+            raise ValueError("parent: [B, T]; seq_lens: [B]")
+        r = self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
+        new = lambda t, heads, name: torch.empty((B, T, heads, D), dtype=torch.bfloat16, device=q.device) if t is None else _dev(t, torch.bfloat16, name)  # noqa: E731
+        out, k_tree, v_tree = new(out, Hq, "out"), new(k_tree, Hkv, "k_tree"), new(v_tree, Hkv, "v_tree")
+        status = torch.empty(B, dtype=torch.int32, device=q.device) if status is None else _dev(status, torch.int32, "status")
+        if out.shape != q.shape or k_tree.shape != k.shape or v_tree.shape != v.shape or status.shape != (B,):
+            raise ValueError("out, k_tree, v_tree: the shapes of q, k, v; status: one word for each sequence")
+        self._here(q, k, v, out, k_tree, v_tree, status, parent, seq_lens)
+        tr = _Tree(B, T, parent.data_ptr(), None)
+        st = self.lib.reader_tree_rotate(self._h, _ptr(q), _ptr(k), _ptr(v), qs, ks, vs, Hq, Hkv, D, ctypes.byref(tr), _ptr(seq_lens),
+                                         ctypes.byref(r), _ptr(out), _ptr(k_tree), _ptr(v_tree), _ptr(status), _stream())
+        if st != OK:
+            raise ReaderError(st, "reader_tree_rotate")
+        return out, k_tree, v_tree, status
+
+    def prompt_workspace(self) -> torch.Tensor:
+        """A cached device buffer for prompt_attn (of the size that any call needs: it is never replaced)."""
+        if self._prompt_ws is None:
+            need = int(self.lib.reader_prompt_workspace_bytes(self._h, 128))
+            self._prompt_ws = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
+        return self._prompt_ws
+
+    def prompt_attn(self, q: torch.Tensor, cache: KvCache, token_start: torch.Tensor, scale: float,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, update_seq_lens: bool = False,
+                    workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        """Causal attention of packed new tokens, whose K and V are in the cache at seq_lens[b] + i, over the cache:
+        q [tokens, Hq, D].  Returns (out, status); lse f32 [tokens, Hq] is filled if given."""
+        c = cache._c()
+        _dev(q, torch.bfloat16, "q")
+        tokens, Hq, D = q.shape
+        if D != c.head_dim:
+            raise ValueError("q: its head dimension is not the cache's")
+        p = self._prompt(cache, token_start, tokens)
+        out = torch.empty_like(q) if out is None else _dev(out, torch.bfloat16, "out")
+        status = torch.empty(p.batch, dtype=torch.int32, device=q.device) if status is None else _dev(status, torch.int32, "status")
+        if out.shape != q.shape or status.shape != (p.batch,):
+            raise ValueError("out: the shape of q; status: one word for each sequence")
+        if lse is not None and _dev(lse, torch.float32, "lse").shape != (tokens, Hq):
+            raise ValueError("lse: [tokens, Hq]")
+        ws = self.prompt_workspace() if workspace is None else _dev(workspace, torch.uint8, "workspace")
+        self._here(q, out, lse, status, ws)
+        st = self.lib.reader_prompt_attn(self._h, _ptr(q), Hq, ctypes.byref(c), ctypes.byref(p), float(scale), int(bool(update_seq_lens)),
+                                         _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _ptr(status), _stream())
+        if st != OK:
+            raise ReaderError(st, "reader_prompt_attn")
+        return out, status
 
 
 # ---------------------------------------------------------------------------------------------

@@ -5,6 +5,7 @@
 
 #include "common.cuh"
 #include "ctx.cuh"
+#include "rotate.cuh"
 
 
 namespace {
@@ -85,12 +86,18 @@ reader_status reader_create(reader_ctx **out, int device) {
         delete ctx;
         return st;
     }
+    if (!prompt_host_init(&ctx->prompt)) {
+        sm100_host_destroy(&ctx->sm100);
+        delete ctx;
+        return READER_ERR_CUDA;
+    }
     *out = ctx;
     return READER_OK;
 }
 
 void reader_destroy(reader_ctx *ctx) {
     if (!ctx) return;
+    prompt_host_destroy(&ctx->prompt);
     sm100_host_destroy(&ctx->sm100);
     delete ctx;
 }
@@ -598,6 +605,178 @@ reader_status reader_kv_commit(reader_ctx *ctx, reader_kv_cache *cache, const vo
     launch_kv_commit(*cache, static_cast<const __nv_bfloat16 *>(k_tree), static_cast<const __nv_bfloat16 *>(v_tree),
                      batch, n_nodes, path, n_acc, max_path, update_seq_lens, slots_out, status_out,
                      (cudaStream_t)stream);
+    return launch_status();
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the two norm-and-rotation calls share: the projection's output and the rotation.
+reader_status check_rotation(const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                             int Hq, int Hkv, int D, const reader_rotation *rot, RotateParams &p) {
+    if (!rot || !q || !k || !v) return READER_ERR_INVALID_ARG;
+    if (Hq < 1 || Hkv < 1 || (rot->q_weight == nullptr) != (rot->k_weight == nullptr)) return READER_ERR_INVALID_ARG;
+    if (Hq % Hkv != 0 || (D != 64 && D != 128)) return READER_ERR_UNSUPPORTED;
+    if (q_stride < (int64_t)Hq * D || k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D || q_stride % 8 != 0 ||
+        k_stride % 8 != 0 || v_stride % 8 != 0)
+        return READER_ERR_INVALID_ARG;
+    if (rot->q_weight && (!(rot->eps >= 0.f) || rot->eps > 3.0e38f)) return READER_ERR_INVALID_ARG;
+    if (rot->rope) {
+        if (rot->max_positions < 1 || rot->rot_dim < 1 || rot->rot_dim > D) return READER_ERR_INVALID_ARG;
+        if (rot->rot_dim % 16 != 0) return READER_ERR_UNSUPPORTED;   // a half is a whole number of 16-byte pieces
+    }
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(rot->q_weight) || !aligned16(rot->k_weight) || !aligned16(rot->rope))
+        return READER_ERR_INVALID_ARG;
+    p.q = static_cast<const __nv_bfloat16 *>(q);
+    p.k = static_cast<const __nv_bfloat16 *>(k);
+    p.v = static_cast<const __nv_bfloat16 *>(v);
+    p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;
+    p.q_weight = static_cast<const __nv_bfloat16 *>(rot->q_weight);
+    p.k_weight = static_cast<const __nv_bfloat16 *>(rot->k_weight);
+    p.rope = rot->rope;
+    p.eps = rot->eps;
+    p.max_positions = rot->max_positions; p.rot = rot->rope ? rot->rot_dim : 0; p.interleaved = rot->interleaved != 0;
+    p.Hq = Hq; p.Hkv = Hkv; p.D = D;
+    return READER_OK;
+}
+
+// The cache as the prompt calls need it (their tensors are checked by the calls).
+reader_status check_prompt(const reader_kv_cache *c, const reader_prompt *t, const int32_t *status_out) {
+    if (t->batch < 0 || t->total_tokens < 0 || !t->token_start || !status_out || !c->k_pool || !c->v_pool || !c->page_table || !c->seq_lens)
+        return READER_ERR_INVALID_ARG;
+    if (c->n_kv_heads < 1 || c->num_pages < 1 || c->max_pages_per_seq < 1 || c->shared_prefix_len < 0 || c->shared_prefix_len % kPage != 0)
+        return READER_ERR_INVALID_ARG;
+    if (c->page_size != kPage || (c->head_dim != 64 && c->head_dim != 128)) return READER_ERR_UNSUPPORTED;
+    if ((int64_t)c->max_pages_per_seq * kPage >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;   // positions are 32-bit
+    if (!aligned16(c->k_pool) || !aligned16(c->v_pool)) return READER_ERR_INVALID_ARG;
+    return READER_OK;
+}
+
+struct PromptWs {
+    size_t partial_o, partial_ml, pieces, gave_up, total;
+};
+PromptWs prompt_ws(const reader_ctx *ctx, int D) {
+    PromptWs w{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { size_t o = at; at = align_up(at + bytes); return o; };
+    const size_t rows = 2 * (size_t)ctx->n_sm * 256;
+    w.partial_o = take(sizeof(float) * rows * D);
+    w.partial_ml = take(sizeof(float) * rows * 2);
+    w.pieces = take(sizeof(PieceDesc) * (size_t)ctx->n_sm);
+    w.gave_up = take(sizeof(int32_t) * (size_t)ctx->n_sm);
+    w.total = at;
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+reader_status reader_prompt_append(reader_ctx *ctx, const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                                   int64_t v_stride, int32_t n_q_heads, reader_kv_cache *cache, const reader_prompt *prompt,
+                                   const reader_rotation *rotation, void *q_out, int32_t *status_out, void *stream) {
+    if (!ctx || !cache || !prompt) return READER_ERR_INVALID_ARG;
+    if (prompt->batch == 0) return READER_OK;
+    if (reader_status st = check_prompt(cache, prompt, status_out)) return st;
+    RotateParams p{};
+    // without a token there is no tensor to point at: only the status words are written
+    static const uint4 nothing = {};
+    const bool empty = prompt->total_tokens == 0;
+    if (reader_status st = check_rotation(empty ? &nothing : q, empty ? &nothing : k, empty ? &nothing : v, q_stride, k_stride, v_stride,
+                                          n_q_heads, cache->n_kv_heads, cache->head_dim, rotation, p))
+        return st;
+    if (!empty && (!q_out || !aligned16(q_out))) return READER_ERR_INVALID_ARG;
+    if ((int64_t)prompt->total_tokens + prompt->batch >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;   // one block each
+    p.B = prompt->batch;
+    p.tokens = prompt->total_tokens;
+    p.token_start = prompt->token_start;
+    p.seq_lens = cache->seq_lens;
+    p.page_table = cache->page_table;
+    p.max_pages = cache->max_pages_per_seq; p.num_pages = cache->num_pages; p.shared_prefix_len = cache->shared_prefix_len;
+    p.q_out = static_cast<__nv_bfloat16 *>(q_out);
+    p.k_out = static_cast<__nv_bfloat16 *>(cache->k_pool);
+    p.v_out = static_cast<__nv_bfloat16 *>(cache->v_pool);
+    p.status = status_out;
+    if (reader_status st = check_device(ctx)) return st;
+    launch_prompt_append(p, (cudaStream_t)stream);
+    return launch_status();
+}
+
+reader_status reader_tree_rotate(reader_ctx *ctx, const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                                 int64_t v_stride, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const reader_tree *tree,
+                                 const int32_t *seq_lens, const reader_rotation *rotation, void *q_out, void *k_tree_out,
+                                 void *v_tree_out, int32_t *status_out, void *stream) {
+    if (!ctx || !tree) return READER_ERR_INVALID_ARG;
+    if (tree->batch == 0) return READER_OK;
+    if (tree->batch < 0 || tree->n_nodes < 1 || tree->n_nodes > kMaxNodes || !tree->parent || !seq_lens || !q_out || !k_tree_out ||
+        !v_tree_out || !status_out || !aligned16(q_out) || !aligned16(k_tree_out) || !aligned16(v_tree_out))
+        return READER_ERR_INVALID_ARG;
+    RotateParams p{};
+    if (reader_status st = check_rotation(q, k, v, q_stride, k_stride, v_stride, n_q_heads, n_kv_heads, head_dim, rotation, p)) return st;
+    if ((int64_t)tree->batch * tree->n_nodes >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
+    p.B = tree->batch;
+    p.T = tree->n_nodes;
+    p.parent = tree->parent;
+    p.seq_lens = seq_lens;
+    p.q_out = static_cast<__nv_bfloat16 *>(q_out);
+    p.k_out = static_cast<__nv_bfloat16 *>(k_tree_out);
+    p.v_out = static_cast<__nv_bfloat16 *>(v_tree_out);
+    p.status = status_out;
+    if (reader_status st = check_device(ctx)) return st;
+    launch_tree_rotate(p, (cudaStream_t)stream);
+    return launch_status();
+}
+
+size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim) {
+    if (!ctx || (head_dim != 64 && head_dim != 128)) return 0;
+    return prompt_ws(ctx, head_dim).total;
+}
+
+reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_heads, reader_kv_cache *cache, const reader_prompt *prompt,
+                                 float softmax_scale, int32_t update_seq_lens, void *out, float *lse_out, void *workspace,
+                                 size_t workspace_bytes, int32_t *status_out, void *stream) {
+    if (!ctx || !cache || !prompt) return READER_ERR_INVALID_ARG;
+    if (prompt->batch == 0) return READER_OK;
+    if (reader_status st = check_prompt(cache, prompt, status_out)) return st;
+    const int B = prompt->batch, tokens = prompt->total_tokens, Hq = n_q_heads, Hkv = cache->n_kv_heads, D = cache->head_dim;
+    if (tokens > 0 && (!q || !out || !aligned16(q) || !aligned16(out))) return READER_ERR_INVALID_ARG;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0 || !aligned16(lse_out) || Hq < 1 || !(softmax_scale == softmax_scale))
+        return READER_ERR_INVALID_ARG;
+    // the row maximum is taken before the scaling, so the scale has to be positive; a query tile is a box of whole tokens
+    if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f || Hq % Hkv != 0 || Hq / Hkv > kTileM) return READER_ERR_UNSUPPORTED;
+    if (B > kPromptMaxBatch || (int64_t)cache->num_pages * Hkv * kPage >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
+    PromptAttnParams p{};
+    p.G = Hq / Hkv;
+    p.tile_tokens = kTileM / p.G;
+    // entries of the unit list, at most
+    const int64_t units = ((int64_t)tokens / (2 * p.tile_tokens) + B) * Hkv;
+    if (units * (((int64_t)cache->max_pages_per_seq + 1) / 2 + kUnitEntries) >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
+    const PromptWs w = prompt_ws(ctx, D);
+    if (workspace_bytes < w.total) return READER_ERR_WORKSPACE;
+    if (reader_status st = check_device(ctx)) return st;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    p.token_start = prompt->token_start;
+    p.seq_lens = cache->seq_lens;
+    p.page_table = cache->page_table;
+    p.B = B; p.tokens = tokens; p.Hq = Hq; p.Hkv = Hkv; p.D = D;
+    p.max_pages = cache->max_pages_per_seq; p.num_pages = cache->num_pages;
+    p.scale_log2 = softmax_scale * 1.4426950408889634f;
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.lse = lse_out;
+    p.status = status_out;
+    p.bump = update_seq_lens ? cache->seq_lens : nullptr;
+    p.partial_o = reinterpret_cast<float *>(ws + w.partial_o);
+    p.partial_ml = reinterpret_cast<float *>(ws + w.partial_ml);
+    p.pieces = reinterpret_cast<PieceDesc *>(ws + w.pieces);
+    p.gave_up = reinterpret_cast<int32_t *>(ws + w.gave_up);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (tokens > 0) {
+        p.n_ctas = ctx->n_sm;
+        if (reader_status s = launch_prompt_attn(&ctx->prompt, ctx->sm100.encode_tiled, p, static_cast<const __nv_bfloat16 *>(q), cache->k_pool, cache->v_pool, st))
+            return s;
+    }
+    launch_prompt_finish(p, st);
     return launch_status();
 }
 

@@ -1,0 +1,87 @@
+// Parameter block and work partition of the prompt attention (reader_prompt_attn).
+#pragma once
+#include "common.cuh"
+
+namespace reader {
+
+constexpr int kPromptMaxBatch = 32768;   // the partition of a call is worked out in shared memory, one word per sequence
+constexpr int kKeyTile = 128;            // keys per tile: two cache pages
+
+// A unit is (sequence, KV head, block of 2 * tile_tokens consecutive new tokens): up to 256 query rows, row
+// = token * G + group member within each of two 128-row tiles.
+//   wide unit    both tiles have rows: a step is one key tile, multiplied with both query tiles
+//   narrow unit  only the first tile has rows (the last block of a sequence, every block of a single-token call):
+//                a step is two key tiles, each multiplied with the one query tile, merged at the unit's end
+// Units in the order (sequence, KV head, block), each kUnitEntries entries (what starting and ending a unit costs)
+// followed by its steps, form one list that is cut into contiguous equal ranges, one per CTA.
+constexpr int kUnitEntries = 2;
+constexpr int kMinEntriesPerCta = 4;
+
+struct PieceDesc {        // a unit that CTA c starts but does not finish: pieces 2c + 1, then 2(c + 1), 2(c + 2), ...
+    int32_t b, h, block;  // b = -1: none
+    int32_t more;         // how many CTAs follow
+    int32_t first_token, tokens, L;
+};
+
+struct PromptAttnParams {
+    const int32_t *token_start;   // [B + 1]
+    const int32_t *seq_lens, *page_table;
+    int B, tokens, Hq, Hkv, G, D, max_pages, num_pages;
+    int tile_tokens;              // tokens per 128-row tile: 128 / G, rounded down
+    float scale_log2;
+    __nv_bfloat16 *out;
+    float *lse;
+    int32_t *status;
+    int32_t *bump;                // seq_lens again when it is to be advanced, else null
+    int n_ctas;
+    // workspace
+    float *partial_o;             // [2 n_ctas][256][D]
+    float *partial_ml;            // [2 n_ctas][256][2]
+    PieceDesc *pieces;            // [n_ctas]
+    int32_t *gave_up;             // [n_ctas]
+};
+
+// Whether a sequence takes part: what the host cannot check and the partition depends on.
+__host__ __device__ inline bool prompt_len_ok(int L, int n, int max_pages) {
+    return n >= 0 && L >= 0 && (int64_t)L + n <= (int64_t)max_pages * kPage;
+}
+
+struct UnitShape {
+    int tokens;     // new tokens in the block
+    int keys;       // keys its last token sees
+    bool narrow;
+    int tiles, steps;
+};
+__host__ __device__ inline UnitShape unit_shape(int L, int n, int block, int tile_tokens) {
+    UnitShape u;
+    const int first = block * 2 * tile_tokens;
+    u.tokens = n - first < 2 * tile_tokens ? n - first : 2 * tile_tokens;
+    u.keys = L + first + u.tokens;
+    u.narrow = u.tokens <= tile_tokens;
+    u.tiles = (u.keys + kKeyTile - 1) / kKeyTile;
+    u.steps = u.narrow ? (u.tiles + 1) / 2 : u.tiles;
+    return u;
+}
+__host__ __device__ inline int unit_blocks(int n, int tile_tokens) { return (n + 2 * tile_tokens - 1) / (2 * tile_tokens); }
+
+// CTAs that share a list of W entries, where a CTA's range begins, and whose entry x is.
+__host__ __device__ inline int prompt_busy_ctas(int n_ctas, int W) {
+    const int want = (W + kMinEntriesPerCta - 1) / kMinEntriesPerCta;
+    return want < 1 ? 1 : want < n_ctas ? want : n_ctas;
+}
+__host__ __device__ inline int prompt_range_begin(int c, int W, int ctas) { return (int)((int64_t)c * W / ctas); }
+__host__ __device__ inline int prompt_range_owner(int x, int W, int ctas) { return (int)((((int64_t)x + 1) * ctas - 1) / W); }
+
+struct PromptMaps;
+struct PromptHost {
+    PromptMaps *maps;
+    bool attr_set;
+};
+bool prompt_host_init(PromptHost *h);
+void prompt_host_destroy(PromptHost *h);
+// `encode_tiled` is the driver's tensor-map encoder.
+reader_status launch_prompt_attn(PromptHost *h, void *encode_tiled, const PromptAttnParams &p, const __nv_bfloat16 *q,
+                                 const void *k_pool, const void *v_pool, cudaStream_t st);
+void launch_prompt_finish(const PromptAttnParams &p, cudaStream_t st);
+
+}  // namespace reader

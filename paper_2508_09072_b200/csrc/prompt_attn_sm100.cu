@@ -1,0 +1,910 @@
+// Causal attention of packed prompts over the paged cache on the sm_100a tensor cores (reader_prompt_attn).
+//
+// Query i of a sequence stands at position L + i and sees the keys 0 .. L + i, all of them in the cache.  One CTA
+// per SM walks its range of the unit list (prompt_attn.cuh).  It holds two 128-row query tiles and runs two
+// independent softmax streams ("slots") beside each other, so that the tensor pipe works for one slot while the
+// other slot's scores become probabilities:
+//
+//   warps 0-3, 4-7  softmax of slot 0 / 1: thread = query row, so a row's maximum and sum need no exchange
+//   warp 8          producer: K and V tiles of 128 keys (two cache pages) by TMA through one ring, in the order in
+//                   which they are multiplied; the query tiles of the next segment
+//   warp 9          issues S = Q K^T and O += P V for both slots:  PV0(i) S0(i+1) PV1(i) S1(i+1) ...
+//   warp 10         prepares the value tiles that hold keys some query of the unit does not see
+//
+// TMEM (512 columns): scores of slot 0 and 1 (128 columns each, fp32), outputs of slot 0 and 1 (D columns each).  The
+// probabilities (bf16 pairs, 64 columns) take the place of their scores.  S(i+1) of a slot is issued behind PV(i),
+// which reads P(i) from the same columns, and the tensor pipe runs a CTA's products in the order of their issue.
+//
+// Softmax: the exponentials of a tile are taken against the maximum known from the tiles before it while the tile's
+// own maximum is found on the side; only if that exceeds the old one by more than 2^8 is the maximum raised, the
+// output rescaled and the tile done again (always on a segment's first tile, hardly ever later).  Scores, maxima,
+// sums and outputs are fp32; P is rounded to bf16 for the value product (relative error of a weight 2^-9 at most, of
+// the size of the output's own rounding), the row sum adds the unrounded weights.
+//
+// Keys that a row does not see get the score -inf by selection, whatever the cache holds there.  Values cannot be
+// selected in a matrix product (0 * inf is NaN), so warp 10 goes over the tiles that hold keys of the unit's own
+// tokens: rows behind the unit's last key are not multiplied or zeroed; an infinity or NaN in a row that some of the
+// queries see is replaced by zero, and the epilogue adds it to exactly the rows that see it.
+//
+// Every wait is bounded: a CTA that waits a second without progress marks its word in the workspace, stops waiting
+// and runs to its end; the finishing kernel turns the mark into status words and zero rows.
+#include <cuda.h>
+
+#include <new>
+
+#include "prompt_attn.cuh"
+#include "ptx_sm100.cuh"
+
+namespace reader {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 11 * 32;
+constexpr int kProducerWarp = 8, kMmaWarp = 9, kValueWarp = 10;
+constexpr uint64_t kWaitLimitNs = 1000000000ull;
+constexpr float kRaiseMaxBy = 8.f;   // log2 units
+constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
+constexpr int kMaxStages = 10;
+constexpr int kPoisonRing = 8;       // segments the value warp may be ahead of an epilogue (the ring holds 5 value tiles)
+
+template <int D>
+struct Cfg {
+    static constexpr int kHalves = D / 64;                   // 64-column (128-byte) blocks per row
+    static constexpr int kBlockBytes = 128 * 128;            // one 64-column block of 128 rows
+    static constexpr int kTileBytes = kHalves * kBlockBytes; // a query, key or value tile
+    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int kOffRing = 2 * kTileBytes;
+    static constexpr int kOffMisc = kOffRing + kStages * kTileBytes;
+    static constexpr int kSmemBytes = kOffMisc + 2048;
+};
+
+struct Misc {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t raw[kMaxStages];  // a value tile that the value warp goes over first has landed; that warp then completes `full`
+    uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], merge_ready, merge_free;
+    float2 ml[128];            // slot 1's row maxima and sums of a narrow unit
+    int32_t poison[kPoisonRing];
+    int32_t seq, head, block, off, w_begin, w_end, W, ctas;
+    uint32_t tmem_base;
+    int32_t abort;
+};
+static_assert(sizeof(Misc) <= 2048, "shared memory behind the ring");
+
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int32_t *abort_s) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*abort_s) return false;
+    const uint64_t t0 = globaltimer_ns();
+    while (true) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_s) return false;
+        if (globaltimer_ns() - t0 > kWaitLimitNs) {
+            *abort_s = 1;
+            return false;
+        }
+    }
+}
+
+// A CTA's piece of a unit.
+struct Piece {
+    int b, h, block;
+    int start;               // first row of the sequence in the packed tensors
+    int L, n;
+    UnitShape u;
+    int t0, nt;              // key tiles of this piece
+    bool full;               // the whole unit
+    int slot;                // where its partial goes
+    int first_token;         // of the unit, within the sequence
+};
+
+// Walks a CTA's range; every role does it for itself.
+struct Walk {
+    int b, h, block, off, left, w;
+    int start, L, n, blocks;
+    __device__ __forceinline__ void open(const PromptAttnParams &p) {
+        start = p.token_start[b];
+        n = p.token_start[b + 1] - start;
+        L = p.seq_lens[b];
+        blocks = prompt_len_ok(L, n, p.max_pages) ? unit_blocks(n, p.tile_tokens) : 0;
+    }
+    __device__ __forceinline__ void init(const PromptAttnParams &p, const Misc *m) {
+        b = m->seq; h = m->head; block = m->block; off = m->off; w = m->w_begin; left = m->w_end - m->w_begin;
+        if (left > 0) open(p);
+    }
+    // The next segment with at least one key tile; false at the end of the range.
+    __device__ __forceinline__ bool next(const PromptAttnParams &p, Piece &s) {
+        while (left > 0) {
+            while (block >= blocks) {   // on to the next head, the next sequence with tokens
+                block = 0;
+                if (blocks == 0 || ++h == p.Hkv) {
+                    h = 0;
+                    if (++b >= p.B) { left = 0; return false; }
+                    open(p);
+                }
+            }
+            s.u = unit_shape(L, n, block, p.tile_tokens);
+            const int entries = kUnitEntries + s.u.steps;
+            const int take = min(entries - off, left);
+            const int s0 = max(0, off - kUnitEntries), s1 = off + take - kUnitEntries;
+            s.b = b; s.h = h; s.block = block;
+            s.start = start; s.L = L; s.n = n;
+            s.first_token = block * 2 * p.tile_tokens;
+            s.t0 = s.u.narrow ? 2 * s0 : s0;
+            s.nt = s1 <= s0 ? 0 : (s.u.narrow ? min(2 * s1, s.u.tiles) : s1) - s.t0;
+            s.full = s0 == 0 && s1 == s.u.steps;
+            s.slot = s0 == 0 ? 1 : 0;
+            w += take;
+            left -= take;
+            off += take;
+            if (off == entries) { off = 0; ++block; }
+            if (s.nt > 0) return true;
+        }
+        return false;
+    }
+};
+
+// Ring places of a segment's tiles.  Order: the first `ahead` key tiles, then V0, K(ahead), V1, K(ahead + 1), ...
+__device__ __forceinline__ int ahead_of(const Piece &s) { return min(s.u.narrow ? 2 : 1, s.nt); }
+__device__ __forceinline__ int place_of_k(int j, int ahead) { return j < ahead ? j : ahead + 2 * (j - ahead) + 1; }
+__device__ __forceinline__ int place_of_v(int j, int ahead, int nt) { return ahead + j + min(j, nt - ahead); }
+
+// Whether key tile t holds keys of the unit's own tokens (or none): its values go through the value warp.
+__device__ __forceinline__ bool has_own_keys(const Piece &s, int t) { return (t + 1) * kKeyTile > s.L + s.first_token; }
+
+// Works out the whole call's partition and this CTA's place in it (all threads; ends with a barrier).
+__device__ void partition(const PromptAttnParams &p, Misc *m, int32_t *sizes /* shared, [B] */) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    bool bad = false;
+    for (int b = tid; b < p.B; b += kThreads) {
+        const int a = p.token_start[b], e = p.token_start[b + 1];
+        bad |= a < 0 || a > e || e > p.tokens;
+    }
+    const bool none = __syncthreads_or(bad);
+    for (int b = warp; b < p.B; b += kThreads / 32) {
+        const int n = p.token_start[b + 1] - p.token_start[b], L = p.seq_lens[b];
+        int sum = 0;
+        if (!none && prompt_len_ok(L, n, p.max_pages)) {
+            const int blocks = unit_blocks(n, p.tile_tokens);
+            for (int i = lane; i < blocks; i += 32) sum += kUnitEntries + unit_shape(L, n, i, p.tile_tokens).steps;
+            sum = __reduce_add_sync(0xffffffffu, sum);
+        }
+        if (lane == 0) sizes[b] = sum;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        int total = 0;   // entries of one head of every sequence so far
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const int mine = b0 + lane < p.B ? sizes[b0 + lane] : 0;
+            int incl = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += up;
+            }
+            if (b0 + lane < p.B) sizes[b0 + lane] = total + incl - mine;
+            total += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        __syncwarp();
+        const int W = total * p.Hkv, ctas = prompt_busy_ctas(p.n_ctas, W), c = blockIdx.x;
+        const int begin = c < ctas ? prompt_range_begin(c, W, ctas) : W, end = c < ctas ? prompt_range_begin(c + 1, W, ctas) : W;
+        int b = 0, h = 0, block = 0, off = 0;
+        if (begin < end) {
+            int lo = 0, hi = p.B;   // the last sequence that begins at or before this CTA's first entry
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (sizes[mid] * p.Hkv <= begin) lo = mid; else hi = mid;
+            }
+            b = lo;
+            const int size = (b + 1 < p.B ? sizes[b + 1] : total) - sizes[b];
+            const int within = begin - sizes[b] * p.Hkv;
+            h = within / size;
+            off = within - h * size;
+            const int n = p.token_start[b + 1] - p.token_start[b], L = p.seq_lens[b];
+            const int blocks = unit_blocks(n, p.tile_tokens);
+            for (int i0 = 0; i0 < blocks; i0 += 32) {
+                const int mine = i0 + lane < blocks ? kUnitEntries + unit_shape(L, n, i0 + lane, p.tile_tokens).steps : 0;
+                int incl = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int up = __shfl_up_sync(0xffffffffu, incl, d);
+                    if (lane >= d) incl += up;
+                }
+                const unsigned here = __ballot_sync(0xffffffffu, off < incl);
+                if (here) {
+                    const int src = __ffs(here) - 1;
+                    block = i0 + src;
+                    off -= __shfl_sync(0xffffffffu, incl - mine, src);
+                    break;
+                }
+                off -= __shfl_sync(0xffffffffu, incl, 31);
+            }
+        }
+        if (lane == 0) {
+            m->seq = b; m->head = h; m->block = block; m->off = off;
+            m->w_begin = begin; m->w_end = end; m->W = W; m->ctas = ctas;
+        }
+    }
+    __syncthreads();
+}
+
+// Page ids of a piece's key tiles, 16 tiles at a time (one id per lane).
+struct PageCursor {
+    int t_first = 0, id = 0;
+    bool loaded = false;
+    __device__ __forceinline__ void get(const PromptAttnParams &p, const Piece &s, int t, int lane, int &a, int &b) {
+        if (!loaded || t - t_first >= 16) {
+            t_first = t;
+            const int i = 2 * t + lane, npages = (s.u.keys + kPage - 1) / kPage;
+            id = i < npages ? p.page_table[(size_t)s.b * p.max_pages + i] : 0;
+            loaded = true;
+        }
+        a = __shfl_sync(0xffffffffu, id, 2 * (t - t_first));
+        b = __shfl_sync(0xffffffffu, id, 2 * (t - t_first) + 1);
+    }
+};
+
+__device__ __forceinline__ bool nonfinite_bits(uint32_t half) { return (half & 0x7f80u) == 0x7f80u; }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                   const __grid_constant__ CUtensorMap vmap, const __nv_bfloat16 *__restrict__ v_pool) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (base & 1023u) {   // the swizzled tiles need 1024-byte alignment; never seen, but checked
+        if (tid == 0) {
+            p.gave_up[blockIdx.x] = 1;
+            p.pieces[blockIdx.x].b = -1;
+        }
+        return;
+    }
+    Misc *m = reinterpret_cast<Misc *>(smem + C::kOffMisc);
+    volatile int32_t *abort_s = &m->abort;
+    const uint32_t sQ = base, sRing = base + C::kOffRing;
+    auto bar = [&](const uint64_t *b) { return smem_u32(b); };
+
+    if (tid == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(bar(&m->full[i]), 1);
+            mbar_init(bar(&m->empty[i]), 1);
+            mbar_init(bar(&m->raw[i]), 1);
+        }
+        mbar_init(bar(&m->q_full), 1);
+        mbar_init(bar(&m->q_empty), 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(&m->s_full[s]), 1);
+            mbar_init(bar(&m->p_full[s]), 128);
+            mbar_init(bar(&m->o_full[s]), 1);
+        }
+        mbar_init(bar(&m->merge_ready), 128);
+        mbar_init(bar(&m->merge_free), 128);
+        m->abort = 0;
+        for (int i = 0; i < kPoisonRing; ++i) m->poison[i] = 0;
+        fence_mbar_init();
+        fence_proxy_async();
+        prefetch_tensormap(&qmap);
+        prefetch_tensormap(&kmap);
+        prefetch_tensormap(&vmap);
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(smem_u32(&m->tmem_base), kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = m->tmem_base;
+    // everything above overlapped the kernel before this one in the stream; its results are read from here on
+    grid_dependency_wait();
+    grid_launch_dependents();
+    partition(p, m, reinterpret_cast<int32_t *>(smem + C::kOffRing));
+    if (tid == 0) fence_proxy_async();   // the ring was scratch until here
+    __syncthreads();
+
+    Walk walk;
+    walk.init(p, m);
+    Piece sg{};
+
+    if (warp == kProducerWarp) {
+        // ------------------------------------------------------------------ producer
+        int r = 0, seg = 0;
+        auto load = [&](const CUtensorMap *map, int page_a, int page_b, int npg, bool raw) {
+            const int stage = r % C::kStages;
+            const bool ok = wait(bar(&m->empty[stage]), ((r / C::kStages) & 1) ^ 1, abort_s);
+            __syncwarp();
+            if (ok && elect_one()) {
+                const uint32_t full = bar(raw ? &m->raw[stage] : &m->full[stage]), dst = sRing + stage * C::kTileBytes;
+                mbar_arrive_expect_tx(full, npg * (C::kTileBytes / 2));
+                const int row_a = (page_a * p.Hkv + sg.h) * kPage, row_b = (page_b * p.Hkv + sg.h) * kPage;
+#pragma unroll
+                for (int hf = 0; hf < C::kHalves; ++hf) {
+                    tma_load_2d(dst + hf * C::kBlockBytes, map, full, hf * 64, row_a);
+                    if (npg > 1) tma_load_2d(dst + hf * C::kBlockBytes + C::kBlockBytes / 2, map, full, hf * 64, row_b);
+                }
+            }
+            __syncwarp();
+            ++r;
+        };
+        const int tile_rows_bytes = p.G * p.tile_tokens * 128;
+        while (!*abort_s && walk.next(p, sg)) {
+            if (wait(bar(&m->q_empty), (seg & 1) ^ 1, abort_s) && elect_one()) {
+                const uint32_t full = bar(&m->q_full);
+                const int tiles = sg.u.narrow ? 1 : 2;
+                mbar_arrive_expect_tx(full, tiles * C::kHalves * tile_rows_bytes);
+                for (int s = 0; s < tiles; ++s)
+#pragma unroll
+                    for (int hf = 0; hf < C::kHalves; ++hf)
+                        tma_load_3d(sQ + s * C::kTileBytes + hf * C::kBlockBytes, &qmap, full, hf * 64, sg.h * p.G,
+                                    sg.start + sg.first_token + s * p.tile_tokens);
+            }
+            __syncwarp();
+            ++seg;
+            const int ahead = ahead_of(sg);
+            PageCursor kc, vc;
+            auto load_j = [&](PageCursor &c, const CUtensorMap *map, int j, bool values) {
+                const int t = sg.t0 + j;
+                int a, b;
+                c.get(p, sg, t, lane, a, b);
+                load(map, a, b, t * kKeyTile + kPage < sg.u.keys ? 2 : 1, values && has_own_keys(sg, t));
+            };
+            for (int j = 0; j < ahead; ++j) load_j(kc, &kmap, j, false);
+            for (int j = 0; j < sg.nt; ++j) {
+                load_j(vc, &vmap, j, true);
+                if (j + ahead < sg.nt) load_j(kc, &kmap, j + ahead, false);
+            }
+        }
+        // a CTA that gave up must not exit under its own copies: let the last ones land (bounded)
+        if (*abort_s) {
+            const uint64_t t0 = globaltimer_ns();
+            for (int i = max(0, r - C::kStages); i < r; ++i)
+                while (!mbar_try_wait(bar(&m->full[i % C::kStages]), (i / C::kStages) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+                }
+            if (seg > 0)
+                while (!mbar_try_wait(bar(&m->q_full), (seg - 1) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+                }
+        }
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------------ issuer of both products
+        constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kKeyTile, false, false);
+        constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, false, true);
+        const uint64_t descQ = smem_desc_sw128(sQ, 16, 1024), descK = smem_desc_sw128(sRing, 16, 1024);
+        const uint64_t descV = smem_desc_sw128(sRing, C::kBlockBytes, 1024);
+        int r0 = 0, seg = 0;
+        uint32_t p_parity = 0;   // one bit per slot
+        auto stage_of = [&](int r) { return r % C::kStages; };
+        auto wait_full = [&](int r) { wait(bar(&m->full[stage_of(r)]), (r / C::kStages) & 1, abort_s); };
+        auto issue_s = [&](int slot, int q_tile, int r, bool release) {
+            tc_fence_after();
+            __syncwarp();
+            if (elect_one()) {
+                const uint64_t qd = descQ + (uint64_t)((q_tile * C::kTileBytes) >> 4);
+                const uint64_t kd = descK + (uint64_t)((stage_of(r) * C::kTileBytes) >> 4);
+#pragma unroll
+                for (int hf = 0; hf < C::kHalves; ++hf)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_bf16_ss(tmem + kTmemS + slot * 128, qd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4),
+                                    kd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
+                mma_commit(bar(&m->s_full[slot]));
+                if (release) mma_commit(bar(&m->empty[stage_of(r)]));
+            }
+            __syncwarp();
+        };
+        auto issue_pv = [&](int slot, int r, int slices, bool first, bool release, bool last) {
+            tc_fence_after();
+            __syncwarp();
+            if (elect_one()) {
+                const uint64_t vd = descV + (uint64_t)((stage_of(r) * C::kTileBytes) >> 4);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    if (kk < slices)
+                        mma_bf16_ts(tmem + kTmemO + slot * D, tmem + kTmemS + slot * 128 + kk * 8, vd + (uint64_t)((kk * 2048) >> 4),
+                                    kIdescPV, !first || kk != 0);
+                if (release) mma_commit(bar(&m->empty[stage_of(r)]));
+                if (last) mma_commit(bar(&m->o_full[slot]));
+            }
+            __syncwarp();
+        };
+        auto commit_q = [&]() {
+            if (elect_one()) mma_commit(bar(&m->q_empty));
+            __syncwarp();
+        };
+        while (!*abort_s && walk.next(p, sg)) {
+            const int ahead = ahead_of(sg), n = sg.nt;
+            const bool narrow = sg.u.narrow;
+            auto wait_v = [&](int j) -> int {
+                const int r = r0 + place_of_v(j, ahead, n);
+                wait_full(r);
+                return r;
+            };
+            auto slices_of = [&](int j) { return (min(kKeyTile, sg.u.keys - (sg.t0 + j) * kKeyTile) + 15) >> 4; };
+            auto wait_p = [&](int slot) {
+                wait(bar(&m->p_full[slot]), (p_parity >> slot) & 1, abort_s);
+                p_parity ^= 1u << slot;
+            };
+            wait(bar(&m->q_full), seg & 1, abort_s);
+            ++seg;
+            if (narrow) {
+                for (int j = 0; j < ahead; ++j) {
+                    const int r = r0 + j;
+                    wait_full(r);
+                    issue_s(j, 0, r, true);
+                }
+                if (n <= 2) commit_q();
+                for (int j = 0; j < n; ++j) {
+                    const int slot = j & 1;
+                    wait_p(slot);
+                    const int rv = wait_v(j);
+                    issue_pv(slot, rv, slices_of(j), j < 2, true, j + 2 >= n);
+                    if (j + 2 < n) {
+                        const int rk = r0 + place_of_k(j + 2, ahead);
+                        wait_full(rk);
+                        issue_s(slot, 0, rk, true);
+                        if (j + 3 == n) commit_q();
+                    }
+                }
+            } else {
+                wait_full(r0);
+                issue_s(0, 0, r0, false);
+                issue_s(1, 1, r0, true);
+                if (n == 1) commit_q();
+                for (int j = 0; j < n; ++j) {
+                    int rv = 0, rk = 0;
+                    for (int slot = 0; slot < 2; ++slot) {
+                        wait_p(slot);
+                        if (slot == 0) rv = wait_v(j);
+                        issue_pv(slot, rv, slices_of(j), j == 0, slot == 1, j + 1 == n);
+                        if (j + 1 < n) {
+                            if (slot == 0) {
+                                rk = r0 + place_of_k(j + 1, ahead);
+                                wait_full(rk);
+                            }
+                            issue_s(slot, slot, rk, slot == 1);
+                        }
+                    }
+                    if (j + 2 == n) commit_q();
+                }
+            }
+            r0 += 2 * n;
+        }
+    } else if (warp == kValueWarp) {
+        // ------------------------------------------------------------------ values some queries do not see; the note on a split unit
+        int r0 = 0, seg = 0;
+        uint32_t raw_parity = 0;   // one bit per ring stage
+        if (lane == 0) p.pieces[blockIdx.x].b = -1;
+        __syncwarp();
+        while (!*abort_s && walk.next(p, sg)) {
+            const int ahead = ahead_of(sg), n = sg.nt, own_key = sg.L + sg.first_token;
+            if (!sg.full && sg.slot == 1 && lane == 0) {
+                const int s1 = sg.u.narrow ? (sg.t0 + sg.nt + 1) / 2 : sg.t0 + sg.nt;
+                const int unit_end = walk.w + (sg.u.steps - s1);   // the walk stands behind this segment's last entry
+                PieceDesc d;
+                d.b = sg.b; d.h = sg.h; d.block = sg.block;
+                d.more = prompt_range_owner(unit_end - 1, m->W, m->ctas) - (int)blockIdx.x;
+                d.first_token = sg.start; d.tokens = sg.n; d.L = sg.L;
+                p.pieces[blockIdx.x] = d;
+            }
+            if (lane == 0) *(volatile int32_t *)&m->poison[seg % kPoisonRing] = 0;
+            __syncwarp();
+            for (int j = max(0, own_key / kKeyTile - sg.t0); j < n; ++j) {
+                const int t = sg.t0 + j;
+                const int r = r0 + place_of_v(j, ahead, n), stage = r % C::kStages;
+                if (!wait(bar(&m->raw[stage]), (raw_parity >> stage) & 1, abort_s)) break;
+                raw_parity ^= 1u << stage;
+                const uint32_t tile = sRing + stage * C::kTileBytes;
+                const int valid = min(kKeyTile, sg.u.keys - t * kKeyTile), end = (valid + 15) & ~15;
+                constexpr int kChunks = D / 8;   // 16-byte pieces per row
+                bool found = false;
+                for (int i = max(0, own_key - t * kKeyTile) * kChunks + lane; i < end * kChunks; i += 32) {
+                    const int row = i / kChunks, c = i % kChunks;
+                    const uint32_t at = tile + (c >> 3) * C::kBlockBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                    uint32_t x[4] = {0, 0, 0, 0};
+                    bool store = row >= valid;
+                    if (!store) {
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (nonfinite_bits(x[e])) { x[e] &= 0xffff0000u; store = found = true; }
+                            if (nonfinite_bits(x[e] >> 16)) { x[e] &= 0x0000ffffu; store = found = true; }
+                        }
+                    }
+                    if (store) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                }
+                if (__any_sync(0xffffffffu, found) && lane == 0) *(volatile int32_t *)&m->poison[seg % kPoisonRing] = 1;
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&m->full[stage]));
+            }
+            r0 += 2 * n;
+            ++seg;
+        }
+    } else {
+        // ------------------------------------------------------------------ softmax / epilogue
+        const int slot = warp >> 2, row = tid & 127;
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + kTmemS + slot * 128 + lane_base, tO = tmem + kTmemO + slot * D + lane_base;
+        constexpr uint32_t kNegInf = 0xff800000u;
+        const int row_token = row / p.G, row_member = row - row_token * p.G;
+        int seg = 0, narrows = 0;
+        uint32_t s_parity = 0, o_parity = 0;
+        while (walk.next(p, sg)) {
+            const bool narrow = sg.u.narrow;
+            const int unit_token = (narrow ? 0 : slot * p.tile_tokens) + row_token;   // within the unit
+            const bool live = row_token < p.tile_tokens && unit_token < sg.u.tokens;
+            const bool warp_live = __any_sync(0xffffffffu, live);
+            // the last key this row sees; rows without a query see what the first row sees
+            const int last_key = sg.L + sg.first_token + (live ? unit_token : 0);
+            const int warp_min = __reduce_min_sync(0xffffffffu, last_key);
+            float mx = -INFINITY, l = 0.f;    // running maximum (scaled, log2 units) and row sum
+            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1;
+            bool any = false;
+            for (int j = j0; j < sg.nt; j += dj) {
+                const int key0 = (sg.t0 + j) * kKeyTile;
+                wait(bar(&m->s_full[slot]), s_parity, abort_s);
+                s_parity ^= 1;
+                tc_fence_after();
+                if (warp_live) {
+                    uint32_t pk[64];
+                    float sum = 0.f, top = -INFINITY;
+                    const bool masked = key0 + kKeyTile - 1 > warp_min;
+                    const int lim = last_key - key0;   // columns 0 .. lim are seen
+                    auto masked_load = [&](int c, uint32_t (&s)[32]) {
+                        tmem_ld32(tS + c * 32, s);
+                        tmem_wait_ld();
+                        if (masked) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (c * 32 + i > lim) s[i] = kNegInf;
+                        }
+                    };
+                    auto maxima = [&](const uint32_t (&s)[32]) {
+                        auto f = [&](int i) { return __uint_as_float(s[i]); };
+                        float a = max3(f(0), f(1), f(2)), b = max3(f(3), f(4), f(5));
+#pragma unroll
+                        for (int i = 6; i < 30; i += 4) {
+                            a = max3(a, f(i), f(i + 1));
+                            b = max3(b, f(i + 2), f(i + 3));
+                        }
+                        top = max3(top, max3(a, f(30), f(31)), b);
+                    };
+                    auto exponentials = [&]() {
+                        const float neg = mx == -INFINITY ? 0.f : -mx;
+                        const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), neg2 = make_float2(neg, neg);
+                        float2 part = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t s[32];
+                            masked_load(c, s);
+                            maxima(s);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc2, neg2);
+                                const float2 e = make_float2(ex2(x.x), ex2(x.y));
+                                part = __fadd2_rn(part, e);
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(e.x, e.y);
+                                pk[c * 16 + i] = *reinterpret_cast<const uint32_t *>(&hh);
+                            }
+                        }
+                        sum = part.x + part.y;
+                    };
+                    bool raise;
+                    if (!any) {
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t s[32];
+                            masked_load(c, s);
+                            maxima(s);
+                        }
+                        mx = top * p.scale_log2;   // (-inf where the row sees none of these keys)
+                        exponentials();
+                    } else {
+                        exponentials();
+                        raise = __any_sync(0xffffffffu, top * p.scale_log2 > mx + kRaiseMaxBy);
+                        if (raise) {
+                            const float up = fmaxf(mx, top * p.scale_log2);
+                            const float alpha = up == -INFINITY ? 1.f : ex2(mx - up);
+                            mx = up;
+                            l *= alpha;
+                            exponentials();
+                            // (the scores of this tile are complete, hence the value product before them is)
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(tO + c, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st32(tO + c, o);
+                            }
+                            tmem_wait_st();
+                        }
+                    }
+                    l += sum;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t half[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) half[i] = pk[c * 32 + i];
+                        tmem_st32(tS + c * 32, half);
+                    }
+                    tmem_wait_st();
+                }
+                any = true;
+                tc_fence_before();
+                mbar_arrive(bar(&m->p_full[slot]));
+            }
+            // ---- segment epilogue
+            if (any) {
+                wait(bar(&m->o_full[slot]), o_parity, abort_s);
+                o_parity ^= 1;
+                tc_fence_after();
+            }
+            float w0 = 1.f, w1 = 0.f, l_all = l, m_all = mx;
+            if (narrow) {
+                if (slot == 1) {
+                    m->ml[row] = make_float2(mx, any ? l : 0.f);
+                    tc_fence_before();
+                    mbar_arrive(bar(&m->merge_ready));
+                    wait(bar(&m->merge_free), narrows & 1, abort_s);
+                    ++narrows;
+                    ++seg;
+                    continue;
+                }
+                wait(bar(&m->merge_ready), narrows & 1, abort_s);
+                tc_fence_after();
+                const float2 other = m->ml[row];
+                m_all = fmaxf(mx, other.x);
+                w0 = mx == -INFINITY ? 0.f : ex2(mx - m_all);
+                w1 = other.x == -INFINITY ? 0.f : ex2(other.x - m_all);
+                l_all = l * w0 + other.y * w1;
+            }
+            const bool poisoned = *(volatile int32_t *)&m->poison[seg % kPoisonRing] != 0;
+            const bool two = narrow && sg.nt > 1;   // slot 1 has an output to add
+            if (warp_live) {
+                const int token = sg.first_token + unit_token;
+                const size_t out_row = ((size_t)(sg.start + (live ? token : 0)) * p.Hq + (size_t)sg.h * p.G + row_member) * D;
+                const float inv = 1.f / l_all;
+                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128 + row) * D;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(tO + c, o);
+                    tmem_wait_ld();
+                    if (two) {
+                        uint32_t o1[32];
+                        tmem_ld32(tO + D + c, o1);
+                        tmem_wait_ld();
+                        // a slot whose keys this row does not see has weight 0 and a finite output
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            o[i] = __float_as_uint(__uint_as_float(o[i]) * w0 + __uint_as_float(o1[i]) * w1);
+                    }
+                    if (poisoned && live) {
+                        // infinities and NaN among the values of the unit's own tokens, for the rows that see them
+                        const int lo = max(sg.L + sg.first_token, sg.t0 * kKeyTile), hi = min(last_key, (sg.t0 + sg.nt) * kKeyTile - 1);
+                        for (int key = lo; key <= hi; ++key) {
+                            const int page = p.page_table[(size_t)sg.b * p.max_pages + key / kPage];
+                            if (page < 0 || page >= p.num_pages) break;
+                            const __nv_bfloat16 *v = v_pool + (((size_t)page * p.Hkv + sg.h) * kPage + key % kPage) * D + c;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const float x = __bfloat162float(v[i]);
+                                if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+                            }
+                        }
+                    }
+                    if (live) {
+                        if (sg.full) {
+                            uint4 *dst = reinterpret_cast<uint4 *>(p.out + out_row + c);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t y[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
+                                    y[e] = *reinterpret_cast<const uint32_t *>(&hh);
+                                }
+                                dst[i] = make_uint4(y[0], y[1], y[2], y[3]);
+                            }
+                        } else {
+                            uint4 *dst = reinterpret_cast<uint4 *>(part_o + c);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                }
+                if (live) {
+                    if (!sg.full)
+                        *reinterpret_cast<float2 *>(p.partial_ml + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128 + row) * 2) = make_float2(m_all, l_all);
+                    else if (p.lse)
+                        p.lse[out_row / D] = (m_all + log2f(l_all)) * 0.6931471805599453f;
+                }
+            }
+            if (narrow) {
+                // slot 1's output has been read: its next product may overwrite it
+                tc_fence_before();
+                mbar_arrive(bar(&m->merge_free));
+                ++narrows;
+            }
+            ++seg;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+    if (tid == 0) p.gave_up[blockIdx.x] = *abort_s;
+}
+
+// After the attention kernel: block c < n_ctas merges the unit that CTA c began and others finished; block
+// n_ctas + b reports sequence b, zeroes its rows if it is rejected and advances its length.
+// A sequence's pages are checked here and not before the attention: an id outside the pool makes a tile load read
+// the fill value, never a fault, and the rows computed with it are zeroed here.
+constexpr int kFinishThreads = 256;
+
+__device__ __forceinline__ bool pages_bad(const PromptAttnParams &p, int b, int keys) {
+    bool bad = false;
+    for (int i = threadIdx.x; i < (keys + kPage - 1) / kPage; i += kFinishThreads) {
+        const int pg = p.page_table[(size_t)b * p.max_pages + i];
+        bad |= pg < 0 || pg >= p.num_pages;
+    }
+    return __syncthreads_or(bad);
+}
+
+__global__ void __launch_bounds__(kFinishThreads) prompt_finish_kernel(const PromptAttnParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tid = threadIdx.x, D = p.D;
+    if ((int)blockIdx.x < p.n_ctas) {
+        const int c = blockIdx.x;
+        const PieceDesc d = p.pieces[c];
+        if (d.b < 0) return;
+        if (pages_bad(p, d.b, d.L + d.tokens)) return;
+        const UnitShape u = unit_shape(d.L, d.tokens, d.block, p.tile_tokens);
+        const int tile_rows = p.tile_tokens * p.G, lanes = D / 4;   // threads per row, four columns each
+        const int rows = u.tokens * p.G;
+        for (int i = tid / lanes; i < rows; i += kFinishThreads / lanes) {
+            const int x = tid % lanes;
+            const int prow = i < tile_rows ? i : 128 + i - tile_rows;   // its row of a piece
+            auto piece = [&](int k) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)) * 256 + prow; };
+            float mx = -INFINITY;
+            for (int k = 0; k <= d.more; ++k) mx = fmaxf(mx, p.partial_ml[piece(k) * 2]);
+            float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k <= d.more; ++k) {
+                const float2 ml = *reinterpret_cast<const float2 *>(p.partial_ml + piece(k) * 2);
+                if (ml.x == -INFINITY) continue;   // this row sees none of the piece's keys
+                const float w = exp2f(ml.x - mx);
+                const float4 y = reinterpret_cast<const float4 *>(p.partial_o + piece(k) * D)[x];
+                l += w * ml.y;
+                o[0] += w * y.x; o[1] += w * y.y; o[2] += w * y.z; o[3] += w * y.w;
+            }
+            const float inv = 1.f / l;
+            const int token = d.block * 2 * p.tile_tokens + i / p.G;
+            const size_t row = (size_t)(d.first_token + token) * p.Hq + (size_t)d.h * p.G + i % p.G;
+            const __nv_bfloat162 a = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), b = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
+            reinterpret_cast<uint2 *>(p.out + row * D)[x] = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+            if (p.lse && x == 0) p.lse[row] = (mx + log2f(l)) * 0.6931471805599453f;
+        }
+        return;
+    }
+    const int b = blockIdx.x - p.n_ctas;
+    bool bad = false, late = false;
+    for (int i = tid; i < p.B; i += kFinishThreads) {
+        const int a = p.token_start[i], e = p.token_start[i + 1];
+        bad |= a < 0 || a > e || e > p.tokens;
+    }
+    for (int i = tid; i < p.n_ctas; i += kFinishThreads) late |= p.gave_up[i] != 0;
+    if (__syncthreads_or(bad)) {
+        if (tid == 0) p.status[b] = READER_ERR_INVALID_ARG;
+        return;   // whose rows are whose is not known: nothing was written
+    }
+    const int start = p.token_start[b], n = p.token_start[b + 1] - start, L = p.seq_lens[b];
+    int st = READER_OK;
+    if (!prompt_len_ok(L, n, p.max_pages)) st = READER_ERR_CAPACITY;
+    else if (n > 0 && pages_bad(p, b, L + n)) st = READER_ERR_BAD_PAGE;
+    if (__syncthreads_or(late) && st == READER_OK) st = READER_ERR_TIMEOUT;
+    if (tid == 0) {
+        p.status[b] = st;
+        if (p.bump && st == READER_OK) p.bump[b] = L + n;
+    }
+    if (st == READER_OK) return;
+    uint4 *rows = reinterpret_cast<uint4 *>(p.out + (size_t)start * p.Hq * D);
+    for (size_t i = tid; i < (size_t)n * p.Hq * D / 8; i += kFinishThreads) rows[i] = make_uint4(0, 0, 0, 0);
+    if (p.lse)
+        for (size_t i = tid; i < (size_t)n * p.Hq; i += kFinishThreads) p.lse[(size_t)start * p.Hq + i] = 0.f;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode(void *fn, CUtensorMap *map, const void *at, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
+    const cuuint32_t one[3] = {1, 1, 1};
+    return reinterpret_cast<EncodeTiledFn>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(at), dims, strides, box, one,
+                                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+// TMA descriptors of the tensors seen last: pools by layer (round robin), the queries of the last call.
+constexpr int kPoolEntries = 128;
+struct PromptMaps {
+    struct Pool {
+        const void *k = nullptr, *v = nullptr;
+        int64_t rows = -1;
+        int D = 0;
+        alignas(64) CUtensorMap kmap, vmap;
+    } pools[kPoolEntries];
+    int next = 0;
+    const void *q = nullptr;
+    int64_t tokens = -1;
+    int Hq = 0, G = 0, D = 0;
+    alignas(64) CUtensorMap qmap;
+};
+
+bool prompt_host_init(PromptHost *h) {
+    h->attr_set = false;
+    h->maps = new (std::nothrow) PromptMaps();
+    return h->maps != nullptr;
+}
+void prompt_host_destroy(PromptHost *h) {
+    delete h->maps;
+    h->maps = nullptr;
+}
+
+reader_status launch_prompt_attn(PromptHost *h, void *fn, const PromptAttnParams &p, const __nv_bfloat16 *q, const void *k_pool,
+                                 const void *v_pool, cudaStream_t st) {
+    if (!h->attr_set) {
+        if (cudaFuncSetAttribute(prompt_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes) != cudaSuccess ||
+            cudaFuncSetAttribute(prompt_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes) != cudaSuccess) {
+            cudaGetLastError();
+            return READER_ERR_CUDA;
+        }
+        h->attr_set = true;
+    }
+    PromptMaps *m = h->maps;
+    const int64_t rows = (int64_t)p.num_pages * p.Hkv * kPage;
+    PromptMaps::Pool *pool = nullptr;
+    for (int i = 0; i < kPoolEntries && !pool; ++i) {
+        PromptMaps::Pool &e = m->pools[i];
+        if (e.k == k_pool && e.v == v_pool && e.rows == rows && e.D == p.D) pool = &e;
+    }
+    if (!pool) {
+        pool = &m->pools[m->next];
+        m->next = (m->next + 1) % kPoolEntries;
+        pool->rows = -1;
+        const cuuint64_t dims[2] = {(cuuint64_t)p.D, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)p.D * 2};
+        const cuuint32_t box[2] = {64, (cuuint32_t)kPage};
+        if (!encode(fn, &pool->kmap, k_pool, 2, dims, strides, box) || !encode(fn, &pool->vmap, v_pool, 2, dims, strides, box)) return READER_ERR_CUDA;
+        pool->k = k_pool; pool->v = v_pool; pool->rows = rows; pool->D = p.D;
+    }
+    if (m->q != q || m->tokens != p.tokens || m->Hq != p.Hq || m->G != p.G || m->D != p.D) {
+        // 64 columns x the G heads of a group x as many tokens as fill 128 rows
+        const cuuint64_t dims[3] = {(cuuint64_t)p.D, (cuuint64_t)p.Hq, (cuuint64_t)p.tokens};
+        const cuuint64_t strides[2] = {(cuuint64_t)p.D * 2, (cuuint64_t)p.Hq * p.D * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens};
+        m->tokens = -1;
+        if (!encode(fn, &m->qmap, q, 3, dims, strides, box)) return READER_ERR_CUDA;
+        m->q = q; m->tokens = p.tokens; m->Hq = p.Hq; m->G = p.G; m->D = p.D;
+    }
+    const bool wide = p.D == 128;
+    const cudaError_t e = launch_pdl(wide ? prompt_attn_kernel<128> : prompt_attn_kernel<64>, dim3((unsigned)p.n_ctas), dim3(kThreads),
+                                     wide ? Cfg<128>::kSmemBytes : Cfg<64>::kSmemBytes, st, p, m->qmap, pool->kmap, pool->vmap,
+                                     static_cast<const __nv_bfloat16 *>(v_pool));
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return READER_ERR_CUDA;
+    }
+    return READER_OK;
+}
+
+void launch_prompt_finish(const PromptAttnParams &p, cudaStream_t st) {
+    launch_pdl(prompt_finish_kernel, dim3((unsigned)(p.n_ctas + p.B)), dim3(kFinishThreads), 0, st, p);
+}
+
+}  // namespace reader
