@@ -699,7 +699,7 @@ reader_status reader_prompt_append(reader_ctx *ctx, const void *q, const void *k
     p.v_out = static_cast<__nv_bfloat16 *>(cache->v_pool);
     p.status = status_out;
     if (reader_status st = check_device(ctx)) return st;
-    launch_prompt_append(p, (cudaStream_t)stream);
+    launch_prompt_append(p, ctx->n_sm, (cudaStream_t)stream);
     return launch_status();
 }
 
@@ -724,7 +724,7 @@ reader_status reader_tree_rotate(reader_ctx *ctx, const void *q, const void *k, 
     p.v_out = static_cast<__nv_bfloat16 *>(v_tree_out);
     p.status = status_out;
     if (reader_status st = check_device(ctx)) return st;
-    launch_tree_rotate(p, (cudaStream_t)stream);
+    launch_tree_rotate(p, ctx->n_sm, (cudaStream_t)stream);
     return launch_status();
 }
 

@@ -740,11 +740,17 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
     if (tid == 0) p.gave_up[blockIdx.x] = *abort_s;
 }
 
-// After the attention kernel: block c < n_ctas merges the unit that CTA c began and others finished; block
-// n_ctas + b reports sequence b, zeroes its rows if it is rejected and advances its length.
-// A sequence's pages are checked here and not before the attention: an id outside the pool makes a tile load read
-// the fill value, never a fault, and the rows computed with it are zeroed here.
+// After the attention kernel: blocks kMergeBlocks * c .. of the first n_ctas * kMergeBlocks merge the unit that CTA c
+// began and others finished; the block of sequence b behind them reports it, zeroes its rows if it is rejected and
+// advances its length.  A sequence's pages are checked here and not before the attention: an id outside the pool makes
+// a tile load read the fill value, never a fault, and the rows computed with it are zeroed here.
+//
+// A merge is latency: a few kilobytes a row, spread over as many blocks and loads in flight as there are (with one block
+// to a unit it took 30 us of a 52 us call).  A unit of few pieces has many rows: a warp takes a row (two at head_dim
+// 64) and goes through the pieces; a unit of many pieces (few rows over a long history) gives a row's pieces to the
+// eight warps of a block, which join their shares in shared memory.
 constexpr int kFinishThreads = 256;
+constexpr int kMergeBlocks = 8;
 
 __device__ __forceinline__ bool pages_bad(const PromptAttnParams &p, int b, int keys) {
     bool bad = false;
@@ -755,43 +761,119 @@ __device__ __forceinline__ bool pages_bad(const PromptAttnParams &p, int b, int 
     return __syncthreads_or(bad);
 }
 
-__global__ void __launch_bounds__(kFinishThreads) prompt_finish_kernel(const PromptAttnParams p) {
-    pdl_wait();
-    pdl_launch_dependents();
-    const int tid = threadIdx.x, D = p.D;
-    if ((int)blockIdx.x < p.n_ctas) {
-        const int c = blockIdx.x;
-        const PieceDesc d = p.pieces[c];
-        if (d.b < 0) return;
-        if (pages_bad(p, d.b, d.L + d.tokens)) return;
-        const UnitShape u = unit_shape(d.L, d.tokens, d.block, p.tile_tokens);
-        const int tile_rows = p.tile_tokens * p.G, lanes = D / 4;   // threads per row, four columns each
-        const int rows = u.tokens * p.G;
-        for (int i = tid / lanes; i < rows; i += kFinishThreads / lanes) {
-            const int x = tid % lanes;
-            const int prow = i < tile_rows ? i : 128 + i - tile_rows;   // its row of a piece
-            auto piece = [&](int k) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)) * 256 + prow; };
-            float mx = -INFINITY;
-            for (int k = 0; k <= d.more; ++k) mx = fmaxf(mx, p.partial_ml[piece(k) * 2]);
-            float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+// Running softmax state of four columns of a row.
+struct Merged {
+    float mx, l, o[4];
+    __device__ __forceinline__ void clear() {
+        mx = -INFINITY;
+        l = o[0] = o[1] = o[2] = o[3] = 0.f;
+    }
+    __device__ __forceinline__ void add(float m2, float l2, const float4 &y) {
+        if (m2 == -INFINITY) return;   // the row sees none of these keys
+        const float up = fmaxf(mx, m2), w = mx == -INFINITY ? 0.f : exp2f(mx - up), w2 = exp2f(m2 - up);
+        mx = up;
+        l = l * w + l2 * w2;
+        o[0] = o[0] * w + y.x * w2; o[1] = o[1] * w + y.y * w2; o[2] = o[2] * w + y.z * w2; o[3] = o[3] * w + y.w * w2;
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void merge_unit(const PromptAttnParams &p, const PieceDesc &d, int c, int chunk) {
+    constexpr int kLanes = D / 4, kRows = kFinishThreads / kLanes, kUnroll = 4;   // four columns a thread; rows at a time
+    __shared__ float s_ml[8][2], s_o[8][D];
+    const int tid = threadIdx.x;
+    const UnitShape u = unit_shape(d.L, d.tokens, d.block, p.tile_tokens);
+    const int tile_rows = p.tile_tokens * p.G, rows = u.tokens * p.G;
+    auto place = [&](int k, int i) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)) * 256 + (i < tile_rows ? i : 128 + i - tile_rows); };
+    auto write = [&](int i, int x, const Merged &m) {
+        const float inv = 1.f / m.l;
+        const int token = d.block * 2 * p.tile_tokens + i / p.G;
+        const size_t row = (size_t)(d.first_token + token) * p.Hq + (size_t)d.h * p.G + i % p.G;
+        const __nv_bfloat162 a = __floats2bfloat162_rn(m.o[0] * inv, m.o[1] * inv), b = __floats2bfloat162_rn(m.o[2] * inv, m.o[3] * inv);
+        reinterpret_cast<uint2 *>(p.out + row * D)[x] = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+        if (p.lse && x == 0) p.lse[row] = (m.mx + log2f(m.l)) * 0.6931471805599453f;
+    };
+    if (d.more < 8) {
+        const int x = tid % kLanes;
+        for (int i0 = chunk + kMergeBlocks * (tid / kLanes); i0 < rows; i0 += kMergeBlocks * kRows * kUnroll) {
+            Merged m[kUnroll];
+#pragma unroll
+            for (int r = 0; r < kUnroll; ++r) m[r].clear();
             for (int k = 0; k <= d.more; ++k) {
-                const float2 ml = *reinterpret_cast<const float2 *>(p.partial_ml + piece(k) * 2);
-                if (ml.x == -INFINITY) continue;   // this row sees none of the piece's keys
-                const float w = exp2f(ml.x - mx);
-                const float4 y = reinterpret_cast<const float4 *>(p.partial_o + piece(k) * D)[x];
-                l += w * ml.y;
-                o[0] += w * y.x; o[1] += w * y.y; o[2] += w * y.z; o[3] += w * y.w;
+                float2 ml[kUnroll];
+                float4 y[kUnroll];
+#pragma unroll
+                for (int r = 0; r < kUnroll; ++r) {
+                    const int i = i0 + r * kMergeBlocks * kRows;
+                    ml[r] = make_float2(-INFINITY, 0.f);
+                    y[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (i < rows) {
+                        ml[r] = *reinterpret_cast<const float2 *>(p.partial_ml + place(k, i) * 2);
+                        y[r] = reinterpret_cast<const float4 *>(p.partial_o + place(k, i) * D)[x];
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < kUnroll; ++r) m[r].add(ml[r].x, ml[r].y, y[r]);
             }
-            const float inv = 1.f / l;
-            const int token = d.block * 2 * p.tile_tokens + i / p.G;
-            const size_t row = (size_t)(d.first_token + token) * p.Hq + (size_t)d.h * p.G + i % p.G;
-            const __nv_bfloat162 a = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), b = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
-            reinterpret_cast<uint2 *>(p.out + row * D)[x] = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
-            if (p.lse && x == 0) p.lse[row] = (mx + log2f(l)) * 0.6931471805599453f;
+#pragma unroll
+            for (int r = 0; r < kUnroll; ++r)
+                if (i0 + r * kMergeBlocks * kRows < rows) write(i0 + r * kMergeBlocks * kRows, x, m[r]);
         }
         return;
     }
-    const int b = blockIdx.x - p.n_ctas;
+    const int warp = tid >> 5, lane = tid & 31, x = lane % kLanes;
+    for (int i = chunk; i < rows; i += kMergeBlocks) {
+        Merged m;
+        m.clear();
+        for (int k0 = warp; k0 <= d.more; k0 += 8 * kUnroll) {
+            float2 ml[kUnroll];
+            float4 y[kUnroll];
+#pragma unroll
+            for (int r = 0; r < kUnroll; ++r) {
+                ml[r] = make_float2(-INFINITY, 0.f);
+                y[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k0 + 8 * r <= d.more) {
+                    ml[r] = *reinterpret_cast<const float2 *>(p.partial_ml + place(k0 + 8 * r, i) * 2);
+                    y[r] = reinterpret_cast<const float4 *>(p.partial_o + place(k0 + 8 * r, i) * D)[x];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < kUnroll; ++r) m.add(ml[r].x, ml[r].y, y[r]);
+        }
+        if (lane < kLanes) {
+            if (lane == 0) {
+                s_ml[warp][0] = m.mx;
+                s_ml[warp][1] = m.l;
+            }
+            *reinterpret_cast<float4 *>(&s_o[warp][4 * x]) = make_float4(m.o[0], m.o[1], m.o[2], m.o[3]);
+        }
+        __syncthreads();
+        if (warp == 0 && lane < kLanes) {
+            Merged all;
+            all.clear();
+#pragma unroll
+            for (int w = 0; w < 8; ++w) all.add(s_ml[w][0], s_ml[w][1], *reinterpret_cast<const float4 *>(&s_o[w][4 * x]));
+            write(i, x, all);
+        }
+        __syncthreads();
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kFinishThreads) prompt_finish_kernel(const PromptAttnParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x < p.n_ctas * kMergeBlocks) {
+        const int c = blockIdx.x / kMergeBlocks;
+        const PieceDesc d = p.pieces[c];
+        if (d.b < 0) return;
+        bool late = false;   // (a rejected sequence's rows are zeroed below: nobody else may write them)
+        for (int i = tid; i < p.n_ctas; i += kFinishThreads) late |= p.gave_up[i] != 0;
+        if (!__syncthreads_or(late) && !pages_bad(p, d.b, d.L + d.tokens)) merge_unit<D>(p, d, c, blockIdx.x % kMergeBlocks);
+        return;
+    }
+    const int b = blockIdx.x - p.n_ctas * kMergeBlocks;
     bool bad = false, late = false;
     for (int i = tid; i < p.B; i += kFinishThreads) {
         const int a = p.token_start[i], e = p.token_start[i + 1];
@@ -904,7 +986,7 @@ reader_status launch_prompt_attn(PromptHost *h, void *fn, const PromptAttnParams
 }
 
 void launch_prompt_finish(const PromptAttnParams &p, cudaStream_t st) {
-    launch_pdl(prompt_finish_kernel, dim3((unsigned)(p.n_ctas + p.B)), dim3(kFinishThreads), 0, st, p);
+    launch_pdl(p.D == 128 ? prompt_finish_kernel<128> : prompt_finish_kernel<64>, dim3((unsigned)(p.n_ctas * kMergeBlocks + p.B)), dim3(kFinishThreads), 0, st, p);
 }
 
 }  // namespace reader

@@ -6,11 +6,12 @@
 // are (j, j + R/2) of the first R = rot_dim elements, or (2j, 2j + 1) when interleaved.
 //
 // Bound: bytes.  A head row is read once and written once, 2 (Hq + 2 Hkv) D bf16 per token; all arithmetic is fp32
-// on values that stay in registers, with one rounding to bf16 at the very end.  One block per token: a thread holds
-// eight consecutive elements (one 16-byte access) of one head, D/8 neighbouring threads hold a head, so the mean
-// square is a few shuffles, the half-split partner is one shuffle away and the table row is read once per thread
-// for all of its heads.  The loads of the head rows are issued before the block finds out which sequence its token
-// belongs to and where it goes.
+// on values that stay in registers, with one rounding to bf16 at the very end.  D/8 neighbouring threads hold a head,
+// each of them the four elements of a first half and the four partners they are rotated with (two 8-byte accesses),
+// so the rotation needs no exchange and the mean square a few shuffles.  A warp walks the heads of one token by
+// itself (or a share of them, when there are too few tokens to fill the GPU), with several accesses under way and the
+// token's table row in registers; its rows are asked for (an L2 prefetch) before it finds out
+// which sequence the token belongs to and where it goes.
 #include "common.cuh"
 #include "rotate.cuh"
 
@@ -18,282 +19,300 @@ namespace reader {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kInFlight = 4;   // head rows a thread loads before it works on the first
+constexpr int kInFlight = 4;   // head rows a thread has under way (two accesses each)
 
-struct Row8 {
-    float x[8];
+__device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t pack(float2 x) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+struct Raw {
+    uint2 a, b;   // four elements each
 };
 
-__device__ __forceinline__ Row8 unpack(const uint4 &raw) {
-    Row8 r;
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.x[2 * i] = __uint_as_float(w[i] << 16);
-        r.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-    return r;
-}
-__device__ __forceinline__ uint4 pack(const Row8 &r) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(r.x[2 * i], r.x[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t *>(&h);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// The token-independent part of a thread's work: its eight elements' weights and their table entries.
+// The token-independent part of a thread's work (which elements it has), and its table entries.
 template <int D>
 struct Turner {
     static constexpr int kLanes = D / 8;   // threads per head
-    int l;                // this thread's place in its head
-    int src_lane;         // half-split: the lane of the partner elements
-    int mode;             // 0: elements pass unrotated, 1: first half of a half-split pair, 2: second half, 3: interleaved
-    float c[8], s[8];
-    uint4 wq, wk;
+    int ea, eb;            // where its two groups of four elements begin
+    int at;                // its four pairs' index in the table; -1: its elements are not rotated
+    uint32_t lo, hi;       // byte selectors that bring the first / second elements of its pairs together
+    float2 c[2], s[2];
 
     __device__ __forceinline__ void init(const RotateParams &p, int lane) {
-        l = lane % kLanes;
-        src_lane = lane;
-        mode = 0;
-        if (p.q_weight) {
-            wq = reinterpret_cast<const uint4 *>(p.q_weight)[l];
-            wk = reinterpret_cast<const uint4 *>(p.k_weight)[l];
-        }
-        if (p.rope && l * 8 < p.rot) {
-            const int half8 = p.rot / 16;   // threads per half
-            if (p.interleaved) {
-                mode = 3;
-            } else {
-                mode = l < half8 ? 1 : 2;
-                src_lane = mode == 1 ? lane + half8 : lane - half8;
-            }
-        }
+        const int l = lane % kLanes, quads = p.rope ? p.rot / 8 : 0;   // threads with rotated elements
+        const bool turned = l < quads, halves = turned && !p.interleaved;
+        at = turned ? 4 * l : -1;
+        ea = halves ? 4 * l : 8 * l;       // (behind the rotated threads the rest of the head, 8 elements each)
+        eb = halves ? ea + p.rot / 2 : ea + 4;
+        // half-split: word i of a and word i of b are two pairs as they stand.  Interleaved: (a0 a1), (b0 b1) are the
+        // pairs, so the even elements (a0 b0) go into one word and the odd ones (a1 b1) into the other.
+        lo = p.interleaved ? 0x5410u : 0x3210u;
+        hi = p.interleaved ? 0x7632u : 0x7654u;
+    }
+    __device__ __forceinline__ Raw load(const __nv_bfloat16 *head) const {
+        return Raw{*reinterpret_cast<const uint2 *>(head + ea), *reinterpret_cast<const uint2 *>(head + eb)};
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *head, const Raw &r) const {
+        *reinterpret_cast<uint2 *>(head + ea) = r.a;
+        *reinterpret_cast<uint2 *>(head + eb) = r.b;
+    }
+    // first elements of the pairs to .a, second ones to .b (its own inverse)
+    __device__ __forceinline__ Raw paired(const Raw &r) const {
+        return Raw{make_uint2(__byte_perm(r.a.x, r.b.x, lo), __byte_perm(r.a.y, r.b.y, lo)),
+                   make_uint2(__byte_perm(r.a.x, r.b.x, hi), __byte_perm(r.a.y, r.b.y, hi))};
     }
     __device__ __forceinline__ void load_table(const RotateParams &p, int64_t pos) {
-        if (mode == 0) return;
-        const int half = p.rot / 2;
-        const float *row = p.rope + pos * p.rot;
-        if (mode == 3) {
-            const float4 a = *reinterpret_cast<const float4 *>(row + 4 * l), b = *reinterpret_cast<const float4 *>(row + half + 4 * l);
-            c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
-            s[0] = b.x; s[1] = b.y; s[2] = b.z; s[3] = b.w;
-        } else {
-            const int at = 8 * l - (mode == 2 ? half : 0);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float4 a = *reinterpret_cast<const float4 *>(row + at + 4 * i), b = *reinterpret_cast<const float4 *>(row + half + at + 4 * i);
-                c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
-                s[4 * i] = b.x; s[4 * i + 1] = b.y; s[4 * i + 2] = b.z; s[4 * i + 3] = b.w;
-            }
-        }
+        if (at < 0) return;
+        const float *row = p.rope + pos * p.rot + at;
+        const float4 x = *reinterpret_cast<const float4 *>(row), y = *reinterpret_cast<const float4 *>(row + p.rot / 2);
+        // pairs 0 .. 3 in the order of the words: (0 1), (2 3), or (0 2), (1 3) when interleaved
+        c[0] = make_float2(x.x, p.interleaved ? x.z : x.y); c[1] = make_float2(p.interleaved ? x.y : x.z, x.w);
+        s[0] = make_float2(y.x, p.interleaved ? y.z : y.y); s[1] = make_float2(p.interleaved ? y.y : y.z, y.w);
     }
-    // Warp-collective (all heads of a warp at once).
-    __device__ __forceinline__ uint4 turn(const RotateParams &p, const uint4 &raw, bool key) const {
-        Row8 r = unpack(raw);
+    // Warp-collective (all heads of a warp at once); w: the weights of its elements, paired.
+    __device__ __forceinline__ Raw turn(const RotateParams &p, const Raw &raw, const float2 (&w)[4]) const {
+        const Raw r = paired(raw);
+        float2 x[4] = {unpack(r.a.x), unpack(r.a.y), unpack(r.b.x), unpack(r.b.y)};
         if (p.q_weight) {
-            float ss = 0.f;
+            float2 sq = __fmul2_rn(x[0], x[0]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(r.x[i], r.x[i], ss);
+            for (int i = 1; i < 4; ++i) sq = __ffma2_rn(x[i], x[i], sq);
+            float ss = sq.x + sq.y;
 #pragma unroll
             for (int d = kLanes / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
             const float f = rsqrtf(ss * (1.f / D) + p.eps);
-            const Row8 w = unpack(key ? wk : wq);
+            const float2 f2 = make_float2(f, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r.x[i] = r.x[i] * f * w.x[i];
+            for (int i = 0; i < 4; ++i) x[i] = __fmul2_rn(__fmul2_rn(x[i], f2), w[i]);
         }
-        if (p.rope) {
-            if (p.interleaved) {
-                if (mode == 3) {
+        if (at >= 0) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = r.x[2 * i], b = r.x[2 * i + 1];
-                        r.x[2 * i] = a * c[i] - b * s[i];
-                        r.x[2 * i + 1] = b * c[i] + a * s[i];
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float o = __shfl_sync(0xffffffffu, r.x[i], src_lane);
-                    if (mode == 1) r.x[i] = r.x[i] * c[i] - o * s[i];
-                    else if (mode == 2) r.x[i] = r.x[i] * c[i] + o * s[i];
-                }
+            for (int i = 0; i < 2; ++i) {
+                const float2 a = x[i], b = x[i + 2], minus = make_float2(-s[i].x, -s[i].y);
+                x[i] = __ffma2_rn(b, minus, __fmul2_rn(a, c[i]));
+                x[i + 2] = __ffma2_rn(a, s[i], __fmul2_rn(b, c[i]));
             }
         }
-        return pack(r);
+        return paired(Raw{make_uint2(pack(x[0]), pack(x[1])), make_uint2(pack(x[2]), pack(x[3]))});
     }
 };
 
-// All head rows of one token: `row` is its row of the projection's output.  place(x, l) gives where piece l of
-// output head x goes (queries first, then keys, then values); `known()` runs once, after the first loads are in
-// flight, and says whether the token is written (1), zeroed (0) or left alone (-1).
-template <int D, typename Known, typename Place>
-__device__ __forceinline__ void token_heads(const RotateParams &p, int64_t row, Turner<D> &t, const Known &known, const Place &place) {
-    constexpr int kLanes = D / 8, kPass = kThreads / kLanes;
-    const int heads = p.Hq + 2 * p.Hkv, slot = threadIdx.x / kLanes;
-    const __nv_bfloat16 *q = p.q + row * p.q_stride, *k = p.k + row * p.k_stride, *v = p.v + row * p.v_stride;
-    int what = 1;
-    for (int x0 = 0; x0 < heads; x0 += kPass * kInFlight) {
-        uint4 raw[kInFlight];
+// One kind of a token's heads (queries, keys or values): from `src` to `dst`, where heads are `dst_stride` elements apart.
+// A warp handles 32 / kLanes heads at once and takes every `share`-th such group, from group `first`; kInFlight of
+// them are loaded before the first is worked on.
+template <int D, bool kTurn>
+__device__ __forceinline__ void walk_heads(const RotateParams &p, const Turner<D> &t, const __nv_bfloat16 *src, __nv_bfloat16 *dst, int heads,
+                                           int dst_stride, int first, const __nv_bfloat16 *weight) {
+    constexpr int kGroup = 32 / Turner<D>::kLanes;
+    const int sub = (threadIdx.x & 31) / Turner<D>::kLanes, step = kGroup * p.share;
+    float2 w[4];
+    if (kTurn && p.q_weight) {
+        const Raw r = t.paired(t.load(weight));
+        w[0] = unpack(r.a.x); w[1] = unpack(r.a.y); w[2] = unpack(r.b.x); w[3] = unpack(r.b.y);
+    }
+    for (int x0 = first * kGroup; x0 < heads; x0 += step * kInFlight) {
+        Raw raw[kInFlight];
+#pragma unroll
+        for (int i = 0; i < kInFlight; ++i)
+            if (x0 + sub + i * step < heads) raw[i] = t.load(src + (x0 + sub + i * step) * D);
 #pragma unroll
         for (int i = 0; i < kInFlight; ++i) {
-            const int x = x0 + i * kPass + slot;
-            raw[i] = make_uint4(0, 0, 0, 0);
-            if (x < heads) {
-                const __nv_bfloat16 *src = x < p.Hq ? q + (size_t)x * D : x < p.Hq + p.Hkv ? k + (size_t)(x - p.Hq) * D : v + (size_t)(x - p.Hq - p.Hkv) * D;
-                raw[i] = reinterpret_cast<const uint4 *>(src)[t.l];
-            }
-        }
-        if (x0 == 0) {
-            what = known();
-            if (what < 0) return;
-        }
-#pragma unroll
-        for (int i = 0; i < kInFlight; ++i) {
-            if (x0 + i * kPass >= heads) break;   // (the same for the whole block)
-            const int x = x0 + i * kPass + slot;
-            const uint4 turned = t.turn(p, raw[i], x >= p.Hq);
-            uint4 y = x < p.Hq + p.Hkv ? turned : raw[i];
-            if (what == 0) y = make_uint4(0, 0, 0, 0);
-            if (x < heads)
-                if (uint4 *dst = place(x)) dst[t.l] = y;
+            const Raw y = kTurn ? t.turn(p, raw[i], w) : raw[i];
+            if (x0 + sub + i * step < heads) t.store(dst + (size_t)(x0 + sub + i * step) * dst_stride, y);
         }
     }
 }
 
-// What is wrong with sequence b of a prompt whose pair (first, last) of token_start is in order; block-wide.
-__device__ __forceinline__ int append_status(const RotateParams &p, int b, int n) {
-    const int L = p.seq_lens[b];
+// A token's heads as this warp has them: every p.share-th group of all heads, queries first, then keys, then values.
+template <int D>
+struct Token {
+    static constexpr int kGroup = 32 / Turner<D>::kLanes;
+    const __nv_bfloat16 *q, *k, *v;
+    int q_first, k_first, v_first;   // this warp's first group of each kind
+
+    __device__ __forceinline__ void init(const RotateParams &p, int64_t row, int first) {
+        q = p.q + row * p.q_stride;
+        k = p.k + row * p.k_stride;
+        v = p.v + row * p.v_stride;
+        const int q_groups = (p.Hq + kGroup - 1) / kGroup, kv_groups = (p.Hkv + kGroup - 1) / kGroup, mask = p.share - 1;
+        q_first = first;
+        k_first = (first - q_groups) & mask;
+        v_first = (first - q_groups - kv_groups) & mask;
+    }
+    // Asks for the warp's rows (its first ones, if it has but a share of them), so that they are under way while it finds
+    // out where they go.
+    __device__ __forceinline__ void prefetch(const RotateParams &p, const Turner<D> &t, int lane) const {
+        auto ask = [&](const __nv_bfloat16 *at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); };
+        if (p.share == 1) {
+            for (int i = lane * 64; i < p.Hq * D; i += 32 * 64) ask(q + i);
+            for (int i = lane * 64; i < p.Hkv * D; i += 32 * 64) {
+                ask(k + i);
+                ask(v + i);
+            }
+            return;
+        }
+        const int sub = lane / Turner<D>::kLanes;
+        auto ask_head = [&](const __nv_bfloat16 *head) {
+            ask(head + t.ea);
+            if (t.eb - t.ea >= 64) ask(head + t.eb);
+        };
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int x = (q_first + i * p.share) * kGroup + sub;
+            if (x < p.Hq) ask_head(q + x * D);
+        }
+        if (k_first * kGroup + sub < p.Hkv) ask_head(k + (k_first * kGroup + sub) * D);
+        if (v_first * kGroup + sub < p.Hkv) ask_head(v + (v_first * kGroup + sub) * D);
+    }
+    __device__ __forceinline__ void move(const RotateParams &p, const Turner<D> &t, __nv_bfloat16 *q_dst, __nv_bfloat16 *k_dst, __nv_bfloat16 *v_dst,
+                                         int kv_stride) const {
+        walk_heads<D, true>(p, t, q, q_dst, p.Hq, D, q_first, p.q_weight);
+        walk_heads<D, true>(p, t, k, k_dst, p.Hkv, kv_stride, k_first, p.k_weight);
+        walk_heads<D, false>(p, t, v, v_dst, p.Hkv, kv_stride, v_first, nullptr);
+    }
+};
+
+// Zeros in place of a warp's share of a rejected token's heads (all warps of the token together: all of it).
+template <int D>
+__device__ __forceinline__ void zero_heads(__nv_bfloat16 *dst, int heads, int first, int share, int lane) {
+    for (int i = first * 32 + lane; i < heads * (D / 8); i += share * 32) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(0, 0, 0, 0);
+}
+
+// What keeps sequence b's n new tokens from being written.  Warp-collective.
+__device__ __forceinline__ int append_status(const RotateParams &p, int b, int n, int L, int lane) {
+    if (n == 0) return L < 0 ? READER_ERR_CAPACITY : READER_OK;
     bool room = L >= 0 && L >= p.shared_prefix_len && (int64_t)L + n <= (int64_t)p.max_pages * kPage;
     if (p.rope && (int64_t)L + n > p.max_positions) room = false;
-    if (n == 0) return L < 0 ? READER_ERR_CAPACITY : READER_OK;
     if (!room) return READER_ERR_CAPACITY;
     bool bad = false;
-    for (int i = L / kPage + threadIdx.x; i <= (L + n - 1) / kPage; i += blockDim.x) {
+    for (int i = L / kPage + lane; i <= (L + n - 1) / kPage; i += 32) {
         const int pg = p.page_table[(size_t)b * p.max_pages + i];
         bad |= pg < 0 || pg >= p.num_pages;
     }
-    return __syncthreads_or(bad) ? READER_ERR_BAD_PAGE : READER_OK;
+    return __any_sync(0xffffffffu, bad) ? READER_ERR_BAD_PAGE : READER_OK;
 }
 
-// Blocks 0 .. total_tokens-1: one token each.  Blocks behind them: one sequence's status word each.
+// Warps 0 .. tokens * share - 1: one token's heads, or a share of them.  Warps behind them: one sequence's status
+// word each.
 template <int D>
-__global__ void __launch_bounds__(kThreads) prompt_append_kernel(const RotateParams p) {
-    __shared__ int s_seq;
+__global__ void __launch_bounds__(kThreads, 3) prompt_append_kernel(const RotateParams p) {
     pdl_wait();
     pdl_launch_dependents();
-    const int token = blockIdx.x < (unsigned)p.tokens ? (int)blockIdx.x : -1;
-    // One pass over token_start: is it in order, and whose token is this?  Block-wide; -1: nobody's.
-    auto owner = [&](int &start, int &n) -> int {
-        if (threadIdx.x == 0) s_seq = -1;
-        __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), writers = (int64_t)p.tokens * p.share;
+    const int token = w < writers ? (int)(w / p.share) : -1;
+    if (w >= writers + p.B) return;
+    // One pass over token_start: is it in order, and whose token is this (-1: nobody's)?
+    int start = 0, n = 0;
+    auto owner = [&]() -> int {
         bool bad = false;
-        for (int i = threadIdx.x; i < p.B; i += kThreads) {
+        int mine = -1;
+        for (int i = lane; i < p.B; i += 32) {
             const int a = p.token_start[i], e = p.token_start[i + 1];
             bad |= a < 0 || a > e || e > p.tokens;
-            if (token >= 0 && a <= token && token < e) s_seq = i;
+            if (token >= 0 && a <= token && token < e) mine = i;
         }
-        if (__syncthreads_or(bad)) return -2;
-        const int b = token >= 0 ? s_seq : (int)blockIdx.x - p.tokens;
+        if (__any_sync(0xffffffffu, bad)) return -2;
+        const int b = token >= 0 ? __reduce_max_sync(0xffffffffu, mine) : (int)(w - writers);
         if (b < 0) return -1;
         start = p.token_start[b];
         n = p.token_start[b + 1] - start;
         return b;
     };
-    int start = 0, n = 0;
     if (token < 0) {
-        const int b = owner(start, n);
-        const int st = b == -2 ? READER_ERR_INVALID_ARG : append_status(p, b, n);
-        if (threadIdx.x == 0) p.status[blockIdx.x - p.tokens] = st;
+        const int b = owner();
+        const int st = b == -2 ? READER_ERR_INVALID_ARG : append_status(p, b, n, p.seq_lens[b], lane);
+        if (lane == 0) p.status[w - writers] = st;
         return;
     }
     Turner<D> t;
-    t.init(p, threadIdx.x & 31);
-    uint4 *k_dst = nullptr, *v_dst = nullptr;
-    token_heads<D>(
-        p, token, t,
-        [&]() {
-            const int b = owner(start, n);
-            if (b < 0) return -1;
-            if (append_status(p, b, n) != READER_OK) return 0;
-            const int pos = p.seq_lens[b] + (token - start);
-            const int page = p.page_table[(size_t)b * p.max_pages + pos / kPage];
-            const size_t at = ((size_t)page * p.Hkv * kPage + pos % kPage) * D;
-            k_dst = reinterpret_cast<uint4 *>(p.k_out + at);
-            v_dst = reinterpret_cast<uint4 *>(p.v_out + at);
-            t.load_table(p, pos);
-            return 1;
-        },
-        [&](int x) -> uint4 * {
-            constexpr size_t kHeadPieces = (size_t)kPage * D / 8;
-            if (x < p.Hq) return reinterpret_cast<uint4 *>(p.q_out + ((size_t)token * p.Hq + x) * D);
-            if (!k_dst) return nullptr;
-            return x < p.Hq + p.Hkv ? k_dst + (x - p.Hq) * kHeadPieces : v_dst + (x - p.Hq - p.Hkv) * kHeadPieces;
-        });
+    t.init(p, lane);
+    const int first = (int)(w % p.share);
+    Token<D> tok;
+    tok.init(p, token, first);
+    tok.prefetch(p, t, lane);
+    const int b = owner();
+    if (b < 0) return;
+    __nv_bfloat16 *q_row = p.q_out + (size_t)token * p.Hq * D;
+    const int L = p.seq_lens[b];
+    if (append_status(p, b, n, L, lane) != READER_OK) return zero_heads<D>(q_row, p.Hq, first, p.share, lane);
+    const int pos = L + (token - start);
+    t.load_table(p, pos);
+    const int page = p.page_table[(size_t)b * p.max_pages + pos / kPage];
+    const size_t at = ((size_t)page * p.Hkv * kPage + pos % kPage) * D;
+    tok.move(p, t, q_row, p.k_out + at, p.v_out + at, kPage * D);
 }
 
-// Block b * T + j: node j of sequence b's tree.
+// Block (y, b): the warps y * 8 .. y * 8 + 7 of sequence b; warp j * share + s: node j of its tree, or a share of its heads.
 template <int D>
-__global__ void __launch_bounds__(kThreads) tree_rotate_kernel(const RotateParams p) {
-    __shared__ int hop[2][kMaxNodes + 1], depth[2][kMaxNodes + 1];
+__global__ void __launch_bounds__(kThreads, 4) tree_rotate_kernel(const RotateParams p) {
+    __shared__ int32_t par[kMaxNodes];
     pdl_wait();
     pdl_launch_dependents();
-    const int b = blockIdx.x / p.T, j = blockIdx.x - b * p.T, tid = threadIdx.x;
-    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 31, blocks = (p.T * p.share + kThreads / 32 - 1) / (kThreads / 32);
+    const int b = blockIdx.x / blocks, w = (blockIdx.x - b * blocks) * (kThreads / 32) + (threadIdx.x >> 5);
+    const int j = w / p.share, first = w - j * p.share;
+    const int64_t row = (int64_t)b * p.T + min(j, p.T - 1);
     Turner<D> t;
-    t.init(p, tid & 31);
-    token_heads<D>(
-        p, row, t,
-        [&]() {
-            // depth of every node by doubling: after step i, hop is the ancestor 2^i levels up (T: above the root) and
-            // depth the nodes passed on the way
-            bool bad = false;
-            for (int i = tid; i <= p.T; i += kThreads) {
-                const int par = i < p.T ? p.parent[(size_t)b * p.T + i] : -1;
-                const bool ok = i == p.T || (i == 0 ? par == -1 : par >= 0 && par < i);
-                bad |= !ok;
-                hop[0][i] = ok && par >= 0 ? par : p.T;
-                depth[0][i] = i < p.T;
-            }
-            const bool bad_tree = __syncthreads_or(bad);
-            int cur = 0;
-            for (int step = 1; step < p.T; step <<= 1) {
-                for (int i = tid; i <= p.T; i += kThreads) {
-                    const int h = hop[cur][i];
-                    depth[cur ^ 1][i] = depth[cur][i] + depth[cur][h];
-                    hop[cur ^ 1][i] = hop[cur][h];
-                }
-                __syncthreads();
-                cur ^= 1;
-            }
-            const int L = p.seq_lens[b];
-            bool far = L < 0;
-            if (p.rope && !bad_tree)
-                for (int i = tid; i < p.T; i += kThreads) far |= (int64_t)L + depth[cur][i] > p.max_positions;
-            const bool no_room = __syncthreads_or(far);
-            if (j == 0 && tid == 0) p.status[b] = bad_tree ? READER_ERR_BAD_TREE : no_room ? READER_ERR_CAPACITY : READER_OK;
-            if (bad_tree || no_room) return 0;
-            t.load_table(p, (int64_t)L + depth[cur][j] - 1);
-            return 1;
-        },
-        [&](int x) -> uint4 * {
-            if (x < p.Hq) return reinterpret_cast<uint4 *>(p.q_out + (row * p.Hq + x) * D);
-            if (x < p.Hq + p.Hkv) return reinterpret_cast<uint4 *>(p.k_out + (row * p.Hkv + x - p.Hq) * D);
-            return reinterpret_cast<uint4 *>(p.v_out + (row * p.Hkv + x - p.Hq - p.Hkv) * D);
-        });
+    t.init(p, lane);
+    Token<D> tok;
+    tok.init(p, row, first);
+    tok.prefetch(p, t, lane);
+    const int L = p.seq_lens[b];
+    bool bad = false;
+    for (int i = threadIdx.x; i < p.T; i += kThreads) {
+        const int above = p.parent[(size_t)b * p.T + i];
+        bad |= !(i == 0 ? above == -1 : above >= 0 && above < i);
+        par[i] = above;
+    }
+    const bool bad_tree = __syncthreads_or(bad);
+    if (j >= p.T) return;
+    auto nodes_above = [&](int i) {   // the chain strictly decreases on a valid tree
+        int n = 0;
+        for (i = par[i]; i >= 0; i = par[i]) ++n;
+        return n;
+    };
+    bool no_room = L < 0;
+    // only a table that might be too short needs every node's depth
+    if (p.rope && !bad_tree && (int64_t)L + p.T > p.max_positions) {
+        for (int i = lane; i < p.T; i += 32) no_room |= (int64_t)L + nodes_above(i) >= p.max_positions;
+        no_room = __any_sync(0xffffffffu, no_room);
+    }
+    if (j == 0 && first == 0 && lane == 0) p.status[b] = bad_tree ? READER_ERR_BAD_TREE : no_room ? READER_ERR_CAPACITY : READER_OK;
+    __nv_bfloat16 *q_row = p.q_out + row * p.Hq * D, *k_row = p.k_out + row * p.Hkv * D, *v_row = p.v_out + row * p.Hkv * D;
+    if (bad_tree || no_room) {
+        zero_heads<D>(q_row, p.Hq, first, p.share, lane);
+        zero_heads<D>(k_row, p.Hkv, first, p.share, lane);
+        zero_heads<D>(v_row, p.Hkv, first, p.share, lane);
+        return;
+    }
+    t.load_table(p, (int64_t)L + nodes_above(j));
+    tok.move(p, t, q_row, k_row, v_row, D);
 }
+
+// Warps per token: one, unless that leaves the GPU short of warps (16 an SM); a power of two, no more than give every
+// group of heads a warp of its own.
+int warps_per_token(int64_t tokens, int heads, int D, int n_sm) {
+    const int groups = (heads * (D / 8) + 31) / 32;
+    int share = 1;
+    while (share < groups && tokens * share < 16 * (int64_t)n_sm) share *= 2;
+    return share;
+}
+dim3 blocks_for(int64_t warps) { return dim3((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32))); }
 
 }  // namespace
 
-void launch_prompt_append(const RotateParams &p, cudaStream_t st) {
-    launch_pdl(p.D == 128 ? prompt_append_kernel<128> : prompt_append_kernel<64>, dim3((unsigned)(p.tokens + p.B)), dim3(kThreads), 0, st, p);
+void launch_prompt_append(RotateParams p, int n_sm, cudaStream_t st) {
+    p.share = warps_per_token(p.tokens, p.Hq + 2 * p.Hkv, p.D, n_sm);
+    launch_pdl(p.D == 128 ? prompt_append_kernel<128> : prompt_append_kernel<64>, blocks_for((int64_t)p.tokens * p.share + p.B), dim3(kThreads), 0, st, p);
 }
 
-void launch_tree_rotate(const RotateParams &p, cudaStream_t st) {
-    launch_pdl(p.D == 128 ? tree_rotate_kernel<128> : tree_rotate_kernel<64>, dim3((unsigned)(p.T * p.B)), dim3(kThreads), 0, st, p);
+void launch_tree_rotate(RotateParams p, int n_sm, cudaStream_t st) {
+    const int64_t nodes = (int64_t)p.B * p.T;
+    p.share = warps_per_token(nodes, p.Hq + 2 * p.Hkv, p.D, n_sm);
+    launch_pdl(p.D == 128 ? tree_rotate_kernel<128> : tree_rotate_kernel<64>, dim3((unsigned)(p.B * ((p.T * p.share + kThreads / 32 - 1) / (kThreads / 32)))), dim3(kThreads), 0, st, p);
 }
 
 }  // namespace reader

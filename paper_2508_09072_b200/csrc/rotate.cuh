@@ -15,6 +15,7 @@ struct RotateParams {
     const int32_t *seq_lens;
     __nv_bfloat16 *q_out, *k_out, *v_out;      // k_out, v_out: the pools, or the tree tensors
     int32_t *status;
+    int share;                                 // warps that share a token's heads
     // prompt
     int tokens;                                // rows of the packed tensors
     const int32_t *token_start;                // [B + 1]
@@ -25,7 +26,7 @@ struct RotateParams {
     const int32_t *parent;
 };
 
-void launch_prompt_append(const RotateParams &p, cudaStream_t st);
-void launch_tree_rotate(const RotateParams &p, cudaStream_t st);
+void launch_prompt_append(RotateParams p, int n_sm, cudaStream_t st);
+void launch_tree_rotate(RotateParams p, int n_sm, cudaStream_t st);
 
 }  // namespace reader
