@@ -8,23 +8,27 @@
 //   warps 0-3, 4-7  softmax of slot 0 / 1: thread = query row, so a row's maximum and sum need no exchange
 //   warp 8          producer: K and V tiles of 128 keys (two cache pages) by TMA through one ring, in the order in
 //                   which they are multiplied; the query tiles of the next segment
-//   warp 9          issues S = Q K^T and O += P V for both slots:  PV0(i) S0(i+1) PV1(i) S1(i+1) ...
+//   warps 9, 11     issue S = Q K^T and O += P V of slot 0 / 1
 //   warp 10         prepares the value tiles that hold keys some query of the unit does not see
 //
 // TMEM (512 columns): scores of slot 0 and 1 (128 columns each, fp32), outputs of slot 0 and 1 (D columns each).  The
 // probabilities (bf16 pairs, 64 columns) take the place of their scores.  S(i+1) of a slot is issued behind PV(i),
-// which reads P(i) from the same columns, and the tensor pipe runs a CTA's products in the order of their issue.
+// which reads P(i) from the same columns, and the tensor pipe runs the products that a thread issues in their order.
+// P comes in two halves of 64 keys, so that the first half's product runs beside the second half's exponentials.
 //
 // Softmax: the exponentials of a tile are taken against the maximum known from the tiles before it while the tile's
 // own maximum is found on the side; only if that exceeds the old one by more than 2^8 is the maximum raised, the
-// output rescaled and the tile done again (always on a segment's first tile, hardly ever later).  Scores, maxima,
-// sums and outputs are fp32; P is rounded to bf16 for the value product (relative error of a weight 2^-9 at most, of
+// output rescaled and the half done again (a segment's first tile looks for its maximum first).  Scores, maxima,
+// sums and outputs are fp32; P is rounded to bf16 for the value product (relative error of a weight 2^-8 at most, of
 // the size of the output's own rounding), the row sum adds the unrounded weights.
 //
 // Keys that a row does not see get the score -inf by selection, whatever the cache holds there.  Values cannot be
 // selected in a matrix product (0 * inf is NaN), so warp 10 goes over the tiles that hold keys of the unit's own
 // tokens: rows behind the unit's last key are not multiplied or zeroed; an infinity or NaN in a row that some of the
 // queries see is replaced by zero, and the epilogue adds it to exactly the rows that see it.
+//
+// Output rows leave through shared memory, 4 KB a warp: a warp's store then fills whole 128-byte lines.  (Straight from the
+// thread = row layout, 16 bytes of 32 lines at a time, a segment's epilogue took 5500 to 9400 cycles.)
 //
 // Every wait is bounded: a CTA that waits a second without progress marks its word in the workspace, stops waiting
 // and runs to its end; the finishing kernel turns the mark into status words and zero rows.
@@ -40,36 +44,33 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 11 * 32;
+constexpr int kThreads = 12 * 32;   // three warpgroups: two of softmax, one of single warps
+// 168 registers a thread at launch; the softmax warpgroups take what the third can spare: 2 * 208 + 88 = 3 * 168
+constexpr int kRegsSoftmax = 208, kRegsOther = 88;
 constexpr int kProducerWarp = 8, kMmaWarp = 9, kValueWarp = 10;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kRaiseMaxBy = 8.f;   // log2 units
+#ifndef POLY
+#define POLY 2
+#endif
+constexpr int kPolyOf8 = POLY;      // of eight pairs of exponentials, how many are computed on the FMA pipe
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
-constexpr int kMaxStages = 10;
-constexpr int kPoisonRing = 8;       // segments the value warp may be ahead of an epilogue (the ring holds 5 value tiles)
+constexpr int kMaxStages = 8;
+constexpr int kPoisonRing = 8;       // segments the value warp may be ahead of an epilogue (the ring holds 4 value tiles)
+
+constexpr int kMiscBytes = 3072;
 
 template <int D>
 struct Cfg {
     static constexpr int kHalves = D / 64;                   // 64-column (128-byte) blocks per row
     static constexpr int kBlockBytes = 128 * 128;            // one 64-column block of 128 rows
     static constexpr int kTileBytes = kHalves * kBlockBytes; // a query, key or value tile
-    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int kStages = D == 128 ? 4 : 8;
     static constexpr int kOffRing = 2 * kTileBytes;
-    static constexpr int kOffMisc = kOffRing + kStages * kTileBytes;
-    static constexpr int kSmemBytes = kOffMisc + 2048;
+    static constexpr int kOffStaging = kOffRing + kStages * kTileBytes;   // 4 KB per softmax warp
+    static constexpr int kOffMisc = kOffStaging + 8 * 4096;
+    static constexpr int kSmemBytes = kOffMisc + kMiscBytes;
 };
-
-struct Misc {
-    uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t raw[kMaxStages];  // a value tile that the value warp goes over first has landed; that warp then completes `full`
-    uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], merge_ready, merge_free;
-    float2 ml[128];            // slot 1's row maxima and sums of a narrow unit
-    int32_t poison[kPoisonRing];
-    int32_t seq, head, block, off, w_begin, w_end, W, ctas;
-    uint32_t tmem_base;
-    int32_t abort;
-};
-static_assert(sizeof(Misc) <= 2048, "shared memory behind the ring");
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int32_t *abort_s) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -97,7 +98,7 @@ struct Piece {
     int first_token;         // of the unit, within the sequence
 };
 
-// Walks a CTA's range; every role does it for itself.
+// Where a warp stands in its CTA's range.
 struct Walk {
     int b, h, block, off, left, w;
     int start, L, n, blocks;
@@ -107,41 +108,74 @@ struct Walk {
         L = p.seq_lens[b];
         blocks = prompt_len_ok(L, n, p.max_pages) ? unit_blocks(n, p.tile_tokens) : 0;
     }
-    __device__ __forceinline__ void init(const PromptAttnParams &p, const Misc *m) {
-        b = m->seq; h = m->head; block = m->block; off = m->off; w = m->w_begin; left = m->w_end - m->w_begin;
-        if (left > 0) open(p);
-    }
-    // The next segment with at least one key tile; false at the end of the range.
-    __device__ __forceinline__ bool next(const PromptAttnParams &p, Piece &s) {
-        while (left > 0) {
-            while (block >= blocks) {   // on to the next head, the next sequence with tokens
-                block = 0;
-                if (blocks == 0 || ++h == p.Hkv) {
-                    h = 0;
-                    if (++b >= p.B) { left = 0; return false; }
-                    open(p);
-                }
-            }
-            s.u = unit_shape(L, n, block, p.tile_tokens);
-            const int entries = kUnitEntries + s.u.steps;
-            const int take = min(entries - off, left);
-            const int s0 = max(0, off - kUnitEntries), s1 = off + take - kUnitEntries;
-            s.b = b; s.h = h; s.block = block;
-            s.start = start; s.L = L; s.n = n;
-            s.first_token = block * 2 * p.tile_tokens;
-            s.t0 = s.u.narrow ? 2 * s0 : s0;
-            s.nt = s1 <= s0 ? 0 : (s.u.narrow ? min(2 * s1, s.u.tiles) : s1) - s.t0;
-            s.full = s0 == 0 && s1 == s.u.steps;
-            s.slot = s0 == 0 ? 1 : 0;
-            w += take;
-            left -= take;
-            off += take;
-            if (off == entries) { off = 0; ++block; }
-            if (s.nt > 0) return true;
-        }
-        return false;
-    }
 };
+
+struct Misc {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t raw[kMaxStages];  // a value tile that the value warp goes over first has landed; that warp then completes `full`
+    uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2], turn[2], merge_ready, merge_free;
+    float2 ml[128];            // slot 1's row maxima and sums of a narrow unit
+    int32_t poison[kPoisonRing];
+    int32_t seq, head, block, off, w_begin, w_end, W, ctas;
+    uint32_t tmem_base;
+    int32_t abort;
+    Walk walk[12];             // one per warp: every role walks the range for itself, and has its registers for other things
+    Piece piece[12];
+};
+static_assert(sizeof(Misc) <= kMiscBytes, "shared memory behind the staging");
+
+__device__ __forceinline__ void walk_init(const PromptAttnParams &p, Misc *m, int warp, int lane) {
+    Walk w;
+    w.b = m->seq; w.h = m->head; w.block = m->block; w.off = m->off; w.w = m->w_begin; w.left = m->w_end - m->w_begin;
+    w.start = w.L = w.n = w.blocks = 0;
+    if (w.left > 0) w.open(p);
+    if (lane == 0) m->walk[warp] = w;
+    __syncwarp();
+}
+
+// The warp's next segment with at least one key tile, in m->piece[warp]; false at the end of the range.
+__device__ __forceinline__ bool walk_next(const PromptAttnParams &p, Misc *m, int warp, int lane) {
+    __syncwarp();
+    Walk w = m->walk[warp];
+    Piece s;
+    s.nt = 0;
+    while (w.left > 0 && s.nt <= 0) {
+        while (w.block >= w.blocks) {   // on to the next head, the next sequence with tokens
+            w.block = 0;
+            if (w.blocks == 0 || ++w.h == p.Hkv) {
+                w.h = 0;
+                if (++w.b >= p.B) break;
+                w.open(p);
+            }
+        }
+        if (w.b >= p.B) {
+            w.left = 0;
+            break;
+        }
+        s.u = unit_shape(w.L, w.n, w.block, p.tile_tokens);
+        const int entries = kUnitEntries + s.u.steps;
+        const int take = min(entries - w.off, w.left);
+        const int s0 = max(0, w.off - kUnitEntries), s1 = w.off + take - kUnitEntries;
+        s.b = w.b; s.h = w.h; s.block = w.block;
+        s.start = w.start; s.L = w.L; s.n = w.n;
+        s.first_token = w.block * 2 * p.tile_tokens;
+        s.t0 = s.u.narrow ? 2 * s0 : s0;
+        s.nt = s1 <= s0 ? 0 : (s.u.narrow ? min(2 * s1, s.u.tiles) : s1) - s.t0;
+        s.full = s0 == 0 && s1 == s.u.steps;
+        s.slot = s0 == 0 ? 1 : 0;
+        w.w += take;
+        w.left -= take;
+        w.off += take;
+        if (w.off == entries) { w.off = 0; ++w.block; }
+    }
+    __syncwarp();
+    if (lane == 0) {
+        m->walk[warp] = w;
+        m->piece[warp] = s;
+    }
+    __syncwarp();
+    return s.nt > 0;
+}
 
 // Ring places of a segment's tiles.  Order: the first `ahead` key tiles, then V0, K(ahead), V1, K(ahead + 1), ...
 __device__ __forceinline__ int ahead_of(const Piece &s) { return min(s.u.narrow ? 2 : 1, s.nt); }
@@ -243,6 +277,26 @@ struct PageCursor {
     }
 };
 
+// 2^x for two arguments on the FMA pipe, beside the 16 results a cycle and SM of the special-function unit: with
+// n = x rounded to an integer (through the 1.5 * 2^23 trick) and f = x - n in [-1/2, 1/2], 2^f is a polynomial (minimax in
+// the relative error, 2.7e-6 in fp32: far below the 2^-9 that the rounding of P to bf16 costs) and n goes into the exponent
+// field.  Arguments below -126 give 2^-126 - 2^-126 = 0; the kernel's arguments stay below 2^7 by far.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+    constexpr float kRound = 12582912.f, kTiny = 1.17549435e-38f;
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const float2 t = __fadd2_rn(x, make_float2(kRound, kRound));
+    const float2 n = __fadd2_rn(t, make_float2(-kRound, -kRound));
+    const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
+    float2 y = __ffma2_rn(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
+    y = __ffma2_rn(y, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    y = __ffma2_rn(y, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    y = __ffma2_rn(y, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
+    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
+    return __fadd2_rn(y, make_float2(-kTiny, -kTiny));
+}
+
 __device__ __forceinline__ bool nonfinite_bits(uint32_t half) { return (half & 0x7f80u) == 0x7f80u; }
 
 template <int D>
@@ -268,21 +322,24 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(bar(&m->full[i]), 1);
-            mbar_init(bar(&m->empty[i]), 1);
+            mbar_init(bar(&m->empty[i]), 2);   // both slots
             mbar_init(bar(&m->raw[i]), 1);
         }
         mbar_init(bar(&m->q_full), 1);
-        mbar_init(bar(&m->q_empty), 1);
+        mbar_init(bar(&m->q_empty), 2);
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar(&m->s_full[s]), 1);
-            mbar_init(bar(&m->p_full[s]), 128);
+            mbar_init(bar(&m->p_full[s][0]), 128);
+            mbar_init(bar(&m->p_full[s][1]), 128);
             mbar_init(bar(&m->o_full[s]), 1);
+            mbar_init(bar(&m->turn[s]), 1);
         }
         mbar_init(bar(&m->merge_ready), 128);
         mbar_init(bar(&m->merge_free), 128);
         m->abort = 0;
         for (int i = 0; i < kPoisonRing; ++i) m->poison[i] = 0;
         fence_mbar_init();
+        mbar_arrive(bar(&m->turn[0]));   // slot 0 has the first turn
         fence_proxy_async();
         prefetch_tensormap(&qmap);
         prefetch_tensormap(&kmap);
@@ -303,10 +360,12 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
     if (tid == 0) fence_proxy_async();   // the ring was scratch until here
     __syncthreads();
 
-    Walk walk;
-    walk.init(p, m);
-    Piece sg{};
+    walk_init(p, m, warp, lane);
+    const Piece &sg = m->piece[warp];
+    auto next = [&]() { return walk_next(p, m, warp, lane); };
 
+    if (warp >= 8) {
+    regs_dec<kRegsOther>();
     if (warp == kProducerWarp) {
         // ------------------------------------------------------------------ producer
         int r = 0, seg = 0;
@@ -328,7 +387,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             ++r;
         };
         const int tile_rows_bytes = p.G * p.tile_tokens * 128;
-        while (!*abort_s && walk.next(p, sg)) {
+        while (!*abort_s && next()) {
             if (wait(bar(&m->q_empty), (seg & 1) ^ 1, abort_s) && elect_one()) {
                 const uint32_t full = bar(&m->q_full);
                 const int tiles = sg.u.narrow ? 1 : 2;
@@ -365,109 +424,112 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 while (!mbar_try_wait(bar(&m->q_full), (seg - 1) & 1) && globaltimer_ns() - t0 < 20000000ull) {
                 }
         }
-    } else if (warp == kMmaWarp) {
-        // ------------------------------------------------------------------ issuer of both products
+    } else if (warp != kValueWarp) {
+        // ------------------------------------------------------------------ issuer of a slot's products
+        const int slot = warp == kMmaWarp ? 0 : 1;
         constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kKeyTile, false, false);
         constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, false, true);
         const uint64_t descQ = smem_desc_sw128(sQ, 16, 1024), descK = smem_desc_sw128(sRing, 16, 1024);
         const uint64_t descV = smem_desc_sw128(sRing, C::kBlockBytes, 1024);
-        int r0 = 0, seg = 0;
-        uint32_t p_parity = 0;   // one bit per slot
-        auto stage_of = [&](int r) { return r % C::kStages; };
-        auto wait_full = [&](int r) { wait(bar(&m->full[stage_of(r)]), (r / C::kStages) & 1, abort_s); };
-        auto issue_s = [&](int slot, int q_tile, int r, bool release) {
-            tc_fence_after();
-            __syncwarp();
-            if (elect_one()) {
-                const uint64_t qd = descQ + (uint64_t)((q_tile * C::kTileBytes) >> 4);
-                const uint64_t kd = descK + (uint64_t)((stage_of(r) * C::kTileBytes) >> 4);
-#pragma unroll
-                for (int hf = 0; hf < C::kHalves; ++hf)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        mma_bf16_ss(tmem + kTmemS + slot * 128, qd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4),
-                                    kd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
-                mma_commit(bar(&m->s_full[slot]));
-                if (release) mma_commit(bar(&m->empty[stage_of(r)]));
-            }
-            __syncwarp();
-        };
-        auto issue_pv = [&](int slot, int r, int slices, bool first, bool release, bool last) {
-            tc_fence_after();
-            __syncwarp();
-            if (elect_one()) {
-                const uint64_t vd = descV + (uint64_t)((stage_of(r) * C::kTileBytes) >> 4);
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    if (kk < slices)
-                        mma_bf16_ts(tmem + kTmemO + slot * D, tmem + kTmemS + slot * 128 + kk * 8, vd + (uint64_t)((kk * 2048) >> 4),
-                                    kIdescPV, !first || kk != 0);
-                if (release) mma_commit(bar(&m->empty[stage_of(r)]));
-                if (last) mma_commit(bar(&m->o_full[slot]));
-            }
-            __syncwarp();
-        };
-        auto commit_q = [&]() {
-            if (elect_one()) mma_commit(bar(&m->q_empty));
-            __syncwarp();
-        };
-        while (!*abort_s && walk.next(p, sg)) {
-            const int ahead = ahead_of(sg), n = sg.nt;
-            const bool narrow = sg.u.narrow;
-            auto wait_v = [&](int j) -> int {
-                const int r = r0 + place_of_v(j, ahead, n);
+        const uint32_t tS = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + slot * D;
+        int r = 0, seg = 0;   // r: the next place in the ring that this warp has not seen
+        uint32_t p_parity = 0, turn_parity = 0;
+        auto wait_full = [&](int place) { wait(bar(&m->full[place % C::kStages]), (place / C::kStages) & 1, abort_s); };
+        // Both issuers see every tile in the ring's order, so that neither can fall a whole turn behind (a parity wait
+        // tells a phase only from the one before it); tiles of the other slot are passed on at once.
+        auto pass_to = [&](int place) {
+            for (; r < place; ++r) {
                 wait_full(r);
-                return r;
+                if (lane == 0) mbar_arrive(bar(&m->empty[r % C::kStages]));
+            }
+            __syncwarp();
+        };
+        auto issue_s = [&](uint64_t qd, int place, bool last) {
+            const uint64_t kd = descK + (uint64_t)(((place % C::kStages) * C::kTileBytes) >> 4);
+#pragma unroll
+            for (int hf = 0; hf < C::kHalves; ++hf)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_bf16_ss(tS, qd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4),
+                                kd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
+            mma_commit(bar(&m->s_full[slot]));
+            mma_commit(bar(&m->empty[place % C::kStages]));
+            if (last) mma_commit(bar(&m->q_empty));
+        };
+        // half 0: the first 64 keys of the tile, half 1: the others
+        auto issue_pv = [&](int half, int place, int slices, bool first) {
+            const uint64_t vd = descV + (uint64_t)(((place % C::kStages) * C::kTileBytes) >> 4);
+#pragma unroll
+            for (int k4 = 0; k4 < 4; ++k4) {
+                const int kk = half * 4 + k4;
+                if (kk < slices) mma_bf16_ts(tO, tS + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), kIdescPV, !first || kk != 0);
+            }
+        };
+        while (!*abort_s && next()) {
+            const int ahead = ahead_of(sg), n = sg.nt, r0 = r, t0 = sg.t0, keys = sg.u.keys;
+            const bool narrow = sg.u.narrow;
+            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1;
+            const uint64_t qd = descQ + (uint64_t)((narrow ? 0 : slot * C::kTileBytes) >> 4);
+            // Left to themselves the two slots fall into step, score products side by side and then both softmaxes
+            // on the special-function units at once (3970 cycles a step).  In a wide unit they therefore take turns with
+            // their score products, slot 0 first: each slot's softmax then runs beside the other's products.
+            auto take_turn = [&]() {
+                if (!narrow) wait(bar(&m->turn[slot]), turn_parity, abort_s);
+                turn_parity ^= narrow ? 0 : 1;
             };
-            auto slices_of = [&](int j) { return (min(kKeyTile, sg.u.keys - (sg.t0 + j) * kKeyTile) + 15) >> 4; };
-            auto wait_p = [&](int slot) {
-                wait(bar(&m->p_full[slot]), (p_parity >> slot) & 1, abort_s);
-                p_parity ^= 1u << slot;
+            auto pass_turn = [&]() {
+                if (!narrow && lane == 0) mbar_arrive(bar(&m->turn[slot ^ 1]));
+                __syncwarp();
             };
             wait(bar(&m->q_full), seg & 1, abort_s);
             ++seg;
-            if (narrow) {
-                for (int j = 0; j < ahead; ++j) {
-                    const int r = r0 + j;
-                    wait_full(r);
-                    issue_s(j, 0, r, true);
-                }
-                if (n <= 2) commit_q();
-                for (int j = 0; j < n; ++j) {
-                    const int slot = j & 1;
-                    wait_p(slot);
-                    const int rv = wait_v(j);
-                    issue_pv(slot, rv, slices_of(j), j < 2, true, j + 2 >= n);
-                    if (j + 2 < n) {
-                        const int rk = r0 + place_of_k(j + 2, ahead);
-                        wait_full(rk);
-                        issue_s(slot, 0, rk, true);
-                        if (j + 3 == n) commit_q();
+            if (j0 < n) {
+                pass_to(r0 + place_of_k(j0, ahead));
+                wait_full(r);
+                take_turn();
+                tc_fence_after();
+                __syncwarp();
+                if (elect_one()) issue_s(qd, r, j0 + dj >= n);
+                __syncwarp();
+                pass_turn();
+                ++r;
+                for (int j = j0; j < n; j += dj) {
+                    const int slices = (min(kKeyTile, keys - (t0 + j) * kKeyTile) + 15) >> 4;
+                    const bool more = j + dj < n;
+                    pass_to(r0 + place_of_v(j, ahead, n));
+                    const int rv = r;
+                    wait_full(r++);
+                    wait(bar(&m->p_full[slot][0]), p_parity, abort_s);
+                    tc_fence_after();
+                    __syncwarp();
+                    if (elect_one()) issue_pv(0, rv, slices, j == j0);
+                    __syncwarp();
+                    if (more) {
+                        pass_to(r0 + place_of_k(j + dj, ahead));
+                        wait_full(r);
+                        take_turn();
+                    }
+                    wait(bar(&m->p_full[slot][1]), p_parity, abort_s);
+                    p_parity ^= 1;
+                    tc_fence_after();
+                    __syncwarp();
+                    if (elect_one()) {
+                        issue_pv(1, rv, slices, j == j0);
+                        mma_commit(bar(&m->empty[rv % C::kStages]));
+                        if (more) issue_s(qd, r, j + 2 * dj >= n);
+                        else mma_commit(bar(&m->o_full[slot]));
+                    }
+                    __syncwarp();
+                    if (more) {
+                        pass_turn();
+                        ++r;
                     }
                 }
             } else {
-                wait_full(r0);
-                issue_s(0, 0, r0, false);
-                issue_s(1, 1, r0, true);
-                if (n == 1) commit_q();
-                for (int j = 0; j < n; ++j) {
-                    int rv = 0, rk = 0;
-                    for (int slot = 0; slot < 2; ++slot) {
-                        wait_p(slot);
-                        if (slot == 0) rv = wait_v(j);
-                        issue_pv(slot, rv, slices_of(j), j == 0, slot == 1, j + 1 == n);
-                        if (j + 1 < n) {
-                            if (slot == 0) {
-                                rk = r0 + place_of_k(j + 1, ahead);
-                                wait_full(rk);
-                            }
-                            issue_s(slot, slot, rk, slot == 1);
-                        }
-                    }
-                    if (j + 2 == n) commit_q();
-                }
+                if (lane == 0) mbar_arrive(bar(&m->q_empty));   // a narrow piece of one tile: slot 1 has none
+                __syncwarp();
             }
-            r0 += 2 * n;
+            pass_to(r0 + 2 * n);
         }
     } else if (warp == kValueWarp) {
         // ------------------------------------------------------------------ values some queries do not see; the note on a split unit
@@ -475,11 +537,11 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         uint32_t raw_parity = 0;   // one bit per ring stage
         if (lane == 0) p.pieces[blockIdx.x].b = -1;
         __syncwarp();
-        while (!*abort_s && walk.next(p, sg)) {
+        while (!*abort_s && next()) {
             const int ahead = ahead_of(sg), n = sg.nt, own_key = sg.L + sg.first_token;
             if (!sg.full && sg.slot == 1 && lane == 0) {
                 const int s1 = sg.u.narrow ? (sg.t0 + sg.nt + 1) / 2 : sg.t0 + sg.nt;
-                const int unit_end = walk.w + (sg.u.steps - s1);   // the walk stands behind this segment's last entry
+                const int unit_end = m->walk[warp].w + (sg.u.steps - s1);   // the walk stands behind this segment's last entry
                 PieceDesc d;
                 d.b = sg.b; d.h = sg.h; d.block = sg.block;
                 d.more = prompt_range_owner(unit_end - 1, m->W, m->ctas) - (int)blockIdx.x;
@@ -495,24 +557,44 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 raw_parity ^= 1u << stage;
                 const uint32_t tile = sRing + stage * C::kTileBytes;
                 const int valid = min(kKeyTile, sg.u.keys - t * kKeyTile), end = (valid + 15) & ~15;
-                constexpr int kChunks = D / 8;   // 16-byte pieces per row
-                bool found = false;
-                for (int i = max(0, own_key - t * kKeyTile) * kChunks + lane; i < end * kChunks; i += 32) {
+                // First a look at the exponents of the rows some queries do not see (all ones: infinity or NaN), sixteen
+                // 16-byte pieces a lane in flight; only if there is one, the walk that replaces it.
+                constexpr int kChunks = D / 8, kBatch = 16;   // 16-byte pieces per row / per lane and turn
+                const int own_row = max(0, own_key - t * kKeyTile);
+                auto piece_at = [&](int i) {
                     const int row = i / kChunks, c = i % kChunks;
-                    const uint32_t at = tile + (c >> 3) * C::kBlockBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
-                    uint32_t x[4] = {0, 0, 0, 0};
-                    bool store = row >= valid;
-                    if (!store) {
+                    return tile + (c >> 3) * C::kBlockBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                };
+                uint32_t ones = 0;
+                for (int i0 = own_row * kChunks + lane; i0 < valid * kChunks; i0 += kBatch * 32) {
+                    uint32_t x[kBatch][4];
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) {
+                        x[k][0] = x[k][1] = x[k][2] = x[k][3] = 0;
+                        if (i0 + k * 32 < valid * kChunks)
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3]) : "r"(piece_at(i0 + k * 32)));
+                    }
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ones |= (x[k][e] & 0x7f807f80u) + 0x00800080u;
+                }
+                if (__any_sync(0xffffffffu, (ones & 0x80008000u) != 0)) {
+                    for (int i = own_row * kChunks + lane; i < valid * kChunks; i += 32) {
+                        uint32_t x[4];
+                        const uint32_t at = piece_at(i);
                         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            if (nonfinite_bits(x[e])) { x[e] &= 0xffff0000u; store = found = true; }
-                            if (nonfinite_bits(x[e] >> 16)) { x[e] &= 0x0000ffffu; store = found = true; }
+                            if (nonfinite_bits(x[e])) x[e] &= 0xffff0000u;
+                            if (nonfinite_bits(x[e] >> 16)) x[e] &= 0x0000ffffu;
                         }
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
                     }
-                    if (store) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                    if (lane == 0) *(volatile int32_t *)&m->poison[seg % kPoisonRing] = 1;
                 }
-                if (__any_sync(0xffffffffu, found) && lane == 0) *(volatile int32_t *)&m->poison[seg % kPoisonRing] = 1;
+                for (int i = valid * kChunks + lane; i < end * kChunks; i += 32)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at(i)), "r"(0u) : "memory");
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(&m->full[stage]));
@@ -520,8 +602,10 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             r0 += 2 * n;
             ++seg;
         }
+    }
     } else {
         // ------------------------------------------------------------------ softmax / epilogue
+        regs_inc<kRegsSoftmax>();
         const int slot = warp >> 2, row = tid & 127;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + kTmemS + slot * 128 + lane_base, tO = tmem + kTmemO + slot * D + lane_base;
@@ -529,7 +613,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         const int row_token = row / p.G, row_member = row - row_token * p.G;
         int seg = 0, narrows = 0;
         uint32_t s_parity = 0, o_parity = 0;
-        while (walk.next(p, sg)) {
+        while (next()) {
             const bool narrow = sg.u.narrow;
             const int unit_token = (narrow ? 0 : slot * p.tile_tokens) + row_token;   // within the unit
             const bool live = row_token < p.tile_tokens && unit_token < sg.u.tokens;
@@ -538,102 +622,91 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             const int last_key = sg.L + sg.first_token + (live ? unit_token : 0);
             const int warp_min = __reduce_min_sync(0xffffffffu, last_key);
             float mx = -INFINITY, l = 0.f;    // running maximum (scaled, log2 units) and row sum
-            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1;
+            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1, nt = sg.nt, t0 = sg.t0;
             bool any = false;
-            for (int j = j0; j < sg.nt; j += dj) {
-                const int key0 = (sg.t0 + j) * kKeyTile;
+            for (int j = j0; j < nt; j += dj) {
+                const int key0 = (t0 + j) * kKeyTile;
                 wait(bar(&m->s_full[slot]), s_parity, abort_s);
                 s_parity ^= 1;
                 tc_fence_after();
                 if (warp_live) {
-                    uint32_t pk[64];
-                    float sum = 0.f, top = -INFINITY;
-                    const bool masked = key0 + kKeyTile - 1 > warp_min;
-                    const int lim = last_key - key0;   // columns 0 .. lim are seen
-                    auto masked_load = [&](int c, uint32_t (&s)[32]) {
-                        tmem_ld32(tS + c * 32, s);
+                    uint32_t sc[128];
+                    auto f = [&](int i) { return __uint_as_float(sc[i]); };
+                    auto tile_top = [&]() {
+                        float tops[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float a = max3(f(c * 32), f(c * 32 + 1), f(c * 32 + 2));
+#pragma unroll
+                            for (int i = 3; i < 31; i += 2) a = max3(a, f(c * 32 + i), f(c * 32 + i + 1));
+                            tops[c] = fmaxf(a, f(c * 32 + 31));
+                        }
+                        return fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * p.scale_log2;
+                    };
+                    const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
+                    float2 neg2, part[2];
+                    uint32_t pk[32];
+                    auto exponentials = [&](int half) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const int at = half * 64 + 2 * i;
+                            const float2 x = __ffma2_rn(make_float2(f(at), f(at + 1)), sc2, neg2);
+                            const float2 e = (i & 7) < kPolyOf8 ? exp2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
+                            part[i & 1] = __fadd2_rn(part[i & 1], e);
+                            const __nv_bfloat162 hh = __floats2bfloat162_rn(e.x, e.y);
+                            pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
+                        }
+                    };
+                    bool first = !any;
+                    while (true) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[c * 32]));
                         tmem_wait_ld();
-                        if (masked) {
+                        if (key0 + kKeyTile - 1 > warp_min) {
+                            const int lim = last_key - key0;   // columns 0 .. lim are seen
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (c * 32 + i > lim) s[i] = kNegInf;
+                            for (int i = 0; i < 128; ++i)
+                                if (i > lim) sc[i] = kNegInf;
                         }
-                    };
-                    auto maxima = [&](const uint32_t (&s)[32]) {
-                        auto f = [&](int i) { return __uint_as_float(s[i]); };
-                        float a = max3(f(0), f(1), f(2)), b = max3(f(3), f(4), f(5));
-#pragma unroll
-                        for (int i = 6; i < 30; i += 4) {
-                            a = max3(a, f(i), f(i + 1));
-                            b = max3(b, f(i + 2), f(i + 3));
-                        }
-                        top = max3(top, max3(a, f(30), f(31)), b);
-                    };
-                    auto exponentials = [&]() {
+                        if (first) mx = tile_top();   // (-inf where the row sees none of these keys)
+                        first = false;
                         const float neg = mx == -INFINITY ? 0.f : -mx;
-                        const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), neg2 = make_float2(neg, neg);
-                        float2 part = make_float2(0.f, 0.f);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t s[32];
-                            masked_load(c, s);
-                            maxima(s);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc2, neg2);
-                                const float2 e = make_float2(ex2(x.x), ex2(x.y));
-                                part = __fadd2_rn(part, e);
-                                const __nv_bfloat162 hh = __floats2bfloat162_rn(e.x, e.y);
-                                pk[c * 16 + i] = *reinterpret_cast<const uint32_t *>(&hh);
-                            }
-                        }
-                        sum = part.x + part.y;
-                    };
-                    bool raise;
-                    if (!any) {
+                        neg2 = make_float2(neg, neg);
+                        part[0] = part[1] = make_float2(0.f, 0.f);
+                        exponentials(0);
+                        const float top = tile_top();
+                        if (!__any_sync(0xffffffffu, top > mx + kRaiseMaxBy)) break;
+                        const float up = fmaxf(mx, top);
+                        const float alpha = up == -INFINITY ? 1.f : ex2(mx - up);
+                        mx = up;
+                        l *= alpha;
+                        // (the scores of this tile are complete, hence the value product before them is)
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t s[32];
-                            masked_load(c, s);
-                            maxima(s);
+                        for (int c = 0; any && c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st16(tO + c, o);
                         }
-                        mx = top * p.scale_log2;   // (-inf where the row sees none of these keys)
-                        exponentials();
-                    } else {
-                        exponentials();
-                        raise = __any_sync(0xffffffffu, top * p.scale_log2 > mx + kRaiseMaxBy);
-                        if (raise) {
-                            const float up = fmaxf(mx, top * p.scale_log2);
-                            const float alpha = up == -INFINITY ? 1.f : ex2(mx - up);
-                            mx = up;
-                            l *= alpha;
-                            exponentials();
-                            // (the scores of this tile are complete, hence the value product before them is)
-#pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t o[32];
-                                tmem_ld32(tO + c, o);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tmem_st32(tO + c, o);
-                            }
-                            tmem_wait_st();
-                        }
+                        tmem_wait_st();
                     }
-                    l += sum;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t half[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) half[i] = pk[c * 32 + i];
-                        tmem_st32(tS + c * 32, half);
-                    }
+                    tmem_st32(tS, pk);
                     tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar(&m->p_full[slot][0]));
+                    exponentials(1);
+                    tmem_st32(tS + 32, pk);
+                    l += (part[0].x + part[1].x) + (part[0].y + part[1].y);
+                    tmem_wait_st();
+                } else {
+                    tc_fence_before();
+                    mbar_arrive(bar(&m->p_full[slot][0]));
                 }
                 any = true;
                 tc_fence_before();
-                mbar_arrive(bar(&m->p_full[slot]));
+                mbar_arrive(bar(&m->p_full[slot][1]));
             }
             // ---- segment epilogue
             if (any) {
@@ -663,13 +736,14 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             const bool poisoned = *(volatile int32_t *)&m->poison[seg % kPoisonRing] != 0;
             const bool two = narrow && sg.nt > 1;   // slot 1 has an output to add
             if (warp_live) {
-                const int token = sg.first_token + unit_token;
-                const size_t out_row = ((size_t)(sg.start + (live ? token : 0)) * p.Hq + (size_t)sg.h * p.G + row_member) * D;
-                const float inv = 1.f / l_all;
-                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128 + row) * D;
-#pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t o[32];
+                const float inv = sg.full ? 1.f / l_all : 1.f;
+                const uint32_t staging = base + C::kOffStaging + warp * 4096;   // 32 rows of 128 bytes, 16-byte pieces swizzled
+                // where this lane's row goes, in rows from the unit's first; -1: nowhere
+                const int to = !live ? -1 : sg.full ? unit_token * p.Hq + row_member : row;
+                __nv_bfloat16 *out = p.out + (((size_t)sg.start + sg.first_token) * p.Hq + (size_t)sg.h * p.G) * D;
+                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128) * D;
+                uint32_t o[32];
+                auto load = [&](int c) {
                     tmem_ld32(tO + c, o);
                     tmem_wait_ld();
                     if (two) {
@@ -695,9 +769,29 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             }
                         }
                     }
-                    if (live) {
-                        if (sg.full) {
-                            uint4 *dst = reinterpret_cast<uint4 *>(p.out + out_row + c);
+                };
+                auto put = [&](int piece, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((piece ^ (lane & 7)) << 4)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+                };
+                // eight lanes write a row's 128 bytes, a warp four rows at a time
+                auto drain = [&](auto *first_row, int c) {
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = i * 4 + (lane >> 3), piece = lane & 7;
+                        const int dst = __shfl_sync(0xffffffffu, to, r);
+                        uint4 y;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(staging + r * 128 + ((piece ^ (r & 7)) << 4)));
+                        if (dst >= 0) reinterpret_cast<uint4 *>(first_row + (size_t)dst * D + c)[piece] = y;
+                    }
+                    __syncwarp();
+                };
+                if (sg.full) {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 64) {
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            load(c + half * 32);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 uint32_t y[4];
@@ -706,20 +800,25 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                                     const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
                                     y[e] = *reinterpret_cast<const uint32_t *>(&hh);
                                 }
-                                dst[i] = make_uint4(y[0], y[1], y[2], y[3]);
+                                put(half * 4 + i, y[0], y[1], y[2], y[3]);
                             }
-                        } else {
-                            uint4 *dst = reinterpret_cast<uint4 *>(part_o + c);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                         }
+                        drain(out, c);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        load(c);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) put(i, o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        drain(part_o, c);
                     }
                 }
                 if (live) {
                     if (!sg.full)
                         *reinterpret_cast<float2 *>(p.partial_ml + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128 + row) * 2) = make_float2(m_all, l_all);
                     else if (p.lse)
-                        p.lse[out_row / D] = (m_all + log2f(l_all)) * 0.6931471805599453f;
+                        p.lse[((size_t)sg.start + sg.first_token + unit_token) * p.Hq + (size_t)sg.h * p.G + row_member] = (m_all + log2f(l_all)) * 0.6931471805599453f;
                 }
             }
             if (narrow) {
