@@ -165,27 +165,15 @@ def _dev(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
 
 
 def _stream() -> c_void_p:
-    return c_void_p(torch.cuda.current_stream().cuda_stream)
+    return c_void_p(_raw_stream())
 
 
-def _rows(t: torch.Tensor, name: str, shape) -> int:
-    """Checks a bf16 tensor [..., heads, head_dim] whose heads are dense and whose tokens are evenly spaced (a tensor of its
-    own or a part of a fused projection's output) and returns the token stride in elements."""
-    if not (t.is_cuda and t.dtype == torch.bfloat16):
-        raise TypeError(f"{name}: need a CUDA tensor of dtype {torch.bfloat16}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: need shape {tuple(shape)}, got {tuple(t.shape)}")
-    heads, d = shape[-2:]
-    if t.numel() == 0:
-        return heads * d
-    if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != d):
-        raise ValueError(f"{name}: the heads of a token must be dense")
-    if len(shape) == 4:
-        b, n = shape[:2]
-        if b > 1 and n > 1 and t.stride(0) != n * t.stride(1):
-            raise ValueError(f"{name}: the tokens must be evenly spaced")
-        return t.stride(1) if n > 1 else t.stride(0) if b > 1 else heads * d
-    return t.stride(0) if shape[0] > 1 else heads * d
+def _raw_stream() -> int:
+    """The handle of the current device's current stream."""
+    try:   # what torch.cuda.current_stream() wraps, without the 3 us that building its Stream object takes
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
 
 
 @dataclass
@@ -574,32 +562,89 @@ class Reader:
         return slots, status
 
     # ---- from a prompt to a cache, from a projection to a tree
-    def _here(self, *tensors: Optional[torch.Tensor]) -> None:
-        for t in tensors:
-            if t is not None and t.device.index != self.device:
-                raise ValueError(f"a tensor is on {t.device}, this reader on cuda:{self.device}")
+    # (These calls may be as short as a few microseconds on the GPU: the checks below are one pass over each argument and
+    # tensors travel as plain addresses.)
+    def _have(self, t: torch.Tensor, dtype, name: str) -> int:
+        """The address of a contiguous tensor of that dtype on this reader's device."""
+        if t.get_device() != self.device:
+            if not t.is_cuda:
+                raise TypeError(f"{name}: need a contiguous CUDA tensor of dtype {dtype}")
+            raise ValueError(f"{name} is on {t.device}, this reader on cuda:{self.device}")
+        if t.dtype is not dtype or not t.is_contiguous():
+            raise TypeError(f"{name}: need a contiguous CUDA tensor of dtype {dtype}")
+        return t.data_ptr()
+
+    def _heads(self, t: torch.Tensor, shape, name: str):
+        """Address and token stride of a bf16 tensor [..., heads, head_dim] whose heads are dense and whose tokens are evenly
+        spaced: a tensor of its own or a part of a fused projection's output."""
+        if t.get_device() != self.device or t.dtype is not torch.bfloat16:
+            if t.is_cuda and t.dtype is torch.bfloat16:
+                raise ValueError(f"{name} is on {t.device}, this reader on cuda:{self.device}")
+            raise TypeError(f"{name}: need a CUDA tensor of dtype {torch.bfloat16}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: need shape {shape}, got {tuple(t.shape)}")
+        *lead, heads, d = shape
+        stride = t.stride()
+        dense = heads * d
+        if t.numel() == 0:
+            return t.data_ptr(), dense
+        if stride[-1] != 1 or (heads > 1 and stride[-2] != d):
+            raise ValueError(f"{name}: the heads of a token must be dense")
+        if len(lead) == 1:
+            return t.data_ptr(), stride[0] if lead[0] > 1 else dense
+        b, n = lead
+        if b > 1 and n > 1 and stride[0] != n * stride[1]:
+            raise ValueError(f"{name}: the tokens must be evenly spaced")
+        return t.data_ptr(), stride[1] if n > 1 else stride[0] if b > 1 else dense
+
+    def _paged(self, c: KvCache) -> _KvCache:
+        k = c.k_pool
+        pages, heads, page, d = k.shape
+        if c.v_pool.shape != k.shape:
+            raise ValueError("v_pool: the shape of k_pool")
+        batch, width = c.page_table.shape
+        if c.seq_lens.shape[0] != batch:
+            raise ValueError("seq_lens: one length for each row of the page table")
+        return _KvCache(self._have(k, torch.bfloat16, "k_pool"), self._have(c.v_pool, torch.bfloat16, "v_pool"), pages, page, heads, d,
+                        self._have(c.page_table, torch.int32, "page_table"), width, self._have(c.seq_lens, torch.int32, "seq_lens"),
+                        int(c.shared_prefix_len))
 
     def _rotation(self, head_dim: int, rope, q_weight, k_weight, eps: float, interleaved: bool) -> _Rotation:
-        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is not None and _dev(w, torch.bfloat16, name).shape != (head_dim,):
-                raise ValueError(f"{name}: need shape ({head_dim},)")
+        q = k = r = None
         positions = rot = 0
+        if q_weight is not None:
+            q = self._have(q_weight, torch.bfloat16, "q_weight")
+        if k_weight is not None:
+            k = self._have(k_weight, torch.bfloat16, "k_weight")
+        for w in (q_weight, k_weight):
+            if w is not None and w.shape != (head_dim,):
+                raise ValueError(f"q_weight, k_weight: need shape ({head_dim},)")
         if rope is not None:
-            _dev(rope, torch.float32, "rope")
+            r = self._have(rope, torch.float32, "rope")
             if rope.dim() != 3 or rope.shape[1] != 2:
                 raise ValueError("rope: need [max_positions, 2, rot_dim / 2]")
-            positions, rot = rope.shape[0], 2 * rope.shape[2]
-        self._here(rope, q_weight, k_weight)
-        return _Rotation(None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-                         float(eps), None if rope is None else rope.data_ptr(), positions, rot, int(bool(interleaved)))
+            positions, _, half = rope.shape
+            rot = 2 * half
+        return _Rotation(q, k, eps, r, positions, rot, 1 if interleaved else 0)
 
-    def _prompt(self, cache: KvCache, token_start: torch.Tensor, tokens: int) -> _Prompt:
-        _dev(token_start, torch.int32, "token_start")
-        B = cache.page_table.shape[0]
-        if token_start.shape != (B + 1,) or cache.seq_lens.shape != (B,):
-            raise ValueError("token_start: one more entry than the cache has sequences; seq_lens: one for each")
-        self._here(token_start, cache.page_table, cache.k_pool, cache.v_pool, cache.seq_lens)
-        return _Prompt(B, tokens, token_start.data_ptr())
+    def _prompt(self, batch: int, token_start: torch.Tensor, tokens: int) -> _Prompt:
+        if token_start.shape != (batch + 1,):
+            raise ValueError("token_start: one entry more than the cache has sequences")
+        return _Prompt(batch, tokens, self._have(token_start, torch.int32, "token_start"))
+
+    def _status(self, status: Optional[torch.Tensor], like: torch.Tensor, batch: int):
+        if status is None:
+            status = like.new_empty(batch)
+        elif status.shape != (batch,):
+            raise ValueError("status: one word for each sequence")
+        return status, self._have(status, torch.int32, "status")
+
+    def _out(self, out: Optional[torch.Tensor], like: torch.Tensor, name: str):
+        if out is None:
+            out = torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
+        elif out.shape != like.shape:
+            raise ValueError(f"{name}: need shape {tuple(like.shape)}, got {tuple(out.shape)}")
+        return out, self._have(out, torch.bfloat16, name)
 
     def prompt_append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: KvCache, token_start: torch.Tensor,
                       rope: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
@@ -607,19 +652,18 @@ class Reader:
                       out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """Head norms, rotation and cache write of packed new tokens: q [tokens, Hq, D], k and v [tokens, Hkv, D] (views of
         a fused projection are fine), rope f32 [max_positions, 2, rot_dim / 2].  Returns (rotated queries, status)."""
-        c = cache._c()
+        c = self._paged(cache)
         tokens, Hq, D = q.shape
-        qs, ks, vs = _rows(q, "q", q.shape), _rows(k, "k", (tokens, c.n_kv_heads, c.head_dim)), _rows(v, "v", (tokens, c.n_kv_heads, c.head_dim))
         if D != c.head_dim:
             raise ValueError("q: its head dimension is not the cache's")
-        p, r = self._prompt(cache, token_start, tokens), self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
-        out = torch.empty((tokens, Hq, D), dtype=torch.bfloat16, device=q.device) if out is None else _dev(out, torch.bfloat16, "out")
-        status = torch.empty(p.batch, dtype=torch.int32, device=q.device) if status is None else _dev(status, torch.int32, "status")
-        if out.shape != q.shape or status.shape != (p.batch,):
-            raise ValueError("out: the shape of q; status: one word for each sequence")
-        self._here(q, k, v, out, status)
-        st = self.lib.reader_prompt_append(self._h, _ptr(q), _ptr(k), _ptr(v), qs, ks, vs, Hq, ctypes.byref(c), ctypes.byref(p),
-                                           ctypes.byref(r), _ptr(out), _ptr(status), _stream())
+        kv = (tokens, c.n_kv_heads, D)
+        (qp, qs), (kp, ks), (vp, vs) = self._heads(q, (tokens, Hq, D), "q"), self._heads(k, kv, "k"), self._heads(v, kv, "v")
+        batch = cache.page_table.shape[0]
+        p, r = self._prompt(batch, token_start, tokens), self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
+        out, op = self._out(out, q, "out")
+        status, sp = self._status(status, token_start, batch)
+        st = self.lib.reader_prompt_append(self._h, qp, kp, vp, qs, ks, vs, Hq, ctypes.byref(c), ctypes.byref(p), ctypes.byref(r), op, sp,
+                                           _raw_stream())
         if st != OK:
             raise ReaderError(st, "reader_prompt_append")
         return out, status
@@ -631,22 +675,20 @@ class Reader:
                     v_tree: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """The same for draft nodes: q [B, T, Hq, D], k and v [B, T, Hkv, D], parent [B, T].  Returns
         (q, k_tree, v_tree, status) for verify_attn and kv_commit."""
-        _dev(parent, torch.int32, "parent"); _dev(seq_lens, torch.int32, "seq_lens")
         B, T, Hq, D = q.shape
         Hkv = k.shape[2]
-        qs, ks, vs = _rows(q, "q", q.shape), _rows(k, "k", (B, T, Hkv, D)), _rows(v, "v", (B, T, Hkv, D))
+        kv = (B, T, Hkv, D)
+        (qp, qs), (kp, ks), (vp, vs) = self._heads(q, (B, T, Hq, D), "q"), self._heads(k, kv, "k"), self._heads(v, kv, "v")
         if parent.shape != (B, T) or seq_lens.shape != (B,):
             raise ValueError("parent: [B, T]; seq_lens: [B]")
+        tr = _Tree(B, T, self._have(parent, torch.int32, "parent"), None)
         r = self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
-        new = lambda t, heads, name: torch.empty((B, T, heads, D), dtype=torch.bfloat16, device=q.device) if t is None else _dev(t, torch.bfloat16, name)  # noqa: E731
-        out, k_tree, v_tree = new(out, Hq, "out"), new(k_tree, Hkv, "k_tree"), new(v_tree, Hkv, "v_tree")
-        status = torch.empty(B, dtype=torch.int32, device=q.device) if status is None else _dev(status, torch.int32, "status")
-        if out.shape != q.shape or k_tree.shape != k.shape or v_tree.shape != v.shape or status.shape != (B,):
-            raise ValueError("out, k_tree, v_tree: the shapes of q, k, v; status: one word for each sequence")
-        self._here(q, k, v, out, k_tree, v_tree, status, parent, seq_lens)
-        tr = _Tree(B, T, parent.data_ptr(), None)
-        st = self.lib.reader_tree_rotate(self._h, _ptr(q), _ptr(k), _ptr(v), qs, ks, vs, Hq, Hkv, D, ctypes.byref(tr), _ptr(seq_lens),
-                                         ctypes.byref(r), _ptr(out), _ptr(k_tree), _ptr(v_tree), _ptr(status), _stream())
+        out, op = self._out(out, q, "out")
+        k_tree, ko = self._out(k_tree, k, "k_tree")
+        v_tree, vo = self._out(v_tree, v, "v_tree")
+        status, sp = self._status(status, parent, B)
+        st = self.lib.reader_tree_rotate(self._h, qp, kp, vp, qs, ks, vs, Hq, Hkv, D, ctypes.byref(tr), self._have(seq_lens, torch.int32, "seq_lens"),
+                                         ctypes.byref(r), op, ko, vo, sp, _raw_stream())
         if st != OK:
             raise ReaderError(st, "reader_tree_rotate")
         return out, k_tree, v_tree, status
@@ -663,22 +705,23 @@ class Reader:
                     workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """Causal attention of packed new tokens, whose K and V are in the cache at seq_lens[b] + i, over the cache:
         q [tokens, Hq, D].  Returns (out, status); lse f32 [tokens, Hq] is filled if given."""
-        c = cache._c()
-        _dev(q, torch.bfloat16, "q")
+        c = self._paged(cache)
         tokens, Hq, D = q.shape
         if D != c.head_dim:
             raise ValueError("q: its head dimension is not the cache's")
-        p = self._prompt(cache, token_start, tokens)
-        out = torch.empty_like(q) if out is None else _dev(out, torch.bfloat16, "out")
-        status = torch.empty(p.batch, dtype=torch.int32, device=q.device) if status is None else _dev(status, torch.int32, "status")
-        if out.shape != q.shape or status.shape != (p.batch,):
-            raise ValueError("out: the shape of q; status: one word for each sequence")
-        if lse is not None and _dev(lse, torch.float32, "lse").shape != (tokens, Hq):
-            raise ValueError("lse: [tokens, Hq]")
-        ws = self.prompt_workspace() if workspace is None else _dev(workspace, torch.uint8, "workspace")
-        self._here(q, out, lse, status, ws)
-        st = self.lib.reader_prompt_attn(self._h, _ptr(q), Hq, ctypes.byref(c), ctypes.byref(p), float(scale), int(bool(update_seq_lens)),
-                                         _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _ptr(status), _stream())
+        batch = cache.page_table.shape[0]
+        p = self._prompt(batch, token_start, tokens)
+        qp = self._have(q, torch.bfloat16, "q")
+        out, op = self._out(out, q, "out")
+        status, sp = self._status(status, token_start, batch)
+        lp = None
+        if lse is not None:
+            lp = self._have(lse, torch.float32, "lse")
+            if lse.shape != (tokens, Hq):
+                raise ValueError("lse: [tokens, Hq]")
+        ws = self.prompt_workspace() if workspace is None else workspace
+        st = self.lib.reader_prompt_attn(self._h, qp, Hq, ctypes.byref(c), ctypes.byref(p), scale, 1 if update_seq_lens else 0, op, lp,
+                                         self._have(ws, torch.uint8, "workspace"), ws.numel(), sp, _raw_stream())
         if st != OK:
             raise ReaderError(st, "reader_prompt_attn")
         return out, status
