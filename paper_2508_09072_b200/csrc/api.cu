@@ -654,7 +654,7 @@ reader_status check_prompt(const reader_kv_cache *c, const reader_prompt *t, con
 }
 
 struct PromptWs {
-    size_t partial_o, partial_ml, pieces, gave_up, total;
+    size_t partial_o, partial_ml, pieces, gave_up, counter, total;
 };
 PromptWs prompt_ws(const reader_ctx *ctx, int D) {
     PromptWs w{};
@@ -665,6 +665,7 @@ PromptWs prompt_ws(const reader_ctx *ctx, int D) {
     w.partial_ml = take(sizeof(float) * rows * 2);
     w.pieces = take(sizeof(PieceDesc) * (size_t)ctx->n_sm);
     w.gave_up = take(sizeof(int32_t) * (size_t)ctx->n_sm);
+    w.counter = take(sizeof(int32_t));
     w.total = at;
     return w;
 }
@@ -772,9 +773,24 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
     p.gave_up = reinterpret_cast<int32_t *>(ws + w.gave_up);
     cudaStream_t st = (cudaStream_t)stream;
     if (tokens > 0) {
-        p.n_ctas = ctx->n_sm;
+        // entries of the list, going by the page table's width; no CTA without work
+        const int64_t max_tiles = ((int64_t)cache->max_pages_per_seq + 1) / 2;
+        const int64_t ctas = prompt_busy_ctas(ctx->n_sm, (int)(units * (max_tiles + kUnitEntries)));
+        p.n_ctas = (int)ctas;
+        const int64_t steps = tokens <= B ? (max_tiles + 1) / 2 : max_tiles;
+        p.alone = !update_seq_lens && units <= ctx->n_sm && steps <= kAloneSteps && steps * (ctx->n_sm - units) <= (int64_t)kAloneIdle * ctx->n_sm;
+        if (p.alone) p.n_ctas = (int)units;
+        // Whole units from a counter when there are enough of them that the last ones to end do not matter.
+        if ((int64_t)tokens / (2 * p.tile_tokens) * Hkv >= (int64_t)kDynamicUnits * ctx->n_sm) {
+            p.counter = reinterpret_cast<int32_t *>(ws + w.counter);
+            if (cudaMemsetAsync(p.counter, 0, sizeof(int32_t), st) != cudaSuccess) {
+                cudaGetLastError();
+                return READER_ERR_CUDA;
+            }
+        }
         if (reader_status s = launch_prompt_attn(&ctx->prompt, ctx->sm100.encode_tiled, p, static_cast<const __nv_bfloat16 *>(q), cache->k_pool, cache->v_pool, st))
             return s;
+        if (p.alone) return launch_status();
     }
     launch_prompt_finish(p, st);
     return launch_status();

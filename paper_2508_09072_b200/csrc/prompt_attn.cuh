@@ -12,10 +12,20 @@ constexpr int kKeyTile = 128;            // keys per tile: two cache pages
 //   wide unit    both tiles have rows: a step is one key tile, multiplied with both query tiles
 //   narrow unit  only the first tile has rows (the last block of a sequence, every block of a single-token call):
 //                a step is two key tiles, each multiplied with the one query tile, merged at the unit's end
-// Units in the order (sequence, KV head, block), each kUnitEntries entries (what starting and ending a unit costs)
-// followed by its steps, form one list that is cut into contiguous equal ranges, one per CTA.
+// A call with many units hands them out whole, from a counter.  Otherwise the units in the order (sequence, KV head,
+// block), each kUnitEntries entries (what starting and ending a unit costs) followed by its steps, form one list that is
+// cut into contiguous equal ranges, one per CTA.
 constexpr int kUnitEntries = 2;
 constexpr int kMinEntriesPerCta = 4;
+// A call is a single launch when its units fit the CTAs and cutting them would not pay for the merge and the second launch
+// (6 to 9 us): going by the page table's width, at most kAloneSteps steps to a unit (lengths may differ, and the longest
+// one decides), and at most kAloneIdle steps that a CTA would gain on average from the CTAs without a unit.  Measured, alone
+// against cut: one token on 1000, 1500, 2000 keys, 8 units: 15.9 / 21.3, 20.0 / 19.8, 24.1 / 20.4 us; 16 tokens on 1500
+// keys each, 128 units: 24.8 / 34.6 us; a prompt of 1500 tokens in 24 units: 35.0 / 30.4 us, of 1000 in 128: 24.5 / 34.2 us.
+constexpr int kAloneSteps = 12, kAloneIdle = 6;
+// Units per CTA from which a call hands them out from a counter (a prompt of 4096 tokens, 3.5 units per CTA: 158 us, cut into
+// equal ranges 167 us; 16 prompts, 16 units per CTA: 314 and 340 us).
+constexpr int kDynamicUnits = 3;
 
 struct PieceDesc {        // a unit that CTA c starts but does not finish: pieces 2c + 1, then 2(c + 1), 2(c + 2), ...
     int32_t b, h, block;  // b = -1: none
@@ -34,6 +44,8 @@ struct PromptAttnParams {
     int32_t *status;
     int32_t *bump;                // seq_lens again when it is to be advanced, else null
     int n_ctas;
+    int32_t *counter;             // next unit to hand out, zero at the start; null: the units are dealt out beforehand
+    bool alone;                   // at most one unit per CTA, each done whole, and no finishing kernel behind
     // workspace
     float *partial_o;             // [2 n_ctas][256][D]
     float *partial_ml;            // [2 n_ctas][256][2]

@@ -30,6 +30,10 @@
 // Output rows leave through shared memory, 4 KB a warp: a warp's store then fills whole 128-byte lines.  (Straight from the
 // thread = row layout, 16 bytes of 32 lines at a time, a segment's epilogue took 5500 to 9400 cycles.)
 //
+// A call with no more units than CTAs, all of them short, is this one launch (the single-launch form): a unit's CTA looks
+// at its sequence's pages itself, writes zero rows if one is bad, and the status word if the unit is the sequence's first.
+// Other calls are followed by the finishing kernel below.
+//
 // Every wait is bounded: a CTA that waits a second without progress marks its word in the workspace, stops waiting
 // and runs to its end; the finishing kernel turns the mark into status words and zero rows.
 #include <cuda.h>
@@ -50,14 +54,9 @@ constexpr int kRegsSoftmax = 208, kRegsOther = 88;
 constexpr int kProducerWarp = 8, kMmaWarp = 9, kValueWarp = 10;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kRaiseMaxBy = 8.f;   // log2 units
-#ifndef POLY
-#define POLY 2
-#endif
-constexpr int kPolyOf8 = POLY;      // of eight pairs of exponentials, how many are computed on the FMA pipe
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 constexpr int kMaxStages = 8;
-constexpr int kPoisonRing = 8;       // segments the value warp may be ahead of an epilogue (the ring holds 4 value tiles)
-
+constexpr int kRotateTiles = 64;     // shortest unit that is begun in the middle
 constexpr int kMiscBytes = 3072;
 
 template <int D>
@@ -92,90 +91,218 @@ struct Piece {
     int start;               // first row of the sequence in the packed tensors
     int L, n;
     UnitShape u;
-    int t0, nt;              // key tiles of this piece
+    int t0, nt, rot;         // key tiles of this piece: t0 + (rot + j) % nt, j = 0 .. nt-1; nt = 0: no more work
     bool full;               // the whole unit
     int slot;                // where its partial goes
     int first_token;         // of the unit, within the sequence
+    int32_t poison;          // infinities or NaN were taken out of its value tiles
+    bool reject;             // (single-launch form) a page id of the sequence is outside the pool: zero rows
+    __device__ __forceinline__ int tile(int j) const { return t0 + (j + rot < nt ? j + rot : j + rot - nt); }
 };
 
-// Where a warp stands in its CTA's range.
-struct Walk {
-    int b, h, block, off, left, w;
-    int start, L, n, blocks;
-    __device__ __forceinline__ void open(const PromptAttnParams &p) {
-        start = p.token_start[b];
-        n = p.token_start[b + 1] - start;
-        L = p.seq_lens[b];
-        blocks = prompt_len_ok(L, n, p.max_pages) ? unit_blocks(n, p.tile_tokens) : 0;
-    }
-};
+constexpr int kPieces = 4;          // pieces in flight between the producer and the other warps
+constexpr int kConsumers = 11;      // those
 
 struct Misc {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t raw[kMaxStages];  // a value tile that the value warp goes over first has landed; that warp then completes `full`
     uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2], turn[2], merge_ready, merge_free;
+    uint64_t piece_full[kPieces], piece_empty[kPieces];
     float2 ml[128];            // slot 1's row maxima and sums of a narrow unit
-    int32_t poison[kPoisonRing];
-    int32_t seq, head, block, off, w_begin, w_end, W, ctas;
+    Piece piece[kPieces];
     uint32_t tmem_base;
     int32_t abort;
-    Walk walk[12];             // one per warp: every role walks the range for itself, and has its registers for other things
-    Piece piece[12];
 };
 static_assert(sizeof(Misc) <= kMiscBytes, "shared memory behind the staging");
 
-__device__ __forceinline__ void walk_init(const PromptAttnParams &p, Misc *m, int warp, int lane) {
-    Walk w;
-    w.b = m->seq; w.h = m->head; w.block = m->block; w.off = m->off; w.w = m->w_begin; w.left = m->w_end - m->w_begin;
-    w.start = w.L = w.n = w.blocks = 0;
-    if (w.left > 0) w.open(p);
-    if (lane == 0) m->walk[warp] = w;
-    __syncwarp();
+__device__ __forceinline__ int inclusive_sum(int x, int lane) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += up;
+    }
+    return x;
 }
 
-// The warp's next segment with at least one key tile, in m->piece[warp]; false at the end of the range.
-__device__ __forceinline__ bool walk_next(const PromptAttnParams &p, Misc *m, int warp, int lane) {
-    __syncwarp();
-    Walk w = m->walk[warp];
-    Piece s;
-    s.nt = 0;
-    while (w.left > 0 && s.nt <= 0) {
-        while (w.block >= w.blocks) {   // on to the next head, the next sequence with tokens
-            w.block = 0;
-            if (w.blocks == 0 || ++w.h == p.Hkv) {
-                w.h = 0;
-                if (++w.b >= p.B) break;
-                w.open(p);
+// Where a CTA's work comes from; one warp (the producer) asks, all its lanes together.
+//   static (few units): the CTA's equal range of the unit list.  Pieces of a unit that is cut take its steps from the last
+//     to the first, and a long unit is begun at the tile that the CTA's clock points to: CTAs that work on the same KV
+//     head then ask for the same key tiles at about the same time, whatever part of the list they have, and a history
+//     larger than the L2 cache is not fetched from HBM by each of them (2 x 32768 cached tokens: 2.95 GB without).
+//   dynamic (many units): whole units from a counter, in the order (sequence, block from the last to the first, KV head):
+//     the longest come first, the heads of one or two sequences fit the L2 cache.
+//   alone (no more units than CTAs, all of them short): CTA i has unit i and nothing follows the kernel, see below.
+struct Schedule {
+    int w, left, w0, W, ctas;                    // static: place in the list, entries to go, where the range began
+    int b, h, block, off, start, L, n, blocks;   // the current sequence, and the place in its unit
+    int first;                                   // dynamic: units before sequence b
+
+    __device__ __forceinline__ int blocks_of(const PromptAttnParams &p, int seq, int &n_, int &L_) const {
+        n_ = p.token_start[seq + 1] - p.token_start[seq];
+        L_ = p.seq_lens[seq];
+        return prompt_len_ok(L_, n_, p.max_pages) ? unit_blocks(n_, p.tile_tokens) : 0;
+    }
+    __device__ __forceinline__ void open(const PromptAttnParams &p) {
+        start = p.token_start[b];
+        blocks = blocks_of(p, b, n, L);
+    }
+    // sizes: scratch in shared memory, [B]
+    __device__ __forceinline__ void init(const PromptAttnParams &p, int32_t *sizes, int lane) {
+        bool bad = false;
+        for (int i = lane; i < p.B; i += 32) {
+            const int a = p.token_start[i], e = p.token_start[i + 1];
+            bad |= a < 0 || a > e || e > p.tokens;
+        }
+        w = left = w0 = W = ctas = b = h = block = off = start = L = n = blocks = first = 0;
+        if (__any_sync(0xffffffffu, bad)) {   // whose rows are whose is not known: no work
+            b = p.B;
+            return;
+        }
+        if (p.counter || p.alone) return;
+        int total = 0;   // entries of one head of every sequence so far
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            int n_ = 0, L_ = 0, m = 0, sum = 0;
+            if (b0 + lane < p.B) m = blocks_of(p, b0 + lane, n_, L_);
+            // few blocks: each lane adds up its own sequence; many: the warp one sequence after the other
+            for (int i = 0; m <= 4 && i < m; ++i) sum += kUnitEntries + unit_shape(L_, n_, i, p.tile_tokens).steps;
+            for (unsigned long_ones = __ballot_sync(0xffffffffu, m > 4); long_ones; long_ones &= long_ones - 1) {
+                const int src = __ffs(long_ones) - 1;
+                const int ns = __shfl_sync(0xffffffffu, n_, src), Ls = __shfl_sync(0xffffffffu, L_, src), ms = __shfl_sync(0xffffffffu, m, src);
+                int part = 0;
+                for (int i = lane; i < ms; i += 32) part += kUnitEntries + unit_shape(Ls, ns, i, p.tile_tokens).steps;
+                part = __reduce_add_sync(0xffffffffu, part);
+                if (lane == src) sum = part;
             }
+            const int incl = inclusive_sum(sum, lane);
+            if (b0 + lane < p.B) sizes[b0 + lane] = total + incl - sum;
+            total += __shfl_sync(0xffffffffu, incl, 31);
         }
-        if (w.b >= p.B) {
-            w.left = 0;
-            break;
+        __syncwarp();
+        W = total * p.Hkv;
+        ctas = prompt_busy_ctas(p.n_ctas, W);
+        const int c = blockIdx.x;
+        if (c >= ctas) return;
+        w0 = w = prompt_range_begin(c, W, ctas);
+        left = prompt_range_begin(c + 1, W, ctas) - w;
+        if (left <= 0) return;
+        int lo = 0, hi = p.B;   // the last sequence that begins at or before this CTA's first entry
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (sizes[mid] * p.Hkv <= w) lo = mid; else hi = mid;
         }
-        s.u = unit_shape(w.L, w.n, w.block, p.tile_tokens);
-        const int entries = kUnitEntries + s.u.steps;
-        const int take = min(entries - w.off, w.left);
-        const int s0 = max(0, w.off - kUnitEntries), s1 = w.off + take - kUnitEntries;
-        s.b = w.b; s.h = w.h; s.block = w.block;
-        s.start = w.start; s.L = w.L; s.n = w.n;
-        s.first_token = w.block * 2 * p.tile_tokens;
-        s.t0 = s.u.narrow ? 2 * s0 : s0;
-        s.nt = s1 <= s0 ? 0 : (s.u.narrow ? min(2 * s1, s.u.tiles) : s1) - s.t0;
-        s.full = s0 == 0 && s1 == s.u.steps;
-        s.slot = s0 == 0 ? 1 : 0;
-        w.w += take;
-        w.left -= take;
-        w.off += take;
-        if (w.off == entries) { w.off = 0; ++w.block; }
+        b = lo;
+        const int size = (b + 1 < p.B ? sizes[b + 1] : total) - sizes[b], within = w - sizes[b] * p.Hkv;
+        h = within / size;
+        off = within - h * size;
+        open(p);
+        for (int i0 = 0; i0 < blocks; i0 += 32) {
+            const int mine = i0 + lane < blocks ? kUnitEntries + unit_shape(L, n, i0 + lane, p.tile_tokens).steps : 0;
+            const int incl = inclusive_sum(mine, lane);
+            const unsigned here = __ballot_sync(0xffffffffu, off < incl);
+            if (here) {
+                const int src = __ffs(here) - 1;
+                block = i0 + src;
+                off -= __shfl_sync(0xffffffffu, incl - mine, src);
+                break;
+            }
+            off -= __shfl_sync(0xffffffffu, incl, 31);
+        }
     }
-    __syncwarp();
-    if (lane == 0) {
-        m->walk[warp] = w;
-        m->piece[warp] = s;
+    __device__ __forceinline__ void describe(const PromptAttnParams &p, Piece &s) const {
+        s.b = b; s.h = h; s.block = block;
+        s.start = start; s.L = L; s.n = n;
+        s.u = unit_shape(L, n, block, p.tile_tokens);
+        s.first_token = block * 2 * p.tile_tokens;
+        s.rot = 0;
+        s.poison = 0;
+        s.reject = false;
     }
-    __syncwarp();
-    return s.nt > 0;
-}
+    // The next piece with at least one key tile; false when there is no more.
+    __device__ __forceinline__ bool next(const PromptAttnParams &p, Piece &s, int lane) {
+        s.nt = 0;
+        if (p.counter || p.alone) {
+            if (b >= p.B) return false;
+            int i = blockIdx.x;
+            if (p.alone) {
+                if (w++ > 0) return false;
+            } else {
+                if (lane == 0) i = atomicAdd(p.counter, 1);
+                i = __shfl_sync(0xffffffffu, i, 0);
+            }
+            while (true) {
+                int n_ = 0, L_ = 0, m = 0;
+                if (b + lane < p.B) m = blocks_of(p, b + lane, n_, L_) * p.Hkv;
+                const int incl = inclusive_sum(m, lane);
+                const unsigned here = __ballot_sync(0xffffffffu, i - first < incl);
+                if (here) {
+                    const int src = __ffs(here) - 1;
+                    b += src;
+                    first += __shfl_sync(0xffffffffu, incl - m, src);
+                    break;
+                }
+                b += 32;
+                first += __shfl_sync(0xffffffffu, incl, 31);
+                if (b >= p.B) return false;
+            }
+            open(p);
+            block = blocks - 1 - (i - first) / p.Hkv;
+            h = (i - first) % p.Hkv;
+            describe(p, s);
+            s.t0 = 0;
+            s.nt = s.u.tiles;
+            s.full = true;
+            s.slot = 0;
+            if (p.alone) {
+                bool bad = false;
+                for (int k = lane; k < (L + n + kPage - 1) / kPage; k += 32) {
+                    const int pg = p.page_table[(size_t)b * p.max_pages + k];
+                    bad |= pg < 0 || pg >= p.num_pages;
+                }
+                s.reject = __any_sync(0xffffffffu, bad);
+                if (h == 0 && block == 0 && lane == 0) p.status[b] = s.reject ? READER_ERR_BAD_PAGE : READER_OK;
+            }
+            return true;
+        }
+        while (left > 0) {
+            while (block >= blocks) {   // on to the next head, the next sequence with tokens
+                block = 0;
+                if (blocks == 0 || ++h == p.Hkv) {
+                    h = 0;
+                    if (++b >= p.B) {
+                        left = 0;
+                        return false;
+                    }
+                    open(p);
+                }
+            }
+            describe(p, s);
+            const int entries = kUnitEntries + s.u.steps, take = min(entries - off, left);
+            const int s0 = max(0, off - kUnitEntries), s1 = off + take - kUnitEntries;
+            const int per = s.u.narrow ? 2 : 1;   // tiles a step
+            if (s1 > s0) {
+                s.t0 = max(0, s.u.tiles - per * s1);
+                s.nt = s.u.tiles - per * s0 - s.t0;
+            }
+            s.full = s0 == 0 && s1 == s.u.steps;
+            s.slot = s0 == 0 ? 1 : 0;
+            if (s.full && s.nt >= kRotateTiles) s.rot = per * (w - w0) % s.nt;
+            w += take;
+            left -= take;
+            off += take;
+            const int rest = s.u.steps - s1;   // of the unit, with the CTAs that follow
+            if (s.nt > 0 && !s.full && s.slot == 1 && lane == 0) {
+                PieceDesc d;
+                d.b = b; d.h = h; d.block = block;
+                d.more = prompt_range_owner(w + rest - 1, W, ctas) - (int)blockIdx.x;
+                d.first_token = start; d.tokens = n; d.L = L;
+                p.pieces[blockIdx.x] = d;
+            }
+            if (off == entries) { off = 0; ++block; }
+            if (s.nt > 0) return true;
+        }
+        return false;
+    }
+};
 
 // Ring places of a segment's tiles.  Order: the first `ahead` key tiles, then V0, K(ahead), V1, K(ahead + 1), ...
 __device__ __forceinline__ int ahead_of(const Piece &s) { return min(s.u.narrow ? 2 : 1, s.nt); }
@@ -185,88 +312,12 @@ __device__ __forceinline__ int place_of_v(int j, int ahead, int nt) { return ahe
 // Whether key tile t holds keys of the unit's own tokens (or none): its values go through the value warp.
 __device__ __forceinline__ bool has_own_keys(const Piece &s, int t) { return (t + 1) * kKeyTile > s.L + s.first_token; }
 
-// Works out the whole call's partition and this CTA's place in it (all threads; ends with a barrier).
-__device__ void partition(const PromptAttnParams &p, Misc *m, int32_t *sizes /* shared, [B] */) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    bool bad = false;
-    for (int b = tid; b < p.B; b += kThreads) {
-        const int a = p.token_start[b], e = p.token_start[b + 1];
-        bad |= a < 0 || a > e || e > p.tokens;
-    }
-    const bool none = __syncthreads_or(bad);
-    for (int b = warp; b < p.B; b += kThreads / 32) {
-        const int n = p.token_start[b + 1] - p.token_start[b], L = p.seq_lens[b];
-        int sum = 0;
-        if (!none && prompt_len_ok(L, n, p.max_pages)) {
-            const int blocks = unit_blocks(n, p.tile_tokens);
-            for (int i = lane; i < blocks; i += 32) sum += kUnitEntries + unit_shape(L, n, i, p.tile_tokens).steps;
-            sum = __reduce_add_sync(0xffffffffu, sum);
-        }
-        if (lane == 0) sizes[b] = sum;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        int total = 0;   // entries of one head of every sequence so far
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const int mine = b0 + lane < p.B ? sizes[b0 + lane] : 0;
-            int incl = mine;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int up = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += up;
-            }
-            if (b0 + lane < p.B) sizes[b0 + lane] = total + incl - mine;
-            total += __shfl_sync(0xffffffffu, incl, 31);
-        }
-        __syncwarp();
-        const int W = total * p.Hkv, ctas = prompt_busy_ctas(p.n_ctas, W), c = blockIdx.x;
-        const int begin = c < ctas ? prompt_range_begin(c, W, ctas) : W, end = c < ctas ? prompt_range_begin(c + 1, W, ctas) : W;
-        int b = 0, h = 0, block = 0, off = 0;
-        if (begin < end) {
-            int lo = 0, hi = p.B;   // the last sequence that begins at or before this CTA's first entry
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (sizes[mid] * p.Hkv <= begin) lo = mid; else hi = mid;
-            }
-            b = lo;
-            const int size = (b + 1 < p.B ? sizes[b + 1] : total) - sizes[b];
-            const int within = begin - sizes[b] * p.Hkv;
-            h = within / size;
-            off = within - h * size;
-            const int n = p.token_start[b + 1] - p.token_start[b], L = p.seq_lens[b];
-            const int blocks = unit_blocks(n, p.tile_tokens);
-            for (int i0 = 0; i0 < blocks; i0 += 32) {
-                const int mine = i0 + lane < blocks ? kUnitEntries + unit_shape(L, n, i0 + lane, p.tile_tokens).steps : 0;
-                int incl = mine;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int up = __shfl_up_sync(0xffffffffu, incl, d);
-                    if (lane >= d) incl += up;
-                }
-                const unsigned here = __ballot_sync(0xffffffffu, off < incl);
-                if (here) {
-                    const int src = __ffs(here) - 1;
-                    block = i0 + src;
-                    off -= __shfl_sync(0xffffffffu, incl - mine, src);
-                    break;
-                }
-                off -= __shfl_sync(0xffffffffu, incl, 31);
-            }
-        }
-        if (lane == 0) {
-            m->seq = b; m->head = h; m->block = block; m->off = off;
-            m->w_begin = begin; m->w_end = end; m->W = W; m->ctas = ctas;
-        }
-    }
-    __syncthreads();
-}
-
 // Page ids of a piece's key tiles, 16 tiles at a time (one id per lane).
 struct PageCursor {
     int t_first = 0, id = 0;
     bool loaded = false;
     __device__ __forceinline__ void get(const PromptAttnParams &p, const Piece &s, int t, int lane, int &a, int &b) {
-        if (!loaded || t - t_first >= 16) {
+        if (!loaded || (unsigned)(t - t_first) >= 16u) {
             t_first = t;
             const int i = 2 * t + lane, npages = (s.u.keys + kPage - 1) / kPage;
             id = i < npages ? p.page_table[(size_t)s.b * p.max_pages + i] : 0;
@@ -277,24 +328,34 @@ struct PageCursor {
     }
 };
 
-// 2^x for two arguments on the FMA pipe, beside the 16 results a cycle and SM of the special-function unit: with
-// n = x rounded to an integer (through the 1.5 * 2^23 trick) and f = x - n in [-1/2, 1/2], 2^f is a polynomial (minimax in
-// the relative error, 2.7e-6 in fp32: far below the 2^-9 that the rounding of P to bf16 costs) and n goes into the exponent
-// field.  Arguments below -126 give 2^-126 - 2^-126 = 0; the kernel's arguments stay below 2^7 by far.
-__device__ __forceinline__ float2 exp2_poly(float2 x) {
-    constexpr float kRound = 12582912.f, kTiny = 1.17549435e-38f;
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
-    const float2 t = __fadd2_rn(x, make_float2(kRound, kRound));
-    const float2 n = __fadd2_rn(t, make_float2(-kRound, -kRound));
-    const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
-    float2 y = __ffma2_rn(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
-    y = __ffma2_rn(y, f, make_float2(0.240247443318367f, 0.240247443318367f));
-    y = __ffma2_rn(y, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-    y = __ffma2_rn(y, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
-    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
-    return __fadd2_rn(y, make_float2(-kTiny, -kTiny));
+__device__ __forceinline__ void zero_sequence(const PromptAttnParams &p, int b, int D, int t, int threads) {
+    const int start = p.token_start[b], n = p.token_start[b + 1] - start;
+    uint4 *rows = reinterpret_cast<uint4 *>(p.out + (size_t)start * p.Hq * D);
+    for (size_t i = t; i < (size_t)n * p.Hq * D / 8; i += threads) rows[i] = make_uint4(0, 0, 0, 0);
+    if (p.lse)
+        for (size_t i = t; i < (size_t)n * p.Hq; i += threads) p.lse[(size_t)start * p.Hq + i] = 0.f;
+}
+
+// Single-launch form: the status words of the sequences without a unit, and zero rows for those of them that have rows.
+// (A sequence with units is reported by the CTA of its first one.)  One warp of one CTA.
+template <int D>
+__device__ void report_idle(const PromptAttnParams &p, int lane) {
+    bool bad = false;
+    for (int b = lane; b < p.B; b += 32) {
+        const int a = p.token_start[b], e = p.token_start[b + 1];
+        bad |= a < 0 || a > e || e > p.tokens;
+    }
+    const bool none = __any_sync(0xffffffffu, bad);
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+        const int b = b0 + lane;
+        bool wrong = false;
+        if (b < p.B) {
+            const int n = p.token_start[b + 1] - p.token_start[b];
+            wrong = !none && !prompt_len_ok(p.seq_lens[b], n, p.max_pages);
+            if (none || wrong || n == 0) p.status[b] = none ? READER_ERR_INVALID_ARG : wrong ? READER_ERR_CAPACITY : READER_OK;
+        }
+        for (unsigned left = __ballot_sync(0xffffffffu, wrong); left; left &= left - 1) zero_sequence(p, b0 + __ffs(left) - 1, D, lane, 32);
+    }
 }
 
 __device__ __forceinline__ bool nonfinite_bits(uint32_t half) { return (half & 0x7f80u) == 0x7f80u; }
@@ -337,7 +398,11 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         mbar_init(bar(&m->merge_ready), 128);
         mbar_init(bar(&m->merge_free), 128);
         m->abort = 0;
-        for (int i = 0; i < kPoisonRing; ++i) m->poison[i] = 0;
+        m->piece[0].nt = 0;
+        for (int i = 0; i < kPieces; ++i) {
+            mbar_init(bar(&m->piece_full[i]), 1);
+            mbar_init(bar(&m->piece_empty[i]), kConsumers);
+        }
         fence_mbar_init();
         mbar_arrive(bar(&m->turn[0]));   // slot 0 has the first turn
         fence_proxy_async();
@@ -356,27 +421,42 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
     // everything above overlapped the kernel before this one in the stream; its results are read from here on
     grid_dependency_wait();
     grid_launch_dependents();
-    partition(p, m, reinterpret_cast<int32_t *>(smem + C::kOffRing));
-    if (tid == 0) fence_proxy_async();   // the ring was scratch until here
-    __syncthreads();
-
-    walk_init(p, m, warp, lane);
-    const Piece &sg = m->piece[warp];
-    auto next = [&]() { return walk_next(p, m, warp, lane); };
-
+    // the piece a warp is working on
+    int pieces = 0;
+    const Piece *sg = m->piece;
+    auto next = [&]() -> bool {
+        const int i = pieces % kPieces;
+        if (!wait(bar(&m->piece_full[i]), (pieces / kPieces) & 1, abort_s)) return false;
+        ++pieces;
+        sg = &m->piece[i];
+        return sg->nt > 0;
+    };
+    auto done = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(&m->piece_empty[(pieces - 1) % kPieces]));
+    };
     if (warp >= 8) {
     regs_dec<kRegsOther>();
     if (warp == kProducerWarp) {
         // ------------------------------------------------------------------ producer
         int r = 0, seg = 0;
-        auto load = [&](const CUtensorMap *map, int page_a, int page_b, int npg, bool raw) {
-            const int stage = r % C::kStages;
+        if (lane == 0) p.pieces[blockIdx.x].b = -1;
+        __syncwarp();
+        Schedule schedule;
+        schedule.init(p, reinterpret_cast<int32_t *>(smem + C::kOffRing), lane);
+        if (lane == 0) fence_proxy_async();   // the ring was scratch until here
+        __syncwarp();
+        Piece s;
+        auto load = [&](PageCursor &cursor, const CUtensorMap *map, int j, bool values) {
+            const int stage = r % C::kStages, t = s.tile(j), npg = t * kKeyTile + kPage < s.u.keys ? 2 : 1;
+            int page_a, page_b;
+            cursor.get(p, s, t, lane, page_a, page_b);
             const bool ok = wait(bar(&m->empty[stage]), ((r / C::kStages) & 1) ^ 1, abort_s);
             __syncwarp();
             if (ok && elect_one()) {
-                const uint32_t full = bar(raw ? &m->raw[stage] : &m->full[stage]), dst = sRing + stage * C::kTileBytes;
+                const uint32_t full = bar(values && has_own_keys(s, t) ? &m->raw[stage] : &m->full[stage]), dst = sRing + stage * C::kTileBytes;
                 mbar_arrive_expect_tx(full, npg * (C::kTileBytes / 2));
-                const int row_a = (page_a * p.Hkv + sg.h) * kPage, row_b = (page_b * p.Hkv + sg.h) * kPage;
+                const int row_a = (page_a * p.Hkv + s.h) * kPage, row_b = (page_b * p.Hkv + s.h) * kPage;
 #pragma unroll
                 for (int hf = 0; hf < C::kHalves; ++hf) {
                     tma_load_2d(dst + hf * C::kBlockBytes, map, full, hf * 64, row_a);
@@ -387,31 +467,34 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             ++r;
         };
         const int tile_rows_bytes = p.G * p.tile_tokens * 128;
-        while (!*abort_s && next()) {
+        while (!*abort_s) {
+            const bool more = schedule.next(p, s, lane);
+            const int i = seg % kPieces;
+            if (!wait(bar(&m->piece_empty[i]), ((seg / kPieces) & 1) ^ 1, abort_s)) break;
+            if (lane == 0) {
+                m->piece[i] = s;
+                mbar_arrive(bar(&m->piece_full[i]));
+            }
+            __syncwarp();
+            if (!more) break;
+            const int ahead = ahead_of(s);
+            PageCursor kc, vc;
+            for (int j = 0; j < ahead; ++j) load(kc, &kmap, j, false);
             if (wait(bar(&m->q_empty), (seg & 1) ^ 1, abort_s) && elect_one()) {
                 const uint32_t full = bar(&m->q_full);
-                const int tiles = sg.u.narrow ? 1 : 2;
+                const int tiles = s.u.narrow ? 1 : 2;
                 mbar_arrive_expect_tx(full, tiles * C::kHalves * tile_rows_bytes);
-                for (int s = 0; s < tiles; ++s)
+                for (int q = 0; q < tiles; ++q)
 #pragma unroll
                     for (int hf = 0; hf < C::kHalves; ++hf)
-                        tma_load_3d(sQ + s * C::kTileBytes + hf * C::kBlockBytes, &qmap, full, hf * 64, sg.h * p.G,
-                                    sg.start + sg.first_token + s * p.tile_tokens);
+                        tma_load_3d(sQ + q * C::kTileBytes + hf * C::kBlockBytes, &qmap, full, hf * 64, s.h * p.G,
+                                    s.start + s.first_token + q * p.tile_tokens);
             }
             __syncwarp();
             ++seg;
-            const int ahead = ahead_of(sg);
-            PageCursor kc, vc;
-            auto load_j = [&](PageCursor &c, const CUtensorMap *map, int j, bool values) {
-                const int t = sg.t0 + j;
-                int a, b;
-                c.get(p, sg, t, lane, a, b);
-                load(map, a, b, t * kKeyTile + kPage < sg.u.keys ? 2 : 1, values && has_own_keys(sg, t));
-            };
-            for (int j = 0; j < ahead; ++j) load_j(kc, &kmap, j, false);
-            for (int j = 0; j < sg.nt; ++j) {
-                load_j(vc, &vmap, j, true);
-                if (j + ahead < sg.nt) load_j(kc, &kmap, j + ahead, false);
+            for (int j = 0; j < s.nt; ++j) {
+                load(vc, &vmap, j, true);
+                if (j + ahead < s.nt) load(kc, &kmap, j + ahead, false);
             }
         }
         // a CTA that gave up must not exit under its own copies: let the last ones land (bounded)
@@ -466,8 +549,8 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             }
         };
         while (!*abort_s && next()) {
-            const int ahead = ahead_of(sg), n = sg.nt, r0 = r, t0 = sg.t0, keys = sg.u.keys;
-            const bool narrow = sg.u.narrow;
+            const int ahead = ahead_of(*sg), n = sg->nt, r0 = r, keys = sg->u.keys;
+            const bool narrow = sg->u.narrow;
             const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1;
             const uint64_t qd = descQ + (uint64_t)((narrow ? 0 : slot * C::kTileBytes) >> 4);
             // Left to themselves the two slots fall into step, score products side by side and then both softmaxes
@@ -494,7 +577,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 pass_turn();
                 ++r;
                 for (int j = j0; j < n; j += dj) {
-                    const int slices = (min(kKeyTile, keys - (t0 + j) * kKeyTile) + 15) >> 4;
+                    const int slices = (min(kKeyTile, keys - sg->tile(j) * kKeyTile) + 15) >> 4;
                     const bool more = j + dj < n;
                     pass_to(r0 + place_of_v(j, ahead, n));
                     const int rv = r;
@@ -530,33 +613,23 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 __syncwarp();
             }
             pass_to(r0 + 2 * n);
+            done();
         }
     } else if (warp == kValueWarp) {
         // ------------------------------------------------------------------ values some queries do not see; the note on a split unit
-        int r0 = 0, seg = 0;
+        int r0 = 0;
         uint32_t raw_parity = 0;   // one bit per ring stage
-        if (lane == 0) p.pieces[blockIdx.x].b = -1;
-        __syncwarp();
+        if (p.alone && blockIdx.x == 0) report_idle<D>(p, lane);
         while (!*abort_s && next()) {
-            const int ahead = ahead_of(sg), n = sg.nt, own_key = sg.L + sg.first_token;
-            if (!sg.full && sg.slot == 1 && lane == 0) {
-                const int s1 = sg.u.narrow ? (sg.t0 + sg.nt + 1) / 2 : sg.t0 + sg.nt;
-                const int unit_end = m->walk[warp].w + (sg.u.steps - s1);   // the walk stands behind this segment's last entry
-                PieceDesc d;
-                d.b = sg.b; d.h = sg.h; d.block = sg.block;
-                d.more = prompt_range_owner(unit_end - 1, m->W, m->ctas) - (int)blockIdx.x;
-                d.first_token = sg.start; d.tokens = sg.n; d.L = sg.L;
-                p.pieces[blockIdx.x] = d;
-            }
-            if (lane == 0) *(volatile int32_t *)&m->poison[seg % kPoisonRing] = 0;
-            __syncwarp();
-            for (int j = max(0, own_key / kKeyTile - sg.t0); j < n; ++j) {
-                const int t = sg.t0 + j;
+            const int ahead = ahead_of(*sg), n = sg->nt, own_key = sg->L + sg->first_token;
+            for (int j = 0; j < n; ++j) {
+                const int t = sg->tile(j);
+                if (!has_own_keys(*sg, t)) continue;
                 const int r = r0 + place_of_v(j, ahead, n), stage = r % C::kStages;
                 if (!wait(bar(&m->raw[stage]), (raw_parity >> stage) & 1, abort_s)) break;
                 raw_parity ^= 1u << stage;
                 const uint32_t tile = sRing + stage * C::kTileBytes;
-                const int valid = min(kKeyTile, sg.u.keys - t * kKeyTile), end = (valid + 15) & ~15;
+                const int valid = min(kKeyTile, sg->u.keys - t * kKeyTile), end = (valid + 15) & ~15;
                 // First a look at the exponents of the rows some queries do not see (all ones: infinity or NaN), sixteen
                 // 16-byte pieces a lane in flight; only if there is one, the walk that replaces it.
                 constexpr int kChunks = D / 8, kBatch = 16;   // 16-byte pieces per row / per lane and turn
@@ -591,7 +664,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                         }
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
                     }
-                    if (lane == 0) *(volatile int32_t *)&m->poison[seg % kPoisonRing] = 1;
+                    if (lane == 0) *(volatile int32_t *)&m->piece[(pieces - 1) % kPieces].poison = 1;
                 }
                 for (int i = valid * kChunks + lane; i < end * kChunks; i += 32)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at(i)), "r"(0u) : "memory");
@@ -600,7 +673,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 if (lane == 0) mbar_arrive(bar(&m->full[stage]));
             }
             r0 += 2 * n;
-            ++seg;
+            done();
         }
     }
     } else {
@@ -611,21 +684,21 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         const uint32_t tS = tmem + kTmemS + slot * 128 + lane_base, tO = tmem + kTmemO + slot * D + lane_base;
         constexpr uint32_t kNegInf = 0xff800000u;
         const int row_token = row / p.G, row_member = row - row_token * p.G;
-        int seg = 0, narrows = 0;
+        int narrows = 0;
         uint32_t s_parity = 0, o_parity = 0;
         while (next()) {
-            const bool narrow = sg.u.narrow;
+            const bool narrow = sg->u.narrow;
             const int unit_token = (narrow ? 0 : slot * p.tile_tokens) + row_token;   // within the unit
-            const bool live = row_token < p.tile_tokens && unit_token < sg.u.tokens;
+            const bool live = row_token < p.tile_tokens && unit_token < sg->u.tokens;
             const bool warp_live = __any_sync(0xffffffffu, live);
             // the last key this row sees; rows without a query see what the first row sees
-            const int last_key = sg.L + sg.first_token + (live ? unit_token : 0);
+            const int last_key = sg->L + sg->first_token + (live ? unit_token : 0);
             const int warp_min = __reduce_min_sync(0xffffffffu, last_key);
             float mx = -INFINITY, l = 0.f;    // running maximum (scaled, log2 units) and row sum
-            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1, nt = sg.nt, t0 = sg.t0;
+            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1, nt = sg->nt;
             bool any = false;
             for (int j = j0; j < nt; j += dj) {
-                const int key0 = (t0 + j) * kKeyTile;
+                const int key0 = sg->tile(j) * kKeyTile;
                 wait(bar(&m->s_full[slot]), s_parity, abort_s);
                 s_parity ^= 1;
                 tc_fence_after();
@@ -651,7 +724,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                         for (int i = 0; i < 32; ++i) {
                             const int at = half * 64 + 2 * i;
                             const float2 x = __ffma2_rn(make_float2(f(at), f(at + 1)), sc2, neg2);
-                            const float2 e = (i & 7) < kPolyOf8 ? exp2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
+                            const float2 e = make_float2(ex2(x.x), ex2(x.y));
                             part[i & 1] = __fadd2_rn(part[i & 1], e);
                             const __nv_bfloat162 hh = __floats2bfloat162_rn(e.x, e.y);
                             pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
@@ -722,7 +795,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                     mbar_arrive(bar(&m->merge_ready));
                     wait(bar(&m->merge_free), narrows & 1, abort_s);
                     ++narrows;
-                    ++seg;
+                    done();
                     continue;
                 }
                 wait(bar(&m->merge_ready), narrows & 1, abort_s);
@@ -733,15 +806,15 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 w1 = other.x == -INFINITY ? 0.f : ex2(other.x - m_all);
                 l_all = l * w0 + other.y * w1;
             }
-            const bool poisoned = *(volatile int32_t *)&m->poison[seg % kPoisonRing] != 0;
-            const bool two = narrow && sg.nt > 1;   // slot 1 has an output to add
+            const bool poisoned = *(const volatile int32_t *)&sg->poison != 0 && !sg->reject;
+            const bool two = narrow && sg->nt > 1;   // slot 1 has an output to add
             if (warp_live) {
-                const float inv = sg.full ? 1.f / l_all : 1.f;
+                const float inv = sg->full && !sg->reject ? 1.f / l_all : 1.f;
                 const uint32_t staging = base + C::kOffStaging + warp * 4096;   // 32 rows of 128 bytes, 16-byte pieces swizzled
                 // where this lane's row goes, in rows from the unit's first; -1: nowhere
-                const int to = !live ? -1 : sg.full ? unit_token * p.Hq + row_member : row;
-                __nv_bfloat16 *out = p.out + (((size_t)sg.start + sg.first_token) * p.Hq + (size_t)sg.h * p.G) * D;
-                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128) * D;
+                const int to = !live ? -1 : sg->full ? unit_token * p.Hq + row_member : row;
+                __nv_bfloat16 *out = p.out + (((size_t)sg->start + sg->first_token) * p.Hq + (size_t)sg->h * p.G) * D;
+                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg->slot) * 256 + slot * 128) * D;
                 uint32_t o[32];
                 auto load = [&](int c) {
                     tmem_ld32(tO + c, o);
@@ -755,13 +828,17 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                         for (int i = 0; i < 32; ++i)
                             o[i] = __float_as_uint(__uint_as_float(o[i]) * w0 + __uint_as_float(o1[i]) * w1);
                     }
+                    if (sg->reject) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0;
+                    }
                     if (poisoned && live) {
                         // infinities and NaN among the values of the unit's own tokens, for the rows that see them
-                        const int lo = max(sg.L + sg.first_token, sg.t0 * kKeyTile), hi = min(last_key, (sg.t0 + sg.nt) * kKeyTile - 1);
+                        const int lo = max(sg->L + sg->first_token, sg->t0 * kKeyTile), hi = min(last_key, (sg->t0 + sg->nt) * kKeyTile - 1);
                         for (int key = lo; key <= hi; ++key) {
-                            const int page = p.page_table[(size_t)sg.b * p.max_pages + key / kPage];
+                            const int page = p.page_table[(size_t)sg->b * p.max_pages + key / kPage];
                             if (page < 0 || page >= p.num_pages) break;
-                            const __nv_bfloat16 *v = v_pool + (((size_t)page * p.Hkv + sg.h) * kPage + key % kPage) * D + c;
+                            const __nv_bfloat16 *v = v_pool + (((size_t)page * p.Hkv + sg->h) * kPage + key % kPage) * D + c;
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
                                 const float x = __bfloat162float(v[i]);
@@ -786,7 +863,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                     }
                     __syncwarp();
                 };
-                if (sg.full) {
+                if (sg->full) {
 #pragma unroll 1
                     for (int c = 0; c < D; c += 64) {
 #pragma unroll
@@ -815,10 +892,10 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                     }
                 }
                 if (live) {
-                    if (!sg.full)
-                        *reinterpret_cast<float2 *>(p.partial_ml + ((size_t)(2 * blockIdx.x + sg.slot) * 256 + slot * 128 + row) * 2) = make_float2(m_all, l_all);
+                    if (!sg->full)
+                        *reinterpret_cast<float2 *>(p.partial_ml + ((size_t)(2 * blockIdx.x + sg->slot) * 256 + slot * 128 + row) * 2) = make_float2(m_all, l_all);
                     else if (p.lse)
-                        p.lse[((size_t)sg.start + sg.first_token + unit_token) * p.Hq + (size_t)sg.h * p.G + row_member] = (m_all + log2f(l_all)) * 0.6931471805599453f;
+                        p.lse[((size_t)sg->start + sg->first_token + unit_token) * p.Hq + (size_t)sg->h * p.G + row_member] = sg->reject ? 0.f : (m_all + log2f(l_all)) * 0.6931471805599453f;
                 }
             }
             if (narrow) {
@@ -827,7 +904,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 mbar_arrive(bar(&m->merge_free));
                 ++narrows;
             }
-            ++seg;
+            done();
         }
     }
     tc_fence_before();
@@ -837,6 +914,10 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         tmem_dealloc(tmem, kTmemCols);
     }
     if (tid == 0) p.gave_up[blockIdx.x] = *abort_s;
+    if (p.alone && *abort_s && m->piece[0].nt > 0) {   // (published before anything could be waited for)
+        zero_sequence(p, m->piece[0].b, D, tid, kThreads);
+        if (tid == 0) p.status[m->piece[0].b] = READER_ERR_TIMEOUT;
+    }
 }
 
 // After the attention kernel: blocks kMergeBlocks * c .. of the first n_ctas * kMergeBlocks merge the unit that CTA c
@@ -851,13 +932,19 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
 constexpr int kFinishThreads = 256;
 constexpr int kMergeBlocks = 8;
 
-__device__ __forceinline__ bool pages_bad(const PromptAttnParams &p, int b, int keys) {
+// This thread's share of a look at the pages of a sequence's first `keys` positions.
+__device__ __forceinline__ bool sees_bad_page(const PromptAttnParams &p, int b, int keys) {
     bool bad = false;
     for (int i = threadIdx.x; i < (keys + kPage - 1) / kPage; i += kFinishThreads) {
         const int pg = p.page_table[(size_t)b * p.max_pages + i];
         bad |= pg < 0 || pg >= p.num_pages;
     }
-    return __syncthreads_or(bad);
+    return bad;
+}
+__device__ __forceinline__ bool sees_late_cta(const PromptAttnParams &p) {
+    bool late = false;
+    for (int i = threadIdx.x; i < p.n_ctas; i += kFinishThreads) late |= p.gave_up[i] != 0;
+    return late;
 }
 
 // Running softmax state of four columns of a row.
@@ -966,37 +1053,32 @@ __global__ void __launch_bounds__(kFinishThreads) prompt_finish_kernel(const Pro
     if ((int)blockIdx.x < p.n_ctas * kMergeBlocks) {
         const int c = blockIdx.x / kMergeBlocks;
         const PieceDesc d = p.pieces[c];
-        if (d.b < 0) return;
-        bool late = false;   // (a rejected sequence's rows are zeroed below: nobody else may write them)
-        for (int i = tid; i < p.n_ctas; i += kFinishThreads) late |= p.gave_up[i] != 0;
-        if (!__syncthreads_or(late) && !pages_bad(p, d.b, d.L + d.tokens)) merge_unit<D>(p, d, c, blockIdx.x % kMergeBlocks);
+        const int chunk = blockIdx.x % kMergeBlocks;
+        if (d.b < 0 || chunk >= unit_shape(d.L, d.tokens, d.block, p.tile_tokens).tokens * p.G) return;
+        // (a rejected sequence's rows are zeroed below: nobody else may write them)
+        if (!__syncthreads_or(sees_late_cta(p) || sees_bad_page(p, d.b, d.L + d.tokens))) merge_unit<D>(p, d, c, chunk);
         return;
     }
     const int b = blockIdx.x - p.n_ctas * kMergeBlocks;
-    bool bad = false, late = false;
+    bool bad = false;
     for (int i = tid; i < p.B; i += kFinishThreads) {
         const int a = p.token_start[i], e = p.token_start[i + 1];
         bad |= a < 0 || a > e || e > p.tokens;
     }
-    for (int i = tid; i < p.n_ctas; i += kFinishThreads) late |= p.gave_up[i] != 0;
+    const int start = p.token_start[b], n = p.token_start[b + 1] - start, L = p.seq_lens[b];
+    const bool len_ok = prompt_len_ok(L, n, p.max_pages);
+    const bool page = len_ok && n > 0 && sees_bad_page(p, b, L + n), late = sees_late_cta(p);
     if (__syncthreads_or(bad)) {
         if (tid == 0) p.status[b] = READER_ERR_INVALID_ARG;
         return;   // whose rows are whose is not known: nothing was written
     }
-    const int start = p.token_start[b], n = p.token_start[b + 1] - start, L = p.seq_lens[b];
-    int st = READER_OK;
-    if (!prompt_len_ok(L, n, p.max_pages)) st = READER_ERR_CAPACITY;
-    else if (n > 0 && pages_bad(p, b, L + n)) st = READER_ERR_BAD_PAGE;
-    if (__syncthreads_or(late) && st == READER_OK) st = READER_ERR_TIMEOUT;
+    const bool any_page = __syncthreads_or(page), any_late = __syncthreads_or(late);
+    const int st = !len_ok ? READER_ERR_CAPACITY : any_page ? READER_ERR_BAD_PAGE : any_late ? READER_ERR_TIMEOUT : READER_OK;
     if (tid == 0) {
         p.status[b] = st;
         if (p.bump && st == READER_OK) p.bump[b] = L + n;
     }
-    if (st == READER_OK) return;
-    uint4 *rows = reinterpret_cast<uint4 *>(p.out + (size_t)start * p.Hq * D);
-    for (size_t i = tid; i < (size_t)n * p.Hq * D / 8; i += kFinishThreads) rows[i] = make_uint4(0, 0, 0, 0);
-    if (p.lse)
-        for (size_t i = tid; i < (size_t)n * p.Hq; i += kFinishThreads) p.lse[(size_t)start * p.Hq + i] = 0.f;
+    if (st != READER_OK) zero_sequence(p, b, D, tid, kFinishThreads);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,

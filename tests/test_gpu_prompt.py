@@ -165,6 +165,47 @@ def test_attn_random_shapes(rd, D):
         check_attn(rd, q, cache, ns, lens, 0.11)
 
 
+def test_attn_units_from_the_counter(rd):
+    """Enough units that they are handed out whole: ragged prompts, with and without a history, an empty one, rows behind."""
+    rng = np.random.default_rng(17)
+    ns, lens = [500, 0, 333, 1, 8, 700, 9, 400], [0, 5, 100, 300, 0, 0, 77, 40]
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 8, 64)
+    q = bf16(rng, sum(ns) + 2, 128, 64).cuda()
+    for _ in range(2):   # the counter starts anew
+        check_attn(rd, q, cache, ns, lens, 0.125)
+
+
+def test_attn_long_histories_begun_in_the_middle(rd):
+    """Whole units of more than 64 key tiles, which different CTAs begin at different tiles; sampled heads."""
+    rng = np.random.default_rng(18)
+    B, Hkv, D = 10, 32, 64
+    ns, lens = [256] * B, [int(x) for x in rng.integers(8200, 8500, B)]
+    ns[3], ns[7] = 100, 77
+    pages = [(a + b + PAGE - 1) // PAGE for a, b in zip(ns, lens)]
+    g = torch.Generator(device="cuda").manual_seed(18)
+    from paper_2508_09072_b200 import binding
+    order = torch.from_numpy(rng.permutation(sum(pages)).astype(np.int32)).cuda()
+    table = torch.full((B, max(pages)), -1, dtype=torch.int32, device="cuda")
+    for b in range(B):
+        table[b, :pages[b]] = order[sum(pages[:b]):sum(pages[:b + 1])]
+    k, v = (torch.randn(sum(pages), Hkv, PAGE, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    cache = binding.KvCache(k, v, table, torch.tensor(lens, dtype=torch.int32).cuda())
+    q = torch.randn(sum(ns), Hkv, D, generator=g, device="cuda").to(torch.bfloat16)
+    out, st = rd.prompt_attn(q, cache, starts(ns), D ** -0.5)
+    assert st.tolist() == [0] * B
+    for b in range(B):
+        at = sum(ns[:b])
+        for h in (b, 31 - b, 15):
+            kk, vv = rows_of(cache, b, lens[b] + ns[b])
+            kk, vv, qq = kk[:, h], vv[:, h], q[at:at + ns[b], h].double().cpu()
+            seen = torch.arange(len(kk))[None] <= lens[b] + torch.arange(ns[b])[:, None]
+            w = torch.softmax((qq @ kk.T * D ** -0.5).masked_fill(~seen, float("-inf")), -1)
+            want = w @ vv
+            delta = D * 2.0 ** -23 * (qq.abs() @ kk.abs().T * D ** -0.5).amax(-1, keepdim=True) + 1e-6
+            tol = (HALF + 4 * delta) * (w @ vv.abs()) + HALF * 1.01 * want.abs()
+            within(out[at:at + ns[b], h], want, tol)
+
+
 def test_attn_many_single_tokens(rd):
     rng = np.random.default_rng(3)
     B = 200
