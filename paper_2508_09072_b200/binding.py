@@ -581,50 +581,55 @@ class Reader:
             if t.is_cuda and t.dtype is torch.bfloat16:
                 raise ValueError(f"{name} is on {t.device}, this reader on cuda:{self.device}")
             raise TypeError(f"{name}: need a CUDA tensor of dtype {torch.bfloat16}")
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name}: need shape {shape}, got {tuple(t.shape)}")
-        *lead, heads, d = shape
-        stride = t.stride()
-        dense = heads * d
-        if t.numel() == 0:
-            return t.data_ptr(), dense
+        if t.shape != shape:
+            raise ValueError(f"{name}: need shape {tuple(shape)}, got {tuple(t.shape)}")
+        stride, heads, d = t.stride(), shape[-2], shape[-1]
+        if 0 in shape:
+            return t.data_ptr(), heads * d
         if stride[-1] != 1 or (heads > 1 and stride[-2] != d):
             raise ValueError(f"{name}: the heads of a token must be dense")
-        if len(lead) == 1:
-            return t.data_ptr(), stride[0] if lead[0] > 1 else dense
-        b, n = lead
+        if len(shape) == 3:
+            return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
+        b, n = shape[0], shape[1]
         if b > 1 and n > 1 and stride[0] != n * stride[1]:
             raise ValueError(f"{name}: the tokens must be evenly spaced")
-        return t.data_ptr(), stride[1] if n > 1 else stride[0] if b > 1 else dense
+        return t.data_ptr(), stride[1] if n > 1 else stride[0] if b > 1 else heads * d
 
     def _paged(self, c: KvCache) -> _KvCache:
-        k = c.k_pool
+        """The cache's C struct.  It is kept with the cache object for as long as that names the same tensors, at the same
+        addresses and of the same shapes."""
+        k, v, table, lens = c.k_pool, c.v_pool, c.page_table, c.seq_lens
+        key = (k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), k.shape, table.shape, c.shared_prefix_len)
+        kept = c.__dict__.get("_kept")
+        if kept is not None and kept[0] is k and kept[1] is v and kept[2] is table and kept[3] is lens and kept[4] == key and kept[5] == self.device:
+            return kept[6]
         pages, heads, page, d = k.shape
-        if c.v_pool.shape != k.shape:
-            raise ValueError("v_pool: the shape of k_pool")
-        batch, width = c.page_table.shape
-        if c.seq_lens.shape[0] != batch:
-            raise ValueError("seq_lens: one length for each row of the page table")
-        return _KvCache(self._have(k, torch.bfloat16, "k_pool"), self._have(c.v_pool, torch.bfloat16, "v_pool"), pages, page, heads, d,
-                        self._have(c.page_table, torch.int32, "page_table"), width, self._have(c.seq_lens, torch.int32, "seq_lens"),
-                        int(c.shared_prefix_len))
+        batch, width = table.shape
+        if v.shape != k.shape or lens.shape != (batch,):
+            raise ValueError("v_pool: the shape of k_pool; seq_lens: one length for each row of the page table")
+        have = self._have
+        st = _KvCache(have(k, torch.bfloat16, "k_pool"), have(v, torch.bfloat16, "v_pool"), pages, page, heads, d,
+                      have(table, torch.int32, "page_table"), width, have(lens, torch.int32, "seq_lens"), int(c.shared_prefix_len))
+        c.__dict__["_kept"] = (k, v, table, lens, key, self.device, st)
+        return st
 
     def _rotation(self, head_dim: int, rope, q_weight, k_weight, eps: float, interleaved: bool) -> _Rotation:
         q = k = r = None
         positions = rot = 0
         if q_weight is not None:
             q = self._have(q_weight, torch.bfloat16, "q_weight")
+            if q_weight.shape != (head_dim,):
+                raise ValueError(f"q_weight: need shape ({head_dim},)")
         if k_weight is not None:
             k = self._have(k_weight, torch.bfloat16, "k_weight")
-        for w in (q_weight, k_weight):
-            if w is not None and w.shape != (head_dim,):
-                raise ValueError(f"q_weight, k_weight: need shape ({head_dim},)")
+            if k_weight.shape != (head_dim,):
+                raise ValueError(f"k_weight: need shape ({head_dim},)")
         if rope is not None:
             r = self._have(rope, torch.float32, "rope")
-            if rope.dim() != 3 or rope.shape[1] != 2:
+            shape = rope.shape
+            if len(shape) != 3 or shape[1] != 2:
                 raise ValueError("rope: need [max_positions, 2, rot_dim / 2]")
-            positions, _, half = rope.shape
-            rot = 2 * half
+            positions, rot = shape[0], 2 * shape[2]
         return _Rotation(q, k, eps, r, positions, rot, 1 if interleaved else 0)
 
     def _prompt(self, batch: int, token_start: torch.Tensor, tokens: int) -> _Prompt:
