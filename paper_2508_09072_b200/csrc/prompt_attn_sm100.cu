@@ -57,6 +57,7 @@ constexpr float kRaiseMaxBy = 8.f;   // log2 units
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 constexpr int kMaxStages = 8;
 constexpr int kRotateTiles = 64;     // shortest unit that is begun in the middle
+constexpr int kLookAheadTiles = 12;  // shortest piece whose values are looked at ahead of their tiles
 constexpr int kMiscBytes = 3072;
 
 template <int D>
@@ -148,21 +149,20 @@ struct Schedule {
     }
     // sizes: scratch in shared memory, [B]
     __device__ __forceinline__ void init(const PromptAttnParams &p, int32_t *sizes, int lane) {
-        bool bad = false;
-        for (int i = lane; i < p.B; i += 32) {
-            const int a = p.token_start[i], e = p.token_start[i + 1];
-            bad |= a < 0 || a > e || e > p.tokens;
-        }
         w = left = w0 = W = ctas = b = h = block = off = start = L = n = blocks = first = 0;
-        if (__any_sync(0xffffffffu, bad)) {   // whose rows are whose is not known: no work
-            b = p.B;
-            return;
-        }
-        if (p.counter || p.alone) return;
+        const bool dealt = !p.counter && !p.alone;
+        bool bad = false;
         int total = 0;   // entries of one head of every sequence so far
         for (int b0 = 0; b0 < p.B; b0 += 32) {
             int n_ = 0, L_ = 0, m = 0, sum = 0;
-            if (b0 + lane < p.B) m = blocks_of(p, b0 + lane, n_, L_);
+            if (b0 + lane < p.B) {
+                const int a = p.token_start[b0 + lane], e = p.token_start[b0 + lane + 1];
+                L_ = p.seq_lens[b0 + lane];
+                bad |= a < 0 || a > e || e > p.tokens;
+                n_ = e - a;
+                if (dealt && !bad && prompt_len_ok(L_, n_, p.max_pages)) m = unit_blocks(n_, p.tile_tokens);
+            }
+            if (!dealt) continue;
             // few blocks: each lane adds up its own sequence; many: the warp one sequence after the other
             for (int i = 0; m <= 4 && i < m; ++i) sum += kUnitEntries + unit_shape(L_, n_, i, p.tile_tokens).steps;
             for (unsigned long_ones = __ballot_sync(0xffffffffu, m > 4); long_ones; long_ones &= long_ones - 1) {
@@ -177,6 +177,11 @@ struct Schedule {
             if (b0 + lane < p.B) sizes[b0 + lane] = total + incl - sum;
             total += __shfl_sync(0xffffffffu, incl, 31);
         }
+        if (__any_sync(0xffffffffu, bad)) {   // whose rows are whose is not known: no work
+            b = p.B;
+            return;
+        }
+        if (!dealt) return;
         __syncwarp();
         W = total * p.Hkv;
         ctas = prompt_busy_ctas(p.n_ctas, W);
@@ -622,50 +627,86 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         if (p.alone && blockIdx.x == 0) report_idle<D>(p, lane);
         while (!*abort_s && next()) {
             const int ahead = ahead_of(*sg), n = sg->nt, own_key = sg->L + sg->first_token;
+            constexpr int kChunks = D / 8;   // 16-byte pieces per row
+            // A look at the exponents (all ones: infinity or NaN) of the value rows that are multiplied although some query does
+            // not see them: the unit's own tokens, and what the last slice of 16 rows holds behind them.  They are read from
+            // the pool, while the tiles are on their way: out of shared memory, whose bandwidth the products take up,
+            // one tile took 6000 cycles.
+            const int lo = max(own_key, sg->t0 * kKeyTile), hi = min((sg->u.keys + 15) & ~15, (sg->t0 + n) * kKeyTile);
+            // (A short piece has no time for that, and few products: its tiles are gone through in shared memory.)
+            bool dirty = n < kLookAheadTiles;
+            if (!dirty && lo < hi) {
+                constexpr int kBatch = 8;    // pieces a lane has in flight
+                const int first_page = lo / kPage;
+                int page = -1;
+                if (first_page + lane <= (hi - 1) / kPage) page = p.page_table[(size_t)sg->b * p.max_pages + first_page + lane];
+                if (page >= p.num_pages) page = -1;
+                uint32_t ones = 0;
+                for (int i0 = 0; i0 < (hi - lo) * kChunks; i0 += kBatch * 32) {
+                    uint4 x[kBatch];
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) {
+                        const int i = i0 + k * 32 + lane, key = lo + i / kChunks;
+                        const int pg = __shfl_sync(0xffffffffu, page, (key / kPage - first_page) & 31);
+                        x[k] = make_uint4(0, 0, 0, 0);
+                        if (key < hi && pg >= 0)
+                            x[k] = __ldg(reinterpret_cast<const uint4 *>(v_pool + (((size_t)pg * p.Hkv + sg->h) * kPage + key % kPage) * D) + i % kChunks);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) {
+                        ones |= ((x[k].x & 0x7f807f80u) + 0x00800080u) | ((x[k].y & 0x7f807f80u) + 0x00800080u);
+                        ones |= ((x[k].z & 0x7f807f80u) + 0x00800080u) | ((x[k].w & 0x7f807f80u) + 0x00800080u);
+                    }
+                }
+                dirty = __any_sync(0xffffffffu, (ones & 0x80008000u) != 0);
+            }
             for (int j = 0; j < n; ++j) {
                 const int t = sg->tile(j);
                 if (!has_own_keys(*sg, t)) continue;
                 const int r = r0 + place_of_v(j, ahead, n), stage = r % C::kStages;
                 if (!wait(bar(&m->raw[stage]), (raw_parity >> stage) & 1, abort_s)) break;
                 raw_parity ^= 1u << stage;
+                if (!dirty) {
+                    if (lane == 0) mbar_arrive(bar(&m->full[stage]));
+                    __syncwarp();
+                    continue;
+                }
                 const uint32_t tile = sRing + stage * C::kTileBytes;
                 const int valid = min(kKeyTile, sg->u.keys - t * kKeyTile), end = (valid + 15) & ~15;
-                // First a look at the exponents of the rows some queries do not see (all ones: infinity or NaN), sixteen
-                // 16-byte pieces a lane in flight; only if there is one, the walk that replaces it.
-                constexpr int kChunks = D / 8, kBatch = 16;   // 16-byte pieces per row / per lane and turn
                 const int own_row = max(0, own_key - t * kKeyTile);
                 auto piece_at = [&](int i) {
                     const int row = i / kChunks, c = i % kChunks;
                     return tile + (c >> 3) * C::kBlockBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
                 };
-                uint32_t ones = 0;
-                for (int i0 = own_row * kChunks + lane; i0 < valid * kChunks; i0 += kBatch * 32) {
-                    uint32_t x[kBatch][4];
+                bool found = false;
+                constexpr int kAtOnce = 8;
+                for (int i0 = own_row * kChunks + lane; i0 < valid * kChunks; i0 += kAtOnce * 32) {
+                    uint32_t x[kAtOnce][4];
+                    uint32_t ones = 0;
 #pragma unroll
-                    for (int k = 0; k < kBatch; ++k) {
+                    for (int k = 0; k < kAtOnce; ++k) {
                         x[k][0] = x[k][1] = x[k][2] = x[k][3] = 0;
                         if (i0 + k * 32 < valid * kChunks)
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3]) : "r"(piece_at(i0 + k * 32)));
                     }
 #pragma unroll
-                    for (int k = 0; k < kBatch; ++k)
+                    for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) ones |= (x[k][e] & 0x7f807f80u) + 0x00800080u;
-                }
-                if (__any_sync(0xffffffffu, (ones & 0x80008000u) != 0)) {
-                    for (int i = own_row * kChunks + lane; i < valid * kChunks; i += 32) {
-                        uint32_t x[4];
-                        const uint32_t at = piece_at(i);
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
+                    if (!(ones & 0x80008000u)) continue;
+                    found = true;
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            if (nonfinite_bits(x[e])) x[e] &= 0xffff0000u;
-                            if (nonfinite_bits(x[e] >> 16)) x[e] &= 0x0000ffffu;
+                            if (nonfinite_bits(x[k][e])) x[k][e] &= 0xffff0000u;
+                            if (nonfinite_bits(x[k][e] >> 16)) x[k][e] &= 0x0000ffffu;
                         }
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                        if (i0 + k * 32 < valid * kChunks)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece_at(i0 + k * 32)), "r"(x[k][0]), "r"(x[k][1]), "r"(x[k][2]), "r"(x[k][3]) : "memory");
                     }
-                    if (lane == 0) *(volatile int32_t *)&m->piece[(pieces - 1) % kPieces].poison = 1;
                 }
+                if (__any_sync(0xffffffffu, found) && lane == 0) *(volatile int32_t *)&m->piece[(pieces - 1) % kPieces].poison = 1;
                 for (int i = valid * kChunks + lane; i < end * kChunks; i += 32)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at(i)), "r"(0u) : "memory");
                 fence_proxy_async();
@@ -806,17 +847,13 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 w1 = other.x == -INFINITY ? 0.f : ex2(other.x - m_all);
                 l_all = l * w0 + other.y * w1;
             }
-            const bool poisoned = *(const volatile int32_t *)&sg->poison != 0 && !sg->reject;
+            const bool poisoned = *(const volatile int32_t *)&sg->poison != 0;
             const bool two = narrow && sg->nt > 1;   // slot 1 has an output to add
-            if (warp_live) {
-                const float inv = sg->full && !sg->reject ? 1.f / l_all : 1.f;
-                const uint32_t staging = base + C::kOffStaging + warp * 4096;   // 32 rows of 128 bytes, 16-byte pieces swizzled
-                // where this lane's row goes, in rows from the unit's first; -1: nowhere
-                const int to = !live ? -1 : sg->full ? unit_token * p.Hq + row_member : row;
-                __nv_bfloat16 *out = p.out + (((size_t)sg->start + sg->first_token) * p.Hq + (size_t)sg->h * p.G) * D;
-                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg->slot) * 256 + slot * 128) * D;
-                uint32_t o[32];
-                auto load = [&](int c) {
+            if (warp_live && (two || poisoned || sg->reject)) {
+                // what few outputs need is done to the output tile in tensor memory before it is written
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
                     tmem_ld32(tO + c, o);
                     tmem_wait_ld();
                     if (two) {
@@ -827,10 +864,6 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             o[i] = __float_as_uint(__uint_as_float(o[i]) * w0 + __uint_as_float(o1[i]) * w1);
-                    }
-                    if (sg->reject) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = 0;
                     }
                     if (poisoned && live) {
                         // infinities and NaN among the values of the unit's own tokens, for the rows that see them
@@ -846,12 +879,49 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             }
                         }
                     }
-                };
+                    if (sg->reject) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0;
+                    }
+                    tmem_st32(tO + c, o);
+                }
+                tmem_wait_st();
+            }
+            if (warp_live) {
+                const bool full = sg->full;
+                const float inv = full && !sg->reject ? 1.f / l_all : 1.f;
+                const uint32_t staging = base + C::kOffStaging + warp * 4096;   // 32 rows of 128 bytes, 16-byte pieces swizzled
+                // where this lane's row goes, in rows from the unit's first; -1: nowhere
+                const int to = !live ? -1 : full ? unit_token * p.Hq + row_member : row;
+                __nv_bfloat16 *out = p.out + (((size_t)sg->start + sg->first_token) * p.Hq + (size_t)sg->h * p.G) * D;
+                float *part_o = p.partial_o + ((size_t)(2 * blockIdx.x + sg->slot) * 256 + slot * 128) * D;
                 auto put = [&](int piece, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((piece ^ (lane & 7)) << 4)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
                 };
-                // eight lanes write a row's 128 bytes, a warp four rows at a time
-                auto drain = [&](auto *first_row, int c) {
+                // eight lanes write a row's 128 bytes (64 bf16 or 32 fp32 columns), a warp four rows at a time
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(tO + c, o);
+                    tmem_wait_ld();
+                    if (full) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
+                                y[e] = *reinterpret_cast<const uint32_t *>(&hh);
+                            }
+                            put(((c >> 3) & 4) + i, y[0], y[1], y[2], y[3]);
+                        }
+                        if (!(c & 32)) continue;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) put(i, o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    }
+                    char *rows = full ? reinterpret_cast<char *>(out + c - 32) : reinterpret_cast<char *>(part_o + c);
+                    const int row_bytes = full ? D * 2 : D * 4;
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -859,37 +929,9 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                         const int dst = __shfl_sync(0xffffffffu, to, r);
                         uint4 y;
                         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(staging + r * 128 + ((piece ^ (r & 7)) << 4)));
-                        if (dst >= 0) reinterpret_cast<uint4 *>(first_row + (size_t)dst * D + c)[piece] = y;
+                        if (dst >= 0) *reinterpret_cast<uint4 *>(rows + (size_t)dst * row_bytes + piece * 16) = y;
                     }
                     __syncwarp();
-                };
-                if (sg->full) {
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 64) {
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            load(c + half * 32);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t y[4];
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
-                                    y[e] = *reinterpret_cast<const uint32_t *>(&hh);
-                                }
-                                put(half * 4 + i, y[0], y[1], y[2], y[3]);
-                            }
-                        }
-                        drain(out, c);
-                    }
-                } else {
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        load(c);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) put(i, o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                        drain(part_o, c);
-                    }
                 }
                 if (live) {
                     if (!sg->full)
