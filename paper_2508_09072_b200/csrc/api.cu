@@ -762,6 +762,7 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
     p.page_table = cache->page_table;
     p.B = B; p.tokens = tokens; p.Hq = Hq; p.Hkv = Hkv; p.D = D;
     p.max_pages = cache->max_pages_per_seq; p.num_pages = cache->num_pages;
+    p.shared_prefix_len = cache->shared_prefix_len;
     p.scale_log2 = softmax_scale * 1.4426950408889634f;
     p.out = static_cast<__nv_bfloat16 *>(out);
     p.lse = lse_out;

@@ -16,6 +16,7 @@ constexpr int kKeyTile = 128;            // keys per tile: two cache pages
 // block), each kUnitEntries entries (what starting and ending a unit costs) followed by its steps, form one list that is
 // cut into contiguous equal ranges, one per CTA.
 constexpr int kUnitEntries = 2;
+constexpr int kNarrowUnitEntries = 1;   // (its loads run on from the unit before it)
 constexpr int kMinEntriesPerCta = 4;
 // A call is a single launch when its units fit the CTAs and cutting them would not pay for the merge and the second launch
 // (6 to 9 us): going by the page table's width, at most kAloneSteps steps to a unit (lengths may differ, and the longest
@@ -37,6 +38,7 @@ struct PromptAttnParams {
     const int32_t *token_start;   // [B + 1]
     const int32_t *seq_lens, *page_table;
     int B, tokens, Hq, Hkv, G, D, max_pages, num_pages;
+    int shared_prefix_len;
     int tile_tokens;              // tokens per 128-row tile: 128 / G, rounded down
     float scale_log2;
     __nv_bfloat16 *out;
@@ -63,6 +65,7 @@ struct UnitShape {
     int keys;       // keys its last token sees
     bool narrow;
     int tiles, steps;
+    __host__ __device__ int entries() const { return (narrow ? kNarrowUnitEntries : kUnitEntries) + steps; }
 };
 __host__ __device__ inline UnitShape unit_shape(int L, int n, int block, int tile_tokens) {
     UnitShape u;

@@ -97,6 +97,7 @@ struct Piece {
     int slot;                // where its partial goes
     int first_token;         // of the unit, within the sequence
     int32_t poison;          // infinities or NaN were taken out of its value tiles
+    bool once;               // nobody else reads the keys and values of this piece
     bool reject;             // (single-launch form) a page id of the sequence is outside the pool: zero rows
     __device__ __forceinline__ int tile(int j) const { return t0 + (j + rot < nt ? j + rot : j + rot - nt); }
 };
@@ -164,12 +165,12 @@ struct Schedule {
             }
             if (!dealt) continue;
             // few blocks: each lane adds up its own sequence; many: the warp one sequence after the other
-            for (int i = 0; m <= 4 && i < m; ++i) sum += kUnitEntries + unit_shape(L_, n_, i, p.tile_tokens).steps;
+            for (int i = 0; m <= 4 && i < m; ++i) sum += unit_shape(L_, n_, i, p.tile_tokens).entries();
             for (unsigned long_ones = __ballot_sync(0xffffffffu, m > 4); long_ones; long_ones &= long_ones - 1) {
                 const int src = __ffs(long_ones) - 1;
                 const int ns = __shfl_sync(0xffffffffu, n_, src), Ls = __shfl_sync(0xffffffffu, L_, src), ms = __shfl_sync(0xffffffffu, m, src);
                 int part = 0;
-                for (int i = lane; i < ms; i += 32) part += kUnitEntries + unit_shape(Ls, ns, i, p.tile_tokens).steps;
+                for (int i = lane; i < ms; i += 32) part += unit_shape(Ls, ns, i, p.tile_tokens).entries();
                 part = __reduce_add_sync(0xffffffffu, part);
                 if (lane == src) sum = part;
             }
@@ -201,7 +202,7 @@ struct Schedule {
         off = within - h * size;
         open(p);
         for (int i0 = 0; i0 < blocks; i0 += 32) {
-            const int mine = i0 + lane < blocks ? kUnitEntries + unit_shape(L, n, i0 + lane, p.tile_tokens).steps : 0;
+            const int mine = i0 + lane < blocks ? unit_shape(L, n, i0 + lane, p.tile_tokens).entries() : 0;
             const int incl = inclusive_sum(mine, lane);
             const unsigned here = __ballot_sync(0xffffffffu, off < incl);
             if (here) {
@@ -220,6 +221,7 @@ struct Schedule {
         s.first_token = block * 2 * p.tile_tokens;
         s.rot = 0;
         s.poison = 0;
+        s.once = blocks == 1 && p.shared_prefix_len == 0;
         s.reject = false;
     }
     // The next piece with at least one key tile; false when there is no more.
@@ -281,8 +283,8 @@ struct Schedule {
                 }
             }
             describe(p, s);
-            const int entries = kUnitEntries + s.u.steps, take = min(entries - off, left);
-            const int s0 = max(0, off - kUnitEntries), s1 = off + take - kUnitEntries;
+            const int entries = s.u.entries(), extra = entries - s.u.steps, take = min(entries - off, left);
+            const int s0 = max(0, off - extra), s1 = off + take - extra;
             const int per = s.u.narrow ? 2 : 1;   // tiles a step
             if (s1 > s0) {
                 s.t0 = max(0, s.u.tiles - per * s1);
@@ -452,6 +454,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         if (lane == 0) fence_proxy_async();   // the ring was scratch until here
         __syncwarp();
         Piece s;
+        const uint64_t stream_policy = l2_policy_evict_first();
         auto load = [&](PageCursor &cursor, const CUtensorMap *map, int j, bool values) {
             const int stage = r % C::kStages, t = s.tile(j), npg = t * kKeyTile + kPage < s.u.keys ? 2 : 1;
             int page_a, page_b;
@@ -464,8 +467,12 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 const int row_a = (page_a * p.Hkv + s.h) * kPage, row_b = (page_b * p.Hkv + s.h) * kPage;
 #pragma unroll
                 for (int hf = 0; hf < C::kHalves; ++hf) {
-                    tma_load_2d(dst + hf * C::kBlockBytes, map, full, hf * 64, row_a);
-                    if (npg > 1) tma_load_2d(dst + hf * C::kBlockBytes + C::kBlockBytes / 2, map, full, hf * 64, row_b);
+                    // what is read once should not push lines that others will ask for out of L2
+                    const uint32_t to = dst + hf * C::kBlockBytes;
+                    if (s.once) tma_load_2d_hint(to, map, full, hf * 64, row_a, stream_policy);
+                    else tma_load_2d(to, map, full, hf * 64, row_a);
+                    if (npg > 1 && s.once) tma_load_2d_hint(to + C::kBlockBytes / 2, map, full, hf * 64, row_b, stream_policy);
+                    else if (npg > 1) tma_load_2d(to + C::kBlockBytes / 2, map, full, hf * 64, row_b);
                 }
             }
             __syncwarp();
