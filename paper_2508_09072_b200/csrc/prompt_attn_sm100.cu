@@ -56,6 +56,7 @@ constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kRaiseMaxBy = 8.f;   // log2 units
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 constexpr int kMaxStages = 8;
+constexpr int kLateStartTiles = 20;  // shortest piece whose slot 1 begins half a step late
 constexpr int kRotateTiles = 64;     // shortest unit that is begun in the middle
 constexpr int kLookAheadTiles = 12;  // shortest piece whose values are looked at ahead of their tiles
 constexpr int kMiscBytes = 3072;
@@ -568,6 +569,9 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             // Left to themselves the two slots fall into step, score products side by side and then both softmaxes
             // on the special-function units at once (3970 cycles a step).  In a wide unit they therefore take turns with
             // their score products, slot 0 first: each slot's softmax then runs beside the other's products.
+            // How far slot 1 begins behind slot 0 is how far it stays: in a long piece it waits for slot 0's first
+            // probabilities, half a step (attn_long 1630 -> 1586 us; in a short piece the wait costs more than it brings).
+            const bool late_start = !narrow && slot == 0 && n >= kLateStartTiles;
             auto take_turn = [&]() {
                 if (!narrow) wait(bar(&m->turn[slot]), turn_parity, abort_s);
                 turn_parity ^= narrow ? 0 : 1;
@@ -586,7 +590,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 __syncwarp();
                 if (elect_one()) issue_s(qd, r, j0 + dj >= n);
                 __syncwarp();
-                pass_turn();
+                if (!late_start) pass_turn();
                 ++r;
                 for (int j = j0; j < n; j += dj) {
                     const int slices = (min(kKeyTile, keys - sg->tile(j) * kKeyTile) + 15) >> 4;
@@ -599,6 +603,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                     __syncwarp();
                     if (elect_one()) issue_pv(0, rv, slices, j == j0);
                     __syncwarp();
+                    if (late_start && j == j0) pass_turn();
                     if (more) {
                         pass_to(r0 + place_of_k(j + dj, ahead));
                         wait_full(r);
