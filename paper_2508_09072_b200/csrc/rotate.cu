@@ -31,104 +31,150 @@ struct Raw {
     uint2 a, b;   // four elements each
 };
 
-// The token-independent part of a thread's work (which elements it has), and its table entries.
-template <int D>
+// A thread's part of a head: which elements it has, and its table entries.
+//   half-split (kInter false): word i of a and word i of b are two pairs as they stand
+//   interleaved: (a0 a1), (b0 b1) are the pairs; the even elements (a0 b0) are brought into one word, the odd ones into the other
+template <int D, bool kInter>
 struct Turner {
     static constexpr int kLanes = D / 8;   // threads per head
     int ea, eb;            // where its two groups of four elements begin
     int at;                // its four pairs' index in the table; -1: its elements are not rotated
-    uint32_t lo, hi;       // byte selectors that bring the first / second elements of its pairs together
     float2 c[2], s[2];
 
     __device__ __forceinline__ void init(const RotateParams &p, int lane) {
         const int l = lane % kLanes, quads = p.rope ? p.rot / 8 : 0;   // threads with rotated elements
-        const bool turned = l < quads, halves = turned && !p.interleaved;
+        const bool turned = l < quads, halves = turned && !kInter;
         at = turned ? 4 * l : -1;
         ea = halves ? 4 * l : 8 * l;       // (behind the rotated threads the rest of the head, 8 elements each)
         eb = halves ? ea + p.rot / 2 : ea + 4;
-        // half-split: word i of a and word i of b are two pairs as they stand.  Interleaved: (a0 a1), (b0 b1) are the
-        // pairs, so the even elements (a0 b0) go into one word and the odd ones (a1 b1) into the other.
-        lo = p.interleaved ? 0x5410u : 0x3210u;
-        hi = p.interleaved ? 0x7632u : 0x7654u;
-    }
-    __device__ __forceinline__ Raw load(const __nv_bfloat16 *head) const {
-        return Raw{*reinterpret_cast<const uint2 *>(head + ea), *reinterpret_cast<const uint2 *>(head + eb)};
-    }
-    __device__ __forceinline__ void store(__nv_bfloat16 *head, const Raw &r) const {
-        *reinterpret_cast<uint2 *>(head + ea) = r.a;
-        *reinterpret_cast<uint2 *>(head + eb) = r.b;
     }
     // first elements of the pairs to .a, second ones to .b (its own inverse)
-    __device__ __forceinline__ Raw paired(const Raw &r) const {
-        return Raw{make_uint2(__byte_perm(r.a.x, r.b.x, lo), __byte_perm(r.a.y, r.b.y, lo)),
-                   make_uint2(__byte_perm(r.a.x, r.b.x, hi), __byte_perm(r.a.y, r.b.y, hi))};
+    static __device__ __forceinline__ Raw paired(const Raw &r) {
+        if (!kInter) return r;
+        return Raw{make_uint2(__byte_perm(r.a.x, r.b.x, 0x5410), __byte_perm(r.a.y, r.b.y, 0x5410)),
+                   make_uint2(__byte_perm(r.a.x, r.b.x, 0x7632), __byte_perm(r.a.y, r.b.y, 0x7632))};
     }
     __device__ __forceinline__ void load_table(const RotateParams &p, int64_t pos) {
         if (at < 0) return;
         const float *row = p.rope + pos * p.rot + at;
         const float4 x = *reinterpret_cast<const float4 *>(row), y = *reinterpret_cast<const float4 *>(row + p.rot / 2);
         // pairs 0 .. 3 in the order of the words: (0 1), (2 3), or (0 2), (1 3) when interleaved
-        c[0] = make_float2(x.x, p.interleaved ? x.z : x.y); c[1] = make_float2(p.interleaved ? x.y : x.z, x.w);
-        s[0] = make_float2(y.x, p.interleaved ? y.z : y.y); s[1] = make_float2(p.interleaved ? y.y : y.z, y.w);
-    }
-    // Warp-collective (all heads of a warp at once); w: the weights of its elements, paired.
-    __device__ __forceinline__ Raw turn(const RotateParams &p, const Raw &raw, const float2 (&w)[4]) const {
-        const Raw r = paired(raw);
-        float2 x[4] = {unpack(r.a.x), unpack(r.a.y), unpack(r.b.x), unpack(r.b.y)};
-        if (p.q_weight) {
-            float2 sq = __fmul2_rn(x[0], x[0]);
-#pragma unroll
-            for (int i = 1; i < 4; ++i) sq = __ffma2_rn(x[i], x[i], sq);
-            float ss = sq.x + sq.y;
-#pragma unroll
-            for (int d = kLanes / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-            const float f = rsqrtf(ss * (1.f / D) + p.eps);
-            const float2 f2 = make_float2(f, f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = __fmul2_rn(__fmul2_rn(x[i], f2), w[i]);
-        }
-        if (at >= 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 a = x[i], b = x[i + 2], minus = make_float2(-s[i].x, -s[i].y);
-                x[i] = __ffma2_rn(b, minus, __fmul2_rn(a, c[i]));
-                x[i + 2] = __ffma2_rn(a, s[i], __fmul2_rn(b, c[i]));
-            }
-        }
-        return paired(Raw{make_uint2(pack(x[0]), pack(x[1])), make_uint2(pack(x[2]), pack(x[3]))});
+        c[0] = make_float2(x.x, kInter ? x.z : x.y); c[1] = make_float2(kInter ? x.y : x.z, x.w);
+        s[0] = make_float2(y.x, kInter ? y.z : y.y); s[1] = make_float2(kInter ? y.y : y.z, y.w);
     }
 };
 
-// One kind of a token's heads (queries, keys or values): from `src` to `dst`, where heads are `dst_stride` elements apart.
-// A warp handles 32 / kLanes heads at once and takes every `share`-th such group, from group `first`; kInFlight of
-// them are loaded before the first is worked on.
-template <int D, bool kTurn>
-__device__ __forceinline__ void walk_heads(const RotateParams &p, const Turner<D> &t, const __nv_bfloat16 *src, __nv_bfloat16 *dst, int heads,
-                                           int dst_stride, int first, const __nv_bfloat16 *weight) {
-    constexpr int kGroup = 32 / Turner<D>::kLanes;
-    const int sub = (threadIdx.x & 31) / Turner<D>::kLanes, step = kGroup * p.share;
-    float2 w[4];
-    if (kTurn && p.q_weight) {
-        const Raw r = t.paired(t.load(weight));
-        w[0] = unpack(r.a.x); w[1] = unpack(r.a.y); w[2] = unpack(r.b.x); w[3] = unpack(r.b.y);
+// What one kind of heads (queries or keys) is multiplied with: the table entries and the norm's weights in one.
+template <int D, bool kInter>
+struct Factors {
+    float2 ac[2], bs[2], bc[2], as[2];   // first elements by cos, second ones by -sin; second ones by cos, first ones by sin
+    __device__ __forceinline__ void init(const RotateParams &p, const Turner<D, kInter> &t, const __nv_bfloat16 *weight) {
+        float2 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = make_float2(1.f, 1.f);
+        if (p.q_weight) {
+            const Raw r = t.paired(Raw{*reinterpret_cast<const uint2 *>(weight + t.ea), *reinterpret_cast<const uint2 *>(weight + t.eb)});
+            w[0] = unpack(r.a.x); w[1] = unpack(r.a.y); w[2] = unpack(r.b.x); w[3] = unpack(r.b.y);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (t.at >= 0) {
+                ac[i] = __fmul2_rn(w[i], t.c[i]);
+                bs[i] = __fmul2_rn(w[i + 2], make_float2(-t.s[i].x, -t.s[i].y));
+                bc[i] = __fmul2_rn(w[i + 2], t.c[i]);
+                as[i] = __fmul2_rn(w[i], t.s[i]);
+            } else {
+                ac[i] = w[i];
+                bc[i] = w[i + 2];
+                bs[i] = as[i] = make_float2(0.f, 0.f);
+            }
+        }
     }
-    for (int x0 = first * kGroup; x0 < heads; x0 += step * kInFlight) {
+    // Warp-collective (all heads of a warp at once).
+    __device__ __forceinline__ Raw turn(const RotateParams &p, const Turner<D, kInter> &t, const Raw &raw) const {
+        const Raw r = t.paired(raw);
+        const float2 a[2] = {unpack(r.a.x), unpack(r.a.y)}, b[2] = {unpack(r.b.x), unpack(r.b.y)};
+        float2 y[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            y[i] = __fmul2_rn(a[i], ac[i]);
+            y[i + 2] = __fmul2_rn(b[i], bc[i]);
+            if (t.at >= 0) {   // (not by a factor of zero: the other element may be infinite)
+                y[i] = __ffma2_rn(b[i], bs[i], y[i]);
+                y[i + 2] = __ffma2_rn(a[i], as[i], y[i + 2]);
+            }
+        }
+        if (p.q_weight) {
+            float2 sq = __fmul2_rn(a[0], a[0]);
+            sq = __ffma2_rn(a[1], a[1], sq);
+            sq = __ffma2_rn(b[0], b[0], sq);
+            sq = __ffma2_rn(b[1], b[1], sq);
+            float ss = sq.x + sq.y;
+#pragma unroll
+            for (int d = Turner<D, kInter>::kLanes / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+            const float f = rsqrtf(ss * (1.f / D) + p.eps);
+            const float2 f2 = make_float2(f, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = __fmul2_rn(y[i], f2);
+        }
+        return t.paired(Raw{make_uint2(pack(y[0]), pack(y[1])), make_uint2(pack(y[2]), pack(y[3]))});
+    }
+};
+
+// One kind of a token's heads (queries, keys or values): from `src` to `dst`, where heads are kStride elements apart.
+// A warp handles 32 / kLanes heads at once and takes every `share`-th such group, from group `first`; kInFlight of
+// them are loaded before the first is worked on.  kShare 1: all groups, at offsets known to the compiler.
+template <int D, bool kInter, int kShare, int kStride, bool kTurn>
+__device__ __forceinline__ void walk_heads(const RotateParams &p, const Turner<D, kInter> &t, const __nv_bfloat16 *src, __nv_bfloat16 *dst, int heads,
+                                           int first, const __nv_bfloat16 *weight) {
+    constexpr int kGroup = 32 / Turner<D, kInter>::kLanes;
+    const int sub = (threadIdx.x & 31) / Turner<D, kInter>::kLanes, step = kShare == 1 ? kGroup : kGroup * p.share;
+    Factors<D, kInter> by;
+    if (kTurn) by.init(p, t, weight);
+    int x = first * kGroup + sub;
+    const __nv_bfloat16 *sa = src + x * D + t.ea, *sb = src + x * D + t.eb;
+    __nv_bfloat16 *da = dst + (size_t)x * kStride + t.ea, *db = dst + (size_t)x * kStride + t.eb;
+    for (; x - sub + step * (kInFlight - 1) + kGroup <= heads; x += step * kInFlight) {
         Raw raw[kInFlight];
 #pragma unroll
-        for (int i = 0; i < kInFlight; ++i)
-            if (x0 + sub + i * step < heads) raw[i] = t.load(src + (x0 + sub + i * step) * D);
+        for (int i = 0; i < kInFlight; ++i) {
+            raw[i].a = *reinterpret_cast<const uint2 *>(sa + i * step * D);
+            raw[i].b = *reinterpret_cast<const uint2 *>(sb + i * step * D);
+        }
 #pragma unroll
         for (int i = 0; i < kInFlight; ++i) {
-            const Raw y = kTurn ? t.turn(p, raw[i], w) : raw[i];
-            if (x0 + sub + i * step < heads) t.store(dst + (size_t)(x0 + sub + i * step) * dst_stride, y);
+            const Raw y = kTurn ? by.turn(p, t, raw[i]) : raw[i];
+            *reinterpret_cast<uint2 *>(da + (size_t)(i * step) * kStride) = y.a;
+            *reinterpret_cast<uint2 *>(db + (size_t)(i * step) * kStride) = y.b;
         }
+        sa += kInFlight * step * D;
+        sb += kInFlight * step * D;
+        da += (size_t)(kInFlight * step) * kStride;
+        db += (size_t)(kInFlight * step) * kStride;
+    }
+#pragma unroll 1
+    for (; x - sub < heads; x += step) {   // the last few groups, the very last perhaps not whole
+        Raw raw{};
+        if (x < heads) {
+            raw.a = *reinterpret_cast<const uint2 *>(sa);
+            raw.b = *reinterpret_cast<const uint2 *>(sb);
+        }
+        const Raw y = kTurn ? by.turn(p, t, raw) : raw;
+        if (x < heads) {
+            *reinterpret_cast<uint2 *>(da) = y.a;
+            *reinterpret_cast<uint2 *>(db) = y.b;
+        }
+        sa += step * D;
+        sb += step * D;
+        da += (size_t)step * kStride;
+        db += (size_t)step * kStride;
     }
 }
 
 // A token's heads as this warp has them: every p.share-th group of all heads, queries first, then keys, then values.
-template <int D>
+template <int D, bool kInter, int kShare>
 struct Token {
-    static constexpr int kGroup = 32 / Turner<D>::kLanes;
+    static constexpr int kGroup = 32 / Turner<D, kInter>::kLanes;
     const __nv_bfloat16 *q, *k, *v;
     int q_first, k_first, v_first;   // this warp's first group of each kind
 
@@ -143,9 +189,9 @@ struct Token {
     }
     // Asks for the warp's rows (its first ones, if it has but a share of them), so that they are under way while it finds
     // out where they go.
-    __device__ __forceinline__ void prefetch(const RotateParams &p, const Turner<D> &t, int lane) const {
+    __device__ __forceinline__ void prefetch(const RotateParams &p, const Turner<D, kInter> &t, int lane) const {
         auto ask = [&](const __nv_bfloat16 *at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); };
-        if (p.share == 1) {
+        if (kShare == 1) {
             for (int i = lane * 64; i < p.Hq * D; i += 32 * 64) ask(q + i);
             for (int i = lane * 64; i < p.Hkv * D; i += 32 * 64) {
                 ask(k + i);
@@ -153,7 +199,7 @@ struct Token {
             }
             return;
         }
-        const int sub = lane / Turner<D>::kLanes;
+        const int sub = lane / Turner<D, kInter>::kLanes;
         auto ask_head = [&](const __nv_bfloat16 *head) {
             ask(head + t.ea);
             if (t.eb - t.ea >= 64) ask(head + t.eb);
@@ -166,11 +212,12 @@ struct Token {
         if (k_first * kGroup + sub < p.Hkv) ask_head(k + (k_first * kGroup + sub) * D);
         if (v_first * kGroup + sub < p.Hkv) ask_head(v + (v_first * kGroup + sub) * D);
     }
-    __device__ __forceinline__ void move(const RotateParams &p, const Turner<D> &t, __nv_bfloat16 *q_dst, __nv_bfloat16 *k_dst, __nv_bfloat16 *v_dst,
-                                         int kv_stride) const {
-        walk_heads<D, true>(p, t, q, q_dst, p.Hq, D, q_first, p.q_weight);
-        walk_heads<D, true>(p, t, k, k_dst, p.Hkv, kv_stride, k_first, p.k_weight);
-        walk_heads<D, false>(p, t, v, v_dst, p.Hkv, kv_stride, v_first, nullptr);
+    template <int kStride>
+    __device__ __forceinline__ void move(const RotateParams &p, const Turner<D, kInter> &t, __nv_bfloat16 *q_dst, __nv_bfloat16 *k_dst,
+                                         __nv_bfloat16 *v_dst) const {
+        walk_heads<D, kInter, kShare, D, true>(p, t, q, q_dst, p.Hq, q_first, p.q_weight);
+        walk_heads<D, kInter, kShare, kStride, true>(p, t, k, k_dst, p.Hkv, k_first, p.k_weight);
+        walk_heads<D, kInter, kShare, kStride, false>(p, t, v, v_dst, p.Hkv, v_first, nullptr);
     }
 };
 
@@ -196,13 +243,14 @@ __device__ __forceinline__ int append_status(const RotateParams &p, int b, int n
 
 // Warps 0 .. tokens * share - 1: one token's heads, or a share of them.  Warps behind them: one sequence's status
 // word each.
-template <int D>
+template <int D, bool kInter, int kShare>
 __global__ void __launch_bounds__(kThreads, 3) prompt_append_kernel(const RotateParams p) {
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), writers = (int64_t)p.tokens * p.share;
-    const int token = w < writers ? (int)(w / p.share) : -1;
+    const int share = kShare == 1 ? 1 : p.share;
+    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), writers = (int64_t)p.tokens * share;
+    const int token = w < writers ? (int)(w / share) : -1;
     if (w >= writers + p.B) return;
     // One pass over token_start: is it in order, and whose token is this (-1: nobody's)?
     int start = 0, n = 0;
@@ -227,37 +275,37 @@ __global__ void __launch_bounds__(kThreads, 3) prompt_append_kernel(const Rotate
         if (lane == 0) p.status[w - writers] = st;
         return;
     }
-    Turner<D> t;
+    Turner<D, kInter> t;
     t.init(p, lane);
-    const int first = (int)(w % p.share);
-    Token<D> tok;
+    const int first = (int)(w % share);
+    Token<D, kInter, kShare> tok;
     tok.init(p, token, first);
     tok.prefetch(p, t, lane);
     const int b = owner();
     if (b < 0) return;
     __nv_bfloat16 *q_row = p.q_out + (size_t)token * p.Hq * D;
     const int L = p.seq_lens[b];
-    if (append_status(p, b, n, L, lane) != READER_OK) return zero_heads<D>(q_row, p.Hq, first, p.share, lane);
+    if (append_status(p, b, n, L, lane) != READER_OK) return zero_heads<D>(q_row, p.Hq, first, share, lane);
     const int pos = L + (token - start);
     t.load_table(p, pos);
     const int page = p.page_table[(size_t)b * p.max_pages + pos / kPage];
     const size_t at = ((size_t)page * p.Hkv * kPage + pos % kPage) * D;
-    tok.move(p, t, q_row, p.k_out + at, p.v_out + at, kPage * D);
+    tok.template move<kPage * D>(p, t, q_row, p.k_out + at, p.v_out + at);
 }
 
 // Block (y, b): the warps y * 8 .. y * 8 + 7 of sequence b; warp j * share + s: node j of its tree, or a share of its heads.
-template <int D>
-__global__ void __launch_bounds__(kThreads, 4) tree_rotate_kernel(const RotateParams p) {
+template <int D, bool kInter, int kShare>
+__global__ void __launch_bounds__(kThreads, 3) tree_rotate_kernel(const RotateParams p) {
     __shared__ int32_t par[kMaxNodes];
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, blocks = (p.T * p.share + kThreads / 32 - 1) / (kThreads / 32);
+    const int share = kShare == 1 ? 1 : p.share, lane = threadIdx.x & 31, blocks = (p.T * share + kThreads / 32 - 1) / (kThreads / 32);
     const int b = blockIdx.x / blocks, w = (blockIdx.x - b * blocks) * (kThreads / 32) + (threadIdx.x >> 5);
-    const int j = w / p.share, first = w - j * p.share;
+    const int j = w / share, first = w - j * share;
     const int64_t row = (int64_t)b * p.T + min(j, p.T - 1);
-    Turner<D> t;
+    Turner<D, kInter> t;
     t.init(p, lane);
-    Token<D> tok;
+    Token<D, kInter, kShare> tok;
     tok.init(p, row, first);
     tok.prefetch(p, t, lane);
     const int L = p.seq_lens[b];
@@ -289,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 4) tree_rotate_kernel(const RotatePa
         return;
     }
     t.load_table(p, (int64_t)L + nodes_above(j));
-    tok.move(p, t, q_row, k_row, v_row, D);
+    tok.template move<D>(p, t, q_row, k_row, v_row);
 }
 
 // Warps per token: one, unless that leaves the GPU short of warps (16 an SM); a power of two, no more than give every
@@ -304,15 +352,22 @@ dim3 blocks_for(int64_t warps) { return dim3((unsigned)((warps + kThreads / 32 -
 
 }  // namespace
 
+// The kernel for the head dimension, the kind of pairs and whether tokens are shared among warps.
+#define ROTATE_KERNEL(name, p)                                                                                               \
+    ((p).D == 128 ? ((p).interleaved ? ((p).share == 1 ? name<128, true, 1> : name<128, true, 0>)                           \
+                                     : ((p).share == 1 ? name<128, false, 1> : name<128, false, 0>))                        \
+                  : ((p).interleaved ? ((p).share == 1 ? name<64, true, 1> : name<64, true, 0>)                             \
+                                     : ((p).share == 1 ? name<64, false, 1> : name<64, false, 0>)))
+
 void launch_prompt_append(RotateParams p, int n_sm, cudaStream_t st) {
     p.share = warps_per_token(p.tokens, p.Hq + 2 * p.Hkv, p.D, n_sm);
-    launch_pdl(p.D == 128 ? prompt_append_kernel<128> : prompt_append_kernel<64>, blocks_for((int64_t)p.tokens * p.share + p.B), dim3(kThreads), 0, st, p);
+    launch_pdl(ROTATE_KERNEL(prompt_append_kernel, p), blocks_for((int64_t)p.tokens * p.share + p.B), dim3(kThreads), 0, st, p);
 }
 
 void launch_tree_rotate(RotateParams p, int n_sm, cudaStream_t st) {
-    const int64_t nodes = (int64_t)p.B * p.T;
-    p.share = warps_per_token(nodes, p.Hq + 2 * p.Hkv, p.D, n_sm);
-    launch_pdl(p.D == 128 ? tree_rotate_kernel<128> : tree_rotate_kernel<64>, dim3((unsigned)(p.B * ((p.T * p.share + kThreads / 32 - 1) / (kThreads / 32)))), dim3(kThreads), 0, st, p);
+    p.share = warps_per_token((int64_t)p.B * p.T, p.Hq + 2 * p.Hkv, p.D, n_sm);
+    const int per_seq = (p.T * p.share + kThreads / 32 - 1) / (kThreads / 32);
+    launch_pdl(ROTATE_KERNEL(tree_rotate_kernel, p), dim3((unsigned)(p.B * per_seq)), dim3(kThreads), 0, st, p);
 }
 
 }  // namespace reader
