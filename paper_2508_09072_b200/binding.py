@@ -1,4 +1,4 @@
-"""ctypes binding of ``libreader_verify.so``: argument marshalling only.
+"""Binding of ``libreader_verify.so``: argument marshalling only (ctypes; a native module for the prompt calls).
 
 Every step of the verification path runs in the library's CUDA kernels.  PyTorch is used for
 device memory and streams; tensors are passed as raw device pointers.  bf16 tensors are
@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_float, c_int32, c_size_t, c_void_p
 from dataclasses import dataclass
 from typing import Optional
 
@@ -50,15 +50,6 @@ class _PaddedCache(Structure):
 
 class _Tree(Structure):
     _fields_ = [("batch", c_int32), ("n_nodes", c_int32), ("parent", c_void_p), ("anc_mask", c_void_p)]
-
-
-class _Prompt(Structure):
-    _fields_ = [("batch", c_int32), ("total_tokens", c_int32), ("token_start", c_void_p)]
-
-
-class _Rotation(Structure):
-    _fields_ = [("q_weight", c_void_p), ("k_weight", c_void_p), ("eps", c_float), ("rope", c_void_p),
-                ("max_positions", c_int32), ("rot_dim", c_int32), ("interleaved", c_int32)]
 
 
 _lib = None
@@ -131,23 +122,23 @@ def load_library() -> ctypes.CDLL:
     lib.reader_padded_append.restype = c_int32
     lib.reader_padded_rearrange.argtypes = [c_void_p, POINTER(_PaddedCache), c_int32, c_void_p, c_void_p]
     lib.reader_padded_rearrange.restype = c_int32
-    lib.reader_prompt_append.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int32,
-                                         POINTER(_KvCache), POINTER(_Prompt), POINTER(_Rotation), c_void_p, c_void_p, c_void_p]
-    lib.reader_prompt_append.restype = c_int32
-    lib.reader_tree_rotate.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int32, c_int32,
-                                       c_int32, POINTER(_Tree), c_void_p, POINTER(_Rotation), c_void_p, c_void_p, c_void_p,
-                                       c_void_p, c_void_p]
-    lib.reader_tree_rotate.restype = c_int32
     lib.reader_prompt_workspace_bytes.argtypes = [c_void_p, c_int32]
     lib.reader_prompt_workspace_bytes.restype = c_size_t
-    lib.reader_prompt_attn.argtypes = [c_void_p, c_void_p, c_int32, POINTER(_KvCache), POINTER(_Prompt), c_float, c_int32,
-                                       c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
-    lib.reader_prompt_attn.restype = c_int32
     lib.reader_kv_commit.argtypes = [c_void_p, POINTER(_KvCache), c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                                      c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
     lib.reader_kv_commit.restype = c_int32
     _lib = lib
     return lib
+
+
+def load_native():
+    """The native module that marshals the prompt calls (it links the same shared library)."""
+    load_library()
+    try:
+        from . import _marshal
+    except ImportError as e:
+        raise ImportError(f"{os.path.join(_HERE, '_marshal.so')} cannot be loaded: build it with `python -m paper_2508_09072_b200.build` ({e})") from e
+    return _marshal
 
 
 def status_string(code: int) -> str:
@@ -217,6 +208,7 @@ class Reader:
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2508_09072_b200 needs a CUDA device; there is no CPU fallback")
         self.lib = load_library()
+        self._native = load_native()
         self.device = int(device)
         torch.cuda.set_device(self.device)
         torch.zeros(1, device=f"cuda:{self.device}")   # make sure the context exists
@@ -562,94 +554,9 @@ class Reader:
         return slots, status
 
     # ---- from a prompt to a cache, from a projection to a tree
-    # (These calls may be as short as a few microseconds on the GPU: the checks below are one pass over each argument and
-    # tensors travel as plain addresses.)
-    def _have(self, t: torch.Tensor, dtype, name: str) -> int:
-        """The address of a contiguous tensor of that dtype on this reader's device."""
-        if t.get_device() != self.device:
-            if not t.is_cuda:
-                raise TypeError(f"{name}: need a contiguous CUDA tensor of dtype {dtype}")
-            raise ValueError(f"{name} is on {t.device}, this reader on cuda:{self.device}")
-        if t.dtype is not dtype or not t.is_contiguous():
-            raise TypeError(f"{name}: need a contiguous CUDA tensor of dtype {dtype}")
-        return t.data_ptr()
-
-    def _heads(self, t: torch.Tensor, shape, name: str):
-        """Address and token stride of a bf16 tensor [..., heads, head_dim] whose heads are dense and whose tokens are evenly
-        spaced: a tensor of its own or a part of a fused projection's output."""
-        if t.get_device() != self.device or t.dtype is not torch.bfloat16:
-            if t.is_cuda and t.dtype is torch.bfloat16:
-                raise ValueError(f"{name} is on {t.device}, this reader on cuda:{self.device}")
-            raise TypeError(f"{name}: need a CUDA tensor of dtype {torch.bfloat16}")
-        if t.shape != shape:
-            raise ValueError(f"{name}: need shape {tuple(shape)}, got {tuple(t.shape)}")
-        stride, heads, d = t.stride(), shape[-2], shape[-1]
-        if 0 in shape:
-            return t.data_ptr(), heads * d
-        if stride[-1] != 1 or (heads > 1 and stride[-2] != d):
-            raise ValueError(f"{name}: the heads of a token must be dense")
-        if len(shape) == 3:
-            return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
-        b, n = shape[0], shape[1]
-        if b > 1 and n > 1 and stride[0] != n * stride[1]:
-            raise ValueError(f"{name}: the tokens must be evenly spaced")
-        return t.data_ptr(), stride[1] if n > 1 else stride[0] if b > 1 else heads * d
-
-    def _paged(self, c: KvCache) -> _KvCache:
-        """The cache's C struct.  It is kept with the cache object for as long as that names the same tensors, at the same
-        addresses and of the same shapes."""
-        k, v, table, lens = c.k_pool, c.v_pool, c.page_table, c.seq_lens
-        key = (k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), k.shape, table.shape, c.shared_prefix_len)
-        kept = c.__dict__.get("_kept")
-        if kept is not None and kept[0] is k and kept[1] is v and kept[2] is table and kept[3] is lens and kept[4] == key and kept[5] == self.device:
-            return kept[6]
-        pages, heads, page, d = k.shape
-        batch, width = table.shape
-        if v.shape != k.shape or lens.shape != (batch,):
-            raise ValueError("v_pool: the shape of k_pool; seq_lens: one length for each row of the page table")
-        have = self._have
-        st = _KvCache(have(k, torch.bfloat16, "k_pool"), have(v, torch.bfloat16, "v_pool"), pages, page, heads, d,
-                      have(table, torch.int32, "page_table"), width, have(lens, torch.int32, "seq_lens"), int(c.shared_prefix_len))
-        c.__dict__["_kept"] = (k, v, table, lens, key, self.device, st)
-        return st
-
-    def _rotation(self, head_dim: int, rope, q_weight, k_weight, eps: float, interleaved: bool) -> _Rotation:
-        q = k = r = None
-        positions = rot = 0
-        if q_weight is not None:
-            q = self._have(q_weight, torch.bfloat16, "q_weight")
-            if q_weight.shape != (head_dim,):
-                raise ValueError(f"q_weight: need shape ({head_dim},)")
-        if k_weight is not None:
-            k = self._have(k_weight, torch.bfloat16, "k_weight")
-            if k_weight.shape != (head_dim,):
-                raise ValueError(f"k_weight: need shape ({head_dim},)")
-        if rope is not None:
-            r = self._have(rope, torch.float32, "rope")
-            shape = rope.shape
-            if len(shape) != 3 or shape[1] != 2:
-                raise ValueError("rope: need [max_positions, 2, rot_dim / 2]")
-            positions, rot = shape[0], 2 * shape[2]
-        return _Rotation(q, k, eps, r, positions, rot, 1 if interleaved else 0)
-
-    def _prompt(self, batch: int, token_start: torch.Tensor, tokens: int) -> _Prompt:
-        if token_start.shape != (batch + 1,):
-            raise ValueError("token_start: one entry more than the cache has sequences")
-        return _Prompt(batch, tokens, self._have(token_start, torch.int32, "token_start"))
-
-    def _status(self, status: Optional[torch.Tensor], like: torch.Tensor, batch: int):
-        if status is None:
-            status = like.new_empty(batch)
-        elif status.shape != (batch,):
-            raise ValueError("status: one word for each sequence")
-        return status, self._have(status, torch.int32, "status")
-
-    def _out(self, out: Optional[torch.Tensor], like: torch.Tensor, name: str):
-        if out is None:
-            out = torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
-        elif out.shape != like.shape:
-            raise ValueError(f"{name}: need shape {tuple(like.shape)}, got {tuple(out.shape)}")
-        return out, self._have(out, torch.bfloat16, name)
+    # (checked and marshalled by the native module, csrc/marshal.cpp: these calls may be as short as 4 us on the GPU)
+    def _handle(self) -> int:
+        return self._h.value if self._h else 0   # (the library refuses a closed reader)
 
     def prompt_append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: KvCache, token_start: torch.Tensor,
                       rope: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
@@ -657,18 +564,9 @@ class Reader:
                       out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """Head norms, rotation and cache write of packed new tokens: q [tokens, Hq, D], k and v [tokens, Hkv, D] (views of
         a fused projection are fine), rope f32 [max_positions, 2, rot_dim / 2].  Returns (rotated queries, status)."""
-        c = self._paged(cache)
-        tokens, Hq, D = q.shape
-        if D != c.head_dim:
-            raise ValueError("q: its head dimension is not the cache's")
-        kv = (tokens, c.n_kv_heads, D)
-        (qp, qs), (kp, ks), (vp, vs) = self._heads(q, (tokens, Hq, D), "q"), self._heads(k, kv, "k"), self._heads(v, kv, "v")
-        batch = cache.page_table.shape[0]
-        p, r = self._prompt(batch, token_start, tokens), self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
-        out, op = self._out(out, q, "out")
-        status, sp = self._status(status, token_start, batch)
-        st = self.lib.reader_prompt_append(self._h, qp, kp, vp, qs, ks, vs, Hq, ctypes.byref(c), ctypes.byref(p), ctypes.byref(r), op, sp,
-                                           _raw_stream())
+        st, out, status = self._native.prompt_append(self._handle(), self.device, q, k, v, cache.k_pool, cache.v_pool, cache.page_table,
+                                                     cache.seq_lens, cache.shared_prefix_len, token_start, rope, q_weight, k_weight, eps,
+                                                     interleaved, out, status)
         if st != OK:
             raise ReaderError(st, "reader_prompt_append")
         return out, status
@@ -680,20 +578,8 @@ class Reader:
                     v_tree: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """The same for draft nodes: q [B, T, Hq, D], k and v [B, T, Hkv, D], parent [B, T].  Returns
         (q, k_tree, v_tree, status) for verify_attn and kv_commit."""
-        B, T, Hq, D = q.shape
-        Hkv = k.shape[2]
-        kv = (B, T, Hkv, D)
-        (qp, qs), (kp, ks), (vp, vs) = self._heads(q, (B, T, Hq, D), "q"), self._heads(k, kv, "k"), self._heads(v, kv, "v")
-        if parent.shape != (B, T) or seq_lens.shape != (B,):
-            raise ValueError("parent: [B, T]; seq_lens: [B]")
-        tr = _Tree(B, T, self._have(parent, torch.int32, "parent"), None)
-        r = self._rotation(D, rope, q_weight, k_weight, eps, interleaved)
-        out, op = self._out(out, q, "out")
-        k_tree, ko = self._out(k_tree, k, "k_tree")
-        v_tree, vo = self._out(v_tree, v, "v_tree")
-        status, sp = self._status(status, parent, B)
-        st = self.lib.reader_tree_rotate(self._h, qp, kp, vp, qs, ks, vs, Hq, Hkv, D, ctypes.byref(tr), self._have(seq_lens, torch.int32, "seq_lens"),
-                                         ctypes.byref(r), op, ko, vo, sp, _raw_stream())
+        st, out, k_tree, v_tree, status = self._native.tree_rotate(self._handle(), self.device, q, k, v, seq_lens, parent, rope, q_weight,
+                                                                   k_weight, eps, interleaved, out, k_tree, v_tree, status)
         if st != OK:
             raise ReaderError(st, "reader_tree_rotate")
         return out, k_tree, v_tree, status
@@ -710,23 +596,11 @@ class Reader:
                     workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """Causal attention of packed new tokens, whose K and V are in the cache at seq_lens[b] + i, over the cache:
         q [tokens, Hq, D].  Returns (out, status); lse f32 [tokens, Hq] is filled if given."""
-        c = self._paged(cache)
-        tokens, Hq, D = q.shape
-        if D != c.head_dim:
-            raise ValueError("q: its head dimension is not the cache's")
-        batch = cache.page_table.shape[0]
-        p = self._prompt(batch, token_start, tokens)
-        qp = self._have(q, torch.bfloat16, "q")
-        out, op = self._out(out, q, "out")
-        status, sp = self._status(status, token_start, batch)
-        lp = None
-        if lse is not None:
-            lp = self._have(lse, torch.float32, "lse")
-            if lse.shape != (tokens, Hq):
-                raise ValueError("lse: [tokens, Hq]")
-        ws = self.prompt_workspace() if workspace is None else workspace
-        st = self.lib.reader_prompt_attn(self._h, qp, Hq, ctypes.byref(c), ctypes.byref(p), scale, 1 if update_seq_lens else 0, op, lp,
-                                         self._have(ws, torch.uint8, "workspace"), ws.numel(), sp, _raw_stream())
+        ws = self._prompt_ws if workspace is None else workspace
+        if ws is None:
+            ws = self.prompt_workspace()
+        st, out, status = self._native.prompt_attn(self._handle(), self.device, q, cache.k_pool, cache.v_pool, cache.page_table, cache.seq_lens,
+                                                   cache.shared_prefix_len, token_start, scale, update_seq_lens, out, lse, ws, status)
         if st != OK:
             raise ReaderError(st, "reader_prompt_attn")
         return out, status

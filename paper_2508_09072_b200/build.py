@@ -1,4 +1,4 @@
-"""Builds ``libreader_verify.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds ``libreader_verify.so`` (nvcc, sm_100a) and the Python module ``_marshal`` (g++) in-tree, without a GPU."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libreader_verify.so")
+MARSHAL = os.path.join(_HERE, "_marshal.so")   # csrc/marshal.cpp: torch tensors in, C ABI calls out
 
 SOURCES = ["api.cu", "tree_encode.cu", "verify_attn_generic.cu", "verify_attn_sm100.cu", "combine.cu",
            "accept.cu", "accept_noalloc.cu", "sample.cu", "kv_commit.cu", "kv_rearrange.cu", "padded_cache.cu", "accept_commit.cu",
@@ -25,9 +26,33 @@ def _newest_source() -> float:
     return t
 
 
+def _marshal_command(out: str) -> list:
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    lib = os.path.join(root, "lib")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+            "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], "-isystem", "/usr/local/cuda/include",
+            os.path.join(CSRC, "marshal.cpp"), "-o", out, "-L", lib, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10",
+            "-L", _HERE, "-l:libreader_verify.so", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{lib}"]
+
+
+def _build_marshal(verbose: bool = False) -> None:
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    p = subprocess.run(_marshal_command(tmp), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if p.returncode != 0 or verbose:
+        sys.stderr.write(f"--- marshal.cpp\n{p.stdout}\n")
+    if p.returncode != 0:
+        raise RuntimeError("g++ failed")
+    os.replace(tmp, MARSHAL)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu into objects under csrc/_build and link the shared library."""
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source():
+    """Compile every .cu into objects under csrc/_build and link the shared library; then the Python module."""
+    newest = _newest_source()
+    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= newest for f in (LIB, MARSHAL)):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     bdir = os.path.join(CSRC, "_build")
@@ -50,6 +75,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + f".tmp{os.getpid()}"
     subprocess.check_call([nvcc, "-shared", "-o", tmp, *objs, "-lcudart"])
     os.replace(tmp, LIB)
+    _build_marshal(verbose)
     return LIB
 
 
