@@ -149,10 +149,50 @@ struct Schedule {
         start = p.token_start[b];
         blocks = blocks_of(p, b, n, L);
     }
+    // The single-launch form's only piece: unit blockIdx.x.  One look at the lengths, for a batch of up to 32 sequences.
+    __device__ __forceinline__ bool alone(const PromptAttnParams &p, Piece &s, int lane) {
+        const int i = blockIdx.x;
+        bool bad = false, found = false;
+        first = b = h = block = start = L = n = blocks = 0;
+        s.nt = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            int a = 0, n_ = 0, L_ = 0, m = 0;
+            if (b0 + lane < p.B) {
+                a = p.token_start[b0 + lane];
+                const int e = p.token_start[b0 + lane + 1];
+                L_ = p.seq_lens[b0 + lane];
+                bad |= a < 0 || a > e || e > p.tokens;
+                n_ = e - a;
+                if (!bad && prompt_len_ok(L_, n_, p.max_pages)) m = unit_blocks(n_, p.tile_tokens);
+            }
+            const int incl = inclusive_sum(m * p.Hkv, lane);
+            const unsigned here = __ballot_sync(0xffffffffu, i - first < incl);
+            if (here && !found) {
+                const int src = __ffs(here) - 1;
+                found = true;
+                b = b0 + src;
+                start = __shfl_sync(0xffffffffu, a, src);
+                n = __shfl_sync(0xffffffffu, n_, src);
+                L = __shfl_sync(0xffffffffu, L_, src);
+                blocks = __shfl_sync(0xffffffffu, m, src);
+                block = i - first - __shfl_sync(0xffffffffu, incl - m * p.Hkv, src);   // its place among the sequence's units
+            }
+            first += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (__any_sync(0xffffffffu, bad) || !found) return false;
+        h = block % p.Hkv;
+        block = block / p.Hkv;
+        describe(p, s);
+        s.t0 = 0;
+        s.nt = s.u.tiles;
+        s.full = true;
+        s.slot = 0;
+        return true;
+    }
     // sizes: scratch in shared memory, [B]
     __device__ __forceinline__ void init(const PromptAttnParams &p, int32_t *sizes, int lane) {
         w = left = w0 = W = ctas = b = h = block = off = start = L = n = blocks = first = 0;
-        const bool dealt = !p.counter && !p.alone;
+        const bool dealt = !p.counter;
         bool bad = false;
         int total = 0;   // entries of one head of every sequence so far
         for (int b0 = 0; b0 < p.B; b0 += 32) {
@@ -228,15 +268,11 @@ struct Schedule {
     // The next piece with at least one key tile; false when there is no more.
     __device__ __forceinline__ bool next(const PromptAttnParams &p, Piece &s, int lane) {
         s.nt = 0;
-        if (p.counter || p.alone) {
+        if (p.counter) {
             if (b >= p.B) return false;
-            int i = blockIdx.x;
-            if (p.alone) {
-                if (w++ > 0) return false;
-            } else {
-                if (lane == 0) i = atomicAdd(p.counter, 1);
-                i = __shfl_sync(0xffffffffu, i, 0);
-            }
+            int i = 0;
+            if (lane == 0) i = atomicAdd(p.counter, 1);
+            i = __shfl_sync(0xffffffffu, i, 0);
             while (true) {
                 int n_ = 0, L_ = 0, m = 0;
                 if (b + lane < p.B) m = blocks_of(p, b + lane, n_, L_) * p.Hkv;
@@ -260,15 +296,6 @@ struct Schedule {
             s.nt = s.u.tiles;
             s.full = true;
             s.slot = 0;
-            if (p.alone) {
-                bool bad = false;
-                for (int k = lane; k < (L + n + kPage - 1) / kPage; k += 32) {
-                    const int pg = p.page_table[(size_t)b * p.max_pages + k];
-                    bad |= pg < 0 || pg >= p.num_pages;
-                }
-                s.reject = __any_sync(0xffffffffu, bad);
-                if (h == 0 && block == 0 && lane == 0) p.status[b] = s.reject ? READER_ERR_BAD_PAGE : READER_OK;
-            }
             return true;
         }
         while (left > 0) {
@@ -451,9 +478,11 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         if (lane == 0) p.pieces[blockIdx.x].b = -1;
         __syncwarp();
         Schedule schedule;
-        schedule.init(p, reinterpret_cast<int32_t *>(smem + C::kOffRing), lane);
-        if (lane == 0) fence_proxy_async();   // the ring was scratch until here
-        __syncwarp();
+        if (!p.alone) {
+            schedule.init(p, reinterpret_cast<int32_t *>(smem + C::kOffRing), lane);
+            if (lane == 0) fence_proxy_async();   // the ring was scratch until here
+            __syncwarp();
+        }
         Piece s;
         const uint64_t stream_policy = l2_policy_evict_first();
         auto load = [&](PageCursor &cursor, const CUtensorMap *map, int j, bool values) {
@@ -481,7 +510,11 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         };
         const int tile_rows_bytes = p.G * p.tile_tokens * 128;
         while (!*abort_s) {
-            const bool more = schedule.next(p, s, lane);
+            bool more;
+            if (!p.alone) more = schedule.next(p, s, lane);
+            else if (seg == 0) more = schedule.alone(p, s, lane);
+            else more = false;
+            if (!more) s.nt = 0;
             const int i = seg % kPieces;
             if (!wait(bar(&m->piece_empty[i]), ((seg / kPieces) & 1) ^ 1, abort_s)) break;
             if (lane == 0) {
@@ -492,6 +525,16 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             if (!more) break;
             const int ahead = ahead_of(s);
             PageCursor kc, vc;
+            bool bad_page = false;
+            if (p.alone) {   // the sequence's pages, to be looked at below; the first 32 serve the loads too
+                const int npages = (s.L + s.n + kPage - 1) / kPage;
+                kc.loaded = vc.loaded = true;
+                if (lane < npages) {
+                    kc.id = p.page_table[(size_t)s.b * p.max_pages + lane];
+                    bad_page = kc.id < 0 || kc.id >= p.num_pages;
+                }
+                vc.id = kc.id;
+            }
             for (int j = 0; j < ahead; ++j) load(kc, &kmap, j, false);
             if (wait(bar(&m->q_empty), (seg & 1) ^ 1, abort_s) && elect_one()) {
                 const uint32_t full = bar(&m->q_full);
@@ -505,6 +548,16 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             }
             __syncwarp();
             ++seg;
+            if (p.alone) {
+                for (int k = 32 + lane; k < (s.L + s.n + kPage - 1) / kPage; k += 32) {
+                    const int pg = p.page_table[(size_t)s.b * p.max_pages + k];
+                    bad_page |= pg < 0 || pg >= p.num_pages;
+                }
+                const bool reject = __any_sync(0xffffffffu, bad_page);
+                if (reject && lane == 0) *(volatile bool *)&m->piece[i].reject = true;
+                __syncwarp();
+                if (s.h == 0 && s.block == 0 && lane == 0) p.status[s.b] = reject ? READER_ERR_BAD_PAGE : READER_OK;
+            }
             for (int j = 0; j < s.nt; ++j) {
                 load(vc, &vmap, j, true);
                 if (j + ahead < s.nt) load(kc, &kmap, j + ahead, false);
@@ -861,7 +914,8 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             }
             const bool poisoned = *(const volatile int32_t *)&sg->poison != 0;
             const bool two = narrow && sg->nt > 1;   // slot 1 has an output to add
-            if (warp_live && (two || poisoned || sg->reject)) {
+            const bool reject = *(const volatile bool *)&sg->reject;
+            if (warp_live && (two || poisoned || reject)) {
                 // what few outputs need is done to the output tile in tensor memory before it is written
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
@@ -891,7 +945,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             }
                         }
                     }
-                    if (sg->reject) {
+                    if (reject) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = 0;
                     }
@@ -901,7 +955,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             }
             if (warp_live) {
                 const bool full = sg->full;
-                const float inv = full && !sg->reject ? 1.f / l_all : 1.f;
+                const float inv = full && !reject ? 1.f / l_all : 1.f;
                 const uint32_t staging = base + C::kOffStaging + warp * 4096;   // 32 rows of 128 bytes, 16-byte pieces swizzled
                 // where this lane's row goes, in rows from the unit's first; -1: nowhere
                 const int to = !live ? -1 : full ? unit_token * p.Hq + row_member : row;
@@ -949,7 +1003,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                     if (!sg->full)
                         *reinterpret_cast<float2 *>(p.partial_ml + ((size_t)(2 * blockIdx.x + sg->slot) * 256 + slot * 128 + row) * 2) = make_float2(m_all, l_all);
                     else if (p.lse)
-                        p.lse[((size_t)sg->start + sg->first_token + unit_token) * p.Hq + (size_t)sg->h * p.G + row_member] = sg->reject ? 0.f : (m_all + log2f(l_all)) * 0.6931471805599453f;
+                        p.lse[((size_t)sg->start + sg->first_token + unit_token) * p.Hq + (size_t)sg->h * p.G + row_member] = reject ? 0.f : (m_all + log2f(l_all)) * 0.6931471805599453f;
                 }
             }
             if (narrow) {
