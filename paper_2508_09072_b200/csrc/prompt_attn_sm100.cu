@@ -685,6 +685,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             pass_to(r0 + 2 * n);
             done();
         }
+        if (*abort_s) __nanosleep(1000000);   // products that are still under way end before their operands go away
     } else if (warp == kValueWarp) {
         // ------------------------------------------------------------------ values some queries do not see; the note on a split unit
         int r0 = 0;

@@ -175,6 +175,105 @@ def test_attn_units_from_the_counter(rd):
         check_attn(rd, q, cache, ns, lens, 0.125)
 
 
+# one sequence of each kind that is turned down, in every form of the call: a single launch (short pages tables), equal
+# ranges (a wide page table), units from the counter (many heads)
+FORMS = [(4, 2, 64, 0), (4, 2, 64, 200), (128, 16, 64, 0)]
+
+
+@pytest.mark.parametrize("form", range(3))
+def test_attn_rejections_in_every_form(rd, form):
+    from paper_2508_09072_b200 import binding
+    Hq, Hkv, D, extra = FORMS[form]
+    rng = np.random.default_rng(40 + form)
+    ns, lens = [300, 40, 0, 310, 20, 300], [70, 10, 0, 100, 30, 0]
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, D, poison=False)
+    if extra:
+        wide = torch.full((len(ns), extra), -1, dtype=torch.int32, device="cuda")
+        wide[:, :cache.page_table.shape[1]] = cache.page_table
+        cache.page_table = wide
+    q = bf16(rng, sum(ns) + 1, Hq, D).cuda()
+    good, st = rd.prompt_attn(q, cache, starts(ns), 0.125)
+    assert st.tolist() == [0] * 6
+    good = good.clone()
+    cache.page_table[1, 0], cache.page_table[3, 6] = -1, cache.k_pool.shape[0]
+    cache.seq_lens[4] = 2 ** 30
+    lse = torch.full((sum(ns) + 1, Hq), 7.0, device="cuda")
+    out = torch.full_like(q, 7.0)
+    _, st = rd.prompt_attn(q, cache, starts(ns), 0.125, out=out, lse=lse)
+    assert st.tolist() == [0, binding.ERR_BAD_PAGE, 0, binding.ERR_BAD_PAGE, binding.ERR_CAPACITY, 0]
+    at = np.concatenate([[0], np.cumsum(ns)])
+    for b in range(6):
+        rows = slice(at[b], at[b + 1])
+        if st[b]:
+            assert not out[rows].any() and not lse[rows].any(), b
+        else:
+            assert torch.equal(out[rows], good[rows]), b
+    assert (out[-1] == 7.0).all() and (lse[-1] == 7.0).all()
+    for bad in ([0, 300, 340, 330, 650, 670, 970], [0, 300, 340, 340, 650, 670, sum(ns) + 2], [-3, 300, 340, 340, 650, 670, 970]):
+        out.fill_(3.0)
+        _, st = rd.prompt_attn(q, cache, torch.tensor(bad, dtype=torch.int32).cuda(), 0.125, out=out)
+        assert st.tolist() == [binding.ERR_INVALID_ARG] * 6 and (out == 3.0).all()
+
+
+def test_attn_infinities_in_long_pieces(rd):
+    """The same as above where the values are looked at ahead of their tiles, and on garbage behind the last key."""
+    rng = np.random.default_rng(43)
+    ns, lens = [300, 300, 301], [1700, 2003, 1500]
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 16, 64)   # NaN and inf behind the last keys
+    for b, j in ((0, 0), (0, 37), (2, 300), (2, 150)):
+        pos = lens[b] + j
+        page = cache.page_table[b, pos // PAGE].long()
+        cache.v_pool[page, ::3, pos % PAGE, 9::13] = float("inf")
+        cache.v_pool[page, 1, pos % PAGE, 4] = float("nan")
+    check_attn(rd, bf16(rng, sum(ns), 32, 64).cuda(), cache, ns, lens, 0.1)
+    ns = [100] * 3
+    lens = [x + 200 for x in lens[:2]] + [1701]
+    cache.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    check_attn(rd, bf16(rng, 300, 32, 64).cuda(), cache, ns, lens, 0.1)
+
+
+def test_attn_very_large_batch(rd):
+    rng = np.random.default_rng(44)
+    B = 3000
+    lens = [int(x) for x in rng.integers(0, 40, B)]
+    ns = [int(x) for x in rng.integers(0, 3, B)]
+    cache = make_cache(rng, lens, [64] * B, 1, 64, poison=False)
+    q = bf16(rng, sum(ns), 2, 64).cuda()
+    check_attn(rd, q, cache, ns, lens, 0.125)
+    k, v = bf16(rng, sum(ns), 1, 64).cuda(), bf16(rng, sum(ns), 1, 64).cuda()
+    _, st = rd.prompt_append(q, k, v, cache, starts(ns))
+    assert not st.any()
+    pos = torch.cat([torch.arange(L, L + n) for n, L in zip(ns, lens)])
+    seq = torch.cat([torch.full((n,), b) for b, n in enumerate(ns)])
+    page = cache.page_table.cpu()[seq, 0].long()
+    assert torch.equal(cache.k_pool.cpu()[page, :, pos], k.cpu()) and torch.equal(cache.v_pool.cpu()[page, :, pos], v.cpu())
+
+
+def test_calls_at_once_on_two_streams(rd):
+    """Two readers, two streams, workspaces of their own."""
+    from paper_2508_09072_b200 import binding
+    rng = np.random.default_rng(45)
+    other = binding.Reader(0)
+    try:
+        work = []
+        for r, ns, lens in ((rd, [400, 30], [100, 900]), (other, [1, 1, 1, 600], [700, 5, 0, 64])):
+            cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 2, 128)
+            work.append((r, ns, lens, cache, bf16(rng, sum(ns), 8, 128).cuda(), torch.cuda.Stream(), starts(ns)))
+        torch.cuda.synchronize()
+        outs = []
+        for _ in range(20):
+            outs = []
+            for r, ns, lens, cache, q, stream, ts in work:
+                with torch.cuda.stream(stream):
+                    outs.append(r.prompt_attn(q, cache, ts, 0.09)[0])
+        torch.cuda.synchronize()
+        for (r, ns, lens, cache, q, stream, ts), out in zip(work, outs):
+            want, _, tol, _ = plain_attn(q, cache, ns, lens, 0.09)
+            within(out, want, tol)
+    finally:
+        other.close()
+
+
 def test_attn_long_histories_begun_in_the_middle(rd):
     """Whole units of more than 64 key tiles, which different CTAs begin at different tiles; sampled heads."""
     rng = np.random.default_rng(18)
