@@ -5,6 +5,7 @@
 
 #include "common.cuh"
 #include "ctx.cuh"
+#include "prompt_attn.cuh"
 #include "rotate.cuh"
 
 
@@ -80,16 +81,12 @@ reader_status reader_create(reader_ctx **out, int device) {
     ctx->partition = 0;
     ctx->ev_start = ctx->ev_stop = nullptr;
     ctx->ev_acc_start = ctx->ev_acc_stop = nullptr;
+    ctx->prompt_attr_set = false;
     ctx->prepared = PreparedRecord{};
     reader_status st = sm100_host_init(&ctx->sm100, device);
     if (st != READER_OK) {
         delete ctx;
         return st;
-    }
-    if (!prompt_host_init(&ctx->prompt)) {
-        sm100_host_destroy(&ctx->sm100);
-        delete ctx;
-        return READER_ERR_CUDA;
     }
     *out = ctx;
     return READER_OK;
@@ -97,7 +94,6 @@ reader_status reader_create(reader_ctx **out, int device) {
 
 void reader_destroy(reader_ctx *ctx) {
     if (!ctx) return;
-    prompt_host_destroy(&ctx->prompt);
     sm100_host_destroy(&ctx->sm100);
     delete ctx;
 }
@@ -789,7 +785,7 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
                 return READER_ERR_CUDA;
             }
         }
-        if (reader_status s = launch_prompt_attn(&ctx->prompt, ctx->sm100.encode_tiled, p, static_cast<const __nv_bfloat16 *>(q), cache->k_pool, cache->v_pool, st))
+        if (reader_status s = launch_prompt_attn(&ctx->prompt_attr_set, ctx->sm100.encode_tiled, p, static_cast<const __nv_bfloat16 *>(q), cache->k_pool, cache->v_pool, st))
             return s;
         if (p.alone) return launch_status();
     }

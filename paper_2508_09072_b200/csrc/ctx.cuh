@@ -1,7 +1,6 @@
 // The library context behind the opaque reader_ctx handle.
 #pragma once
 #include "common.cuh"
-#include "prompt_attn.cuh"
 #include "verify_attn_sm100.cuh"
 
 // What reader_verify_prepare left in a workspace, so that reader_verify_attn_prepared can tell whether it is
@@ -19,7 +18,7 @@ struct reader_ctx {
     int attn_kernel;  // 0 auto, 1 generic (CUDA cores), 2 tensor-core kernel only
     int partition;    // 0 auto, 1 equal ranges, 2 aligned whenever a prefix is shared
     reader::Sm100Host sm100;
-    reader::PromptHost prompt;
+    bool prompt_attr_set;   // the prompt attention kernels have their shared-memory limit
     cudaEvent_t ev_start, ev_stop;  // optional timing hooks around the main attention kernel
     cudaEvent_t ev_acc_start, ev_acc_stop;  // and around the argmax kernel of reader_accept
     PreparedRecord prepared;

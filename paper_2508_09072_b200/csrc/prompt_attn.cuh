@@ -87,15 +87,8 @@ __host__ __device__ inline int prompt_busy_ctas(int n_ctas, int W) {
 __host__ __device__ inline int prompt_range_begin(int c, int W, int ctas) { return (int)((int64_t)c * W / ctas); }
 __host__ __device__ inline int prompt_range_owner(int x, int W, int ctas) { return (int)((((int64_t)x + 1) * ctas - 1) / W); }
 
-struct PromptMaps;
-struct PromptHost {
-    PromptMaps *maps;
-    bool attr_set;
-};
-bool prompt_host_init(PromptHost *h);
-void prompt_host_destroy(PromptHost *h);
-// `encode_tiled` is the driver's tensor-map encoder.
-reader_status launch_prompt_attn(PromptHost *h, void *encode_tiled, const PromptAttnParams &p, const __nv_bfloat16 *q,
+// `attr_set`: whether the kernels have their shared-memory limit yet; `encode_tiled`: the driver's tensor-map encoder.
+reader_status launch_prompt_attn(bool *attr_set, void *encode_tiled, const PromptAttnParams &p, const __nv_bfloat16 *q,
                                  const void *k_pool, const void *v_pool, cudaStream_t st);
 void launch_prompt_finish(const PromptAttnParams &p, cudaStream_t st);
 

@@ -38,8 +38,6 @@
 // and runs to its end; the finishing kernel turns the mark into status words and zero rows.
 #include <cuda.h>
 
-#include <new>
-
 #include "prompt_attn.cuh"
 #include "ptx_sm100.cuh"
 
@@ -149,7 +147,7 @@ struct Schedule {
         start = p.token_start[b];
         blocks = blocks_of(p, b, n, L);
     }
-    // The single-launch form's only piece: unit blockIdx.x.  One look at the lengths, for a batch of up to 32 sequences.
+    // The single-launch form's only piece: unit blockIdx.x.  One look at the lengths, 32 sequences at a time.
     __device__ __forceinline__ bool alone(const PromptAttnParams &p, Piece &s, int lane) {
         const int i = blockIdx.x;
         bool bad = false, found = false;
@@ -471,318 +469,318 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         if (lane == 0) mbar_arrive(bar(&m->piece_empty[(pieces - 1) % kPieces]));
     };
     if (warp >= 8) {
-    regs_dec<kRegsOther>();
-    if (warp == kProducerWarp) {
-        // ------------------------------------------------------------------ producer
-        int r = 0, seg = 0;
-        if (lane == 0) p.pieces[blockIdx.x].b = -1;
-        __syncwarp();
-        Schedule schedule;
-        if (!p.alone) {
-            schedule.init(p, reinterpret_cast<int32_t *>(smem + C::kOffRing), lane);
-            if (lane == 0) fence_proxy_async();   // the ring was scratch until here
+        regs_dec<kRegsOther>();
+        if (warp == kProducerWarp) {
+            // ------------------------------------------------------------------ producer
+            int r = 0, seg = 0;
+            if (lane == 0) p.pieces[blockIdx.x].b = -1;
             __syncwarp();
-        }
-        Piece s;
-        const uint64_t stream_policy = l2_policy_evict_first();
-        auto load = [&](PageCursor &cursor, const CUtensorMap *map, int j, bool values) {
-            const int stage = r % C::kStages, t = s.tile(j), npg = t * kKeyTile + kPage < s.u.keys ? 2 : 1;
-            int page_a, page_b;
-            cursor.get(p, s, t, lane, page_a, page_b);
-            const bool ok = wait(bar(&m->empty[stage]), ((r / C::kStages) & 1) ^ 1, abort_s);
-            __syncwarp();
-            if (ok && elect_one()) {
-                const uint32_t full = bar(values && has_own_keys(s, t) ? &m->raw[stage] : &m->full[stage]), dst = sRing + stage * C::kTileBytes;
-                mbar_arrive_expect_tx(full, npg * (C::kTileBytes / 2));
-                const int row_a = (page_a * p.Hkv + s.h) * kPage, row_b = (page_b * p.Hkv + s.h) * kPage;
-#pragma unroll
-                for (int hf = 0; hf < C::kHalves; ++hf) {
-                    // what is read once should not push lines that others will ask for out of L2
-                    const uint32_t to = dst + hf * C::kBlockBytes;
-                    if (s.once) tma_load_2d_hint(to, map, full, hf * 64, row_a, stream_policy);
-                    else tma_load_2d(to, map, full, hf * 64, row_a);
-                    if (npg > 1 && s.once) tma_load_2d_hint(to + C::kBlockBytes / 2, map, full, hf * 64, row_b, stream_policy);
-                    else if (npg > 1) tma_load_2d(to + C::kBlockBytes / 2, map, full, hf * 64, row_b);
-                }
-            }
-            __syncwarp();
-            ++r;
-        };
-        const int tile_rows_bytes = p.G * p.tile_tokens * 128;
-        while (!*abort_s) {
-            bool more;
-            if (!p.alone) more = schedule.next(p, s, lane);
-            else if (seg == 0) more = schedule.alone(p, s, lane);
-            else more = false;
-            if (!more) s.nt = 0;
-            const int i = seg % kPieces;
-            if (!wait(bar(&m->piece_empty[i]), ((seg / kPieces) & 1) ^ 1, abort_s)) break;
-            if (lane == 0) {
-                m->piece[i] = s;
-                mbar_arrive(bar(&m->piece_full[i]));
-            }
-            __syncwarp();
-            if (!more) break;
-            const int ahead = ahead_of(s);
-            PageCursor kc, vc;
-            bool bad_page = false;
-            if (p.alone) {   // the sequence's pages, to be looked at below; the first 32 serve the loads too
-                const int npages = (s.L + s.n + kPage - 1) / kPage;
-                kc.loaded = vc.loaded = true;
-                if (lane < npages) {
-                    kc.id = p.page_table[(size_t)s.b * p.max_pages + lane];
-                    bad_page = kc.id < 0 || kc.id >= p.num_pages;
-                }
-                vc.id = kc.id;
-            }
-            for (int j = 0; j < ahead; ++j) load(kc, &kmap, j, false);
-            if (wait(bar(&m->q_empty), (seg & 1) ^ 1, abort_s) && elect_one()) {
-                const uint32_t full = bar(&m->q_full);
-                const int tiles = s.u.narrow ? 1 : 2;
-                mbar_arrive_expect_tx(full, tiles * C::kHalves * tile_rows_bytes);
-                for (int q = 0; q < tiles; ++q)
-#pragma unroll
-                    for (int hf = 0; hf < C::kHalves; ++hf)
-                        tma_load_3d(sQ + q * C::kTileBytes + hf * C::kBlockBytes, &qmap, full, hf * 64, s.h * p.G,
-                                    s.start + s.first_token + q * p.tile_tokens);
-            }
-            __syncwarp();
-            ++seg;
-            if (p.alone) {
-                for (int k = 32 + lane; k < (s.L + s.n + kPage - 1) / kPage; k += 32) {
-                    const int pg = p.page_table[(size_t)s.b * p.max_pages + k];
-                    bad_page |= pg < 0 || pg >= p.num_pages;
-                }
-                const bool reject = __any_sync(0xffffffffu, bad_page);
-                if (reject && lane == 0) *(volatile bool *)&m->piece[i].reject = true;
+            Schedule schedule;
+            if (!p.alone) {
+                schedule.init(p, reinterpret_cast<int32_t *>(smem + C::kOffRing), lane);
+                if (lane == 0) fence_proxy_async();   // the ring was scratch until here
                 __syncwarp();
-                if (s.h == 0 && s.block == 0 && lane == 0) p.status[s.b] = reject ? READER_ERR_BAD_PAGE : READER_OK;
             }
-            for (int j = 0; j < s.nt; ++j) {
-                load(vc, &vmap, j, true);
-                if (j + ahead < s.nt) load(kc, &kmap, j + ahead, false);
-            }
-        }
-        // a CTA that gave up must not exit under its own copies: let the last ones land (bounded)
-        if (*abort_s) {
-            const uint64_t t0 = globaltimer_ns();
-            for (int i = max(0, r - C::kStages); i < r; ++i)
-                while (!mbar_try_wait(bar(&m->full[i % C::kStages]), (i / C::kStages) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+            Piece s;
+            const uint64_t stream_policy = l2_policy_evict_first();
+            auto load = [&](PageCursor &cursor, const CUtensorMap *map, int j, bool values) {
+                const int stage = r % C::kStages, t = s.tile(j), npg = t * kKeyTile + kPage < s.u.keys ? 2 : 1;
+                int page_a, page_b;
+                cursor.get(p, s, t, lane, page_a, page_b);
+                const bool ok = wait(bar(&m->empty[stage]), ((r / C::kStages) & 1) ^ 1, abort_s);
+                __syncwarp();
+                if (ok && elect_one()) {
+                    const uint32_t full = bar(values && has_own_keys(s, t) ? &m->raw[stage] : &m->full[stage]), dst = sRing + stage * C::kTileBytes;
+                    mbar_arrive_expect_tx(full, npg * (C::kTileBytes / 2));
+                    const int row_a = (page_a * p.Hkv + s.h) * kPage, row_b = (page_b * p.Hkv + s.h) * kPage;
+#pragma unroll
+                    for (int hf = 0; hf < C::kHalves; ++hf) {
+                        // what is read once should not push lines that others will ask for out of L2
+                        const uint32_t to = dst + hf * C::kBlockBytes;
+                        if (s.once) tma_load_2d_hint(to, map, full, hf * 64, row_a, stream_policy);
+                        else tma_load_2d(to, map, full, hf * 64, row_a);
+                        if (npg > 1 && s.once) tma_load_2d_hint(to + C::kBlockBytes / 2, map, full, hf * 64, row_b, stream_policy);
+                        else if (npg > 1) tma_load_2d(to + C::kBlockBytes / 2, map, full, hf * 64, row_b);
+                    }
                 }
-            if (seg > 0)
-                while (!mbar_try_wait(bar(&m->q_full), (seg - 1) & 1) && globaltimer_ns() - t0 < 20000000ull) {
-                }
-        }
-    } else if (warp != kValueWarp) {
-        // ------------------------------------------------------------------ issuer of a slot's products
-        const int slot = warp == kMmaWarp ? 0 : 1;
-        constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kKeyTile, false, false);
-        constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, false, true);
-        const uint64_t descQ = smem_desc_sw128(sQ, 16, 1024), descK = smem_desc_sw128(sRing, 16, 1024);
-        const uint64_t descV = smem_desc_sw128(sRing, C::kBlockBytes, 1024);
-        const uint32_t tS = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + slot * D;
-        int r = 0, seg = 0;   // r: the next place in the ring that this warp has not seen
-        uint32_t p_parity = 0, turn_parity = 0;
-        auto wait_full = [&](int place) { wait(bar(&m->full[place % C::kStages]), (place / C::kStages) & 1, abort_s); };
-        // Both issuers see every tile in the ring's order, so that neither can fall a whole turn behind (a parity wait
-        // tells a phase only from the one before it); tiles of the other slot are passed on at once.
-        auto pass_to = [&](int place) {
-            for (; r < place; ++r) {
-                wait_full(r);
-                if (lane == 0) mbar_arrive(bar(&m->empty[r % C::kStages]));
-            }
-            __syncwarp();
-        };
-        auto issue_s = [&](uint64_t qd, int place, bool last) {
-            const uint64_t kd = descK + (uint64_t)(((place % C::kStages) * C::kTileBytes) >> 4);
-#pragma unroll
-            for (int hf = 0; hf < C::kHalves; ++hf)
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    mma_bf16_ss(tS, qd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4),
-                                kd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
-            mma_commit(bar(&m->s_full[slot]));
-            mma_commit(bar(&m->empty[place % C::kStages]));
-            if (last) mma_commit(bar(&m->q_empty));
-        };
-        // half 0: the first 64 keys of the tile, half 1: the others
-        auto issue_pv = [&](int half, int place, int slices, bool first) {
-            const uint64_t vd = descV + (uint64_t)(((place % C::kStages) * C::kTileBytes) >> 4);
-#pragma unroll
-            for (int k4 = 0; k4 < 4; ++k4) {
-                const int kk = half * 4 + k4;
-                if (kk < slices) mma_bf16_ts(tO, tS + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), kIdescPV, !first || kk != 0);
-            }
-        };
-        while (!*abort_s && next()) {
-            const int ahead = ahead_of(*sg), n = sg->nt, r0 = r, keys = sg->u.keys;
-            const bool narrow = sg->u.narrow;
-            const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1;
-            const uint64_t qd = descQ + (uint64_t)((narrow ? 0 : slot * C::kTileBytes) >> 4);
-            // Left to themselves the two slots fall into step, score products side by side and then both softmaxes
-            // on the special-function units at once (3970 cycles a step).  In a wide unit they therefore take turns with
-            // their score products, slot 0 first: each slot's softmax then runs beside the other's products.
-            // How far slot 1 begins behind slot 0 is how far it stays: in a long piece it waits for slot 0's first
-            // probabilities, half a step (attn_long 1630 -> 1586 us; in a short piece the wait costs more than it brings).
-            const bool late_start = !narrow && slot == 0 && n >= kLateStartTiles;
-            auto take_turn = [&]() {
-                if (!narrow) wait(bar(&m->turn[slot]), turn_parity, abort_s);
-                turn_parity ^= narrow ? 0 : 1;
-            };
-            auto pass_turn = [&]() {
-                if (!narrow && lane == 0) mbar_arrive(bar(&m->turn[slot ^ 1]));
                 __syncwarp();
-            };
-            wait(bar(&m->q_full), seg & 1, abort_s);
-            ++seg;
-            if (j0 < n) {
-                pass_to(r0 + place_of_k(j0, ahead));
-                wait_full(r);
-                take_turn();
-                tc_fence_after();
-                __syncwarp();
-                if (elect_one()) issue_s(qd, r, j0 + dj >= n);
-                __syncwarp();
-                if (!late_start) pass_turn();
                 ++r;
-                for (int j = j0; j < n; j += dj) {
-                    const int slices = (min(kKeyTile, keys - sg->tile(j) * kKeyTile) + 15) >> 4;
-                    const bool more = j + dj < n;
-                    pass_to(r0 + place_of_v(j, ahead, n));
-                    const int rv = r;
-                    wait_full(r++);
-                    wait(bar(&m->p_full[slot][0]), p_parity, abort_s);
-                    tc_fence_after();
-                    __syncwarp();
-                    if (elect_one()) issue_pv(0, rv, slices, j == j0);
-                    __syncwarp();
-                    if (late_start && j == j0) pass_turn();
-                    if (more) {
-                        pass_to(r0 + place_of_k(j + dj, ahead));
-                        wait_full(r);
-                        take_turn();
-                    }
-                    wait(bar(&m->p_full[slot][1]), p_parity, abort_s);
-                    p_parity ^= 1;
-                    tc_fence_after();
-                    __syncwarp();
-                    if (elect_one()) {
-                        issue_pv(1, rv, slices, j == j0);
-                        mma_commit(bar(&m->empty[rv % C::kStages]));
-                        if (more) issue_s(qd, r, j + 2 * dj >= n);
-                        else mma_commit(bar(&m->o_full[slot]));
-                    }
-                    __syncwarp();
-                    if (more) {
-                        pass_turn();
-                        ++r;
-                    }
+            };
+            const int tile_rows_bytes = p.G * p.tile_tokens * 128;
+            while (!*abort_s) {
+                bool more;
+                if (!p.alone) more = schedule.next(p, s, lane);
+                else if (seg == 0) more = schedule.alone(p, s, lane);
+                else more = false;
+                if (!more) s.nt = 0;
+                const int i = seg % kPieces;
+                if (!wait(bar(&m->piece_empty[i]), ((seg / kPieces) & 1) ^ 1, abort_s)) break;
+                if (lane == 0) {
+                    m->piece[i] = s;
+                    mbar_arrive(bar(&m->piece_full[i]));
                 }
-            } else {
-                if (lane == 0) mbar_arrive(bar(&m->q_empty));   // a narrow piece of one tile: slot 1 has none
                 __syncwarp();
-            }
-            pass_to(r0 + 2 * n);
-            done();
-        }
-        if (*abort_s) __nanosleep(1000000);   // products that are still under way end before their operands go away
-    } else if (warp == kValueWarp) {
-        // ------------------------------------------------------------------ values some queries do not see; the note on a split unit
-        int r0 = 0;
-        uint32_t raw_parity = 0;   // one bit per ring stage
-        if (p.alone && blockIdx.x == 0) report_idle<D>(p, lane);
-        while (!*abort_s && next()) {
-            const int ahead = ahead_of(*sg), n = sg->nt, own_key = sg->L + sg->first_token;
-            constexpr int kChunks = D / 8;   // 16-byte pieces per row
-            // A look at the exponents (all ones: infinity or NaN) of the value rows that are multiplied although some query does
-            // not see them: the unit's own tokens, and what the last slice of 16 rows holds behind them.  They are read from
-            // the pool, while the tiles are on their way: out of shared memory, whose bandwidth the products take up,
-            // one tile took 6000 cycles.
-            const int lo = max(own_key, sg->t0 * kKeyTile), hi = min((sg->u.keys + 15) & ~15, (sg->t0 + n) * kKeyTile);
-            // (A short piece has no time for that, and few products: its tiles are gone through in shared memory.)
-            bool dirty = n < kLookAheadTiles;
-            if (!dirty && lo < hi) {
-                constexpr int kBatch = 8;    // pieces a lane has in flight
-                const int first_page = lo / kPage;
-                int page = -1;
-                if (first_page + lane <= (hi - 1) / kPage) page = p.page_table[(size_t)sg->b * p.max_pages + first_page + lane];
-                if (page >= p.num_pages) page = -1;
-                uint32_t ones = 0;
-                for (int i0 = 0; i0 < (hi - lo) * kChunks; i0 += kBatch * 32) {
-                    uint4 x[kBatch];
-#pragma unroll
-                    for (int k = 0; k < kBatch; ++k) {
-                        const int i = i0 + k * 32 + lane, key = lo + i / kChunks;
-                        const int pg = __shfl_sync(0xffffffffu, page, (key / kPage - first_page) & 31);
-                        x[k] = make_uint4(0, 0, 0, 0);
-                        if (key < hi && pg >= 0)
-                            x[k] = __ldg(reinterpret_cast<const uint4 *>(v_pool + (((size_t)pg * p.Hkv + sg->h) * kPage + key % kPage) * D) + i % kChunks);
+                if (!more) break;
+                const int ahead = ahead_of(s);
+                PageCursor kc, vc;
+                bool bad_page = false;
+                if (p.alone) {   // the sequence's pages, to be looked at below; the first 32 serve the loads too
+                    const int npages = (s.L + s.n + kPage - 1) / kPage;
+                    kc.loaded = vc.loaded = true;
+                    if (lane < npages) {
+                        kc.id = p.page_table[(size_t)s.b * p.max_pages + lane];
+                        bad_page = kc.id < 0 || kc.id >= p.num_pages;
                     }
-#pragma unroll
-                    for (int k = 0; k < kBatch; ++k) {
-                        ones |= ((x[k].x & 0x7f807f80u) + 0x00800080u) | ((x[k].y & 0x7f807f80u) + 0x00800080u);
-                        ones |= ((x[k].z & 0x7f807f80u) + 0x00800080u) | ((x[k].w & 0x7f807f80u) + 0x00800080u);
-                    }
+                    vc.id = kc.id;
                 }
-                dirty = __any_sync(0xffffffffu, (ones & 0x80008000u) != 0);
-            }
-            for (int j = 0; j < n; ++j) {
-                const int t = sg->tile(j);
-                if (!has_own_keys(*sg, t)) continue;
-                const int r = r0 + place_of_v(j, ahead, n), stage = r % C::kStages;
-                if (!wait(bar(&m->raw[stage]), (raw_parity >> stage) & 1, abort_s)) break;
-                raw_parity ^= 1u << stage;
-                if (!dirty) {
-                    if (lane == 0) mbar_arrive(bar(&m->full[stage]));
+                for (int j = 0; j < ahead; ++j) load(kc, &kmap, j, false);
+                if (wait(bar(&m->q_empty), (seg & 1) ^ 1, abort_s) && elect_one()) {
+                    const uint32_t full = bar(&m->q_full);
+                    const int tiles = s.u.narrow ? 1 : 2;
+                    mbar_arrive_expect_tx(full, tiles * C::kHalves * tile_rows_bytes);
+                    for (int q = 0; q < tiles; ++q)
+#pragma unroll
+                        for (int hf = 0; hf < C::kHalves; ++hf)
+                            tma_load_3d(sQ + q * C::kTileBytes + hf * C::kBlockBytes, &qmap, full, hf * 64, s.h * p.G,
+                                        s.start + s.first_token + q * p.tile_tokens);
+                }
+                __syncwarp();
+                ++seg;
+                if (p.alone) {
+                    for (int k = 32 + lane; k < (s.L + s.n + kPage - 1) / kPage; k += 32) {
+                        const int pg = p.page_table[(size_t)s.b * p.max_pages + k];
+                        bad_page |= pg < 0 || pg >= p.num_pages;
+                    }
+                    const bool reject = __any_sync(0xffffffffu, bad_page);
+                    if (reject && lane == 0) *(volatile bool *)&m->piece[i].reject = true;
                     __syncwarp();
-                    continue;
+                    if (s.h == 0 && s.block == 0 && lane == 0) p.status[s.b] = reject ? READER_ERR_BAD_PAGE : READER_OK;
                 }
-                const uint32_t tile = sRing + stage * C::kTileBytes;
-                const int valid = min(kKeyTile, sg->u.keys - t * kKeyTile), end = (valid + 15) & ~15;
-                const int own_row = max(0, own_key - t * kKeyTile);
-                auto piece_at = [&](int i) {
-                    const int row = i / kChunks, c = i % kChunks;
-                    return tile + (c >> 3) * C::kBlockBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                for (int j = 0; j < s.nt; ++j) {
+                    load(vc, &vmap, j, true);
+                    if (j + ahead < s.nt) load(kc, &kmap, j + ahead, false);
+                }
+            }
+            // a CTA that gave up must not exit under its own copies: let the last ones land (bounded)
+            if (*abort_s) {
+                const uint64_t t0 = globaltimer_ns();
+                for (int i = max(0, r - C::kStages); i < r; ++i)
+                    while (!mbar_try_wait(bar(&m->full[i % C::kStages]), (i / C::kStages) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+                    }
+                if (seg > 0)
+                    while (!mbar_try_wait(bar(&m->q_full), (seg - 1) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+                    }
+            }
+        } else if (warp != kValueWarp) {
+            // ------------------------------------------------------------------ issuer of a slot's products
+            const int slot = warp == kMmaWarp ? 0 : 1;
+            constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kKeyTile, false, false);
+            constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, false, true);
+            const uint64_t descQ = smem_desc_sw128(sQ, 16, 1024), descK = smem_desc_sw128(sRing, 16, 1024);
+            const uint64_t descV = smem_desc_sw128(sRing, C::kBlockBytes, 1024);
+            const uint32_t tS = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + slot * D;
+            int r = 0, seg = 0;   // r: the next place in the ring that this warp has not seen
+            uint32_t p_parity = 0, turn_parity = 0;
+            auto wait_full = [&](int place) { wait(bar(&m->full[place % C::kStages]), (place / C::kStages) & 1, abort_s); };
+            // Both issuers see every tile in the ring's order, so that neither can fall a whole turn behind (a parity wait
+            // tells a phase only from the one before it); tiles of the other slot are passed on at once.
+            auto pass_to = [&](int place) {
+                for (; r < place; ++r) {
+                    wait_full(r);
+                    if (lane == 0) mbar_arrive(bar(&m->empty[r % C::kStages]));
+                }
+                __syncwarp();
+            };
+            auto issue_s = [&](uint64_t qd, int place, bool last) {
+                const uint64_t kd = descK + (uint64_t)(((place % C::kStages) * C::kTileBytes) >> 4);
+#pragma unroll
+                for (int hf = 0; hf < C::kHalves; ++hf)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_bf16_ss(tS, qd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4),
+                                    kd + (uint64_t)((hf * C::kBlockBytes + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
+                mma_commit(bar(&m->s_full[slot]));
+                mma_commit(bar(&m->empty[place % C::kStages]));
+                if (last) mma_commit(bar(&m->q_empty));
+            };
+            // half 0: the first 64 keys of the tile, half 1: the others
+            auto issue_pv = [&](int half, int place, int slices, bool first) {
+                const uint64_t vd = descV + (uint64_t)(((place % C::kStages) * C::kTileBytes) >> 4);
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    const int kk = half * 4 + k4;
+                    if (kk < slices) mma_bf16_ts(tO, tS + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), kIdescPV, !first || kk != 0);
+                }
+            };
+            while (!*abort_s && next()) {
+                const int ahead = ahead_of(*sg), n = sg->nt, r0 = r, keys = sg->u.keys;
+                const bool narrow = sg->u.narrow;
+                const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1;
+                const uint64_t qd = descQ + (uint64_t)((narrow ? 0 : slot * C::kTileBytes) >> 4);
+                // Left to themselves the two slots fall into step, score products side by side and then both softmaxes
+                // on the special-function units at once (3970 cycles a step).  In a wide unit they therefore take turns with
+                // their score products, slot 0 first: each slot's softmax then runs beside the other's products.
+                // How far slot 1 begins behind slot 0 is how far it stays: in a long piece it waits for slot 0's first
+                // probabilities, half a step (attn_long 1630 -> 1586 us; in a short piece the wait costs more than it brings).
+                const bool late_start = !narrow && slot == 0 && n >= kLateStartTiles;
+                auto take_turn = [&]() {
+                    if (!narrow) wait(bar(&m->turn[slot]), turn_parity, abort_s);
+                    turn_parity ^= narrow ? 0 : 1;
                 };
-                bool found = false;
-                constexpr int kAtOnce = 8;
-                for (int i0 = own_row * kChunks + lane; i0 < valid * kChunks; i0 += kAtOnce * 32) {
-                    uint32_t x[kAtOnce][4];
-                    uint32_t ones = 0;
-#pragma unroll
-                    for (int k = 0; k < kAtOnce; ++k) {
-                        x[k][0] = x[k][1] = x[k][2] = x[k][3] = 0;
-                        if (i0 + k * 32 < valid * kChunks)
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3]) : "r"(piece_at(i0 + k * 32)));
-                    }
-#pragma unroll
-                    for (int k = 0; k < kAtOnce; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) ones |= (x[k][e] & 0x7f807f80u) + 0x00800080u;
-                    if (!(ones & 0x80008000u)) continue;
-                    found = true;
-#pragma unroll
-                    for (int k = 0; k < kAtOnce; ++k) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (nonfinite_bits(x[k][e])) x[k][e] &= 0xffff0000u;
-                            if (nonfinite_bits(x[k][e] >> 16)) x[k][e] &= 0x0000ffffu;
+                auto pass_turn = [&]() {
+                    if (!narrow && lane == 0) mbar_arrive(bar(&m->turn[slot ^ 1]));
+                    __syncwarp();
+                };
+                wait(bar(&m->q_full), seg & 1, abort_s);
+                ++seg;
+                if (j0 < n) {
+                    pass_to(r0 + place_of_k(j0, ahead));
+                    wait_full(r);
+                    take_turn();
+                    tc_fence_after();
+                    __syncwarp();
+                    if (elect_one()) issue_s(qd, r, j0 + dj >= n);
+                    __syncwarp();
+                    if (!late_start) pass_turn();
+                    ++r;
+                    for (int j = j0; j < n; j += dj) {
+                        const int slices = (min(kKeyTile, keys - sg->tile(j) * kKeyTile) + 15) >> 4;
+                        const bool more = j + dj < n;
+                        pass_to(r0 + place_of_v(j, ahead, n));
+                        const int rv = r;
+                        wait_full(r++);
+                        wait(bar(&m->p_full[slot][0]), p_parity, abort_s);
+                        tc_fence_after();
+                        __syncwarp();
+                        if (elect_one()) issue_pv(0, rv, slices, j == j0);
+                        __syncwarp();
+                        if (late_start && j == j0) pass_turn();
+                        if (more) {
+                            pass_to(r0 + place_of_k(j + dj, ahead));
+                            wait_full(r);
+                            take_turn();
                         }
-                        if (i0 + k * 32 < valid * kChunks)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece_at(i0 + k * 32)), "r"(x[k][0]), "r"(x[k][1]), "r"(x[k][2]), "r"(x[k][3]) : "memory");
+                        wait(bar(&m->p_full[slot][1]), p_parity, abort_s);
+                        p_parity ^= 1;
+                        tc_fence_after();
+                        __syncwarp();
+                        if (elect_one()) {
+                            issue_pv(1, rv, slices, j == j0);
+                            mma_commit(bar(&m->empty[rv % C::kStages]));
+                            if (more) issue_s(qd, r, j + 2 * dj >= n);
+                            else mma_commit(bar(&m->o_full[slot]));
+                        }
+                        __syncwarp();
+                        if (more) {
+                            pass_turn();
+                            ++r;
+                        }
                     }
+                } else {
+                    if (lane == 0) mbar_arrive(bar(&m->q_empty));   // a narrow piece of one tile: slot 1 has none
+                    __syncwarp();
                 }
-                if (__any_sync(0xffffffffu, found) && lane == 0) *(volatile int32_t *)&m->piece[(pieces - 1) % kPieces].poison = 1;
-                for (int i = valid * kChunks + lane; i < end * kChunks; i += 32)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at(i)), "r"(0u) : "memory");
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&m->full[stage]));
+                pass_to(r0 + 2 * n);
+                done();
             }
-            r0 += 2 * n;
-            done();
+            if (*abort_s) __nanosleep(1000000);   // products that are still under way end before their operands go away
+        } else if (warp == kValueWarp) {
+            // ------------------------------------------------------------------ values some queries do not see; the note on a split unit
+            int r0 = 0;
+            uint32_t raw_parity = 0;   // one bit per ring stage
+            if (p.alone && blockIdx.x == 0) report_idle<D>(p, lane);
+            while (!*abort_s && next()) {
+                const int ahead = ahead_of(*sg), n = sg->nt, own_key = sg->L + sg->first_token;
+                constexpr int kChunks = D / 8;   // 16-byte pieces per row
+                // A look at the exponents (all ones: infinity or NaN) of the value rows that are multiplied although some query does
+                // not see them: the unit's own tokens, and what the last slice of 16 rows holds behind them.  They are read from
+                // the pool, while the tiles are on their way: out of shared memory, whose bandwidth the products take up,
+                // one tile took 6000 cycles.
+                const int lo = max(own_key, sg->t0 * kKeyTile), hi = min((sg->u.keys + 15) & ~15, (sg->t0 + n) * kKeyTile);
+                // (A short piece has no time for that, and few products: its tiles are gone through in shared memory.)
+                bool dirty = n < kLookAheadTiles;
+                if (!dirty && lo < hi) {
+                    constexpr int kBatch = 8;    // pieces a lane has in flight
+                    const int first_page = lo / kPage;
+                    int page = -1;
+                    if (first_page + lane <= (hi - 1) / kPage) page = p.page_table[(size_t)sg->b * p.max_pages + first_page + lane];
+                    if (page >= p.num_pages) page = -1;
+                    uint32_t ones = 0;
+                    for (int i0 = 0; i0 < (hi - lo) * kChunks; i0 += kBatch * 32) {
+                        uint4 x[kBatch];
+#pragma unroll
+                        for (int k = 0; k < kBatch; ++k) {
+                            const int i = i0 + k * 32 + lane, key = lo + i / kChunks;
+                            const int pg = __shfl_sync(0xffffffffu, page, (key / kPage - first_page) & 31);
+                            x[k] = make_uint4(0, 0, 0, 0);
+                            if (key < hi && pg >= 0)
+                                x[k] = __ldg(reinterpret_cast<const uint4 *>(v_pool + (((size_t)pg * p.Hkv + sg->h) * kPage + key % kPage) * D) + i % kChunks);
+                        }
+#pragma unroll
+                        for (int k = 0; k < kBatch; ++k) {
+                            ones |= ((x[k].x & 0x7f807f80u) + 0x00800080u) | ((x[k].y & 0x7f807f80u) + 0x00800080u);
+                            ones |= ((x[k].z & 0x7f807f80u) + 0x00800080u) | ((x[k].w & 0x7f807f80u) + 0x00800080u);
+                        }
+                    }
+                    dirty = __any_sync(0xffffffffu, (ones & 0x80008000u) != 0);
+                }
+                for (int j = 0; j < n; ++j) {
+                    const int t = sg->tile(j);
+                    if (!has_own_keys(*sg, t)) continue;
+                    const int r = r0 + place_of_v(j, ahead, n), stage = r % C::kStages;
+                    if (!wait(bar(&m->raw[stage]), (raw_parity >> stage) & 1, abort_s)) break;
+                    raw_parity ^= 1u << stage;
+                    if (!dirty) {
+                        if (lane == 0) mbar_arrive(bar(&m->full[stage]));
+                        __syncwarp();
+                        continue;
+                    }
+                    const uint32_t tile = sRing + stage * C::kTileBytes;
+                    const int valid = min(kKeyTile, sg->u.keys - t * kKeyTile), end = (valid + 15) & ~15;
+                    const int own_row = max(0, own_key - t * kKeyTile);
+                    auto piece_at = [&](int i) {
+                        const int row = i / kChunks, c = i % kChunks;
+                        return tile + (c >> 3) * C::kBlockBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                    };
+                    bool found = false;
+                    constexpr int kAtOnce = 8;
+                    for (int i0 = own_row * kChunks + lane; i0 < valid * kChunks; i0 += kAtOnce * 32) {
+                        uint32_t x[kAtOnce][4];
+                        uint32_t ones = 0;
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k) {
+                            x[k][0] = x[k][1] = x[k][2] = x[k][3] = 0;
+                            if (i0 + k * 32 < valid * kChunks)
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3]) : "r"(piece_at(i0 + k * 32)));
+                        }
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) ones |= (x[k][e] & 0x7f807f80u) + 0x00800080u;
+                        if (!(ones & 0x80008000u)) continue;
+                        found = true;
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if (nonfinite_bits(x[k][e])) x[k][e] &= 0xffff0000u;
+                                if (nonfinite_bits(x[k][e] >> 16)) x[k][e] &= 0x0000ffffu;
+                            }
+                            if (i0 + k * 32 < valid * kChunks)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece_at(i0 + k * 32)), "r"(x[k][0]), "r"(x[k][1]), "r"(x[k][2]), "r"(x[k][3]) : "memory");
+                        }
+                    }
+                    if (__any_sync(0xffffffffu, found) && lane == 0) *(volatile int32_t *)&m->piece[(pieces - 1) % kPieces].poison = 1;
+                    for (int i = valid * kChunks + lane; i < end * kChunks; i += 32)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece_at(i)), "r"(0u) : "memory");
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(&m->full[stage]));
+                }
+                r0 += 2 * n;
+                done();
+            }
         }
-    }
     } else {
         // ------------------------------------------------------------------ softmax / epilogue
         regs_inc<kRegsSoftmax>();
@@ -1203,70 +1201,30 @@ bool encode(void *fn, CUtensorMap *map, const void *at, int rank, const cuuint64
 
 }  // namespace
 
-// TMA descriptors of the tensors seen last: pools by layer (round robin), the queries of the last call.
-constexpr int kPoolEntries = 128;
-struct PromptMaps {
-    struct Pool {
-        const void *k = nullptr, *v = nullptr;
-        int64_t rows = -1;
-        int D = 0;
-        alignas(64) CUtensorMap kmap, vmap;
-    } pools[kPoolEntries];
-    int next = 0;
-    const void *q = nullptr;
-    int64_t tokens = -1;
-    int Hq = 0, G = 0, D = 0;
-    alignas(64) CUtensorMap qmap;
-};
-
-bool prompt_host_init(PromptHost *h) {
-    h->attr_set = false;
-    h->maps = new (std::nothrow) PromptMaps();
-    return h->maps != nullptr;
-}
-void prompt_host_destroy(PromptHost *h) {
-    delete h->maps;
-    h->maps = nullptr;
-}
-
-reader_status launch_prompt_attn(PromptHost *h, void *fn, const PromptAttnParams &p, const __nv_bfloat16 *q, const void *k_pool,
+reader_status launch_prompt_attn(bool *attr_set, void *fn, const PromptAttnParams &p, const __nv_bfloat16 *q, const void *k_pool,
                                  const void *v_pool, cudaStream_t st) {
-    if (!h->attr_set) {
+    if (!*attr_set) {
         if (cudaFuncSetAttribute(prompt_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes) != cudaSuccess ||
             cudaFuncSetAttribute(prompt_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes) != cudaSuccess) {
             cudaGetLastError();
             return READER_ERR_CUDA;
         }
-        h->attr_set = true;
+        *attr_set = true;
     }
-    PromptMaps *m = h->maps;
-    const int64_t rows = (int64_t)p.num_pages * p.Hkv * kPage;
-    PromptMaps::Pool *pool = nullptr;
-    for (int i = 0; i < kPoolEntries && !pool; ++i) {
-        PromptMaps::Pool &e = m->pools[i];
-        if (e.k == k_pool && e.v == v_pool && e.rows == rows && e.D == p.D) pool = &e;
-    }
-    if (!pool) {
-        pool = &m->pools[m->next];
-        m->next = (m->next + 1) % kPoolEntries;
-        pool->rows = -1;
-        const cuuint64_t dims[2] = {(cuuint64_t)p.D, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)p.D * 2};
-        const cuuint32_t box[2] = {64, (cuuint32_t)kPage};
-        if (!encode(fn, &pool->kmap, k_pool, 2, dims, strides, box) || !encode(fn, &pool->vmap, v_pool, 2, dims, strides, box)) return READER_ERR_CUDA;
-        pool->k = k_pool; pool->v = v_pool; pool->rows = rows; pool->D = p.D;
-    }
-    if (m->q != q || m->tokens != p.tokens || m->Hq != p.Hq || m->G != p.G || m->D != p.D) {
-        // 64 columns x the G heads of a group x as many tokens as fill 128 rows
-        const cuuint64_t dims[3] = {(cuuint64_t)p.D, (cuuint64_t)p.Hq, (cuuint64_t)p.tokens};
-        const cuuint64_t strides[2] = {(cuuint64_t)p.D * 2, (cuuint64_t)p.Hq * p.D * 2};
-        const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens};
-        m->tokens = -1;
-        if (!encode(fn, &m->qmap, q, 3, dims, strides, box)) return READER_ERR_CUDA;
-        m->q = q; m->tokens = p.tokens; m->Hq = p.Hq; m->G = p.G; m->D = p.D;
-    }
+    // The descriptors are made anew for every call: about 0.1 us each, and nothing to go stale.
+    alignas(64) CUtensorMap qmap, kmap, vmap;
+    const cuuint64_t pool_dims[2] = {(cuuint64_t)p.D, (cuuint64_t)p.num_pages * p.Hkv * kPage}, pool_strides[1] = {(cuuint64_t)p.D * 2};
+    const cuuint32_t pool_box[2] = {64, (cuuint32_t)kPage};
+    // 64 columns x the G heads of a group x as many tokens as fill 128 rows
+    const cuuint64_t q_dims[3] = {(cuuint64_t)p.D, (cuuint64_t)p.Hq, (cuuint64_t)p.tokens};
+    const cuuint64_t q_strides[2] = {(cuuint64_t)p.D * 2, (cuuint64_t)p.Hq * p.D * 2};
+    const cuuint32_t q_box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens};
+    if (!encode(fn, &kmap, k_pool, 2, pool_dims, pool_strides, pool_box) || !encode(fn, &vmap, v_pool, 2, pool_dims, pool_strides, pool_box) ||
+        !encode(fn, &qmap, q, 3, q_dims, q_strides, q_box))
+        return READER_ERR_CUDA;
     const bool wide = p.D == 128;
     const cudaError_t e = launch_pdl(wide ? prompt_attn_kernel<128> : prompt_attn_kernel<64>, dim3((unsigned)p.n_ctas), dim3(kThreads),
-                                     wide ? Cfg<128>::kSmemBytes : Cfg<64>::kSmemBytes, st, p, m->qmap, pool->kmap, pool->vmap,
+                                     wide ? Cfg<128>::kSmemBytes : Cfg<64>::kSmemBytes, st, p, qmap, kmap, vmap,
                                      static_cast<const __nv_bfloat16 *>(v_pool));
     if (e != cudaSuccess) {
         cudaGetLastError();
