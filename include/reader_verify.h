@@ -481,8 +481,9 @@ size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  *              share it must not overlap on the GPU
  *   status_out i32 [batch]: READER_ERR_CAPACITY, READER_ERR_BAD_PAGE, READER_ERR_TIMEOUT: that sequence's rows of out and
  *              lse_out are zero and its length is not advanced
- * softmax_scale > 0, n_q_heads / n_kv_heads at most 128, batch at most 32768, else READER_ERR_UNSUPPORTED.  What the
- * cache holds at positions a token does not see has no influence on its row, infinities and NaN included.
+ * softmax_scale > 0 and at most 2e38, n_q_heads / n_kv_heads at most 128, batch at most 32768, else
+ * READER_ERR_UNSUPPORTED.  What the cache holds at positions a token does not see has no influence on its row,
+ * infinities and NaN included.
  * Arithmetic: bf16 inputs, fp32 accumulation and softmax, probabilities rounded to bf16 before the value product, bf16
  * (nearest-even) output.
  */

@@ -741,7 +741,7 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0 || !aligned16(lse_out) || Hq < 1 || !(softmax_scale == softmax_scale))
         return READER_ERR_INVALID_ARG;
     // the row maximum is taken before the scaling, so the scale has to be positive; a query tile is a box of whole tokens
-    if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f || Hq % Hkv != 0 || Hq / Hkv > kTileM) return READER_ERR_UNSUPPORTED;
+    if (!(softmax_scale > 0.f) || softmax_scale > 2.0e38f || Hq % Hkv != 0 || Hq / Hkv > kTileM) return READER_ERR_UNSUPPORTED;
     if (B > kPromptMaxBatch || (int64_t)cache->num_pages * Hkv * kPage >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
     PromptAttnParams p{};
     p.G = Hq / Hkv;

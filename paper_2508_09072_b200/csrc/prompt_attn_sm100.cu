@@ -18,9 +18,10 @@
 //
 // Softmax: the exponentials of a tile are taken against the maximum known from the tiles before it while the tile's
 // own maximum is found on the side; only if that exceeds the old one by more than 2^8 is the maximum raised, the
-// output rescaled and the half done again (a segment's first tile looks for its maximum first).  Scores, maxima,
-// sums and outputs are fp32; P is rounded to bf16 for the value product (relative error of a weight 2^-8 at most, of
-// the size of the output's own rounding), the row sum adds the unrounded weights.
+// output rescaled and the half done again (a segment's first tile looks for its maximum first).  Scores whose rounding
+// exceeds what an exponential can hold (2^29 and up) take a slower path, tile by tile.  Scores, maxima, sums and
+// outputs are fp32; P is rounded to bf16 for the value product (relative error of a weight 2^-8 at most, of the size
+// of the output's own rounding), the row sum adds the unrounded weights.
 //
 // Keys that a row does not see get the score -inf by selection, whatever the cache holds there.  Values cannot be
 // selected in a matrix product (0 * inf is NaN), so warp 10 goes over the tiles that hold keys of the unit's own
@@ -52,6 +53,9 @@ constexpr int kRegsSoftmax = 208, kRegsOther = 88;
 constexpr int kProducerWarp = 8, kMmaWarp = 9, kValueWarp = 10;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kRaiseMaxBy = 8.f;   // log2 units
+constexpr float kHugeScore = 536870912.f;
+// -infinity: every tile takes the slow path
+__device__ __forceinline__ float margin_of(float mx) { return fabsf(mx) > kHugeScore && fabsf(mx) < INFINITY ? -INFINITY : kRaiseMaxBy; }
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 constexpr int kMaxStages = 8;
 constexpr int kLateStartTiles = 20;  // shortest piece whose slot 1 begins half a step late
@@ -801,6 +805,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             const int warp_min = __reduce_min_sync(0xffffffffu, last_key);
             float mx = -INFINITY, l = 0.f;    // running maximum (scaled, log2 units) and row sum
             const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1, nt = sg->nt;
+            float margin = kRaiseMaxBy;       // the maximum is raised by scores that exceed it by more
             bool any = false;
             for (int j = j0; j < nt; j += dj) {
                 const int key0 = sg->tile(j) * kKeyTile;
@@ -835,7 +840,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
                         }
                     };
-                    bool first = !any;
+                    bool first = !any, huge = false;
                     while (true) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[c * 32]));
@@ -846,14 +851,17 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             for (int i = 0; i < 128; ++i)
                                 if (i > lim) sc[i] = kNegInf;
                         }
-                        if (first) mx = tile_top();   // (-inf where the row sees none of these keys)
-                        first = false;
+                        if (first) {
+                            mx = tile_top();   // (-inf where the row sees none of these keys)
+                            margin = margin_of(mx);
+                            first = false;
+                        }
                         const float neg = mx == -INFINITY ? 0.f : -mx;
                         neg2 = make_float2(neg, neg);
                         part[0] = part[1] = make_float2(0.f, 0.f);
                         exponentials(0);
                         const float top = tile_top();
-                        if (!__any_sync(0xffffffffu, top > mx + kRaiseMaxBy)) break;
+                        if (!__any_sync(0xffffffffu, top > mx + margin)) break;
                         const float up = fmaxf(mx, top);
                         const float alpha = up == -INFINITY ? 1.f : ex2(mx - up);
                         mx = up;
@@ -868,16 +876,49 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
                             tmem_st16(tO + c, o);
                         }
+                        margin = margin_of(mx);
+                        if (__any_sync(0xffffffffu, margin != kRaiseMaxBy)) {
+                            huge = true;
+                            break;
+                        }
                         tmem_wait_st();
                     }
-                    tmem_st32(tS, pk);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(bar(&m->p_full[slot][0]));
-                    exponentials(1);
-                    tmem_st32(tS + 32, pk);
-                    l += (part[0].x + part[1].x) + (part[0].y + part[1].y);
-                    tmem_wait_st();
+                    if (__builtin_expect(huge, 0)) {
+                        // Past 2^29 the rounding of the maximum is no longer small against what an exponential holds, and the
+                        // fused product would keep it: here scores are scaled and rounded like the maximum before they meet.
+                        const float neg = mx == -INFINITY ? 0.f : -mx;
+#pragma unroll 1
+                        for (int c = 0; c < kKeyTile; c += 32) {
+                            uint32_t x[32];
+                            tmem_ld32(tS + c, x);
+                            tmem_wait_ld();
+                            float e[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                e[i] = key0 + c + i > last_key ? 0.f : ex2(__fadd_rn(__fmul_rn(__uint_as_float(x[i]), p.scale_log2), neg));
+                                l += e[i];
+                            }
+                            uint32_t y[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(e[2 * i], e[2 * i + 1]);
+                                y[i] = *reinterpret_cast<const uint32_t *>(&hh);
+                            }
+                            tmem_st16(tS + c / 2, y);   // (columns that have been read)
+                        }
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(bar(&m->p_full[slot][0]));
+                    } else {
+                        tmem_st32(tS, pk);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(bar(&m->p_full[slot][0]));
+                        exponentials(1);
+                        tmem_st32(tS + 32, pk);
+                        l += (part[0].x + part[1].x) + (part[0].y + part[1].y);
+                        tmem_wait_st();
+                    }
                 } else {
                     tc_fence_before();
                     mbar_arrive(bar(&m->p_full[slot][0]));

@@ -330,6 +330,60 @@ def test_attn_rising_scores_are_rescaled(rd):
         check_attn(rd, q, cache, [n], [0], 1.0)
 
 
+def test_attn_scores_beyond_the_exponents_range(rd):
+    """Scores of 10^12, where the rounding of a maximum is many times what an exponential can hold, after ordinary ones.
+
+    Every key of a head has its own score: a row's largest lies 10^9 above the rest, so its weight is 1 and the others' 0.
+    q and k are powers of two times at most 8 bits, and the products of a row are alike, so a score's sum is exact; its
+    scaling and the maximum's move the log of the denominator by a few 2^-24 of it."""
+    rng = np.random.default_rng(46)
+    n, D = 600, 128
+    cache = make_cache(rng, [0], [n], 2, D)
+    pos = torch.arange(n)
+    page = cache.page_table[0].cpu()[pos // PAGE].long()
+    size = torch.stack([torch.tensor(f)[pos // 128] * (1 + pos % 128 / 128) for f in
+                        ([2.0 ** -40, 1, 0.125, 2, 0.5], [1, 0.125, 2, 0.5, 4])])          # [head, position]
+    k = (size * 2.0 ** 18).to(torch.bfloat16)
+    assert torch.equal(k.float(), size * 2.0 ** 18)
+    pool = cache.k_pool.cpu()
+    for h in range(2):
+        pool[page, h, pos % PAGE] = k[h][:, None].expand(n, D)
+    cache.k_pool.copy_(pool)
+    sign = torch.tensor([1.0, -1.0, 1.0, -1.0])
+    q = (sign * 2.0 ** 18)[None, :, None].expand(n, 4, D).to(torch.bfloat16).contiguous()
+    for pieces in ([n], [1] * 3, [300]):
+        m = sum(pieces)
+        lens = [n - m]
+        if len(pieces) > 1:      # single tokens of three sequences that share the pages
+            lens = [n - 1, 200, 5]
+            many = type(cache)(cache.k_pool, cache.v_pool, cache.page_table.repeat(3, 1), torch.tensor(lens, dtype=torch.int32).cuda())
+        else:
+            many = cache
+            many.seq_lens.fill_(lens[0])
+        lse = torch.empty(m, 4, device="cuda")
+        out, st = rd.prompt_attn(q[:m].cuda(), many, starts(pieces), 0.125, lse=lse)
+        assert not st.any()
+        want, wlse, _, _ = plain_attn(q[:m], many, pieces, lens, 0.125)
+        out, lse = out.double().cpu(), lse.double().cpu()
+        last = torch.cat([torch.arange(L, L + c) for c, L in zip(pieces, lens)])
+        ordinary = torch.zeros(m, 4, dtype=torch.bool)
+        ordinary[:, 1] = True                  # the small scores are the largest ones
+        ordinary[last < 128, 0] = True         # nothing else is seen
+        assert torch.equal(out[~ordinary], want[~ordinary])
+        assert ((lse - wlse)[~ordinary].abs() <= 2.0 ** -21 * wlse[~ordinary].abs()).all()
+        v = rows_of(cache, 0, 128)[1][:, 0]
+        delta = D * 2.0 ** -23 * 2 + 1e-6      # scores of at most 2
+        s = 0.125 * D * 2.0 ** 36 * size[0, :128].double()
+        for i, h in ordinary.nonzero().tolist():
+            w = torch.softmax((sign[h] * s)[:int(last[i]) + 1], 0)
+            o, top = w @ v[:len(w)], w @ v[:len(w)].abs()
+            assert ((out[i, h] - o).abs() <= (HALF + 4 * delta) * top + HALF * 1.01 * o.abs()).all()
+    from paper_2508_09072_b200 import binding
+    with pytest.raises(binding.ReaderError) as e:   # times log2(e) it is infinite
+        rd.prompt_attn(q.cuda(), cache, starts([n]), 2.5e38)
+    assert e.value.code == binding.ERR_UNSUPPORTED
+
+
 def test_attn_infinities_in_later_tokens_do_not_reach_earlier_rows(rd):
     rng = np.random.default_rng(5)
     for ns, lens, where in [((200,), (0,), (0, 3, 64, 150, 199)), ((50, 90), (70, 20), (10, 33)), ((300,), (100,), (299,)), ((1,), (90,), (90 - 1,))]:
