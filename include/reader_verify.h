@@ -474,7 +474,7 @@ size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  * Causal attention of the new tokens over the cache, which already holds their own keys and values (from
  * reader_prompt_append): token i of sequence b attends to the positions 0 .. seq_lens[b] + i.  With seq_lens[b] = 0 it
  * is a whole prompt, otherwise the next piece of one, with a single token plain decoding; a call may mix them.
- *   q, out     bf16 [total_tokens][n_q_heads][head_dim]
+ *   q, out     bf16 [total_tokens][n_q_heads][head_dim]; out may be q
  *   lse_out    f32 [total_tokens][n_q_heads], natural log of the softmax denominator; nullable
  *   update_seq_lens  non-zero: seq_lens[b] += new tokens afterwards (pass 0 for all but the last layer)
  *   workspace  at least reader_prompt_workspace_bytes(...) bytes, 256-byte aligned; contents are scratch, calls that

@@ -232,6 +232,19 @@ def test_attn_infinities_in_long_pieces(rd):
     check_attn(rd, bf16(rng, 300, 32, 64).cuda(), cache, ns, lens, 0.1)
 
 
+@pytest.mark.parametrize("case", [((40,), (10,), 8, 2), ((300, 1, 77), (2000, 5000, 0), 8, 2), ((1,) * 5, (900, 0, 7, 4000, 64), 8, 2),
+                                  ((4000, 3300), (0, 50), 16, 16)])
+def test_attn_in_place(rd, case):
+    """out may be q: a unit's queries have been read before its rows are written, in every form of the call."""
+    ns, lens, Hq, Hkv = case
+    rng = np.random.default_rng(47)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, 64)
+    q = bf16(rng, sum(ns), Hq, 64).cuda()
+    want, _ = rd.prompt_attn(q, cache, starts(ns), 0.125)
+    out, st = rd.prompt_attn(q, cache, starts(ns), 0.125, out=q)
+    assert out is q and not st.any() and torch.equal(out, want)
+
+
 def test_attn_very_large_batch(rd):
     rng = np.random.default_rng(44)
     B = 3000
