@@ -1102,9 +1102,10 @@ struct Merged {
         mx = -INFINITY;
         l = o[0] = o[1] = o[2] = o[3] = 0.f;
     }
+    // A share with the maximum -inf has weight 0, not no weight: the row may see none of its keys (sum and output are 0), or
+    // scores that are all NaN beside masked ones, which a maximum ignores and only the sum and the output tell.
     __device__ __forceinline__ void add(float m2, float l2, const float4 &y) {
-        if (m2 == -INFINITY) return;   // the row sees none of these keys
-        const float up = fmaxf(mx, m2), w = mx == -INFINITY ? 0.f : exp2f(mx - up), w2 = exp2f(m2 - up);
+        const float up = fmaxf(mx, m2), w = mx == -INFINITY ? 0.f : exp2f(mx - up), w2 = m2 == -INFINITY ? 0.f : exp2f(m2 - up);
         mx = up;
         l = l * w + l2 * w2;
         o[0] = o[0] * w + y.x * w2; o[1] = o[1] * w + y.y * w2; o[2] = o[2] * w + y.z * w2; o[3] = o[3] * w + y.w * w2;

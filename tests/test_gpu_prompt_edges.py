@@ -1,0 +1,81 @@
+"""Prompt attention and append where they can go wrong quietly: NaN in units that are cut and merged, rows that belong to
+nobody beside rows that count, the long forms at both head dimensions, in-place calls.  Tolerances as in test_gpu_prompt."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_prompt import PAGE, bf16, check_attn, make_cache, plain_attn, rd, starts, within  # noqa: F401 (rd: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def run(rd, q, cache, ns, scale):
+    tokens, Hq, D = q.shape
+    out = torch.full((tokens, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((tokens, Hq), 7.0, dtype=torch.float32, device="cuda")
+    rd.prompt_workspace().fill_(0xFF)
+    _, st = rd.prompt_attn(q, cache, starts(ns), scale, out=out, lse=lse)
+    assert st.tolist() == [0] * len(ns)
+    return out.cpu(), lse.cpu()
+
+
+def nan_rows_only(got, want, nan):
+    """Rows where `nan` [tokens, heads] holds are NaN throughout, the others are what they are without the NaN."""
+    (out, lse), (o, z, tol, ltol) = got, want
+    assert torch.isnan(out[nan]).all() and torch.isnan(lse[nan]).all()
+    within(out[~nan], o[~nan], tol[~nan])
+    assert ((lse.double() - z).abs()[~nan] <= ltol[~nan]).all()
+
+
+# ---------------------------------------------------------------------------------------------- NaN in units that are cut
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_keys_from_a_tile_boundary_on_reach_every_row_that_sees_them(rd, D):
+    """Units of two 128-row tiles cut into a few pieces.  In the tile where the NaN begin, a row sees NaN keys and keys that
+    are masked, nothing else: a piece that holds only this tile for it has the maximum -inf and a NaN sum."""
+    rng = np.random.default_rng(60 + D)
+    n, L, scale = 1500, 1300, 0.09
+    cache = make_cache(rng, [L], [L + n], 2, D)
+    q = bf16(rng, n, 2, D).cuda()
+    want = plain_attn(q, cache, [n], [L], scale)
+    pos = torch.arange(L + n)
+    page = cache.page_table[0].cpu()[pos // PAGE].long().cuda()
+    clean = cache.k_pool.clone()
+    for t in range(0, (L + n) // 128 + 1):
+        cache.k_pool.copy_(clean)
+        first = 128 * t
+        cache.k_pool[page[first:], 1, pos[first:].cuda() % PAGE] = float("nan")
+        nan = torch.zeros(n, 2, dtype=torch.bool)
+        nan[max(0, first - L):, 1] = True
+        nan_rows_only(run(rd, q, cache, [n], scale), want, nan)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_keys_over_whole_pieces_of_a_long_history(rd, D):
+    """Few rows over a long history: twenty pieces to a unit, some of them NaN from end to end."""
+    rng = np.random.default_rng(62 + D)
+    n, L, scale = 3, 20000, 0.09
+    cache = make_cache(rng, [L], [L + n], 2, D)
+    q = bf16(rng, n, 4, D).cuda()
+    want = plain_attn(q, cache, [n], [L], scale)
+    pos = torch.arange(L + n)
+    page = cache.page_table[0].cpu()[pos // PAGE].long().cuda()
+    clean = cache.k_pool.clone()
+    for lo, hi in ((4096, 8192), (0, 2048), (16384, L + n), (0, L + n), (12800, 12801)):
+        cache.k_pool.copy_(clean)
+        cache.k_pool[page[lo:hi], 0, pos[lo:hi].cuda() % PAGE] = float("nan")
+        nan = torch.zeros(n, 4, dtype=torch.bool)
+        nan[:, :2] = True
+        nan_rows_only(run(rd, q, cache, [n], scale), want, nan)
+
+
+@pytest.mark.parametrize("ns,L", [((1500,), 1300), ((3,), 20000), ((40,), 10), ((1,), 100)])
+def test_a_nan_query_is_nan_in_output_and_lse(rd, ns, L):
+    rng = np.random.default_rng(64)
+    n = ns[0]
+    cache = make_cache(rng, [L], [L + n], 2, 128)
+    q = bf16(rng, n, 4, 128)
+    want = plain_attn(q, cache, ns, [L], 0.09)
+    nan = torch.zeros(n, 4, dtype=torch.bool)
+    nan[n // 2, 1] = nan[n - 1, 2] = True
+    q[nan] = float("nan")
+    nan_rows_only(run(rd, q.cuda(), cache, ns, 0.09), want, nan)
