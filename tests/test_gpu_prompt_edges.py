@@ -79,3 +79,40 @@ def test_a_nan_query_is_nan_in_output_and_lse(rd, ns, L):
     nan[n // 2, 1] = nan[n - 1, 2] = True
     q[nan] = float("nan")
     nan_rows_only(run(rd, q.cuda(), cache, ns, 0.09), want, nan)
+
+
+# ---------------------------------------------------------------------------------------------- rows that belong to nobody
+@pytest.mark.parametrize("ns,lens,extra", [((37, 60), (700, 0), 0), ((37, 60), (700, 0), 200), ((1, 1, 1, 1), (900, 3, 40, 17), 0),
+                                           ((1, 1, 1, 1), (900, 3, 40, 17), 300), ((300, 90), (2300, 0), 0)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_sequences_bits_do_not_depend_on_its_neighbour(rd, ns, lens, extra, D):
+    """A query tile that a sequence does not fill holds the next sequence's queries behind it."""
+    rng = np.random.default_rng(70)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 2, D)
+    if extra:   # a wide page table: the call is cut into ranges
+        wide = torch.full((len(ns), extra), -1, dtype=torch.int32, device="cuda")
+        wide[:, :cache.page_table.shape[1]] = cache.page_table
+        cache.page_table = wide
+    q = bf16(rng, sum(ns), 8, D)
+    calm, calm_lse = run(rd, q.cuda(), cache, ns, 0.09)
+    for by in (40.0, -40.0, float("nan"), float("inf"), 2.0 ** 100):
+        other = q.clone()
+        other[ns[0]:] *= by
+        out, lse = run(rd, other.cuda(), cache, ns, 0.09)
+        assert torch.equal(out[:ns[0]], calm[:ns[0]]) and torch.equal(lse[:ns[0]], calm_lse[:ns[0]]), by
+
+
+@pytest.mark.parametrize("Hq", [3, 5, 7])
+def test_bits_do_not_depend_on_what_an_earlier_call_left_in_shared_memory(rd, Hq):
+    """Groups that do not divide 128 leave rows of the query tile that no copy writes."""
+    rng = np.random.default_rng(71)
+    B, n, L = 200, 2 * (128 // Hq), 400
+    filler = make_cache(rng, [0] * B, [256] * B, 1, 64)
+    cache = make_cache(rng, [L] * 3, [L + n] * 3, 1, 64)
+    q = bf16(rng, 3 * n, Hq, 64).cuda()
+    seen = []
+    for by in (1.0, 50.0, 2.0 ** 100):
+        rd.prompt_attn(bf16(rng, 256 * B, 1, 64, scale=by).cuda(), filler, starts([256] * B), 0.125)   # every SM's query tiles
+        seen.append(run(rd, q, cache, [n] * 3, 0.125))
+    for out, lse in seen[1:]:
+        assert torch.equal(out, seen[0][0]) and torch.equal(lse, seen[0][1])
