@@ -54,11 +54,8 @@ constexpr int kProducerWarp = 8, kMmaWarp = 9, kValueWarp = 10;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kRaiseMaxBy = 8.f;   // log2 units
 constexpr float kHugeScore = 536870912.f;
-// -infinity: every tile takes the slow path.  +infinity for a row without a query (the next sequence's, or what an earlier
-// call left in shared memory): it has no say in how the rows that share its warp are computed, so their bits do not depend on it.
-__device__ __forceinline__ float margin_of(float mx, bool live) {
-    return !live ? INFINITY : fabsf(mx) > kHugeScore && fabsf(mx) < INFINITY ? -INFINITY : kRaiseMaxBy;
-}
+// -infinity: every tile takes the slow path
+__device__ __forceinline__ float margin_of(float mx) { return fabsf(mx) > kHugeScore && fabsf(mx) < INFINITY ? -INFINITY : kRaiseMaxBy; }
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 constexpr int kMaxStages = 8;
 constexpr int kLateStartTiles = 20;  // shortest piece whose slot 1 begins half a step late
@@ -806,9 +803,13 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             // the last key this row sees; rows without a query see what the first row sees
             const int last_key = sg->L + sg->first_token + (live ? unit_token : 0);
             const int warp_min = __reduce_min_sync(0xffffffffu, last_key);
-            float mx = -INFINITY, l = 0.f;    // running maximum (scaled, log2 units) and row sum
+            // Running maximum (scaled, log2 units) and row sum.  A row without a query (it holds the next sequence's, or what an
+            // earlier call left in shared memory) has the maximum +inf from the start: it never asks for a higher one, so the
+            // rows that share its warp are computed as if it were not there.  (A margin of its own for such rows, or its vote
+            // masked, costs a register in the loop: four long prompts 1600 us, this way 1578.)
+            float mx = live ? -INFINITY : INFINITY, l = 0.f;
             const int j0 = narrow ? slot : 0, dj = narrow ? 2 : 1, nt = sg->nt;
-            float margin = INFINITY;          // the maximum is raised by scores that exceed it by more
+            float margin = kRaiseMaxBy;       // the maximum is raised by scores that exceed it by more
             bool any = false;
             for (int j = j0; j < nt; j += dj) {
                 const int key0 = sg->tile(j) * kKeyTile;
@@ -855,8 +856,8 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                                 if (i > lim) sc[i] = kNegInf;
                         }
                         if (first) {
-                            mx = tile_top();   // (-inf where the row sees none of these keys)
-                            margin = margin_of(mx, live);
+                            mx = fmaxf(mx, tile_top());   // (-inf where the row sees none of these keys)
+                            margin = margin_of(mx);
                             first = false;
                         }
                         const float neg = mx == -INFINITY ? 0.f : -mx;
@@ -879,8 +880,8 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
                             tmem_st16(tO + c, o);
                         }
-                        margin = margin_of(mx, live);
-                        if (__any_sync(0xffffffffu, margin == -INFINITY)) {
+                        margin = margin_of(mx);
+                        if (__any_sync(0xffffffffu, margin != kRaiseMaxBy)) {
                             huge = true;
                             break;
                         }
