@@ -482,7 +482,8 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
             Schedule schedule;
             if (!p.alone) {
                 schedule.init(p, reinterpret_cast<int32_t *>(smem + C::kOffRing), lane);
-                if (lane == 0) fence_proxy_async();   // the ring was scratch until here
+                // the ring was every lane's scratch until here: each orders its own accesses before the copies that one of them issues
+                fence_proxy_async();
                 __syncwarp();
             }
             Piece s;

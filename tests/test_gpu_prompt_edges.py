@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_prompt import PAGE, bf16, check_attn, make_cache, plain_attn, rd, starts, within  # noqa: F401 (rd: a fixture)
+from test_gpu_prompt import HALF, PAGE, bf16, check_attn, make_cache, plain_attn, rd, starts, within  # noqa: F401 (rd: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +116,36 @@ def test_bits_do_not_depend_on_what_an_earlier_call_left_in_shared_memory(rd, Hq
         seen.append(run(rd, q, cache, [n] * 3, 0.125))
     for out, lse in seen[1:]:
         assert torch.equal(out, seen[0][0]) and torch.equal(lse, seen[0][1])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_largest_batch(rd, D):
+    """As many sequences as a call takes: the partition's words fill the whole ring before its first copy."""
+    from paper_2508_09072_b200 import binding
+    B = 32768
+    g = torch.Generator(device="cuda").manual_seed(72)
+    lens = torch.randint(0, PAGE - 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    ns = (torch.rand(B, generator=g, device="cuda") < 0.9).int()
+    start = torch.cat([ns.new_zeros(1), ns.cumsum(0)]).int()
+    tokens = int(start[-1])
+    k, v = (torch.randn(B, 1, PAGE, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    cache = binding.KvCache(k, v, torch.randperm(B, generator=g, device="cuda").int()[:, None].contiguous(), lens)
+    q = torch.randn(tokens, 2, D, generator=g, device="cuda").to(torch.bfloat16)
+    out, st = rd.prompt_attn(q, cache, start, 0.1)
+    assert not st.any()
+    seq = ns.nonzero().flatten()
+    page = cache.page_table[seq, 0].long()
+    for lo in range(0, tokens, 4096):
+        at = slice(lo, min(lo + 4096, tokens))
+        kk, vv, qq = k[page[at], 0].double(), v[page[at], 0].double(), q[at].double()
+        seen = torch.arange(PAGE, device="cuda") <= lens[seq[at], None]
+        s = (torch.einsum("thd,tkd->thk", qq, kk) * 0.1).masked_fill(~seen[:, None], float("-inf"))
+        mag = (torch.einsum("thd,tkd->thk", qq.abs(), kk.abs()) * 0.1).amax(-1, keepdim=True)
+        w = torch.softmax(s, -1)
+        want = torch.einsum("thk,tkd->thd", w, vv)
+        tol = (HALF + 4 * (D * 2.0 ** -23 * mag + 1e-6)) * torch.einsum("thk,tkd->thd", w, vv.abs()) + HALF * 1.01 * want.abs() + 1e-30
+        assert ((out[at].double() - want).abs() <= tol).all()
+    with pytest.raises(binding.ReaderError) as e:   # one more is refused
+        more = binding.KvCache(k, v, torch.zeros(B + 1, 1, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda"))
+        rd.prompt_attn(q, more, torch.zeros(B + 2, dtype=torch.int32, device="cuda"), 0.1)
+    assert e.value.code == binding.ERR_UNSUPPORTED
