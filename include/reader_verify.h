@@ -480,7 +480,8 @@ size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  *   workspace  at least reader_prompt_workspace_bytes(...) bytes, 256-byte aligned; contents are scratch, calls that
  *              share it must not overlap on the GPU
  *   status_out i32 [batch]: READER_ERR_CAPACITY, READER_ERR_BAD_PAGE, READER_ERR_TIMEOUT: that sequence's rows of out and
- *              lse_out are zero and its length is not advanced
+ *              lse_out are zero and its length is not advanced.  (After READER_ERR_TIMEOUT rows may also hold their values,
+ *              and a later call with the same workspace may report the same event once more.)
  * softmax_scale > 0 and at most 2e38, n_q_heads / n_kv_heads at most 128, batch at most 32768, else
  * READER_ERR_UNSUPPORTED.  What the cache holds at positions a token does not see has no influence on its row,
  * infinities and NaN included.
@@ -491,6 +492,10 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
                                  const reader_prompt *prompt, float softmax_scale, int32_t update_seq_lens, void *out,
                                  float *lse_out, void *workspace, size_t workspace_bytes, int32_t *status_out,
                                  void *stream);
+
+/* Testing aid (host call): thread block `cta` of each following reader_prompt_attn call on this context acts, once its work
+ * is done, as one that gave up a bounded wait (READER_ERR_TIMEOUT); no wait runs out.  -1 turns it off. */
+reader_status reader_set_prompt_give_up(reader_ctx *ctx, int32_t cta);
 
 #ifdef __cplusplus
 }

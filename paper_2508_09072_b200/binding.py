@@ -28,7 +28,8 @@ EXPORTS = ("reader_create", "reader_destroy", "reader_status_string", "reader_se
            "reader_kv_commit", "reader_accept_noalloc", "reader_sample_targets", "reader_kv_rearrange", "reader_kv_commit_layers",
            "reader_accept_commit", "reader_verify_prepare", "reader_verify_attn_prepared",
            "reader_padded_workspace_bytes", "reader_verify_attn_padded", "reader_padded_append", "reader_padded_rearrange",
-           "reader_prompt_append", "reader_tree_rotate", "reader_prompt_workspace_bytes", "reader_prompt_attn")
+           "reader_prompt_append", "reader_tree_rotate", "reader_prompt_workspace_bytes", "reader_prompt_attn",
+           "reader_set_prompt_give_up")
 
 
 class ReaderError(RuntimeError):
@@ -124,6 +125,8 @@ def load_library() -> ctypes.CDLL:
     lib.reader_padded_rearrange.restype = c_int32
     lib.reader_prompt_workspace_bytes.argtypes = [c_void_p, c_int32]
     lib.reader_prompt_workspace_bytes.restype = c_size_t
+    lib.reader_set_prompt_give_up.argtypes = [c_void_p, c_int32]
+    lib.reader_set_prompt_give_up.restype = c_int32
     lib.reader_kv_commit.argtypes = [c_void_p, POINTER(_KvCache), c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                                      c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
     lib.reader_kv_commit.restype = c_int32
@@ -583,6 +586,12 @@ class Reader:
         if st != OK:
             raise ReaderError(st, "reader_tree_rotate")
         return out, k_tree, v_tree, status
+
+    def set_prompt_give_up(self, cta: int = -1) -> None:
+        """Testing aid: that thread block of the following prompt_attn calls reports a wait that ran out; -1: none."""
+        st = self.lib.reader_set_prompt_give_up(self._h, int(cta))
+        if st != OK:
+            raise ReaderError(st, "reader_set_prompt_give_up")
 
     def prompt_workspace(self) -> torch.Tensor:
         """A cached device buffer for prompt_attn (of the size that any call needs: it is never replaced)."""

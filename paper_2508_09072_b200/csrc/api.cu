@@ -82,6 +82,7 @@ reader_status reader_create(reader_ctx **out, int device) {
     ctx->ev_start = ctx->ev_stop = nullptr;
     ctx->ev_acc_start = ctx->ev_acc_stop = nullptr;
     ctx->prompt_attr_set = false;
+    ctx->prompt_give_up = -1;
     ctx->prepared = PreparedRecord{};
     reader_status st = sm100_host_init(&ctx->sm100, device);
     if (st != READER_OK) {
@@ -650,7 +651,7 @@ reader_status check_prompt(const reader_kv_cache *c, const reader_prompt *t, con
 }
 
 struct PromptWs {
-    size_t partial_o, partial_ml, pieces, gave_up, counter, total;
+    size_t partial_o, partial_ml, pieces, gave_up, late_notes, counter, total;
 };
 PromptWs prompt_ws(const reader_ctx *ctx, int D) {
     PromptWs w{};
@@ -661,6 +662,7 @@ PromptWs prompt_ws(const reader_ctx *ctx, int D) {
     w.partial_ml = take(sizeof(float) * rows * 2);
     w.pieces = take(sizeof(PieceDesc) * (size_t)ctx->n_sm);
     w.gave_up = take(sizeof(int32_t) * (size_t)ctx->n_sm);
+    w.late_notes = take(sizeof(uint64_t) * (size_t)ctx->n_sm);
     w.counter = take(sizeof(int32_t));
     w.total = at;
     return w;
@@ -725,6 +727,12 @@ reader_status reader_tree_rotate(reader_ctx *ctx, const void *q, const void *k, 
     return launch_status();
 }
 
+reader_status reader_set_prompt_give_up(reader_ctx *ctx, int32_t cta) {
+    if (!ctx || cta < -1) return READER_ERR_INVALID_ARG;
+    ctx->prompt_give_up = cta;
+    return READER_OK;
+}
+
 size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim) {
     if (!ctx || (head_dim != 64 && head_dim != 128)) return 0;
     return prompt_ws(ctx, head_dim).total;
@@ -768,6 +776,8 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
     p.partial_ml = reinterpret_cast<float *>(ws + w.partial_ml);
     p.pieces = reinterpret_cast<PieceDesc *>(ws + w.pieces);
     p.gave_up = reinterpret_cast<int32_t *>(ws + w.gave_up);
+    p.late_notes = reinterpret_cast<uint64_t *>(ws + w.late_notes);
+    p.give_up = ctx->prompt_give_up;
     cudaStream_t st = (cudaStream_t)stream;
     if (tokens > 0) {
         // entries of the list, going by the page table's width; no CTA without work

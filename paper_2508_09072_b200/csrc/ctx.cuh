@@ -19,6 +19,7 @@ struct reader_ctx {
     int partition;    // 0 auto, 1 equal ranges, 2 aligned whenever a prefix is shared
     reader::Sm100Host sm100;
     bool prompt_attr_set;   // the prompt attention kernels have their shared-memory limit
+    int prompt_give_up;     // thread block of the prompt attention that reports a wait that ran out (testing aid); -1: none
     cudaEvent_t ev_start, ev_stop;  // optional timing hooks around the main attention kernel
     cudaEvent_t ev_acc_start, ev_acc_stop;  // and around the argmax kernel of reader_accept
     PreparedRecord prepared;

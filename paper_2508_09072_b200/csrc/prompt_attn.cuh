@@ -53,7 +53,10 @@ struct PromptAttnParams {
     float *partial_ml;            // [2 n_ctas][256][2]
     PieceDesc *pieces;            // [n_ctas]
     int32_t *gave_up;             // [n_ctas]
+    uint64_t *late_notes;         // [n_ctas], single-launch form: kLateNote in the word of a sequence's first unit, see note_late
+    int give_up;                  // a CTA that says it gave up when it is done (testing aid); -1: none
 };
+constexpr uint64_t kLateNote = 0x9d6b2f04c18e73a5ull;   // (the workspace holds anything beforehand)
 
 // Whether a sequence takes part: what the host cannot check and the partition depends on.
 __host__ __device__ inline bool prompt_len_ok(int L, int n, int max_pages) {

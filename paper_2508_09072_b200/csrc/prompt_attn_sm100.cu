@@ -36,7 +36,8 @@
 // Other calls are followed by the finishing kernel below.
 //
 // Every wait is bounded: a CTA that waits a second without progress marks its word in the workspace, stops waiting
-// and runs to its end; the finishing kernel turns the mark into status words and zero rows.
+// and runs to its end; the finishing kernel turns the mark into status words and zero rows.  In the single-launch form the
+// CTA itself zeroes its unit's rows and sees to the status word (note_late).
 #include <cuda.h>
 
 #include "prompt_attn.cuh"
@@ -395,6 +396,26 @@ __device__ void report_idle(const PromptAttnParams &p, int lane) {
     }
 }
 
+// Single-launch form: the status word of a sequence whose units several CTAs do.  The CTA of its first unit (`first`) writes it
+// (report), and one that gives up, READER_ERR_TIMEOUT (note_late), in no order: the first unit's CTA may even start after
+// another one's second has passed.  So that the error is what stays, the one that gives up leaves a note before it writes,
+// and the other one looks for the note after it has written: whichever write is the last, it is the error.  (A note may come
+// after that look, and is then found by the next call that puts the sequence's units on the same CTA with the same
+// workspace: a call that gave up can be reported once more, never less.)
+__device__ __forceinline__ void note_late(const PromptAttnParams &p, int b, int first) {
+    *(volatile uint64_t *)&p.late_notes[first] = kLateNote;
+    __threadfence();
+    *(volatile int32_t *)&p.status[b] = READER_ERR_TIMEOUT;
+}
+__device__ __forceinline__ void report(const PromptAttnParams &p, int b, int first, int status) {
+    *(volatile int32_t *)&p.status[b] = status;
+    __threadfence();
+    if (*(volatile uint64_t *)&p.late_notes[first] == kLateNote) {
+        *(volatile uint64_t *)&p.late_notes[first] = 0;
+        *(volatile int32_t *)&p.status[b] = READER_ERR_TIMEOUT;
+    }
+}
+
 __device__ __forceinline__ bool nonfinite_bits(uint32_t half) { return (half & 0x7f80u) == 0x7f80u; }
 
 template <int D>
@@ -405,11 +426,13 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (base & 1023u) {   // the swizzled tiles need 1024-byte alignment; never seen, but checked
+    if (base & 1023u) {   // the swizzled tiles need 1024-byte alignment; never seen, but checked (it is the same for all CTAs)
+        grid_dependency_wait();
         if (tid == 0) {
             p.gave_up[blockIdx.x] = 1;
             p.pieces[blockIdx.x].b = -1;
         }
+        for (int b = tid; p.alone && blockIdx.x == 0 && b < p.B; b += kThreads) p.status[b] = READER_ERR_CUDA;
         return;
     }
     Misc *m = reinterpret_cast<Misc *>(smem + C::kOffMisc);
@@ -557,14 +580,16 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                         bad_page |= pg < 0 || pg >= p.num_pages;
                     }
                     const bool reject = __any_sync(0xffffffffu, bad_page);
-                    if (reject && lane == 0) *(volatile bool *)&m->piece[i].reject = true;
+                    if (reject && lane == 0) *(volatile bool *)&m->piece[i].reject = true;   // (before the values are asked for)
                     __syncwarp();
-                    if (s.h == 0 && s.block == 0 && lane == 0) p.status[s.b] = reject ? READER_ERR_BAD_PAGE : READER_OK;
                 }
                 for (int j = 0; j < s.nt; ++j) {
                     load(vc, &vmap, j, true);
                     if (j + ahead < s.nt) load(kc, &kmap, j + ahead, false);
                 }
+                // (beside the last products and the epilogue this takes no time)
+                if (p.alone && s.h == 0 && s.block == 0 && lane == 0) report(p, s.b, blockIdx.x, m->piece[0].reject ? READER_ERR_BAD_PAGE : READER_OK);
+                __syncwarp();
             }
             // a CTA that gave up must not exit under its own copies: let the last ones land (bounded)
             if (*abort_s) {
@@ -1066,10 +1091,17 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
-    if (tid == 0) p.gave_up[blockIdx.x] = *abort_s;
-    if (p.alone && *abort_s && m->piece[0].nt > 0) {   // (published before anything could be waited for)
-        zero_sequence(p, m->piece[0].b, D, tid, kThreads);
-        if (tid == 0) p.status[m->piece[0].b] = READER_ERR_TIMEOUT;
+    const bool late = *abort_s || (int)blockIdx.x == p.give_up;
+    if (tid == 0) p.gave_up[blockIdx.x] = late;
+    const Piece &s = m->piece[0];
+    if (p.alone && late && s.nt > 0) {   // (published before anything could be waited for)
+        const int row_pieces = p.G * (D / 8);   // of the unit's heads of a token
+        for (int i = tid; i < s.u.tokens * row_pieces; i += kThreads) {
+            const size_t row = (size_t)(s.start + s.first_token + i / row_pieces) * p.Hq + (size_t)s.h * p.G;
+            reinterpret_cast<uint4 *>(p.out + row * D)[i % row_pieces] = make_uint4(0, 0, 0, 0);
+            if (p.lse && i % (D / 8) == 0) p.lse[row + i % row_pieces / (D / 8)] = 0.f;
+        }
+        if (tid == 0) note_late(p, s.b, (int)blockIdx.x - (s.block * p.Hkv + s.h));
     }
 }
 

@@ -149,3 +149,90 @@ def test_the_largest_batch(rd, D):
         more = binding.KvCache(k, v, torch.zeros(B + 1, 1, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda"))
         rd.prompt_attn(q, more, torch.zeros(B + 2, dtype=torch.int32, device="cuda"), 0.1)
     assert e.value.code == binding.ERR_UNSUPPORTED
+
+
+# ---------------------------------------------------------------------------------------------- a thread block that gives up
+# (no wait runs out in these tests: a thread block says so when its work is done, or the host leaves the note that one would)
+@pytest.fixture
+def give_up(rd):
+    yield rd.set_prompt_give_up
+    rd.set_prompt_give_up(-1)
+
+
+def unit_of(cta, ns, Hkv, tokens_per_unit):
+    """(sequence, block, head) of a single-launch call's thread block."""
+    for b, n in enumerate(ns):
+        units = -(-n // tokens_per_unit) * Hkv
+        if cta < units:
+            return b, cta // Hkv, cta % Hkv
+        cta -= units
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_one_that_gives_up_in_the_single_launch_form(rd, give_up, D):
+    from paper_2508_09072_b200 import binding
+    rng = np.random.default_rng(75)
+    ns, lens, Hq, Hkv = [100, 0, 1, 64], [70, 3, 200, 0], 8, 2     # 64 tokens a unit: 2 + 0 + 1 + 1 blocks of 2 heads
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, D)
+    q = bf16(rng, sum(ns) + 1, Hq, D).cuda()
+    good, good_lse = check_attn(rd, q, cache, ns, lens, 0.1)
+    at = np.concatenate([[0], np.cumsum(ns)])
+    ws = torch.full_like(rd.prompt_workspace(), 0xFF)
+
+    def call():
+        out, lse = torch.full_like(q, 7.0), torch.full((len(q), Hq), 7.0, device="cuda")
+        _, st = rd.prompt_attn(q, cache, starts(ns), 0.1, out=out, lse=lse, workspace=ws)
+        return out, lse, st.tolist()
+    for cta in range(9):
+        give_up(cta)
+        out, lse, st = call()
+        want, want_lse, want_st = good.clone(), good_lse.clone(), [0] * 4
+        if cta < 8:
+            b, block, h = unit_of(cta, ns, Hkv, 64)
+            rows = slice(at[b] + 64 * block, min(at[b] + 64 * block + 64, at[b + 1]))
+            want[rows, 4 * h:4 * h + 4] = 0
+            want_lse[rows, 4 * h:4 * h + 4] = 0
+            want_st[b] = binding.ERR_TIMEOUT
+        assert st == want_st, cta
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), cta
+        give_up(-1)
+        out, lse, st = call()      # the event may be reported once more, with the right rows
+        assert all(x in (0, y) for x, y in zip(st, want_st)) and torch.equal(out, good)
+        out, lse, st = call()
+        assert st == [0] * 4 and torch.equal(out, good) and torch.equal(lse, good_lse)
+    # the note of one that gave up before the first unit's thread block began
+    ws.view(torch.int64).fill_(0x9d6b2f04c18e73a5 - 2 ** 64)
+    out, lse, st = call()
+    assert st == [binding.ERR_TIMEOUT, 0, binding.ERR_TIMEOUT, binding.ERR_TIMEOUT] and torch.equal(out, good)
+    assert call()[2] == [0] * 4
+    # a bad page is still reported, and the one that gives up has the last word
+    cache.page_table[3, 0] = -1
+    assert call()[2] == [0, 0, 0, binding.ERR_BAD_PAGE]
+    give_up(7)
+    out, lse, st = call()
+    assert st == [0, 0, 0, binding.ERR_TIMEOUT] and not out[at[3]:at[4]].any() and torch.equal(out[:at[3]], good[:at[3]])
+
+
+@pytest.mark.parametrize("form", ["ranges", "counter", "advancing"])
+def test_one_that_gives_up_in_the_other_forms(rd, give_up, form):
+    from paper_2508_09072_b200 import binding
+    rng = np.random.default_rng(76)
+    ns, lens = [300, 0, 40, 310], [70, 5, 10, 1900]
+    Hq, Hkv, D = (128, 16, 64) if form == "counter" else (4, 2, 128)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, D)
+    q = bf16(rng, sum(ns) + 1, Hq, D).cuda()
+    update = form == "advancing"
+    good, _ = rd.prompt_attn(q, cache, starts(ns), 0.1)
+    for cta in (0, 5):
+        out, lse = torch.full_like(q, 7.0), torch.full((len(q), Hq), 7.0, device="cuda")
+        give_up(cta)
+        _, st = rd.prompt_attn(q, cache, starts(ns), 0.1, out=out, lse=lse, update_seq_lens=update)
+        assert st.tolist() == [binding.ERR_TIMEOUT] * 4 and cache.seq_lens.tolist() == lens
+        assert not out[:-1].any() and not lse[:-1].any() and (out[-1] == 7.0).all() and (lse[-1] == 7.0).all()
+        give_up(-1)
+        out, st = rd.prompt_attn(q, cache, starts(ns), 0.1)
+        assert st.tolist() == [0] * 4 and torch.equal(out[:-1], good[:-1])
+    assert cache.seq_lens.tolist() == lens
+    with pytest.raises(binding.ReaderError) as e:
+        give_up(-2)
+    assert e.value.code == binding.ERR_INVALID_ARG

@@ -47,3 +47,8 @@ def test_the_native_module_takes_cuda_tensors_only(native):
         native.tree_rotate()
     with pytest.raises(TypeError, match="integer"):
         native.prompt_attn(*args(device="cuda"))
+
+
+def test_the_testing_aid_refuses_a_missing_context(native):
+    from paper_2508_09072_b200 import binding
+    assert binding.load_library().reader_set_prompt_give_up(None, 0) == binding.ERR_INVALID_ARG
