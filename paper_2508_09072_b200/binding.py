@@ -8,6 +8,7 @@ present, calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, Structure, c_float, c_int32, c_size_t, c_void_p
 from dataclasses import dataclass
@@ -211,7 +212,6 @@ class Reader:
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2508_09072_b200 needs a CUDA device; there is no CPU fallback")
         self.lib = load_library()
-        self._native = load_native()
         self.device = int(device)
         torch.cuda.set_device(self.device)
         torch.zeros(1, device=f"cuda:{self.device}")   # make sure the context exists
@@ -222,6 +222,11 @@ class Reader:
         self._h = h
         self._ws: Optional[torch.Tensor] = None
         self._prompt_ws: Optional[torch.Tensor] = None
+
+    @functools.cached_property
+    def _native(self):
+        # loaded by the first prompt call: the other calls need the library alone
+        return load_native()
 
     def close(self):
         if getattr(self, "_h", None):

@@ -10,6 +10,7 @@ CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libreader_verify.so")
 MARSHAL = os.path.join(_HERE, "_marshal.so")   # csrc/marshal.cpp: torch tensors in, C ABI calls out
+MARSHAL_MADE_FOR = os.path.join(CSRC, "_build", "marshal_made_for.txt")   # what it was compiled against, beside its source
 
 SOURCES = ["api.cu", "tree_encode.cu", "verify_attn_generic.cu", "verify_attn_sm100.cu", "combine.cu",
            "accept.cu", "accept_noalloc.cu", "sample.cu", "kv_commit.cu", "kv_rearrange.cu", "padded_cache.cu", "accept_commit.cu",
@@ -19,11 +20,26 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-I", INCLUDE, "-I", CSRC]
 
 
-def _newest_source() -> float:
-    t = os.path.getmtime(os.path.join(INCLUDE, "reader_verify.h"))
-    for f in os.listdir(CSRC):
-        t = max(t, os.path.getmtime(os.path.join(CSRC, f)))
-    return t
+def _newest(files) -> float:
+    return max(os.path.getmtime(f) for f in [os.path.join(INCLUDE, "reader_verify.h"), *files])
+
+
+def _library_is_current() -> bool:
+    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))]
+    return os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(files)
+
+
+def _marshal_made_for() -> str:
+    """What the module has to be compiled anew for: it is bound to this torch's C++ interface and this Python's."""
+    import torch
+    return f"torch {torch.__version__} at {os.path.dirname(torch.__file__)}, python {sys.version}"
+
+
+def _marshal_is_current() -> bool:
+    if not (os.path.exists(MARSHAL) and os.path.exists(MARSHAL_MADE_FOR)):
+        return False
+    with open(MARSHAL_MADE_FOR) as f:
+        return f.read() == _marshal_made_for() and os.path.getmtime(MARSHAL) >= _newest([os.path.join(CSRC, "marshal.cpp")])
 
 
 def _marshal_command(out: str) -> list:
@@ -47,13 +63,22 @@ def _build_marshal(verbose: bool = False) -> None:
     if p.returncode != 0:
         raise RuntimeError("g++ failed")
     os.replace(tmp, MARSHAL)
+    os.makedirs(os.path.dirname(MARSHAL_MADE_FOR), exist_ok=True)
+    with open(MARSHAL_MADE_FOR, "w") as f:
+        f.write(_marshal_made_for())
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu into objects under csrc/_build and link the shared library; then the Python module."""
-    newest = _newest_source()
-    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= newest for f in (LIB, MARSHAL)):
-        return LIB
+    """The shared library, then the Python module that only the prompt calls need: what is missing or out of date of them."""
+    if force or not _library_is_current():
+        _build_library(verbose)
+    if force or not _marshal_is_current():
+        _build_marshal(verbose)
+    return LIB
+
+
+def _build_library(verbose: bool = False) -> None:
+    """Compile every .cu into objects under csrc/_build and link the shared library."""
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     bdir = os.path.join(CSRC, "_build")
     os.makedirs(bdir, exist_ok=True)
@@ -75,8 +100,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + f".tmp{os.getpid()}"
     subprocess.check_call([nvcc, "-shared", "-o", tmp, *objs, "-lcudart"])
     os.replace(tmp, LIB)
-    _build_marshal(verbose)
-    return LIB
 
 
 if __name__ == "__main__":
