@@ -88,6 +88,15 @@ float real(PyObject *o, const char *name) {
     return (float)x;
 }
 
+bool truth(PyObject *o, const char *name) {
+    const int x = PyObject_IsTrue(o);
+    if (x < 0) {
+        PyErr_Clear();
+        wrong_type(name, "need a truth value");
+    }
+    return x != 0;
+}
+
 struct Cache {
     reader_kv_cache c;
     int32_t batch;
@@ -131,7 +140,7 @@ reader_rotation rotation_of(PyObject *const *a, int64_t head_dim, int device) {
         (i == 1 ? r.q_weight : r.k_weight) = address(w);
     }
     r.eps = real(a[3], "eps");
-    r.interleaved = PyObject_IsTrue(a[4]) == 1;
+    r.interleaved = truth(a[4], "interleaved");
     return r;
 }
 
@@ -248,6 +257,7 @@ PyObject *prompt_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (q.size(2) != c.c.head_dim) wrong_value("q", "its head dimension is not the cache's");
         const reader_prompt p = prompt_of(a[8], c.batch, tokens, device);
         const float scale = real(a[9], "scale");
+        const bool update = truth(a[10], "update_seq_lens");
         const at::Tensor out = output(a[11], q.sizes(), at::kBFloat16, device, "out");
         float *lse = nullptr;
         if (a[12] != Py_None) {
@@ -257,7 +267,7 @@ PyObject *prompt_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
         }
         const at::Tensor &ws = dense(a[13], at::kByte, 1, device, "workspace");
         const at::Tensor status = output(a[14], {c.batch}, at::kInt, device, "status");
-        const reader_status st = reader_prompt_attn(context(a[0]), address(q), small(hq, "q"), &c.c, &p, scale, PyObject_IsTrue(a[10]) == 1,
+        const reader_status st = reader_prompt_attn(context(a[0]), address(q), small(hq, "q"), &c.c, &p, scale, update,
                                                     address(out), lse, address(ws), (size_t)ws.numel(),
                                                     static_cast<int32_t *>(address(status)), stream());
         return results(st, {given_back(a[11], out), given_back(a[14], status)});

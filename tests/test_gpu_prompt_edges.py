@@ -236,3 +236,21 @@ def test_one_that_gives_up_in_the_other_forms(rd, give_up, form):
     with pytest.raises(binding.ReaderError) as e:
         give_up(-2)
     assert e.value.code == binding.ERR_INVALID_ARG
+
+
+# ---------------------------------------------------------------------------------------------- arguments
+def test_a_value_that_is_neither_true_nor_false_is_refused(rd):
+    rng = np.random.default_rng(78)
+    cache = make_cache(rng, [3], [8], 2, 64)
+    q, k = bf16(rng, 5, 4, 64).cuda(), bf16(rng, 5, 2, 64).cuda()
+    neither = torch.tensor([True, False])
+    before = cache.k_pool.clone()
+    with pytest.raises(TypeError, match="interleaved"):
+        rd.prompt_append(q, k, k, cache, starts([5]), interleaved=neither)
+    with pytest.raises(TypeError, match="update_seq_lens"):
+        rd.prompt_attn(q, cache, starts([5]), 0.1, update_seq_lens=neither)
+    with pytest.raises(TypeError, match="interleaved"):
+        rd.tree_rotate(q[None], k[None], k[None], cache.seq_lens, torch.tensor([[-1, 0, 1, 2, 3]], dtype=torch.int32, device="cuda"), interleaved=neither)
+    assert torch.equal(cache.k_pool.view(torch.int16), before.view(torch.int16)) and cache.seq_lens.tolist() == [3]
+    _, st = rd.prompt_append(q, k, k, cache, starts([5]), interleaved=np.bool_(False))
+    assert not st.any()
