@@ -254,3 +254,149 @@ def test_a_value_that_is_neither_true_nor_false_is_refused(rd):
     assert torch.equal(cache.k_pool.view(torch.int16), before.view(torch.int16)) and cache.seq_lens.tolist() == [3]
     _, st = rd.prompt_append(q, k, k, cache, starts([5]), interleaved=np.bool_(False))
     assert not st.any()
+
+
+# ---------------------------------------------------------------------------------------------- long forms, both head dimensions
+@pytest.mark.parametrize("D", [64, 128])
+def test_units_from_the_counter(rd, D):
+    rng = np.random.default_rng(80 + D)
+    ns, lens = [500, 0, 333, 1, 8, 700, 9, 400], [0, 5, 100, 300, 0, 2900, 77, 40]
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 8, D)
+    q = bf16(rng, sum(ns) + 2, 64, D).cuda()
+    for _ in range(2):   # the counter starts anew
+        check_attn(rd, q, cache, ns, lens, 0.09)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L", [1500, 2700])   # pieces of 12 and of 20 key tiles and more
+def test_infinities_in_long_pieces(rd, D, L):
+    rng = np.random.default_rng(82 + D)
+    ns, lens = [300, 300, 301], [L + 200, L + 503, L]
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 16, D)   # NaN and inf behind the last keys
+    q = bf16(rng, sum(ns), 32, D).cuda()
+    check_attn(rd, q, cache, ns, lens, 0.1)
+    for b, j in ((0, 0), (0, 37), (2, 300), (2, 150)):
+        pos = lens[b] + j
+        page = cache.page_table[b, pos // PAGE].long()
+        cache.v_pool[page, ::3, pos % PAGE, 9::13] = float("inf")
+        cache.v_pool[page, 1, pos % PAGE, 4] = float("nan")
+    check_attn(rd, q, cache, ns, lens, 0.1)
+
+
+@pytest.mark.parametrize("D,Hq", [(64, 32), (128, 32), (128, 48)])
+def test_whole_long_units(rd, D, Hq):
+    """Wide units of 20 key tiles and more that one CTA does from end to end: three or so to an equal range (two heads to a
+    group), from the counter (three)."""
+    rng = np.random.default_rng(84 + D)
+    ns, lens = [2600, 700], [1000, 2300]
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 16, D)
+    check_attn(rd, bf16(rng, sum(ns), Hq, D).cuda(), cache, ns, lens, 0.09)
+
+
+def test_long_histories_begun_in_the_middle_at_head_dim_128(rd):
+    """Whole units of more than 64 key tiles at four ring stages; sampled heads."""
+    from paper_2508_09072_b200 import binding
+    rng = np.random.default_rng(86)
+    B, Hkv, D = 10, 32, 128
+    ns, lens = [256] * B, [int(x) for x in rng.integers(8200, 8500, B)]
+    ns[3], ns[7] = 100, 77
+    pages = [(a + b + PAGE - 1) // PAGE for a, b in zip(ns, lens)]
+    g = torch.Generator(device="cuda").manual_seed(86)
+    order = torch.from_numpy(rng.permutation(sum(pages)).astype(np.int32)).cuda()
+    table = torch.full((B, max(pages)), -1, dtype=torch.int32, device="cuda")
+    for b in range(B):
+        table[b, :pages[b]] = order[sum(pages[:b]):sum(pages[:b + 1])]
+    k, v = (torch.randn(sum(pages), Hkv, PAGE, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    cache = binding.KvCache(k, v, table, torch.tensor(lens, dtype=torch.int32).cuda())
+    q = torch.randn(sum(ns), Hkv, D, generator=g, device="cuda").to(torch.bfloat16)
+    out, st = rd.prompt_attn(q, cache, starts(ns), D ** -0.5)
+    assert st.tolist() == [0] * B
+    for b in range(B):
+        at = sum(ns[:b])
+        for h in (b, 31 - b, 15):
+            one = binding.KvCache(k[:, h:h + 1], v[:, h:h + 1], table[b:b + 1], cache.seq_lens[b:b + 1])
+            want, _, tol, _ = plain_attn(q[at:at + ns[b], h:h + 1], one, [ns[b]], [lens[b]], D ** -0.5)
+            within(out[at:at + ns[b], h:h + 1], want, tol)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("case", [((40,), (10,), 8, 2), ((300, 1, 77), (2000, 5000, 0), 8, 2), ((1,) * 5, (900, 0, 7, 4000, 64), 8, 2),
+                                  ((4000, 3300), (0, 50), 16, 16), ((43, 85), (700, 0), 6, 2)])
+def test_attn_in_place(rd, case, D):
+    """out may be q, in every form of the call: the result is that of a call with an output of its own, every time."""
+    ns, lens, Hq, Hkv = case
+    rng = np.random.default_rng(87)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, D)
+    q = bf16(rng, sum(ns), Hq, D).cuda()
+    want, _ = rd.prompt_attn(q, cache, starts(ns), 0.125)
+    for _ in range(3):
+        again = q.clone()
+        out, st = rd.prompt_attn(again, cache, starts(ns), 0.125, out=again)
+        assert out is again and not st.any() and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("tokens", [5, 3000])   # several warps to a token, and one
+@pytest.mark.parametrize("D,Hq,Hkv,inter,rot", [(128, 32, 8, False, 128), (64, 6, 2, True, 32)])
+def test_append_in_place(rd, tokens, D, Hq, Hkv, inter, rot):
+    rng = np.random.default_rng(88)
+    ns, lens = [tokens // 2, 0, tokens - tokens // 2], [70, 3, 0]
+    angle = np.arange(tokens + 80)[:, None] * 10000.0 ** (-np.arange(0, rot, 2) / rot)
+    rope = torch.from_numpy(np.stack([np.cos(angle), np.sin(angle)], 1).astype(np.float32)).cuda()
+    caches = [make_cache(np.random.default_rng(89), lens, [a + b for a, b in zip(ns, lens)], Hkv, D) for _ in range(2)]
+    q, k, v = (bf16(rng, tokens + 1, h, D).cuda() for h in (Hq, Hkv, Hkv))
+    qw, kw = bf16(rng, D).cuda(), bf16(rng, D).cuda()
+    kw_args = dict(rope=rope, q_weight=qw, k_weight=kw, interleaved=inter)
+    want = torch.full_like(q, 7.0)
+    rd.prompt_append(q, k, v, caches[0], starts(ns), out=want, **kw_args)
+    last = q[-1].clone()
+    out, st = rd.prompt_append(q, k, v, caches[1], starts(ns), out=q, **kw_args)
+    assert out is q and not st.any() and torch.equal(q[:-1], want[:-1]) and torch.equal(q[-1], last)
+    for pool in ("k_pool", "v_pool"):
+        assert torch.equal(*(getattr(c, pool).view(torch.int16) for c in caches))
+
+
+# ---------------------------------------------------------------------------------------------- a shared prefix
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ns,lens,prefix", [((1,) * 6, (512, 700, 513, 900, 640, 512), 512), ((33, 1, 0, 300), (256, 300, 256, 1000), 256),
+                                            ((1,) * 4, (4096, 4100, 4500, 4097), 4096)])
+def test_attention_behind_a_shared_prefix(rd, ns, lens, prefix, D):
+    rng = np.random.default_rng(90)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 2, D)
+    cache.page_table[:, :prefix // PAGE] = cache.page_table[0, :prefix // PAGE]
+    q = bf16(rng, sum(ns), 8, D).cuda()
+    plain, _ = rd.prompt_attn(q, cache, starts(ns), 0.09)
+    cache.shared_prefix_len = prefix
+    out, _ = check_attn(rd, q, cache, ns, lens, 0.09)
+    assert torch.equal(out, plain)
+
+
+# ---------------------------------------------------------------------------------------------- large pools
+@pytest.mark.parametrize("D,Hkv", [(64, 8), (128, 8)])
+def test_pages_whose_offsets_pass_32_bits(rd, D, Hkv):
+    """Pools of more than 2^32 elements; the call's pages lie at both ends and around 2^31 and 2^32."""
+    from paper_2508_09072_b200 import binding
+    rng = np.random.default_rng(92)
+    row = Hkv * PAGE * D
+    total = 2 ** 32 // row + 40
+    k_pool, v_pool = (torch.empty(total, Hkv, PAGE, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ns, lens = [300, 1, 70], [1500, 90, 0]
+    pages = [(a + b + PAGE - 1) // PAGE for a, b in zip(ns, lens)]
+    some = [total - 1, 0, 2 ** 31 // row, 2 ** 32 // row, 2 ** 31 // row - 1, 2 ** 32 // row - 1]
+    some += [x for x in range(total - 30, total - 1) if x not in some]
+    table = torch.full((3, max(pages)), -1, dtype=torch.int32)
+    for b in range(3):
+        table[b, :pages[b]] = torch.tensor(some[sum(pages[:b]):sum(pages[:b + 1])])
+    cache = binding.KvCache(k_pool, v_pool, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda())
+    used = torch.tensor(some[:sum(pages)]).cuda()
+    for pool in (k_pool, v_pool):
+        pool[used] = bf16(rng, len(used), Hkv, PAGE, D).cuda()
+    tokens = sum(ns)
+    q, k, v = (bf16(rng, tokens, h, D).cuda() for h in (2 * Hkv, Hkv, Hkv))
+    v[5, 1, 3], v[250, 0, D - 1] = float("inf"), float("nan")
+    q2, st = rd.prompt_append(q, k, v, cache, starts(ns))
+    assert not st.any() and torch.equal(q2, q)
+    pos = torch.cat([torch.arange(L, L + n) for n, L in zip(ns, lens)])
+    seq = torch.cat([torch.full((n,), b) for b, n in enumerate(ns)])
+    page, at = table[seq, pos // PAGE].long().cuda(), (pos % PAGE).cuda()
+    assert torch.equal(k_pool[page, :, at], k) and torch.equal(v_pool[page, :, at].view(torch.int16), v.view(torch.int16))
+    check_attn(rd, q, cache, ns, lens, 0.1)
