@@ -482,8 +482,13 @@ size_t reader_prompt_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  *   status_out i32 [batch]: READER_ERR_CAPACITY, READER_ERR_BAD_PAGE, READER_ERR_TIMEOUT: that sequence's rows of out and
  *              lse_out are zero and its length is not advanced.  (After READER_ERR_TIMEOUT rows may also hold their values,
  *              and a later call with the same workspace may report the same event once more.)
- * softmax_scale > 0 and at most 2e38, n_q_heads / n_kv_heads at most 128, batch at most 32768, else
- * READER_ERR_UNSUPPORTED.  What the cache holds at positions a token does not see has no influence on its row,
+ * READER_ERR_UNSUPPORTED unless: softmax_scale > 0 and at most 2e38; n_q_heads a multiple of n_kv_heads, at most 128 times it;
+ * batch at most 32768; num_pages * n_kv_heads * 64 and max_pages_per_seq * 64 below 2^31; and, with g = 128 / (n_q_heads /
+ * n_kv_heads) rounded down, (total_tokens / (2 g) + batch) * n_kv_heads * (max_pages_per_seq / 2 + 3) below 2^31.
+ * How a call is divided is chosen on the host from batch, total_tokens and max_pages_per_seq, not from the lengths: a page
+ * table or a captured call's tensors much larger than a step needs cost time (one token on 511: 10 or 19 us; one token on
+ * 30000 in a call captured for 4096: 241 us instead of 32), and never results.  A shared prefix is read for each sequence.
+ * What the cache holds at positions a token does not see has no influence on its row,
  * infinities and NaN included.
  * Arithmetic: bf16 inputs, fp32 accumulation and softmax, probabilities rounded to bf16 before the value product, bf16
  * (nearest-even) output.

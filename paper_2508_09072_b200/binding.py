@@ -610,7 +610,8 @@ class Reader:
                     workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
         """Causal attention of packed new tokens, whose K and V are in the cache at seq_lens[b] + i, over the cache:
         q [tokens, Hq, D].  Returns (out, status); lse f32 [tokens, Hq] is filled if given.  Without a workspace the
-        reader's own serves: calls that may overlap on the GPU (two streams) need one each."""
+        reader's own serves: calls that may overlap on the GPU (two streams) need one each, and a captured call needs its
+        workspace (or the reader) for as long as the graph lives."""
         ws = self._prompt_ws if workspace is None else workspace
         if ws is None:
             ws = self.prompt_workspace()

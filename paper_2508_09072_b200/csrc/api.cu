@@ -686,7 +686,7 @@ reader_status reader_prompt_append(reader_ctx *ctx, const void *q, const void *k
                                           n_q_heads, cache->n_kv_heads, cache->head_dim, rotation, p))
         return st;
     if (!empty && (!q_out || !aligned16(q_out))) return READER_ERR_INVALID_ARG;
-    if ((int64_t)prompt->total_tokens + prompt->batch >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;   // one block each
+    if ((int64_t)prompt->total_tokens + prompt->batch >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;   // a warp each, at least
     p.B = prompt->batch;
     p.tokens = prompt->total_tokens;
     p.token_start = prompt->token_start;

@@ -15,17 +15,26 @@ constexpr int kKeyTile = 128;            // keys per tile: two cache pages
 // A call with many units hands them out whole, from a counter.  Otherwise the units in the order (sequence, KV head,
 // block), each kUnitEntries entries (what starting and ending a unit costs) followed by its steps, form one list that is
 // cut into contiguous equal ranges, one per CTA.
+// Measured, us at 32/8/128 heads.  kUnitEntries 1, 2, 4: a prompt of 1500 tokens 52, 54, 57 (runs differ by 5 %), of 2500 90, 87,
+// 92; two pieces on 30 k histories 939, 928, 946; 16 pieces of 1 to 300 on 500 to 3000 120, 120, 126.  kNarrowUnitEntries 0, 1, 3
+// (a narrow unit's loads run on from the unit before it): 32 single tokens on 1024 to 4096 74.6, 71.1, 70.5; 8 x 16 tokens
+// on 2000 to 4000 35.6, 35.0, 35.4.  kMinEntriesPerCta 2, 4, 8: one token on 16000 24.9, 23.4, 35.1; four on 1000 to 2000
+// 21.2, 23.8, 31.5; calls with entries for every CTA do not notice.
 constexpr int kUnitEntries = 2;
-constexpr int kNarrowUnitEntries = 1;   // (its loads run on from the unit before it)
+constexpr int kNarrowUnitEntries = 1;
 constexpr int kMinEntriesPerCta = 4;
 // A call is a single launch when its units fit the CTAs and cutting them would not pay for the merge and the second launch
 // (6 to 9 us): going by the page table's width, at most kAloneSteps steps to a unit (lengths may differ, and the longest
 // one decides), and at most kAloneIdle steps that a CTA would gain on average from the CTAs without a unit.  Measured, alone
 // against cut: one token on 1000, 1500, 2000 keys, 8 units: 15.9 / 21.3, 20.0 / 19.8, 24.1 / 20.4 us; 16 tokens on 1500
 // keys each, 128 units: 24.8 / 34.6 us; a prompt of 1500 tokens in 24 units: 35.0 / 30.4 us, of 1000 in 128: 24.5 / 34.2 us.
+// The host does not know the lengths: one token on 511 keys takes 9.6 us behind a table of 8 pages and 19.4 behind one of 32
+// or of 2048, where the call is cut; and a call that advances the lengths is never alone.
 constexpr int kAloneSteps = 12, kAloneIdle = 6;
 // Units per CTA from which a call hands them out from a counter (a prompt of 4096 tokens, 3.5 units per CTA: 158 us, cut into
-// equal ranges 167 us; 16 prompts, 16 units per CTA: 314 and 340 us).
+// equal ranges 167 us; 16 prompts, 16 units per CTA: 314 and 340 us).  Here too it is the tensors' rows that count, not the
+// tokens in them: 32 single tokens on 1024 to 4000 keys take 69 us in a call made for 32 rows and 75 in one made for 4096;
+// one token on 30000, which the counter does not cut, 32 and 241 us.
 constexpr int kDynamicUnits = 3;
 
 struct PieceDesc {        // a unit that CTA c starts but does not finish: pieces 2c + 1, then 2(c + 1), 2(c + 2), ...

@@ -59,9 +59,13 @@ constexpr float kHugeScore = 536870912.f;
 __device__ __forceinline__ float margin_of(float mx) { return fabsf(mx) > kHugeScore && fabsf(mx) < INFINITY ? -INFINITY : kRaiseMaxBy; }
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 constexpr int kMaxStages = 8;
-constexpr int kLateStartTiles = 20;  // shortest piece whose slot 1 begins half a step late
-constexpr int kRotateTiles = 64;     // shortest unit that is begun in the middle
-constexpr int kLookAheadTiles = 12;  // shortest piece whose values are looked at ahead of their tiles
+// Lengths of pieces, in key tiles, from which a form is taken.  Measured, us at 32/8/128 heads:
+//   slot 1 begins half a step late, from 6, from 20, never: four prompts of 6001 to 8192 1600, 1599, 1608; two pieces on 30 k
+//     histories 972, 932, 962; 16 prompts of up to 2048 313, 304, 304; a prompt of 4096 155, 153, 153
+//   begun in the middle, from 16, from 64, never: the two pieces 928, 921, 957; 6 x 300 tokens on 2000 to 4000 133, 130, 130
+//   values looked at ahead of their tiles, always, from 12, never: 5 prompts of 33 to 700 (8/8/64) 27.6, 20.6, 20.6; the 16
+//     prompts 315, 304, 303; the prompt of 4096 154, 149, 155; the two pieces 936, 950, 953
+constexpr int kLateStartTiles = 20, kRotateTiles = 64, kLookAheadTiles = 12;
 constexpr int kMiscBytes = 3072;
 
 template <int D>
