@@ -41,7 +41,7 @@
 #include <cuda.h>
 
 #include "prompt_attn.cuh"
-#include "ptx_sm100.cuh"
+#include "prompt_ptx.cuh"
 
 namespace reader {
 namespace {
