@@ -400,3 +400,23 @@ def test_pages_whose_offsets_pass_32_bits(rd, D, Hkv):
     page, at = table[seq, pos // PAGE].long().cuda(), (pos % PAGE).cuda()
     assert torch.equal(k_pool[page, :, at], k) and torch.equal(v_pool[page, :, at].view(torch.int16), v.view(torch.int16))
     check_attn(rd, q, cache, ns, lens, 0.1)
+
+
+# ---------------------------------------------------------------------------------------------- many calls
+@pytest.mark.parametrize("D,Hq,Hkv,ns,lens", [(64, 8, 8, (1,), (511,)), (128, 8, 2, (40, 1, 130), (10, 300, 0)),       # a single launch
+                                              (128, 32, 8, (1,) * 16, tuple(range(500, 2100, 100))), (128, 4, 2, (700, 3), (900, 3000)),
+                                              (64, 128, 16, (300, 90, 310), (70, 5, 1000)), (128, 96, 16, (500, 300), (0, 40))])   # counter
+def test_thousands_of_calls_never_give_up_a_wait(rd, D, Hq, Hkv, ns, lens):
+    """Every wait of the kernel is bounded: a lost wake-up would show as READER_ERR_TIMEOUT in one call of many."""
+    rng = np.random.default_rng(95)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, D)
+    q, ts = bf16(rng, sum(ns), Hq, D).cuda(), starts(ns)
+    first, st = rd.prompt_attn(q, cache, ts, 0.1)
+    out, status = torch.empty_like(q), torch.empty_like(st)
+    worst, differs = torch.zeros_like(st), torch.zeros((), dtype=torch.bool, device="cuda")
+    for i in range(2000):
+        rd.prompt_attn(q, cache, ts, 0.1, out=out, status=status)
+        worst = torch.maximum(worst, status)
+        if i % 20 == 0:
+            differs |= (out != first).any()
+    assert not worst.any() and not differs
