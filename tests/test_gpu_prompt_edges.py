@@ -420,3 +420,115 @@ def test_thousands_of_calls_never_give_up_a_wait(rd, D, Hq, Hkv, ns, lens):
         if i % 20 == 0:
             differs |= (out != first).any()
     assert not worst.any() and not differs
+
+
+# ---------------------------------------------------------------------------------------------- calls that the documentation allows
+@pytest.mark.parametrize("Hq,Hkv,D,ns,lens,width", [(8, 2, 128, (40, 0, 3), (10, 5, 300), 0), (8, 2, 128, (40, 0, 3), (10, 5, 300), 100),
+                                                    (128, 16, 64, (300, 0, 310), (70, 5, 100), 0)])
+def test_rows_in_front_of_the_first_sequence(rd, Hq, Hkv, D, ns, lens, width):
+    """token_start need not begin at 0: rows in front are nobody's, like those behind."""
+    rng = np.random.default_rng(97)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], Hkv, D)
+    if width:
+        wide = torch.full((len(ns), width), -1, dtype=torch.int32, device="cuda")
+        wide[:, :cache.page_table.shape[1]] = cache.page_table
+        cache.page_table = wide
+    q = bf16(rng, sum(ns) + 7, Hq, D).cuda()
+    k, v = bf16(rng, sum(ns) + 7, Hkv, D).cuda(), bf16(rng, sum(ns) + 7, Hkv, D).cuda()
+    ts = starts(ns) + 5
+    q2 = torch.full_like(q, 7.0)
+    _, st = rd.prompt_append(q, k, v, cache, ts, out=q2)
+    assert not st.any() and torch.equal(q2[5:-2], q[5:-2]) and (q2[:5] == 7.0).all() and (q2[-2:] == 7.0).all()
+    out, lse = torch.full_like(q, 7.0), torch.full((len(q), Hq), 7.0, device="cuda")
+    _, st = rd.prompt_attn(q2, cache, ts, 0.1, out=out, lse=lse)
+    assert not st.any() and (out[:5] == 7.0).all() and (out[-2:] == 7.0).all() and (lse[:5] == 7.0).all() and (lse[-2:] == 7.0).all()
+    want, wlse, tol, ltol = plain_attn(q[5:-2], cache, ns, lens, 0.1)
+    within(out[5:-2], want, tol)
+    assert ((lse[5:-2].double().cpu() - wlse).abs() <= ltol).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,ns,lens", [(128, (300,), (200,)), (65, (70, 1), (0, 900)), (127, (9, 40), (130, 3)), (63, (50,), (64,)), (43, (90,), (1,))])
+def test_wide_groups(rd, D, G, ns, lens):
+    rng = np.random.default_rng(98)
+    cache = make_cache(rng, lens, [a + b for a, b in zip(ns, lens)], 1, D)
+    check_attn(rd, bf16(rng, sum(ns) + 1, G, D).cuda(), cache, ns, lens, D ** -0.5)
+
+
+def test_append_and_tree_captured_and_replayed_on_another_stream(rd):
+    rng = np.random.default_rng(99)
+    Hq, Hkv, D, T, B = 8, 2, 128, 9, 3
+    room = [400, 300, 200]
+    cache = make_cache(rng, [0] * B, room, Hkv, D)
+    angle = np.arange(500)[:, None] * 10000.0 ** (-np.arange(0, D, 2) / D)
+    rope = torch.from_numpy(np.stack([np.cos(angle), np.sin(angle)], 1).astype(np.float32)).cuda()
+    q, k, v = (bf16(rng, 120, h, D).cuda() for h in (Hq, Hkv, Hkv))
+    tq, tk, tv = (bf16(rng, B, T, h, D).cuda() for h in (Hq, Hkv, Hkv))
+    parent = torch.tensor([[-1, 0, 0, 1, 2, 3, 3, 0, 7]] * B, dtype=torch.int32).cuda()
+    ts, out, st = starts([1, 1, 1]), torch.empty_like(q), torch.empty(B, dtype=torch.int32, device="cuda")
+    touts = [torch.empty_like(x) for x in (tq, tk, tv)]
+    tst = torch.empty_like(st)
+
+    def calls():
+        rd.prompt_append(q, k, v, cache, ts, rope=rope, out=out, status=st)
+        rd.tree_rotate(tq, tk, tv, cache.seq_lens, parent, rope=rope, out=touts[0], k_tree=touts[1], v_tree=touts[2], status=tst)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            calls()
+    torch.cuda.synchronize()
+    for ns, lens in (([70, 1, 33], [5, 200, 0]), ([0, 0, 0], [1, 2, 3]), ([1, 100, 19], [399, 150, 181])):
+        ts.copy_(starts(ns))
+        cache.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (out, cache.k_pool, cache.v_pool, *touts, st, tst)]
+        out.fill_(7.0)
+        calls()
+        assert all(torch.equal(a.view(torch.int16) if a.dtype == torch.bfloat16 else a, b.view(torch.int16) if b.dtype == torch.bfloat16 else b)
+                   for a, b in zip(got, (out, cache.k_pool, cache.v_pool, *touts, st, tst)))
+        assert not st.any() and not tst.any() and (out[sum(ns):] == 7.0).all()
+
+
+def test_empty_calls(rd):
+    from paper_2508_09072_b200 import binding
+    rng = np.random.default_rng(100)
+    cache = make_cache(rng, [5, 0, 64], [5, 0, 64], 2, 64)
+    cache.seq_lens[1] = -1
+    none = lambda h: torch.empty(0, h, 64, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    out, st = rd.prompt_append(none(4), none(2), none(2), cache, starts([0, 0, 0]))
+    assert out.shape == (0, 4, 64) and st.tolist() == [0, binding.ERR_CAPACITY, 0]
+    out, st = rd.prompt_attn(none(4), cache, starts([0, 0, 0]), 0.1)
+    assert st.tolist() == [0, binding.ERR_CAPACITY, 0]
+    nobody = binding.KvCache(cache.k_pool, cache.v_pool, cache.page_table[:0], cache.seq_lens[:0])
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert rd.prompt_append(none(4), none(2), none(2), nobody, one)[1].numel() == 0
+    assert rd.prompt_attn(none(4), nobody, one, 0.1)[1].numel() == 0
+    tree = lambda h: torch.empty(0, 3, h, 64, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    got = rd.tree_rotate(tree(4), tree(2), tree(2), one[:0], torch.empty(0, 3, dtype=torch.int32, device="cuda"))
+    assert got[0].shape == (0, 3, 4, 64) and got[3].numel() == 0
+
+
+@pytest.mark.parametrize("B,T", [(3000, 1), (700, 5)])
+def test_tree_rotate_of_many_trees(rd, B, T):
+    rng = np.random.default_rng(101)
+    Hq, Hkv, D = 6, 2, 64
+    parent = torch.tensor([[-1, 0, 1, 0, 3][:T]] * B, dtype=torch.int32)
+    level = torch.tensor([0, 1, 2, 1, 2][:T])
+    lens = torch.from_numpy(rng.integers(0, 90, B).astype(np.int32))
+    angle = np.arange(100)[:, None] * 10000.0 ** (-np.arange(0, D, 2) / D)
+    rope = torch.from_numpy(np.stack([np.cos(angle), np.sin(angle)], 1).astype(np.float32))
+    q, k, v = (bf16(rng, B, T, h, D) for h in (Hq, Hkv, Hkv))
+    got = rd.tree_rotate(q.cuda(), k.cuda(), v.cuda(), lens.cuda(), parent.cuda(), rope=rope.cuda())
+    assert not got[3].any() and torch.equal(got[2].cpu(), v)
+    row = rope[(lens[:, None] + level).long()].double()
+    for x, y in ((q, got[0]), (k, got[1])):
+        x = x.double()
+        a, b, c, s = x[..., :D // 2], x[..., D // 2:], row[:, :, None, 0], row[:, :, None, 1]
+        want = torch.cat([a * c - b * s, b * c + a * s], -1)
+        mag = torch.cat([a.abs() + b.abs()] * 2, -1)
+        within(y, want, HALF * want.abs() + 2.0 ** -20 * mag)
