@@ -425,7 +425,7 @@ __device__ __forceinline__ bool nonfinite_bits(uint32_t half) { return (half & 0
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-                   const __grid_constant__ CUtensorMap vmap, const __nv_bfloat16 *__restrict__ v_pool) {
+                   const __grid_constant__ CUtensorMap vmap, const __nv_bfloat16 *v_pool) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
@@ -729,7 +729,8 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                 // A look at the exponents (all ones: infinity or NaN) of the value rows that are multiplied although some query does
                 // not see them: the unit's own tokens, and what the last slice of 16 rows holds behind them.  They are read from
                 // the pool, while the tiles are on their way: out of shared memory, whose bandwidth the products take up,
-                // one tile took 6000 cycles.
+                // one tile took 6000 cycles.  (Plain loads: the kernel before may still have been writing these rows when this one was
+                // launched, so they are not read-only for its lifetime.)
                 const int lo = max(own_key, sg->t0 * kKeyTile), hi = min((sg->u.keys + 15) & ~15, (sg->t0 + n) * kKeyTile);
                 // (A short piece has no time for that, and few products: its tiles are gone through in shared memory.)
                 bool dirty = n < kLookAheadTiles;
@@ -748,7 +749,7 @@ prompt_attn_kernel(const PromptAttnParams p, const __grid_constant__ CUtensorMap
                             const int pg = __shfl_sync(0xffffffffu, page, (key / kPage - first_page) & 31);
                             x[k] = make_uint4(0, 0, 0, 0);
                             if (key < hi && pg >= 0)
-                                x[k] = __ldg(reinterpret_cast<const uint4 *>(v_pool + (((size_t)pg * p.Hkv + sg->h) * kPage + key % kPage) * D) + i % kChunks);
+                                x[k] = *(reinterpret_cast<const uint4 *>(v_pool + (((size_t)pg * p.Hkv + sg->h) * kPage + key % kPage) * D) + i % kChunks);
                         }
 #pragma unroll
                         for (int k = 0; k < kBatch; ++k) {

@@ -532,3 +532,27 @@ def test_tree_rotate_of_many_trees(rd, B, T):
         want = torch.cat([a * c - b * s, b * c + a * s], -1)
         mag = torch.cat([a.abs() + b.abs()] * 2, -1)
         within(y, want, HALF * want.abs() + 2.0 ** -20 * mag)
+
+
+def test_values_that_the_call_before_has_just_written(rd):
+    """Decoding steps back to back, each of which brings an infinity into one column of one head: the attention looks at value
+    rows that the append right before it wrote, next to rows that the attention before that has looked at."""
+    rng = np.random.default_rng(103)
+    Hq, Hkv, D, L, steps = 16, 8, 128, 1700, 300
+    cache = make_cache(rng, [L], [L + steps], Hkv, D, poison=False)
+    q, k, v = (bf16(rng, steps, h, D) for h in (Hq, Hkv, Hkv))
+    where = torch.from_numpy(rng.permutation(Hkv * D)[:steps])
+    v.view(steps, -1)[torch.arange(steps), where] = float("inf")
+    q, k, v, ts = q.cuda(), k.cuda(), v.cuda(), starts([1])
+    outs, worst = torch.empty_like(q), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for i in range(steps):
+        one = slice(i, i + 1)
+        _, st = rd.prompt_append(q[one], k[one], v[one], cache, ts)
+        _, st2 = rd.prompt_attn(q[one], cache, ts, 0.09, out=outs[one], update_seq_lens=True)
+        worst = torch.maximum(worst, torch.maximum(st, st2))
+    assert not worst.any() and cache.seq_lens.tolist() == [L + steps]
+    seen = torch.zeros(steps, Hkv * D, dtype=torch.bool)
+    seen[torch.arange(steps), where] = True
+    seen = (seen.cumsum(0) > 0).view(steps, Hkv, 1, D).expand(steps, Hkv, Hq // Hkv, D).reshape(steps, Hq, D)
+    got = outs.cpu()
+    assert torch.isfinite(got[~seen]).all() and not torch.isfinite(got[seen]).any()
