@@ -502,6 +502,152 @@ reader_status reader_prompt_attn(reader_ctx *ctx, const void *q, int32_t n_q_hea
  * is done, as one that gave up a bounded wait (READER_ERR_TIMEOUT); no wait runs out.  -1 turns it off. */
 reader_status reader_set_prompt_give_up(reader_ctx *ctx, int32_t cta);
 
+/*
+ * ---- A cache in 4 bits ---------------------------------------------------------------------------------------------
+ * The calls below keep a layer's keys and values in 4.5 bits an element instead of 16: 3.55 times the tokens in the same memory,
+ * and as much less to read for each token.  In the same conventions:
+ *   prompt, per layer:   reader_prompt_append -> reader_prompt_attn on a bf16 cache (one for all layers will do), then
+ *                        reader_q4_store; a prompt that comes in pieces: reader_q4_load first
+ *   step:                reader_tree_rotate -> reader_q4_verify_attn per layer -> reader_accept -> reader_q4_commit
+ * A cache in 4 bits is a reader_kv_cache whose
+ *   k_pool, v_pool   u8 [num_pages][n_kv_heads][36 * head_dim]: 64 positions of one head, numbers and scales
+ * (csrc/q4_format.cuh has the places of the bits; these calls are the only ones that write or read them).
+ *
+ * 16 consecutive elements of a head share a scale s = (1 + m/8) 2^(e-18), m = 0..7, e = 0..31 (m < 7 if e = 31): the smallest with 7.5 s >=
+ * their largest magnitude.  An element x is held as the whole number nearest x / s (ties to even), from -7 to 7, and stands for
+ * that number of scales: within s / 2 of x, and exact in bf16.  Magnitudes above 107520 are held as the largest number; 16
+ * elements with an infinity or a NaN among them all read as NaN.
+ */
+
+/*
+ * Positions first[b] .. last[b] - 1 of every sequence from bf16 caches to 4-bit ones, layer by layer (none if first[b] >= last[b]).
+ *   from, to     HOST arrays [n_layers]: from[i] in bf16, to[i] in 4 bits.  All of `from` share page_table, num_pages, n_kv_heads,
+ *                head_dim and max_pages_per_seq, and so do all of `to` (and shared_prefix_len), else READER_ERR_INVALID_ARG; the two
+ *                page tables may differ, heads and head_dim may not.  seq_lens are neither read nor changed and may be NULL.
+ *   first, last  i32 [batch]
+ *   status_out   i32 [batch]: READER_ERR_CAPACITY when first[b] < 0, first[b] < shared_prefix_len of `to` or a page table is too
+ *                short, READER_ERR_BAD_PAGE when a page of either is outside its pool: nothing of that sequence is written
+ * Positions outside the range keep what they hold.  Sequences must not share a page that the call writes to.  head_dim 64 or 128.
+ */
+reader_status reader_q4_store(reader_ctx *ctx, const reader_kv_cache *from, const reader_kv_cache *to, int32_t n_layers, int32_t batch,
+                              const int32_t *first, const int32_t *last, int32_t *status_out, void *stream);
+
+/* The other way: from[i] in 4 bits, to[i] in bf16; what the numbers stand for, exactly. */
+reader_status reader_q4_load(reader_ctx *ctx, const reader_kv_cache *from, const reader_kv_cache *to, int32_t n_layers, int32_t batch,
+                             const int32_t *first, const int32_t *last, int32_t *status_out, void *stream);
+
+/* reader_kv_commit_layers into 4-bit caches (n_layers = 1: reader_kv_commit). */
+reader_status reader_q4_commit(reader_ctx *ctx, const reader_kv_cache *caches, const void *const *k_trees, const void *const *v_trees,
+                               int32_t n_layers, int32_t batch, int32_t n_nodes, const int32_t *path, const int32_t *n_acc,
+                               int32_t max_path, int32_t update_seq_lens, int32_t *slots_out, int32_t *status_out, void *stream);
+
+/* Bytes of device scratch that reader_q4_verify_attn needs, whatever the batch.  Host call, no CUDA work; 0 on bad arguments. */
+size_t reader_q4_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
+
+/*
+ * reader_verify_attn over a cache in 4 bits: the committed keys and values are what the numbers stand for, those of the tree are
+ * bf16 as ever.  A tree of one node is plain decoding.  Arguments, outputs and status words are those of reader_verify_attn, except
+ *   workspace  at least reader_q4_workspace_bytes(...) bytes, 256-byte aligned; contents are scratch, calls that share it must
+ *              not overlap on the GPU
+ *   status_out READER_ERR_TIMEOUT besides (rows of that sequence may also hold their values)
+ * READER_ERR_UNSUPPORTED unless: softmax_scale > 0 and at most 2e38; n_q_heads a multiple of n_kv_heads; batch at most 65536; and batch *
+ * n_kv_heads * (n_nodes * n_q_heads / n_kv_heads / 16 + 1) * (max_pages_per_seq + 4) below 2^31.
+ * Bytes at positions that are not committed have no influence, whatever they are.
+ * Arithmetic: fp32 accumulation and softmax, probabilities rounded to bf16 before the value product, bf16 (nearest-even) output.
+ */
+reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_heads, const void *k_tree, const void *v_tree,
+                                    const reader_kv_cache *cache, const reader_tree *tree, float softmax_scale, void *out,
+                                    float *lse_out, void *workspace, size_t workspace_bytes, int32_t *status_out, void *stream);
+
+/* Testing aid (host call): a share of the following reader_q4_verify_attn calls on this context acts as one whose bounded wait
+ * ran out (READER_ERR_TIMEOUT); no wait runs out.  -1 turns it off. */
+reader_status reader_set_q4_give_up(reader_ctx *ctx, int32_t worker);
+
+/*
+ * ---- The pages of a cache ------------------------------------------------------------------------------------------
+ * Which page of the pools holds what is the caller's affair in the calls above: they follow page_table.  The calls below look
+ * after the table on the device, without a host that waits for lengths, for caches of either kind.
+ *   refs         i32 [num_pages]: how many entries of the page table name a page; 0 = the page is free.  The caller sets it up
+ *                (all zero for an empty cache); pages that are not to be handed out get a count of their own
+ *   page_table   i32 [rows][max_pages_per_seq], -1 = no page (as for reader_kv_cache: one table for all layers of a model)
+ *   seq_lens     i32 [rows]
+ *   pools        HOST array [n_pools] of device pointers, 16-byte aligned: every pool whose pages the table names (keys and
+ *                values of all layers), each num_pages * page_bytes bytes; page_bytes is a multiple of 16
+ * Row numbers, counts and lengths live on the device; requests come as arrays [n], answers as status_out[n].  A request with a
+ * status other than READER_OK changes nothing, unless it says so, and does not disturb the others.
+ * Free pages are handed out lowest number first, in the order of the requests: the same inputs give the same pages.
+ * Pages that a call takes out of the table are free for the next call.
+ */
+typedef struct {
+    int32_t *refs;
+    int32_t num_pages;
+    int32_t *page_table;
+    int32_t rows, max_pages_per_seq;
+    int32_t *seq_lens;
+    void *const *pools;
+    int32_t n_pools;
+    size_t page_bytes;
+} reader_pages;
+
+/* Bytes of device scratch that reader_pages_fork, reader_pages_reserve (of at most n requests) and reader_pages_compact need.
+ * Host call, no CUDA work; 0 on bad arguments. */
+size_t reader_pages_workspace_bytes(int32_t num_pages, int32_t rows, int32_t max_pages_per_seq, int32_t n);
+
+/*
+ * Row dst[i] becomes what row src[i] is: its length, and the pages of its positions, which both rows name from now on (no data
+ * are copied).  The pages that row dst[i] named are released.  All at once: every source is read before any row is written, so rows
+ * may be permuted (a beam search's reordering), one source may have many destinations, and src[i] = dst[i] is allowed.
+ *   workspace   256-byte aligned; contents are scratch, calls that share it must not overlap on the GPU
+ *   status_out  READER_ERR_INVALID_ARG: a row outside the table, or a dst that an earlier request names; READER_ERR_CAPACITY: a length
+ *               outside [0, max_pages_per_seq * 64]; READER_ERR_BAD_PAGE: a page of the source's positions outside the pool
+ * pools are not looked at.  n * max_pages_per_seq < 2^31, else READER_ERR_UNSUPPORTED (here and in reader_pages_reserve).
+ */
+reader_status reader_pages_fork(reader_ctx *ctx, const reader_pages *pages, const int32_t *src, const int32_t *dst, int32_t n,
+                                void *workspace, size_t workspace_bytes, int32_t *status_out, void *stream);
+
+/*
+ * Makes positions seq_lens[r] .. seq_lens[r] + tokens[i] - 1 of row r = rows[i] the row's own to write: entries without a page get a
+ * free one, entries whose page other entries name too get a free one in its place, and where such a page holds positions
+ * below seq_lens[r] its data are copied, in all pools.  Whether a page is shared goes by refs before the call: two rows that share a
+ * page and are both among the requests get a page each, and the shared one is released.
+ *   status_out  READER_ERR_INVALID_ARG: a row outside the table or named by an earlier request, tokens[i] < 0; READER_ERR_BAD_PAGE: an
+ *               entry outside the pool, or no page where positions are committed; READER_ERR_CAPACITY: the row is too short for the
+ *               new length, or too few pages are free: requests are served in order, and from the first that does not find enough
+ *               on none that needs a page is
+ * workspace as for reader_pages_fork.
+ */
+reader_status reader_pages_reserve(reader_ctx *ctx, const reader_pages *pages, const int32_t *rows, const int32_t *tokens, int32_t n,
+                                   void *workspace, size_t workspace_bytes, int32_t *status_out, void *stream);
+
+/*
+ * Row rows[i] keeps its first keep[i] tokens (keep NULL: none): entries behind their pages are released and become -1, and the
+ * length is lowered to keep[i] if it is larger.  A row may be named more than once (the lowest of the keeps counts).
+ *   status_out  READER_ERR_INVALID_ARG: a row outside the table, keep[i] < 0; READER_ERR_BAD_PAGE: an entry outside the pool was among
+ *               those that became -1
+ * pools are not looked at.
+ */
+reader_status reader_pages_free(reader_ctx *ctx, const reader_pages *pages, const int32_t *rows, const int32_t *keep, int32_t n,
+                                int32_t *status_out, void *stream);
+
+/*
+ * Moves the pages in use to the front of the pools: with n of them, those numbered n and above move, in ascending order, to the
+ * free numbers below n, in ascending order; page_table and refs follow, the data of all pools move.  As few pages move as can.
+ *   n_used_out  i32 [1]: pages in use; pages from that number on are free afterwards
+ * workspace as for reader_pages_fork (any n).
+ */
+reader_status reader_pages_compact(reader_ctx *ctx, const reader_pages *pages, int32_t *n_used_out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
+/*
+ * Copies page from_ids[i] of from_pools[j] to page to_ids[i] of to_pools[j], for all i < n and j < n_pools: within pools or to others
+ * (a page saved aside, a pool that grows).  HOST arrays of device pointers, 16-byte aligned; page_bytes a multiple of 16.
+ * No page may be written twice, nor written and read, in one call.
+ *   status_out  i32 [n]: READER_ERR_BAD_PAGE where an id is outside [0, from_pages) or [0, to_pages): nothing is copied
+ */
+reader_status reader_pages_copy(reader_ctx *ctx, const void *const *from_pools, int32_t from_pages, void *const *to_pools,
+                                int32_t to_pages, int32_t n_pools, size_t page_bytes, const int32_t *from_ids, const int32_t *to_ids,
+                                int32_t n, int32_t *status_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

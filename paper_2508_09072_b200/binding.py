@@ -1,4 +1,4 @@
-"""Binding of ``libreader_verify.so``: argument marshalling only (ctypes; a native module for the prompt calls).
+"""Binding of ``libreader_verify.so``: argument marshalling only (ctypes; a native module for the prompt, 4-bit cache and page calls).
 
 Every step of the verification path runs in the library's CUDA kernels.  PyTorch is used for
 device memory and streams; tensors are passed as raw device pointers.  bf16 tensors are
@@ -30,7 +30,10 @@ EXPORTS = ("reader_create", "reader_destroy", "reader_status_string", "reader_se
            "reader_accept_commit", "reader_verify_prepare", "reader_verify_attn_prepared",
            "reader_padded_workspace_bytes", "reader_verify_attn_padded", "reader_padded_append", "reader_padded_rearrange",
            "reader_prompt_append", "reader_tree_rotate", "reader_prompt_workspace_bytes", "reader_prompt_attn",
-           "reader_set_prompt_give_up")
+           "reader_set_prompt_give_up",
+           "reader_q4_store", "reader_q4_load", "reader_q4_commit", "reader_q4_workspace_bytes", "reader_q4_verify_attn",
+           "reader_set_q4_give_up", "reader_pages_workspace_bytes", "reader_pages_fork", "reader_pages_reserve", "reader_pages_free",
+           "reader_pages_compact", "reader_pages_copy")
 
 
 class ReaderError(RuntimeError):
@@ -128,6 +131,12 @@ def load_library() -> ctypes.CDLL:
     lib.reader_prompt_workspace_bytes.restype = c_size_t
     lib.reader_set_prompt_give_up.argtypes = [c_void_p, c_int32]
     lib.reader_set_prompt_give_up.restype = c_int32
+    lib.reader_q4_workspace_bytes.argtypes = [c_void_p, c_int32]
+    lib.reader_q4_workspace_bytes.restype = c_size_t
+    lib.reader_set_q4_give_up.argtypes = [c_void_p, c_int32]
+    lib.reader_set_q4_give_up.restype = c_int32
+    lib.reader_pages_workspace_bytes.argtypes = [c_int32, c_int32, c_int32, c_int32]
+    lib.reader_pages_workspace_bytes.restype = c_size_t
     lib.reader_kv_commit.argtypes = [c_void_p, POINTER(_KvCache), c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                                      c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
     lib.reader_kv_commit.restype = c_int32
@@ -136,7 +145,7 @@ def load_library() -> ctypes.CDLL:
 
 
 def load_native():
-    """The native module that marshals the prompt calls (it links the same shared library)."""
+    """The native module that marshals the prompt, 4-bit cache and page calls (it links the same shared library)."""
     load_library()
     try:
         from . import _marshal
@@ -189,6 +198,26 @@ class KvCache:
 
 
 @dataclass
+class Q4Cache:
+    """One layer's paged cache in 4 bits (q4_store, q4_commit write it); tensors live on the device and are owned by the caller."""
+    k_pool: torch.Tensor      # u8 [num_pages, Hkv, 36 * D]
+    v_pool: torch.Tensor
+    page_table: torch.Tensor  # i32 [B, max_pages]
+    seq_lens: torch.Tensor    # i32 [B]
+    shared_prefix_len: int = 0
+
+
+@dataclass
+class Pages:
+    """A page table with the counts of its pages' holders and the pools whose pages it names (keys and values of all layers, bf16 or
+    4 bits); tensors live on the device and are owned by the caller."""
+    refs: torch.Tensor        # i32 [num_pages]: entries of the table that name a page, 0 = free
+    page_table: torch.Tensor  # i32 [rows, max_pages], -1 = no page
+    seq_lens: torch.Tensor    # i32 [rows]
+    pools: list               # tensors [num_pages, ...] with pages of one size
+
+
+@dataclass
 class PaddedCache:
     """The padded batch cache of Sec. 4.3; tensors live on the device and are owned by the caller."""
     k: torch.Tensor        # bf16 [B, Hkv, capacity, D]
@@ -222,10 +251,12 @@ class Reader:
         self._h = h
         self._ws: Optional[torch.Tensor] = None
         self._prompt_ws: Optional[torch.Tensor] = None
+        self._q4_ws: Optional[torch.Tensor] = None
+        self._pages_ws: list = []
 
     @functools.cached_property
     def _native(self):
-        # loaded by the first prompt call: the other calls need the library alone
+        # loaded by the first prompt, 4-bit cache or page call: the other calls need the library alone
         return load_native()
 
     def close(self):
@@ -620,6 +651,112 @@ class Reader:
         if st != OK:
             raise ReaderError(st, "reader_prompt_attn")
         return out, status
+
+    # ---- a cache in 4 bits
+    def q4_store(self, source, destination, first: torch.Tensor, last: torch.Tensor, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Positions first[b] .. last[b] - 1 of every sequence from bf16 caches (a list of KvCache, one per layer) to 4-bit ones (a list
+        of Q4Cache).  Returns the status words."""
+        st, status = self._native.q4_convert(self._handle(), self.device, True, source, destination, first, last, status)
+        if st != OK:
+            raise ReaderError(st, "reader_q4_store")
+        return status
+
+    def q4_load(self, source, destination, first: torch.Tensor, last: torch.Tensor, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The other way: what the numbers stand for, exactly.  Returns the status words."""
+        st, status = self._native.q4_convert(self._handle(), self.device, False, source, destination, first, last, status)
+        if st != OK:
+            raise ReaderError(st, "reader_q4_load")
+        return status
+
+    def q4_commit(self, caches, k_trees, v_trees, path: torch.Tensor, n_acc: torch.Tensor, update_seq_lens: bool = True,
+                  slots: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        """kv_commit_layers into 4-bit caches: lists of Q4Cache sharing page_table and seq_lens, and of tree K / V tensors.  Returns
+        (slots, status)."""
+        st, slots, status = self._native.q4_commit(self._handle(), self.device, caches, k_trees, v_trees, path, n_acc, update_seq_lens, slots, status)
+        if st != OK:
+            raise ReaderError(st, "reader_q4_commit")
+        return slots, status
+
+    def q4_workspace(self) -> torch.Tensor:
+        """A cached device buffer for q4_verify_attn (of the size that any call needs: it is never replaced)."""
+        if self._q4_ws is None:
+            need = int(self.lib.reader_q4_workspace_bytes(self._h, 128))
+            self._q4_ws = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
+        return self._q4_ws
+
+    def q4_verify_attn(self, q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, cache: Q4Cache, parent: torch.Tensor, scale: float,
+                       anc_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+        """verify_attn over a 4-bit cache (one node per tree: plain decoding).  Returns (out, status).  Without a workspace the reader's
+        own serves: calls that may overlap on the GPU (two streams) need one each, and a captured call needs its workspace (or the
+        reader) for as long as the graph lives."""
+        ws = self._q4_ws if workspace is None else workspace
+        if ws is None:
+            ws = self.q4_workspace()
+        st, out, status = self._native.q4_verify_attn(self._handle(), self.device, q, k_tree, v_tree, cache, parent, scale, anc_mask, out, lse, status, ws)
+        if st != OK:
+            raise ReaderError(st, "reader_q4_verify_attn")
+        return out, status
+
+    def set_q4_give_up(self, worker: int = -1) -> None:
+        """Testing aid: that share of the following q4_verify_attn calls reports a wait that ran out; -1: none."""
+        st = self.lib.reader_set_q4_give_up(self._h, int(worker))
+        if st != OK:
+            raise ReaderError(st, "reader_set_q4_give_up")
+
+    # ---- the pages of a cache
+    def pages_workspace(self, pages: Pages, n: int = 0) -> torch.Tensor:
+        """A cached device buffer for page calls of n requests.  A larger one is made when it is needed; those before it live as long
+        as the reader (a captured call may use them)."""
+        need = int(self.lib.reader_pages_workspace_bytes(pages.refs.shape[0], *pages.page_table.shape, n))
+        if need == 0:
+            raise ReaderError(ERR_INVALID_ARG, "reader_pages_workspace_bytes")
+        if not self._pages_ws or self._pages_ws[-1].numel() < need:
+            self._pages_ws.append(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
+        return self._pages_ws[-1]
+
+    def pages_fork(self, pages: Pages, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows dst become what rows src are, all at once; their pages are shared, those that rows dst had are released.  Returns the
+        status words.  Workspaces as for q4_verify_attn."""
+        ws = workspace if workspace is not None else self.pages_workspace(pages, src.shape[0])
+        st, status = self._native.pages_fork(self._handle(), self.device, pages, src, dst, ws, status)
+        if st != OK:
+            raise ReaderError(st, "reader_pages_fork")
+        return status
+
+    def pages_reserve(self, pages: Pages, rows: torch.Tensor, tokens: torch.Tensor, status: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Pages of their own for the next tokens[i] positions of rows[i]: missing ones are taken from the free ones, shared ones replaced,
+        and copied where they hold committed positions.  Returns the status words."""
+        ws = workspace if workspace is not None else self.pages_workspace(pages, rows.shape[0])
+        st, status = self._native.pages_reserve(self._handle(), self.device, pages, rows, tokens, ws, status)
+        if st != OK:
+            raise ReaderError(st, "reader_pages_reserve")
+        return status
+
+    def pages_free(self, pages: Pages, rows: torch.Tensor, keep: Optional[torch.Tensor] = None,
+                   status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows keep their first keep[i] tokens (None: none); the pages behind them are released.  Returns the status words."""
+        st, status = self._native.pages_free(self._handle(), self.device, pages, rows, keep, status)
+        if st != OK:
+            raise ReaderError(st, "reader_pages_free")
+        return status
+
+    def pages_compact(self, pages: Pages, n_used: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The pages in use move to the front of the pools.  Returns their number (i32 [1], on the device)."""
+        ws = workspace if workspace is not None else self.pages_workspace(pages)
+        st, n_used = self._native.pages_compact(self._handle(), self.device, pages, ws, n_used)
+        if st != OK:
+            raise ReaderError(st, "reader_pages_compact")
+        return n_used
+
+    def pages_copy(self, from_pools, to_pools, from_ids: torch.Tensor, to_ids: torch.Tensor, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Pages from_ids of every pool of a list to pages to_ids of the pools of another.  Returns the status words."""
+        st, status = self._native.pages_copy(self._handle(), self.device, from_pools, to_pools, from_ids, to_ids, status)
+        if st != OK:
+            raise ReaderError(st, "reader_pages_copy")
+        return status
 
 
 # ---------------------------------------------------------------------------------------------

@@ -20,6 +20,8 @@ struct reader_ctx {
     reader::Sm100Host sm100;
     bool prompt_attr_set;   // the prompt attention kernels have their shared-memory limit
     int prompt_give_up;     // thread block of the prompt attention that reports a wait that ran out (testing aid); -1: none
+    bool q4_attr_set;       // the same for the attention over a 4-bit cache
+    int q4_give_up;
     cudaEvent_t ev_start, ev_stop;  // optional timing hooks around the main attention kernel
     cudaEvent_t ev_acc_start, ev_acc_stop;  // and around the argmax kernel of reader_accept
     PreparedRecord prepared;

@@ -1,0 +1,33 @@
+// Parameter block and launchers of the attention over a 4-bit cache.
+#pragma once
+#include "common.cuh"
+
+namespace reader {
+
+constexpr int kQ4Rows = 16;             // query rows of a unit of the few-rows kernel
+constexpr int kQ4Warps = 12;            // of a thread block, each a worker of its own
+constexpr int kQ4MaxBatch = 1 << 16;
+
+struct Q4AttnParams {
+    const __nv_bfloat16 *q, *k_tree, *v_tree;
+    const unsigned char *k_pool, *v_pool;
+    const int32_t *page_table, *seq_lens, *parent;
+    const uint64_t *anc;       // nullable: [B][T][2]
+    __nv_bfloat16 *out;
+    float *lse;                // nullable
+    int32_t *status;
+    int B, T, Hq, Hkv, G, D;
+    int max_pages, num_pages, shared_prefix_pages;
+    float scale_log2, scale;
+    int give_up;               // worker that reports a wait that ran out (testing aid); -1: none
+    // workspace
+    int32_t *counters;         // [4 * workers]: arrivals of a group's shares, of a unit's groups
+    int32_t *flags;            // [2 * workers] what is wrong with a share
+    float2 *partial_ml;        // [2 * workers][kQ4Rows] largest score, sum
+    float *partial_o;          // [2 * workers][kQ4Rows][D]
+    int n_ctas;                // thread blocks; kQ4Warps workers each
+};
+
+reader_status launch_q4_attn_rows(bool *attr_set, const Q4AttnParams &p, cudaStream_t st);
+
+}  // namespace reader

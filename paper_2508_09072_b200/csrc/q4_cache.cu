@@ -1,0 +1,227 @@
+// The 4-bit cache outside the attention: rows of a bf16 cache stored in 4 bits (reader_q4_store), their values loaded back
+// (reader_q4_load), accepted tree rows committed (reader_q4_commit).
+//
+// Bound: bytes.  A block of 16 elements (32 bytes in bf16) belongs to one thread, from the loads to the numbers: the largest
+// magnitude is found in its own registers, so nothing is exchanged and nothing is read twice.  Two neighbouring positions of a
+// value tile share their words; the thread that has a block has both positions' (reading the word first where only one of them is
+// written), so that no two threads of a launch write the same word.
+#include "q4_cache.cuh"
+#include "q4_format.cuh"
+
+namespace reader {
+namespace {
+
+constexpr int kThreads = 256;
+
+// What keeps the positions first .. last - 1 of sequence b from being converted.  Block-collective.
+__device__ __forceinline__ int convert_status(const Q4Convert &p, int b, int first, int last) {
+    if (last <= first) return READER_OK;
+    const int64_t room = (int64_t)min(p.from_width, p.to_width) * kPage;
+    if (first < 0 || first < p.shared_prefix_len || last > room) return READER_ERR_CAPACITY;
+    bool bad = false;
+    for (int i = first / kPage + threadIdx.x; i <= (last - 1) / kPage; i += kThreads) {
+        const int a = p.from_table[(size_t)b * p.from_width + i], c = p.to_table[(size_t)b * p.to_width + i];
+        bad |= a < 0 || a >= p.from_pages || c < 0 || c >= p.to_pages;
+    }
+    return __syncthreads_or(bad) ? READER_ERR_BAD_PAGE : READER_OK;
+}
+
+// One tile (page, head): rows lo .. hi - 1 of a bf16 tile of keys (values) to a 4-bit one.
+template <int D>
+__device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bfloat16 *v, unsigned char *k4, unsigned char *v4, int lo, int hi) {
+    constexpr int kBlocks = D / q4::kBlock, kKeyTasks = kPage * kBlocks / kThreads, kPairs = kPage / 2 * kBlocks;
+    const int tid = threadIdx.x;
+    uint4 x[kKeyTasks][2], y[2][2];
+#pragma unroll
+    for (int i = 0; i < kKeyTasks; ++i) {
+        const int task = i * kThreads + tid, r = task / kBlocks;
+        if (r < lo || r >= hi) continue;
+        const uint4 *at = reinterpret_cast<const uint4 *>(k) + task * 2;
+        x[i][0] = __ldcs(at);
+        x[i][1] = __ldcs(at + 1);
+    }
+    const int t = tid / kBlocks, u = tid % kBlocks;   // value pair of this thread (128 of the 256 have none at head_dim 64)
+    bool has[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        has[e] = tid < kPairs && 2 * t + e >= lo && 2 * t + e < hi;
+        y[e][0] = y[e][1] = make_uint4(0, 0, 0, 0);
+        if (!has[e]) continue;
+        const uint4 *at = reinterpret_cast<const uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2;
+        y[e][0] = __ldcs(at);
+        y[e][1] = __ldcs(at + 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kKeyTasks; ++i) {
+        const int task = i * kThreads + tid, r = task / kBlocks;
+        if (r >= lo && r < hi) q4::put_key_block<D>(k4, r, task % kBlocks, q4::quantise(x[i][0], x[i][1]));
+    }
+    if (has[0] || has[1])
+        q4::put_value_blocks<D>(v4, t, u, has[0], q4::quantise(y[0][0], y[0][1]), has[1], q4::quantise(y[1][0], y[1][1]));
+}
+
+// The other way.
+template <int D>
+__device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigned char *v4, __nv_bfloat16 *k, __nv_bfloat16 *v, int lo, int hi) {
+    constexpr int kBlocks = D / q4::kBlock, kKeyTasks = kPage * kBlocks / kThreads, kPairs = kPage / 2 * kBlocks;
+    const int tid = threadIdx.x;
+    uint2 kw[kKeyTasks];
+    int kc[kKeyTasks];
+#pragma unroll
+    for (int i = 0; i < kKeyTasks; ++i) {
+        const int task = i * kThreads + tid, r = task / kBlocks;
+        if (r < lo || r >= hi) continue;
+        kw[i] = *reinterpret_cast<const uint2 *>(k4 + task * 8);
+        kc[i] = k4[q4::scales_at(D) + q4::k_scale_at<D>(r, task % kBlocks)];
+    }
+    const int t = tid / kBlocks, u = tid % kBlocks;
+    const bool has[2] = {tid < kPairs && 2 * t >= lo && 2 * t < hi, tid < kPairs && 2 * t + 1 >= lo && 2 * t + 1 < hi};
+    uint4 vw = make_uint4(0, 0, 0, 0);
+    int vc = 0;
+    if (has[0] || has[1]) {
+        constexpr int kChunkWords = D / 32;
+        vw = *reinterpret_cast<const uint4 *>(v4 + t * D + q4::v_chunk<D>(t, u * (4 / kChunkWords)) * kChunkWords * 4);
+        vc = *reinterpret_cast<const uint16_t *>(v4 + q4::scales_at(D) + q4::v_scale_at<D>(2 * t, u));
+    }
+#pragma unroll
+    for (int i = 0; i < kKeyTasks; ++i) {
+        const int task = i * kThreads + tid, r = task / kBlocks;
+        if (r < lo || r >= hi) continue;
+        const float s = q4::scale_of(kc[i]);
+        uint4 *at = reinterpret_cast<uint4 *>(k) + task * 2;
+        __stcs(at, q4::values_of(q4::evens_apart(q4::plain_of(kw[i].x)), s));
+        __stcs(at + 1, q4::values_of(q4::evens_apart(q4::plain_of(kw[i].y)), s));
+    }
+    const uint32_t w[4] = {q4::plain_of(vw.x), q4::plain_of(vw.y), q4::plain_of(vw.z), q4::plain_of(vw.w)};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if (!has[e]) continue;
+        const float s = q4::scale_of((vc >> (8 * e)) & 255);
+        uint4 *at = reinterpret_cast<uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2;
+        const int sh = 16 * e;
+        __stcs(at, q4::values_of(((w[0] >> sh) & 0xffffu) | (((w[1] >> sh) & 0xffffu) << 16), s));
+        __stcs(at + 1, q4::values_of(((w[2] >> sh) & 0xffffu) | (((w[3] >> sh) & 0xffffu) << 16), s));
+    }
+}
+
+// Blocks b * per_seq .. + per_seq - 1 walk the tiles (layer, page, head) of sequence b, heads fastest.
+template <int D, bool kStore>
+__global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p, const __grid_constant__ Q4Layers layers) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int b = blockIdx.x / p.per_seq, x = blockIdx.x - b * p.per_seq;
+    const int first = p.first[b], last = p.last[b];
+    const int st = convert_status(p, b, first, last);
+    if (x == 0 && threadIdx.x == 0 && p.status) p.status[b] = st;
+    if (st != READER_OK || last <= first) return;
+    const int page0 = first / kPage, n_pages = (last - 1) / kPage - page0 + 1;
+    const int64_t items = (int64_t)n_pages * p.Hkv * p.layers;
+    for (int64_t i = x; i < items; i += p.per_seq) {
+        const int h = (int)(i % p.Hkv);
+        const int64_t j = i / p.Hkv;
+        const int page = page0 + (int)(j % n_pages), l = (int)(j / n_pages);
+        const int lo = max(0, first - page * kPage), hi = min(kPage, last - page * kPage);
+        const size_t from = (size_t)p.from_table[(size_t)b * p.from_width + page] * p.Hkv + h;
+        const size_t to = (size_t)p.to_table[(size_t)b * p.to_width + page] * p.Hkv + h;
+        constexpr size_t kWide = (size_t)kPage * D, kNarrow = q4::tile_bytes(D);
+        if (kStore)
+            store_tile<D>(static_cast<const __nv_bfloat16 *>(layers.k_from[l]) + from * kWide, static_cast<const __nv_bfloat16 *>(layers.v_from[l]) + from * kWide,
+                          static_cast<unsigned char *>(layers.k_to[l]) + to * kNarrow, static_cast<unsigned char *>(layers.v_to[l]) + to * kNarrow, lo, hi);
+        else
+            load_tile<D>(static_cast<const unsigned char *>(layers.k_from[l]) + from * kNarrow, static_cast<const unsigned char *>(layers.v_from[l]) + from * kNarrow,
+                         static_cast<__nv_bfloat16 *>(layers.k_to[l]) + to * kWide, static_cast<__nv_bfloat16 *>(layers.v_to[l]) + to * kWide, lo, hi);
+    }
+}
+
+// Block (b, l) commits sequence b into layer l: the accepted nodes' rows to the positions seq_lens[b] + k.
+template <int D>
+__global__ void __launch_bounds__(kThreads) q4_commit_kernel(const Q4Commit p, const __grid_constant__ Q4Layers layers) {
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int kBlocks = D / q4::kBlock;
+    const int b = blockIdx.x, l = blockIdx.y, tid = threadIdx.x;
+    const int L = p.seq_lens[b], n = p.n_acc[b];
+    const int32_t *table = p.page_table + (size_t)b * p.max_pages, *path = p.path + (size_t)b * p.max_path;
+    int32_t *slots = p.slots && l == 0 ? p.slots + (size_t)b * p.max_path : nullptr;
+    bool bad = n > 0 && (n > p.max_path || L < 0 || L < p.shared_prefix_len || (int64_t)L + n > (int64_t)p.max_pages * kPage);
+    if (!bad)
+        for (int k = tid; k < n; k += kThreads) {
+            const int page = table[(L + k) / kPage], node = path[k];
+            bad |= page < 0 || page >= p.num_pages || node < 0 || node >= p.T;
+        }
+    bad = __syncthreads_or(bad);
+    if (tid == 0 && p.status && l == 0) p.status[b] = bad ? READER_ERR_CAPACITY : READER_OK;
+    if (slots)
+        for (int k = tid; k < p.max_path; k += kThreads)
+            slots[k] = !bad && k < n ? table[(L + k) / kPage] * kPage + (L + k) % kPage : -1;
+    if (bad || n <= 0) return;
+    auto row = [&](const void *tree, int k, int h, int u) {
+        return reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(tree) + (((size_t)b * p.T + path[k]) * p.Hkv + h) * D + u * q4::kBlock);
+    };
+    auto tile = [&](void *pool, int pos, int h) {
+        return static_cast<unsigned char *>(pool) + ((size_t)table[pos / kPage] * p.Hkv + h) * q4::tile_bytes(D);
+    };
+    const int per_pos = p.Hkv * kBlocks, key_tasks = n * per_pos;
+    const int pair0 = L / 2, value_tasks = ((L + n - 1) / 2 - pair0 + 1) * per_pos;
+    for (int i = tid; i < key_tasks + value_tasks; i += kThreads) {
+        if (i < key_tasks) {
+            const int k = i / per_pos, h = (i - k * per_pos) / kBlocks, u = i % kBlocks;
+            const uint4 *src = row(layers.k_from[l], k, h, u);
+            q4::put_key_block<D>(tile(layers.k_to[l], L + k, h), (L + k) % kPage, u, q4::quantise(src[0], src[1]));
+        } else {
+            const int j = i - key_tasks, pair = j / per_pos, h = (j - pair * per_pos) / kBlocks, u = j % kBlocks;
+            const int pos = 2 * (pair0 + pair);   // the pair's even position
+            const bool has_even = pos >= L, has_odd = pos + 1 < L + n;
+            const uint4 *even = row(layers.v_from[l], has_even ? pos - L : 0, h, u), *odd = row(layers.v_from[l], has_odd ? pos + 1 - L : 0, h, u);
+            const uint4 x[4] = {even[0], even[1], odd[0], odd[1]};
+            q4::put_value_blocks<D>(tile(layers.v_to[l], pos, h), (pos % kPage) / 2, u, has_even, q4::quantise(x[0], x[1]), has_odd, q4::quantise(x[2], x[3]));
+        }
+    }
+    if (p.update) {   // the only block that reads this length
+        __syncthreads();
+        if (tid == 0) p.seq_lens[b] = L + n;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) q4_advance_kernel(int32_t *__restrict__ seq_lens, const int32_t *__restrict__ n_acc,
+                                                              const int32_t *__restrict__ status, int B) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int b = blockIdx.x * kThreads + threadIdx.x;
+    if (b < B && status[b] == READER_OK && n_acc[b] > 0) seq_lens[b] += n_acc[b];
+}
+
+}  // namespace
+
+void launch_q4_convert(bool store, Q4Convert p, const Q4Layers *chunks, int n_layers, int n_sm, cudaStream_t st) {
+    // The lengths live on the device: as many thread blocks for a sequence as fill the GPU sixteen times over with all of them,
+    // at most one per tile of the narrower table.
+    const int32_t *status = p.status;
+    for (int l0 = 0; l0 < n_layers; l0 += kQ4LayersPerLaunch) {
+        p.layers = n_layers - l0 < kQ4LayersPerLaunch ? n_layers - l0 : kQ4LayersPerLaunch;
+        const int64_t tiles = (int64_t)(p.from_width < p.to_width ? p.from_width : p.to_width) * p.Hkv * p.layers;
+        const int64_t share = (16 * (int64_t)n_sm + p.B - 1) / p.B;
+        p.per_seq = (int)(tiles < share ? tiles : share);
+        p.status = l0 == 0 ? const_cast<int32_t *>(status) : nullptr;
+        auto kernel = p.D == 128 ? (store ? q4_convert_kernel<128, true> : q4_convert_kernel<128, false>)
+                                 : (store ? q4_convert_kernel<64, true> : q4_convert_kernel<64, false>);
+        launch_pdl(kernel, dim3((unsigned)(p.B * p.per_seq)), dim3(kThreads), 0, st, p, chunks[l0 / kQ4LayersPerLaunch]);
+    }
+}
+
+void launch_q4_commit(Q4Commit p, const Q4Layers *chunks, int n_layers, bool update_seq_lens, cudaStream_t st) {
+    int32_t *status = p.status, *slots = p.slots;
+    p.update = update_seq_lens && n_layers == 1;
+    for (int l0 = 0; l0 < n_layers; l0 += kQ4LayersPerLaunch) {
+        const int layers = n_layers - l0 < kQ4LayersPerLaunch ? n_layers - l0 : kQ4LayersPerLaunch;
+        p.status = l0 == 0 ? status : nullptr;
+        p.slots = l0 == 0 ? slots : nullptr;
+        launch_pdl(p.D == 128 ? q4_commit_kernel<128> : q4_commit_kernel<64>, dim3((unsigned)p.B, (unsigned)layers), dim3(kThreads), 0, st, p,
+                   chunks[l0 / kQ4LayersPerLaunch]);
+    }
+    if (update_seq_lens && n_layers > 1)
+        launch_pdl(q4_advance_kernel, dim3((unsigned)((p.B + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p.seq_lens, p.n_acc,
+                   static_cast<const int32_t *>(status), p.B);
+}
+
+}  // namespace reader
