@@ -276,7 +276,7 @@ __device__ __noinline__ void merge(const Q4AttnParams &p, int b, int h, int rt, 
                 if (r >= live) continue;
                 if (final) {
                     const size_t row = out_row(p, b, h, rt, r);
-                    const float inv = 1.f / total[i];
+                    const float inv = total[i] == 0.f ? 0.f : 1.f / total[i];
                     if (has)
                         *reinterpret_cast<uint2 *>(p.out + row * D + lane * 4) =
                             flag ? make_uint2(0u, 0u) : make_uint2(pack(acc[i].x * inv, acc[i].y * inv), pack(acc[i].z * inv, acc[i].w * inv));
@@ -593,7 +593,7 @@ struct Worker {
             const int r = g + 8 * e;
             if (r >= live) continue;
             const size_t row = out_row(p, u.b, u.h, u.rt, r);
-            const float inv = flag ? 0.f : 1.f / l[e];
+            const float inv = flag || l[e] == 0.f ? 0.f : 1.f / l[e];   // (a row that sees nothing: zeros)
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * D + c * (D / 4));
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) {
