@@ -83,7 +83,7 @@ reader_status reader_create(reader_ctx **out, int device) {
     ctx->ev_acc_start = ctx->ev_acc_stop = nullptr;
     ctx->prompt_attr_set = false;
     ctx->prompt_give_up = -1;
-    ctx->q4_attr_set = false;
+    ctx->q4_attr = Q4AttrSet{};
     ctx->q4_give_up = -1;
     ctx->prepared = PreparedRecord{};
     reader_status st = sm100_host_init(&ctx->sm100, device);

@@ -83,11 +83,11 @@ Q4Ws q4_ws(const reader_ctx *ctx, int D) {
     Q4Ws w{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes); return o; };
-    const size_t workers = (size_t)ctx->n_sm * kQ4Warps;
+    const size_t workers = (size_t)ctx->n_sm * kQ4MaxWorkers, rows = (size_t)ctx->n_sm * kQ4WorkerRows;
     w.counters = take(sizeof(int32_t) * 4 * workers);
     w.flags = take(sizeof(int32_t) * 2 * workers);
-    w.partial_ml = take(sizeof(float2) * 2 * workers * kQ4Rows);
-    w.partial_o = take(sizeof(float) * 2 * workers * kQ4Rows * D);
+    w.partial_ml = take(sizeof(float2) * 2 * rows);
+    w.partial_o = take(sizeof(float) * 2 * rows * D);
     w.total = at;
     return w;
 }
@@ -238,7 +238,7 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
         return READER_ERR_INVALID_ARG;
     // the row maximum is taken before the scaling, so the scale has to be positive
     if (!(softmax_scale > 0.f) || softmax_scale > 2.0e38f || Hq % Hkv != 0 || B > kQ4MaxBatch) return READER_ERR_UNSUPPORTED;
-    const int64_t units = (int64_t)B * Hkv * ((int64_t)T * (Hq / Hkv) / kQ4Rows + 1);
+    const int64_t units = (int64_t)B * Hkv * ((int64_t)T * (Hq / Hkv) / 16 + 1);
     if (units * ((int64_t)cache->max_pages_per_seq + 4) >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
     const Q4Ws w = q4_ws(ctx, D);
     if (workspace_bytes < w.total) return READER_ERR_WORKSPACE;
@@ -268,8 +268,7 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
     p.flags = reinterpret_cast<int32_t *>(ws + w.flags);
     p.partial_ml = reinterpret_cast<float2 *>(ws + w.partial_ml);
     p.partial_o = reinterpret_cast<float *>(ws + w.partial_o);
-    p.n_ctas = ctx->n_sm;
-    if (reader_status s = launch_q4_attn_rows(&ctx->q4_attr_set, p, (cudaStream_t)stream)) return s;
+    if (reader_status s = launch_q4_attn_rows(&ctx->q4_attr, p, ctx->n_sm, (cudaStream_t)stream)) return s;
     return launch_status();
 }
 

@@ -1,6 +1,7 @@
 // The library context behind the opaque reader_ctx handle.
 #pragma once
 #include "common.cuh"
+#include "q4_attn.cuh"
 #include "verify_attn_sm100.cuh"
 
 // What reader_verify_prepare left in a workspace, so that reader_verify_attn_prepared can tell whether it is
@@ -20,7 +21,7 @@ struct reader_ctx {
     reader::Sm100Host sm100;
     bool prompt_attr_set;   // the prompt attention kernels have their shared-memory limit
     int prompt_give_up;     // thread block of the prompt attention that reports a wait that ran out (testing aid); -1: none
-    bool q4_attr_set;       // the same for the attention over a 4-bit cache
+    reader::Q4AttrSet q4_attr;   // the same for the attention over a 4-bit cache
     int q4_give_up;
     cudaEvent_t ev_start, ev_stop;  // optional timing hooks around the main attention kernel
     cudaEvent_t ev_acc_start, ev_acc_stop;  // and around the argmax kernel of reader_accept

@@ -4,8 +4,8 @@
 
 namespace reader {
 
-constexpr int kQ4Rows = 16;             // query rows of a unit of the few-rows kernel
-constexpr int kQ4Warps = 12;            // of a thread block, each a worker of its own
+// Workers (warps) of a thread block of the few-rows kernels, and rows of all of an SM's workers together, at most.
+constexpr int kQ4MaxWorkers = 16, kQ4WorkerRows = 192;
 constexpr int kQ4MaxBatch = 1 << 16;
 
 struct Q4AttnParams {
@@ -23,11 +23,16 @@ struct Q4AttnParams {
     // workspace
     int32_t *counters;         // [4 * workers]: arrivals of a group's shares, of a unit's groups
     int32_t *flags;            // [2 * workers] what is wrong with a share
-    float2 *partial_ml;        // [2 * workers][kQ4Rows] largest score, sum
-    float *partial_o;          // [2 * workers][kQ4Rows][D]
-    int n_ctas;                // thread blocks; kQ4Warps workers each
+    float2 *partial_ml;        // [2 * workers][rows] largest score, sum
+    float *partial_o;          // [2 * workers][rows][D]
+    int n_ctas;                // thread blocks (list form)
+    int split;                 // thread blocks of a unit (alone)
 };
 
-reader_status launch_q4_attn_rows(bool *attr_set, const Q4AttnParams &p, cudaStream_t st);
+// Which kernels have their attributes set.
+struct Q4AttrSet {
+    bool rows[4];
+};
+reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
 
 }  // namespace reader

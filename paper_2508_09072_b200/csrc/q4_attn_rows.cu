@@ -1,19 +1,22 @@
 // Tree-masked attention over a 4-bit cache for few query rows (reader_q4_verify_attn): single tokens, small trees.
 //
-// A unit is (sequence, KV head, 16 query rows).  Bound: bytes, 72 D of every 64 positions and head, if the numbers become
-// operands fast enough.  So they never leave a warp: each warp is a worker of its own that brings tiles (one page of keys and
-// values of one head, 72 D bytes) into its own ring in shared memory by bulk copies and computes S = Q K^T and O += P V with
-// m16n8k16 products whose B fragments it unpacks in registers, two bf16 in 2.75 instructions; the pages are laid out so that
-// a lane's words, and their scales, are one or two 16-byte loads.  (Feeding tcgen05.mma instead means writing every tile in
-// bf16 to shared memory and reading it back: worth it once many rows share it, not for 4 or 16.)  A fragment's column order is
-// free as long as both operands agree: of the elements, lane (g, c) = (lane / 4, lane % 4) has D/4 consecutive ones of a key,
-// and D/8 consecutive ones of a pair of values, with one or two scales; P comes out of the score product in the place where the
-// value product wants it.
+// A unit is (sequence, KV head, 8 or 16 query rows).  Bound: bytes, 72 D of every 64 positions and head, if the numbers become
+// operands fast enough.  So they never leave a warp: each warp is a worker of its own that brings tiles (one page of keys or
+// values of one head, 36 D bytes) into its own ring in shared memory by bulk copies and computes S^T = K Q^T and O^T += V^T P^T with
+// m16n8k16 products: keys and values are the 16-row operand, query rows the 8-column one, so that a row of queries costs
+// nothing that is not its own.  The A fragments are unpacked in registers, two bf16 in 2.75 instructions; the pages are laid
+// out so that a lane's words, and their scales, are one or two 16-byte loads.  (Feeding tcgen05.mma instead means writing every
+// tile in bf16 to shared memory and reading it back: worth it once many rows share it, not for 4 or 16.)  A product's inner order
+// is free as long as both operands agree: of the elements, lane (g, c) = (lane / 4, lane % 4) has D/4 consecutive ones of a key,
+// and D/8 consecutive ones of a pair of values, with one or two scales; P^T gets from the score product's result to the value
+// product's operand by one transposing move per 8 x 8 block.
 //
-// Work.  The units, each preceded by kUnitCost entries for its start and end, form one flat list of tiles that is cut into equal
+// Two forms.  (Alone) A call with few units is one launch: a cluster of thread blocks per unit, whose workers share its
+// tiles; shares (m, l, O) are merged in shared memory, those of the cluster's blocks through the workspace after its barrier.
+// (List) The units, each preceded by kUnitCost entries for its start and end, form one flat list of tiles that is cut into equal
 // ranges, one per worker.  Every thread block makes the list's prefix sums from seq_lens itself.  A unit that lies in several
-// ranges leaves shares (m, l, O) in the workspace; the last to arrive of a group of 16 merges the group, the last group the
-// unit, always in the order of the shares, whoever comes last.  The counters are zeroed by a launch in front.
+// ranges leaves shares in the workspace; the last to arrive of a group of them merges the group, the last group the unit, always in
+// the order of the shares, whoever comes last.  The counters are zeroed by a launch in front.
 //
 // What is checked where: lengths by every block, page ids by the worker that reads them, a tree by the worker of the unit's
 // tree tiles; what is wrong travels with the share and zeroes the unit's rows.  Bytes behind a sequence's end never reach a
@@ -30,8 +33,12 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = kQ4Warps * 32;
-constexpr int kStages = 2;
+// Workers of a thread block, and their ring's slots (a tile of keys or of values each): what registers and shared memory allow.
+template <int NT>
+struct Shape {
+    static constexpr int kWarps = NT == 1 ? 16 : 12, kSlots = NT == 1 ? 3 : 4;
+    static constexpr int kThreads = kWarps * 32, kRows = 8 * NT;
+};
 constexpr int kUnitCost = 2;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = 4;     // a smaller range costs more in merging than it saves in time
 constexpr int kOneLevel = 16;      // up to so many shares are merged at once, more in groups
@@ -39,18 +46,21 @@ constexpr int kMaxShares = 32 * 32;
 constexpr int kPrefix = 1024;      // entries of the prefix table in shared memory
 constexpr float kRaiseBy = 8.f;    // log2 units by which a score may exceed the maximum in use
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
-constexpr int kBadTree = 1, kBadPage = 2, kGaveUp = 4;
+constexpr int kBadTree = 1, kBadLength = 2, kBadPage = 4, kGaveUp = 8;
+constexpr int kMaxCluster = 16;
 
-template <int D>
+template <int D, int NT>
 struct Cfg {
+    using S = Shape<NT>;
     static constexpr int kTile = q4::tile_bytes(D);
-    static constexpr int kStageBytes = 2 * kTile;
-    static constexpr int kRing = kQ4Warps * kStages * kStageBytes;
-    static constexpr int kOffBars = kRing;
-    static constexpr int kOffParents = kOffBars + kQ4Warps * kStages * 8;
-    static constexpr int kOffPrefix = kOffParents + kQ4Warps * kMaxNodes;
+    static constexpr int kRingBytes = S::kSlots * kTile;   // of one worker; its share (rows x D floats) when all is done
+    static constexpr int kOffBars = S::kWarps * kRingBytes;
+    static constexpr int kOffParents = kOffBars + S::kWarps * S::kSlots * 8;
+    static constexpr int kOffMasks = kOffParents + S::kWarps * kMaxNodes;
+    static constexpr int kOffShares = kOffMasks + S::kWarps * S::kRows * 16;           // (m, l) of the workers' rows
+    static constexpr int kOffPrefix = kOffShares + S::kWarps * S::kRows * 8;
     static constexpr int kSmem = kOffPrefix + (kPrefix + 1) * 4;
-    static_assert(kSmem <= 227 * 1024, "shared memory");
+    static_assert(kSmem + 256 <= 227 * 1024 && kRingBytes >= S::kRows * D * 4, "shared memory");
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy, bool streamed) {
@@ -77,10 +87,16 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(a));
     return x;
 }
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The transposed 8 x 8 block of 16-bit elements: lane (g, c) gives elements (g, 2 c), (g, 2 c + 1) and gets (2 c, g), (2 c + 1, g).
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -103,23 +119,24 @@ struct Scale2 {
 };
 constexpr uint32_t kScaleOne = (uint32_t)((127 - q4::kScaleBias) << 7) * 0x10001u;
 // codes: two of them, in bits 0-7 and 16-23
-__device__ __forceinline__ Scale2 scale2(uint32_t codes, bool any_nan) {
+template <bool kWhole>
+__device__ __forceinline__ Scale2 scale2(uint32_t codes) {
     Scale2 r;
     r.s = codes * 16u + kScaleOne;
-    if (any_nan) {
+    if (!kWhole) {
         if ((codes & 0xffffu) == q4::kNanCode) r.s |= 0x7fffu;
         if ((codes >> 16) == q4::kNanCode) r.s |= 0x7fff0000u;
     }
     r.m24 = mul_bf16x2(r.s, 0xc1c0c1c0u);
     return r;
 }
-// Whether one of eight codes is kNanCode (four bytes 255 have all bits set in some byte).
-__device__ __forceinline__ bool has_nan(uint32_t a, uint32_t b) { return (__vcmpeq4(a, 0xffffffffu) | __vcmpeq4(b, 0xffffffffu)) != 0; }
+// Whether a byte of the word is kNanCode: its lower seven bits carry into the eighth, and that is set.
+__device__ __forceinline__ uint32_t nan_bits(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u; }
 // Pair i of a word: numbers n in the mantissas of 16 + n, times the scales, minus 24 of them: (n - 8) s, exactly.
 template <int i>
-__device__ __forceinline__ uint32_t pair(uint32_t w, const Scale2 &s) {
+__device__ __forceinline__ uint32_t pair(uint32_t w, const Scale2 &s, uint32_t sixteen) {
     const uint32_t x = i ? __funnelshift_r(w, w, 4 * i) : w;
-    return fma_bf16x2((x & 0x00780078u) | 0x41804180u, s.s, s.m24);
+    return fma_bf16x2((x & 0x00780078u) | sixteen, s.s, s.m24);
 }
 
 // ---- the work list
@@ -204,113 +221,160 @@ __device__ __forceinline__ Unit unit_at(const Q4AttnParams &p, const List &l, co
 }
 
 // ---- rows of a unit
+template <int NT>
 __device__ __forceinline__ size_t out_row(const Q4AttnParams &p, int b, int h, int rt, int r) {
-    const int row = rt * kQ4Rows + r, j = row / p.G;
+    const int row = rt * Shape<NT>::kRows + r, j = row / p.G;
     return ((size_t)b * p.T + j) * p.Hq + h * p.G + (row - j * p.G);
 }
-__device__ __forceinline__ int live_rows(const Q4AttnParams &p, int rt) { return min(kQ4Rows, p.T * p.G - rt * kQ4Rows); }
+template <int NT>
+__device__ __forceinline__ int live_rows(const Q4AttnParams &p, int rt) { return min(Shape<NT>::kRows, p.T * p.G - rt * Shape<NT>::kRows); }
+__device__ __forceinline__ int code_of_flag(int flag) {
+    return (flag & kBadTree) ? READER_ERR_BAD_TREE : (flag & kBadLength) ? READER_ERR_CAPACITY : (flag & kBadPage) ? READER_ERR_BAD_PAGE : flag ? READER_ERR_TIMEOUT : READER_OK;
+}
 __device__ __forceinline__ void note(const Q4AttnParams &p, int b, int flag, int lane) {
-    if (flag && lane == 0) atomicMax(p.status + b, (flag & kBadTree) ? READER_ERR_BAD_TREE : (flag & kBadPage) ? READER_ERR_BAD_PAGE : READER_ERR_TIMEOUT);
+    if (flag && lane == 0) atomicMax(p.status + b, code_of_flag(flag));
 }
 
-    // (Not inlined: its registers are not those of a worker's loop.)  Merges the shares in slots first, then base + 2 k for k = 1 .. count - 1 (times `apart`), into the result or into slot `first`.
-    // (count <= 32.)  A share whose maximum is -inf has weight 0 and is still added, so that a NaN in it stays.
-    template <int D>
-__device__ __noinline__ void merge(const Q4AttnParams &p, int b, int h, int rt, int first, int base, int apart, int count, bool final) {
+// Merges rows r0 .. r0 + kRowsAtOnce - 1 of `count` <= 32 shares: lane k knows (m, l) of share k, at(k, r) is where its row r of O stands.
+// A share whose maximum is -inf has weight 0 and is still added, so that a NaN in it stays.
+constexpr int kRowsAtOnce = 4;
+struct Merged {
+    float top[kRowsAtOnce], total[kRowsAtOnce];
+    float4 o[kRowsAtOnce];   // elements 4 lane .. + 3
+};
+template <int D, bool kGlobal, typename At>
+__device__ __forceinline__ Merged merge_rows(const float2 (&ml)[kRowsAtOnce], int count, int rows, float scale_log2, const At &at) {
     const int lane = threadIdx.x & 31;
-        auto slot_of = [&](int k) { return k == 0 ? first : base + 2 * apart * k; };
-        int flag = lane < count ? __ldcg(p.flags + slot_of(lane)) : 0;
-        flag = __reduce_or_sync(0xffffffffu, flag);
-        const int live = live_rows(p, rt);
-        if (final) note(p, b, flag, lane);
-        constexpr int kRows = 4;       // rows under way at once
-        const bool has = lane * 4 < D;
+    const bool has = lane * 4 < D;
+    Merged x;
+    float weight[kRowsAtOnce];
+#pragma unroll
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+        x.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        float t = ml[i].x;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+        x.top[i] = t;
+        weight[i] = ml[i].x == -INFINITY ? 0.f : ml[i].x == t ? 1.f : ex2((ml[i].x - t) * scale_log2);
+        t = ml[i].y * weight[i];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+        x.total[i] = t;
+    }
 #pragma unroll 1
-        for (int r0 = 0; r0 < live; r0 += kRows) {
-            float weight[kRows], total[kRows], top[kRows];
-            float4 acc[kRows];
-            float2 ml[kRows];
+    for (int k0 = 0; k0 < count; k0 += 4) {
+        float4 y[4][kRowsAtOnce];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                ml[i] = make_float2(-INFINITY, 0.f);
-                if (lane < count && r0 + i < live) ml[i] = __ldcg(p.partial_ml + slot_of(lane) * kQ4Rows + r0 + i);
-                acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < kRowsAtOnce; ++i) {
+                y[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!has || k0 + k >= count || i >= rows) continue;
+                const float4 *src = reinterpret_cast<const float4 *>(at(k0 + k, i) + lane * 4);
+                y[k][i] = kGlobal ? __ldcg(src) : *src;
             }
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                float t = ml[i].x;
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-                top[i] = t;
-                weight[i] = ml[i].x == -INFINITY ? 0.f : ml[i].x == t ? 1.f : ex2((ml[i].x - t) * p.scale_log2);
-                t = ml[i].y * weight[i];
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-                total[i] = t;
+            for (int i = 0; i < kRowsAtOnce; ++i) {
+                const float w = __shfl_sync(0xffffffffu, weight[i], min(k0 + k, 31));   // (behind the last share: 0 times 0)
+                x.o[i].x = fmaf(y[k][i].x, w, x.o[i].x);
+                x.o[i].y = fmaf(y[k][i].y, w, x.o[i].y);
+                x.o[i].z = fmaf(y[k][i].z, w, x.o[i].z);
+                x.o[i].w = fmaf(y[k][i].w, w, x.o[i].w);
             }
+    }
+    return x;
+}
+// A merged row as the call's result.
+template <int D>
+__device__ __forceinline__ void put_row(const Q4AttnParams &p, size_t row, float top, float total, const float4 &o, int flag) {
+    const int lane = threadIdx.x & 31;
+    const float inv = total == 0.f ? 0.f : 1.f / total;   // (a row that sees nothing: zeros)
+    if (lane * 4 < D)
+        *reinterpret_cast<uint2 *>(p.out + row * D + lane * 4) = flag ? make_uint2(0u, 0u) : make_uint2(pack(o.x * inv, o.y * inv), pack(o.z * inv, o.w * inv));
+    if (p.lse && lane == 0) p.lse[row] = flag ? 0.f : fmaf(top, p.scale, log2f(total) * 0.6931471805599453f);
+}
+
+// (Not inlined: its registers are not those of a worker's loop.)  Merges the shares in slots `first`, then base + 2 apart k for
+// k = 1 .. count - 1, into the result or into slot `first`.
+template <int D, int NT>
+__device__ __noinline__ void merge(const Q4AttnParams &p, int b, int h, int rt, int first, int base, int apart, int count, bool final) {
+    constexpr int kRows = Shape<NT>::kRows;
+    const int lane = threadIdx.x & 31;
+    auto slot_of = [&](int k) { return k == 0 ? first : base + 2 * apart * k; };
+    int flag = lane < count ? __ldcg(p.flags + slot_of(lane)) : 0;
+    flag = __reduce_or_sync(0xffffffffu, flag);
+    const int live = live_rows<NT>(p, rt);
+    if (final) note(p, b, flag, lane);
 #pragma unroll 1
-            for (int k0 = 0; k0 < count; k0 += 4) {
-                float4 x[4][kRows];
+    for (int r0 = 0; r0 < live; r0 += kRowsAtOnce) {
+        float2 ml[kRowsAtOnce];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        x[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (has && k0 + k < count && r0 + i < live)
-                            x[k][i] = __ldcg(reinterpret_cast<const float4 *>(p.partial_o + ((size_t)slot_of(k0 + k) * kQ4Rows + r0 + i) * D + lane * 4));
-                    }
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const float w = __shfl_sync(0xffffffffu, weight[i], min(k0 + k, 31));   // (behind the last share: 0 times 0)
-                        acc[i].x = fmaf(x[k][i].x, w, acc[i].x);
-                        acc[i].y = fmaf(x[k][i].y, w, acc[i].y);
-                        acc[i].z = fmaf(x[k][i].z, w, acc[i].z);
-                        acc[i].w = fmaf(x[k][i].w, w, acc[i].w);
-                    }
-            }
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int r = r0 + i;
-                if (r >= live) continue;
-                if (final) {
-                    const size_t row = out_row(p, b, h, rt, r);
-                    const float inv = total[i] == 0.f ? 0.f : 1.f / total[i];
-                    if (has)
-                        *reinterpret_cast<uint2 *>(p.out + row * D + lane * 4) =
-                            flag ? make_uint2(0u, 0u) : make_uint2(pack(acc[i].x * inv, acc[i].y * inv), pack(acc[i].z * inv, acc[i].w * inv));
-                    if (p.lse && lane == 0) p.lse[row] = flag ? 0.f : fmaf(top[i], p.scale, log2f(total[i]) * 0.6931471805599453f);
-                } else {
-                    if (has) *reinterpret_cast<float4 *>(p.partial_o + ((size_t)first * kQ4Rows + r) * D + lane * 4) = acc[i];
-                    if (lane == 0) p.partial_ml[first * kQ4Rows + r] = make_float2(top[i], total[i]);
-                }
-            }
+        for (int i = 0; i < kRowsAtOnce; ++i) {
+            ml[i] = make_float2(-INFINITY, 0.f);
+            if (lane < count && r0 + i < live) ml[i] = __ldcg(p.partial_ml + slot_of(lane) * kRows + r0 + i);
         }
-        if (!final) {
-            __syncwarp();
-            if (lane == 0) p.flags[first] = flag;
+        const Merged x = merge_rows<D, true>(ml, count, live - r0, p.scale_log2,
+                                             [&](int k, int i) { return p.partial_o + ((size_t)slot_of(k) * kRows + r0 + i) * D; });
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i) {
+            const int r = r0 + i;
+            if (r >= live) continue;
+            if (final) {
+                put_row<D>(p, out_row<NT>(p, b, h, rt, r), x.top[i], x.total[i], x.o[i], flag);
+            } else {
+                if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + ((size_t)first * kRows + r) * D + lane * 4) = x.o[i];
+                if (lane == 0) p.partial_ml[first * kRows + r] = make_float2(x.top[i], x.total[i]);
+            }
         }
     }
+    if (!final) {
+        __syncwarp();
+        if (lane == 0) p.flags[first] = flag;
+    }
+}
 
 // ---- one worker
-template <int D>
+template <int D, int NT>
 struct Worker {
-    static constexpr int kSteps = D / 16;    // k-steps of the score product; also scale blocks of a head
-    static constexpr int kCols = D / 8;      // n-tiles of the value product = value elements of a lane
+    using S = Shape<NT>;
+    using C = Cfg<D, NT>;
+    static constexpr int kSteps = D / 16;    // inner steps of the score product, 16-row tiles of the value product
+    static constexpr int kOwn = D / 8;       // value elements of a lane
     const Q4AttnParams &p;
     uint32_t ring, bars;
+    uint32_t sixteen;        // 16 in bf16, twice; in a register of its own (a second constant in the instruction cannot be)
     int lane, g, c;
-    int issued, used;        // tiles, counted over the worker's life
+    int issued, used;        // tiles of keys or values, counted over the worker's life
     bool gave_up;
     // the unit's page ids, 32 at a time
-    int ids, ids_next, ids_at;
+    int ids, ids_next, ids_at, t_issue;
 
-    uint32_t qf[kSteps][4];
-    float o[kCols][4];
-    float m[2], l[2];        // rows g and g + 8; l: this lane's share
+    uint32_t qf[kSteps][NT][2];
+    float o[kSteps][NT][4];   // O^T: elements 16 g' .. of rows 2 c, 2 c + 1 of each 8
+    float m[NT][2], l[NT][2]; // rows 2 c, 2 c + 1; l: this lane's share
 
     __device__ __forceinline__ Worker(const Q4AttnParams &p_) : p(p_) {}
+
+    __device__ __forceinline__ void init(unsigned char *smem, int warp) {
+        lane = threadIdx.x & 31; g = lane >> 2; c = lane & 3;
+        const uint32_t base = smem_u32(smem);
+        ring = base + warp * C::kRingBytes;
+        bars = base + C::kOffBars + warp * S::kSlots * 8;
+        issued = used = 0;
+        gave_up = false;
+        volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + warp * C::kRingBytes);
+        if (lane == 0) {
+            *word = 0x41804180u;
+            for (int s = 0; s < S::kSlots; ++s) mbar_init(bars + s * 8, 1);
+            fence_mbar_init();
+        }
+        __syncwarp();
+        sixteen = *word;
+        __syncwarp();
+        fence_proxy_async();
+    }
 
     // ---- tiles
     __device__ __forceinline__ int page_ids(const Unit &u, int t, int &flag) {
@@ -325,12 +389,9 @@ struct Worker {
         }
         return id;
     }
-    __device__ __forceinline__ void start(const Unit &u, int &flag) {
-        ids_at = u.t0;
-        ids = page_ids(u, u.t0, flag);
-        ids_next = page_ids(u, u.t0 + 32, flag);
-    }
-    __device__ __forceinline__ void issue(const Unit &u, int t, uint64_t policy, bool streamed, int &flag) {
+    // The next tile of the unit: keys of page t, values of page t, keys of page t + 1, ...
+    __device__ __forceinline__ void issue(const Unit &u, uint64_t policy, bool once, int &flag) {
+        const int t = t_issue >> 1;
         if (t - ids_at == 32) {
             ids_at = t;
             ids = ids_next;
@@ -338,17 +399,27 @@ struct Worker {
         }
         const int page = __shfl_sync(0xffffffffu, ids, t - ids_at);
         if (lane == 0) {
-            const int s = issued % kStages;
-            const uint32_t bar = bars + s * 8, dst = ring + s * Cfg<D>::kStageBytes;
-            const size_t at = ((size_t)page * p.Hkv + u.h) * Cfg<D>::kTile;
-            mbar_arrive_expect_tx(bar, Cfg<D>::kStageBytes);
-            bulk_load(dst, p.k_pool + at, Cfg<D>::kTile, bar, policy, streamed);
-            bulk_load(dst + Cfg<D>::kTile, p.v_pool + at, Cfg<D>::kTile, bar, policy, streamed);
+            const int s = issued % S::kSlots;
+            const uint32_t bar = bars + s * 8;
+            mbar_arrive_expect_tx(bar, C::kTile);
+            bulk_load(ring + s * C::kTile, ((t_issue & 1) ? p.v_pool : p.k_pool) + ((size_t)page * p.Hkv + u.h) * C::kTile, C::kTile, bar, policy,
+                      once && t >= p.shared_prefix_pages);
         }
         ++issued;
+        ++t_issue;
     }
-    __device__ __forceinline__ void await() {
-        const uint32_t bar = bars + (used % kStages) * 8, parity = (used / kStages) & 1;
+    __device__ __forceinline__ void start(const Unit &u, int pages_end, uint64_t policy, bool once, int &flag) {
+        ids_at = u.t0;
+        t_issue = 2 * u.t0;
+        ids = page_ids(u, u.t0, flag);
+        ids_next = page_ids(u, u.t0 + 32, flag);
+#pragma unroll 1
+        for (int i = 0; i < S::kSlots && t_issue < 2 * pages_end; ++i) issue(u, policy, once, flag);
+    }
+    // The slot of the next tile once it is there.
+    __device__ __forceinline__ uint32_t await() {
+        const int s = used % S::kSlots;
+        const uint32_t bar = bars + s * 8, parity = (used / S::kSlots) & 1;
         if (!mbar_try_wait(bar, parity)) {
             const uint64_t t0 = globaltimer_ns();
             while (!mbar_try_wait(bar, parity))
@@ -358,145 +429,97 @@ struct Worker {
                 }
         }
         gave_up = __any_sync(0xffffffffu, gave_up);
+        return ring + s * C::kTile;
+    }
+    __device__ __forceinline__ void release() {
+        ++used;
+        __syncwarp();
     }
 
-    // ---- queries: lane (g, c) has elements c D/4 .. of rows g and g + 8
-    __device__ __forceinline__ void load_queries(const Unit &u) {
+    // ---- queries: lane (g, c) has elements c D/4 .. of row g of each 8
+    __device__ __forceinline__ void begin(const Unit &u) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = u.rt * kQ4Rows + g + 8 * e;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = u.rt * S::kRows + 8 * nt + g;
             const bool live = r < p.T * p.G;
             const int j = live ? r / p.G : 0, hq = u.h * p.G + (live ? r - j * p.G : 0);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (((size_t)u.b * p.T + j) * p.Hq + hq) * D + c * (D / 4));
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) {
                 const uint4 v = live ? src[x] : make_uint4(0, 0, 0, 0);
-                qf[2 * x][e] = v.x; qf[2 * x][2 + e] = v.y;
-                qf[2 * x + 1][e] = v.z; qf[2 * x + 1][2 + e] = v.w;
+                qf[2 * x][nt][0] = v.x; qf[2 * x][nt][1] = v.y;
+                qf[2 * x + 1][nt][0] = v.z; qf[2 * x + 1][nt][1] = v.w;
             }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                m[nt][e] = -INFINITY;
+                l[nt][e] = 0.f;
+            }
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[x][nt][i] = 0.f;
         }
     }
 
-    // ---- softmax of kN n-tiles of scores (columns 8 j + 2 c, + 1): probabilities in place
-    template <int kN>
-    __device__ __forceinline__ void softmax(float (&s)[kN][4]) {
-        float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            top[0] = max3(top[0], s[j][0], s[j][1]);
-            top[1] = max3(top[1], s[j][2], s[j][3]);
-        }
-        // the maximum in use is raised only when a score exceeds it by 2^8: the vote needs no exchange within the rows
+    // ---- softmax of 16 kM keys (keys g and g + 8 of each 16, rows 2 c and 2 c + 1 of each 8): probabilities in place
+    template <int kM>
+    __device__ __forceinline__ void softmax(float (&s)[kM][NT][4]) {
+        float top[NT][2];
+        bool rises = false;
+        // the maximum in use is raised only when a score exceeds it by 2^8: the vote needs no exchange
         const float by = kRaiseBy / p.scale_log2;
-        if (__any_sync(0xffffffffu, top[0] > m[0] + by || top[1] > m[1] + by)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
-                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2));
-                const float now = fmaxf(m[e], top[e]);
-                const float f = m[e] == now ? 1.f : ex2((m[e] - now) * p.scale_log2);   // (-inf before the first score: 0)
-                m[e] = now;
-                l[e] *= f;
+                float t = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
 #pragma unroll
-                for (int n = 0; n < kCols; ++n) {
-                    o[n][2 * e] *= f;
-                    o[n][2 * e + 1] *= f;
-                }
+                for (int j = 1; j < kM; ++j) t = max3(t, s[j][nt][e], s[j][nt][2 + e]);
+                top[nt][e] = t;
+                rises |= t > m[nt][e] + by;
             }
+        if (__any_sync(0xffffffffu, rises)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float t = top[nt][e];
+                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+                    const float now = fmaxf(m[nt][e], t);
+                    const float f = m[nt][e] == now ? 1.f : ex2((m[nt][e] - now) * p.scale_log2);   // (-inf before the first score: 0)
+                    m[nt][e] = now;
+                    l[nt][e] *= f;
+#pragma unroll
+                    for (int x = 0; x < kSteps; ++x) {
+                        o[x][nt][e] *= f;
+                        o[x][nt][2 + e] *= f;
+                    }
+                }
         }
         // The difference to the maximum is taken before the scaling: whatever the scores' size, it is as exact as they are.
         const float2 sc = make_float2(p.scale_log2, p.scale_log2);
-        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        const float from[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
 #pragma unroll
-        for (int j = 0; j < kN; ++j)
+        for (int nt = 0; nt < NT; ++nt) {
+            const float2 from = make_float2(m[nt][0] == -INFINITY ? 0.f : -m[nt][0], m[nt][1] == -INFINITY ? 0.f : -m[nt][1]);
+            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float2 x = __fmul2_rn(__fadd2_rn(make_float2(s[j][2 * e], s[j][2 * e + 1]), make_float2(from[e], from[e])), sc);
-                const float2 y = make_float2(ex2(x.x), ex2(x.y));
-                s[j][2 * e] = y.x;
-                s[j][2 * e + 1] = y.y;
-                sum[e] = __fadd2_rn(sum[e], y);
-            }
-        l[0] += sum[0].x + sum[0].y;
-        l[1] += sum[1].x + sum[1].y;
-    }
-
-    // ---- one tile of the cache, `valid` of its 64 positions committed: two halves, so that scores take 16 registers
-    __device__ __forceinline__ void tile(uint32_t k, int valid) {
-        constexpr int kPer = D / 64;   // key scales of a lane and position
-        const uint32_t v = k + Cfg<D>::kTile;
-        const uint32_t k_row = k + g * (D / 2) + c * (D / 8);
-        const uint32_t k_codes = k + q4::scales_at(D) + lane * (8 * kPer);
-        // row 4 j + c of D bytes; of its eight chunks the one with this lane's elements
-        const uint32_t v_row = v + c * D + q4::v_chunk<D>(c, g) * (D / 8);
-        const uint32_t v_codes = v + q4::scales_at(D) + ((D == 128 ? g : g >> 1) * 4 + c) * 16;
+            for (int j = 0; j < kM; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (h == 1 && valid <= kPage / 2) break;
-            float s[4][4];
-            {
-                uint32_t cw[2] = {};
-                if (D == 128) { const uint2 x = lds64(k_codes + h * 8); cw[0] = x.x; cw[1] = x.y; }
-                else cw[0] = lds32(k_codes + h * 4);
-                const bool nan = has_nan(cw[0], cw[1]);
-#pragma unroll
-                for (int jj = 0; jj < 4; ++jj) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[jj][i] = 0.f;
-                    uint32_t w[D / 32];
-                    load_words(w, k_row + (4 * h + jj) * (8 * D / 2));
-#pragma unroll
-                    for (int x = 0; x < D / 32; ++x) {
-                        // the code of block x / 2 of this position, twice
-                        const int byte = jj * kPer + x / 2;
-                        const Scale2 sc = scale2(__byte_perm(cw[byte / 4], 0, 0x4040 | (byte % 4) | ((byte % 4) << 8)), nan);
-                        mma(s[jj], qf[2 * x], pair<0>(w[x], sc), pair<1>(w[x], sc));
-                        mma(s[jj], qf[2 * x + 1], pair<2>(w[x], sc), pair<3>(w[x], sc));
-                    }
+                for (int k = 0; k < 2; ++k) {
+                    const float2 x = __fmul2_rn(__fadd2_rn(make_float2(s[j][nt][2 * k], s[j][nt][2 * k + 1]), from), sc);
+                    const float2 y = make_float2(ex2(x.x), ex2(x.y));
+                    s[j][nt][2 * k] = y.x;
+                    s[j][nt][2 * k + 1] = y.y;
+                    sum = __fadd2_rn(sum, y);
                 }
-            }
-            if (valid < kPage) {
-#pragma unroll
-                for (int jj = 0; jj < 4; ++jj) {
-                    const int key = 8 * (4 * h + jj) + 2 * c;
-                    if (key >= valid) s[jj][0] = s[jj][2] = -INFINITY;
-                    if (key + 1 >= valid) s[jj][1] = s[jj][3] = -INFINITY;
-                }
-            }
-            softmax<4>(s);
-            {
-                const uint2 cx = lds64(v_codes + h * 8);
-                const uint32_t cw[2] = {cx.x, cx.y};
-                const bool nan = has_nan(cw[0], cw[1]);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const uint32_t a[4] = {pack(s[2 * t][0], s[2 * t][1]), pack(s[2 * t][2], s[2 * t][3]), pack(s[2 * t + 1][0], s[2 * t + 1][1]),
-                                           pack(s[2 * t + 1][2], s[2 * t + 1][3])};
-                    uint32_t w[2][D / 32];
-                    Scale2 sc[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int jj = 2 * t + e, j = 4 * h + jj;
-                        load_words(w[e], v_row + j * (4 * D));
-                        sc[e] = scale2(__byte_perm(cw[jj / 2], 0, jj % 2 ? 0x4342 : 0x4140), nan);
-                        if (valid < kPage) {   // positions behind the end: scale 0, whatever their code
-                            const int key = 8 * j + 2 * c;
-                            if (key >= valid) { sc[e].s &= 0xffff0000u; sc[e].m24 &= 0xffff0000u; }
-                            if (key + 1 >= valid) { sc[e].s &= 0xffffu; sc[e].m24 &= 0xffffu; }
-                        }
-                    }
-#pragma unroll
-                    for (int y = 0; y < D / 32; ++y) {
-                        mma(o[4 * y + 0], a, pair<0>(w[0][y], sc[0]), pair<0>(w[1][y], sc[1]));
-                        mma(o[4 * y + 1], a, pair<1>(w[0][y], sc[0]), pair<1>(w[1][y], sc[1]));
-                        mma(o[4 * y + 2], a, pair<2>(w[0][y], sc[0]), pair<2>(w[1][y], sc[1]));
-                        mma(o[4 * y + 3], a, pair<3>(w[0][y], sc[0]), pair<3>(w[1][y], sc[1]));
-                    }
-                }
-            }
+            l[nt][0] += sum.x;
+            l[nt][1] += sum.y;
         }
     }
+
     static __device__ __forceinline__ void load_words(uint32_t (&w)[D / 32], uint32_t at) {
         if constexpr (D == 128) {
             const uint4 x = lds128(at);
@@ -506,9 +529,170 @@ struct Worker {
             w[0] = x.x; w[1] = x.y;
         }
     }
+    // Whether a tile (of keys or values) holds a block that reads as NaN.
+    __device__ __forceinline__ bool holds_nan(uint32_t tile) const {
+        uint32_t any;
+        if (D == 128) {
+            const uint4 a = lds128(tile + q4::scales_at(D) + lane * 16);
+            any = nan_bits(a.x) | nan_bits(a.y) | nan_bits(a.z) | nan_bits(a.w);
+        } else {
+            const uint2 a = lds64(tile + q4::scales_at(D) + lane * 8);
+            any = nan_bits(a.x) | nan_bits(a.y);
+        }
+        return __any_sync(0xffffffffu, any != 0);
+    }
 
-    // ---- the tree's own keys and values (bf16), nodes n0 .. n1 - 1, 16 at a time.  `parents`: 128 bytes of this warp's own.
-    __device__ __forceinline__ void tree(const Unit &u, int n0, int n1, unsigned char *parents, int &flag) {
+    static constexpr int kPart = NT == 1 ? 4 : 2;   // 16-key tiles that go through the softmax together
+
+    // Scores of the 16 kPart keys from key 16 j0 on.  kWhole: all committed, no block that reads as NaN.
+    template <bool kWhole>
+    __device__ __forceinline__ void scores(uint32_t k, int j0, int valid, float (&s)[kPart][NT][4]) {
+        constexpr int kPer = D / 64;   // scales of a lane and key
+        const uint32_t row = k + g * (D / 2) + c * (D / 8), at = k + q4::scales_at(D) + lane * (8 * kPer) + j0 * 2 * kPer;
+        uint32_t cw[2] = {};
+        if constexpr (kPart * kPer == 8) { const uint4 x = lds128(at); scores_of<kWhole>(row, j0, valid, s, {x.x, x.y, x.z, x.w}); return; }
+        if constexpr (kPart * kPer == 4) { const uint2 x = lds64(at); cw[0] = x.x; cw[1] = x.y; }
+        if constexpr (kPart * kPer == 2) cw[0] = lds32(at);
+        scores_of<kWhole>(row, j0, valid, s, {cw[0], cw[1], 0, 0});
+    }
+    struct Words4 {
+        uint32_t w[4];
+    };
+    template <bool kWhole>
+    __device__ __forceinline__ void scores_of(uint32_t row, int j0, int valid, float (&s)[kPart][NT][4], const Words4 &cw) {
+        constexpr int kPer = D / 64;
+#pragma unroll
+        for (int j = 0; j < kPart; ++j) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[j][nt][i] = 0.f;
+            uint32_t wa[D / 32], wb[D / 32];   // keys 16 j + g and 16 j + 8 + g
+            load_words(wa, row + (j0 + j) * (16 * D / 2));
+            load_words(wb, row + (j0 + j) * (16 * D / 2) + 8 * D / 2);
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) {
+                // the code of block x / 2 of either key, twice
+                const int ba = 2 * j * kPer + x / 2, bb = ba + kPer;
+                const Scale2 sa = scale2<kWhole>(__byte_perm(cw.w[ba / 4], 0, 0x4040 | (ba % 4) | ((ba % 4) << 8)));
+                const Scale2 sb = scale2<kWhole>(__byte_perm(cw.w[bb / 4], 0, 0x4040 | (bb % 4) | ((bb % 4) << 8)));
+                {
+                    const uint32_t a0 = pair<0>(wa[x], sa, sixteen), a1 = pair<0>(wb[x], sb, sixteen), a2 = pair<1>(wa[x], sa, sixteen), a3 = pair<1>(wb[x], sb, sixteen);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(s[j][nt], a0, a1, a2, a3, qf[2 * x][nt][0], qf[2 * x][nt][1]);
+                }
+                {
+                    const uint32_t a0 = pair<2>(wa[x], sa, sixteen), a1 = pair<2>(wb[x], sb, sixteen), a2 = pair<3>(wa[x], sa, sixteen), a3 = pair<3>(wb[x], sb, sixteen);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(s[j][nt], a0, a1, a2, a3, qf[2 * x + 1][nt][0], qf[2 * x + 1][nt][1]);
+                }
+            }
+            if (!kWhole) {
+                const int key = 16 * (j0 + j) + g;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (key >= valid) s[j][nt][0] = s[j][nt][1] = -INFINITY;
+                    if (key + 8 >= valid) s[j][nt][2] = s[j][nt][3] = -INFINITY;
+                }
+            }
+        }
+    }
+    // O^T += V^T P^T of the same keys.
+    template <bool kWhole>
+    __device__ __forceinline__ void values(uint32_t v, int j0, int valid, const float (&s)[kPart][NT][4]) {
+        // position pair 8 j + 4 e + c: row of D bytes; of its eight chunks the one with this lane's elements
+        const uint32_t row = v + c * D + q4::v_chunk<D>(c, g) * (D / 8);
+        const uint32_t at = v + q4::scales_at(D) + ((D == 128 ? g : g >> 1) * 4 + c) * 16 + j0 * 4;
+#pragma unroll
+        for (int j = 0; j < kPart; ++j) {
+            uint32_t b[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                b[nt][0] = transposed(pack(s[j][nt][0], s[j][nt][1]));
+                b[nt][1] = transposed(pack(s[j][nt][2], s[j][nt][3]));
+            }
+            const uint32_t cw = lds32(at + 4 * j);
+            uint32_t w[2][D / 32];
+            Scale2 sc[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                load_words(w[e], row + (2 * (j0 + j) + e) * (4 * D));
+                sc[e] = scale2<kWhole>(__byte_perm(cw, 0, e ? 0x4342 : 0x4140));
+                if (!kWhole) {   // positions behind the end: scale 0, whatever their code
+                    const int key = 8 * (2 * (j0 + j) + e) + 2 * c;
+                    if (key >= valid) { sc[e].s &= 0xffff0000u; sc[e].m24 &= 0xffff0000u; }
+                    if (key + 1 >= valid) { sc[e].s &= 0xffffu; sc[e].m24 &= 0xffffu; }
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < D / 32; ++y) {
+                {
+                    const uint32_t a0 = pair<0>(w[0][y], sc[0], sixteen), a1 = pair<1>(w[0][y], sc[0], sixteen), a2 = pair<0>(w[1][y], sc[1], sixteen), a3 = pair<1>(w[1][y], sc[1], sixteen);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(o[2 * y][nt], a0, a1, a2, a3, b[nt][0], b[nt][1]);
+                }
+                {
+                    const uint32_t a0 = pair<2>(w[0][y], sc[0], sixteen), a1 = pair<3>(w[0][y], sc[0], sixteen), a2 = pair<2>(w[1][y], sc[1], sixteen), a3 = pair<3>(w[1][y], sc[1], sixteen);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(o[2 * y + 1][nt], a0, a1, a2, a3, b[nt][0], b[nt][1]);
+                }
+            }
+        }
+    }
+
+    // ---- the unit's pages from t0 on
+    __device__ __forceinline__ void walk(const Unit &u, int pages_end, uint64_t policy, bool once, int &flag) {
+#pragma unroll 1
+        for (int t = u.t0; t < pages_end; ++t) {
+            const int valid = min(kPage, u.L - t * kPage);
+            float s[kPart][NT][4];
+            const uint32_t k = await();
+            if (gave_up) return;
+            const bool k_whole = valid == kPage && !holds_nan(k);
+            if (kPart == 4) {
+                if (k_whole) scores<true>(k, 0, valid, s);
+                else scores<false>(k, 0, valid, s);
+                release();
+                if (t_issue < 2 * pages_end) issue(u, policy, once, flag);
+                softmax<kPart>(s);
+                const uint32_t v = await();
+                if (gave_up) return;
+                if (valid == kPage && !holds_nan(v)) values<true>(v, 0, valid, s);
+                else values<false>(v, 0, valid, s);
+                release();
+                if (t_issue < 2 * pages_end) issue(u, policy, once, flag);
+            } else {
+                // both tiles are needed at once
+                ++used;
+                const uint32_t v = await();
+                --used;
+                if (gave_up) return;
+                const bool whole = k_whole && !holds_nan(v);
+                if (whole) {
+                    scores<true>(k, 0, valid, s);
+                    softmax<kPart>(s);
+                    values<true>(v, 0, valid, s);
+                    scores<true>(k, kPart, valid, s);
+                    softmax<kPart>(s);
+                    values<true>(v, kPart, valid, s);
+                } else {
+#pragma unroll 1
+                    for (int j0 = 0; 16 * j0 < valid; j0 += kPart) {
+                        scores<false>(k, j0, valid, s);
+                        softmax<kPart>(s);
+                        values<false>(v, j0, valid, s);
+                    }
+                }
+                used += 2;
+                __syncwarp();
+                if (t_issue < 2 * pages_end) issue(u, policy, once, flag);
+                if (t_issue < 2 * pages_end) issue(u, policy, once, flag);
+            }
+        }
+    }
+
+    // ---- the tree's own keys and values (bf16), nodes n0 .. n1 - 1, 16 at a time.  `parents`, `masks`: this warp's own.
+    __device__ __forceinline__ void tree(const Unit &u, int n0, int n1, unsigned char *parents, uint64_t *masks, int &flag) {
         const int32_t *par = p.parent + (size_t)u.b * p.T;
         bool bad = false;
         for (int j = lane; j < p.T; j += 32) {
@@ -521,110 +705,128 @@ struct Worker {
             flag |= kBadTree;
             return;
         }
-        uint64_t sees[2][2];   // rows g and g + 8: the nodes they see
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = u.rt * kQ4Rows + g + 8 * e;
-            sees[e][0] = sees[e][1] = 0;
-            if (r >= p.T * p.G) continue;
-            const int j = r / p.G;
-            if (p.anc) {
-                sees[e][0] = p.anc[((size_t)u.b * p.T + j) * 2];
-                sees[e][1] = p.anc[((size_t)u.b * p.T + j) * 2 + 1];
-            } else {
-                for (int i = j; i != 255; i = parents[i]) {   // (strictly falling on a valid tree)
-                    if (i < 64) sees[e][0] |= 1ull << i;
-                    else sees[e][1] |= 1ull << (i - 64);
+        if (lane < S::kRows) {   // the nodes that each row sees
+            const int r = u.rt * S::kRows + lane;
+            uint64_t lo = 0, hi = 0;
+            if (r < p.T * p.G) {
+                const int j = r / p.G;
+                if (p.anc) {
+                    lo = p.anc[((size_t)u.b * p.T + j) * 2];
+                    hi = p.anc[((size_t)u.b * p.T + j) * 2 + 1];
+                } else {
+                    for (int i = j; i != 255; i = parents[i]) {   // (strictly falling on a valid tree)
+                        if (i < 64) lo |= 1ull << i;
+                        else hi |= 1ull << (i - 64);
+                    }
                 }
             }
+            masks[2 * lane] = lo;
+            masks[2 * lane + 1] = hi;
         }
+        __syncwarp();
 #pragma unroll 1
         for (int n = n0; n < n1; n += 16) {
-            float s[2][4];
             const int left = n1 - n;
+            float s[1][NT][4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[j][i] = 0.f;
-                const bool live = 8 * j + g < left;
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.k_tree + (((size_t)u.b * p.T + (live ? n + 8 * j + g : n)) * p.Hkv + u.h) * D + c * (D / 4));
+                for (int i = 0; i < 4; ++i) s[0][nt][i] = 0.f;
+            const __nv_bfloat16 *k = p.k_tree + (((size_t)u.b * p.T + n) * p.Hkv + u.h) * D + c * (D / 4);
+            const uint4 *ka = reinterpret_cast<const uint4 *>(k + (size_t)g * p.Hkv * D), *kb = reinterpret_cast<const uint4 *>(k + (size_t)(g + 8) * p.Hkv * D);
 #pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    const uint4 w = live ? src[x] : make_uint4(0, 0, 0, 0);
-                    mma(s[j], qf[2 * x], w.x, w.y);
-                    mma(s[j], qf[2 * x + 1], w.z, w.w);
+            for (int x = 0; x < D / 32; ++x) {
+                const uint4 a = g < left ? ka[x] : make_uint4(0, 0, 0, 0), b = g + 8 < left ? kb[x] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma(s[0][nt], a.x, b.x, a.y, b.y, qf[2 * x][nt][0], qf[2 * x][nt][1]);
+                    mma(s[0][nt], a.z, b.z, a.w, b.w, qf[2 * x + 1][nt][0], qf[2 * x + 1][nt][1]);
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int node = n + 8 * j + 2 * c + (i & 1);
-                    const bool seen = 8 * j + 2 * c + (i & 1) < left && ((sees[i >> 1][node >> 6] >> (node & 63)) & 1ull);
-                    if (!seen) s[j][i] = -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t sees = (uint32_t)(masks[2 * (8 * nt + 2 * c + e) + (n >> 6)] >> (n & 63));
+                    if (g >= left || !((sees >> g) & 1u)) s[0][nt][e] = -INFINITY;
+                    if (g + 8 >= left || !((sees >> (g + 8)) & 1u)) s[0][nt][2 + e] = -INFINITY;
                 }
-            softmax<2>(s);
-            const uint32_t a[4] = {pack(s[0][0], s[0][1]), pack(s[0][2], s[0][3]), pack(s[1][0], s[1][1]), pack(s[1][2], s[1][3])};
+            softmax<1>(s);
+            uint32_t b[NT][2];
 #pragma unroll
-            for (int x = 0; x < kCols / 8; ++x) {   // eight elements of two pairs of nodes at a time
+            for (int nt = 0; nt < NT; ++nt) {
+                b[nt][0] = transposed(pack(s[0][nt][0], s[0][nt][1]));
+                b[nt][1] = transposed(pack(s[0][nt][2], s[0][nt][3]));
+            }
+            const __nv_bfloat16 *v = p.v_tree + (((size_t)u.b * p.T + n) * p.Hkv + u.h) * D + g * kOwn;
+#pragma unroll
+            for (int x = 0; x < kOwn / 8; ++x) {   // eight elements of two pairs of nodes at a time
                 uint4 w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = 2 * c + (i & 1) + 8 * (i >> 1);
                     w[i] = make_uint4(0, 0, 0, 0);
-                    if (key < left) w[i] = *reinterpret_cast<const uint4 *>(p.v_tree + (((size_t)u.b * p.T + n + key) * p.Hkv + u.h) * D + g * kCols + 8 * x);
+                    if (key < left) w[i] = *reinterpret_cast<const uint4 *>(v + (size_t)key * p.Hkv * D + 8 * x);
                 }
-                const uint32_t b[4][4] = {{w[0].x, w[0].y, w[0].z, w[0].w}, {w[1].x, w[1].y, w[1].z, w[1].w}, {w[2].x, w[2].y, w[2].z, w[2].w}, {w[3].x, w[3].y, w[3].z, w[3].w}};
+                const uint32_t a[4][4] = {{w[0].x, w[0].y, w[0].z, w[0].w}, {w[1].x, w[1].y, w[1].z, w[1].w}, {w[2].x, w[2].y, w[2].z, w[2].w}, {w[3].x, w[3].y, w[3].z, w[3].w}};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    mma(o[8 * x + 2 * i], a, __byte_perm(b[0][i], b[1][i], 0x5410), __byte_perm(b[2][i], b[3][i], 0x5410));
-                    mma(o[8 * x + 2 * i + 1], a, __byte_perm(b[0][i], b[1][i], 0x7632), __byte_perm(b[2][i], b[3][i], 0x7632));
-                }
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        mma(o[4 * x + i][nt], __byte_perm(a[0][i], a[1][i], 0x5410), __byte_perm(a[0][i], a[1][i], 0x7632), __byte_perm(a[2][i], a[3][i], 0x5410),
+                            __byte_perm(a[2][i], a[3][i], 0x7632), b[nt][0], b[nt][1]);
             }
         }
     }
 
-    // ---- results.  Lane (g, c) has of rows g and g + 8 the elements c D/4 .. + D/4 - 1: n-tile n, column 2 c + e is element (2 c + e) D/8 + n.
+    // ---- results.  Lane (g, c) has of rows 2 c and 2 c + 1 of each 8 the elements g D/8 .. + D/8 - 1: 2 x and 2 x + 1 in tile x.
+    __device__ __forceinline__ void sum_up() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 4);
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 8);
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 16);
+            }
+    }
     __device__ __forceinline__ void write_rows(const Unit &u, int flag) {
         note(p, u.b, flag, lane);
-        const int live = live_rows(p, u.rt);
+        const int live = live_rows<NT>(p, u.rt);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = g + 8 * e;
-            if (r >= live) continue;
-            const size_t row = out_row(p, u.b, u.h, u.rt, r);
-            const float inv = flag || l[e] == 0.f ? 0.f : 1.f / l[e];   // (a row that sees nothing: zeros)
-            uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * D + c * (D / 4));
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int x = 0; x < D / 32; ++x) {
-                uint32_t w[4];
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * nt + 2 * c + e;
+                if (r >= live) continue;
+                const size_t row = out_row<NT>(p, u.b, u.h, u.rt, r);
+                const float inv = flag || l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e];   // (a row that sees nothing: zeros)
+                uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * D + g * kOwn);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = 8 * x + 2 * i, n = k % kCols, col = 2 * e + k / kCols;
-                    w[i] = flag ? 0u : pack(o[n][col] * inv, o[n + 1][col] * inv);
+                for (int x = 0; x < kOwn / 8; ++x) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = flag ? 0u : pack(o[4 * x + i][nt][e] * inv, o[4 * x + i][nt][2 + e] * inv);
+                    dst[x] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                dst[x] = make_uint4(w[0], w[1], w[2], w[3]);
+                if (p.lse && g == 0) p.lse[row] = flag ? 0.f : fmaf(m[nt][e], p.scale, log2f(l[nt][e]) * 0.6931471805599453f);
             }
-            if (p.lse && c == 0) p.lse[row] = flag ? 0.f : fmaf(m[e], p.scale, log2f(l[e]) * 0.6931471805599453f);
-        }
     }
-    __device__ __forceinline__ void write_share(const Unit &u, int slot, int flag) {
-        const int live = live_rows(p, u.rt);
+    // The worker's share of a unit: O to dst [rows][D], (m, l) to ml [rows].
+    __device__ __forceinline__ void write_share(const Unit &u, float *dst, float2 *ml) {
+        const int live = live_rows<NT>(p, u.rt);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = g + 8 * e;
-            if (r >= live) continue;
-            float4 *dst = reinterpret_cast<float4 *>(p.partial_o + ((size_t)slot * kQ4Rows + r) * D + c * (D / 4));
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int x = 0; x < D / 16; ++x) {
-                const int k = 4 * x, n = k % kCols, col = 2 * e + k / kCols;
-                dst[x] = make_float4(o[n][col], o[n + 1][col], o[n + 2][col], o[n + 3][col]);
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * nt + 2 * c + e;
+                if (r >= live) continue;
+                float4 *at = reinterpret_cast<float4 *>(dst + (size_t)r * D + g * kOwn);
+#pragma unroll
+                for (int x = 0; x < kOwn / 4; ++x) at[x] = make_float4(o[2 * x][nt][e], o[2 * x][nt][2 + e], o[2 * x + 1][nt][e], o[2 * x + 1][nt][2 + e]);
+                if (g == 0) ml[r] = make_float2(m[nt][e], l[nt][e]);
             }
-            if (c == 0) p.partial_ml[slot * kQ4Rows + r] = make_float2(m[e], l[e]);
-        }
-        if (lane == 0) p.flags[slot] = flag;
     }
-
     // Whether this warp is the last of `count` to arrive; what the others wrote before is visible to it.
     __device__ __forceinline__ bool last_to_arrive(int32_t *counter, int count) {
         __threadfence();
@@ -637,18 +839,16 @@ struct Worker {
         return true;
     }
     __device__ __forceinline__ void finish(const Unit &u, const List &list, int worker, int flag) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
-            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-        }
+        sum_up();
         if (u.t0 == 0 && u.t1 == u.ntiles) {
             write_rows(u, flag);
             return;
         }
         // the unit's shares belong to the workers c0 .. c1; a worker's slots: 2 c + 1 for a unit that it begins, else 2 c
         const int c0 = list.worker_of(u.w0 + kUnitCost), c1 = list.worker_of(u.w0 + kUnitCost + u.ntiles - 1);
-        write_share(u, 2 * worker + (u.t0 == 0 ? 1 : 0), flag);
+        const int slot = 2 * worker + (u.t0 == 0 ? 1 : 0);
+        write_share(u, p.partial_o + (size_t)slot * S::kRows * D, p.partial_ml + slot * S::kRows);
+        if (lane == 0) p.flags[slot] = flag;
         // up to kOneLevel shares: one group; more: about as many groups as shares in a group
         const int shares = c1 - c0 + 1;
         int size = shares;
@@ -659,41 +859,51 @@ struct Worker {
         const int groups = (shares + size - 1) / size, group = (worker - c0) / size, lead = c0 + group * size;
         const int lead_slot = 2 * lead + (group == 0 ? 1 : 0), members = min(size, c1 - lead + 1);
         if (!last_to_arrive(p.counters + lead_slot, members)) return;
-        merge<D>(p, u.b, u.h, u.rt, lead_slot, 2 * lead, 1, members, groups == 1);
+        merge<D, NT>(p, u.b, u.h, u.rt, lead_slot, 2 * lead, 1, members, groups == 1);
         if (groups == 1) return;
-        if (!last_to_arrive(p.counters + 2 * (p.n_ctas * kQ4Warps) + 2 * c0 + 1, groups)) return;
-        merge<D>(p, u.b, u.h, u.rt, 2 * c0 + 1, 2 * c0, size, groups, true);
+        if (!last_to_arrive(p.counters + 2 * (p.n_ctas * S::kWarps) + 2 * c0 + 1, groups)) return;
+        merge<D, NT>(p, u.b, u.h, u.rt, 2 * c0 + 1, 2 * c0, size, groups, true);
+    }
+    // The block does not end under its own copies.
+    __device__ __forceinline__ void drain() {
+        if (!gave_up) return;
+        const uint64_t t0 = globaltimer_ns();
+        for (; used < issued; ++used)
+            while (!mbar_try_wait(bars + (used % S::kSlots) * 8, (used / S::kSlots) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+            }
     }
 };
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1) q4_attn_rows_kernel(const __grid_constant__ Q4AttnParams p) {
-    extern __shared__ __align__(128) unsigned char smem[];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t base = smem_u32(smem);
-    int32_t *prefix = reinterpret_cast<int32_t *>(smem + Cfg<D>::kOffPrefix);
-    Worker<D> k(p);
-    k.ring = base + warp * kStages * Cfg<D>::kStageBytes;
-    k.bars = base + Cfg<D>::kOffBars + warp * kStages * 8;
-    k.lane = lane; k.g = lane >> 2; k.c = lane & 3;
-    k.issued = k.used = 0;
-    k.gave_up = false;
-    if (lane == 0) {
-        for (int s = 0; s < kStages; ++s) mbar_init(k.bars + s * 8, 1);
-        fence_mbar_init();
-        fence_proxy_async();
+// Whether parent array b is a tree.  Warp-collective.
+__device__ __forceinline__ bool tree_ok(const Q4AttnParams &p, int b, int lane) {
+    bool bad = false;
+    for (int j = lane; j < p.T; j += 32) {
+        const int a = p.parent[(size_t)b * p.T + j];
+        bad |= !(j == 0 ? a == -1 : a >= 0 && a < j);
     }
+    return !__any_sync(0xffffffffu, bad);
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(const __grid_constant__ Q4AttnParams p) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    using S = Shape<NT>;
+    using C = Cfg<D, NT>;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int32_t *prefix = reinterpret_cast<int32_t *>(smem + C::kOffPrefix);
+    Worker<D, NT> k(p);
+    k.init(smem, warp);
     pdl_wait();
     pdl_launch_dependents();
 
     // the list: prefix sums over the sequences
     List list;
-    list.per_seq = p.Hkv * ((p.T * p.G + kQ4Rows - 1) / kQ4Rows);
+    list.per_seq = p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows);
     list.tree_tiles = (p.T + kPage - 1) / kPage;
     list.step = (p.B + kPrefix - 1) / kPrefix;
-    __shared__ int warp_sum[kQ4Warps];
+    __shared__ int warp_sum[S::kWarps];
     int carry = 0, longest = 0;
-    for (int b0 = 0; b0 < p.B; b0 += kThreads) {
+    for (int b0 = 0; b0 < p.B; b0 += S::kThreads) {
         const int b = b0 + tid;
         const int L = b < p.B ? p.seq_lens[b] : 0;
         const int e = b < p.B ? entries_of(p, list, L) : 0;
@@ -709,7 +919,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_rows_kernel(const __grid_
         __syncthreads();
         int before = 0, all = 0;
 #pragma unroll
-        for (int i = 0; i < kQ4Warps; ++i) {
+        for (int i = 0; i < S::kWarps; ++i) {
             const int x = warp_sum[i];
             before += i < warp ? x : 0;
             all += x;
@@ -722,24 +932,19 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_rows_kernel(const __grid_
     if (lane == 0) warp_sum[warp] = longest;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kQ4Warps; ++i) longest = max(longest, warp_sum[i]);
+    for (int i = 0; i < S::kWarps; ++i) longest = max(longest, warp_sum[i]);
     list.W = carry;
-    list.n_workers = max(1, min(p.n_ctas * kQ4Warps, list.W / kMinEntries));
+    list.n_workers = max(1, min(p.n_ctas * S::kWarps, list.W / kMinEntries));
     // two levels of merging hold 32 x 32 shares of a unit
     longest /= list.per_seq;
     if ((int64_t)longest * list.n_workers > (int64_t)(kMaxShares - 2) * list.W)
         list.n_workers = max(1, (int)((int64_t)(kMaxShares - 2) * list.W / longest));
 
-    // a sequence whose length cannot be: zero rows, from one block
-    for (int b = blockIdx.x * kQ4Warps + warp; b < p.B; b += p.n_ctas * kQ4Warps) {
+    // a sequence whose length cannot be: zero rows, from one warp
+    for (int b = blockIdx.x * S::kWarps + warp; b < p.B; b += p.n_ctas * S::kWarps) {
         if (length_ok(p, p.seq_lens[b])) continue;
-        bool bad = false;
-        for (int j = lane; j < p.T; j += 32) {
-            const int a = p.parent[(size_t)b * p.T + j];
-            bad |= !(j == 0 ? a == -1 : a >= 0 && a < j);
-        }
-        bad = __any_sync(0xffffffffu, bad);
-        if (lane == 0) p.status[b] = bad ? READER_ERR_BAD_TREE : READER_ERR_CAPACITY;
+        const bool tree = tree_ok(p, b, lane);
+        if (lane == 0) p.status[b] = tree ? READER_ERR_CAPACITY : READER_ERR_BAD_TREE;
         const size_t rows = (size_t)p.T * p.Hq;
         uint4 *o = reinterpret_cast<uint4 *>(p.out + (size_t)b * rows * D);
         for (size_t i = lane; i < rows * (D / 8); i += 32) o[i] = make_uint4(0, 0, 0, 0);
@@ -754,59 +959,144 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_rows_kernel(const __grid_
     const int w_end = list.begin(worker + 1);
     const uint64_t policy = l2_policy_evict_first();
     const bool once = list.per_seq == p.Hkv;   // no other unit reads these pages
-    unsigned char *parents = smem + Cfg<D>::kOffParents + warp * kMaxNodes;
+    unsigned char *parents = smem + C::kOffParents + warp * kMaxNodes;
+    uint64_t *masks = reinterpret_cast<uint64_t *>(smem + C::kOffMasks) + warp * S::kRows * 2;
 
     Unit u;
     u.any = false;
-    int flag = 0;
+    int flag = 0, pages_end = 0;
     for (;;) {
         // The next unit's first tiles are on their way before this one's results are written.
         Unit coming;
-        int coming_flag = 0;
+        int coming_flag = 0, coming_end = 0;
         coming.any = false;
         while (w < w_end && !coming.any) {
             coming = unit_at(p, list, prefix, w, w_end, lane);
             w += coming.entries;
         }
         if (coming.any && !k.gave_up) {
-            if (p.num_pages == 0 && coming.t0 < coming.npages) coming_flag |= kBadPage;   // no pool to read from
-            else {
-                k.start(coming, coming_flag);
-                for (int t = coming.t0; t < min(coming.npages, coming.t1) && t < coming.t0 + kStages; ++t)
-                    k.issue(coming, t, policy, once && t >= p.shared_prefix_pages, coming_flag);
+            coming_end = min(coming.npages, coming.t1);
+            if (p.num_pages == 0 && coming.t0 < coming_end) {   // no pool to read from
+                coming_flag |= kBadPage;
+                coming_end = coming.t0;
             }
+            k.start(coming, coming_end, policy, once, coming_flag);
         }
         if (u.any) k.finish(u, list, worker, flag);
         if (!coming.any) break;
         u = coming;
         flag = coming_flag;
-        k.load_queries(u);
-        k.m[0] = k.m[1] = -INFINITY;
-        k.l[0] = k.l[1] = 0.f;
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) k.o[n][i] = 0.f;
-        const int pages_end = p.num_pages == 0 ? u.t0 : min(u.npages, u.t1);
-#pragma unroll 1
-        for (int t = u.t0; t < pages_end && !k.gave_up; ++t) {
-            k.await();
-            if (k.gave_up) break;
-            k.tile(k.ring + (k.used % kStages) * Cfg<D>::kStageBytes, min(kPage, u.L - t * kPage));
-            ++k.used;
-            __syncwarp();
-            if (t + kStages < pages_end) k.issue(u, t + kStages, policy, once && t + kStages >= p.shared_prefix_pages, flag);
-        }
+        pages_end = coming_end;
+        k.begin(u);
+        // (the tree first: its rows come while the first tiles are on their way)
         const int n0 = max(0, u.t0 - u.npages) * kPage, n1 = min(p.T, (u.t1 - u.npages) * kPage);
-        if (n1 > n0) k.tree(u, n0, n1, parents, flag);
+        if (n1 > n0) k.tree(u, n0, n1, parents, masks, flag);
+        if (!k.gave_up) k.walk(u, pages_end, policy, once, flag);
         flag = __reduce_or_sync(0xffffffffu, flag);
         if (k.gave_up || worker == p.give_up) flag |= kGaveUp;   // (the rest of the range is given up with the unit)
     }
-    if (k.gave_up) {   // the block does not end under its own copies
-        const uint64_t t0 = globaltimer_ns();
-        for (; k.used < k.issued; ++k.used)
-            while (!mbar_try_wait(k.bars + (k.used % kStages) * 8, (k.used / kStages) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+    k.drain();
+}
+
+// The other form: a cluster of thread blocks per sequence, p.split of them for each of its units.
+template <int D, int NT>
+__global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(const __grid_constant__ Q4AttnParams p) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    using S = Shape<NT>;
+    using C = Cfg<D, NT>;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    Worker<D, NT> k(p);
+    k.init(smem, warp);
+    __shared__ int flags;
+    if (tid == 0) flags = 0;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int size = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
+    const int n_rt = (p.T * p.G + S::kRows - 1) / S::kRows, unit = rank / p.split, piece = rank - unit * p.split;
+    Unit u;
+    u.b = blockIdx.x / size;
+    u.h = unit / n_rt;
+    u.rt = unit - u.h * n_rt;
+    u.L = p.seq_lens[u.b];
+    const bool ok = length_ok(p, u.L);
+    u.npages = ok ? (u.L + kPage - 1) / kPage : 0;
+    u.ntiles = ok ? u.npages + (p.T + kPage - 1) / kPage : 0;
+    const int workers = p.split * S::kWarps, mine = piece * S::kWarps + warp;
+    u.t0 = mul_div(mine, u.ntiles, workers);
+    u.t1 = mul_div(mine + 1, u.ntiles, workers);
+    u.any = u.t1 > u.t0;
+    int flag = 0;
+    float *share = reinterpret_cast<float *>(smem + warp * C::kRingBytes);   // the ring, when no copy is under way any more
+    float2 *ml_all = reinterpret_cast<float2 *>(smem + C::kOffShares), *ml_mine = ml_all + warp * S::kRows;
+    if (u.any) {
+        const uint64_t policy = l2_policy_evict_first();
+        const bool once = n_rt == 1;
+        int pages_end = min(u.npages, u.t1);
+        if (p.num_pages == 0 && u.t0 < pages_end) {   // no pool to read from
+            flag |= kBadPage;
+            pages_end = u.t0;
+        }
+        k.start(u, pages_end, policy, once, flag);
+        k.begin(u);
+        const int n0 = max(0, u.t0 - u.npages) * kPage, n1 = min(p.T, (u.t1 - u.npages) * kPage);
+        if (n1 > n0)
+            k.tree(u, n0, n1, smem + C::kOffParents + warp * kMaxNodes, reinterpret_cast<uint64_t *>(smem + C::kOffMasks) + warp * S::kRows * 2, flag);
+        k.walk(u, pages_end, policy, once, flag);
+        flag = __reduce_or_sync(0xffffffffu, flag);
+        if (k.gave_up || (int)blockIdx.x * S::kWarps + warp == p.give_up) flag |= kGaveUp;
+        k.drain();
+        k.sum_up();
+        k.write_share(u, share, ml_mine);
+    } else {
+        for (int i = lane; i < S::kRows * D / 4; i += 32) reinterpret_cast<float4 *>(share)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (lane < S::kRows) ml_mine[lane] = make_float2(-INFINITY, 0.f);
+        // (without a tile nobody looks at the tree: the first worker does)
+        if (!ok && mine == 0) flag = tree_ok(p, u.b, lane) ? kBadLength : kBadTree;
+    }
+    if (flag && lane == 0) atomicOr(&flags, flag);
+    __syncthreads();
+    const int live = live_rows<NT>(p, u.rt), block_flag = ok ? flags : flags | kBadLength;
+    // the block's shares, four rows to a warp
+    for (int r0 = warp * kRowsAtOnce; r0 < live; r0 += S::kWarps * kRowsAtOnce) {
+        float2 ml[kRowsAtOnce];
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i) ml[i] = lane < S::kWarps && r0 + i < live ? ml_all[lane * S::kRows + r0 + i] : make_float2(-INFINITY, 0.f);
+        const Merged x = merge_rows<D, false>(ml, S::kWarps, live - r0, p.scale_log2, [&](int w, int i) {
+            return reinterpret_cast<const float *>(smem + w * C::kRingBytes) + (r0 + i) * D;
+        });
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i) {
+            const int r = r0 + i;
+            if (r >= live) continue;
+            if (p.split == 1) {
+                put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r), x.top[i], x.total[i], x.o[i], block_flag);
+            } else {
+                if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + ((size_t)blockIdx.x * S::kRows + r) * D + lane * 4) = x.o[i];
+                if (lane == 0) p.partial_ml[blockIdx.x * S::kRows + r] = make_float2(x.top[i], x.total[i]);
             }
+        }
+    }
+    if (tid == 0) p.flags[blockIdx.x] = block_flag;
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    const int block0 = blockIdx.x - rank;   // the cluster's first
+    if (rank == 0 && warp == 0) {
+        const int all = __reduce_or_sync(0xffffffffu, lane < size ? __ldcg(p.flags + block0 + lane) : 0);
+        if (lane == 0) p.status[u.b] = code_of_flag(all);
+    }
+    if (p.split == 1) return;
+    // the shares of the unit's blocks, four rows to a warp of them
+    const int first = block0 + unit * p.split, unit_flag = __reduce_or_sync(0xffffffffu, lane < p.split ? __ldcg(p.flags + first + lane) : 0);
+    for (int r0 = (warp * p.split + piece) * kRowsAtOnce; r0 < live; r0 += workers * kRowsAtOnce) {
+        float2 ml[kRowsAtOnce];
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i)
+            ml[i] = lane < p.split && r0 + i < live ? __ldcg(p.partial_ml + (first + lane) * S::kRows + r0 + i) : make_float2(-INFINITY, 0.f);
+        const Merged x = merge_rows<D, true>(ml, p.split, live - r0, p.scale_log2,
+                                             [&](int w, int i) { return p.partial_o + ((size_t)(first + w) * S::kRows + r0 + i) * D; });
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i)
+            if (r0 + i < live) put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r0 + i), x.top[i], x.total[i], x.o[i], unit_flag);
     }
 }
 
@@ -819,22 +1109,63 @@ __global__ void __launch_bounds__(1024) q4_attn_zero_kernel(int4 *counters, int 
     for (int b = i; b < B; b += gridDim.x * 1024) status[b] = READER_OK;
 }
 
-}  // namespace
+constexpr int kAloneTiles = 6;
 
-reader_status launch_q4_attn_rows(bool *attr_set, const Q4AttnParams &p, cudaStream_t st) {
+template <int D, int NT>
+reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) {
+    using S = Shape<NT>;
+    using C = Cfg<D, NT>;
     if (!*attr_set) {
-        if (cudaFuncSetAttribute(q4_attn_rows_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmem) != cudaSuccess ||
-            cudaFuncSetAttribute(q4_attn_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmem) != cudaSuccess) {
+        if (cudaFuncSetAttribute(q4_attn_list_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(q4_attn_alone_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(q4_attn_alone_kernel<D, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
             cudaGetLastError();
             return READER_ERR_CUDA;
         }
         *attr_set = true;
     }
-    const int words = p.n_ctas * kQ4Warps;   // 4 counters a worker
+    // Alone: the units of a sequence fit a cluster, the clusters the GPU, and, going by the page table's width, a worker gets at most
+    // kAloneTiles tiles.
+    const int units = p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows);
+    const int tiles = p.max_pages + (p.T + kPage - 1) / kPage;
+    if (units <= kMaxCluster) {
+        int split = 1;
+        while (2 * split * units <= kMaxCluster && 2 * split * units * (int64_t)p.B <= n_sm && tiles > split * S::kWarps) split *= 2;
+        if ((int64_t)units * split * p.B <= n_sm && tiles <= (int64_t)kAloneTiles * split * S::kWarps) {
+            p.split = split;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(p.B * units * split));
+            cfg.blockDim = dim3(S::kThreads);
+            cfg.dynamicSmemBytes = C::kSmem;
+            cfg.stream = st;
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim.x = (unsigned)(units * split);
+            attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 2;
+            if (cudaLaunchKernelEx(&cfg, q4_attn_alone_kernel<D, NT>, p) != cudaSuccess) {
+                cudaGetLastError();
+                return READER_ERR_CUDA;
+            }
+            return READER_OK;
+        }
+    }
+    p.n_ctas = n_sm;
+    const int words = n_sm * S::kWarps;   // 4 counters a worker
     launch_pdl(q4_attn_zero_kernel, dim3((unsigned)((words + 1023) / 1024)), dim3(1024), 0, st, reinterpret_cast<int4 *>(p.counters), words, p.status, p.B);
-    launch_pdl(p.D == 128 ? q4_attn_rows_kernel<128> : q4_attn_rows_kernel<64>, dim3((unsigned)p.n_ctas), dim3(kThreads),
-               (size_t)(p.D == 128 ? Cfg<128>::kSmem : Cfg<64>::kSmem), st, p);
+    launch_pdl(q4_attn_list_kernel<D, NT>, dim3((unsigned)n_sm), dim3(S::kThreads), (size_t)C::kSmem, st, p);
     return READER_OK;
+}
+
+}  // namespace
+
+reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st) {
+    const bool few = p.T * p.G <= 8;
+    if (p.D == 128) return few ? launch<128, 1>(&attr->rows[0], p, n_sm, st) : launch<128, 2>(&attr->rows[1], p, n_sm, st);
+    return few ? launch<64, 1>(&attr->rows[2], p, n_sm, st) : launch<64, 2>(&attr->rows[3], p, n_sm, st);
 }
 
 }  // namespace reader
