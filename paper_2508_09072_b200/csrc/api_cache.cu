@@ -83,11 +83,11 @@ Q4Ws q4_ws(const reader_ctx *ctx, int D) {
     Q4Ws w{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes); return o; };
-    const size_t workers = (size_t)ctx->n_sm * kQ4MaxWorkers, rows = (size_t)ctx->n_sm * kQ4WorkerRows;
-    w.counters = take(sizeof(int32_t) * 4 * workers);
-    w.flags = take(sizeof(int32_t) * 2 * workers);
-    w.partial_ml = take(sizeof(float2) * 2 * rows);
-    w.partial_o = take(sizeof(float) * 2 * rows * D);
+    const size_t rows = (size_t)ctx->n_sm * kQ4ShareRows;
+    w.counters = take(sizeof(int32_t) * (size_t)ctx->n_sm);
+    w.flags = take(sizeof(int32_t) * 2 * (size_t)ctx->n_sm);
+    w.partial_ml = take(sizeof(float2) * rows);
+    w.partial_o = take(sizeof(float) * rows * D);
     w.total = at;
     return w;
 }

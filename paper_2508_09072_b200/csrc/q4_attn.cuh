@@ -4,8 +4,8 @@
 
 namespace reader {
 
-// Workers (warps) of a thread block of the few-rows kernels, and rows of all of an SM's workers together, at most.
-constexpr int kQ4MaxWorkers = 16, kQ4WorkerRows = 192;
+// Rows of the shares of a thread block's workers and of its own two, at most (few-rows kernels).
+constexpr int kQ4ShareRows = 192 + 32;
 constexpr int kQ4MaxBatch = 1 << 16;
 
 struct Q4AttnParams {
@@ -21,10 +21,10 @@ struct Q4AttnParams {
     float scale_log2, scale;
     int give_up;               // worker that reports a wait that ran out (testing aid); -1: none
     // workspace
-    int32_t *counters;         // [4 * workers]: arrivals of a group's shares, of a unit's groups
-    int32_t *flags;            // [2 * workers] what is wrong with a share
-    float2 *partial_ml;        // [2 * workers][rows] largest score, sum
-    float *partial_o;          // [2 * workers][rows][D]
+    int32_t *counters;         // [thread blocks] arrivals at the unit that a block begins and others go on with
+    int32_t *flags;            // [2 * thread blocks] what is wrong with a block's shares
+    float2 *partial_ml;        // [shares][rows] largest score, sum: of workers, behind them of blocks
+    float *partial_o;          // [shares][rows][D]
     int n_ctas;                // thread blocks (list form)
     int split;                 // thread blocks of a unit (alone)
 };

@@ -14,9 +14,11 @@
 // Two forms.  (Alone) A call with few units is one launch: a cluster of thread blocks per unit, whose workers share its
 // tiles; shares (m, l, O) are merged in shared memory, those of the cluster's blocks through the workspace after its barrier.
 // (List) The units, each preceded by kUnitCost entries for its start and end, form one flat list of tiles that is cut into equal
-// ranges, one per worker.  Every thread block makes the list's prefix sums from seq_lens itself.  A unit that lies in several
-// ranges leaves shares in the workspace; the last to arrive of a group of them merges the group, the last group the unit, always in
-// the order of the shares, whoever comes last.  The counters are zeroed by a launch in front.
+// ranges, one per worker, those of a thread block side by side.  Every thread block makes the list's prefix sums from seq_lens
+// itself.  A worker writes a unit that lies in its range whole, and leaves a share (m, l, O) of any other; when all of a block's
+// workers are done, they merge the shares of each unit in the block, most of them in shared memory; the block that comes
+// last of those that have a unit in common merges theirs, through the workspace.  Always in the order of the shares, whoever
+// comes last.  The counters are zeroed by a launch in front.
 //
 // What is checked where: lengths by every block, page ids by the worker that reads them, a tree by the worker of the unit's
 // tree tiles; what is wrong travels with the share and zeroes the unit's rows.  Bytes behind a sequence's end never reach a
@@ -40,10 +42,8 @@ struct Shape {
     static constexpr int kThreads = kWarps * 32, kRows = 8 * NT;
 };
 constexpr int kUnitCost = 2;       // entries that stand for a unit's start and end
-constexpr int kMinEntries = 4;     // a smaller range costs more in merging than it saves in time
-constexpr int kOneLevel = 16;      // up to so many shares are merged at once, more in groups
-constexpr int kMaxShares = 32 * 32;
-constexpr int kPrefix = 1024;      // entries of the prefix table in shared memory
+constexpr int kMinEntries = kUnitCost + 1;   // of a range: so every one of them holds a tile
+constexpr int kPrefix = 256;       // entries of the prefix table in shared memory
 constexpr float kRaiseBy = 8.f;    // log2 units by which a score may exceed the maximum in use
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr int kBadTree = 1, kBadLength = 2, kBadPage = 4, kGaveUp = 8;
@@ -58,9 +58,9 @@ struct Cfg {
     static constexpr int kOffParents = kOffBars + S::kWarps * S::kSlots * 8;
     static constexpr int kOffMasks = kOffParents + S::kWarps * kMaxNodes;
     static constexpr int kOffShares = kOffMasks + S::kWarps * S::kRows * 16;           // (m, l) of the workers' rows
-    static constexpr int kOffPrefix = kOffShares + S::kWarps * S::kRows * 8;
-    static constexpr int kSmem = kOffPrefix + (kPrefix + 1) * 4;
-    static_assert(kSmem + 256 <= 227 * 1024 && kRingBytes >= S::kRows * D * 4, "shared memory");
+    static constexpr int kOffPrefix = kOffShares + S::kWarps * S::kRows * 8;           // first entry, length of each sequence
+    static constexpr int kSmem = kOffPrefix + kPrefix * 8;
+    static_assert(kSmem + 1024 <= 227 * 1024 && kRingBytes >= S::kRows * D * 4, "shared memory");
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy, bool streamed) {
@@ -149,7 +149,7 @@ struct Unit {
 };
 
 struct List {
-    int W, n_workers, per_seq, tree_tiles, step;   // step: sequences per entry of the prefix table
+    int W, n_workers, per_block, per_seq, tree_tiles, step;   // step: sequences per entry of the prefix table
     __device__ __forceinline__ int begin(int worker) const { return mul_div(worker, W, n_workers); }
     // the worker whose range holds entry w
     __device__ __forceinline__ int worker_of(int w) const {
@@ -160,6 +160,16 @@ struct List {
         return c;
     }
 };
+// A unit whose shares a thread block merges: those of its workers first .. last (first < 0: none); whether the first of them begins it;
+// the blocks block0 .. block1 have it in common.
+struct Task {
+    int b, h, rt, first, last, begins, block0, block1;
+};
+// The sequences: for up to 32 in the lanes' registers, beyond that a table in shared memory.
+struct Seqs {
+    int start, L;            // of sequence `lane`
+    const int2 *table;       // (start, length) of every list.step-th
+};
 
 __device__ __forceinline__ bool length_ok(const Q4AttnParams &p, int L) { return L >= 0 && (int64_t)L <= (int64_t)p.max_pages * kPage; }
 __device__ __forceinline__ int entries_of(const Q4AttnParams &p, const List &l, int L) {
@@ -167,41 +177,47 @@ __device__ __forceinline__ int entries_of(const Q4AttnParams &p, const List &l, 
 }
 
 // The part of the list from w on that lies in one unit (and before w_end).  Warp-collective.
-__device__ __forceinline__ Unit unit_at(const Q4AttnParams &p, const List &l, const int32_t *prefix, int w, int w_end, int lane) {
+__device__ __forceinline__ Unit unit_at(const Q4AttnParams &p, const List &l, const Seqs &seqs, int w, int w_end, int lane) {
     Unit u;
-    // the last prefix entry that is not behind w
-    const int n = (p.B + l.step - 1) / l.step;
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (prefix[mid] <= w) lo = mid; else hi = mid;
-    }
-    int start = prefix[lo], b = lo * l.step;
-    if (l.step == 1) {
-        u.L = p.seq_lens[b];
-    } else {   // at most 64 sequences from there on
-        int left = min(l.step, p.B - b);
-        for (;;) {
-            const int L = lane < left ? p.seq_lens[b + lane] : -1;
-            const int e = lane < left ? entries_of(p, l, L) : 0;
-            int incl = e;
+    int start, b;
+    if (p.B <= 32) {   // the last sequence that begins at or before w (one without entries begins where the next one does)
+        b = 31 - __clz(__ballot_sync(0xffffffffu, seqs.start <= w));
+        start = __shfl_sync(0xffffffffu, seqs.start, b);
+        u.L = __shfl_sync(0xffffffffu, seqs.L, b);
+    } else {
+        int lo = 0, hi = (p.B + l.step - 1) / l.step;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (seqs.table[mid].x <= w) lo = mid; else hi = mid;
+        }
+        const int2 x = seqs.table[lo];
+        start = x.x;
+        u.L = x.y;
+        b = lo * l.step;
+        if (l.step > 1) {   // at most 256 sequences from there on
+            int left = min(l.step, p.B - b);
+            for (;;) {
+                const int L = lane < left ? p.seq_lens[b + lane] : -1;
+                const int e = lane < left ? entries_of(p, l, L) : 0;
+                int incl = e;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int t = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += t;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int t = __shfl_up_sync(0xffffffffu, incl, d);
+                    if (lane >= d) incl += t;
+                }
+                const unsigned here = __ballot_sync(0xffffffffu, e > 0 && start + incl > w);
+                if (here) {
+                    const int j = __ffs(here) - 1;
+                    start += __shfl_sync(0xffffffffu, incl - e, j);
+                    u.L = __shfl_sync(0xffffffffu, L, j);
+                    b += j;
+                    break;
+                }
+                start += __shfl_sync(0xffffffffu, incl, 31);
+                b += 32;
+                left -= 32;
+                if (left <= 0) break;   // (cannot be: w lies before the next entry)
             }
-            const unsigned here = __ballot_sync(0xffffffffu, e > 0 && start + incl > w);
-            if (here) {
-                const int j = __ffs(here) - 1;
-                start += __shfl_sync(0xffffffffu, incl - e, j);
-                u.L = __shfl_sync(0xffffffffu, L, j);
-                b += j;
-                break;
-            }
-            start += __shfl_sync(0xffffffffu, incl, 31);
-            b += 32;
-            left -= 32;
-            if (left <= 0) break;   // (cannot be: w lies before the next entry)
         }
     }
     u.b = b;
@@ -235,104 +251,67 @@ __device__ __forceinline__ void note(const Q4AttnParams &p, int b, int flag, int
     if (flag && lane == 0) atomicMax(p.status + b, code_of_flag(flag));
 }
 
-// Merges rows r0 .. r0 + kRowsAtOnce - 1 of `count` <= 32 shares: lane k knows (m, l) of share k, at(k, r) is where its row r of O stands.
-// A share whose maximum is -inf has weight 0 and is still added, so that a NaN in it stays.
-constexpr int kRowsAtOnce = 4;
-struct Merged {
-    float top[kRowsAtOnce], total[kRowsAtOnce];
-    float4 o[kRowsAtOnce];   // elements 4 lane .. + 3
+// One row of `count` shares: ml(k) and at(k) are share k's (m, l) and its row of O.  A share whose maximum is -inf has weight 0 and is
+// still added, so that a NaN in it stays.
+struct Row {
+    float top, total;
+    float4 o;   // elements 4 lane .. + 3
 };
-template <int D, bool kGlobal, typename At>
-__device__ __forceinline__ Merged merge_rows(const float2 (&ml)[kRowsAtOnce], int count, int rows, float scale_log2, const At &at) {
+template <int D, typename Ml, typename At>
+__device__ __forceinline__ Row merge_row(int count, float scale_log2, const Ml &ml_of, const At &at) {
     const int lane = threadIdx.x & 31;
     const bool has = lane * 4 < D;
-    Merged x;
-    float weight[kRowsAtOnce];
-#pragma unroll
-    for (int i = 0; i < kRowsAtOnce; ++i) {
-        x.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        float t = ml[i].x;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-        x.top[i] = t;
-        weight[i] = ml[i].x == -INFINITY ? 0.f : ml[i].x == t ? 1.f : ex2((ml[i].x - t) * scale_log2);
-        t = ml[i].y * weight[i];
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-        x.total[i] = t;
-    }
+    constexpr int kAtOnce = 8;   // (this code runs once, with a cold instruction cache: 16 at once are no faster)
+    Row x = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 1
-    for (int k0 = 0; k0 < count; k0 += 4) {
-        float4 y[4][kRowsAtOnce];
+    for (int k0 = 0; k0 < count; k0 += kAtOnce) {
+        const int n = min(kAtOnce, count - k0);
+        const float2 ml = lane < n ? ml_of(k0 + lane) : make_float2(-INFINITY, 0.f);
+        float4 y[kAtOnce];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < kAtOnce; ++k) {
+            y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (has && k < n) y[k] = *reinterpret_cast<const float4 *>(at(k0 + k) + lane * 4);
+        }
+        float top = ml.x;
 #pragma unroll
-            for (int i = 0; i < kRowsAtOnce; ++i) {
-                y[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (!has || k0 + k >= count || i >= rows) continue;
-                const float4 *src = reinterpret_cast<const float4 *>(at(k0 + k, i) + lane * 4);
-                y[k][i] = kGlobal ? __ldcg(src) : *src;
-            }
+        for (int d = 4; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        top = fmaxf(x.top, __shfl_sync(0xffffffffu, top, 0));
+        const float keep = x.top == top ? 1.f : ex2((x.top - top) * scale_log2);
+        const float weight = ml.x == -INFINITY ? 0.f : ml.x == top ? 1.f : ex2((ml.x - top) * scale_log2);
+        float sum = ml.y * weight;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        x.top = top;
+        x.total = fmaf(x.total, keep, __shfl_sync(0xffffffffu, sum, 0));
+        x.o.x *= keep; x.o.y *= keep; x.o.z *= keep; x.o.w *= keep;
 #pragma unroll
-            for (int i = 0; i < kRowsAtOnce; ++i) {
-                const float w = __shfl_sync(0xffffffffu, weight[i], min(k0 + k, 31));   // (behind the last share: 0 times 0)
-                x.o[i].x = fmaf(y[k][i].x, w, x.o[i].x);
-                x.o[i].y = fmaf(y[k][i].y, w, x.o[i].y);
-                x.o[i].z = fmaf(y[k][i].z, w, x.o[i].z);
-                x.o[i].w = fmaf(y[k][i].w, w, x.o[i].w);
-            }
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float w = __shfl_sync(0xffffffffu, weight, k);   // (behind the last share: 0 times 0)
+            x.o.x = fmaf(y[k].x, w, x.o.x);
+            x.o.y = fmaf(y[k].y, w, x.o.y);
+            x.o.z = fmaf(y[k].z, w, x.o.z);
+            x.o.w = fmaf(y[k].w, w, x.o.w);
+        }
     }
     return x;
 }
 // A merged row as the call's result.
 template <int D>
-__device__ __forceinline__ void put_row(const Q4AttnParams &p, size_t row, float top, float total, const float4 &o, int flag) {
+__device__ __forceinline__ void put_row(const Q4AttnParams &p, size_t row, const Row &x, int flag) {
     const int lane = threadIdx.x & 31;
-    const float inv = total == 0.f ? 0.f : 1.f / total;   // (a row that sees nothing: zeros)
+    const float inv = x.total == 0.f ? 0.f : 1.f / x.total;   // (a row that sees nothing: zeros)
     if (lane * 4 < D)
-        *reinterpret_cast<uint2 *>(p.out + row * D + lane * 4) = flag ? make_uint2(0u, 0u) : make_uint2(pack(o.x * inv, o.y * inv), pack(o.z * inv, o.w * inv));
-    if (p.lse && lane == 0) p.lse[row] = flag ? 0.f : fmaf(top, p.scale, log2f(total) * 0.6931471805599453f);
+        *reinterpret_cast<uint2 *>(p.out + row * D + lane * 4) = flag ? make_uint2(0u, 0u) : make_uint2(pack(x.o.x * inv, x.o.y * inv), pack(x.o.z * inv, x.o.w * inv));
+    if (p.lse && lane == 0) p.lse[row] = flag ? 0.f : fmaf(x.top, p.scale, log2f(x.total) * 0.6931471805599453f);
 }
 
-// (Not inlined: its registers are not those of a worker's loop.)  Merges the shares in slots `first`, then base + 2 apart k for
-// k = 1 .. count - 1, into the result or into slot `first`.
-template <int D, int NT>
-__device__ __noinline__ void merge(const Q4AttnParams &p, int b, int h, int rt, int first, int base, int apart, int count, bool final) {
-    constexpr int kRows = Shape<NT>::kRows;
+// A row as a share in the workspace.
+template <int D>
+__device__ __forceinline__ void keep_row(const Q4AttnParams &p, size_t row, const Row &x) {
     const int lane = threadIdx.x & 31;
-    auto slot_of = [&](int k) { return k == 0 ? first : base + 2 * apart * k; };
-    int flag = lane < count ? __ldcg(p.flags + slot_of(lane)) : 0;
-    flag = __reduce_or_sync(0xffffffffu, flag);
-    const int live = live_rows<NT>(p, rt);
-    if (final) note(p, b, flag, lane);
-#pragma unroll 1
-    for (int r0 = 0; r0 < live; r0 += kRowsAtOnce) {
-        float2 ml[kRowsAtOnce];
-#pragma unroll
-        for (int i = 0; i < kRowsAtOnce; ++i) {
-            ml[i] = make_float2(-INFINITY, 0.f);
-            if (lane < count && r0 + i < live) ml[i] = __ldcg(p.partial_ml + slot_of(lane) * kRows + r0 + i);
-        }
-        const Merged x = merge_rows<D, true>(ml, count, live - r0, p.scale_log2,
-                                             [&](int k, int i) { return p.partial_o + ((size_t)slot_of(k) * kRows + r0 + i) * D; });
-#pragma unroll
-        for (int i = 0; i < kRowsAtOnce; ++i) {
-            const int r = r0 + i;
-            if (r >= live) continue;
-            if (final) {
-                put_row<D>(p, out_row<NT>(p, b, h, rt, r), x.top[i], x.total[i], x.o[i], flag);
-            } else {
-                if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + ((size_t)first * kRows + r) * D + lane * 4) = x.o[i];
-                if (lane == 0) p.partial_ml[first * kRows + r] = make_float2(x.top[i], x.total[i]);
-            }
-        }
-    }
-    if (!final) {
-        __syncwarp();
-        if (lane == 0) p.flags[first] = flag;
-    }
+    if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + row * D + lane * 4) = x.o;
+    if (lane == 0) p.partial_ml[row] = make_float2(x.top, x.total);
 }
 
 // ---- one worker
@@ -827,42 +806,21 @@ struct Worker {
                 if (g == 0) ml[r] = make_float2(m[nt][e], l[nt][e]);
             }
     }
-    // Whether this warp is the last of `count` to arrive; what the others wrote before is visible to it.
-    __device__ __forceinline__ bool last_to_arrive(int32_t *counter, int count) {
-        __threadfence();
-        __syncwarp();
-        int before = 0;
-        if (lane == 0) before = atomicAdd(counter, 1);
-        before = __shfl_sync(0xffffffffu, before, 0);
-        if (before != count - 1) return false;
-        __threadfence();
-        return true;
-    }
-    __device__ __forceinline__ void finish(const Unit &u, const List &list, int worker, int flag) {
+    // What becomes of a unit when its tiles in this range are done: it is whole, or there is a share (in the worker's ring if the range
+    // ends with it, else in the workspace) and, from the first of the block's workers that has one, a task.
+    __device__ __forceinline__ void finish(const Unit &u, const List &list, int worker, int warp, bool at_end, float *own, float2 *own_ml, Task *tasks, int flag) {
         sum_up();
         if (u.t0 == 0 && u.t1 == u.ntiles) {
             write_rows(u, flag);
             return;
         }
-        // the unit's shares belong to the workers c0 .. c1; a worker's slots: 2 c + 1 for a unit that it begins, else 2 c
-        const int c0 = list.worker_of(u.w0 + kUnitCost), c1 = list.worker_of(u.w0 + kUnitCost + u.ntiles - 1);
-        const int slot = 2 * worker + (u.t0 == 0 ? 1 : 0);
-        write_share(u, p.partial_o + (size_t)slot * S::kRows * D, p.partial_ml + slot * S::kRows);
-        if (lane == 0) p.flags[slot] = flag;
-        // up to kOneLevel shares: one group; more: about as many groups as shares in a group
-        const int shares = c1 - c0 + 1;
-        int size = shares;
-        if (shares > kOneLevel) {
-            size = 4;
-            while (size * size < shares) ++size;
-        }
-        const int groups = (shares + size - 1) / size, group = (worker - c0) / size, lead = c0 + group * size;
-        const int lead_slot = 2 * lead + (group == 0 ? 1 : 0), members = min(size, c1 - lead + 1);
-        if (!last_to_arrive(p.counters + lead_slot, members)) return;
-        merge<D, NT>(p, u.b, u.h, u.rt, lead_slot, 2 * lead, 1, members, groups == 1);
-        if (groups == 1) return;
-        if (!last_to_arrive(p.counters + 2 * (p.n_ctas * S::kWarps) + 2 * c0 + 1, groups)) return;
-        merge<D, NT>(p, u.b, u.h, u.rt, 2 * c0 + 1, 2 * c0, size, groups, true);
+        if (at_end) write_share(u, own, own_ml);
+        else write_share(u, p.partial_o + (size_t)worker * S::kRows * D, p.partial_ml + worker * S::kRows);
+        if (u.t0 != 0 && warp != 0) return;
+        // the unit's shares belong to the workers c0 .. c1
+        const int c0 = u.t0 == 0 ? worker : list.worker_of(u.w0 + kUnitCost), c1 = list.worker_of(u.w0 + kUnitCost + u.ntiles - 1);
+        if (lane == 0)
+            tasks[u.t0 == 0 ? warp : S::kWarps] = Task{u.b, u.h, u.rt, warp, min(c1 - (int)blockIdx.x * list.per_block, list.per_block - 1), u.t0 == 0, c0 / list.per_block, c1 / list.per_block};
     }
     // The block does not end under its own copies.
     __device__ __forceinline__ void drain() {
@@ -890,7 +848,6 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     using S = Shape<NT>;
     using C = Cfg<D, NT>;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int32_t *prefix = reinterpret_cast<int32_t *>(smem + C::kOffPrefix);
     Worker<D, NT> k(p);
     k.init(smem, warp);
     pdl_wait();
@@ -901,44 +858,53 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     list.per_seq = p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows);
     list.tree_tiles = (p.T + kPage - 1) / kPage;
     list.step = (p.B + kPrefix - 1) / kPrefix;
-    __shared__ int warp_sum[S::kWarps];
-    int carry = 0, longest = 0;
-    for (int b0 = 0; b0 < p.B; b0 += S::kThreads) {
-        const int b = b0 + tid;
-        const int L = b < p.B ? p.seq_lens[b] : 0;
-        const int e = b < p.B ? entries_of(p, list, L) : 0;
-        longest = max(longest, e);
+    Seqs seqs;
+    int2 *table = reinterpret_cast<int2 *>(smem + C::kOffPrefix);
+    seqs.table = table;
+    seqs.start = INT_MAX;
+    seqs.L = 0;
+    int carry = 0;
+    if (p.B <= 32) {   // every warp by itself
+        const int L = lane < p.B ? p.seq_lens[lane] : -1, e = lane < p.B ? entries_of(p, list, L) : 0;
         int incl = e;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int t = __shfl_up_sync(0xffffffffu, incl, d);
             if (lane >= d) incl += t;
         }
-        __syncthreads();
-        if (lane == 31) warp_sum[warp] = incl;
-        __syncthreads();
-        int before = 0, all = 0;
+        if (lane < p.B) seqs.start = incl - e;
+        seqs.L = L;
+        carry = __shfl_sync(0xffffffffu, incl, 31);
+    } else {
+        __shared__ int warp_sum[S::kWarps];
+        for (int b0 = 0; b0 < p.B; b0 += S::kThreads) {
+            const int b = b0 + tid;
+            const int L = b < p.B ? p.seq_lens[b] : 0;
+            const int e = b < p.B ? entries_of(p, list, L) : 0;
+            int incl = e;
 #pragma unroll
-        for (int i = 0; i < S::kWarps; ++i) {
-            const int x = warp_sum[i];
-            before += i < warp ? x : 0;
-            all += x;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int t = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += t;
+            }
+            __syncthreads();
+            if (lane == 31) warp_sum[warp] = incl;
+            __syncthreads();
+            int before = 0, all = 0;
+#pragma unroll
+            for (int i = 0; i < S::kWarps; ++i) {
+                const int x = warp_sum[i];
+                before += i < warp ? x : 0;
+                all += x;
+            }
+            if (b < p.B && b % list.step == 0) table[b / list.step] = make_int2(carry + before + incl - e, L);
+            carry += all;
         }
-        if (b < p.B && b % list.step == 0) prefix[b / list.step] = carry + before + incl - e;
-        carry += all;
     }
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    __syncthreads();
-    if (lane == 0) warp_sum[warp] = longest;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < S::kWarps; ++i) longest = max(longest, warp_sum[i]);
     list.W = carry;
-    list.n_workers = max(1, min(p.n_ctas * S::kWarps, list.W / kMinEntries));
-    // two levels of merging hold 32 x 32 shares of a unit
-    longest /= list.per_seq;
-    if ((int64_t)longest * list.n_workers > (int64_t)(kMaxShares - 2) * list.W)
-        list.n_workers = max(1, (int)((int64_t)(kMaxShares - 2) * list.W / longest));
+    // fewer workers when there is little to do, spread over the thread blocks
+    list.per_block = max(1, min(S::kWarps, list.W / (kMinEntries * p.n_ctas)));
+    list.n_workers = list.per_block * max(1, min(p.n_ctas, list.W / (kMinEntries * list.per_block)));
 
     // a sequence whose length cannot be: zero rows, from one warp
     for (int b = blockIdx.x * S::kWarps + warp; b < p.B; b += p.n_ctas * S::kWarps) {
@@ -952,50 +918,124 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
             for (size_t i = lane; i < rows; i += 32) p.lse[(size_t)b * rows + i] = 0.f;
     }
 
-    // neighbouring ranges go to different SMs, so that few of them are spread over the GPU
-    const int worker = warp * p.n_ctas + blockIdx.x;
-    if (worker >= list.n_workers || list.W == 0) return;
-    int w = list.begin(worker);
-    const int w_end = list.begin(worker + 1);
-    const uint64_t policy = l2_policy_evict_first();
-    const bool once = list.per_seq == p.Hkv;   // no other unit reads these pages
-    unsigned char *parents = smem + C::kOffParents + warp * kMaxNodes;
-    uint64_t *masks = reinterpret_cast<uint64_t *>(smem + C::kOffMasks) + warp * S::kRows * 2;
-
-    Unit u;
-    u.any = false;
-    int flag = 0, pages_end = 0;
-    for (;;) {
-        // The next unit's first tiles are on their way before this one's results are written.
-        Unit coming;
-        int coming_flag = 0, coming_end = 0;
-        coming.any = false;
-        while (w < w_end && !coming.any) {
-            coming = unit_at(p, list, prefix, w, w_end, lane);
-            w += coming.entries;
-        }
-        if (coming.any && !k.gave_up) {
-            coming_end = min(coming.npages, coming.t1);
-            if (p.num_pages == 0 && coming.t0 < coming_end) {   // no pool to read from
-                coming_flag |= kBadPage;
-                coming_end = coming.t0;
+    __shared__ Task tasks[S::kWarps + 1];   // of the units that the workers begin, and of the one that the block's first continues
+    __shared__ int16_t segments[S::kWarps], first_flag[S::kWarps], end_flag[S::kWarps];   // units in a worker's range; what is wrong with its shares
+    __shared__ int last[2];
+    if (tid <= S::kWarps) tasks[tid].first = -1;
+    if (tid < 2) last[tid] = 0;
+    if (lane == 0) segments[warp] = first_flag[warp] = end_flag[warp] = 0;
+    __syncthreads();
+    float *own = reinterpret_cast<float *>(smem + warp * C::kRingBytes);
+    float2 *ml_all = reinterpret_cast<float2 *>(smem + C::kOffShares);
+    const int worker = blockIdx.x * list.per_block + warp;
+    if (warp < list.per_block && worker < list.n_workers && list.W > 0) {
+        int w = list.begin(worker);
+        const int w_end = list.begin(worker + 1);
+        const uint64_t policy = l2_policy_evict_first();
+        const bool once = list.per_seq == p.Hkv;   // no other unit reads these pages
+        unsigned char *parents = smem + C::kOffParents + warp * kMaxNodes;
+        uint64_t *masks = reinterpret_cast<uint64_t *>(smem + C::kOffMasks) + warp * S::kRows * 2;
+        Unit u;
+        u.any = false;
+        int flag = 0, pages_end = 0;
+        for (;;) {
+            // The next unit's first tiles are on their way before this one's results are written.
+            Unit coming;
+            int coming_flag = 0, coming_end = 0;
+            coming.any = false;
+            while (w < w_end && !coming.any) {
+                coming = unit_at(p, list, seqs, w, w_end, lane);
+                w += coming.entries;
             }
-            k.start(coming, coming_end, policy, once, coming_flag);
+            if (coming.any && !k.gave_up) {
+                coming_end = min(coming.npages, coming.t1);
+                if (p.num_pages == 0 && coming.t0 < coming_end) {   // no pool to read from
+                    coming_flag |= kBadPage;
+                    coming_end = coming.t0;
+                }
+                k.start(coming, coming_end, policy, once, coming_flag);
+            }
+            if (u.any) {
+                k.finish(u, list, worker, warp, !coming.any, own, ml_all + warp * S::kRows, tasks, flag);
+                if (lane == 0) {
+                    if (segments[warp]++ == 0) first_flag[warp] = (int16_t)flag;
+                    end_flag[warp] = (int16_t)flag;
+                }
+            }
+            if (!coming.any) break;
+            u = coming;
+            flag = coming_flag;
+            pages_end = coming_end;
+            k.begin(u);
+            // (the tree first: its rows come while the first tiles are on their way)
+            const int n0 = max(0, u.t0 - u.npages) * kPage, n1 = min(p.T, (u.t1 - u.npages) * kPage);
+            if (n1 > n0) k.tree(u, n0, n1, parents, masks, flag);
+            if (!k.gave_up) k.walk(u, pages_end, policy, once, flag);
+            flag = __reduce_or_sync(0xffffffffu, flag);
+            if (k.gave_up || worker == p.give_up) flag |= kGaveUp;   // (the rest of the range is given up with the unit)
         }
-        if (u.any) k.finish(u, list, worker, flag);
-        if (!coming.any) break;
-        u = coming;
-        flag = coming_flag;
-        pages_end = coming_end;
-        k.begin(u);
-        // (the tree first: its rows come while the first tiles are on their way)
-        const int n0 = max(0, u.t0 - u.npages) * kPage, n1 = min(p.T, (u.t1 - u.npages) * kPage);
-        if (n1 > n0) k.tree(u, n0, n1, parents, masks, flag);
-        if (!k.gave_up) k.walk(u, pages_end, policy, once, flag);
-        flag = __reduce_or_sync(0xffffffffu, flag);
-        if (k.gave_up || worker == p.give_up) flag |= kGaveUp;   // (the rest of the range is given up with the unit)
+        k.drain();
     }
-    k.drain();
+    __syncthreads();
+
+    // The block's shares, a row of a unit to a warp at a time.
+    const int block_shares = p.n_ctas * S::kWarps;   // shares of blocks stand behind those of workers: 2 x block, + 1 for a unit that it begins
+#pragma unroll 1
+    for (int job = warp; job < (S::kWarps + 1) * S::kRows; job += S::kWarps) {
+        const Task t = tasks[job / S::kRows];
+        const int r = job % S::kRows;
+        if (t.first < 0 || r >= live_rows<NT>(p, t.rt)) continue;
+        // worker i's share is that of its last unit if it begins the unit, else that of its first
+        auto in_ring = [&](int i) { return (i == t.first && t.begins) || segments[i] == 1; };
+        auto at = [&](int k) {
+            const int i = t.first + k;
+            return in_ring(i) ? reinterpret_cast<const float *>(smem + i * C::kRingBytes) + r * D
+                              : p.partial_o + ((size_t)(blockIdx.x * list.per_block + i) * S::kRows + r) * D;
+        };
+        auto ml = [&](int k) {
+            const int i = t.first + k;
+            return in_ring(i) ? ml_all[i * S::kRows + r] : p.partial_ml[(blockIdx.x * list.per_block + i) * S::kRows + r];
+        };
+        int flag = 0;
+        if (lane <= t.last - t.first) flag = lane == 0 && t.begins ? end_flag[t.first] : first_flag[t.first + lane];
+        flag = __reduce_or_sync(0xffffffffu, flag);
+        const Row x = merge_row<D>(t.last - t.first + 1, p.scale_log2, ml, at);
+        if (t.block0 == t.block1) {
+            if (r == 0) note(p, t.b, flag, lane);
+            put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
+        } else {
+            const int slot = 2 * blockIdx.x + t.begins;
+            keep_row<D>(p, (size_t)(block_shares + slot) * S::kRows + r, x);
+            if (r == 0 && lane == 0) p.flags[slot] = flag;
+        }
+    }
+    __syncthreads();
+    // A unit that other blocks have shares of, too: at most one that goes on from the block before, one that goes on in the next.
+    if (tid <= S::kWarps && tasks[tid].first >= 0 && tasks[tid].block0 != tasks[tid].block1) {
+        __threadfence();
+        if (atomicAdd(p.counters + tasks[tid].block0, 1) == tasks[tid].block1 - tasks[tid].block0) {
+            __threadfence();
+            last[tasks[tid].begins] = tid + 1;
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+        if (last[i] == 0) continue;
+        const Task t = tasks[last[i] - 1];
+        const int count = t.block1 - t.block0 + 1;
+        auto slot = [&](int k) { return 2 * (t.block0 + k) + (k == 0 ? 1 : 0); };
+        int flag = 0;
+        for (int k = lane; k < count; k += 32) flag |= __ldcg(p.flags + slot(k));
+        flag = __reduce_or_sync(0xffffffffu, flag);
+        if (warp == 0) note(p, t.b, flag, lane);
+        for (int r = warp; r < live_rows<NT>(p, t.rt); r += S::kWarps) {
+            const Row x = merge_row<D>(
+                count, p.scale_log2, [&](int k) { return __ldcg(p.partial_ml + (size_t)(block_shares + slot(k)) * S::kRows + r); },
+                [&](int k) { return p.partial_o + ((size_t)(block_shares + slot(k)) * S::kRows + r) * D; });
+            put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
+        }
+    }
 }
 
 // The other form: a cluster of thread blocks per sequence, p.split of them for each of its units.
@@ -1056,24 +1096,15 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
     if (flag && lane == 0) atomicOr(&flags, flag);
     __syncthreads();
     const int live = live_rows<NT>(p, u.rt), block_flag = ok ? flags : flags | kBadLength;
-    // the block's shares, four rows to a warp
-    for (int r0 = warp * kRowsAtOnce; r0 < live; r0 += S::kWarps * kRowsAtOnce) {
-        float2 ml[kRowsAtOnce];
-#pragma unroll
-        for (int i = 0; i < kRowsAtOnce; ++i) ml[i] = lane < S::kWarps && r0 + i < live ? ml_all[lane * S::kRows + r0 + i] : make_float2(-INFINITY, 0.f);
-        const Merged x = merge_rows<D, false>(ml, S::kWarps, live - r0, p.scale_log2, [&](int w, int i) {
-            return reinterpret_cast<const float *>(smem + w * C::kRingBytes) + (r0 + i) * D;
-        });
-#pragma unroll
-        for (int i = 0; i < kRowsAtOnce; ++i) {
-            const int r = r0 + i;
-            if (r >= live) continue;
-            if (p.split == 1) {
-                put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r), x.top[i], x.total[i], x.o[i], block_flag);
-            } else {
-                if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + ((size_t)blockIdx.x * S::kRows + r) * D + lane * 4) = x.o[i];
-                if (lane == 0) p.partial_ml[blockIdx.x * S::kRows + r] = make_float2(x.top[i], x.total[i]);
-            }
+    // the block's shares, a row to a warp
+    for (int r = warp; r < live; r += S::kWarps) {
+        const Row x = merge_row<D>(
+            S::kWarps, p.scale_log2, [&](int w) { return ml_all[w * S::kRows + r]; },
+            [&](int w) { return reinterpret_cast<const float *>(smem + w * C::kRingBytes) + r * D; });
+        if (p.split == 1) {
+            put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r), x, block_flag);
+        } else {
+            keep_row<D>(p, (size_t)blockIdx.x * S::kRows + r, x);
         }
     }
     if (tid == 0) p.flags[blockIdx.x] = block_flag;
@@ -1085,28 +1116,22 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
         if (lane == 0) p.status[u.b] = code_of_flag(all);
     }
     if (p.split == 1) return;
-    // the shares of the unit's blocks, four rows to a warp of them
+    // the shares of the unit's blocks, a row to a warp of them
     const int first = block0 + unit * p.split, unit_flag = __reduce_or_sync(0xffffffffu, lane < p.split ? __ldcg(p.flags + first + lane) : 0);
-    for (int r0 = (warp * p.split + piece) * kRowsAtOnce; r0 < live; r0 += workers * kRowsAtOnce) {
-        float2 ml[kRowsAtOnce];
-#pragma unroll
-        for (int i = 0; i < kRowsAtOnce; ++i)
-            ml[i] = lane < p.split && r0 + i < live ? __ldcg(p.partial_ml + (first + lane) * S::kRows + r0 + i) : make_float2(-INFINITY, 0.f);
-        const Merged x = merge_rows<D, true>(ml, p.split, live - r0, p.scale_log2,
-                                             [&](int w, int i) { return p.partial_o + ((size_t)(first + w) * S::kRows + r0 + i) * D; });
-#pragma unroll
-        for (int i = 0; i < kRowsAtOnce; ++i)
-            if (r0 + i < live) put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r0 + i), x.top[i], x.total[i], x.o[i], unit_flag);
+    for (int r = warp * p.split + piece; r < live; r += workers) {
+        const Row x = merge_row<D>(
+            p.split, p.scale_log2, [&](int w) { return __ldcg(p.partial_ml + (first + w) * S::kRows + r); },
+            [&](int w) { return p.partial_o + ((size_t)(first + w) * S::kRows + r) * D; });
+        put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r), x, unit_flag);
     }
 }
 
 // Zeroes what the call counts in.
-__global__ void __launch_bounds__(1024) q4_attn_zero_kernel(int4 *counters, int n, int32_t *status, int B) {
+__global__ void __launch_bounds__(1024) q4_attn_zero_kernel(int32_t *counters, int n, int32_t *status, int B) {
     pdl_launch_dependents();   // the attention may be set up meanwhile; it waits for this kernel's end
     pdl_wait();
-    const int i = blockIdx.x * 1024 + threadIdx.x;
-    if (i < n) counters[i] = make_int4(0, 0, 0, 0);
-    for (int b = i; b < B; b += gridDim.x * 1024) status[b] = READER_OK;
+    for (int i = threadIdx.x; i < n; i += 1024) counters[i] = 0;
+    for (int b = threadIdx.x; b < B; b += 1024) status[b] = READER_OK;
 }
 
 constexpr int kAloneTiles = 6;
@@ -1154,8 +1179,7 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
         }
     }
     p.n_ctas = n_sm;
-    const int words = n_sm * S::kWarps;   // 4 counters a worker
-    launch_pdl(q4_attn_zero_kernel, dim3((unsigned)((words + 1023) / 1024)), dim3(1024), 0, st, reinterpret_cast<int4 *>(p.counters), words, p.status, p.B);
+    launch_pdl(q4_attn_zero_kernel, dim3(1), dim3(1024), 0, st, p.counters, n_sm, p.status, p.B);
     launch_pdl(q4_attn_list_kernel<D, NT>, dim3((unsigned)n_sm), dim3(S::kThreads), (size_t)C::kSmem, st, p);
     return READER_OK;
 }
