@@ -550,7 +550,8 @@ size_t reader_q4_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  *   workspace  at least reader_q4_workspace_bytes(...) bytes, 256-byte aligned; contents are scratch, calls that share it must
  *              not overlap on the GPU
  *   status_out READER_ERR_TIMEOUT besides (rows of that sequence may also hold their values)
- * READER_ERR_UNSUPPORTED unless: softmax_scale > 0 and at most 2e38; n_q_heads a multiple of n_kv_heads; batch at most 65536; and batch *
+ * READER_ERR_UNSUPPORTED unless: softmax_scale > 0 and at most 2e38; n_q_heads a multiple of n_kv_heads, at most 4096
+ * times it; batch at most 65536; and batch *
  * n_kv_heads * (n_nodes * n_q_heads / n_kv_heads / 16 + 1) * (max_pages_per_seq + 4) below 2^31.
  * Bytes at positions that are not committed have no influence, whatever they are.  A row that sees nothing (an anc_mask without the
  * node itself, on an empty cache) is zero, its lse -inf.

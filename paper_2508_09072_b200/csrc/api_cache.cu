@@ -237,7 +237,8 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
         reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
         return READER_ERR_INVALID_ARG;
     // the row maximum is taken before the scaling, so the scale has to be positive
-    if (!(softmax_scale > 0.f) || softmax_scale > 2.0e38f || Hq % Hkv != 0 || B > kQ4MaxBatch) return READER_ERR_UNSUPPORTED;
+    if (!(softmax_scale > 0.f) || softmax_scale > 2.0e38f || Hq % Hkv != 0 || Hq / Hkv > kQ4MaxGroup || B > kQ4MaxBatch)
+        return READER_ERR_UNSUPPORTED;
     const int64_t units = (int64_t)B * Hkv * ((int64_t)T * (Hq / Hkv) / 16 + 1);
     if (units * ((int64_t)cache->max_pages_per_seq + 4) >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
     const Q4Ws w = q4_ws(ctx, D);

@@ -7,6 +7,7 @@ namespace reader {
 // Rows of the shares of a thread block's workers and of its own two, at most (few-rows kernels).
 constexpr int kQ4ShareRows = 192 + 32;
 constexpr int kQ4MaxBatch = 1 << 16;
+constexpr int kQ4MaxGroup = 1 << 12;   // (128 nodes: 128 G^2 < 2^32, as the division by G wants it)
 
 struct Q4AttnParams {
     const __nv_bfloat16 *q, *k_tree, *v_tree;
@@ -25,6 +26,8 @@ struct Q4AttnParams {
     int32_t *flags;            // [2 * thread blocks] what is wrong with a block's shares
     float2 *partial_ml;        // [shares][rows] largest score, sum: of workers, behind them of blocks
     float *partial_o;          // [shares][rows][D]
+    int n_rt;                  // units of a KV head
+    unsigned inv_G;            // 2^32 / G, rounded up
     int n_ctas;                // thread blocks (list form)
     int split;                 // thread blocks of a unit (alone)
 };

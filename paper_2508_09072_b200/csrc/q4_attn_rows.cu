@@ -150,14 +150,12 @@ struct Unit {
 
 struct List {
     int W, n_workers, per_block, per_seq, tree_tiles, step;   // step: sequences per entry of the prefix table
-    __device__ __forceinline__ int begin(int worker) const { return mul_div(worker, W, n_workers); }
+    int each, more;   // entries of a range; the first `more` ranges have one more
+    __device__ __forceinline__ int begin(int worker) const { return worker * each + min(worker, more); }
     // the worker whose range holds entry w
     __device__ __forceinline__ int worker_of(int w) const {
-        int c = (int)((float)w * (float)n_workers / (float)W);
-        c = max(0, min(c, n_workers - 1));
-        while (c + 1 < n_workers && begin(c + 1) <= w) ++c;
-        while (c > 0 && begin(c) > w) --c;
-        return c;
+        const int longer = more * (each + 1);
+        return w < longer ? w / (each + 1) : more + (w - longer) / each;
     }
 };
 // A unit whose shares a thread block merges: those of its workers first .. last (first < 0: none); whether the first of them begins it;
@@ -224,8 +222,8 @@ __device__ __forceinline__ Unit unit_at(const Q4AttnParams &p, const List &l, co
     u.npages = (u.L + kPage - 1) / kPage;
     u.ntiles = u.npages + l.tree_tiles;
     const int per_unit = u.ntiles + kUnitCost, local = w - start, unit = local / per_unit, pos = local - unit * per_unit;
-    const int n_rt = l.per_seq / p.Hkv;
-    u.h = unit / n_rt;
+    const int n_rt = p.n_rt;
+    u.h = n_rt == 1 ? unit : unit / n_rt;
     u.rt = unit - u.h * n_rt;
     const int pos_end = min(per_unit, pos + (w_end - w));
     u.entries = pos_end - pos;
@@ -237,9 +235,11 @@ __device__ __forceinline__ Unit unit_at(const Q4AttnParams &p, const List &l, co
 }
 
 // ---- rows of a unit
+// row / G (the host has checked that row * G < 2^32)
+__device__ __forceinline__ int node_of(const Q4AttnParams &p, int row) { return p.G == 1 ? row : (int)__umulhi((unsigned)row, p.inv_G); }
 template <int NT>
 __device__ __forceinline__ size_t out_row(const Q4AttnParams &p, int b, int h, int rt, int r) {
-    const int row = rt * Shape<NT>::kRows + r, j = row / p.G;
+    const int row = rt * Shape<NT>::kRows + r, j = node_of(p, row);
     return ((size_t)b * p.T + j) * p.Hq + h * p.G + (row - j * p.G);
 }
 template <int NT>
@@ -312,6 +312,47 @@ __device__ __forceinline__ void keep_row(const Q4AttnParams &p, size_t row, cons
     const int lane = threadIdx.x & 31;
     if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + row * D + lane * 4) = x.o;
     if (lane == 0) p.partial_ml[row] = make_float2(x.top, x.total);
+}
+
+// Row r of a unit.  kOfWorkers: from the shares of the block's workers, into the result or, if other blocks have shares too, as the
+// block's share into the workspace; kOfBlocks: from the blocks' shares into the result.
+enum MergeMode { kOfWorkers, kOfBlocks };
+struct Shares {   // of a block's workers
+    const int16_t *segments, *first_flag, *end_flag;   // units in a worker's range; what is wrong with its first and its last share
+};
+template <int D, int NT>
+__device__ __forceinline__ void merge_one(const Q4AttnParams &p, unsigned char *smem, const Shares &s, const Task &t, int per_block, int r, MergeMode mode) {
+    using C = Cfg<D, NT>;
+    constexpr int kRows = Shape<NT>::kRows;
+    const int lane = threadIdx.x & 31;
+    const float2 *ml_all = reinterpret_cast<const float2 *>(smem + C::kOffShares);
+    const int of_blocks = p.n_ctas * Shape<NT>::kWarps;   // shares of blocks stand behind those of workers: 2 x block, + 1 for a unit that it begins
+    const int count = mode == kOfBlocks ? t.block1 - t.block0 + 1 : t.last - t.first + 1;
+    auto block_slot = [&](int k) { return 2 * (t.block0 + k) + (k == 0 ? 1 : 0); };
+    // worker i's share is that of its last unit if it begins the unit, else that of its first; it stands in its ring if its range ends with it
+    auto in_ring = [&](int i) { return (i == t.first && t.begins) || s.segments[i] <= 1; };
+    auto row_of = [&](int k) {   // row of the workspace's arrays
+        return (size_t)(mode == kOfBlocks ? of_blocks + block_slot(k) : (int)blockIdx.x * per_block + t.first + k) * kRows + r;
+    };
+    auto at = [&](int k) {
+        return mode != kOfBlocks && in_ring(t.first + k) ? reinterpret_cast<const float *>(smem + (t.first + k) * C::kRingBytes) + r * D : p.partial_o + row_of(k) * D;
+    };
+    auto ml = [&](int k) {
+        return mode != kOfBlocks && in_ring(t.first + k) ? ml_all[(t.first + k) * kRows + r] : __ldcg(p.partial_ml + row_of(k));
+    };
+    int flag = 0;
+    for (int k = lane; k < count; k += 32)
+        flag |= mode == kOfBlocks ? __ldcg(p.flags + block_slot(k)) : k == 0 && t.begins ? s.end_flag[t.first] : s.first_flag[t.first + k];
+    flag = __reduce_or_sync(0xffffffffu, flag);
+    const Row x = merge_row<D>(count, p.scale_log2, ml, at);
+    if (mode == kOfBlocks || t.block0 == t.block1) {
+        if (r == 0) note(p, t.b, flag, lane);
+        put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
+    } else {
+        const int slot = 2 * blockIdx.x + t.begins;
+        keep_row<D>(p, (size_t)(of_blocks + slot) * kRows + r, x);
+        if (r == 0 && lane == 0) p.flags[slot] = flag;
+    }
 }
 
 // ---- one worker
@@ -391,7 +432,7 @@ struct Worker {
         ids_at = u.t0;
         t_issue = 2 * u.t0;
         ids = page_ids(u, u.t0, flag);
-        ids_next = page_ids(u, u.t0 + 32, flag);
+        ids_next = pages_end - u.t0 > 32 ? page_ids(u, u.t0 + 32, flag) : 0;
 #pragma unroll 1
         for (int i = 0; i < S::kSlots && t_issue < 2 * pages_end; ++i) issue(u, policy, once, flag);
     }
@@ -421,7 +462,7 @@ struct Worker {
         for (int nt = 0; nt < NT; ++nt) {
             const int r = u.rt * S::kRows + 8 * nt + g;
             const bool live = r < p.T * p.G;
-            const int j = live ? r / p.G : 0, hq = u.h * p.G + (live ? r - j * p.G : 0);
+            const int j = live ? node_of(p, r) : 0, hq = u.h * p.G + (live ? r - j * p.G : 0);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (((size_t)u.b * p.T + j) * p.Hq + hq) * D + c * (D / 4));
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) {
@@ -688,7 +729,7 @@ struct Worker {
             const int r = u.rt * S::kRows + lane;
             uint64_t lo = 0, hi = 0;
             if (r < p.T * p.G) {
-                const int j = r / p.G;
+                const int j = node_of(p, r);
                 if (p.anc) {
                     lo = p.anc[((size_t)u.b * p.T + j) * 2];
                     hi = p.anc[((size_t)u.b * p.T + j) * 2 + 1];
@@ -855,7 +896,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
 
     // the list: prefix sums over the sequences
     List list;
-    list.per_seq = p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows);
+    list.per_seq = p.Hkv * p.n_rt;
     list.tree_tiles = (p.T + kPage - 1) / kPage;
     list.step = (p.B + kPrefix - 1) / kPrefix;
     Seqs seqs;
@@ -905,6 +946,8 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     // fewer workers when there is little to do, spread over the thread blocks
     list.per_block = max(1, min(S::kWarps, list.W / (kMinEntries * p.n_ctas)));
     list.n_workers = list.per_block * max(1, min(p.n_ctas, list.W / (kMinEntries * list.per_block)));
+    list.each = list.W / list.n_workers;
+    list.more = list.W - list.each * list.n_workers;
 
     // a sequence whose length cannot be: zero rows, from one warp
     for (int b = blockIdx.x * S::kWarps + warp; b < p.B; b += p.n_ctas * S::kWarps) {
@@ -925,6 +968,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     if (tid < 2) last[tid] = 0;
     if (lane == 0) segments[warp] = first_flag[warp] = end_flag[warp] = 0;
     __syncthreads();
+    const Shares shares = {segments, first_flag, end_flag};
     float *own = reinterpret_cast<float *>(smem + warp * C::kRingBytes);
     float2 *ml_all = reinterpret_cast<float2 *>(smem + C::kOffShares);
     const int worker = blockIdx.x * list.per_block + warp;
@@ -978,63 +1022,29 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     }
     __syncthreads();
 
-    // The block's shares, a row of a unit to a warp at a time.
-    const int block_shares = p.n_ctas * S::kWarps;   // shares of blocks stand behind those of workers: 2 x block, + 1 for a unit that it begins
+    // The block's shares, then, of a unit that other blocks have shares of, too (at most one that goes on from the block before, one that goes
+    // on in the next), the blocks': a row of a unit to a warp at a time.  (One loop for both: the code is there the second time.)
+    const int rows = min(S::kRows, p.T * p.G);   // of a unit, at most
 #pragma unroll 1
-    for (int job = warp; job < (S::kWarps + 1) * S::kRows; job += S::kWarps) {
-        const Task t = tasks[job / S::kRows];
-        const int r = job % S::kRows;
-        if (t.first < 0 || r >= live_rows<NT>(p, t.rt)) continue;
-        // worker i's share is that of its last unit if it begins the unit, else that of its first
-        auto in_ring = [&](int i) { return (i == t.first && t.begins) || segments[i] == 1; };
-        auto at = [&](int k) {
-            const int i = t.first + k;
-            return in_ring(i) ? reinterpret_cast<const float *>(smem + i * C::kRingBytes) + r * D
-                              : p.partial_o + ((size_t)(blockIdx.x * list.per_block + i) * S::kRows + r) * D;
-        };
-        auto ml = [&](int k) {
-            const int i = t.first + k;
-            return in_ring(i) ? ml_all[i * S::kRows + r] : p.partial_ml[(blockIdx.x * list.per_block + i) * S::kRows + r];
-        };
-        int flag = 0;
-        if (lane <= t.last - t.first) flag = lane == 0 && t.begins ? end_flag[t.first] : first_flag[t.first + lane];
-        flag = __reduce_or_sync(0xffffffffu, flag);
-        const Row x = merge_row<D>(t.last - t.first + 1, p.scale_log2, ml, at);
-        if (t.block0 == t.block1) {
-            if (r == 0) note(p, t.b, flag, lane);
-            put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
-        } else {
-            const int slot = 2 * blockIdx.x + t.begins;
-            keep_row<D>(p, (size_t)(block_shares + slot) * S::kRows + r, x);
-            if (r == 0 && lane == 0) p.flags[slot] = flag;
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+        for (int job = warp; job < (S::kWarps + 1) * rows; job += S::kWarps) {
+            const int i = job / rows, r = job - i * rows;
+            const Task t = tasks[i];
+            if (t.first < 0 || r >= live_rows<NT>(p, t.rt) || (pass == 1 && last[t.begins] != i + 1)) continue;
+            merge_one<D, NT>(p, smem, shares, t, list.per_block, r, pass == 0 ? kOfWorkers : kOfBlocks);
         }
-    }
-    __syncthreads();
-    // A unit that other blocks have shares of, too: at most one that goes on from the block before, one that goes on in the next.
-    if (tid <= S::kWarps && tasks[tid].first >= 0 && tasks[tid].block0 != tasks[tid].block1) {
-        __threadfence();
-        if (atomicAdd(p.counters + tasks[tid].block0, 1) == tasks[tid].block1 - tasks[tid].block0) {
+        if (pass == 1) break;
+        __syncthreads();
+        if (tid <= S::kWarps && tasks[tid].first >= 0 && tasks[tid].block0 != tasks[tid].block1) {
             __threadfence();
-            last[tasks[tid].begins] = tid + 1;
+            if (atomicAdd(p.counters + tasks[tid].block0, 1) == tasks[tid].block1 - tasks[tid].block0) {
+                __threadfence();
+                last[tasks[tid].begins] = tid + 1;
+            }
         }
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
-        if (last[i] == 0) continue;
-        const Task t = tasks[last[i] - 1];
-        const int count = t.block1 - t.block0 + 1;
-        auto slot = [&](int k) { return 2 * (t.block0 + k) + (k == 0 ? 1 : 0); };
-        int flag = 0;
-        for (int k = lane; k < count; k += 32) flag |= __ldcg(p.flags + slot(k));
-        flag = __reduce_or_sync(0xffffffffu, flag);
-        if (warp == 0) note(p, t.b, flag, lane);
-        for (int r = warp; r < live_rows<NT>(p, t.rt); r += S::kWarps) {
-            const Row x = merge_row<D>(
-                count, p.scale_log2, [&](int k) { return __ldcg(p.partial_ml + (size_t)(block_shares + slot(k)) * S::kRows + r); },
-                [&](int k) { return p.partial_o + ((size_t)(block_shares + slot(k)) * S::kRows + r) * D; });
-            put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
-        }
+        __syncthreads();
+        if (last[0] == 0 && last[1] == 0) break;
     }
 }
 
@@ -1052,7 +1062,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
     pdl_wait();
     pdl_launch_dependents();
     const int size = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
-    const int n_rt = (p.T * p.G + S::kRows - 1) / S::kRows, unit = rank / p.split, piece = rank - unit * p.split;
+    const int n_rt = p.n_rt, unit = rank / p.split, piece = rank - unit * p.split;
     Unit u;
     u.b = blockIdx.x / size;
     u.h = unit / n_rt;
@@ -1151,7 +1161,9 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
     }
     // Alone: the units of a sequence fit a cluster, the clusters the GPU, and, going by the page table's width, a worker gets at most
     // kAloneTiles tiles.
-    const int units = p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows);
+    p.n_rt = (p.T * p.G + S::kRows - 1) / S::kRows;
+    p.inv_G = (unsigned)((((uint64_t)1 << 32) + p.G - 1) / p.G);
+    const int units = p.Hkv * p.n_rt;
     const int tiles = p.max_pages + (p.T + kPage - 1) / kPage;
     if (units <= kMaxCluster) {
         int split = 1;
