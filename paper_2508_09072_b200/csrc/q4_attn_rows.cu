@@ -24,16 +24,12 @@
 // tree tiles; what is wrong travels with the share and zeroes the unit's rows.  Bytes behind a sequence's end never reach a
 // product: their scores are replaced by -inf and their values' scale by 0.  Every wait is bounded; a worker that gives up says so
 // in its share, waits (bounded) for its copies and goes on without them.
-#include <climits>
-
-#include "ptx_sm100.cuh"
-#include "q4_attn.cuh"
-#include "q4_format.cuh"
+#include "q4_attn_common.cuh"
 
 namespace reader {
 namespace {
 
-using namespace ptx;
+using namespace q4;
 
 // Workers of a thread block, and their ring's slots (a tile of keys or of values each): what registers and shared memory allow.
 template <int NT>
@@ -43,10 +39,6 @@ struct Shape {
 };
 constexpr int kUnitCost = 2;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = kUnitCost + 1;   // of a range: so every one of them holds a tile
-constexpr int kPrefix = 256;       // entries of the prefix table in shared memory
-constexpr float kRaiseBy = 8.f;    // log2 units by which a score may exceed the maximum in use
-constexpr uint64_t kWaitLimitNs = 1000000000ull;
-constexpr int kBadTree = 1, kBadLength = 2, kBadPage = 4, kGaveUp = 8;
 constexpr int kMaxCluster = 16;
 
 template <int D, int NT>
@@ -63,30 +55,6 @@ struct Cfg {
     static_assert(kSmem + 1024 <= 227 * 1024 && kRingBytes >= S::kRows * D * 4, "shared memory");
 };
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy, bool streamed) {
-    if (streamed)
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
-                     "l"(src), "r"(bytes), "r"(bar), "l"(policy)
-                     : "memory");
-    else
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-                     : "memory");
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-    uint4 x;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(a));
-    return x;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-    uint32_t x;
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(a));
-    return x;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-    uint2 x;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(a));
-    return x;
-}
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -98,145 +66,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
-// A pair of scales as bf16 and the pair times -24.
-struct Scale2 {
-    uint32_t s, m24;
-};
-constexpr uint32_t kScaleOne = (uint32_t)((127 - q4::kScaleBias) << 7) * 0x10001u;
-// codes: two of them, in bits 0-7 and 16-23
-template <bool kWhole>
-__device__ __forceinline__ Scale2 scale2(uint32_t codes) {
-    Scale2 r;
-    r.s = codes * 16u + kScaleOne;
-    if (!kWhole) {
-        if ((codes & 0xffffu) == q4::kNanCode) r.s |= 0x7fffu;
-        if ((codes >> 16) == q4::kNanCode) r.s |= 0x7fff0000u;
-    }
-    r.m24 = mul_bf16x2(r.s, 0xc1c0c1c0u);
-    return r;
-}
-// Whether a byte of the word is kNanCode: its lower seven bits carry into the eighth, and that is set.
-__device__ __forceinline__ uint32_t nan_bits(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u; }
-// Pair i of a word: numbers n in the mantissas of 16 + n, times the scales, minus 24 of them: (n - 8) s, exactly.
-template <int i>
-__device__ __forceinline__ uint32_t pair(uint32_t w, const Scale2 &s, uint32_t sixteen) {
-    const uint32_t x = i ? __funnelshift_r(w, w, 4 * i) : w;
-    return fma_bf16x2((x & 0x00780078u) | sixteen, s.s, s.m24);
-}
-
-// ---- the work list
-struct Unit {
-    int b, h, rt, L, npages, ntiles;
-    int t0, t1;              // this range's tiles
-    int w0;                  // flat index of the unit's first entry
-    int entries;             // of the flat list that this range has of the unit
-    bool any;
-};
-
-struct List {
-    int W, n_workers, per_block, per_seq, tree_tiles, step;   // step: sequences per entry of the prefix table
-    int each, more;   // entries of a range; the first `more` ranges have one more
-    __device__ __forceinline__ int begin(int worker) const { return worker * each + min(worker, more); }
-    // the worker whose range holds entry w
-    __device__ __forceinline__ int worker_of(int w) const {
-        const int longer = more * (each + 1);
-        return w < longer ? w / (each + 1) : more + (w - longer) / each;
-    }
-};
-// A unit whose shares a thread block merges: those of its workers first .. last (first < 0: none); whether the first of them begins it;
-// the blocks block0 .. block1 have it in common.
-struct Task {
-    int b, h, rt, first, last, begins, block0, block1;
-};
-// The sequences: for up to 32 in the lanes' registers, beyond that a table in shared memory.
-struct Seqs {
-    int start, L;            // of sequence `lane`
-    const int2 *table;       // (start, length) of every list.step-th
-};
-
-__device__ __forceinline__ bool length_ok(const Q4AttnParams &p, int L) { return L >= 0 && (int64_t)L <= (int64_t)p.max_pages * kPage; }
-__device__ __forceinline__ int entries_of(const Q4AttnParams &p, const List &l, int L) {
-    return length_ok(p, L) ? ((L + kPage - 1) / kPage + l.tree_tiles + kUnitCost) * l.per_seq : 0;
-}
-
-// The part of the list from w on that lies in one unit (and before w_end).  Warp-collective.
-__device__ __forceinline__ Unit unit_at(const Q4AttnParams &p, const List &l, const Seqs &seqs, int w, int w_end, int lane) {
-    Unit u;
-    int start, b;
-    if (p.B <= 32) {   // the last sequence that begins at or before w (one without entries begins where the next one does)
-        b = 31 - __clz(__ballot_sync(0xffffffffu, seqs.start <= w));
-        start = __shfl_sync(0xffffffffu, seqs.start, b);
-        u.L = __shfl_sync(0xffffffffu, seqs.L, b);
-    } else {
-        int lo = 0, hi = (p.B + l.step - 1) / l.step;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (seqs.table[mid].x <= w) lo = mid; else hi = mid;
-        }
-        const int2 x = seqs.table[lo];
-        start = x.x;
-        u.L = x.y;
-        b = lo * l.step;
-        if (l.step > 1) {   // at most 256 sequences from there on
-            int left = min(l.step, p.B - b);
-            for (;;) {
-                const int L = lane < left ? p.seq_lens[b + lane] : -1;
-                const int e = lane < left ? entries_of(p, l, L) : 0;
-                int incl = e;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int t = __shfl_up_sync(0xffffffffu, incl, d);
-                    if (lane >= d) incl += t;
-                }
-                const unsigned here = __ballot_sync(0xffffffffu, e > 0 && start + incl > w);
-                if (here) {
-                    const int j = __ffs(here) - 1;
-                    start += __shfl_sync(0xffffffffu, incl - e, j);
-                    u.L = __shfl_sync(0xffffffffu, L, j);
-                    b += j;
-                    break;
-                }
-                start += __shfl_sync(0xffffffffu, incl, 31);
-                b += 32;
-                left -= 32;
-                if (left <= 0) break;   // (cannot be: w lies before the next entry)
-            }
-        }
-    }
-    u.b = b;
-    u.npages = (u.L + kPage - 1) / kPage;
-    u.ntiles = u.npages + l.tree_tiles;
-    const int per_unit = u.ntiles + kUnitCost, local = w - start, unit = local / per_unit, pos = local - unit * per_unit;
-    const int n_rt = p.n_rt;
-    u.h = n_rt == 1 ? unit : unit / n_rt;
-    u.rt = unit - u.h * n_rt;
-    const int pos_end = min(per_unit, pos + (w_end - w));
-    u.entries = pos_end - pos;
-    u.w0 = w - pos;
-    u.t0 = max(0, pos - kUnitCost);
-    u.t1 = max(0, pos_end - kUnitCost);
-    u.any = u.t1 > u.t0;
-    return u;
-}
-
 // ---- rows of a unit
-// row / G (the host has checked that row * G < 2^32)
-__device__ __forceinline__ int node_of(const Q4AttnParams &p, int row) { return p.G == 1 ? row : (int)__umulhi((unsigned)row, p.inv_G); }
 template <int NT>
 __device__ __forceinline__ size_t out_row(const Q4AttnParams &p, int b, int h, int rt, int r) {
     const int row = rt * Shape<NT>::kRows + r, j = node_of(p, row);
@@ -244,76 +74,11 @@ __device__ __forceinline__ size_t out_row(const Q4AttnParams &p, int b, int h, i
 }
 template <int NT>
 __device__ __forceinline__ int live_rows(const Q4AttnParams &p, int rt) { return min(Shape<NT>::kRows, p.T * p.G - rt * Shape<NT>::kRows); }
-__device__ __forceinline__ int code_of_flag(int flag) {
-    return (flag & kBadTree) ? READER_ERR_BAD_TREE : (flag & kBadLength) ? READER_ERR_CAPACITY : (flag & kBadPage) ? READER_ERR_BAD_PAGE : flag ? READER_ERR_TIMEOUT : READER_OK;
-}
-__device__ __forceinline__ void note(const Q4AttnParams &p, int b, int flag, int lane) {
-    if (flag && lane == 0) atomicMax(p.status + b, code_of_flag(flag));
-}
-
-// One row of `count` shares: ml(k) and at(k) are share k's (m, l) and its row of O.  A share whose maximum is -inf has weight 0 and is
-// still added, so that a NaN in it stays.
-struct Row {
-    float top, total;
-    float4 o;   // elements 4 lane .. + 3
+// A unit whose shares a thread block merges: those of its workers first .. last (first < 0: none); whether the first of them begins it;
+// the blocks block0 .. block1 have it in common.
+struct Task {
+    int b, h, rt, first, last, begins, block0, block1;
 };
-template <int D, typename Ml, typename At>
-__device__ __forceinline__ Row merge_row(int count, float scale_log2, const Ml &ml_of, const At &at) {
-    const int lane = threadIdx.x & 31;
-    const bool has = lane * 4 < D;
-    constexpr int kAtOnce = 8;   // (this code runs once, with a cold instruction cache: 16 at once are no faster)
-    Row x = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 1
-    for (int k0 = 0; k0 < count; k0 += kAtOnce) {
-        const int n = min(kAtOnce, count - k0);
-        const float2 ml = lane < n ? ml_of(k0 + lane) : make_float2(-INFINITY, 0.f);
-        float4 y[kAtOnce];
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-            y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (has && k < n) y[k] = *reinterpret_cast<const float4 *>(at(k0 + k) + lane * 4);
-        }
-        float top = ml.x;
-#pragma unroll
-        for (int d = 4; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        top = fmaxf(x.top, __shfl_sync(0xffffffffu, top, 0));
-        const float keep = x.top == top ? 1.f : ex2((x.top - top) * scale_log2);
-        const float weight = ml.x == -INFINITY ? 0.f : ml.x == top ? 1.f : ex2((ml.x - top) * scale_log2);
-        float sum = ml.y * weight;
-#pragma unroll
-        for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        x.top = top;
-        x.total = fmaf(x.total, keep, __shfl_sync(0xffffffffu, sum, 0));
-        x.o.x *= keep; x.o.y *= keep; x.o.z *= keep; x.o.w *= keep;
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-            const float w = __shfl_sync(0xffffffffu, weight, k);   // (behind the last share: 0 times 0)
-            x.o.x = fmaf(y[k].x, w, x.o.x);
-            x.o.y = fmaf(y[k].y, w, x.o.y);
-            x.o.z = fmaf(y[k].z, w, x.o.z);
-            x.o.w = fmaf(y[k].w, w, x.o.w);
-        }
-    }
-    return x;
-}
-// A merged row as the call's result.
-template <int D>
-__device__ __forceinline__ void put_row(const Q4AttnParams &p, size_t row, const Row &x, int flag) {
-    const int lane = threadIdx.x & 31;
-    const float inv = x.total == 0.f ? 0.f : 1.f / x.total;   // (a row that sees nothing: zeros)
-    if (lane * 4 < D)
-        *reinterpret_cast<uint2 *>(p.out + row * D + lane * 4) = flag ? make_uint2(0u, 0u) : make_uint2(pack(x.o.x * inv, x.o.y * inv), pack(x.o.z * inv, x.o.w * inv));
-    if (p.lse && lane == 0) p.lse[row] = flag ? 0.f : fmaf(x.top, p.scale, log2f(x.total) * 0.6931471805599453f);
-}
-
-// A row as a share in the workspace.
-template <int D>
-__device__ __forceinline__ void keep_row(const Q4AttnParams &p, size_t row, const Row &x) {
-    const int lane = threadIdx.x & 31;
-    if (lane * 4 < D) *reinterpret_cast<float4 *>(p.partial_o + row * D + lane * 4) = x.o;
-    if (lane == 0) p.partial_ml[row] = make_float2(x.top, x.total);
-}
-
 // Row r of a unit.  kOfWorkers: from the shares of the block's workers, into the result or, if other blocks have shares too, as the
 // block's share into the workspace; kOfBlocks: from the blocks' shares into the result.
 enum MergeMode { kOfWorkers, kOfBlocks };
@@ -334,8 +99,9 @@ __device__ __forceinline__ void merge_one(const Q4AttnParams &p, unsigned char *
     auto row_of = [&](int k) {   // row of the workspace's arrays
         return (size_t)(mode == kOfBlocks ? of_blocks + block_slot(k) : (int)blockIdx.x * per_block + t.first + k) * kRows + r;
     };
-    auto at = [&](int k) {
-        return mode != kOfBlocks && in_ring(t.first + k) ? reinterpret_cast<const float *>(smem + (t.first + k) * C::kRingBytes) + r * D : p.partial_o + row_of(k) * D;
+    auto o = [&](int k) {
+        if (mode != kOfBlocks && in_ring(t.first + k)) return *reinterpret_cast<const float4 *>(smem + (t.first + k) * C::kRingBytes + (r * D + lane * 4) * 4);
+        return __ldcg(reinterpret_cast<const float4 *>(p.partial_o + row_of(k) * D + lane * 4));
     };
     auto ml = [&](int k) {
         return mode != kOfBlocks && in_ring(t.first + k) ? ml_all[(t.first + k) * kRows + r] : __ldcg(p.partial_ml + row_of(k));
@@ -344,7 +110,7 @@ __device__ __forceinline__ void merge_one(const Q4AttnParams &p, unsigned char *
     for (int k = lane; k < count; k += 32)
         flag |= mode == kOfBlocks ? __ldcg(p.flags + block_slot(k)) : k == 0 && t.begins ? s.end_flag[t.first] : s.first_flag[t.first + k];
     flag = __reduce_or_sync(0xffffffffu, flag);
-    const Row x = merge_row<D>(count, p.scale_log2, ml, at);
+    const Row x = merge_row<D>(count, p.scale_log2, ml, o);
     if (mode == kOfBlocks || t.block0 == t.block1) {
         if (r == 0) note(p, t.b, flag, lane);
         put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
@@ -779,6 +545,7 @@ struct Worker {
                 b[nt][1] = transposed(pack(s[0][nt][2], s[0][nt][3]));
             }
             const __nv_bfloat16 *v = p.v_tree + (((size_t)u.b * p.T + n) * p.Hkv + u.h) * D + g * kOwn;
+            bool dirty = false;
 #pragma unroll
             for (int x = 0; x < kOwn / 8; ++x) {   // eight elements of two pairs of nodes at a time
                 uint4 w[4];
@@ -787,6 +554,7 @@ struct Worker {
                     const int key = 2 * c + (i & 1) + 8 * (i >> 1);
                     w[i] = make_uint4(0, 0, 0, 0);
                     if (key < left) w[i] = *reinterpret_cast<const uint4 *>(v + (size_t)key * p.Hkv * D + 8 * x);
+                    dirty |= clean(w[i]);
                 }
                 const uint32_t a[4][4] = {{w[0].x, w[0].y, w[0].z, w[0].w}, {w[1].x, w[1].y, w[1].z, w[1].w}, {w[2].x, w[2].y, w[2].z, w[2].w}, {w[3].x, w[3].y, w[3].z, w[3].w}};
 #pragma unroll
@@ -795,6 +563,28 @@ struct Worker {
                     for (int nt = 0; nt < NT; ++nt)
                         mma(o[4 * x + i][nt], __byte_perm(a[0][i], a[1][i], 0x5410), __byte_perm(a[0][i], a[1][i], 0x7632), __byte_perm(a[2][i], a[3][i], 0x5410),
                             __byte_perm(a[2][i], a[3][i], 0x7632), b[nt][0], b[nt][1]);
+            }
+            // Infinities and NaN among the values: 0 times them is NaN, so they were left out of the product; the rows that see them get them.
+            if (__any_sync(0xffffffffu, dirty)) {
+#pragma unroll 1
+                for (int k = 0; k < min(left, 16); ++k) {
+                    const uint32_t *row = reinterpret_cast<const uint32_t *>(v + (size_t)k * p.Hkv * D);
+#pragma unroll
+                    for (int x = 0; x < kOwn / 2; ++x) {
+                        const uint32_t w = row[x];
+                        const float lo = nonfinite(w << 16) ? bf16lo(w) : 0.f, hi = nonfinite(w) ? bf16hi(w) : 0.f;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const bool sees = (masks[2 * (8 * nt + 2 * c + e) + (n >> 6)] >> ((n & 63) + k)) & 1;
+                                if (sees) {
+                                    o[x][nt][e] += lo;
+                                    o[x][nt][2 + e] += hi;
+                                }
+                            }
+                    }
+                }
             }
         }
     }
@@ -859,7 +649,7 @@ struct Worker {
         else write_share(u, p.partial_o + (size_t)worker * S::kRows * D, p.partial_ml + worker * S::kRows);
         if (u.t0 != 0 && warp != 0) return;
         // the unit's shares belong to the workers c0 .. c1
-        const int c0 = u.t0 == 0 ? worker : list.worker_of(u.w0 + kUnitCost), c1 = list.worker_of(u.w0 + kUnitCost + u.ntiles - 1);
+        const int c0 = u.t0 == 0 ? worker : list.worker_of(u.first_entry(kUnitCost)), c1 = list.worker_of(u.last_entry(kUnitCost));
         if (lane == 0)
             tasks[u.t0 == 0 ? warp : S::kWarps] = Task{u.b, u.h, u.rt, warp, min(c1 - (int)blockIdx.x * list.per_block, list.per_block - 1), u.t0 == 0, c0 / list.per_block, c1 / list.per_block};
     }
@@ -873,16 +663,6 @@ struct Worker {
     }
 };
 
-// Whether parent array b is a tree.  Warp-collective.
-__device__ __forceinline__ bool tree_ok(const Q4AttnParams &p, int b, int lane) {
-    bool bad = false;
-    for (int j = lane; j < p.T; j += 32) {
-        const int a = p.parent[(size_t)b * p.T + j];
-        bad |= !(j == 0 ? a == -1 : a >= 0 && a < j);
-    }
-    return !__any_sync(0xffffffffu, bad);
-}
-
 template <int D, int NT>
 __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(const __grid_constant__ Q4AttnParams p) {
     extern __shared__ __align__(128) unsigned char smem[];
@@ -894,72 +674,19 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     pdl_wait();
     pdl_launch_dependents();
 
-    // the list: prefix sums over the sequences
+    __shared__ int warp_sum[S::kWarps];
     List list;
-    list.per_seq = p.Hkv * p.n_rt;
+    list.cost = kUnitCost;
+    list.pages = list.weight = 1;
+    list.n_wide = p.n_rt;
+    list.narrow = 0;
     list.tree_tiles = (p.T + kPage - 1) / kPage;
-    list.step = (p.B + kPrefix - 1) / kPrefix;
     Seqs seqs;
-    int2 *table = reinterpret_cast<int2 *>(smem + C::kOffPrefix);
-    seqs.table = table;
-    seqs.start = INT_MAX;
-    seqs.L = 0;
-    int carry = 0;
-    if (p.B <= 32) {   // every warp by itself
-        const int L = lane < p.B ? p.seq_lens[lane] : -1, e = lane < p.B ? entries_of(p, list, L) : 0;
-        int incl = e;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += t;
-        }
-        if (lane < p.B) seqs.start = incl - e;
-        seqs.L = L;
-        carry = __shfl_sync(0xffffffffu, incl, 31);
-    } else {
-        __shared__ int warp_sum[S::kWarps];
-        for (int b0 = 0; b0 < p.B; b0 += S::kThreads) {
-            const int b = b0 + tid;
-            const int L = b < p.B ? p.seq_lens[b] : 0;
-            const int e = b < p.B ? entries_of(p, list, L) : 0;
-            int incl = e;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int t = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += t;
-            }
-            __syncthreads();
-            if (lane == 31) warp_sum[warp] = incl;
-            __syncthreads();
-            int before = 0, all = 0;
-#pragma unroll
-            for (int i = 0; i < S::kWarps; ++i) {
-                const int x = warp_sum[i];
-                before += i < warp ? x : 0;
-                all += x;
-            }
-            if (b < p.B && b % list.step == 0) table[b / list.step] = make_int2(carry + before + incl - e, L);
-            carry += all;
-        }
-    }
-    list.W = carry;
+    make_list<S::kWarps>(p, list, seqs, reinterpret_cast<int2 *>(smem + C::kOffPrefix), warp_sum);
     // fewer workers when there is little to do, spread over the thread blocks
     list.per_block = max(1, min(S::kWarps, list.W / (kMinEntries * p.n_ctas)));
-    list.n_workers = list.per_block * max(1, min(p.n_ctas, list.W / (kMinEntries * list.per_block)));
-    list.each = list.W / list.n_workers;
-    list.more = list.W - list.each * list.n_workers;
-
-    // a sequence whose length cannot be: zero rows, from one warp
-    for (int b = blockIdx.x * S::kWarps + warp; b < p.B; b += p.n_ctas * S::kWarps) {
-        if (length_ok(p, p.seq_lens[b])) continue;
-        const bool tree = tree_ok(p, b, lane);
-        if (lane == 0) p.status[b] = tree ? READER_ERR_CAPACITY : READER_ERR_BAD_TREE;
-        const size_t rows = (size_t)p.T * p.Hq;
-        uint4 *o = reinterpret_cast<uint4 *>(p.out + (size_t)b * rows * D);
-        for (size_t i = lane; i < rows * (D / 8); i += 32) o[i] = make_uint4(0, 0, 0, 0);
-        if (p.lse)
-            for (size_t i = lane; i < rows; i += 32) p.lse[(size_t)b * rows + i] = 0.f;
-    }
+    list.cut(list.per_block * max(1, min(p.n_ctas, list.W / (kMinEntries * list.per_block))));
+    reject_lengths<D>(p, blockIdx.x * S::kWarps + warp, p.n_ctas * S::kWarps, lane);
 
     __shared__ Task tasks[S::kWarps + 1];   // of the units that the workers begin, and of the one that the block's first continues
     __shared__ int16_t segments[S::kWarps], first_flag[S::kWarps], end_flag[S::kWarps];   // units in a worker's range; what is wrong with its shares
@@ -976,7 +703,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
         int w = list.begin(worker);
         const int w_end = list.begin(worker + 1);
         const uint64_t policy = l2_policy_evict_first();
-        const bool once = list.per_seq == p.Hkv;   // no other unit reads these pages
+        const bool once = p.n_rt == 1;   // no other unit reads these pages
         unsigned char *parents = smem + C::kOffParents + warp * kMaxNodes;
         uint64_t *masks = reinterpret_cast<uint64_t *>(smem + C::kOffMasks) + warp * S::kRows * 2;
         Unit u;
@@ -1110,7 +837,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
     for (int r = warp; r < live; r += S::kWarps) {
         const Row x = merge_row<D>(
             S::kWarps, p.scale_log2, [&](int w) { return ml_all[w * S::kRows + r]; },
-            [&](int w) { return reinterpret_cast<const float *>(smem + w * C::kRingBytes) + r * D; });
+            [&](int w) { return *reinterpret_cast<const float4 *>(smem + w * C::kRingBytes + (r * D + lane * 4) * 4); });
         if (p.split == 1) {
             put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r), x, block_flag);
         } else {
@@ -1131,7 +858,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
     for (int r = warp * p.split + piece; r < live; r += workers) {
         const Row x = merge_row<D>(
             p.split, p.scale_log2, [&](int w) { return __ldcg(p.partial_ml + (first + w) * S::kRows + r); },
-            [&](int w) { return p.partial_o + ((size_t)(first + w) * S::kRows + r) * D; });
+            [&](int w) { return __ldcg(reinterpret_cast<const float4 *>(p.partial_o + ((size_t)(first + w) * S::kRows + r) * D + lane * 4)); });
         put_row<D>(p, out_row<NT>(p, u.b, u.h, u.rt, r), x, unit_flag);
     }
 }

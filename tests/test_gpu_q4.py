@@ -677,3 +677,31 @@ def test_a_prompt_and_decoding_steps_on_a_4_bit_cache(rd):
             ks[s] = torch.cat([ks[s], held(kt[s, path[s, :n_acc[s]]])])
             vs[s] = torch.cat([vs[s], held(vt[s, path[s, :n_acc[s]]])])
         assert seq_lens.tolist() == [len(x) for x in ks]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,group", [(5, 1), (40, 4), (100, 3)])
+def test_infinite_values_of_nodes_reach_the_rows_that_see_them_alone(rd, d, T, group):
+    rng = np.random.default_rng(24)
+    lens = [70, 0]
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, group, d)
+    want = plain_attn(both, lens, q, kt, vt, parent, 0.1)
+    sees = np.stack([sees_of(x) for x in parent])
+    for value in (float("inf"), float("-inf"), float("nan")):
+        for key, what in ((False, vt), (True, kt)):
+            x = what.clone()
+            node = T // 2
+            x[0, node, 1, 3] = value
+            x[1, T - 1, 0, d - 1] = value
+            out, lse, st = attend(rd, cache, q, x if key else kt, vt if key else x, parent, 0.1)
+            assert st == [0, 0]
+            hit = torch.zeros(out.shape, dtype=torch.bool)
+            for b, h, n, e in ((0, 1, node, 3), (1, 0, T - 1, d - 1)):
+                rows = torch.from_numpy(np.nonzero(sees[b][:, n])[0])
+                hit[b, rows, h * group:(h + 1) * group] |= True if key else (torch.arange(d) == e)
+            if key:   # (a score of -inf is a key that is not seen: only NaN is NaN throughout)
+                if np.isnan(value):
+                    assert torch.isnan(out[hit]).all()
+            else:
+                assert (torch.isnan(out[hit]) if np.isnan(value) else out[hit] == value).all()
+            assert ((out.double() - want[0]).abs() <= want[2])[~hit].all()
