@@ -14,7 +14,7 @@ MARSHAL_MADE_FOR = os.path.join(CSRC, "_build", "marshal_made_for.txt")   # what
 
 SOURCES = ["api.cu", "tree_encode.cu", "verify_attn_generic.cu", "verify_attn_sm100.cu", "combine.cu",
            "accept.cu", "accept_noalloc.cu", "sample.cu", "kv_commit.cu", "kv_rearrange.cu", "padded_cache.cu", "accept_commit.cu",
-           "rotate.cu", "prompt_attn_sm100.cu", "q4_cache.cu", "q4_attn_rows.cu", "pages.cu", "api_cache.cu"]
+           "rotate.cu", "prompt_attn_sm100.cu", "q4_cache.cu", "q4_attn_rows.cu", "q4_attn_sm100.cu", "pages.cu", "api_cache.cu"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-I", INCLUDE, "-I", CSRC]

@@ -269,7 +269,9 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
     p.flags = reinterpret_cast<int32_t *>(ws + w.flags);
     p.partial_ml = reinterpret_cast<float2 *>(ws + w.partial_ml);
     p.partial_o = reinterpret_cast<float *>(ws + w.partial_o);
-    if (reader_status s = launch_q4_attn_rows(&ctx->q4_attr, p, ctx->n_sm, (cudaStream_t)stream)) return s;
+    p.inv_G = (unsigned)((((uint64_t)1 << 32) + p.G - 1) / p.G);
+    const bool few = (int64_t)T * p.G <= kQ4FewRows;
+    if (reader_status s = (few ? launch_q4_attn_rows : launch_q4_attn_sm100)(&ctx->q4_attr, p, ctx->n_sm, (cudaStream_t)stream)) return s;
     return launch_status();
 }
 

@@ -4,8 +4,9 @@
 
 namespace reader {
 
+constexpr int kQ4FewRows = 16;          // query rows of a KV head up to which the few-rows kernels are faster
 // Rows of the shares of a thread block's workers and of its own two, at most (few-rows kernels).
-constexpr int kQ4ShareRows = 192 + 32;
+constexpr int kQ4ShareRows = 512;   // (a block of the many-rows kernel: two shares of 256 rows)
 constexpr int kQ4MaxBatch = 1 << 16;
 constexpr int kQ4MaxGroup = 1 << 12;   // (128 nodes: 128 G^2 < 2^32, as the division by G wants it)
 
@@ -34,8 +35,12 @@ struct Q4AttnParams {
 
 // Which kernels have their attributes set.
 struct Q4AttrSet {
-    bool rows[4];
+    bool rows[4], sm100[2];
 };
+// Few query rows of a KV head (q4_attn_rows.cu), many (q4_attn_sm100.cu).
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
+reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
+// Zeroes the counters and the status words in front of a kernel that adds to them.
+void launch_q4_attn_zero(const Q4AttnParams &p, int n_sm, cudaStream_t st);
 
 }  // namespace reader

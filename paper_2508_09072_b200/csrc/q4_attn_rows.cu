@@ -889,7 +889,6 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
     // Alone: the units of a sequence fit a cluster, the clusters the GPU, and, going by the page table's width, a worker gets at most
     // kAloneTiles tiles.
     p.n_rt = (p.T * p.G + S::kRows - 1) / S::kRows;
-    p.inv_G = (unsigned)((((uint64_t)1 << 32) + p.G - 1) / p.G);
     const int units = p.Hkv * p.n_rt;
     const int tiles = p.max_pages + (p.T + kPage - 1) / kPage;
     if (units <= kMaxCluster) {
@@ -918,12 +917,16 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
         }
     }
     p.n_ctas = n_sm;
-    launch_pdl(q4_attn_zero_kernel, dim3(1), dim3(1024), 0, st, p.counters, n_sm, p.status, p.B);
+    launch_q4_attn_zero(p, n_sm, st);
     launch_pdl(q4_attn_list_kernel<D, NT>, dim3((unsigned)n_sm), dim3(S::kThreads), (size_t)C::kSmem, st, p);
     return READER_OK;
 }
 
 }  // namespace
+
+void launch_q4_attn_zero(const Q4AttnParams &p, int n_sm, cudaStream_t st) {
+    launch_pdl(q4_attn_zero_kernel, dim3(1), dim3(1024), 0, st, p.counters, n_sm, p.status, p.B);
+}
 
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st) {
     const bool few = p.T * p.G <= 8;
