@@ -12,8 +12,10 @@
 //                    products run beside the results being written.
 //   warps 8-11       unpack pages (and copy the tree's own keys and values) into the tiles
 //   warp 12          brings pages into a ring by bulk copies
-//   warp 13          issues the products: S = Q K^T, O += P V
-//   warp 14          zero rows for sequences whose length cannot be
+//   warps 13, 14     issue the products of slot 0 and 1: S = Q K^T, O += P V.  (One warp for both was busy all the time: 3 us a tile.)
+//   warp 15          finds the block's units and puts them into a small ring that the others read; zero rows for sequences whose
+//                    length cannot be.  (With the search in every role the code did not fit the instruction caches any more, and
+//                    warps stood waiting for instructions.)
 // A unit of more than 128 rows is wide: each slot has its own rows and both work on every tile.  A narrow one has up to 128 rows;
 // the slots take the tiles in turns and their two results are merged at its end.
 //
@@ -23,7 +25,7 @@
 // Work: a flat list of tiles cut into equal ranges, one per thread block, shares of units in several ranges merged by the block that
 // comes last (q4_attn_common.cuh).  Bytes that are not committed never reach a product: their scores become -inf, and their values 0 or
 // not multiplied at all (16-key slices behind the end).  Every wait is bounded: a block that gives up reports all its units.
-#include <cuda.h>
+#include <type_traits>
 
 #include "prompt_ptx.cuh"
 #include "q4_attn_common.cuh"
@@ -35,14 +37,15 @@ using namespace q4;
 
 constexpr int kThreads = 512;
 constexpr int kSoftmaxThreads = 256;
-constexpr int kUnpackWarp = 8, kLoadWarp = 12, kMmaWarp = 13, kRejectWarp = 14;
+constexpr int kUnpackWarp = 8, kLoadWarp = 12, kMmaWarp = 13, kListWarp = 15;
+constexpr int kReaders = 15;       // warps that read the ring of units: all but kListWarp
 // Registers of a thread: softmax, unpacking, the rest; 128 (2 x 184 + 80 + 64) = 65536, what the block is launched with.
 constexpr int kRegsSoftmax = 184, kRegsUnpack = 80, kRegsRest = 64;
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
 constexpr int kUnitCost = 6;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = 8;     // of a range
 constexpr int kRawSlots = 3;       // of the ring: keys or values of a tile's pages each
-constexpr int kAhead = 8;          // units that a role may be ahead of another, at most (two tiles and a ring of one and a half)
+constexpr int kAhead = 8;          // units in the ring
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 
 template <int D>
@@ -63,16 +66,28 @@ struct Cfg {
     static constexpr int kOffMl = kOffParents + kAhead / 2 * kMaxNodes;   // (m, l) of slot 1's rows, and of slot 0's
     static constexpr int kOffTable = kOffMl + 2 * 128 * 8;
     static constexpr int kOffBars = kOffTable + kPrefix * 8;
-    static constexpr int kSmem = kOffBars + 512;
-    static_assert(kSmem + 512 <= 227 * 1024, "shared memory");
+    static constexpr int kSmem = kOffBars + 1024;
+    static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
 struct ShareTask {   // a unit that other blocks have shares of
     int b, h, rt, rows, block0, block1;   // block0 < 0: none
 };
+// A unit as the roles see it: its tiles t0 .. t0 + tiles - 1 are this block's.
+struct Piece {
+    int b, h, rt, L, npages, ntiles, t0, tiles;   // tiles = 0: no more units
+    int wide, rows, c0, c1;                       // rows of the unit; the blocks c0 .. c1 have it in common
+    __device__ __forceinline__ bool whole() const { return tiles == ntiles; }
+    // committed tiles come first, the tree's is the last
+    __device__ __forceinline__ bool is_tree(int tile) const { return t0 + tile == ntiles - 1; }
+    __device__ __forceinline__ int valid(int T, int tile) const { return is_tree(tile) ? T : min(kTileKeys, L - (t0 + tile) * kTileKeys); }
+    // tiles of a slot: every one, or (narrow) every other
+    __device__ __forceinline__ int first(int slot) const { return wide ? 0 : slot; }
+    __device__ __forceinline__ int step() const { return wide ? 1 : 2; }
+};
 struct Bars {
     uint64_t raw_full[kRawSlots], raw_empty[kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2];
+    uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2], piece_full[kAhead], piece_empty[kAhead];
     uint32_t tmem_base;
     int32_t abort;
     int32_t raw_bad[kRawSlots];   // a page outside the pool among the slot's
@@ -81,8 +96,9 @@ struct Bars {
     int32_t last[2];
     int32_t warp_sum[kThreads / 32];
     ShareTask task[2];
+    Piece piece[kAhead];
 };
-static_assert(sizeof(Bars) <= 512, "barrier block");
+static_assert(sizeof(Bars) <= 1024, "barrier block");
 
 // Bounded wait of a whole warp.  False, in every lane, when the block has given up.
 __device__ __forceinline__ bool gone(volatile int32_t *abort_s) { return __any_sync(0xffffffffu, *abort_s != 0); }
@@ -107,33 +123,18 @@ __device__ __forceinline__ uint32_t lds16(uint32_t a) {
 }
 __device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory"); }
 
-// A block's walk over its range: the units, and how their tiles are dealt out.
-struct Walk {
-    int w, w_end, seg;      // seg: units so far
-    Unit u;
-    int tiles, rows, visits;   // tiles here; rows of the unit; score products (both slots')
-    bool wide, whole;
-    __device__ __forceinline__ bool next(const Q4AttnParams &p, const List &l, const Seqs &s, int lane) {
-        while (w < w_end) {
-            u = unit_at(p, l, s, w, w_end, lane);
-            w += u.entries;
-            if (!u.any) continue;
-            tiles = u.t1 - u.t0;
-            rows = min(256, p.T * p.G - u.rt * 256);
-            wide = u.weight == 2;
-            visits = wide ? 2 * tiles : tiles;
-            whole = u.t0 == 0 && u.t1 == u.ntiles;
-            ++seg;
-            return true;
-        }
-        return false;
-    }
-    __device__ __forceinline__ int tile_of(int visit) const { return wide ? visit >> 1 : visit; }
-    // committed tiles of the sequence; the tree's tile comes behind them
-    __device__ __forceinline__ int committed() const { return u.ntiles - 1; }
-    __device__ __forceinline__ bool is_tree(int tile) const { return u.t0 + tile == committed(); }
-    __device__ __forceinline__ int valid(const Q4AttnParams &p, int tile) const { return is_tree(tile) ? p.T : min(kTileKeys, u.L - (u.t0 + tile) * kTileKeys); }
-};
+// Among the softmax threads and kListWarp.
+template <int kId>
+__device__ __forceinline__ void end_barrier() { asm volatile("bar.sync %0, %1;" ::"n"(kId), "n"(kSoftmaxThreads + 32) : "memory"); }
+// Unit number `seg` from the ring, for a whole warp; false when there is none, or when the block has given up.
+__device__ __forceinline__ bool next_piece(Bars *m, Piece &x, int seg, int lane, volatile int32_t *abort_s) {
+    const int i = seg % kAhead;
+    if (!wait(smem_u32(&m->piece_full[i]), (seg / kAhead) & 1, abort_s)) return false;
+    x = m->piece[i];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&m->piece_empty[i]));
+    return x.tiles > 0;
+}
 
 // ---- unpacking, by 128 threads (`t` among them)
 // A page of keys into rows row0 .. + 63 of a K tile.  Thread (w, g): word w of the positions 8 j + g (at head_dim 64, of half of the j).
@@ -148,14 +149,22 @@ __device__ __forceinline__ void unpack_keys(uint32_t raw, uint32_t tile, int row
     if constexpr (D == 128) { const uint4 x = lds128(at); codes[0] = x.x; codes[1] = x.y; codes[2] = x.z; codes[3] = x.w; }
     else codes[0] = lds32(at);
     const uint32_t dst = tile + (w >> 3) * Cfg<D>::kBlock + (row0 + 8 * j0 + g) * 128 + (((w & 7) ^ g) << 4), src = raw + (8 * j0 + g) * (D / 2) + w * 4;
+    constexpr int kWordsHere = 8 / kSplit;
+    uint32_t word[kWordsHere];
 #pragma unroll
-    for (int j = 0; j < 8 / kSplit; ++j) {
-        const uint32_t word = lds32(src + j * 8 * (D / 2));
-        const int byte = j * kPer;
-        const uint32_t sel = (byte & 3) + (kPer == 2 ? (u & 1) : 0);
-        const Scale2 s = scale2<false>(__byte_perm(codes[byte >> 2], 0, 0x4040 | sel | (sel << 8)));
-        sts128(dst + j * 8 * 128, pair<0>(word, s, sixteen), pair<1>(word, s, sixteen), pair<2>(word, s, sixteen), pair<3>(word, s, sixteen));
-    }
+    for (int j = 0; j < kWordsHere; ++j) word[j] = lds32(src + j * 8 * (D / 2));
+    const uint32_t odd = kPer == 2 ? (u & 1) * 0x0101u : 0u;
+    auto go = [&](auto whole) {
+#pragma unroll
+        for (int j = 0; j < kWordsHere; ++j) {
+            constexpr bool kWhole = decltype(whole)::value;
+            const uint32_t sel = 0x4040u | (j * kPer & 3) * 0x0101u;
+            const Scale2 s = scale2<kWhole>(__byte_perm(codes[j * kPer >> 2], 0, sel + odd));
+            sts128(dst + j * 8 * 128, pair<0>(word[j], s, sixteen), pair<1>(word[j], s, sixteen), pair<2>(word[j], s, sixteen), pair<3>(word[j], s, sixteen));
+        }
+    };
+    if (nan_bits(codes[0]) | nan_bits(codes[1]) | nan_bits(codes[2]) | nan_bits(codes[3])) go(std::false_type());
+    else go(std::true_type());
 }
 // A page of values into a page of V^T, `valid` of its positions committed (the others become 0).  64 threads: (q, z) = the positions 8 q .. + 7 of
 // the elements z D/8 .. + D/8 - 1.
@@ -195,17 +204,24 @@ __device__ __forceinline__ void unpack_values(uint32_t raw, uint32_t page, int v
         }
     }
     Scale2 s[4];
+    const uint32_t both01 = codes[0] | codes[1] << 16, both23 = codes[2] | codes[3] << 16;
+    if (8 * q + 8 <= valid && !(nan_bits(both01) | nan_bits(both23))) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        s[e] = scale2<false>(__byte_perm(codes[e], 0, 0x4140));
-        const int key = 8 * q + 2 * e;
-        if (key >= valid) { s[e].s &= 0xffff0000u; s[e].m24 &= 0xffff0000u; }
-        if (key + 1 >= valid) { s[e].s &= 0xffffu; s[e].m24 &= 0xffffu; }
+        for (int e = 0; e < 4; ++e) s[e] = scale2<true>(__byte_perm(codes[e], 0, 0x4140));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s[e] = scale2<false>(__byte_perm(codes[e], 0, 0x4140));
+            const int key = 8 * q + 2 * e;
+            if (key >= valid) { s[e].s &= 0xffff0000u; s[e].m24 &= 0xffff0000u; }
+            if (key + 1 >= valid) { s[e].s &= 0xffffu; s[e].m24 &= 0xffffu; }
+        }
     }
 #pragma unroll
     for (int y = 0; y < kWords; ++y) {
-        const int d0 = z * (D / 8) + 4 * y;
-        auto row = [&](int i) { return page + (d0 + i) * 128 + ((q ^ ((d0 + i) & 7)) << 4); };
+        // row d = z D/8 + 4 y + i; D/8 is a multiple of 8
+        const uint32_t rows = page + z * (D / 8) * 128;
+        auto row = [&](int i) { return rows + (4 * y + i) * 128 + ((q ^ ((4 * y + i) & 7)) << 4); };
         sts128(row(0), pair<0>(w[0][y], s[0], sixteen), pair<0>(w[1][y], s[1], sixteen), pair<0>(w[2][y], s[2], sixteen), pair<0>(w[3][y], s[3], sixteen));
         sts128(row(1), pair<1>(w[0][y], s[0], sixteen), pair<1>(w[1][y], s[1], sixteen), pair<1>(w[2][y], s[2], sixteen), pair<1>(w[3][y], s[3], sixteen));
         sts128(row(2), pair<2>(w[0][y], s[0], sixteen), pair<2>(w[1][y], s[1], sixteen), pair<2>(w[2][y], s[2], sixteen), pair<2>(w[3][y], s[3], sixteen));
@@ -271,9 +287,9 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(&m->k_full[i]), 4);
-            mbar_init(bar(&m->k_empty[i]), 1);
+            mbar_init(bar(&m->k_empty[i]), 2);
             mbar_init(bar(&m->v_full[i]), 4);
-            mbar_init(bar(&m->v_empty[i]), 1);
+            mbar_init(bar(&m->v_empty[i]), 2);
             mbar_init(bar(&m->s_full[i]), 1);
             mbar_init(bar(&m->p_full[i][0]), 128);
             mbar_init(bar(&m->p_full[i][1]), 128);
@@ -282,8 +298,12 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             m->last[i] = 0;
         }
         mbar_init(bar(&m->q_full), kSoftmaxThreads);
-        mbar_init(bar(&m->q_empty), 1);
-        for (int i = 0; i < kAhead; ++i) m->flags[i] = m->poison[i] = 0;
+        mbar_init(bar(&m->q_empty), 2);
+        for (int i = 0; i < kAhead; ++i) {
+            mbar_init(bar(&m->piece_full[i]), 1);
+            mbar_init(bar(&m->piece_empty[i]), kReaders);
+            m->flags[i] = m->poison[i] = 0;
+        }
         m->abort = (base & 1023u) ? 1 : 0;   // (the swizzled tiles want 1024-byte alignment; never seen otherwise, but checked)
         fence_mbar_init();
         fence_proxy_async();
@@ -312,30 +332,78 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     __syncthreads();
     list.per_block = 1;
     list.cut(max(1, min(p.n_ctas, list.W / kMinEntries)));
-    Walk k;
-    k.seg = -1;
-    k.w = k.w_end = 0;
-    if ((int)blockIdx.x < list.n_workers && list.W > 0) {
-        k.w = list.begin(blockIdx.x);
-        k.w_end = list.begin(blockIdx.x + 1);
-    }
 
     if (warp >= 12) {
         regs_dec<kRegsRest>();
+        if (warp == kListWarp) {
+            // ------------------------------------------------------------------ units
+            int w = 0, w_end = 0;
+            if ((int)blockIdx.x < list.n_workers && list.W > 0) {
+                w = list.begin(blockIdx.x);
+                w_end = list.begin(blockIdx.x + 1);
+            }
+            for (int seg = 0;; ++seg) {
+                Piece x{};
+                while (w < w_end) {
+                    const Unit u = unit_at(p, list, seqs, w, w_end, lane);
+                    w += u.entries;
+                    if (!u.any) continue;
+                    x = Piece{u.b, u.h, u.rt, u.L, u.npages, u.ntiles, u.t0, u.t1 - u.t0, u.weight == 2, min(256, p.T * p.G - u.rt * 256), 0, 0};
+                    if (!x.whole()) {
+                        x.c0 = list.worker_of(u.first_entry(kUnitCost));
+                        x.c1 = list.worker_of(u.last_entry(kUnitCost));
+                    }
+                    break;
+                }
+                const int i = seg % kAhead;
+                if (!wait(bar(&m->piece_empty[i]), ((seg / kAhead) & 1) ^ 1, abort_s)) break;
+                if (lane == 0) {
+                    m->piece[i] = x;
+                    mbar_arrive(bar(&m->piece_full[i]));
+                }
+                __syncwarp();
+                if (x.tiles == 0) break;
+            }
+            reject_lengths<D>(p, blockIdx.x, gridDim.x, lane);
+            end_barrier<3>();
+            if (gone(abort_s) && (int)blockIdx.x < list.n_workers && list.W > 0) {
+                // The block has given up: whatever became of its units, whole ones are zeroed and reported, shares are reported to those who merge.
+                w = list.begin(blockIdx.x);
+                while (w < w_end) {
+                    const Unit u = unit_at(p, list, seqs, w, w_end, lane);
+                    w += u.entries;
+                    if (!u.any) continue;
+                    const int rows = min(256, p.T * p.G - u.rt * 256);
+                    if (u.t0 == 0 && u.t1 == u.ntiles) {
+                        note(p, u.b, kGaveUp, lane);
+                        for (int r = 0; r < rows; ++r) {
+                            const int g = u.rt * 256 + r, j = node_of(p, g);
+                            put_row<D>(p, ((size_t)u.b * p.T + j) * p.Hq + u.h * p.G + (g - j * p.G), Row{0.f, 1.f, make_float4(0.f, 0.f, 0.f, 0.f)}, kGaveUp);
+                        }
+                    } else if (lane == 0) {
+                        const int i = u.t0 == 0 ? 1 : 0;
+                        p.flags[2 * blockIdx.x + i] = kGaveUp;
+                        m->task[i] = ShareTask{u.b, u.h, u.rt, rows, list.worker_of(u.first_entry(kUnitCost)), list.worker_of(u.last_entry(kUnitCost))};
+                    }
+                }
+            }
+            end_barrier<4>();
+        } else
         if (warp == kLoadWarp) {
             // ------------------------------------------------------------------ pages
             const uint64_t policy = l2_policy_evict_first();
             const bool once = list.n_wide + list.narrow == 1;   // no other unit reads these pages
             int n = 0;   // slots of the ring so far
-            while (!gone(abort_s) && k.next(p, list, seqs, lane)) {
-                const int pages_end = min(k.u.npages, 2 * k.u.t1);
+            Piece x;
+            for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
+                const int pages_end = min(x.npages, 2 * (x.t0 + x.tiles));
                 int ids = 0, at = -32;
-                for (int t = 0; t < k.tiles && !gone(abort_s); ++t) {
-                    if (k.is_tree(t)) break;
-                    const int page0 = 2 * (k.u.t0 + t);
+                for (int t = 0; t < x.tiles && !gone(abort_s); ++t) {
+                    if (x.is_tree(t)) break;
+                    const int page0 = 2 * (x.t0 + t);
                     if (page0 - at >= 32) {
                         at = page0;
-                        ids = page0 + lane < pages_end ? p.page_table[(size_t)k.u.b * p.max_pages + page0 + lane] : 0;
+                        ids = page0 + lane < pages_end ? p.page_table[(size_t)x.b * p.max_pages + page0 + lane] : 0;
                     }
                     const int id0 = __shfl_sync(0xffffffffu, ids, page0 - at), id1 = __shfl_sync(0xffffffffu, ids, page0 - at + 1);
                     const int count = min(2, pages_end - page0);
@@ -351,8 +419,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                             const unsigned char *pool = kv ? p.v_pool : p.k_pool;
                             const int bytes = (ok0 ? C::kPageBytes : 0) + (count == 2 && ok1 ? C::kPageBytes : 0);
                             mbar_arrive_expect_tx(full, bytes);   // (a page outside the pool is not read; what the slot holds is never shown)
-                            if (ok0) bulk_load(dst, pool + ((size_t)id0 * p.Hkv + k.u.h) * C::kPageBytes, C::kPageBytes, full, policy, streamed);
-                            if (count == 2 && ok1) bulk_load(dst + C::kPageBytes, pool + ((size_t)id1 * p.Hkv + k.u.h) * C::kPageBytes, C::kPageBytes, full, policy, streamed);
+                            if (ok0) bulk_load(dst, pool + ((size_t)id0 * p.Hkv + x.h) * C::kPageBytes, C::kPageBytes, full, policy, streamed);
+                            if (count == 2 && ok1) bulk_load(dst + C::kPageBytes, pool + ((size_t)id1 * p.Hkv + x.h) * C::kPageBytes, C::kPageBytes, full, policy, streamed);
                         }
                         __syncwarp();
                     }
@@ -364,66 +432,96 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     while (!mbar_try_wait(bar(&m->raw_full[i % kRawSlots]), (i / kRawSlots) & 1) && globaltimer_ns() - t0 < 20000000ull) {
                     }
             }
-        } else if (warp == kMmaWarp) {
-            // ------------------------------------------------------------------ products
+        } else {
+            // ------------------------------------------------------------------ products of a slot
+            const int slot = warp - kMmaWarp;
             constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kTileKeys, false, false), kIdescPV = idesc_bf16_f32(128, D, false, false);
             const uint64_t descQ = smem_desc_sw128(base + C::kOffQ, 16, 1024), descK = smem_desc_sw128(base + C::kOffK, 16, 1024);
             const uint64_t descV = smem_desc_sw128(base + C::kOffV, 16, 1024);
-            int done = 0;                 // tiles of the units before
-            uint32_t p_parity = 0;        // one bit per slot
-            while (!gone(abort_s) && k.next(p, list, seqs, lane)) {
-                wait(bar(&m->q_full), k.seg & 1, abort_s);
-                auto score = [&](int v) {
-                    const int slot = v & 1, t = k.tile_of(v), n = done + t, buf = n & 1;
-                    wait(bar(&m->k_full[buf]), (n >> 1) & 1, abort_s);
-                    tc_fence_after();
+            const uint32_t tS = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + slot * D;
+            // Both issuers see every tile of keys and of values in order, so that neither can fall a whole turn behind (a parity wait tells
+            // a phase only from the one before it); tiles of the other slot are passed on at once.
+            int nk = 0, nv = 0, done = 0;   // tiles of keys, of values seen; of the units before
+            uint32_t p_parity = 0;
+            auto pass_keys = [&](int to) {
+                for (; nk < to; ++nk) {
+                    wait(bar(&m->k_full[nk & 1]), (nk >> 1) & 1, abort_s);
+                    if (lane == 0) mbar_arrive(bar(&m->k_empty[nk & 1]));
                     __syncwarp();
-                    if (!gone(abort_s) && elect_one()) {
-                        const uint64_t qd = descQ + (uint64_t)((k.wide ? slot * C::kQBytes : 0) >> 4), kd = descK + (uint64_t)((buf * C::kKBytes) >> 4);
+                }
+            };
+            auto pass_values = [&](int to) {
+                for (; nv < to; ++nv) {
+                    wait(bar(&m->v_full[nv & 1]), (nv >> 1) & 1, abort_s);
+                    if (lane == 0) mbar_arrive(bar(&m->v_empty[nv & 1]));
+                    __syncwarp();
+                }
+            };
+            Piece x;
+            for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
+                wait(bar(&m->q_full), seg & 1, abort_s);
+                const int step = x.step();
+                const uint64_t qd = descQ + (uint64_t)((x.wide ? slot * C::kQBytes : 0) >> 4);
+                auto score = [&](int t) {
+                    pass_keys(done + t);
+                    const int buf = nk & 1;
+                    wait(bar(&m->k_full[buf]), (nk >> 1) & 1, abort_s);
+                    ++nk;
+                    tc_fence_after();
+                    const bool go = !gone(abort_s);
+                    if (go && elect_one()) {
+                        const uint64_t kd = descK + (uint64_t)((buf * C::kKBytes) >> 4);
 #pragma unroll
                         for (int hf = 0; hf < C::kHalves; ++hf)
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
-                                mma_bf16_ss(tmem + kTmemS + slot * 128, qd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4),
-                                            kIdescQK, (hf | kk) != 0);
+                                mma_bf16_ss(tS, qd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
                         mma_commit(bar(&m->s_full[slot]));
-                        if (!k.wide || slot == 1) mma_commit(bar(&m->k_empty[buf]));
-                        if (v == k.visits - 1) mma_commit(bar(&m->q_empty));
+                        mma_commit(bar(&m->k_empty[buf]));
+                        if (t + step >= x.tiles) mma_commit(bar(&m->q_empty));
                     }
                     __syncwarp();
                 };
-                for (int v = 0; v < min(2, k.visits); ++v) score(v);
-                for (int v = 0; v < k.visits; ++v) {
-                    const int slot = v & 1, t = k.tile_of(v), n = done + t, buf = n & 1;
-                    const int slices = (k.valid(p, t) + 15) >> 4;
-                    const uint32_t tS = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + slot * D;
-                    wait(bar(&m->v_full[buf]), (n >> 1) & 1, abort_s);
+                const int t0 = x.first(slot);
+                if (t0 < x.tiles) {
 #pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
-                        wait(bar(&m->p_full[slot][half]), (p_parity >> slot) & 1, abort_s);
-                        tc_fence_after();
-                        __syncwarp();
-                        if (!gone(abort_s) && elect_one()) {
-                            const uint64_t vd = descV + (uint64_t)((buf * C::kVBytes + half * C::kVPage) >> 4);
+                    for (int t = t0 - step; t < x.tiles; t += step) {
+                        if (t >= t0) {
+                            pass_values(done + t);
+                            const int buf = nv & 1, slices = (x.valid(p.T, t) + 15) >> 4;
+                            wait(bar(&m->v_full[buf]), (nv >> 1) & 1, abort_s);
+                            ++nv;
+#pragma unroll 1
+                            for (int half = 0; half < 2; ++half) {
+                                wait(bar(&m->p_full[slot][half]), p_parity, abort_s);
+                                tc_fence_after();
+                                const bool go = !gone(abort_s);
+                                if (go && elect_one()) {
+                                    const uint64_t vd = descV + (uint64_t)((buf * C::kVBytes + half * C::kVPage) >> 4);
 #pragma unroll
-                            for (int kk = 0; kk < 4; ++kk)
-                                if (half * 4 + kk < slices)
-                                    mma_bf16_ts(tO, tS + (half * 4 + kk) * 8, vd + (uint64_t)((kk * 32) >> 4), kIdescPV, v >= 2 || half + kk != 0);
-                            if (half == 1) {
-                                if (!k.wide || slot == 1) mma_commit(bar(&m->v_empty[buf]));
-                                if (v + 2 >= k.visits) mma_commit(bar(&m->o_full[slot]));
+                                    for (int kk = 0; kk < 4; ++kk)
+                                        if (half * 4 + kk < slices)
+                                            mma_bf16_ts(tO, tS + (half * 4 + kk) * 8, vd + (uint64_t)((kk * 32) >> 4), kIdescPV, t != t0 || half + kk != 0);
+                                    if (half == 1) {
+                                        mma_commit(bar(&m->v_empty[buf]));
+                                        if (t + step >= x.tiles) mma_commit(bar(&m->o_full[slot]));
+                                    }
+                                }
+                                __syncwarp();
                             }
+                            p_parity ^= 1;
                         }
-                        __syncwarp();
+                        if (t + step < x.tiles) score(t + step);
                     }
-                    p_parity ^= 1u << slot;
-                    if (v + 2 < k.visits) score(v + 2);
+                } else {   // (a narrow piece of one tile: slot 1 has none)
+                    if (lane == 0) mbar_arrive(bar(&m->q_empty));
+                    __syncwarp();
                 }
-                done += k.tiles;
+                done += x.tiles;
+                pass_keys(done);
+                pass_values(done);
             }
             if (gone(abort_s)) __nanosleep(1000000);   // products that are still under way end before their operands go away
-        } else if (warp == kRejectWarp) {
-            reject_lengths<D>(p, blockIdx.x, gridDim.x, lane);
         }
     } else if (warp >= kUnpackWarp) {
         // ------------------------------------------------------------------ unpacking
@@ -435,30 +533,31 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         const uint32_t sixteen = *word;
         asm volatile("bar.sync 2, 128;" ::: "memory");
         int n = 0, raw = 0, trees = 0;   // tiles, slots of the ring, trees so far
-        while (!gone(abort_s) && k.next(p, list, seqs, lane)) {
-            for (int i = 0; i < k.tiles && !gone(abort_s); ++i, ++n) {
+        Piece x;
+        for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
+            for (int i = 0; i < x.tiles && !gone(abort_s); ++i, ++n) {
                 const int buf = n & 1;
                 const uint32_t kt = base + C::kOffK + buf * C::kKBytes, vt = base + C::kOffV + buf * C::kVBytes;
-                const bool tree = k.is_tree(i);
-                const int valid = k.valid(p, i);
+                const bool tree = x.is_tree(i);
+                const int valid = x.valid(p.T, i);
                 // keys
                 if (!wait(bar(&m->k_empty[buf]), ((n >> 1) & 1) ^ 1, abort_s)) break;
                 if (tree) {
                     unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
                     if (t < p.T) {
-                        const int a = p.parent[(size_t)k.u.b * p.T + t];
+                        const int a = p.parent[(size_t)x.b * p.T + t];
                         parents[t] = (unsigned char)a;
-                        if (!(t == 0 ? a == -1 : a >= 0 && a < t)) atomicOr(&m->flags[k.seg & (kAhead - 1)], kBadTree);
+                        if (!(t == 0 ? a == -1 : a >= 0 && a < t)) atomicOr(&m->flags[seg & (kAhead - 1)], kBadTree);
                     }
-                    copy_tree_keys<D>(p, k.u.b, k.u.h, kt, t);
+                    copy_tree_keys<D>(p, x.b, x.h, kt, t);
                     ++trees;
                 } else {
                     const int s = raw % kRawSlots;
                     if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
-                    if (m->raw_bad[s] && t == 0) atomicOr(&m->flags[k.seg & (kAhead - 1)], kBadPage);
-                    unpack_keys<D>(src, kt, 0, t, sixteen);
-                    if (valid > kPage) unpack_keys<D>(src + C::kPageBytes, kt, kPage, t, sixteen);
+                    if (m->raw_bad[s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
+#pragma unroll 1
+                    for (int page = 0; page * kPage < valid; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
                     ++raw;
@@ -469,14 +568,13 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 // values
                 if (!wait(bar(&m->v_empty[buf]), ((n >> 1) & 1) ^ 1, abort_s)) break;
                 if (tree) {
-                    if (copy_tree_values<D>(p, k.u.b, k.u.h, vt, t)) atomicOr(&m->poison[k.seg & (kAhead - 1)], 1);
+                    if (copy_tree_values<D>(p, x.b, x.h, vt, t)) atomicOr(&m->poison[seg & (kAhead - 1)], 1);
                 } else {
                     const int s = raw % kRawSlots;
                     if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
-                    // a page to 64 threads
-                    if (t < 64) unpack_values<D>(src, vt, min(valid, kPage), t, sixteen);
-                    else if (valid > kPage) unpack_values<D>(src + C::kPageBytes, vt + C::kVPage, valid - kPage, t - 64, sixteen);
+                    const int page = t >> 6;   // a page to 64 threads
+                    if (page * kPage < valid) unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t & 63, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
                     ++raw;
@@ -499,11 +597,11 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         int trees = 0;   // (both slots count all of them)
 
         // Queries of unit x: rows of this slot (wide) or this slot's half of the columns of all of them (narrow).
-        auto load_queries = [&](const Walk &x) {
-            const int r = x.u.rt * 256 + (x.wide ? slot * 128 : 0) + row;
+        auto load_queries = [&](const Piece &x) {
+            const int r = x.rt * 256 + (x.wide ? slot * 128 : 0) + row;
             const bool live = r < p.T * p.G;
-            const int j = live ? node_of(p, r) : 0, hq = x.u.h * p.G + (live ? r - j * p.G : 0);
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (((size_t)x.u.b * p.T + j) * p.Hq + hq) * D);
+            const int j = live ? node_of(p, r) : 0, hq = x.h * p.G + (live ? r - j * p.G : 0);
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (((size_t)x.b * p.T + j) * p.Hq + hq) * D);
             constexpr int kChunks = D / 8;
             const uint32_t dst = base + C::kOffQ + (x.wide ? slot * C::kQBytes : 0) + row * 128;
             const int c0 = x.wide ? 0 : slot * (kChunks / 2);
@@ -520,19 +618,29 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             fence_proxy_async();
             mbar_arrive(bar(&m->q_full));
         };
-        // (Given up or not, every thread goes through all units: the barriers among the softmax threads want that.)
-        bool more = k.next(p, list, seqs, lane);
+        // Whether there is another unit is decided together: a block that gives up may do so between two warps' looks at the ring, and the
+        // barriers among the softmax threads want all of them.
+        auto next_for_all = [&](Piece &y, int seg) {
+            const bool got = next_piece(m, y, seg, lane, abort_s);
+            int all;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((int)got) : "memory");
+            return all != 0;
+        };
+        Piece k;
+        int seg = 0;
+        bool more = next_for_all(k, 0);
         if (more) load_queries(k);
         while (more) {
-            const int grow = k.u.rt * 256 + (k.wide ? slot * 128 : 0) + row;   // among the head's rows
+            const int grow = k.rt * 256 + (k.wide ? slot * 128 : 0) + row;   // among the head's rows
             const bool live = grow < p.T * p.G;
             const bool warp_live = __any_sync(0xffffffffu, live);
             const int node = live ? node_of(p, grow) : 0;
             // a row without a query never asks for a higher maximum
             float mx = live ? -INFINITY : INFINITY, l = 0.f;
             const bool has_tree = k.is_tree(k.tiles - 1);
-            for (int v = slot; v < k.visits; v += 2) {
-                const int t = k.tile_of(v);
+            const int t_first = k.first(slot);
+#pragma unroll 1
+            for (int t = t_first; t < k.tiles; t += k.step()) {
                 wait(bar(&m->s_full[slot]), s_parity, abort_s);
                 s_parity ^= 1;
                 tc_fence_after();
@@ -542,13 +650,16 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(s + c * 32));
                     tmem_wait_ld();
                     auto f = [&](int i) { return __uint_as_float(s[i]); };
-                    if (k.is_tree(t)) {
-                        uint64_t lo = 0, hi = 0;   // the nodes this row sees
-                        if (live) {
+                    const int valid = k.valid(p.T, t);
+                    if (valid < kTileKeys || k.is_tree(t)) {   // the keys this row sees
+                        uint64_t lo = 0, hi = 0;
+                        if (!k.is_tree(t)) {
+                            lo = hi = ~0ull;
+                        } else if (live) {
                             if (p.anc) {
-                                lo = p.anc[((size_t)k.u.b * p.T + node) * 2];
-                                hi = p.anc[((size_t)k.u.b * p.T + node) * 2 + 1];
-                            } else if (!(*(volatile int32_t *)&m->flags[k.seg & (kAhead - 1)] & kBadTree)) {
+                                lo = p.anc[((size_t)k.b * p.T + node) * 2];
+                                hi = p.anc[((size_t)k.b * p.T + node) * 2 + 1];
+                            } else if (!(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
                                 const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
                                 for (int i = node; i != 255; i = parents[i]) {   // (strictly falling on a valid tree)
                                     if (i < 64) lo |= 1ull << i;
@@ -556,19 +667,12 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                                 }
                             }
                         }
-                        if (p.T < 64) lo &= (1ull << p.T) - 1;
-                        if (p.T < 128) hi &= p.T <= 64 ? 0 : (1ull << (p.T - 64)) - 1;
+                        if (valid < 64) lo &= (1ull << valid) - 1;
+                        if (valid < 128) hi &= valid <= 64 ? 0 : (1ull << (valid - 64)) - 1;
 #pragma unroll
                         for (int i = 0; i < 64; ++i) {
                             if (!((lo >> i) & 1)) s[i] = kNegInf;
                             if (!((hi >> i) & 1)) s[64 + i] = kNegInf;
-                        }
-                    } else {
-                        const int valid = k.valid(p, t);
-                        if (valid < kTileKeys) {
-#pragma unroll
-                            for (int i = 0; i < kTileKeys; ++i)
-                                if (i >= valid) s[i] = kNegInf;
                         }
                     }
                     float tops[4];
@@ -585,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         const float g = mx == now ? 1.f : ex2((mx - now) * p.scale_log2);   // (-inf before the first score: 0)
                         mx = now;
                         l *= g;
-                        if (v >= 2) {   // (the products before this tile's scores are done)
+                        if (t != t_first) {   // (the products before this tile's scores are done)
 #pragma unroll 1
                             for (int c = 0; c < D; c += 16) {
                                 uint32_t o[16];
@@ -629,17 +733,12 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 mbar_arrive(bar(&m->p_full[slot][1]));
             }
             // The next unit's queries, when this one's last scores are done; then this one's results.
-            const Walk x = k;
-            wait(bar(&m->q_empty), x.seg & 1, abort_s);
-            more = k.next(p, list, seqs, lane);
+            const Piece x = k;
+            const int seg_x = seg++;
+            wait(bar(&m->q_empty), seg_x & 1, abort_s);
+            more = next_for_all(k, seg);
             if (more) load_queries(k);
-            const bool slot_has[2] = {true, x.visits > 1};
-            float2 other = make_float2(-INFINITY, 0.f);
-            if (!x.wide) {
-                ml_s[slot * 128 + row] = make_float2(live ? mx : -INFINITY, l);
-                softmax_barrier();
-                other = ml_s[(slot ^ 1) * 128 + row];
-            }
+            const bool slot_has[2] = {true, x.wide || x.tiles > 1};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if (!slot_has[i]) continue;
@@ -648,9 +747,41 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 o_parity[i] ^= 1;
             }
             tc_fence_after();
-            int flag = *(volatile int32_t *)&m->flags[x.seg & (kAhead - 1)];
-            const bool poison = *(volatile int32_t *)&m->poison[x.seg & (kAhead - 1)] != 0;
+            int flag = *(volatile int32_t *)&m->flags[seg_x % kAhead];
             if (*abort_s || (int)blockIdx.x == p.give_up) flag |= kGaveUp;
+            if (has_tree && *(volatile int32_t *)&m->poison[seg_x % kAhead] && (x.wide || slot == ((x.tiles - 1) & 1)) && warp_live) {
+                // infinities and NaN were left out of the product: the rows that see them get them
+#pragma unroll 1
+                for (int n = 0; n < p.T && !(flag & kBadTree); ++n) {
+                    bool sees = false;
+                    if (live && p.anc) sees = (p.anc[((size_t)x.b * p.T + node) * 2 + (n >> 6)] >> (n & 63)) & 1;
+                    if (live && !p.anc)
+                        for (int i = node; i >= n; i = p.parent[(size_t)x.b * p.T + i]) sees |= i == n;
+                    const uint32_t *val = reinterpret_cast<const uint32_t *>(p.v_tree + (((size_t)x.b * p.T + n) * p.Hkv + x.h) * D);
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(tO + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t w = val[c / 2 + i];
+                            if (sees && nonfinite(w << 16)) o[2 * i] = __float_as_uint(__uint_as_float(o[2 * i]) + bf16lo(w));
+                            if (sees && nonfinite(w)) o[2 * i + 1] = __float_as_uint(__uint_as_float(o[2 * i + 1]) + bf16hi(w));
+                        }
+                        tmem_st16(tO + c, o);
+                    }
+                }
+                tmem_wait_st();
+                tc_fence_before();
+            }
+            float2 other = make_float2(-INFINITY, 0.f);
+            if (!x.wide) {
+                ml_s[slot * 128 + row] = make_float2(live ? mx : -INFINITY, l);
+                softmax_barrier();
+                tc_fence_after();
+                other = ml_s[(slot ^ 1) * 128 + row];
+            }
             // weights of the slots' results; a narrow unit's slot writes half of the columns
             float w_own = 1.f, w_other = 0.f;
             if (!x.wide) {
@@ -665,8 +796,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             const uint32_t tOwn = tmem + kTmemO + (x.wide ? slot * D : 0) + lane_base, tOther = tmem + kTmemO + D + lane_base;
             // narrow: slot 0's result with its weight, then slot 1's
             const float w0 = x.wide ? 1.f : slot == 0 ? w_own : w_other, w1 = slot == 0 ? w_other : w_own;
-            const size_t orow = ((size_t)x.u.b * p.T + node) * p.Hq + x.u.h * p.G + (grow - node * p.G);
-            const int share = 2 * blockIdx.x + (x.u.t0 == 0 ? 1 : 0);
+            const size_t orow = ((size_t)x.b * p.T + node) * p.Hq + x.h * p.G + (grow - node * p.G);
+            const int share = 2 * blockIdx.x + (x.t0 == 0 ? 1 : 0);
             const size_t srow = (size_t)share * 256 + (x.wide ? slot * 128 : 0) + row;
             const float inv = flag || l == 0.f ? 0.f : 1.f / l;   // (a row that sees nothing: zeros)
             if (warp_live) {
@@ -682,28 +813,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         if (!x.wide && slot_has[1]) y = fmaf(__uint_as_float(o1[i]), w1, y);
                         o[i] = __float_as_uint(y);
                     }
-                    if (poison && has_tree && live) {   // infinities and NaN were left out of the product: the rows that see them get them
-                        for (int n = 0; n < p.T; ++n) {
-                            bool sees = false;
-                            if (p.anc) sees = (p.anc[((size_t)x.u.b * p.T + node) * 2 + (n >> 6)] >> (n & 63)) & 1;
-                            else for (int i = node; i != -1; i = p.parent[(size_t)x.u.b * p.T + i]) {
-                                if (i == n) sees = true;
-                                if (flag & kBadTree) break;
-                            }
-                            if (!sees) continue;
-                            const __nv_bfloat16 *val = p.v_tree + (((size_t)x.u.b * p.T + n) * p.Hkv + x.u.h) * D + c;
-                            for (int i = 0; i < 16; ++i) {
-                                const uint32_t bits = (uint32_t)*reinterpret_cast<const uint16_t *>(val + i) << 16;
-                                if (nonfinite(bits)) {
-#pragma unroll
-                                    for (int e = 0; e < 16; ++e)
-                                        if (e == i) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float(bits));
-                                }
-                            }
-                        }
-                    }
                     if (!live) continue;
-                    if (x.whole) {
+                    if (x.whole()) {
                         uint4 y[2];
                         uint32_t *w = reinterpret_cast<uint32_t *>(y);
 #pragma unroll
@@ -718,27 +829,27 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     }
                 }
                 if (live && (x.wide || slot == 0)) {
-                    if (!x.whole) p.partial_ml[srow] = make_float2(mx, l);
+                    if (!x.whole()) p.partial_ml[srow] = make_float2(mx, l);
                     else if (p.lse) p.lse[orow] = flag ? 0.f : fmaf(mx, p.scale, log2f(l) * 0.6931471805599453f);
                 }
             }
             tc_fence_before();
             softmax_barrier();   // both slots have read what the next unit's value products and results will overwrite
             if (tid == 0) {
-                m->flags[x.seg & (kAhead - 1)] = 0;
-                m->poison[x.seg & (kAhead - 1)] = 0;
-                if (x.whole) {
-                    note(p, x.u.b, flag, 0);
+                m->flags[seg_x % kAhead] = 0;
+                m->poison[seg_x % kAhead] = 0;
+                if (x.whole()) {
+                    note(p, x.b, flag, 0);
                 } else {
                     p.flags[share] = flag;
-                    const int c0 = list.worker_of(x.u.first_entry(kUnitCost)), c1 = list.worker_of(x.u.last_entry(kUnitCost));
-                    m->task[share & 1] = ShareTask{x.u.b, x.u.h, x.u.rt, x.rows, c0, c1};
+                    m->task[share & 1] = ShareTask{x.b, x.h, x.rt, x.rows, x.c0, x.c1};
                 }
             }
             trees += has_tree;
         }
+        end_barrier<3>();
+        end_barrier<4>();
         // Units that other blocks have shares of: at most one that goes on from the block before, one that goes on in the next.
-        softmax_barrier();
         if (tid < 2 && m->task[tid].block0 >= 0) {
             __threadfence();
             if (atomicAdd(p.counters + m->task[tid].block0, 1) == m->task[tid].block1 - m->task[tid].block0) {
