@@ -2,7 +2,7 @@
 //
 // Bound: the tensor pipe and the exponentials, 2048 cycles each for 256 query rows and 128 keys; what 4 bits add is turning
 // numbers into bf16 operands, 16384 of them for each, once for all rows that share them.  So a thread block (one per SM) has up to
-// 256 rows of one KV head, two slots of 128, and four warps of it do nothing but unpack: a tile of 128 keys (two pages) becomes
+// 256 rows of one KV head, two slots of 128, and eight warps of it do nothing but unpack: a tile of 128 keys (two pages) becomes
 // the rows of K, and its values the rows of V^T (position pairs are neighbours in the pages, so a pair of numbers is a
 // pair of bf16 along the value product's inner axis as it stands), in the 128-byte swizzle of the matrix instructions.
 //
@@ -10,10 +10,12 @@
 //                    score exceeds it by 2^8 (O is rescaled in tensor memory then); probabilities replace the scores as bf16 and are the
 //                    value product's A operand from there.  At a unit's end they fetch the next one's queries, so that its first
 //                    products run beside the results being written.
-//   warps 8-11       unpack pages (and copy the tree's own keys and values) into the tiles
-//   warp 12          brings pages into a ring by bulk copies
-//   warps 13, 14     issue the products of slot 0 and 1: S = Q K^T, O += P V.  (One warp for both was busy all the time: 3 us a tile.)
-//   warp 15          finds the block's units and puts them into a small ring that the others read; zero rows for sequences whose
+//   warps 8-15       unpack pages (and copy the tree's own keys and values) into the tiles
+//   warp 16          brings pages into a ring by bulk copies
+//   warps 17, 18     issue the products of slot 0 and 1: S = Q K^T, O += P V.  In a wide piece they take turns with their score products,
+//                    and slot 1 begins half a step late: left to themselves the slots fall into step, both at the exponentials and
+//                    then both at the products
+//   warp 19          finds the block's units and puts them into a small ring that the others read; zero rows for sequences whose
 //                    length cannot be.  (With the search in every role the code did not fit the instruction caches any more, and
 //                    warps stood waiting for instructions.)
 // A unit of more than 128 rows is wide: each slot has its own rows and both work on every tile.  A narrow one has up to 128 rows;
@@ -35,12 +37,14 @@ namespace {
 
 using namespace q4;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 640;
 constexpr int kSoftmaxThreads = 256;
-constexpr int kUnpackWarp = 8, kLoadWarp = 12, kMmaWarp = 13, kListWarp = 15;
-constexpr int kReaders = 15;       // warps that read the ring of units: all but kListWarp
-// Registers of a thread: softmax, unpacking, the rest; 128 (2 x 184 + 80 + 64) = 65536, what the block is launched with.
-constexpr int kRegsSoftmax = 184, kRegsUnpack = 80, kRegsRest = 64;
+constexpr int kUnpackWarp = 8, kLoadWarp = 16, kMmaWarp = 17, kListWarp = 19;
+constexpr int kUnpackThreads = 256, kUnpackWarps = 8;
+constexpr int kReaders = 19;       // warps that read the ring of units: all but kListWarp
+// Registers of a thread: softmax, unpacking, the rest: 256 x 112 + 256 x 72 + 128 x 96 = 59392 of the 640 x 96 that the block is launched with.
+constexpr int kRegsSoftmax = 112, kRegsUnpack = 72;
+constexpr int kLateStart = 6;      // tiles of a wide piece from which slot 1 begins half a step behind slot 0
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
 constexpr int kUnitCost = 6;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = 8;     // of a range
@@ -87,7 +91,7 @@ struct Piece {
 };
 struct Bars {
     uint64_t raw_full[kRawSlots], raw_empty[kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2], piece_full[kAhead], piece_empty[kAhead];
+    uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2], turn[2], piece_full[kAhead], piece_empty[kAhead];
     uint32_t tmem_base;
     int32_t abort;
     int32_t raw_bad[kRawSlots];   // a page outside the pool among the slot's
@@ -136,7 +140,7 @@ __device__ __forceinline__ bool next_piece(Bars *m, Piece &x, int seg, int lane,
     return x.tiles > 0;
 }
 
-// ---- unpacking, by 128 threads (`t` among them)
+// ---- unpacking (`t`: among the 128 threads of a page)
 // A page of keys into rows row0 .. + 63 of a K tile.  Thread (w, g): word w of the positions 8 j + g (at head_dim 64, of half of the j).
 template <int D>
 __device__ __forceinline__ void unpack_keys(uint32_t raw, uint32_t tile, int row0, int t, uint32_t sixteen) {
@@ -166,12 +170,12 @@ __device__ __forceinline__ void unpack_keys(uint32_t raw, uint32_t tile, int row
     if (nan_bits(codes[0]) | nan_bits(codes[1]) | nan_bits(codes[2]) | nan_bits(codes[3])) go(std::false_type());
     else go(std::true_type());
 }
-// A page of values into a page of V^T, `valid` of its positions committed (the others become 0).  64 threads: (q, z) = the positions 8 q .. + 7 of
-// the elements z D/8 .. + D/8 - 1.
+// A page of values into a page of V^T, `valid` of its positions committed (the others become 0).  Thread (q, z, f): the positions 8 q .. + 7 of half f
+// of the elements z D/8 .. + D/8 - 1.
 template <int D>
 __device__ __forceinline__ void unpack_values(uint32_t raw, uint32_t page, int valid, int t, uint32_t sixteen) {
-    constexpr int kWords = D / 32;
-    const int q = t & 7, z = t >> 3;
+    constexpr int kWords = D / 64;
+    const int q = t & 7, z = (t >> 3) & 7, f = t >> 6;
     if (8 * q >= ((valid + 15) & ~15)) return;   // (behind the last slice that is multiplied)
     // The four position pairs 4 q + e, each lane's in an order that begins with e = q mod 4 (in one order for all, eight lanes would meet in
     // the same banks): k-th load e = (k + q) mod 4.
@@ -179,9 +183,9 @@ __device__ __forceinline__ void unpack_values(uint32_t raw, uint32_t page, int v
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int e = (k + q) & 3, pr = 4 * q + e;
-        const uint32_t at = raw + pr * D + v_chunk<D>(pr, z) * (D / 8);
-        if constexpr (D == 128) { const uint4 x = lds128(at); w[k][0] = x.x; w[k][1] = x.y; w[k][2] = x.z; w[k][3] = x.w; }
-        else { const uint2 x = lds64(at); w[k][0] = x.x; w[k][1] = x.y; }
+        const uint32_t at = raw + pr * D + v_chunk<D>(pr, z) * (D / 8) + f * (D / 16);
+        if constexpr (D == 128) { const uint2 x = lds64(at); w[k][0] = x.x; w[k][1] = x.y; }
+        else w[k][0] = lds32(at);
         codes[k] = lds16(raw + scales_at(D) + ((((D == 128 ? z : z >> 1) * 4 + e) * 8 + q) * 2));
     }
     // back in order: turned by q mod 4
@@ -219,9 +223,10 @@ __device__ __forceinline__ void unpack_values(uint32_t raw, uint32_t page, int v
     }
 #pragma unroll
     for (int y = 0; y < kWords; ++y) {
-        // row d = z D/8 + 4 y + i; D/8 is a multiple of 8
-        const uint32_t rows = page + z * (D / 8) * 128;
-        auto row = [&](int i) { return rows + (4 * y + i) * 128 + ((q ^ ((4 * y + i) & 7)) << 4); };
+        // row d = z D/8 + f D/16 + 4 y + i
+        const uint32_t rows = page + (z * (D / 8) + f * (D / 16)) * 128;
+        const int turn = D == 128 ? 0 : 4 * f;   // (of the row's number, what its place in the swizzle goes by)
+        auto row = [&](int i) { return rows + (4 * y + i) * 128 + ((q ^ ((turn + 4 * y + i) & 7)) << 4); };
         sts128(row(0), pair<0>(w[0][y], s[0], sixteen), pair<0>(w[1][y], s[1], sixteen), pair<0>(w[2][y], s[2], sixteen), pair<0>(w[3][y], s[3], sixteen));
         sts128(row(1), pair<1>(w[0][y], s[0], sixteen), pair<1>(w[1][y], s[1], sixteen), pair<1>(w[2][y], s[2], sixteen), pair<1>(w[3][y], s[3], sixteen));
         sts128(row(2), pair<2>(w[0][y], s[0], sixteen), pair<2>(w[1][y], s[1], sixteen), pair<2>(w[2][y], s[2], sixteen), pair<2>(w[3][y], s[3], sixteen));
@@ -233,7 +238,7 @@ template <int D>
 __device__ __forceinline__ void copy_tree_keys(const Q4AttnParams &p, int b, int h, uint32_t tile, int t) {
     constexpr int kChunks = D / 8;
 #pragma unroll 4
-    for (int i = t; i < p.T * kChunks; i += 128) {
+    for (int i = t; i < p.T * kChunks; i += kUnpackThreads) {
         const int r = i / kChunks, w = i % kChunks;
         const uint4 x = *reinterpret_cast<const uint4 *>(p.k_tree + (((size_t)b * p.T + r) * p.Hkv + h) * D + w * 8);
         sts128(tile + (w >> 3) * Cfg<D>::kBlock + r * 128 + (((w & 7) ^ (r & 7)) << 4), x.x, x.y, x.z, x.w);
@@ -247,7 +252,7 @@ __device__ __forceinline__ bool copy_tree_values(const Q4AttnParams &p, int b, i
     const int groups = (p.T + 15) / 16 * 2;   // of eight nodes, up to the last slice's end
     bool dirty = false;
 #pragma unroll 1
-    for (int i = t; i < groups * kChunks; i += 128) {
+    for (int i = t; i < groups * kChunks; i += kUnpackThreads) {
         const int z = i % kChunks, q = i / kChunks;
         uint4 x[8];
 #pragma unroll
@@ -283,12 +288,13 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     if (tid == 0) {
         for (int i = 0; i < kRawSlots; ++i) {
             mbar_init(bar(&m->raw_full[i]), 1);
-            mbar_init(bar(&m->raw_empty[i]), 4);
+            mbar_init(bar(&m->raw_empty[i]), kUnpackWarps);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&m->k_full[i]), 4);
+            mbar_init(bar(&m->k_full[i]), kUnpackWarps);
             mbar_init(bar(&m->k_empty[i]), 2);
-            mbar_init(bar(&m->v_full[i]), 4);
+            mbar_init(bar(&m->v_full[i]), kUnpackWarps);
+            mbar_init(bar(&m->turn[i]), 1);
             mbar_init(bar(&m->v_empty[i]), 2);
             mbar_init(bar(&m->s_full[i]), 1);
             mbar_init(bar(&m->p_full[i][0]), 128);
@@ -307,6 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         m->abort = (base & 1023u) ? 1 : 0;   // (the swizzled tiles want 1024-byte alignment; never seen otherwise, but checked)
         fence_mbar_init();
         fence_proxy_async();
+        mbar_arrive(bar(&m->turn[0]));   // slot 0 has the first turn
     }
     if (warp == kMmaWarp) {
         tmem_alloc(smem_u32(&m->tmem_base), kTmemCols);
@@ -333,8 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     list.per_block = 1;
     list.cut(max(1, min(p.n_ctas, list.W / kMinEntries)));
 
-    if (warp >= 12) {
-        regs_dec<kRegsRest>();
+    if (warp >= kLoadWarp) {
         if (warp == kListWarp) {
             // ------------------------------------------------------------------ units
             int w = 0, w_end = 0;
@@ -442,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             // Both issuers see every tile of keys and of values in order, so that neither can fall a whole turn behind (a parity wait tells
             // a phase only from the one before it); tiles of the other slot are passed on at once.
             int nk = 0, nv = 0, done = 0;   // tiles of keys, of values seen; of the units before
-            uint32_t p_parity = 0;
+            uint32_t p_parity = 0, turn_parity = 0;
             auto pass_keys = [&](int to) {
                 for (; nk < to; ++nk) {
                     wait(bar(&m->k_full[nk & 1]), (nk >> 1) & 1, abort_s);
@@ -462,11 +468,20 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 wait(bar(&m->q_full), seg & 1, abort_s);
                 const int step = x.step();
                 const uint64_t qd = descQ + (uint64_t)((x.wide ? slot * C::kQBytes : 0) >> 4);
+                const bool late = x.wide && slot == 0 && x.tiles >= kLateStart;
+                auto pass_turn = [&]() {
+                    if (x.wide && lane == 0) mbar_arrive(bar(&m->turn[slot ^ 1]));
+                    __syncwarp();
+                };
                 auto score = [&](int t) {
                     pass_keys(done + t);
                     const int buf = nk & 1;
                     wait(bar(&m->k_full[buf]), (nk >> 1) & 1, abort_s);
                     ++nk;
+                    if (x.wide) {
+                        wait(bar(&m->turn[slot]), turn_parity, abort_s);
+                        turn_parity ^= 1;
+                    }
                     tc_fence_after();
                     const bool go = !gone(abort_s);
                     if (go && elect_one()) {
@@ -481,6 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         if (t + step >= x.tiles) mma_commit(bar(&m->q_empty));
                     }
                     __syncwarp();
+                    if (!(late && t == 0)) pass_turn();
                 };
                 const int t0 = x.first(slot);
                 if (t0 < x.tiles) {
@@ -494,6 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
 #pragma unroll 1
                             for (int half = 0; half < 2; ++half) {
                                 wait(bar(&m->p_full[slot][half]), p_parity, abort_s);
+                                if (late && t == 0 && half == 0) pass_turn();
                                 tc_fence_after();
                                 const bool go = !gone(abort_s);
                                 if (go && elect_one()) {
@@ -529,9 +546,9 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         const int t = tid - kUnpackWarp * 32;
         volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + C::kOffMl);   // (an opaque constant: see pair())
         if (t == 0) *word = 0x41804180u;
-        asm volatile("bar.sync 2, 128;" ::: "memory");
+        asm volatile("bar.sync 2, 256;" ::: "memory");
         const uint32_t sixteen = *word;
-        asm volatile("bar.sync 2, 128;" ::: "memory");
+        asm volatile("bar.sync 2, 256;" ::: "memory");
         int n = 0, raw = 0, trees = 0;   // tiles, slots of the ring, trees so far
         Piece x;
         for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
@@ -556,8 +573,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
                     if (m->raw_bad[s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
-#pragma unroll 1
-                    for (int page = 0; page * kPage < valid; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
+                    const int page = t >> 7;   // a page to 128 threads
+                    if (page * kPage < valid) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t & 127, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
                     ++raw;
@@ -573,8 +590,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     const int s = raw % kRawSlots;
                     if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
-                    const int page = t >> 6;   // a page to 64 threads
-                    if (page * kPage < valid) unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t & 63, sixteen);
+                    const int page = t >> 7;
+                    if (page * kPage < valid) unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t & 127, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
                     ++raw;
@@ -645,45 +662,53 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 s_parity ^= 1;
                 tc_fence_after();
                 if (warp_live) {
-                    uint32_t s[128];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(s + c * 32));
-                    tmem_wait_ld();
-                    auto f = [&](int i) { return __uint_as_float(s[i]); };
                     const int valid = k.valid(p.T, t);
-                    if (valid < kTileKeys || k.is_tree(t)) {   // the keys this row sees
-                        uint64_t lo = 0, hi = 0;
-                        if (!k.is_tree(t)) {
-                            lo = hi = ~0ull;
-                        } else if (live) {
-                            if (p.anc) {
-                                lo = p.anc[((size_t)k.b * p.T + node) * 2];
-                                hi = p.anc[((size_t)k.b * p.T + node) * 2 + 1];
-                            } else if (!(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
+                    const bool masked = valid < kTileKeys || k.is_tree(t);
+                    uint64_t sees[2] = {~0ull, ~0ull};   // the keys this row sees
+                    if (masked) {
+                        if (k.is_tree(t)) {
+                            sees[0] = sees[1] = 0;
+                            if (live && p.anc) {
+                                sees[0] = p.anc[((size_t)k.b * p.T + node) * 2];
+                                sees[1] = p.anc[((size_t)k.b * p.T + node) * 2 + 1];
+                            } else if (live && !(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
                                 const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
                                 for (int i = node; i != 255; i = parents[i]) {   // (strictly falling on a valid tree)
-                                    if (i < 64) lo |= 1ull << i;
-                                    else hi |= 1ull << (i - 64);
+                                    if (i < 64) sees[0] |= 1ull << i;
+                                    else sees[1] |= 1ull << (i - 64);
                                 }
                             }
                         }
-                        if (valid < 64) lo &= (1ull << valid) - 1;
-                        if (valid < 128) hi &= valid <= 64 ? 0 : (1ull << (valid - 64)) - 1;
+                        if (valid < 64) sees[0] &= (1ull << valid) - 1;
+                        if (valid < 128) sees[1] &= valid <= 64 ? 0 : (1ull << (valid - 64)) - 1;
+                    }
+                    // Half a tile's scores at a time, twice: for the maximum, then for the probabilities.  (All 128 in registers leave none
+                    // for the warps that unpack; tensor memory is read in a fraction of the time that the exponentials take.)
+                    uint32_t x[2][32];
+                    auto f = [&](int i) { return __uint_as_float(x[i >> 5][i & 31]); };
+                    auto fetch = [&](int half) {
+                        tmem_ld32(tS + half * 64, x[0]);
+                        tmem_ld32(tS + half * 64 + 32, x[1]);
+                        tmem_wait_ld();
+                        if (masked) {
+                            const uint64_t bits = sees[half];
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) {
-                            if (!((lo >> i) & 1)) s[i] = kNegInf;
-                            if (!((hi >> i) & 1)) s[64 + i] = kNegInf;
+                            for (int i = 0; i < 64; ++i)
+                                if (!((bits >> i) & 1)) x[i >> 5][i & 31] = kNegInf;
                         }
-                    }
-                    float tops[4];
+                    };
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        fetch(half);
+                        float a = max3(f(0), f(1), f(2)), b = max3(f(3), f(4), f(5));
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float a = max3(f(c * 32), f(c * 32 + 1), f(c * 32 + 2));
-#pragma unroll
-                        for (int i = 3; i < 31; i += 2) a = max3(a, f(c * 32 + i), f(c * 32 + i + 1));
-                        tops[c] = fmaxf(a, f(c * 32 + 31));
+                        for (int i = 6; i < 62; i += 4) {
+                            a = max3(a, f(i), f(i + 1));
+                            b = max3(b, f(i + 2), f(i + 3));
+                        }
+                        top = fmaxf(top, fmaxf(max3(a, f(62), f(63)), b));
                     }
-                    const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
                     if (__any_sync(0xffffffffu, top > mx + by)) {
                         const float now = fmaxf(mx, top);
                         const float g = mx == now ? 1.f : ex2((mx - now) * p.scale_log2);   // (-inf before the first score: 0)
@@ -706,31 +731,31 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     const float from = mx == -INFINITY ? 0.f : -mx;
                     const float2 from2 = make_float2(from, from), sc = make_float2(p.scale_log2, p.scale_log2);
                     float2 sum = make_float2(0.f, 0.f);
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {   // (P of a half is written over scores that have been read)
+                        fetch(half);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t pk[16];
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t pk[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float2 x = __fmul2_rn(__fadd2_rn(make_float2(f(c * 32 + 2 * i), f(c * 32 + 2 * i + 1)), from2), sc);
-                            const float2 e = make_float2(ex2(x.x), ex2(x.y));
-                            sum = __fadd2_rn(sum, e);
-                            pk[i] = pack(e.x, e.y);
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 y = __fmul2_rn(__fadd2_rn(make_float2(f(c * 32 + 2 * i), f(c * 32 + 2 * i + 1)), from2), sc);
+                                const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                                sum = __fadd2_rn(sum, e);
+                                pk[i] = pack(e.x, e.y);
+                            }
+                            tmem_st16(tS + half * 32 + c * 16, pk);
                         }
-                        tmem_st16(tS + c * 16, pk);
-                        if (c == 1) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            mbar_arrive(bar(&m->p_full[slot][0]));
-                        }
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(bar(&m->p_full[slot][half]));
                     }
                     l += sum.x + sum.y;
-                    tmem_wait_st();
                 } else {
                     tc_fence_before();
                     mbar_arrive(bar(&m->p_full[slot][0]));
+                    mbar_arrive(bar(&m->p_full[slot][1]));
                 }
-                tc_fence_before();
-                mbar_arrive(bar(&m->p_full[slot][1]));
             }
             // The next unit's queries, when this one's last scores are done; then this one's results.
             const Piece x = k;
