@@ -77,7 +77,7 @@ reader_status convert(bool store, reader_ctx *ctx, const reader_kv_cache *from, 
 
 // ---- attention
 struct Q4Ws {
-    size_t counters, flags, partial_ml, partial_o, total;
+    size_t counters, flags, partial_ml, partial_o, tasks, total;
 };
 Q4Ws q4_ws(const reader_ctx *ctx, int D) {
     Q4Ws w{};
@@ -88,6 +88,7 @@ Q4Ws q4_ws(const reader_ctx *ctx, int D) {
     w.flags = take(sizeof(int32_t) * 2 * (size_t)ctx->n_sm);
     w.partial_ml = take(sizeof(float2) * rows);
     w.partial_o = take(sizeof(float) * rows * D);
+    w.tasks = take(sizeof(ShareTask) * (size_t)ctx->n_sm);
     w.total = at;
     return w;
 }
@@ -269,6 +270,7 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
     p.flags = reinterpret_cast<int32_t *>(ws + w.flags);
     p.partial_ml = reinterpret_cast<float2 *>(ws + w.partial_ml);
     p.partial_o = reinterpret_cast<float *>(ws + w.partial_o);
+    p.tasks = reinterpret_cast<ShareTask *>(ws + w.tasks);
     p.inv_G = (unsigned)((((uint64_t)1 << 32) + p.G - 1) / p.G);
     const bool few = (int64_t)T * p.G <= kQ4FewRows;
     if (reader_status s = (few ? launch_q4_attn_rows : launch_q4_attn_sm100)(&ctx->q4_attr, p, ctx->n_sm, (cudaStream_t)stream)) return s;

@@ -10,6 +10,10 @@ constexpr int kQ4ShareRows = 512;   // (a block of the many-rows kernel: two sha
 constexpr int kQ4MaxBatch = 1 << 16;
 constexpr int kQ4MaxGroup = 1 << 12;   // (128 nodes: 128 G^2 < 2^32, as the division by G wants it)
 
+struct ShareTask {   // a unit that the thread blocks block0 .. block1 have shares of
+    int b, h, rt, rows, block0, block1;   // block0 < 0: none
+};
+
 struct Q4AttnParams {
     const __nv_bfloat16 *q, *k_tree, *v_tree;
     const unsigned char *k_pool, *v_pool;
@@ -27,6 +31,7 @@ struct Q4AttnParams {
     int32_t *flags;            // [2 * thread blocks] what is wrong with a block's shares
     float2 *partial_ml;        // [shares][rows] largest score, sum: of workers, behind them of blocks
     float *partial_o;          // [shares][rows][D]
+    ShareTask *tasks;          // [thread blocks] the unit that a block begins and others go on with (many-rows kernel)
     int n_rt;                  // units of a KV head
     unsigned inv_G;            // 2^32 / G, rounded up
     int n_ctas;                // thread blocks (list form)

@@ -24,9 +24,10 @@
 // Tensor memory: S of either slot (128 columns each; P over its first 64), O of either slot.  The products of a slot are issued by one
 // thread and run in order, so S[i + 1] may be written over P[i] as soon as the value product that reads it has been issued.
 //
-// Work: a flat list of tiles cut into equal ranges, one per thread block, shares of units in several ranges merged by the block that
-// comes last (q4_attn_common.cuh).  Bytes that are not committed never reach a product: their scores become -inf, and their values 0 or
+// Work: a flat list of tiles cut into equal ranges, one per thread block (q4_attn_common.cuh); shares of units in several ranges are merged by
+// a launch behind.  Bytes that are not committed never reach a product: their scores become -inf, and their values 0 or
 // not multiplied at all (16-key slices behind the end).  Every wait is bounded: a block that gives up reports all its units.
+#include <algorithm>
 #include <type_traits>
 
 #include "prompt_ptx.cuh"
@@ -74,13 +75,10 @@ struct Cfg {
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
-struct ShareTask {   // a unit that other blocks have shares of
-    int b, h, rt, rows, block0, block1;   // block0 < 0: none
-};
 // A unit as the roles see it: its tiles t0 .. t0 + tiles - 1 are this block's.
 struct Piece {
     int b, h, rt, L, npages, ntiles, t0, tiles;   // tiles = 0: no more units
-    int wide, rows, c0, c1;                       // rows of the unit; the blocks c0 .. c1 have it in common
+    int wide, rows, last;                         // rows of the unit; the block that has its last tile
     __device__ __forceinline__ bool whole() const { return tiles == ntiles; }
     // committed tiles come first, the tree's is the last
     __device__ __forceinline__ bool is_tree(int tile) const { return t0 + tile == ntiles - 1; }
@@ -97,9 +95,8 @@ struct Bars {
     int32_t raw_bad[kRawSlots];   // a page outside the pool among the slot's
     int32_t flags[kAhead];        // what is wrong with unit i mod kAhead
     int32_t poison[kAhead];       // its tree has infinities or NaN among the values
-    int32_t last[2];
     int32_t warp_sum[kThreads / 32];
-    ShareTask task[2];
+    ShareTask task;               // the unit that this block begins and others go on with
     Piece piece[kAhead];
 };
 static_assert(sizeof(Bars) <= 1024, "barrier block");
@@ -300,9 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             mbar_init(bar(&m->p_full[i][0]), 128);
             mbar_init(bar(&m->p_full[i][1]), 128);
             mbar_init(bar(&m->o_full[i]), 1);
-            m->task[i].block0 = -1;
-            m->last[i] = 0;
         }
+        m->task.block0 = -1;
         mbar_init(bar(&m->q_full), kSoftmaxThreads);
         mbar_init(bar(&m->q_empty), 2);
         for (int i = 0; i < kAhead; ++i) {
@@ -354,11 +350,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     const Unit u = unit_at(p, list, seqs, w, w_end, lane);
                     w += u.entries;
                     if (!u.any) continue;
-                    x = Piece{u.b, u.h, u.rt, u.L, u.npages, u.ntiles, u.t0, u.t1 - u.t0, u.weight == 2, min(256, p.T * p.G - u.rt * 256), 0, 0};
-                    if (!x.whole()) {
-                        x.c0 = list.worker_of(u.first_entry(kUnitCost));
-                        x.c1 = list.worker_of(u.last_entry(kUnitCost));
-                    }
+                    x = Piece{u.b, u.h, u.rt, u.L, u.npages, u.ntiles, u.t0, u.t1 - u.t0, u.weight == 2, min(256, p.T * p.G - u.rt * 256), 0};
+                    if (!x.whole()) x.last = list.worker_of(u.last_entry(kUnitCost));
                     break;
                 }
                 const int i = seg % kAhead;
@@ -389,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     } else if (lane == 0) {
                         const int i = u.t0 == 0 ? 1 : 0;
                         p.flags[2 * blockIdx.x + i] = kGaveUp;
-                        m->task[i] = ShareTask{u.b, u.h, u.rt, rows, list.worker_of(u.first_entry(kUnitCost)), list.worker_of(u.last_entry(kUnitCost))};
+                        if (i) m->task = ShareTask{u.b, u.h, u.rt, rows, (int)blockIdx.x, list.worker_of(u.last_entry(kUnitCost))};
                     }
                 }
             }
@@ -867,40 +860,14 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     note(p, x.b, flag, 0);
                 } else {
                     p.flags[share] = flag;
-                    m->task[share & 1] = ShareTask{x.b, x.h, x.rt, x.rows, x.c0, x.c1};
+                    if (share & 1) m->task = ShareTask{x.b, x.h, x.rt, x.rows, (int)blockIdx.x, x.last};
                 }
             }
             trees += has_tree;
         }
         end_barrier<3>();
         end_barrier<4>();
-        // Units that other blocks have shares of: at most one that goes on from the block before, one that goes on in the next.
-        if (tid < 2 && m->task[tid].block0 >= 0) {
-            __threadfence();
-            if (atomicAdd(p.counters + m->task[tid].block0, 1) == m->task[tid].block1 - m->task[tid].block0) {
-                __threadfence();
-                m->last[tid] = 1;
-            }
-        }
-        softmax_barrier();
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            if (!m->last[i]) continue;
-            const ShareTask t = m->task[i];
-            const int count = t.block1 - t.block0 + 1;
-            auto slot_of = [&](int n) { return 2 * (t.block0 + n) + (n == 0 ? 1 : 0); };
-            int flag = 0;
-            for (int n = lane; n < count; n += 32) flag |= __ldcg(p.flags + slot_of(n));
-            flag = __reduce_or_sync(0xffffffffu, flag);
-            if (warp == 0) note(p, t.b, flag, lane);
-            for (int r = warp; r < t.rows; r += 8) {
-                const int g = t.rt * 256 + r, j = node_of(p, g);
-                const Row y = merge_row<D>(
-                    count, p.scale_log2, [&](int n) { return __ldcg(p.partial_ml + (size_t)slot_of(n) * 256 + r); },
-                    [&](int n) { return __ldcg(reinterpret_cast<const float4 *>(p.partial_o + ((size_t)slot_of(n) * 256 + r) * D + lane * 4)); });
-                put_row<D>(p, ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G), y, flag);
-            }
-        }
+        if (tid == 0) p.tasks[blockIdx.x] = m->task;
     }
     tc_fence_before();
     __syncthreads();
@@ -908,6 +875,28 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
+}
+
+// Units that several blocks have shares of: eight rows of the one that block blockIdx.x of the attention begins, a warp to a row.  (A launch of its
+// own: the block that came last did this at first, and took 25 us for the shares of 128 rows and 60 us for those of 256, the others waiting.)
+template <int D>
+__global__ void __launch_bounds__(256) q4_attn_merge_kernel(const __grid_constant__ Q4AttnParams p) {
+    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    pdl_wait();
+    pdl_launch_dependents();
+    const ShareTask t = p.tasks[blockIdx.x];
+    if (t.block0 < 0 || r >= t.rows) return;
+    const int count = t.block1 - t.block0 + 1;
+    auto slot_of = [&](int n) { return 2 * (t.block0 + n) + (n == 0 ? 1 : 0); };
+    int flag = 0;
+    for (int n = lane; n < count; n += 32) flag |= p.flags[slot_of(n)];
+    flag = __reduce_or_sync(0xffffffffu, flag);
+    if (r == 0) note(p, t.b, flag, lane);
+    const int g = t.rt * 256 + r, j = node_of(p, g);
+    const Row y = merge_row<D>(
+        count, p.scale_log2, [&](int n) { return p.partial_ml[(size_t)slot_of(n) * 256 + r]; },
+        [&](int n) { return *reinterpret_cast<const float4 *>(p.partial_o + ((size_t)slot_of(n) * 256 + r) * D + lane * 4); });
+    put_row<D>(p, ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G), y, flag);
 }
 
 }  // namespace
@@ -927,6 +916,8 @@ reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &params, 
     launch_q4_attn_zero(p, n_sm, st);
     launch_pdl(p.D == 128 ? q4_attn_sm100_kernel<128> : q4_attn_sm100_kernel<64>, dim3((unsigned)n_sm), dim3(kThreads),
                (size_t)(p.D == 128 ? Cfg<128>::kSmem : Cfg<64>::kSmem), st, p);
+    launch_pdl(p.D == 128 ? q4_attn_merge_kernel<128> : q4_attn_merge_kernel<64>, dim3((unsigned)n_sm, (unsigned)((std::min(256, p.T * p.G) + 7) / 8)), dim3(256), 0,
+               st, p);
     return READER_OK;
 }
 
