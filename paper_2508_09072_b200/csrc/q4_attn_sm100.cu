@@ -6,23 +6,21 @@
 // the rows of K, and its values the rows of V^T (position pairs are neighbours in the pages, so a pair of numbers is a
 // pair of bf16 along the value product's inner axis as it stands), in the 128-byte swizzle of the matrix instructions.
 //
-//   warps 0-3, 4-7   softmax of slot 0 and 1: a thread per row.  Scores come from tensor memory; the maximum in use is raised when a
-//                    score exceeds it by 2^8 (O is rescaled in tensor memory then); probabilities replace the scores as bf16 and are the
-//                    value product's A operand from there.  At a unit's end they fetch the next one's queries, so that its first
-//                    products run beside the results being written.
-//   warps 8-15       unpack pages (and copy the tree's own keys and values) into the tiles
+//   warps 0-7        softmax, all of them a step's 128 rows, two threads to a row, each with half of its keys: while they are at one slot's
+//                    scores, the other's products run.  Scores come from tensor memory once; the maximum in use is raised when a score
+//                    exceeds it by 2^8 (O is rescaled in tensor memory then), the one thing that a row's threads must agree on;
+//                    probabilities replace the scores as bf16 and are the value product's A operand from there.  (A thread to a row and four
+//                    warps to a slot: the tile's steps took 2.95 us, each slot's products waiting for its own exponentials and these for them.)
+//   warps 8-11, 12-15  unpack pages (and copy the tree's own keys and values) into the tiles, every other tile each
 //   warp 16          brings pages into a ring by bulk copies
-//   warps 17, 18     issue the products of slot 0 and 1: S = Q K^T, O += P V.  In a wide piece they take turns with their score products,
-//                    and slot 1 begins half a step late: left to themselves the slots fall into step, both at the exponentials and
-//                    then both at the products
+//   warp 17          issues the products: S = Q K^T, O += P V
+//   warp 18          brings queries
 //   warp 19          finds the block's units and puts them into a small ring that the others read; zero rows for sequences whose
-//                    length cannot be.  (With the search in every role the code did not fit the instruction caches any more, and
-//                    warps stood waiting for instructions.)
-// A unit of more than 128 rows is wide: each slot has its own rows and both work on every tile.  A narrow one has up to 128 rows;
-// the slots take the tiles in turns and their two results are merged at its end.
+//                    length cannot be
 //
-// Tensor memory: S of either slot (128 columns each; P over its first 64), O of either slot.  The products of a slot are issued by one
-// thread and run in order, so S[i + 1] may be written over P[i] as soon as the value product that reads it has been issued.
+// A step is 128 rows and a tile: of a unit of more than 128 rows (wide) the two slots of every tile, else (narrow) every tile, in the slots in turn.
+// Products are issued by one thread and run in order, so S[i + 2] may be written over P[i] as soon as the value product that reads it
+// has been issued.
 //
 // Work: a flat list of tiles cut into equal ranges, one per thread block (q4_attn_common.cuh); shares of units in several ranges are merged by
 // a launch behind.  Bytes that are not committed never reach a product: their scores become -inf, and their values 0 or
@@ -40,12 +38,11 @@ using namespace q4;
 
 constexpr int kThreads = 640;
 constexpr int kSoftmaxThreads = 256;
-constexpr int kUnpackWarp = 8, kLoadWarp = 16, kMmaWarp = 17, kListWarp = 19;
-constexpr int kUnpackThreads = 256, kUnpackWarps = 8;
+constexpr int kUnpackWarp = 8, kLoadWarp = 16, kMmaWarp = 17, kQueryWarp = 18, kListWarp = 19;
+constexpr int kUnpackThreads = 128, kUnpackWarps = 4;   // of a tile
 constexpr int kReaders = 19;       // warps that read the ring of units: all but kListWarp
-// Registers of a thread: softmax, unpacking, the rest: 256 x 112 + 256 x 72 + 128 x 96 = 59392 of the 640 x 96 that the block is launched with.
-constexpr int kRegsSoftmax = 112, kRegsUnpack = 72;
-constexpr int kLateStart = 6;      // tiles of a wide piece from which slot 1 begins half a step behind slot 0
+// Registers of a thread: softmax, unpacking, the rest: 256 x 136 + 256 x 72 + 128 x 64 = the 640 x 96 that the block is launched with.
+constexpr int kRegsSoftmax = 136, kRegsUnpack = 72, kRegsRest = 64;
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
 constexpr int kUnitCost = 6;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = 8;     // of a range
@@ -68,8 +65,8 @@ struct Cfg {
     static constexpr int kOffRaw = kOffV + 2 * kVBytes;
     static constexpr int kRawBytes = 2 * kPageBytes;
     static constexpr int kOffParents = kOffRaw + kRawSlots * kRawBytes;   // kAhead / 2 trees
-    static constexpr int kOffMl = kOffParents + kAhead / 2 * kMaxNodes;   // (m, l) of slot 1's rows, and of slot 0's
-    static constexpr int kOffTable = kOffMl + 2 * 128 * 8;
+    static constexpr int kOffSwap = kOffParents + kAhead / 2 * kMaxNodes;   // what the two threads of a row tell each other: largest scores, sums
+    static constexpr int kOffTable = kOffSwap + 2 * 256 * 4;
     static constexpr int kOffBars = kOffTable + kPrefix * 8;
     static constexpr int kSmem = kOffBars + 1024;
     static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -83,13 +80,13 @@ struct Piece {
     // committed tiles come first, the tree's is the last
     __device__ __forceinline__ bool is_tree(int tile) const { return t0 + tile == ntiles - 1; }
     __device__ __forceinline__ int valid(int T, int tile) const { return is_tree(tile) ? T : min(kTileKeys, L - (t0 + tile) * kTileKeys); }
-    // tiles of a slot: every one, or (narrow) every other
-    __device__ __forceinline__ int first(int slot) const { return wide ? 0 : slot; }
-    __device__ __forceinline__ int step() const { return wide ? 1 : 2; }
+    // A wide unit's steps are its tiles for slot 0 and for slot 1, in turn; a narrow one's are its tiles, in the slots in turn.
+    __device__ __forceinline__ int steps() const { return wide ? 2 * tiles : tiles; }
+    __device__ __forceinline__ int tile_of(int step) const { return wide ? step >> 1 : step; }
 };
 struct Bars {
     uint64_t raw_full[kRawSlots], raw_empty[kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_full[2], turn[2], piece_full[kAhead], piece_empty[kAhead];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], pv_done, o_full, piece_full[kAhead], piece_empty[kAhead];
     uint32_t tmem_base;
     int32_t abort;
     int32_t raw_bad[kRawSlots];   // a page outside the pool among the slot's
@@ -289,18 +286,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(&m->k_full[i]), kUnpackWarps);
-            mbar_init(bar(&m->k_empty[i]), 2);
+            mbar_init(bar(&m->k_empty[i]), 1);
             mbar_init(bar(&m->v_full[i]), kUnpackWarps);
-            mbar_init(bar(&m->turn[i]), 1);
-            mbar_init(bar(&m->v_empty[i]), 2);
+            mbar_init(bar(&m->v_empty[i]), 1);
+            mbar_init(bar(&m->q_full[i]), 1);
+            mbar_init(bar(&m->q_empty[i]), 1);
             mbar_init(bar(&m->s_full[i]), 1);
-            mbar_init(bar(&m->p_full[i][0]), 128);
-            mbar_init(bar(&m->p_full[i][1]), 128);
-            mbar_init(bar(&m->o_full[i]), 1);
+            mbar_init(bar(&m->p_full[i]), kSoftmaxThreads / 32);
         }
         m->task.block0 = -1;
-        mbar_init(bar(&m->q_full), kSoftmaxThreads);
-        mbar_init(bar(&m->q_empty), 2);
+        mbar_init(bar(&m->pv_done), 1);
+        mbar_init(bar(&m->o_full), 1);
         for (int i = 0; i < kAhead; ++i) {
             mbar_init(bar(&m->piece_full[i]), 1);
             mbar_init(bar(&m->piece_empty[i]), kReaders);
@@ -309,7 +305,6 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         m->abort = (base & 1023u) ? 1 : 0;   // (the swizzled tiles want 1024-byte alignment; never seen otherwise, but checked)
         fence_mbar_init();
         fence_proxy_async();
-        mbar_arrive(bar(&m->turn[0]));   // slot 0 has the first turn
     }
     if (warp == kMmaWarp) {
         tmem_alloc(smem_u32(&m->tmem_base), kTmemCols);
@@ -337,6 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     list.cut(max(1, min(p.n_ctas, list.W / kMinEntries)));
 
     if (warp >= kLoadWarp) {
+        regs_dec<kRegsRest>();
         if (warp == kListWarp) {
             // ------------------------------------------------------------------ units
             int w = 0, w_end = 0;
@@ -431,113 +427,104 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     while (!mbar_try_wait(bar(&m->raw_full[i % kRawSlots]), (i / kRawSlots) & 1) && globaltimer_ns() - t0 < 20000000ull) {
                     }
             }
+        } else if (warp == kQueryWarp) {
+            // ------------------------------------------------------------------ queries
+            // A wide unit's rows fill both halves of the place, and it has them when the unit before is done with its own; narrow ones have the
+            // halves in turn, so that one's queries come while the one before is worked on.
+            constexpr int kChunks = D / 8, kRowsAtOnce = 32 / kChunks;
+            const int ch = lane % kChunks, r0 = lane / kChunks;
+            bool wide_before = false;
+            Piece x;
+            for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
+                const int after = x.wide || wide_before ? 1 : 2;   // the unit that was there before: that many before this
+                if (seg >= after) wait(bar(&m->q_empty[(seg - after) & 1]), ((seg - after) >> 1) & 1, abort_s);
+                wide_before = x.wide;
+                const uint32_t place = base + C::kOffQ + (x.wide ? 0 : (seg & 1) * C::kQBytes) + (ch >> 3) * C::kBlock;
+                const int rows = x.wide ? 256 : 128;
+#pragma unroll 4
+                for (int r = r0; r < rows; r += kRowsAtOnce) {
+                    const bool live = r < x.rows;
+                    const int g = x.rt * 256 + (live ? r : 0), j = node_of(p, g);
+                    const __nv_bfloat16 *src = p.q + (((size_t)x.b * p.T + j) * p.Hq + x.h * p.G + (g - j * p.G)) * D + ch * 8;
+                    const uint32_t dst = place + (r >> 7) * C::kQBytes + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&m->q_full[seg & 1]));
+            }
         } else {
-            // ------------------------------------------------------------------ products of a slot
-            const int slot = warp - kMmaWarp;
+            // ------------------------------------------------------------------ products
             constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kTileKeys, false, false), kIdescPV = idesc_bf16_f32(128, D, false, false);
             const uint64_t descQ = smem_desc_sw128(base + C::kOffQ, 16, 1024), descK = smem_desc_sw128(base + C::kOffK, 16, 1024);
             const uint64_t descV = smem_desc_sw128(base + C::kOffV, 16, 1024);
-            const uint32_t tS = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + slot * D;
-            // Both issuers see every tile of keys and of values in order, so that neither can fall a whole turn behind (a parity wait tells
-            // a phase only from the one before it); tiles of the other slot are passed on at once.
-            int nk = 0, nv = 0, done = 0;   // tiles of keys, of values seen; of the units before
-            uint32_t p_parity = 0, turn_parity = 0;
-            auto pass_keys = [&](int to) {
-                for (; nk < to; ++nk) {
-                    wait(bar(&m->k_full[nk & 1]), (nk >> 1) & 1, abort_s);
-                    if (lane == 0) mbar_arrive(bar(&m->k_empty[nk & 1]));
-                    __syncwarp();
-                }
-            };
-            auto pass_values = [&](int to) {
-                for (; nv < to; ++nv) {
-                    wait(bar(&m->v_full[nv & 1]), (nv >> 1) & 1, abort_s);
-                    if (lane == 0) mbar_arrive(bar(&m->v_empty[nv & 1]));
-                    __syncwarp();
-                }
-            };
+            int nk = 0, nv = 0;          // tiles of keys, of values so far
+            uint32_t p_parity = 0;       // bit `slot`
             Piece x;
             for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
-                wait(bar(&m->q_full), seg & 1, abort_s);
-                const int step = x.step();
-                const uint64_t qd = descQ + (uint64_t)((x.wide ? slot * C::kQBytes : 0) >> 4);
-                const bool late = x.wide && slot == 0 && x.tiles >= kLateStart;
-                auto pass_turn = [&]() {
-                    if (x.wide && lane == 0) mbar_arrive(bar(&m->turn[slot ^ 1]));
-                    __syncwarp();
-                };
-                auto score = [&](int t) {
-                    pass_keys(done + t);
-                    const int buf = nk & 1;
-                    wait(bar(&m->k_full[buf]), (nk >> 1) & 1, abort_s);
-                    ++nk;
-                    if (x.wide) {
-                        wait(bar(&m->turn[slot]), turn_parity, abort_s);
-                        turn_parity ^= 1;
+                wait(bar(&m->q_full[seg & 1]), (seg >> 1) & 1, abort_s);
+                const int steps = x.steps();
+                auto score = [&](int i) {
+                    const int slot = i & 1;
+                    if (!x.wide || slot == 0) {
+                        wait(bar(&m->k_full[nk & 1]), (nk >> 1) & 1, abort_s);
+                        ++nk;
                     }
                     tc_fence_after();
                     const bool go = !gone(abort_s);
                     if (go && elect_one()) {
-                        const uint64_t kd = descK + (uint64_t)((buf * C::kKBytes) >> 4);
+                        const int buf = (nk - 1) & 1;
+                        const uint64_t kd = descK + (uint64_t)((buf * C::kKBytes) >> 4), qd = descQ + (uint64_t)(((x.wide ? slot : seg & 1) * C::kQBytes) >> 4);
+                        const uint32_t tS = tmem + kTmemS + slot * 128;
 #pragma unroll
                         for (int hf = 0; hf < C::kHalves; ++hf)
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
                                 mma_bf16_ss(tS, qd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
                         mma_commit(bar(&m->s_full[slot]));
-                        mma_commit(bar(&m->k_empty[buf]));
-                        if (t + step >= x.tiles) mma_commit(bar(&m->q_empty));
+                        if (!x.wide || slot == 1) mma_commit(bar(&m->k_empty[buf]));
+                        if (i == steps - 1) mma_commit(bar(&m->q_empty[seg & 1]));
                     }
                     __syncwarp();
-                    if (!(late && t == 0)) pass_turn();
                 };
-                const int t0 = x.first(slot);
-                if (t0 < x.tiles) {
 #pragma unroll 1
-                    for (int t = t0 - step; t < x.tiles; t += step) {
-                        if (t >= t0) {
-                            pass_values(done + t);
-                            const int buf = nv & 1, slices = (x.valid(p.T, t) + 15) >> 4;
-                            wait(bar(&m->v_full[buf]), (nv >> 1) & 1, abort_s);
+                for (int i = -2; i < steps; ++i) {
+                    if (i >= 0) {
+                        const int slot = i & 1, slices = (x.valid(p.T, x.tile_of(i)) + 15) >> 4;
+                        if (!x.wide || slot == 0) {
+                            wait(bar(&m->v_full[nv & 1]), (nv >> 1) & 1, abort_s);
                             ++nv;
-#pragma unroll 1
-                            for (int half = 0; half < 2; ++half) {
-                                wait(bar(&m->p_full[slot][half]), p_parity, abort_s);
-                                if (late && t == 0 && half == 0) pass_turn();
-                                tc_fence_after();
-                                const bool go = !gone(abort_s);
-                                if (go && elect_one()) {
-                                    const uint64_t vd = descV + (uint64_t)((buf * C::kVBytes + half * C::kVPage) >> 4);
-#pragma unroll
-                                    for (int kk = 0; kk < 4; ++kk)
-                                        if (half * 4 + kk < slices)
-                                            mma_bf16_ts(tO, tS + (half * 4 + kk) * 8, vd + (uint64_t)((kk * 32) >> 4), kIdescPV, t != t0 || half + kk != 0);
-                                    if (half == 1) {
-                                        mma_commit(bar(&m->v_empty[buf]));
-                                        if (t + step >= x.tiles) mma_commit(bar(&m->o_full[slot]));
-                                    }
-                                }
-                                __syncwarp();
-                            }
-                            p_parity ^= 1;
                         }
-                        if (t + step < x.tiles) score(t + step);
+                        wait(bar(&m->p_full[slot]), (p_parity >> slot) & 1, abort_s);
+                        p_parity ^= 1u << slot;
+                        tc_fence_after();
+                        const bool go = !gone(abort_s);
+                        if (go && elect_one()) {
+                            const int buf = (nv - 1) & 1;
+                            const uint64_t vd = descV + (uint64_t)((buf * C::kVBytes) >> 4);
+                            const uint32_t tP = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + (x.wide ? slot * D : 0);
+                            const bool fresh = x.tile_of(i) == 0;
+#pragma unroll
+                            for (int kk = 0; kk < 8; ++kk)   // (P of the keys 64 .. 127 lies over their scores)
+                                if (kk < slices)
+                                    mma_bf16_ts(tO, tP + (kk >> 2) * 64 + (kk & 3) * 8, vd + (uint64_t)(((kk >> 2) * C::kVPage + (kk & 3) * 32) >> 4), kIdescPV, !fresh || kk != 0);
+                            if (!x.wide || slot == 1) mma_commit(bar(&m->v_empty[buf]));
+                            if (i == steps - 1) mma_commit(bar(&m->o_full));
+                            if (!x.wide) mma_commit(bar(&m->pv_done));
+                        }
+                        __syncwarp();
                     }
-                } else {   // (a narrow piece of one tile: slot 1 has none)
-                    if (lane == 0) mbar_arrive(bar(&m->q_empty));
-                    __syncwarp();
+                    if (i + 2 < steps) score(i + 2);
                 }
-                done += x.tiles;
-                pass_keys(done);
-                pass_values(done);
             }
             if (gone(abort_s)) __nanosleep(1000000);   // products that are still under way end before their operands go away
         }
     } else if (warp >= kUnpackWarp) {
         // ------------------------------------------------------------------ unpacking
         regs_dec<kRegsUnpack>();
-        const int t = tid - kUnpackWarp * 32;
-        volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + C::kOffMl);   // (an opaque constant: see pair())
+        const int group = (warp - kUnpackWarp) >> 2, t = tid & 127;   // the groups of four warps unpack every other tile
+        volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + C::kOffSwap);   // (an opaque constant: see pair())
         if (t == 0) *word = 0x41804180u;
         asm volatile("bar.sync 2, 256;" ::: "memory");
         const uint32_t sixteen = *word;
@@ -547,6 +534,11 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
             for (int i = 0; i < x.tiles && !gone(abort_s); ++i, ++n) {
                 const int buf = n & 1;
+                if (buf != group) {
+                    if (x.is_tree(i)) ++trees;
+                    else raw += 2;
+                    continue;
+                }
                 const uint32_t kt = base + C::kOffK + buf * C::kKBytes, vt = base + C::kOffV + buf * C::kVBytes;
                 const bool tree = x.is_tree(i);
                 const int valid = x.valid(p.T, i);
@@ -566,8 +558,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
                     if (m->raw_bad[s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
-                    const int page = t >> 7;   // a page to 128 threads
-                    if (page * kPage < valid) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t & 127, sixteen);
+#pragma unroll 1
+                    for (int page = 0; page * kPage < valid && page < 2; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
                     ++raw;
@@ -583,8 +575,9 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     const int s = raw % kRawSlots;
                     if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
-                    const int page = t >> 7;
-                    if (page * kPage < valid) unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t & 127, sixteen);
+#pragma unroll 1
+                    for (int page = 0; page * kPage < valid && page < 2; ++page)
+                        unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
                     ++raw;
@@ -597,37 +590,16 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     } else {
         // ------------------------------------------------------------------ softmax, results
         regs_inc<kRegsSoftmax>();
-        const int slot = warp >> 2, row = tid & 127;
+        // Two threads to a row, of warps `half` = 0 and 1: keys 64 half .. + 63 of a tile.
+        const int half = warp >> 2, row = tid & 127;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + kTmemS + slot * 128 + lane_base, tO = tmem + kTmemO + slot * D + lane_base;
         constexpr uint32_t kNegInf = 0xff800000u;
-        float2 *ml_s = reinterpret_cast<float2 *>(smem + C::kOffMl);
+        float *top_s = reinterpret_cast<float *>(smem + C::kOffSwap), *sum_s = top_s + 256;
         const float by = kRaiseBy / p.scale_log2;
-        uint32_t s_parity = 0, o_parity[2] = {0, 0};
-        int trees = 0;   // (both slots count all of them)
-
-        // Queries of unit x: rows of this slot (wide) or this slot's half of the columns of all of them (narrow).
-        auto load_queries = [&](const Piece &x) {
-            const int r = x.rt * 256 + (x.wide ? slot * 128 : 0) + row;
-            const bool live = r < p.T * p.G;
-            const int j = live ? node_of(p, r) : 0, hq = x.h * p.G + (live ? r - j * p.G : 0);
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (((size_t)x.b * p.T + j) * p.Hq + hq) * D);
-            constexpr int kChunks = D / 8;
-            const uint32_t dst = base + C::kOffQ + (x.wide ? slot * C::kQBytes : 0) + row * 128;
-            const int c0 = x.wide ? 0 : slot * (kChunks / 2);
-            auto part = [&](int c1) {
-#pragma unroll
-                for (int i = 0; i < kChunks / 2; ++i) {
-                    const int ch = c1 + i;
-                    const uint4 q = live ? src[ch] : make_uint4(0, 0, 0, 0);
-                    sts128(dst + (ch >> 3) * C::kBlock + (((ch & 7) ^ (row & 7)) << 4), q.x, q.y, q.z, q.w);
-                }
-            };
-            part(c0);
-            if (x.wide) part(kChunks / 2);
-            fence_proxy_async();
-            mbar_arrive(bar(&m->q_full));
-        };
+        auto pair_barrier = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(5 + (warp & 3)) : "memory"); };
+        uint32_t s_parity = 0;   // bit `slot`
+        uint32_t narrow_steps = 0;
+        int trees = 0;
         // Whether there is another unit is decided together: a block that gives up may do so between two warps' looks at the ring, and the
         // barriers among the softmax threads want all of them.
         auto next_for_all = [&](Piece &y, int seg) {
@@ -636,138 +608,132 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((int)got) : "memory");
             return all != 0;
         };
-        Piece k;
-        int seg = 0;
-        bool more = next_for_all(k, 0);
-        if (more) load_queries(k);
-        while (more) {
-            const int grow = k.rt * 256 + (k.wide ? slot * 128 : 0) + row;   // among the head's rows
-            const bool live = grow < p.T * p.G;
-            const bool warp_live = __any_sync(0xffffffffu, live);
-            const int node = live ? node_of(p, grow) : 0;
-            // a row without a query never asks for a higher maximum
-            float mx = live ? -INFINITY : INFINITY, l = 0.f;
-            const bool has_tree = k.is_tree(k.tiles - 1);
-            const int t_first = k.first(slot);
+        Piece x;
+        for (int seg = 0; next_for_all(x, seg); ++seg) {
+            // A row without a query never asks for a higher maximum.  (m, l) of the step's slot, and of the other (wide)
+            const int r_end = x.rows;
+            float mx = row < r_end ? -INFINITY : INFINITY, l = 0.f, mx_other = 128 + row < r_end ? -INFINITY : INFINITY, l_other = 0.f;
+            const bool has_tree = x.is_tree(x.tiles - 1);
+            const int steps = x.steps();
 #pragma unroll 1
-            for (int t = t_first; t < k.tiles; t += k.step()) {
-                wait(bar(&m->s_full[slot]), s_parity, abort_s);
-                s_parity ^= 1;
+            for (int i = 0; i < steps; ++i) {
+                const int slot = i & 1, t = x.tile_of(i), r = (x.wide ? slot * 128 : 0) + row;
+                const uint32_t tS = tmem + kTmemS + slot * 128 + half * 64 + lane_base;
+                const bool live = r < r_end, warp_live = __any_sync(0xffffffffu, live);
+                wait(bar(&m->s_full[slot]), (s_parity >> slot) & 1, abort_s);
+                s_parity ^= 1u << slot;
                 tc_fence_after();
                 if (warp_live) {
-                    const int valid = k.valid(p.T, t);
-                    const bool masked = valid < kTileKeys || k.is_tree(t);
-                    uint64_t sees[2] = {~0ull, ~0ull};   // the keys this row sees
-                    if (masked) {
-                        if (k.is_tree(t)) {
-                            sees[0] = sees[1] = 0;
-                            if (live && p.anc) {
-                                sees[0] = p.anc[((size_t)k.b * p.T + node) * 2];
-                                sees[1] = p.anc[((size_t)k.b * p.T + node) * 2 + 1];
-                            } else if (live && !(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
-                                const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
-                                for (int i = node; i != 255; i = parents[i]) {   // (strictly falling on a valid tree)
-                                    if (i < 64) sees[0] |= 1ull << i;
-                                    else sees[1] |= 1ull << (i - 64);
-                                }
-                            }
+                    uint32_t s[64];
+                    tmem_ld32(tS, reinterpret_cast<uint32_t(&)[32]>(s[0]));
+                    tmem_ld32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(s[32]));
+                    const int valid = x.valid(p.T, t) - half * 64;   // of this half's keys
+                    uint64_t sees = ~0ull;                           // the ones this row sees
+                    if (x.is_tree(t)) {
+                        const int g = x.rt * 256 + r, node = live ? node_of(p, g) : 0;
+                        sees = 0;
+                        if (live && p.anc) {
+                            sees = p.anc[((size_t)x.b * p.T + node) * 2 + half];
+                        } else if (live && !(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
+                            const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
+                            for (int n = node; n != 255; n = parents[n])   // (strictly falling on a valid tree)
+                                if ((n >> 6) == half) sees |= 1ull << (n & 63);
                         }
-                        if (valid < 64) sees[0] &= (1ull << valid) - 1;
-                        if (valid < 128) sees[1] &= valid <= 64 ? 0 : (1ull << (valid - 64)) - 1;
                     }
-                    // Half a tile's scores at a time, twice: for the maximum, then for the probabilities.  (All 128 in registers leave none
-                    // for the warps that unpack; tensor memory is read in a fraction of the time that the exponentials take.)
-                    uint32_t x[2][32];
-                    auto f = [&](int i) { return __uint_as_float(x[i >> 5][i & 31]); };
-                    auto fetch = [&](int half) {
-                        tmem_ld32(tS + half * 64, x[0]);
-                        tmem_ld32(tS + half * 64 + 32, x[1]);
-                        tmem_wait_ld();
-                        if (masked) {
-                            const uint64_t bits = sees[half];
+                    if (valid < 64) sees &= valid <= 0 ? 0 : (1ull << valid) - 1;
+                    auto f = [&](int k) { return __uint_as_float(s[k]); };
+                    tmem_wait_ld();
+                    if (valid < 64 || x.is_tree(t)) {
 #pragma unroll
-                            for (int i = 0; i < 64; ++i)
-                                if (!((bits >> i) & 1)) x[i >> 5][i & 31] = kNegInf;
-                        }
-                    };
-                    float top = -INFINITY;
-#pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
-                        fetch(half);
-                        float a = max3(f(0), f(1), f(2)), b = max3(f(3), f(4), f(5));
-#pragma unroll
-                        for (int i = 6; i < 62; i += 4) {
-                            a = max3(a, f(i), f(i + 1));
-                            b = max3(b, f(i + 2), f(i + 3));
-                        }
-                        top = fmaxf(top, fmaxf(max3(a, f(62), f(63)), b));
+                        for (int k = 0; k < 64; ++k)
+                            if (!((sees >> k) & 1)) s[k] = kNegInf;
                     }
-                    if (__any_sync(0xffffffffu, top > mx + by)) {
-                        const float now = fmaxf(mx, top);
+                    float a[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) a[c] = max3(f(3 * c), f(3 * c + 1), f(3 * c + 2));
+#pragma unroll
+                    for (int k = 12; k < 60; k += 8)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) a[c] = max3(a[c], f(k + 2 * c), f(k + 2 * c + 1));
+                    float top = max3(max3(a[0], f(60), f(61)), max3(a[1], f(62), f(63)), fmaxf(a[2], a[3]));
+                    int raise;
+                    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.gt.f32 p, %1, %2;\n\tbarrier.cta.red.or.pred q, %3, 64, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                                 : "=r"(raise) : "f"(top), "f"(mx + by), "r"(5 + (warp & 3)) : "memory");
+                    if (raise) {
+                        top_s[half * 128 + row] = top;
+                        pair_barrier();
+                        const float now = max3(mx, top, top_s[(half ^ 1) * 128 + row]);
                         const float g = mx == now ? 1.f : ex2((mx - now) * p.scale_log2);   // (-inf before the first score: 0)
                         mx = now;
                         l *= g;
-                        if (t != t_first) {   // (the products before this tile's scores are done)
+                        if (t > 0) {
+                            // A wide unit's products of this slot are done, these scores having come behind them; a narrow one's last are awaited.
+                            if (!x.wide) {
+                                wait(bar(&m->pv_done), (narrow_steps - 1) & 1, abort_s);
+                                tc_fence_after();
+                            }
+                            const uint32_t tO = tmem + kTmemO + (x.wide ? slot * D : 0) + half * (D / 2) + lane_base;
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 16) {
+                            for (int c = 0; c < D / 2; c += 16) {
                                 uint32_t o[16];
                                 tmem_ld16(tO + c, o);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * g);
+                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * g);
                                 tmem_st16(tO + c, o);
                             }
-                            tmem_wait_st();
                         }
                     }
-                    // The difference to the maximum is taken before the scaling: whatever the scores' size, it is as exact as they are.
-                    const float from = mx == -INFINITY ? 0.f : -mx;
+                    // 2^((s - max) scale) by one multiplication and addition.  The maximum times the scale is rounded, by the same for all keys of a
+                    // row: it cancels, but where it is so large that its rounding is not small against 1 the difference is taken first.
+                    float from = mx == -INFINITY ? 0.f : -mx * p.scale_log2;
+                    if (__any_sync(0xffffffffu, fabsf(from) > 65536.f && fabsf(from) < INFINITY)) {
+#pragma unroll
+                        for (int k = 0; k < 64; ++k) s[k] = __float_as_uint(f(k) - (mx == -INFINITY ? 0.f : mx));
+                        from = 0.f;
+                    }
                     const float2 from2 = make_float2(from, from), sc = make_float2(p.scale_log2, p.scale_log2);
                     float2 sum = make_float2(0.f, 0.f);
-#pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {   // (P of a half is written over scores that have been read)
-                        fetch(half);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t pk[16];
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t pk[16];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float2 y = __fmul2_rn(__fadd2_rn(make_float2(f(c * 32 + 2 * i), f(c * 32 + 2 * i + 1)), from2), sc);
-                                const float2 e = make_float2(ex2(y.x), ex2(y.y));
-                                sum = __fadd2_rn(sum, e);
-                                pk[i] = pack(e.x, e.y);
-                            }
-                            tmem_st16(tS + half * 32 + c * 16, pk);
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 y = __ffma2_rn(make_float2(f(c * 32 + 2 * k), f(c * 32 + 2 * k + 1)), sc, from2);
+                            const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                            sum = __fadd2_rn(sum, e);
+                            pk[k] = pack(e.x, e.y);
                         }
-                        tmem_wait_st();
-                        tc_fence_before();
-                        mbar_arrive(bar(&m->p_full[slot][half]));
+                        tmem_st16(tS + c * 16, pk);
                     }
                     l += sum.x + sum.y;
-                } else {
-                    tc_fence_before();
-                    mbar_arrive(bar(&m->p_full[slot][0]));
-                    mbar_arrive(bar(&m->p_full[slot][1]));
+                    tmem_wait_st();
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&m->p_full[slot]));
+                if (x.wide) {
+                    const float a = mx, b = l;
+                    mx = mx_other; l = l_other;
+                    mx_other = a; l_other = b;
+                } else ++narrow_steps;
             }
-            // The next unit's queries, when this one's last scores are done; then this one's results.
-            const Piece x = k;
-            const int seg_x = seg++;
-            wait(bar(&m->q_empty), seg_x & 1, abort_s);
-            more = next_for_all(k, seg);
-            if (more) load_queries(k);
-            const bool slot_has[2] = {true, x.wide || x.tiles > 1};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (!slot_has[i]) continue;
-                // (a wide unit's slot needs its own alone, but both keep count of both)
-                wait(bar(&m->o_full[i]), o_parity[i], abort_s);
-                o_parity[i] ^= 1;
-            }
+            // Results: a wide unit's slot `half`; of a narrow one half of the columns.
+            wait(bar(&m->o_full), seg & 1, abort_s);
             tc_fence_after();
-            int flag = *(volatile int32_t *)&m->flags[seg_x % kAhead];
+            const int r = (x.wide ? half * 128 : 0) + row, grow = x.rt * 256 + r;   // among the unit's rows, the head's
+            const bool live = r < r_end, warp_live = __any_sync(0xffffffffu, live);
+            const int node = live ? node_of(p, grow) : 0;
+            const bool swap = x.wide && half == 1;
+            sum_s[half * 128 + row] = x.wide && half == 0 ? l_other : l;
+            softmax_barrier();
+            mx = swap ? mx_other : mx;
+            l = (swap ? l_other : l) + sum_s[(half ^ 1) * 128 + row];
+            const int col0 = x.wide ? 0 : half * (D / 2), col1 = x.wide ? D : col0 + D / 2;
+            const uint32_t tO = tmem + kTmemO + (x.wide ? half * D : 0) + lane_base;
+            int flag = *(volatile int32_t *)&m->flags[seg % kAhead];
             if (*abort_s || (int)blockIdx.x == p.give_up) flag |= kGaveUp;
-            if (has_tree && *(volatile int32_t *)&m->poison[seg_x % kAhead] && (x.wide || slot == ((x.tiles - 1) & 1)) && warp_live) {
+            if (has_tree && *(volatile int32_t *)&m->poison[seg % kAhead] && warp_live) {
                 // infinities and NaN were left out of the product: the rows that see them get them
 #pragma unroll 1
                 for (int n = 0; n < p.T && !(flag & kBadTree); ++n) {
@@ -777,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         for (int i = node; i >= n; i = p.parent[(size_t)x.b * p.T + i]) sees |= i == n;
                     const uint32_t *val = reinterpret_cast<const uint32_t *>(p.v_tree + (((size_t)x.b * p.T + n) * p.Hkv + x.h) * D);
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
+                    for (int c = col0; c < col1; c += 16) {
                         uint32_t o[16];
                         tmem_ld16(tO + c, o);
                         tmem_wait_ld();
@@ -791,46 +757,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     }
                 }
                 tmem_wait_st();
-                tc_fence_before();
             }
-            float2 other = make_float2(-INFINITY, 0.f);
-            if (!x.wide) {
-                ml_s[slot * 128 + row] = make_float2(live ? mx : -INFINITY, l);
-                softmax_barrier();
-                tc_fence_after();
-                other = ml_s[(slot ^ 1) * 128 + row];
-            }
-            // weights of the slots' results; a narrow unit's slot writes half of the columns
-            float w_own = 1.f, w_other = 0.f;
-            if (!x.wide) {
-                const float now = fmaxf(live ? mx : -INFINITY, other.x);
-                w_own = mx == now ? 1.f : (mx == -INFINITY || !live) ? 0.f : ex2((mx - now) * p.scale_log2);
-                w_other = other.x == -INFINITY ? 0.f : other.x == now ? 1.f : ex2((other.x - now) * p.scale_log2);
-                if (mx == -INFINITY) w_own = 0.f;
-                l = l * w_own + other.y * w_other;
-                mx = now;
-            }
-            const int col0 = x.wide ? 0 : slot * (D / 2), col1 = x.wide ? D : col0 + D / 2;
-            const uint32_t tOwn = tmem + kTmemO + (x.wide ? slot * D : 0) + lane_base, tOther = tmem + kTmemO + D + lane_base;
-            // narrow: slot 0's result with its weight, then slot 1's
-            const float w0 = x.wide ? 1.f : slot == 0 ? w_own : w_other, w1 = slot == 0 ? w_other : w_own;
             const size_t orow = ((size_t)x.b * p.T + node) * p.Hq + x.h * p.G + (grow - node * p.G);
             const int share = 2 * blockIdx.x + (x.t0 == 0 ? 1 : 0);
-            const size_t srow = (size_t)share * 256 + (x.wide ? slot * 128 : 0) + row;
+            const size_t srow = (size_t)share * 256 + r;
             const float inv = flag || l == 0.f ? 0.f : 1.f / l;   // (a row that sees nothing: zeros)
             if (warp_live) {
 #pragma unroll 1
                 for (int c = col0; c < col1; c += 16) {
-                    uint32_t o[16], o1[16];
-                    tmem_ld16(tOwn + c, o);
-                    if (!x.wide && slot_has[1]) tmem_ld16(tOther + c, o1);
+                    uint32_t o[16];
+                    tmem_ld16(tO + c, o);
                     tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float y = __uint_as_float(o[i]) * w0;
-                        if (!x.wide && slot_has[1]) y = fmaf(__uint_as_float(o1[i]), w1, y);
-                        o[i] = __float_as_uint(y);
-                    }
                     if (!live) continue;
                     if (x.whole()) {
                         uint4 y[2];
@@ -846,16 +783,16 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
                 }
-                if (live && (x.wide || slot == 0)) {
+                if (live && (x.wide || half == 0)) {
                     if (!x.whole()) p.partial_ml[srow] = make_float2(mx, l);
                     else if (p.lse) p.lse[orow] = flag ? 0.f : fmaf(mx, p.scale, log2f(l) * 0.6931471805599453f);
                 }
             }
             tc_fence_before();
-            softmax_barrier();   // both slots have read what the next unit's value products and results will overwrite
+            softmax_barrier();   // all have read the flags
             if (tid == 0) {
-                m->flags[seg_x % kAhead] = 0;
-                m->poison[seg_x % kAhead] = 0;
+                m->flags[seg % kAhead] = 0;
+                m->poison[seg % kAhead] = 0;
                 if (x.whole()) {
                     note(p, x.b, flag, 0);
                 } else {
