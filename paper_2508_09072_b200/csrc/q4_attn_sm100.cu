@@ -41,8 +41,8 @@ constexpr int kSoftmaxThreads = 256;
 constexpr int kUnpackWarp = 8, kLoadWarp = 16, kMmaWarp = 17, kQueryWarp = 18, kListWarp = 19;
 constexpr int kUnpackThreads = 128, kUnpackWarps = 4;   // of a tile
 constexpr int kReaders = 19;       // warps that read the ring of units: all but kListWarp
-// Registers of a thread: softmax, unpacking, the rest: 256 x 136 + 256 x 72 + 128 x 64 = the 640 x 96 that the block is launched with.
-constexpr int kRegsSoftmax = 136, kRegsUnpack = 72, kRegsRest = 64;
+// Registers of a thread: softmax, unpacking, the rest: 256 x 120 + 256 x 88 + 128 x 64 = the 640 x 96 that the block is launched with.
+constexpr int kRegsSoftmax = 120, kRegsUnpack = 88, kRegsRest = 64;
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
 constexpr int kUnitCost = 6;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = 8;     // of a range
@@ -472,8 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         ++nk;
                     }
                     tc_fence_after();
-                    const bool go = !gone(abort_s);
-                    if (go && elect_one()) {
+                    if (elect_one()) {
                         const int buf = (nk - 1) & 1;
                         const uint64_t kd = descK + (uint64_t)((buf * C::kKBytes) >> 4), qd = descQ + (uint64_t)(((x.wide ? slot : seg & 1) * C::kQBytes) >> 4);
                         const uint32_t tS = tmem + kTmemS + slot * 128;
@@ -499,8 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         wait(bar(&m->p_full[slot]), (p_parity >> slot) & 1, abort_s);
                         p_parity ^= 1u << slot;
                         tc_fence_after();
-                        const bool go = !gone(abort_s);
-                        if (go && elect_one()) {
+                        if (elect_one()) {
                             const int buf = (nv - 1) & 1;
                             const uint64_t vd = descV + (uint64_t)((buf * C::kVBytes) >> 4);
                             const uint32_t tP = tmem + kTmemS + slot * 128, tO = tmem + kTmemO + (x.wide ? slot * D : 0);
@@ -778,9 +776,9 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         dst[0] = y[0];
                         dst[1] = y[1];
                     } else {
-                        uint4 *dst = reinterpret_cast<uint4 *>(p.partial_o + srow * D + c);
+                        uint4 *dst = reinterpret_cast<uint4 *>(p.partial_o) + (size_t)share * 256 * (D / 4) + (c / 4) * 256 + r;   // [D / 4][rows]: neighbouring threads' together
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        for (int i = 0; i < 4; ++i) dst[i * 256] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
                 }
                 if (live && (x.wide || half == 0)) {
@@ -814,26 +812,44 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     }
 }
 
-// Units that several blocks have shares of: eight rows of the one that block blockIdx.x of the attention begins, a warp to a row.  (A launch of its
-// own: the block that came last did this at first, and took 25 us for the shares of 128 rows and 60 us for those of 256, the others waiting.)
+// Units that several blocks have shares of: eight rows of the one that block blockIdx.x of the attention begins, a thread to four elements of a row.
+// Always in the shares' order.  A share whose maximum is -inf has weight 0 and is still added, so that a NaN in it stays.  (A launch of its own: the
+// block that came last did this at first, and took 25 us for the shares of 128 rows and 60 us for those of 256, the others waiting.)
 template <int D>
-__global__ void __launch_bounds__(256) q4_attn_merge_kernel(const __grid_constant__ Q4AttnParams p) {
-    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+__global__ void __launch_bounds__(2 * D) q4_attn_merge_kernel(const __grid_constant__ Q4AttnParams p) {
+    const int r = blockIdx.y * 8 + (threadIdx.x & 7), c = threadIdx.x >> 3;
     pdl_wait();
     pdl_launch_dependents();
     const ShareTask t = p.tasks[blockIdx.x];
     if (t.block0 < 0 || r >= t.rows) return;
+    const float2 *ml = p.partial_ml + r;
+    const float4 *o = reinterpret_cast<const float4 *>(p.partial_o) + c * 256 + r;
+    constexpr int kStep = 2 * 256;                     // rows from one block's share to the next one's
+    const size_t first = (size_t)(2 * t.block0 + 1) * 256, others = (size_t)(2 * t.block0) * 256;   // (a block's second share begins a unit)
     const int count = t.block1 - t.block0 + 1;
-    auto slot_of = [&](int n) { return 2 * (t.block0 + n) + (n == 0 ? 1 : 0); };
+    auto at = [&](int n) { return n ? others + (size_t)n * kStep : first; };
+    float top = -INFINITY, total = 0.f;
     int flag = 0;
-    for (int n = lane; n < count; n += 32) flag |= p.flags[slot_of(n)];
-    flag = __reduce_or_sync(0xffffffffu, flag);
-    if (r == 0) note(p, t.b, flag, lane);
+    for (int n = 0; n < count; ++n) {
+        top = fmaxf(top, ml[at(n)].x);
+        flag |= p.flags[at(n) / 256];
+    }
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int n = 0; n < count; ++n) {
+        const float2 s = ml[at(n)];
+        const float4 y = o[at(n) * (D / 4)];
+        const float w = s.x == -INFINITY ? 0.f : s.x == top ? 1.f : ex2((s.x - top) * p.scale_log2);
+        total = fmaf(s.y, w, total);
+        x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
+    }
     const int g = t.rt * 256 + r, j = node_of(p, g);
-    const Row y = merge_row<D>(
-        count, p.scale_log2, [&](int n) { return p.partial_ml[(size_t)slot_of(n) * 256 + r]; },
-        [&](int n) { return *reinterpret_cast<const float4 *>(p.partial_o + ((size_t)slot_of(n) * 256 + r) * D + lane * 4); });
-    put_row<D>(p, ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G), y, flag);
+    const size_t row = ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G);
+    const float inv = total == 0.f ? 0.f : 1.f / total;   // (a row that sees nothing: zeros)
+    *reinterpret_cast<uint2 *>(p.out + row * D + c * 4) = flag ? make_uint2(0u, 0u) : make_uint2(pack(x.x * inv, x.y * inv), pack(x.z * inv, x.w * inv));
+    if (c != 0) return;
+    if (p.lse) p.lse[row] = flag ? 0.f : fmaf(top, p.scale, log2f(total) * 0.6931471805599453f);
+    if (r == 0) note(p, t.b, flag, 0);
 }
 
 }  // namespace
@@ -853,7 +869,7 @@ reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &params, 
     launch_q4_attn_zero(p, n_sm, st);
     launch_pdl(p.D == 128 ? q4_attn_sm100_kernel<128> : q4_attn_sm100_kernel<64>, dim3((unsigned)n_sm), dim3(kThreads),
                (size_t)(p.D == 128 ? Cfg<128>::kSmem : Cfg<64>::kSmem), st, p);
-    launch_pdl(p.D == 128 ? q4_attn_merge_kernel<128> : q4_attn_merge_kernel<64>, dim3((unsigned)n_sm, (unsigned)((std::min(256, p.T * p.G) + 7) / 8)), dim3(256), 0,
+    launch_pdl(p.D == 128 ? q4_attn_merge_kernel<128> : q4_attn_merge_kernel<64>, dim3((unsigned)n_sm, (unsigned)((std::min(256, p.T * p.G) + 7) / 8)), dim3(2 * p.D), 0,
                st, p);
     return READER_OK;
 }
