@@ -530,18 +530,15 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         int n = 0, raw = 0, trees = 0;   // tiles, slots of the ring, trees so far
         Piece x;
         for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
-            for (int i = 0; i < x.tiles && !gone(abort_s); ++i, ++n) {
-                const int buf = n & 1;
-                if (buf != group) {
-                    if (x.is_tree(i)) ++trees;
-                    else raw += 2;
-                    continue;
-                }
-                const uint32_t kt = base + C::kOffK + buf * C::kKBytes, vt = base + C::kOffV + buf * C::kVBytes;
-                const bool tree = x.is_tree(i);
+            const bool has_tree = x.is_tree(x.tiles - 1);
+            for (int i = (n ^ group) & 1; i < x.tiles; i += 2) {
+                const uint32_t kt = base + C::kOffK + group * C::kKBytes, vt = base + C::kOffV + group * C::kVBytes;
+                const uint32_t free = (((n + i) >> 1) & 1) ^ 1;
+                const bool tree = has_tree && i == x.tiles - 1;
                 const int valid = x.valid(p.T, i);
+                int s = (raw + 2 * i) % kRawSlots, full = ((raw + 2 * i) / kRawSlots) & 1;
                 // keys
-                if (!wait(bar(&m->k_empty[buf]), ((n >> 1) & 1) ^ 1, abort_s)) break;
+                if (!wait(bar(&m->k_empty[group]), free, abort_s)) break;
                 if (tree) {
                     unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
                     if (t < p.T) {
@@ -550,40 +547,40 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         if (!(t == 0 ? a == -1 : a >= 0 && a < t)) atomicOr(&m->flags[seg & (kAhead - 1)], kBadTree);
                     }
                     copy_tree_keys<D>(p, x.b, x.h, kt, t);
-                    ++trees;
                 } else {
-                    const int s = raw % kRawSlots;
-                    if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
+                    if (!wait(bar(&m->raw_full[s]), full, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
                     if (m->raw_bad[s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
-                    ++raw;
+                    full ^= s == kRawSlots - 1;
+                    s = s == kRawSlots - 1 ? 0 : s + 1;
                 }
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&m->k_full[buf]));
+                if (lane == 0) mbar_arrive(bar(&m->k_full[group]));
                 // values
-                if (!wait(bar(&m->v_empty[buf]), ((n >> 1) & 1) ^ 1, abort_s)) break;
+                if (!wait(bar(&m->v_empty[group]), free, abort_s)) break;
                 if (tree) {
                     if (copy_tree_values<D>(p, x.b, x.h, vt, t)) atomicOr(&m->poison[seg & (kAhead - 1)], 1);
                 } else {
-                    const int s = raw % kRawSlots;
-                    if (!wait(bar(&m->raw_full[s]), (raw / kRawSlots) & 1, abort_s)) break;
+                    if (!wait(bar(&m->raw_full[s]), full, abort_s)) break;
                     const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page)
                         unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t, sixteen);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
-                    ++raw;
                 }
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&m->v_full[buf]));
+                if (lane == 0) mbar_arrive(bar(&m->v_full[group]));
             }
+            n += x.tiles;
+            raw += 2 * (x.tiles - has_tree);
+            trees += has_tree;
         }
     } else {
         // ------------------------------------------------------------------ softmax, results
