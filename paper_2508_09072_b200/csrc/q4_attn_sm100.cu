@@ -41,8 +41,9 @@ constexpr int kSoftmaxThreads = 256;
 constexpr int kUnpackWarp = 8, kLoadWarp = 16, kMmaWarp = 17, kQueryWarp = 18, kListWarp = 19;
 constexpr int kUnpackThreads = 128, kUnpackWarps = 4;   // of a tile
 constexpr int kReaders = 19;       // warps that read the ring of units: all but kListWarp
-// Registers of a thread: softmax, unpacking, the rest: 256 x 120 + 256 x 88 + 128 x 64 = the 640 x 96 that the block is launched with.
-constexpr int kRegsSoftmax = 120, kRegsUnpack = 88, kRegsRest = 64;
+// Registers of a thread: softmax, unpacking, the rest: 256 x 112 + 256 x 96 + 128 x 64 = the 640 x 96 that the block is launched with.
+constexpr int kRegsSoftmax = 112, kRegsUnpack = 96, kRegsRest = 64;
+static_assert(2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsRest <= 5 * 96 && kRegsSoftmax >= 96 && kRegsUnpack <= 96 && kRegsRest <= 96, "what a block is launched with");
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
 constexpr int kUnitCost = 6;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = 8;     // of a range
@@ -142,27 +143,28 @@ __device__ __forceinline__ void unpack_keys(uint32_t raw, uint32_t tile, int row
     constexpr int kSplit = 128 / (8 * kWords);
     const int w = t % kWords, g = (t / kWords) & 7, u = w >> 1, j0 = t / (kWords * 8) * (8 / kSplit);
     // the codes of the positions 8 j + g: bytes kPer j + u mod kPer of 8 kPer
-    const uint32_t at = raw + scales_at(D) + (g * 4 + u / kPer) * 8 * kPer + j0 * kPer;
-    uint32_t codes[4] = {};
-    if constexpr (D == 128) { const uint4 x = lds128(at); codes[0] = x.x; codes[1] = x.y; codes[2] = x.z; codes[3] = x.w; }
-    else codes[0] = lds32(at);
-    const uint32_t dst = tile + (w >> 3) * Cfg<D>::kBlock + (row0 + 8 * j0 + g) * 128 + (((w & 7) ^ g) << 4), src = raw + (8 * j0 + g) * (D / 2) + w * 4;
-    constexpr int kWordsHere = 8 / kSplit;
-    uint32_t word[kWordsHere];
-#pragma unroll
-    for (int j = 0; j < kWordsHere; ++j) word[j] = lds32(src + j * 8 * (D / 2));
+    uint32_t at = raw + scales_at(D) + (g * 4 + u / kPer) * 8 * kPer + j0 * kPer;
+    uint32_t dst = tile + (w >> 3) * Cfg<D>::kBlock + (row0 + 8 * j0 + g) * 128 + (((w & 7) ^ g) << 4), src = raw + (8 * j0 + g) * (D / 2) + w * 4;
     const uint32_t odd = kPer == 2 ? (u & 1) * 0x0101u : 0u;
-    auto go = [&](auto whole) {
+#pragma unroll 1
+    for (int n = 0; n < 8 / kSplit; n += 4, at += 4 * kPer, src += 4 * 8 * (D / 2), dst += 4 * 8 * 128) {   // (all eight at once: more code than the instruction caches like)
+        uint32_t codes[2] = {}, word[4];
+        if constexpr (D == 128) { const uint2 x = lds64(at); codes[0] = x.x; codes[1] = x.y; }
+        else codes[0] = lds32(at);
 #pragma unroll
-        for (int j = 0; j < kWordsHere; ++j) {
-            constexpr bool kWhole = decltype(whole)::value;
-            const uint32_t sel = 0x4040u | (j * kPer & 3) * 0x0101u;
-            const Scale2 s = scale2<kWhole>(__byte_perm(codes[j * kPer >> 2], 0, sel + odd));
-            sts128(dst + j * 8 * 128, pair<0>(word[j], s, sixteen), pair<1>(word[j], s, sixteen), pair<2>(word[j], s, sixteen), pair<3>(word[j], s, sixteen));
-        }
-    };
-    if (nan_bits(codes[0]) | nan_bits(codes[1]) | nan_bits(codes[2]) | nan_bits(codes[3])) go(std::false_type());
-    else go(std::true_type());
+        for (int j = 0; j < 4; ++j) word[j] = lds32(src + j * 8 * (D / 2));
+        auto go = [&](auto whole) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                constexpr bool kWhole = decltype(whole)::value;
+                const uint32_t sel = 0x4040u | (j * kPer & 3) * 0x0101u;
+                const Scale2 s = scale2<kWhole>(__byte_perm(codes[j * kPer >> 2], 0, sel + odd));
+                sts128(dst + j * 8 * 128, pair<0>(word[j], s, sixteen), pair<1>(word[j], s, sixteen), pair<2>(word[j], s, sixteen), pair<3>(word[j], s, sixteen));
+            }
+        };
+        if (nan_bits(codes[0]) | nan_bits(codes[1])) go(std::false_type());
+        else go(std::true_type());
+    }
 }
 // A page of values into a page of V^T, `valid` of its positions committed (the others become 0).  Thread (q, z, f): the positions 8 q .. + 7 of half f
 // of the elements z D/8 .. + D/8 - 1.
@@ -215,16 +217,18 @@ __device__ __forceinline__ void unpack_values(uint32_t raw, uint32_t page, int v
             if (key + 1 >= valid) { s[e].s &= 0xffffu; s[e].m24 &= 0xffffu; }
         }
     }
-#pragma unroll
+    const uint32_t rows = page + (z * (D / 8) + f * (D / 16)) * 128;
+#pragma unroll 1
     for (int y = 0; y < kWords; ++y) {
         // row d = z D/8 + f D/16 + 4 y + i
-        const uint32_t rows = page + (z * (D / 8) + f * (D / 16)) * 128;
-        const int turn = D == 128 ? 0 : 4 * f;   // (of the row's number, what its place in the swizzle goes by)
-        auto row = [&](int i) { return rows + (4 * y + i) * 128 + ((q ^ ((turn + 4 * y + i) & 7)) << 4); };
-        sts128(row(0), pair<0>(w[0][y], s[0], sixteen), pair<0>(w[1][y], s[1], sixteen), pair<0>(w[2][y], s[2], sixteen), pair<0>(w[3][y], s[3], sixteen));
-        sts128(row(1), pair<1>(w[0][y], s[0], sixteen), pair<1>(w[1][y], s[1], sixteen), pair<1>(w[2][y], s[2], sixteen), pair<1>(w[3][y], s[3], sixteen));
-        sts128(row(2), pair<2>(w[0][y], s[0], sixteen), pair<2>(w[1][y], s[1], sixteen), pair<2>(w[2][y], s[2], sixteen), pair<2>(w[3][y], s[3], sixteen));
-        sts128(row(3), pair<3>(w[0][y], s[0], sixteen), pair<3>(w[1][y], s[1], sixteen), pair<3>(w[2][y], s[2], sixteen), pair<3>(w[3][y], s[3], sixteen));
+        const int turn = 4 * y + (D == 128 ? 0 : 4 * f);   // (of the row's number, what its place in the swizzle goes by)
+        auto row = [&](int i) { return rows + (4 * y + i) * 128 + ((q ^ (turn + i)) << 4); };
+        sts128(row(0), pair<0>(w[0][0], s[0], sixteen), pair<0>(w[1][0], s[1], sixteen), pair<0>(w[2][0], s[2], sixteen), pair<0>(w[3][0], s[3], sixteen));
+        sts128(row(1), pair<1>(w[0][0], s[0], sixteen), pair<1>(w[1][0], s[1], sixteen), pair<1>(w[2][0], s[2], sixteen), pair<1>(w[3][0], s[3], sixteen));
+        sts128(row(2), pair<2>(w[0][0], s[0], sixteen), pair<2>(w[1][0], s[1], sixteen), pair<2>(w[2][0], s[2], sixteen), pair<2>(w[3][0], s[3], sixteen));
+        sts128(row(3), pair<3>(w[0][0], s[0], sixteen), pair<3>(w[1][0], s[1], sixteen), pair<3>(w[2][0], s[2], sixteen), pair<3>(w[3][0], s[3], sixteen));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k][0] = w[k][kWords - 1];
     }
 }
 // The tree's own keys as a K tile.
@@ -619,38 +623,52 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 s_parity ^= 1u << slot;
                 tc_fence_after();
                 if (warp_live) {
-                    uint32_t s[64];
-                    tmem_ld32(tS, reinterpret_cast<uint32_t(&)[32]>(s[0]));
-                    tmem_ld32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(s[32]));
                     const int valid = x.valid(p.T, t) - half * 64;   // of this half's keys
-                    uint64_t sees = ~0ull;                           // the ones this row sees
-                    if (x.is_tree(t)) {
-                        const int g = x.rt * 256 + r, node = live ? node_of(p, g) : 0;
-                        sees = 0;
-                        if (live && p.anc) {
-                            sees = p.anc[((size_t)x.b * p.T + node) * 2 + half];
-                        } else if (live && !(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
-                            const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
-                            for (int n = node; n != 255; n = parents[n])   // (strictly falling on a valid tree)
-                                if ((n >> 6) == half) sees |= 1ull << (n & 63);
+                    if (valid < 64 || x.is_tree(t)) {                // scores of keys that a row does not see become -inf
+                        uint64_t sees = ~0ull;
+                        if (x.is_tree(t)) {
+                            const int g = x.rt * 256 + r, node = live ? node_of(p, g) : 0;
+                            sees = 0;
+                            if (live && p.anc) {
+                                sees = p.anc[((size_t)x.b * p.T + node) * 2 + half];
+                            } else if (live && !(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
+                                const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
+                                for (int n = node; n != 255; n = parents[n])   // (strictly falling on a valid tree)
+                                    if ((n >> 6) == half) sees |= 1ull << (n & 63);
+                            }
                         }
+                        if (valid < 64) sees &= valid <= 0 ? 0 : (1ull << valid) - 1;
+#pragma unroll 1
+                        for (int c = 0; c < 64; c += 16, sees >>= 16) {
+                            uint32_t y[16];
+                            tmem_ld16(tS + c, y);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                if (!((sees >> k) & 1)) y[k] = kNegInf;
+                            tmem_st16(tS + c, y);
+                        }
+                        tmem_wait_st();
                     }
-                    if (valid < 64) sees &= valid <= 0 ? 0 : (1ull << valid) - 1;
+                    // Half of the scores at a time, the second ones first, so that the first are at hand for what follows
+                    uint32_t s[32];
                     auto f = [&](int k) { return __uint_as_float(s[k]); };
-                    tmem_wait_ld();
-                    if (valid < 64 || x.is_tree(t)) {
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c = 32; c >= 0; c -= 32) {
+                        tmem_ld32(tS + c, s);
+                        tmem_wait_ld();
+                        float a[4];
 #pragma unroll
-                        for (int k = 0; k < 64; ++k)
-                            if (!((sees >> k) & 1)) s[k] = kNegInf;
+                        for (int k = 0; k < 4; ++k) a[k] = max3(f(8 * k), f(8 * k + 1), f(8 * k + 2));
+#pragma unroll
+                        for (int i = 3; i < 7; i += 2)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) a[k] = max3(a[k], f(8 * k + i), f(8 * k + i + 1));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) a[k] = fmaxf(a[k], f(8 * k + 7));
+                        top = max3(max3(top, a[0], a[1]), a[2], a[3]);
                     }
-                    float a[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) a[c] = max3(f(3 * c), f(3 * c + 1), f(3 * c + 2));
-#pragma unroll
-                    for (int k = 12; k < 60; k += 8)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) a[c] = max3(a[c], f(k + 2 * c), f(k + 2 * c + 1));
-                    float top = max3(max3(a[0], f(60), f(61)), max3(a[1], f(62), f(63)), fmaxf(a[2], a[3]));
                     int raise;
                     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.gt.f32 p, %1, %2;\n\tbarrier.cta.red.or.pred q, %3, 64, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
                                  : "=r"(raise) : "f"(top), "f"(mx + by), "r"(5 + (warp & 3)) : "memory");
@@ -683,23 +701,37 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     // row: it cancels, but where it is so large that its rounding is not small against 1 the difference is taken first.
                     float from = mx == -INFINITY ? 0.f : -mx * p.scale_log2;
                     if (__any_sync(0xffffffffu, fabsf(from) > 65536.f && fabsf(from) < INFINITY)) {
+#pragma unroll 1
+                        for (int c = 0; c < 64; c += 16) {
+                            uint32_t y[16];
+                            tmem_ld16(tS + c, y);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int k = 0; k < 64; ++k) s[k] = __float_as_uint(f(k) - (mx == -INFINITY ? 0.f : mx));
+                            for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) - (mx == -INFINITY ? 0.f : mx));
+                            tmem_st16(tS + c, y);
+                        }
+                        tmem_wait_st();
+                        tmem_ld32(tS, s);
+                        tmem_wait_ld();
                         from = 0.f;
                     }
                     const float2 from2 = make_float2(from, from), sc = make_float2(p.scale_log2, p.scale_log2);
                     float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
+#pragma unroll 1
+                    for (int c = 0; c < 32; c += 16) {   // (probabilities over scores that have been read)
                         uint32_t pk[16];
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            const float2 y = __ffma2_rn(make_float2(f(c * 32 + 2 * k), f(c * 32 + 2 * k + 1)), sc, from2);
+                            const float2 y = __ffma2_rn(make_float2(f(2 * k), f(2 * k + 1)), sc, from2);
                             const float2 e = make_float2(ex2(y.x), ex2(y.y));
                             sum = __fadd2_rn(sum, e);
                             pk[k] = pack(e.x, e.y);
                         }
-                        tmem_st16(tS + c * 16, pk);
+                        tmem_st16(tS + c, pk);
+                        if (c == 0) {
+                            tmem_ld32(tS + 32, s);
+                            tmem_wait_ld();
+                        }
                     }
                     l += sum.x + sum.y;
                     tmem_wait_st();
