@@ -45,8 +45,8 @@ constexpr int kReaders = 19;       // warps that read the ring of units: all but
 constexpr int kRegsSoftmax = 112, kRegsUnpack = 96, kRegsRest = 64;
 static_assert(2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsRest <= 5 * 96 && kRegsSoftmax >= 96 && kRegsUnpack <= 96 && kRegsRest <= 96, "what a block is launched with");
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
-constexpr int kUnitCost = 6;       // entries that stand for a unit's start and end
-constexpr int kMinEntries = 8;     // of a range
+constexpr int kUnitCost = 4;       // entries that stand for a unit's start and end (6: 32 x 32 nodes 82 instead of 80 us)
+constexpr int kMinEntries = kUnitCost + 2;   // of a range: so every one of them holds a tile
 constexpr int kRawSlots = 3;       // of the ring: keys or values of a tile's pages each
 constexpr int kAhead = 8;          // units in the ring
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
@@ -443,15 +443,18 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 const int after = x.wide || wide_before ? 1 : 2;   // the unit that was there before: that many before this
                 if (seg >= after) wait(bar(&m->q_empty[(seg - after) & 1]), ((seg - after) >> 1) & 1, abort_s);
                 wide_before = x.wide;
-                const uint32_t place = base + C::kOffQ + (x.wide ? 0 : (seg & 1) * C::kQBytes) + (ch >> 3) * C::kBlock;
-                const int rows = x.wide ? 256 : 128;
-#pragma unroll 4
-                for (int r = r0; r < rows; r += kRowsAtOnce) {
-                    const bool live = r < x.rows;
-                    const int g = x.rt * 256 + (live ? r : 0), j = node_of(p, g);
-                    const __nv_bfloat16 *src = p.q + (((size_t)x.b * p.T + j) * p.Hq + x.h * p.G + (g - j * p.G)) * D + ch * 8;
-                    const uint32_t dst = place + (r >> 7) * C::kQBytes + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4);
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+                // row r of the head: of node g / G, (j Hq + h G + g - j G) D elements behind the sequence's first
+                const __nv_bfloat16 *src = p.q + ((size_t)x.b * p.T * p.Hq + x.h * p.G) * D + ch * 8;
+                uint32_t dst = base + C::kOffQ + (x.wide ? 0 : (seg & 1) * C::kQBytes) + (ch >> 3) * C::kBlock + r0 * 128;
+                for (int r = r0; r < (x.wide ? 256 : 128); r += 8, dst += 8 * 128) {
+                    if (r == 128 + r0) dst += C::kQBytes - C::kBlock;
+#pragma unroll
+                    for (int i = 0; i < 8; i += kRowsAtOnce) {
+                        const bool live = r + i < x.rows;
+                        const int g = x.rt * 256 + (live ? r + i : 0);
+                        const __nv_bfloat16 *at = src + (size_t)(unsigned)(node_of(p, g) * (p.Hq - p.G) + g) * D;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 128 + (((ch & 7) ^ (r0 + i)) << 4)), "l"(at), "r"(live ? 16 : 0) : "memory");
+                    }
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_proxy_async();
@@ -859,18 +862,41 @@ __global__ void __launch_bounds__(2 * D) q4_attn_merge_kernel(const __grid_const
     auto at = [&](int n) { return n ? others + (size_t)n * kStep : first; };
     float top = -INFINITY, total = 0.f;
     int flag = 0;
-    for (int n = 0; n < count; ++n) {
-        top = fmaxf(top, ml[at(n)].x);
-        flag |= p.flags[at(n) / 256];
-    }
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int n = 0; n < count; ++n) {
-        const float2 s = ml[at(n)];
-        const float4 y = o[at(n) * (D / 4)];
-        const float w = s.x == -INFINITY ? 0.f : s.x == top ? 1.f : ex2((s.x - top) * p.scale_log2);
-        total = fmaf(s.y, w, total);
-        x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
+    constexpr int kAtOnce = 4;   // shares that are read before the first is used
+#pragma unroll 1
+    for (int n0 = 0; n0 < count; n0 += kAtOnce) {
+        float2 s[kAtOnce];
+        float4 y[kAtOnce];
+        int f[kAtOnce];
+        float now = top;
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            const size_t k = at(n0 + n);
+            s[n] = make_float2(-INFINITY, 0.f);
+            y[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+            f[n] = 0;
+            if (n0 + n < count) {
+                s[n] = ml[k];
+                y[n] = o[k * (D / 4)];
+                f[n] = p.flags[k / 256];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            now = fmaxf(now, s[n].x);
+            flag |= f[n];
+        }
+        const float keep = top == now ? 1.f : ex2((top - now) * p.scale_log2);
+        top = now;
+        total *= keep;
+        x.x *= keep; x.y *= keep; x.z *= keep; x.w *= keep;
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            const float w = s[n].x == -INFINITY ? 0.f : s[n].x == top ? 1.f : ex2((s[n].x - top) * p.scale_log2);
+            total = fmaf(s[n].y, w, total);
+            x.x = fmaf(y[n].x, w, x.x); x.y = fmaf(y[n].y, w, x.y); x.z = fmaf(y[n].z, w, x.z); x.w = fmaf(y[n].w, w, x.w);
+        }
     }
     const int g = t.rt * 256 + r, j = node_of(p, g);
     const size_t row = ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G);
