@@ -278,13 +278,19 @@ PyObject *prompt_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // ---- the 4-bit cache and the page calls
 
+// A name that attributes are asked for by, made once (a string made for every question costs more than the question).
+struct Name {
+    const char *text;
+    PyObject *o;
+    explicit Name(const char *s) : text(s), o(PyUnicode_InternFromString(s)) {}
+};
 // An attribute of a cache or pages object, for as long as this lives.
 struct Attr {
     PyObject *o;
-    Attr(PyObject *from, const char *name) : o(PyObject_GetAttrString(from, name)) {
+    Attr(PyObject *from, const Name &name) : o(name.o ? PyObject_GetAttr(from, name.o) : nullptr) {
         if (!o) {
             PyErr_Clear();
-            wrong_type(name, "the object has no such attribute");
+            wrong_type(name.text, "the object has no such attribute");
         }
     }
     ~Attr() { Py_DECREF(o); }
@@ -306,9 +312,17 @@ struct Items {
     PyObject *operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(seq, i); }
 };
 
+const Name &k_pool_name() { static const Name n("k_pool"); return n; }
+const Name &v_pool_name() { static const Name n("v_pool"); return n; }
+const Name &table_name() { static const Name n("page_table"); return n; }
+const Name &lens_name() { static const Name n("seq_lens"); return n; }
+const Name &prefix_name() { static const Name n("shared_prefix_len"); return n; }
+const Name &refs_name() { static const Name n("refs"); return n; }
+const Name &pools_name() { static const Name n("pools"); return n; }
+
 // A KvCache (bf16 pools) or a Q4Cache (4-bit ones).
 Cache cache_object(PyObject *o, bool narrow, int device) {
-    const Attr ko(o, "k_pool"), vo(o, "v_pool"), to(o, "page_table"), lo(o, "seq_lens"), po(o, "shared_prefix_len");
+    const Attr ko(o, k_pool_name()), vo(o, v_pool_name()), to(o, table_name()), lo(o, lens_name()), po(o, prefix_name());
     if (!narrow) {
         PyObject *const a[5] = {ko.o, vo.o, to.o, lo.o, po.o};
         return cache_of(a, device);
@@ -441,7 +455,7 @@ int64_t bytes_of_page(const at::Tensor &t, int64_t num_pages, const char *name) 
     return num_pages ? (int64_t)t.nbytes() / num_pages : 0;
 }
 void pages_of(PyObject *o, int device, bool with_pools, PagesArgs &r) {
-    const Attr ro(o, "refs"), to(o, "page_table"), lo(o, "seq_lens");
+    const Attr ro(o, refs_name()), to(o, table_name()), lo(o, lens_name());
     const at::Tensor &refs = dense(ro.o, at::kInt, 1, device, "refs"), &table = dense(to.o, at::kInt, 2, device, "page_table");
     r.p = reader_pages{};
     r.p.refs = static_cast<int32_t *>(address(refs));
@@ -451,7 +465,7 @@ void pages_of(PyObject *o, int device, bool with_pools, PagesArgs &r) {
     r.p.max_pages_per_seq = small(table.size(1), "page_table");
     r.p.seq_lens = const_cast<int32_t *>(ints(lo.o, table.size(0), device, "seq_lens"));
     if (!with_pools) return;
-    const Attr po(o, "pools");
+    const Attr po(o, pools_name());
     const Items pools(po.o, "pools");
     for (Py_ssize_t i = 0; i < pools.n; ++i) {
         const at::Tensor &t = tensor(pools[i], "pools");

@@ -13,6 +13,29 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// A block of 16 elements in bf16: 32 bytes, by one instruction where the pools lie on such a border (two of 16 bytes each ask for every 32-byte sector
+// twice), streamed past the caches' other users.
+__device__ __forceinline__ void load_block(const uint4 *at, bool whole, uint4 (&x)[2]) {
+    if (whole) {
+        asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(x[0].x), "=r"(x[0].y), "=r"(x[0].z), "=r"(x[0].w), "=r"(x[1].x), "=r"(x[1].y), "=r"(x[1].z), "=r"(x[1].w)
+                     : "l"(at));
+    } else {
+        x[0] = __ldcs(at);
+        x[1] = __ldcs(at + 1);
+    }
+}
+__device__ __forceinline__ void store_block(uint4 *at, bool whole, const uint4 &a, const uint4 &b) {
+    if (whole) {
+        asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x),
+                     "r"(b.y), "r"(b.z), "r"(b.w)
+                     : "memory");
+    } else {
+        __stcs(at, a);
+        __stcs(at + 1, b);
+    }
+}
+
 // What keeps the positions first .. last - 1 of sequence b from being converted.  Block-collective.
 __device__ __forceinline__ int convert_status(const Q4Convert &p, int b, int first, int last) {
     if (last <= first) return READER_OK;
@@ -28,7 +51,7 @@ __device__ __forceinline__ int convert_status(const Q4Convert &p, int b, int fir
 
 // One tile (page, head): rows lo .. hi - 1 of a bf16 tile of keys (values) to a 4-bit one.
 template <int D>
-__device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bfloat16 *v, unsigned char *k4, unsigned char *v4, int lo, int hi) {
+__device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bfloat16 *v, unsigned char *k4, unsigned char *v4, int lo, int hi, bool whole) {
     constexpr int kBlocks = D / q4::kBlock, kKeyTasks = kPage * kBlocks / kThreads, kPairs = kPage / 2 * kBlocks;
     const int tid = threadIdx.x;
     uint4 x[kKeyTasks][2], y[2][2];
@@ -36,9 +59,7 @@ __device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bf
     for (int i = 0; i < kKeyTasks; ++i) {
         const int task = i * kThreads + tid, r = task / kBlocks;
         if (r < lo || r >= hi) continue;
-        const uint4 *at = reinterpret_cast<const uint4 *>(k) + task * 2;
-        x[i][0] = __ldcs(at);
-        x[i][1] = __ldcs(at + 1);
+        load_block(reinterpret_cast<const uint4 *>(k) + task * 2, whole, x[i]);
     }
     const int t = tid / kBlocks, u = tid % kBlocks;   // value pair of this thread (128 of the 256 have none at head_dim 64)
     bool has[2];
@@ -47,9 +68,7 @@ __device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bf
         has[e] = tid < kPairs && 2 * t + e >= lo && 2 * t + e < hi;
         y[e][0] = y[e][1] = make_uint4(0, 0, 0, 0);
         if (!has[e]) continue;
-        const uint4 *at = reinterpret_cast<const uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2;
-        y[e][0] = __ldcs(at);
-        y[e][1] = __ldcs(at + 1);
+        load_block(reinterpret_cast<const uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2, whole, y[e]);
     }
 #pragma unroll
     for (int i = 0; i < kKeyTasks; ++i) {
@@ -62,7 +81,7 @@ __device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bf
 
 // The other way.
 template <int D>
-__device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigned char *v4, __nv_bfloat16 *k, __nv_bfloat16 *v, int lo, int hi) {
+__device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigned char *v4, __nv_bfloat16 *k, __nv_bfloat16 *v, int lo, int hi, bool whole) {
     constexpr int kBlocks = D / q4::kBlock, kKeyTasks = kPage * kBlocks / kThreads, kPairs = kPage / 2 * kBlocks;
     const int tid = threadIdx.x;
     uint2 kw[kKeyTasks];
@@ -88,19 +107,18 @@ __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigne
         const int task = i * kThreads + tid, r = task / kBlocks;
         if (r < lo || r >= hi) continue;
         const float s = q4::scale_of(kc[i]);
-        uint4 *at = reinterpret_cast<uint4 *>(k) + task * 2;
-        __stcs(at, q4::values_of(q4::evens_apart(q4::plain_of(kw[i].x)), s));
-        __stcs(at + 1, q4::values_of(q4::evens_apart(q4::plain_of(kw[i].y)), s));
+        store_block(reinterpret_cast<uint4 *>(k) + task * 2, whole, q4::values_of(q4::evens_apart(q4::plain_of(kw[i].x)), s),
+                    q4::values_of(q4::evens_apart(q4::plain_of(kw[i].y)), s));
     }
     const uint32_t w[4] = {q4::plain_of(vw.x), q4::plain_of(vw.y), q4::plain_of(vw.z), q4::plain_of(vw.w)};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         if (!has[e]) continue;
         const float s = q4::scale_of((vc >> (8 * e)) & 255);
-        uint4 *at = reinterpret_cast<uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2;
         const int sh = 16 * e;
-        __stcs(at, q4::values_of(((w[0] >> sh) & 0xffffu) | (((w[1] >> sh) & 0xffffu) << 16), s));
-        __stcs(at + 1, q4::values_of(((w[2] >> sh) & 0xffffu) | (((w[3] >> sh) & 0xffffu) << 16), s));
+        store_block(reinterpret_cast<uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2, whole,
+                    q4::values_of(((w[0] >> sh) & 0xffffu) | (((w[1] >> sh) & 0xffffu) << 16), s),
+                    q4::values_of(((w[2] >> sh) & 0xffffu) | (((w[3] >> sh) & 0xffffu) << 16), s));
     }
 }
 
@@ -126,10 +144,10 @@ __global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p,
         constexpr size_t kWide = (size_t)kPage * D, kNarrow = q4::tile_bytes(D);
         if (kStore)
             store_tile<D>(static_cast<const __nv_bfloat16 *>(layers.k_from[l]) + from * kWide, static_cast<const __nv_bfloat16 *>(layers.v_from[l]) + from * kWide,
-                          static_cast<unsigned char *>(layers.k_to[l]) + to * kNarrow, static_cast<unsigned char *>(layers.v_to[l]) + to * kNarrow, lo, hi);
+                          static_cast<unsigned char *>(layers.k_to[l]) + to * kNarrow, static_cast<unsigned char *>(layers.v_to[l]) + to * kNarrow, lo, hi, p.whole);
         else
             load_tile<D>(static_cast<const unsigned char *>(layers.k_from[l]) + from * kNarrow, static_cast<const unsigned char *>(layers.v_from[l]) + from * kNarrow,
-                         static_cast<__nv_bfloat16 *>(layers.k_to[l]) + to * kWide, static_cast<__nv_bfloat16 *>(layers.v_to[l]) + to * kWide, lo, hi);
+                         static_cast<__nv_bfloat16 *>(layers.k_to[l]) + to * kWide, static_cast<__nv_bfloat16 *>(layers.v_to[l]) + to * kWide, lo, hi, p.whole);
     }
 }
 
@@ -203,6 +221,12 @@ void launch_q4_convert(bool store, Q4Convert p, const Q4Layers *chunks, int n_la
         const int64_t share = (16 * (int64_t)n_sm + p.B - 1) / p.B;
         p.per_seq = (int)(tiles < share ? tiles : share);
         p.status = l0 == 0 ? const_cast<int32_t *>(status) : nullptr;
+        const Q4Layers &c = chunks[l0 / kQ4LayersPerLaunch];
+        uintptr_t places = 0;
+        for (int l = 0; l < p.layers; ++l)
+            places |= store ? reinterpret_cast<uintptr_t>(c.k_from[l]) | reinterpret_cast<uintptr_t>(c.v_from[l])
+                            : reinterpret_cast<uintptr_t>(c.k_to[l]) | reinterpret_cast<uintptr_t>(c.v_to[l]);
+        p.whole = places % 32 == 0;
         auto kernel = p.D == 128 ? (store ? q4_convert_kernel<128, true> : q4_convert_kernel<128, false>)
                                  : (store ? q4_convert_kernel<64, true> : q4_convert_kernel<64, false>);
         launch_pdl(kernel, dim3((unsigned)(p.B * p.per_seq)), dim3(kThreads), 0, st, p, chunks[l0 / kQ4LayersPerLaunch]);

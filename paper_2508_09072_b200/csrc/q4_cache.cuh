@@ -18,6 +18,7 @@ struct Q4Convert {
     int shared_prefix_len;                 // of the destination
     int Hkv, D, B, layers;
     int per_seq;                           // thread blocks of a sequence
+    bool whole;                            // the bf16 pools lie on 32-byte borders
     int32_t *status;                       // null: not reported (layers behind the first launch)
 };
 void launch_q4_convert(bool store, Q4Convert p, const Q4Layers *chunks, int n_layers, int n_sm, cudaStream_t st);
