@@ -73,10 +73,10 @@ __device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bf
 #pragma unroll
     for (int i = 0; i < kKeyTasks; ++i) {
         const int task = i * kThreads + tid, r = task / kBlocks;
-        if (r >= lo && r < hi) q4::put_key_block<D>(k4, r, task % kBlocks, q4::quantise(x[i][0], x[i][1]));
+        if (r >= lo && r < hi) q4::put_key_block<D>(k4, r, task % kBlocks, q4::quantise<true>(x[i][0], x[i][1]));
     }
     if (has[0] || has[1])
-        q4::put_value_blocks<D>(v4, t, u, has[0], q4::quantise(y[0][0], y[0][1]), has[1], q4::quantise(y[1][0], y[1][1]));
+        q4::put_value_blocks<D>(v4, t, u, has[0], q4::quantise<false>(y[0][0], y[0][1]), has[1], q4::quantise<false>(y[1][0], y[1][1]));
 }
 
 // The other way.
@@ -107,8 +107,8 @@ __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigne
         const int task = i * kThreads + tid, r = task / kBlocks;
         if (r < lo || r >= hi) continue;
         const float s = q4::scale_of(kc[i]);
-        store_block(reinterpret_cast<uint4 *>(k) + task * 2, whole, q4::values_of(q4::evens_apart(q4::plain_of(kw[i].x)), s),
-                    q4::values_of(q4::evens_apart(q4::plain_of(kw[i].y)), s));
+        store_block(reinterpret_cast<uint4 *>(k) + task * 2, whole, q4::values_of(q4::in_order(q4::plain_of(kw[i].x)), s),
+                    q4::values_of(q4::in_order(q4::plain_of(kw[i].y)), s));
     }
     const uint32_t w[4] = {q4::plain_of(vw.x), q4::plain_of(vw.y), q4::plain_of(vw.z), q4::plain_of(vw.w)};
 #pragma unroll
@@ -124,7 +124,7 @@ __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigne
 
 // Blocks b * per_seq .. + per_seq - 1 walk the tiles (layer, page, head) of sequence b, heads fastest.
 template <int D, bool kStore>
-__global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p, const __grid_constant__ Q4Layers layers) {
+__global__ void __launch_bounds__(kThreads, kStore ? 4 : 1) q4_convert_kernel(const Q4Convert p, const __grid_constant__ Q4Layers layers) {
     pdl_wait();
     pdl_launch_dependents();
     const int b = blockIdx.x / p.per_seq, x = blockIdx.x - b * p.per_seq;
@@ -133,11 +133,11 @@ __global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p,
     if (x == 0 && threadIdx.x == 0 && p.status) p.status[b] = st;
     if (st != READER_OK || last <= first) return;
     const int page0 = first / kPage, n_pages = (last - 1) / kPage - page0 + 1;
-    const int64_t items = (int64_t)n_pages * p.Hkv * p.layers;
-    for (int64_t i = x; i < items; i += p.per_seq) {
-        const int h = (int)(i % p.Hkv);
-        const int64_t j = i / p.Hkv;
-        const int page = page0 + (int)(j % n_pages), l = (int)(j / n_pages);
+    // item (l, page, h) number x + k per_seq, by carrying (a division each time costs as much as an eighth of the tile)
+    const int q = x / p.Hkv, dq = p.per_seq / p.Hkv, dh = p.per_seq - dq * p.Hkv, dl = dq / n_pages, dj = dq - dl * n_pages;
+    int h = x - q * p.Hkv, l = q / n_pages, j = q - l * n_pages;
+    while (l < p.layers) {
+        const int page = page0 + j;
         const int lo = max(0, first - page * kPage), hi = min(kPage, last - page * kPage);
         const size_t from = (size_t)p.from_table[(size_t)b * p.from_width + page] * p.Hkv + h;
         const size_t to = (size_t)p.to_table[(size_t)b * p.to_width + page] * p.Hkv + h;
@@ -148,6 +148,11 @@ __global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p,
         else
             load_tile<D>(static_cast<const unsigned char *>(layers.k_from[l]) + from * kNarrow, static_cast<const unsigned char *>(layers.v_from[l]) + from * kNarrow,
                          static_cast<__nv_bfloat16 *>(layers.k_to[l]) + to * kWide, static_cast<__nv_bfloat16 *>(layers.v_to[l]) + to * kWide, lo, hi, p.whole);
+        h += dh;
+        j += dj;
+        l += dl;
+        if (h >= p.Hkv) { h -= p.Hkv; ++j; }
+        if (j >= n_pages) { j -= n_pages; ++l; }
     }
 }
 
@@ -185,14 +190,14 @@ __global__ void __launch_bounds__(kThreads) q4_commit_kernel(const Q4Commit p, c
         if (i < key_tasks) {
             const int k = i / per_pos, h = (i - k * per_pos) / kBlocks, u = i % kBlocks;
             const uint4 *src = row(layers.k_from[l], k, h, u);
-            q4::put_key_block<D>(tile(layers.k_to[l], L + k, h), (L + k) % kPage, u, q4::quantise(src[0], src[1]));
+            q4::put_key_block<D>(tile(layers.k_to[l], L + k, h), (L + k) % kPage, u, q4::quantise<true>(src[0], src[1]));
         } else {
             const int j = i - key_tasks, pair = j / per_pos, h = (j - pair * per_pos) / kBlocks, u = j % kBlocks;
             const int pos = 2 * (pair0 + pair);   // the pair's even position
             const bool has_even = pos >= L, has_odd = pos + 1 < L + n;
             const uint4 *even = row(layers.v_from[l], has_even ? pos - L : 0, h, u), *odd = row(layers.v_from[l], has_odd ? pos + 1 - L : 0, h, u);
             const uint4 x[4] = {even[0], even[1], odd[0], odd[1]};
-            q4::put_value_blocks<D>(tile(layers.v_to[l], pos, h), (pos % kPage) / 2, u, has_even, q4::quantise(x[0], x[1]), has_odd, q4::quantise(x[2], x[3]));
+            q4::put_value_blocks<D>(tile(layers.v_to[l], pos, h), (pos % kPage) / 2, u, has_even, q4::quantise<false>(x[0], x[1]), has_odd, q4::quantise<false>(x[2], x[3]));
         }
     }
     if (p.update) {   // the only block that reads this length

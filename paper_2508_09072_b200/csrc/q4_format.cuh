@@ -50,67 +50,88 @@ __device__ __forceinline__ float scale_of(int code) {
     return code == kNanCode ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(code + ((127 - kScaleBias) << 3)) << 20);
 }
 
-// The scale code of a block whose largest magnitude is `top` (finite, >= 0).  A first guess from the bits of top / 7.5, made
-// exact by comparing (7.5 s has at most 8 significant bits: no rounding).
-__device__ __forceinline__ int code_of(float top) {
-    int c = (int)(__float_as_uint(top * (1.f / 7.5f)) >> 20) - ((127 - kScaleBias) << 3);
-    c = max(0, min(c, kMaxCode));
-    while (c > 0 && 7.5f * scale_of(c - 1) >= top) --c;
-    while (c < kMaxCode && 7.5f * scale_of(c) < top) ++c;
-    return c;
+// The scale code of a block whose largest magnitude is the bf16 with these bits (finite, no sign).  Where it is (128 + t) / 128 2^e, the smallest m
+// with 7.5 (8 + m) / 8 2^(e - 3) no less has 15 (8 + m) >= 128 + t; m of 8 and 9 carry into the exponent and mean the scales they should.
+__device__ __forceinline__ int code_of(uint32_t top) {
+    const int e = (int)(top >> 7) - 127, t = top & 127;
+    return max(0, min(kMaxCode, (e - 3 + kScaleBias) * 8 + (128 + t + 14) / 15 - 8));
 }
 
-// x / s to the nearest whole number plus 8.  x * (1 / s) may miss a tie by one unit in the last place (it does for 15 / 8); one
-// correction with the remainder, which an fma gives without rounding, makes it the quotient.
-__device__ __forceinline__ uint32_t number_of(float x, float s, float r) {
-    float y = x * r;
-    y = fmaf(fmaf(-y, s, x), r, y);
-    y = fminf(fmaxf(y, -7.f), 7.f);
-    return __float_as_uint(y + 12582920.f) & 15u;   // 1.5 * 2^23 + 8: the whole part stands in the lowest bits, ties to even
+// 1 / s to within a unit in the last place or so.
+__device__ __forceinline__ float reciprocal(float s) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return r;
+}
+// Two bf16, each brought into least .. most.
+__device__ __forceinline__ uint32_t bf16x2_within(uint32_t x, uint32_t least, uint32_t most) {
+    uint32_t d;
+    asm("{\n\t.reg .b32 t;\n\tmax.bf16x2 t, %1, %2;\n\tmin.bf16x2 %0, t, %3;\n\t}" : "=r"(d) : "r"(x), "r"(least), "r"(most));
+    return d;
 }
 
 __device__ __forceinline__ uint32_t turned(uint32_t plain) { return __funnelshift_l(plain, plain, 3); }
 __device__ __forceinline__ uint32_t plain_of(uint32_t word) { return __funnelshift_r(word, word, 3); }
 
 struct Block {   // 16 elements
-    uint32_t n[2];   // element e at bits 4 (e mod 8) of n[e / 8]
+    uint32_t n[2];   // of eight elements each
     int code;
 };
 
-// raw: 16 bf16.
+// raw: 16 bf16.  Element e stands at bits 4 (e mod 8) of n[e / 8], or (kEvensApart) at 4 (e mod 8) / 2, odd ones 16 higher.
+// A number is x / s to the nearest whole one, ties to even, plus 8.  x * (1 / s) may miss a tie by some units in the last place; one
+// correction with the remainder, which an fma gives without rounding, makes it the quotient (to 2^-44, so exactly where that is a float).  Elements beyond 7 s (a bf16) are
+// that first: 7.5 s would become 8.  Added to 1.5 * 2^23 + 8 the numbers stand in the lowest bits of floats, and sixteen times one of them plus the next, as whole
+// numbers, is a shift and an or; what is above the numbers adds up to a constant.  (12 instructions for an element before, 6 now: a kernel
+// that stores was bound by them.)
+template <bool kEvensApart>
 __device__ __forceinline__ Block quantise(const uint4 &a, const uint4 &b) {
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t top = 0;   // magnitudes compare as whole numbers; infinity and NaN are the largest
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t tops = 0;   // magnitudes compare as whole numbers; infinity and NaN are the largest
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
+    for (int i = 0; i < 8; ++i) tops = __vmaxu2(tops, w[i] & 0x7fff7fffu);
+    const uint32_t top = max(tops << 16, tops & 0xffff0000u);
     Block r;
     if (top >= 0x7f800000u) {
         r.code = kNanCode;
         r.n[0] = r.n[1] = 0x88888888u;
         return r;
     }
-    r.code = code_of(__uint_as_float(top));
-    const float s = scale_of(r.code), inv = 1.f / s;
+    r.code = code_of(top >> 16);
+    const float s = scale_of(r.code), inv = reciprocal(s);
+    const uint32_t most = (__float_as_uint(7.f * s) >> 16) * 0x10001u, least = most | 0x80008000u;
+    const float2 minus_s = make_float2(-s, -s), inv2 = make_float2(inv, inv), base = make_float2(12582920.f, 12582920.f);
+    constexpr uint32_t kAbove = 0x4b400000u * 0x11111111u;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        r.n[h] = 0;
+        uint32_t lo[4], hi[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            r.n[h] |= number_of(bf16lo(w[4 * h + i]), s, inv) << (8 * i);
-            r.n[h] |= number_of(bf16hi(w[4 * h + i]), s, inv) << (8 * i + 4);
+            const uint32_t v = bf16x2_within(w[4 * h + i], least, most);
+            const float2 x = make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+            float2 y = __fmul2_rn(x, inv2);
+            y = __ffma2_rn(__ffma2_rn(y, minus_s, x), inv2, y);
+            y = __fadd2_rn(y, base);
+            lo[i] = __float_as_uint(y.x);
+            hi[i] = __float_as_uint(y.y);
         }
+        uint32_t n = 0;
+        if (kEvensApart) {
+#pragma unroll
+            for (int i = 3; i >= 0; --i) n = n * 16u + hi[i];
+#pragma unroll
+            for (int i = 3; i >= 0; --i) n = n * 16u + lo[i];
+        } else {
+#pragma unroll
+            for (int i = 3; i >= 0; --i) n = (n * 16u + hi[i]) * 16u + lo[i];
+        }
+        r.n[h] = n - kAbove;
     }
     return r;
 }
 
-// Even elements of eight to the low half of a word, odd ones to the high half (and back).
-__device__ __forceinline__ uint32_t evens_low(uint32_t n) {
-    uint32_t e = n & 0x0f0f0f0fu, o = (n >> 4) & 0x0f0f0f0fu;
-    e = (e | (e >> 4)) & 0x00ff00ffu;
-    o = (o | (o >> 4)) & 0x00ff00ffu;
-    return ((e | (e >> 8)) & 0xffffu) | ((o | (o >> 8)) << 16);
-}
-__device__ __forceinline__ uint32_t evens_apart(uint32_t w) {
+// Back from evens apart: a word's eight numbers in the elements' order.
+__device__ __forceinline__ uint32_t in_order(uint32_t w) {
     uint32_t e = w & 0xffffu, o = w >> 16;
     e = (e | (e << 8)) & 0x00ff00ffu;
     o = (o | (o << 8)) & 0x00ff00ffu;
@@ -131,17 +152,17 @@ __device__ __forceinline__ uint4 values_of(uint32_t n, float s) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Block u of position r of a key tile.
+// Block u of position r of a key tile (evens apart).
 template <int D>
 __device__ __forceinline__ void put_key_block(unsigned char *tile, int r, int u, const Block &b) {
     uint2 w;
-    w.x = turned(evens_low(b.n[0]));
-    w.y = turned(evens_low(b.n[1]));
+    w.x = turned(b.n[0]);
+    w.y = turned(b.n[1]);
     *reinterpret_cast<uint2 *>(tile + r * (D / 2) + u * 8) = w;
     tile[scales_at(D) + k_scale_at<D>(r, u)] = (unsigned char)b.code;
 }
 
-// Block u of a position pair of a value tile: one of the two or both; the other keeps what it is.
+// Block u of a position pair of a value tile (in order): one of the two or both; the other keeps what it is.
 template <int D>
 __device__ __forceinline__ void put_value_blocks(unsigned char *tile, int t, int u, bool has_even, const Block &even, bool has_odd,
                                                  const Block &odd) {
