@@ -124,7 +124,7 @@ __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigne
 
 // Blocks b * per_seq .. + per_seq - 1 walk the tiles (layer, page, head) of sequence b, heads fastest.
 template <int D, bool kStore>
-__global__ void __launch_bounds__(kThreads, kStore ? 4 : 1) q4_convert_kernel(const Q4Convert p, const __grid_constant__ Q4Layers layers) {
+__global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p, const __grid_constant__ Q4Layers layers) {
     pdl_wait();
     pdl_launch_dependents();
     const int b = blockIdx.x / p.per_seq, x = blockIdx.x - b * p.per_seq;
