@@ -77,18 +77,17 @@ reader_status convert(bool store, reader_ctx *ctx, const reader_kv_cache *from, 
 
 // ---- attention
 struct Q4Ws {
-    size_t counters, flags, partial_ml, partial_o, tasks, total;
+    size_t flags, partial_ml, partial_o, tasks, total;
 };
 Q4Ws q4_ws(const reader_ctx *ctx, int D) {
     Q4Ws w{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes); return o; };
     const size_t rows = (size_t)ctx->n_sm * kQ4ShareRows;
-    w.counters = take(sizeof(int32_t) * (size_t)ctx->n_sm);
-    w.flags = take(sizeof(int32_t) * 2 * (size_t)ctx->n_sm);
+    w.flags = take(sizeof(int32_t) * 2 * kQ4Ranges * (size_t)ctx->n_sm);
     w.partial_ml = take(sizeof(float2) * rows);
     w.partial_o = take(sizeof(float) * rows * D);
-    w.tasks = take(sizeof(ShareTask) * (size_t)ctx->n_sm);
+    w.tasks = take(sizeof(ShareTask) * kQ4Ranges * (size_t)ctx->n_sm);
     w.total = at;
     return w;
 }
@@ -266,7 +265,6 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
     p.scale = softmax_scale;
     p.scale_log2 = softmax_scale * 1.4426950408889634f;
     p.give_up = ctx->q4_give_up;
-    p.counters = reinterpret_cast<int32_t *>(ws + w.counters);
     p.flags = reinterpret_cast<int32_t *>(ws + w.flags);
     p.partial_ml = reinterpret_cast<float2 *>(ws + w.partial_ml);
     p.partial_o = reinterpret_cast<float *>(ws + w.partial_o);

@@ -4,14 +4,16 @@
 
 namespace reader {
 
-constexpr int kQ4FewRows = 16;          // query rows of a KV head up to which the few-rows kernels are faster
-// Rows of the shares of a thread block's workers and of its own two, at most (few-rows kernels).
-constexpr int kQ4ShareRows = 512;   // (a block of the many-rows kernel: two shares of 256 rows)
+// Query rows of a KV head up to which the few-rows kernels are faster: 32 sequences on 1024-4096, 16 rows 54 against 73 us, 32 rows 98 against 75.
+constexpr int kQ4FewRows = 16;
+constexpr int kQ4ShareRows = 512;      // rows of a thread block's shares: two of 256, or two of each worker's 8 or 16, at most
+constexpr int kQ4Ranges = 16;          // ranges of a thread block, at most
 constexpr int kQ4MaxBatch = 1 << 16;
 constexpr int kQ4MaxGroup = 1 << 12;   // (128 nodes: 128 G^2 < 2^32, as the division by G wants it)
 
-struct ShareTask {   // a unit that the thread blocks block0 .. block1 have shares of
-    int b, h, rt, rows, block0, block1;   // block0 < 0: none
+// A unit that several ranges of the work list (workers of the few-rows kernel, thread blocks of the many-rows one) have shares of.
+struct ShareTask {
+    int b, h, rt, rows, first, last;   // the ranges first .. last; first < 0: none
 };
 
 struct Q4AttnParams {
@@ -27,11 +29,10 @@ struct Q4AttnParams {
     float scale_log2, scale;
     int give_up;               // worker that reports a wait that ran out (testing aid); -1: none
     // workspace
-    int32_t *counters;         // [thread blocks] arrivals at the unit that a block begins and others go on with
-    int32_t *flags;            // [2 * thread blocks] what is wrong with a block's shares
-    float2 *partial_ml;        // [shares][rows] largest score, sum: of workers, behind them of blocks
-    float *partial_o;          // [shares][rows][D]
-    ShareTask *tasks;          // [thread blocks] the unit that a block begins and others go on with (many-rows kernel)
+    int32_t *flags;            // [2 * ranges] what is wrong with a range's shares: of the unit it goes on with, of the unit it begins
+    float2 *partial_ml;        // [2 * ranges][rows] largest score, sum
+    float *partial_o;          // [2 * ranges][rows of D elements, in the kernel's own order]
+    ShareTask *tasks;          // [ranges] the unit that a range begins and others go on with
     int n_rt;                  // units of a KV head
     unsigned inv_G;            // 2^32 / G, rounded up
     int n_ctas;                // thread blocks (list form)
@@ -45,7 +46,7 @@ struct Q4AttrSet {
 // Few query rows of a KV head (q4_attn_rows.cu), many (q4_attn_sm100.cu).
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
 reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
-// Zeroes the counters and the status words in front of a kernel that adds to them.
-void launch_q4_attn_zero(const Q4AttnParams &p, int n_sm, cudaStream_t st);
+// The status words before a kernel raises some.
+void launch_q4_attn_status(const Q4AttnParams &p, cudaStream_t st);
 
 }  // namespace reader

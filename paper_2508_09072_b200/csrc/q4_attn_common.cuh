@@ -282,6 +282,70 @@ __device__ __forceinline__ void keep_row(const Q4AttnParams &p, size_t row, cons
     if (lane == 0) p.partial_ml[row] = make_float2(x.top, x.total);
 }
 
+// Four elements of a row of a unit, from some of its shares.
+struct Part {
+    float top, total;
+    int flag;
+    float4 x;
+    // With another's added.  A part whose maximum is -inf has weight 0 and is still added, so that a NaN in it stays.
+    __device__ __forceinline__ void weigh(float now, float scale_log2) {
+        const float keep = top == -INFINITY ? 0.f : top == now ? 1.f : ex2((top - now) * scale_log2);
+        top = now;
+        total *= keep;
+        x.x *= keep; x.y *= keep; x.z *= keep; x.w *= keep;
+    }
+    __device__ __forceinline__ void add(const Part &y, float scale_log2) {
+        weigh(fmaxf(top, y.top), scale_log2);
+        const float w = y.top == -INFINITY ? 0.f : y.top == top ? 1.f : ex2((y.top - top) * scale_log2);
+        flag |= y.flag;
+        total = fmaf(y.total, w, total);
+        x.x = fmaf(y.x.x, w, x.x); x.y = fmaf(y.x.y, w, x.y); x.z = fmaf(y.x.z, w, x.z); x.w = fmaf(y.x.w, w, x.w);
+    }
+};
+// Shares n0 .. n1 - 1 of a task, in order, by one thread; o(share) are its four elements of a share.
+template <typename O>
+__device__ __forceinline__ Part merge_shares(const Q4AttnParams &p, const ShareTask &t, int n0, int n1, int share_rows, int r, const O &o) {
+    constexpr int kAtOnce = 4;   // shares that are read before the first is used
+    Part sum = {-INFINITY, 0.f, 0, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 1
+    for (int n = n0; n < n1; n += kAtOnce) {
+        Part y[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            y[i] = Part{-INFINITY, 0.f, 0, make_float4(0.f, 0.f, 0.f, 0.f)};
+            if (n + i < n1) {
+                const int share = 2 * (t.first + n + i) + (n + i == 0 ? 1 : 0);
+                const float2 ml = p.partial_ml[(size_t)share * share_rows + r];
+                y[i] = Part{ml.x, ml.y, p.flags[share], o(share)};
+            }
+        }
+        float now = sum.top;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) now = fmaxf(now, y[i].top);
+        sum.weigh(now, p.scale_log2);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const float w = y[i].top == -INFINITY ? 0.f : y[i].top == now ? 1.f : ex2((y[i].top - now) * p.scale_log2);
+            sum.flag |= y[i].flag;
+            sum.total = fmaf(y[i].total, w, sum.total);
+            sum.x.x = fmaf(y[i].x.x, w, sum.x.x); sum.x.y = fmaf(y[i].x.y, w, sum.x.y);
+            sum.x.z = fmaf(y[i].x.z, w, sum.x.z); sum.x.w = fmaf(y[i].x.w, w, sum.x.w);
+        }
+    }
+    return sum;
+}
+// The call's result: elements 4 c .. + 3 of row r of a task's unit.
+template <int D>
+__device__ __forceinline__ void put_merged(const Q4AttnParams &p, const ShareTask &t, int unit_rows, int r, int c, const Part &y) {
+    const int g = t.rt * unit_rows + r, j = node_of(p, g);
+    const size_t row = ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G);
+    const float inv = y.total == 0.f ? 0.f : 1.f / y.total;   // (a row that sees nothing: zeros)
+    *reinterpret_cast<uint2 *>(p.out + row * D + c * 4) = y.flag ? make_uint2(0u, 0u) : make_uint2(pack(y.x.x * inv, y.x.y * inv), pack(y.x.z * inv, y.x.w * inv));
+    if (c != 0) return;
+    if (p.lse) p.lse[row] = y.flag ? 0.f : fmaf(y.top, p.scale, log2f(y.total) * 0.6931471805599453f);
+    if (r == 0) note(p, t.b, y.flag, 0);
+}
+
 // Whether parent array b is a tree.  Warp-collective.
 __device__ __forceinline__ bool tree_ok(const Q4AttnParams &p, int b, int lane) {
     bool bad = false;

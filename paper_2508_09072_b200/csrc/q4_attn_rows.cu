@@ -15,15 +15,16 @@
 // tiles; shares (m, l, O) are merged in shared memory, those of the cluster's blocks through the workspace after its barrier.
 // (List) The units, each preceded by kUnitCost entries for its start and end, form one flat list of tiles that is cut into equal
 // ranges, one per worker, those of a thread block side by side.  Every thread block makes the list's prefix sums from seq_lens
-// itself.  A worker writes a unit that lies in its range whole, and leaves a share (m, l, O) of any other; when all of a block's
-// workers are done, they merge the shares of each unit in the block, most of them in shared memory; the block that comes
-// last of those that have a unit in common merges theirs, through the workspace.  Always in the order of the shares, whoever
-// comes last.  The counters are zeroed by a launch in front.
+// itself.  A worker writes a unit that lies in its range whole, and leaves a share (m, l, O) of any other in the workspace; a launch behind merges them.
+// (The blocks did it themselves at first, in shared memory, and then the one that came last: 9 us of a call over 32 contexts of 1024-4096 for 4 rows,
+// 24 us for 16.)
 //
 // What is checked where: lengths by every block, page ids by the worker that reads them, a tree by the worker of the unit's
 // tree tiles; what is wrong travels with the share and zeroes the unit's rows.  Bytes behind a sequence's end never reach a
 // product: their scores are replaced by -inf and their values' scale by 0.  Every wait is bounded; a worker that gives up says so
 // in its share, waits (bounded) for its copies and goes on without them.
+#include <algorithm>
+
 #include "q4_attn_common.cuh"
 
 namespace reader {
@@ -74,53 +75,6 @@ __device__ __forceinline__ size_t out_row(const Q4AttnParams &p, int b, int h, i
 }
 template <int NT>
 __device__ __forceinline__ int live_rows(const Q4AttnParams &p, int rt) { return min(Shape<NT>::kRows, p.T * p.G - rt * Shape<NT>::kRows); }
-// A unit whose shares a thread block merges: those of its workers first .. last (first < 0: none); whether the first of them begins it;
-// the blocks block0 .. block1 have it in common.
-struct Task {
-    int b, h, rt, first, last, begins, block0, block1;
-};
-// Row r of a unit.  kOfWorkers: from the shares of the block's workers, into the result or, if other blocks have shares too, as the
-// block's share into the workspace; kOfBlocks: from the blocks' shares into the result.
-enum MergeMode { kOfWorkers, kOfBlocks };
-struct Shares {   // of a block's workers
-    const int16_t *segments, *first_flag, *end_flag;   // units in a worker's range; what is wrong with its first and its last share
-};
-template <int D, int NT>
-__device__ __forceinline__ void merge_one(const Q4AttnParams &p, unsigned char *smem, const Shares &s, const Task &t, int per_block, int r, MergeMode mode) {
-    using C = Cfg<D, NT>;
-    constexpr int kRows = Shape<NT>::kRows;
-    const int lane = threadIdx.x & 31;
-    const float2 *ml_all = reinterpret_cast<const float2 *>(smem + C::kOffShares);
-    const int of_blocks = p.n_ctas * Shape<NT>::kWarps;   // shares of blocks stand behind those of workers: 2 x block, + 1 for a unit that it begins
-    const int count = mode == kOfBlocks ? t.block1 - t.block0 + 1 : t.last - t.first + 1;
-    auto block_slot = [&](int k) { return 2 * (t.block0 + k) + (k == 0 ? 1 : 0); };
-    // worker i's share is that of its last unit if it begins the unit, else that of its first; it stands in its ring if its range ends with it
-    auto in_ring = [&](int i) { return (i == t.first && t.begins) || s.segments[i] <= 1; };
-    auto row_of = [&](int k) {   // row of the workspace's arrays
-        return (size_t)(mode == kOfBlocks ? of_blocks + block_slot(k) : (int)blockIdx.x * per_block + t.first + k) * kRows + r;
-    };
-    auto o = [&](int k) {
-        if (mode != kOfBlocks && in_ring(t.first + k)) return *reinterpret_cast<const float4 *>(smem + (t.first + k) * C::kRingBytes + (r * D + lane * 4) * 4);
-        return __ldcg(reinterpret_cast<const float4 *>(p.partial_o + row_of(k) * D + lane * 4));
-    };
-    auto ml = [&](int k) {
-        return mode != kOfBlocks && in_ring(t.first + k) ? ml_all[(t.first + k) * kRows + r] : __ldcg(p.partial_ml + row_of(k));
-    };
-    int flag = 0;
-    for (int k = lane; k < count; k += 32)
-        flag |= mode == kOfBlocks ? __ldcg(p.flags + block_slot(k)) : k == 0 && t.begins ? s.end_flag[t.first] : s.first_flag[t.first + k];
-    flag = __reduce_or_sync(0xffffffffu, flag);
-    const Row x = merge_row<D>(count, p.scale_log2, ml, o);
-    if (mode == kOfBlocks || t.block0 == t.block1) {
-        if (r == 0) note(p, t.b, flag, lane);
-        put_row<D>(p, out_row<NT>(p, t.b, t.h, t.rt, r), x, flag);
-    } else {
-        const int slot = 2 * blockIdx.x + t.begins;
-        keep_row<D>(p, (size_t)(of_blocks + slot) * kRows + r, x);
-        if (r == 0 && lane == 0) p.flags[slot] = flag;
-    }
-}
-
 // ---- one worker
 template <int D, int NT>
 struct Worker {
@@ -637,21 +591,19 @@ struct Worker {
                 if (g == 0) ml[r] = make_float2(m[nt][e], l[nt][e]);
             }
     }
-    // What becomes of a unit when its tiles in this range are done: it is whole, or there is a share (in the worker's ring if the range
-    // ends with it, else in the workspace) and, from the first of the block's workers that has one, a task.
-    __device__ __forceinline__ void finish(const Unit &u, const List &list, int worker, int warp, bool at_end, float *own, float2 *own_ml, Task *tasks, int flag) {
+    // What becomes of a unit when its tiles in this range are done: it is whole, or there is a share and, from the worker that begins it, a task.
+    __device__ __forceinline__ void finish(const Unit &u, const List &list, int worker, ShareTask *task, int flag) {
         sum_up();
         if (u.t0 == 0 && u.t1 == u.ntiles) {
             write_rows(u, flag);
             return;
         }
-        if (at_end) write_share(u, own, own_ml);
-        else write_share(u, p.partial_o + (size_t)worker * S::kRows * D, p.partial_ml + worker * S::kRows);
-        if (u.t0 != 0 && warp != 0) return;
-        // the unit's shares belong to the workers c0 .. c1
-        const int c0 = u.t0 == 0 ? worker : list.worker_of(u.first_entry(kUnitCost)), c1 = list.worker_of(u.last_entry(kUnitCost));
-        if (lane == 0)
-            tasks[u.t0 == 0 ? warp : S::kWarps] = Task{u.b, u.h, u.rt, warp, min(c1 - (int)blockIdx.x * list.per_block, list.per_block - 1), u.t0 == 0, c0 / list.per_block, c1 / list.per_block};
+        const int share = 2 * worker + (u.t0 == 0 ? 1 : 0);
+        write_share(u, p.partial_o + (size_t)share * S::kRows * D, p.partial_ml + (size_t)share * S::kRows);
+        if (lane == 0) p.flags[share] = flag;
+        if (u.t0 != 0) return;
+        const int last = list.worker_of(u.last_entry(kUnitCost));
+        if (lane == 0) *task = ShareTask{u.b, u.h, u.rt, live_rows<NT>(p, u.rt), worker, last};
     }
     // The block does not end under its own copies.
     __device__ __forceinline__ void drain() {
@@ -688,16 +640,9 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
     list.cut(list.per_block * max(1, min(p.n_ctas, list.W / (kMinEntries * list.per_block))));
     reject_lengths<D>(p, blockIdx.x * S::kWarps + warp, p.n_ctas * S::kWarps, lane);
 
-    __shared__ Task tasks[S::kWarps + 1];   // of the units that the workers begin, and of the one that the block's first continues
-    __shared__ int16_t segments[S::kWarps], first_flag[S::kWarps], end_flag[S::kWarps];   // units in a worker's range; what is wrong with its shares
-    __shared__ int last[2];
-    if (tid <= S::kWarps) tasks[tid].first = -1;
-    if (tid < 2) last[tid] = 0;
-    if (lane == 0) segments[warp] = first_flag[warp] = end_flag[warp] = 0;
+    ShareTask *task = p.tasks + blockIdx.x * S::kWarps + warp;
+    if (lane == 0) task->first = -1;
     __syncthreads();
-    const Shares shares = {segments, first_flag, end_flag};
-    float *own = reinterpret_cast<float *>(smem + warp * C::kRingBytes);
-    float2 *ml_all = reinterpret_cast<float2 *>(smem + C::kOffShares);
     const int worker = blockIdx.x * list.per_block + warp;
     if (warp < list.per_block && worker < list.n_workers && list.W > 0) {
         int w = list.begin(worker);
@@ -727,11 +672,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
                 k.start(coming, coming_end, policy, once, coming_flag);
             }
             if (u.any) {
-                k.finish(u, list, worker, warp, !coming.any, own, ml_all + warp * S::kRows, tasks, flag);
-                if (lane == 0) {
-                    if (segments[warp]++ == 0) first_flag[warp] = (int16_t)flag;
-                    end_flag[warp] = (int16_t)flag;
-                }
+                k.finish(u, list, worker, task, flag);
             }
             if (!coming.any) break;
             u = coming;
@@ -747,32 +688,45 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
         }
         k.drain();
     }
-    __syncthreads();
+}
 
-    // The block's shares, then, of a unit that other blocks have shares of, too (at most one that goes on from the block before, one that goes
-    // on in the next), the blocks': a row of a unit to a warp at a time.  (One loop for both: the code is there the second time.)
-    const int rows = min(S::kRows, p.T * p.G);   // of a unit, at most
+// Units that several workers have shares of: those that the workers of block blockIdx.x of the attention begin, some rows of each, a thread to four
+// elements of a row.  Four groups of threads take a unit each; a long one (at most one of a block's workers begins a unit that goes on behind
+// the block) is all groups' at once.  (By a group alone the 300 shares of each unit of a single token on 32768 took 30 us.)
+constexpr int kGroup = 128, kGroups = 4, kLongTask = 16;
+template <int D, int NT>
+__global__ void __launch_bounds__(kGroup *kGroups) q4_attn_list_merge_kernel(const __grid_constant__ Q4AttnParams p) {
+    using S = Shape<NT>;
+    constexpr int kRows = S::kRows;
+    const int tid = threadIdx.x, group = tid / kGroup, r = blockIdx.y * (4 * kGroup / D) + tid % kGroup / (D / 4), c = tid % (D / 4);
+    __shared__ Part parts[kGroup * kGroups];
+    pdl_wait();
+    pdl_launch_dependents();
+    const ShareTask *tasks = p.tasks + blockIdx.x * S::kWarps;
+    auto merge = [&](const ShareTask &t, int n0, int n1) {
+        return merge_shares(p, t, n0, n1, kRows, r, [&](int share) { return reinterpret_cast<const float4 *>(p.partial_o)[((size_t)share * kRows + r) * (D / 4) + c]; });
+    };
+    const int lane = tid & 31, own_first = lane < S::kWarps ? tasks[lane].first : -1, own_last = lane < S::kWarps ? tasks[lane].last : -1;
+    const bool is_long = own_first >= 0 && own_last - own_first >= kLongTask;
+    const unsigned long_ones = __ballot_sync(0xffffffffu, is_long);
+    unsigned others = __ballot_sync(0xffffffffu, own_first >= 0 && !is_long);
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-        for (int job = warp; job < (S::kWarps + 1) * rows; job += S::kWarps) {
-            const int i = job / rows, r = job - i * rows;
-            const Task t = tasks[i];
-            if (t.first < 0 || r >= live_rows<NT>(p, t.rt) || (pass == 1 && last[t.begins] != i + 1)) continue;
-            merge_one<D, NT>(p, smem, shares, t, list.per_block, r, pass == 0 ? kOfWorkers : kOfBlocks);
-        }
-        if (pass == 1) break;
-        __syncthreads();
-        if (tid <= S::kWarps && tasks[tid].first >= 0 && tasks[tid].block0 != tasks[tid].block1) {
-            __threadfence();
-            if (atomicAdd(p.counters + tasks[tid].block0, 1) == tasks[tid].block1 - tasks[tid].block0) {
-                __threadfence();
-                last[tasks[tid].begins] = tid + 1;
-            }
-        }
-        __syncthreads();
-        if (last[0] == 0 && last[1] == 0) break;
+    for (int n = 0; others; ++n, others &= others - 1) {
+        if (n % kGroups != group) continue;
+        const ShareTask t = tasks[__ffs(others) - 1];
+        if (r < t.rows) put_merged<D>(p, t, kRows, r, c, merge(t, 0, t.last - t.first + 1));
     }
+    if (!long_ones) return;
+    const int long_task = __ffs(long_ones) - 1;
+    const ShareTask t = tasks[long_task];
+    const int count = t.last - t.first + 1, each = (count + kGroups - 1) / kGroups;
+    if (r < t.rows) parts[tid] = merge(t, group * each, min(count, (group + 1) * each));
+    __syncthreads();
+    if (group != 0 || r >= t.rows) return;
+    Part y = parts[tid];
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i) y.add(parts[tid + i * kGroup], p.scale_log2);
+    put_merged<D>(p, t, kRows, r, c, y);
 }
 
 // The other form: a cluster of thread blocks per sequence, p.split of them for each of its units.
@@ -863,11 +817,9 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
     }
 }
 
-// Zeroes what the call counts in.
-__global__ void __launch_bounds__(1024) q4_attn_zero_kernel(int32_t *counters, int n, int32_t *status, int B) {
+__global__ void __launch_bounds__(1024) q4_attn_status_kernel(int32_t *status, int B) {
     pdl_launch_dependents();   // the attention may be set up meanwhile; it waits for this kernel's end
     pdl_wait();
-    for (int i = threadIdx.x; i < n; i += 1024) counters[i] = 0;
     for (int b = threadIdx.x; b < B; b += 1024) status[b] = READER_OK;
 }
 
@@ -917,16 +869,17 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
         }
     }
     p.n_ctas = n_sm;
-    launch_q4_attn_zero(p, n_sm, st);
+    launch_q4_attn_status(p, st);
     launch_pdl(q4_attn_list_kernel<D, NT>, dim3((unsigned)n_sm), dim3(S::kThreads), (size_t)C::kSmem, st, p);
+    static_assert(S::kWarps <= kLongTask && S::kWarps <= kQ4Ranges && 2 * S::kWarps * S::kRows <= kQ4ShareRows, "workspace");
+    launch_pdl(q4_attn_list_merge_kernel<D, NT>, dim3((unsigned)n_sm, (unsigned)((std::min(S::kRows, p.T * p.G) * D + 4 * kGroup - 1) / (4 * kGroup))), dim3(kGroup * kGroups), 0,
+               st, p);
     return READER_OK;
 }
 
 }  // namespace
 
-void launch_q4_attn_zero(const Q4AttnParams &p, int n_sm, cudaStream_t st) {
-    launch_pdl(q4_attn_zero_kernel, dim3(1), dim3(1024), 0, st, p.counters, n_sm, p.status, p.B);
-}
+void launch_q4_attn_status(const Q4AttnParams &p, cudaStream_t st) { launch_pdl(q4_attn_status_kernel, dim3(1), dim3(1024), 0, st, p.status, p.B); }
 
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st) {
     const bool few = p.T * p.G <= 8;

@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             mbar_init(bar(&m->s_full[i]), 1);
             mbar_init(bar(&m->p_full[i]), kSoftmaxThreads / 32);
         }
-        m->task.block0 = -1;
+        m->task.first = -1;
         mbar_init(bar(&m->pv_done), 1);
         mbar_init(bar(&m->o_full), 1);
         for (int i = 0; i < kAhead; ++i) {
@@ -845,66 +845,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
 }
 
 // Units that several blocks have shares of: eight rows of the one that block blockIdx.x of the attention begins, a thread to four elements of a row.
-// Always in the shares' order.  A share whose maximum is -inf has weight 0 and is still added, so that a NaN in it stays.  (A launch of its own: the
-// block that came last did this at first, and took 25 us for the shares of 128 rows and 60 us for those of 256, the others waiting.)
+// (A launch of its own: the block that came last did this at first, and took 25 us for the shares of 128 rows and 60 us for those of 256,
+// the others waiting.)
 template <int D>
 __global__ void __launch_bounds__(2 * D) q4_attn_merge_kernel(const __grid_constant__ Q4AttnParams p) {
     const int r = blockIdx.y * 8 + (threadIdx.x & 7), c = threadIdx.x >> 3;
     pdl_wait();
     pdl_launch_dependents();
     const ShareTask t = p.tasks[blockIdx.x];
-    if (t.block0 < 0 || r >= t.rows) return;
-    const float2 *ml = p.partial_ml + r;
-    const float4 *o = reinterpret_cast<const float4 *>(p.partial_o) + c * 256 + r;
-    constexpr int kStep = 2 * 256;                     // rows from one block's share to the next one's
-    const size_t first = (size_t)(2 * t.block0 + 1) * 256, others = (size_t)(2 * t.block0) * 256;   // (a block's second share begins a unit)
-    const int count = t.block1 - t.block0 + 1;
-    auto at = [&](int n) { return n ? others + (size_t)n * kStep : first; };
-    float top = -INFINITY, total = 0.f;
-    int flag = 0;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kAtOnce = 4;   // shares that are read before the first is used
-#pragma unroll 1
-    for (int n0 = 0; n0 < count; n0 += kAtOnce) {
-        float2 s[kAtOnce];
-        float4 y[kAtOnce];
-        int f[kAtOnce];
-        float now = top;
-#pragma unroll
-        for (int n = 0; n < kAtOnce; ++n) {
-            const size_t k = at(n0 + n);
-            s[n] = make_float2(-INFINITY, 0.f);
-            y[n] = make_float4(0.f, 0.f, 0.f, 0.f);
-            f[n] = 0;
-            if (n0 + n < count) {
-                s[n] = ml[k];
-                y[n] = o[k * (D / 4)];
-                f[n] = p.flags[k / 256];
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < kAtOnce; ++n) {
-            now = fmaxf(now, s[n].x);
-            flag |= f[n];
-        }
-        const float keep = top == now ? 1.f : ex2((top - now) * p.scale_log2);
-        top = now;
-        total *= keep;
-        x.x *= keep; x.y *= keep; x.z *= keep; x.w *= keep;
-#pragma unroll
-        for (int n = 0; n < kAtOnce; ++n) {
-            const float w = s[n].x == -INFINITY ? 0.f : s[n].x == top ? 1.f : ex2((s[n].x - top) * p.scale_log2);
-            total = fmaf(s[n].y, w, total);
-            x.x = fmaf(y[n].x, w, x.x); x.y = fmaf(y[n].y, w, x.y); x.z = fmaf(y[n].z, w, x.z); x.w = fmaf(y[n].w, w, x.w);
-        }
-    }
-    const int g = t.rt * 256 + r, j = node_of(p, g);
-    const size_t row = ((size_t)t.b * p.T + j) * p.Hq + t.h * p.G + (g - j * p.G);
-    const float inv = total == 0.f ? 0.f : 1.f / total;   // (a row that sees nothing: zeros)
-    *reinterpret_cast<uint2 *>(p.out + row * D + c * 4) = flag ? make_uint2(0u, 0u) : make_uint2(pack(x.x * inv, x.y * inv), pack(x.z * inv, x.w * inv));
-    if (c != 0) return;
-    if (p.lse) p.lse[row] = flag ? 0.f : fmaf(top, p.scale, log2f(total) * 0.6931471805599453f);
-    if (r == 0) note(p, t.b, flag, 0);
+    if (t.first < 0 || r >= t.rows) return;
+    const Part y = merge_shares(p, t, 0, t.last - t.first + 1, 256, r, [&](int share) { return reinterpret_cast<const float4 *>(p.partial_o)[(size_t)share * 256 * (D / 4) + c * 256 + r]; });
+    put_merged<D>(p, t, 256, r, c, y);
 }
 
 }  // namespace
@@ -921,7 +872,7 @@ reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &params, 
         set = true;
     }
     p.n_ctas = n_sm;
-    launch_q4_attn_zero(p, n_sm, st);
+    launch_q4_attn_status(p, st);
     launch_pdl(p.D == 128 ? q4_attn_sm100_kernel<128> : q4_attn_sm100_kernel<64>, dim3((unsigned)n_sm), dim3(kThreads),
                (size_t)(p.D == 128 ? Cfg<128>::kSmem : Cfg<64>::kSmem), st, p);
     launch_pdl(p.D == 128 ? q4_attn_merge_kernel<128> : q4_attn_merge_kernel<64>, dim3((unsigned)n_sm, (unsigned)((std::min(256, p.T * p.G) + 7) / 8)), dim3(2 * p.D), 0,
