@@ -4,7 +4,7 @@
 
 namespace reader {
 
-// Query rows of a KV head up to which the few-rows kernels are faster: 32 sequences on 1024-4096, 16 rows 54 against 73 us, 32 rows 98 against 75.
+// Query rows of a KV head up to which the few-rows kernels are faster: 32 sequences on 1024-4096, 16 rows 51 against 73 us, 32 rows 81 against 74.
 constexpr int kQ4FewRows = 16;
 constexpr int kQ4ShareRows = 512;      // rows of a thread block's shares: two of 256, or two of each worker's 8 or 16, at most
 constexpr int kQ4Ranges = 16;          // ranges of a thread block, at most
@@ -43,7 +43,10 @@ struct Q4AttnParams {
 struct Q4AttrSet {
     bool rows[4], sm100[2];
 };
-// Few query rows of a KV head (q4_attn_rows.cu), many (q4_attn_sm100.cu).
+// Few query rows of a KV head (q4_attn_rows.cu), many (q4_attn_sm100.cu).  The former, too, for some small calls
+// with more rows, in their form of one launch: 32 rows and 8 heads on 512 positions 9 against 15 us, 4 x 80 rows and 2 heads 12 against 18, 256 rows on 1400
+// 21 against 26; but 8 x 128 rows on 1000, half a GPU full, 27 against 21, and they stay with the latter.
+bool q4_attn_rows_faster(const Q4AttnParams &p, int n_sm);
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
 reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
 // The status words before a kernel raises some.

@@ -823,7 +823,18 @@ __global__ void __launch_bounds__(1024) q4_attn_status_kernel(int32_t *status, i
     for (int b = threadIdx.x; b < B; b += 1024) status[b] = READER_OK;
 }
 
-constexpr int kAloneTiles = 6;
+// Thread blocks of a unit in the alone form, 0 if the call is not one for it: the units of a sequence have to fit a cluster, the clusters the GPU, and,
+// going by the page table's width, a worker gets at most `most` tiles.
+constexpr int kAloneTiles = 6, kAloneTilesManyRows = 2;
+template <int NT>
+int alone_split(const Q4AttnParams &p, int n_sm, int most) {
+    using S = Shape<NT>;
+    const int64_t units = (int64_t)p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows), tiles = p.max_pages + (p.T + kPage - 1) / kPage;
+    if (units > kMaxCluster) return 0;
+    int split = 1;
+    while (2 * split * units <= kMaxCluster && 2 * split * units * p.B <= n_sm && tiles > split * S::kWarps) split *= 2;
+    return units * split * p.B <= n_sm && tiles <= (int64_t)most * split * S::kWarps ? split : 0;
+}
 
 template <int D, int NT>
 reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) {
@@ -838,35 +849,28 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
         }
         *attr_set = true;
     }
-    // Alone: the units of a sequence fit a cluster, the clusters the GPU, and, going by the page table's width, a worker gets at most
-    // kAloneTiles tiles.
     p.n_rt = (p.T * p.G + S::kRows - 1) / S::kRows;
-    const int units = p.Hkv * p.n_rt;
-    const int tiles = p.max_pages + (p.T + kPage - 1) / kPage;
-    if (units <= kMaxCluster) {
-        int split = 1;
-        while (2 * split * units <= kMaxCluster && 2 * split * units * (int64_t)p.B <= n_sm && tiles > split * S::kWarps) split *= 2;
-        if ((int64_t)units * split * p.B <= n_sm && tiles <= (int64_t)kAloneTiles * split * S::kWarps) {
-            p.split = split;
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3((unsigned)(p.B * units * split));
-            cfg.blockDim = dim3(S::kThreads);
-            cfg.dynamicSmemBytes = C::kSmem;
-            cfg.stream = st;
-            cudaLaunchAttribute attr[2];
-            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-            attr[0].val.programmaticStreamSerializationAllowed = 1;
-            attr[1].id = cudaLaunchAttributeClusterDimension;
-            attr[1].val.clusterDim.x = (unsigned)(units * split);
-            attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-            cfg.attrs = attr;
-            cfg.numAttrs = 2;
-            if (cudaLaunchKernelEx(&cfg, q4_attn_alone_kernel<D, NT>, p) != cudaSuccess) {
-                cudaGetLastError();
-                return READER_ERR_CUDA;
-            }
-            return READER_OK;
+    p.split = alone_split<NT>(p, n_sm, kAloneTiles);
+    if (p.split) {
+        const int blocks = p.Hkv * p.n_rt * p.split;   // of a sequence
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(p.B * blocks));
+        cfg.blockDim = dim3(S::kThreads);
+        cfg.dynamicSmemBytes = C::kSmem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)blocks;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        if (cudaLaunchKernelEx(&cfg, q4_attn_alone_kernel<D, NT>, p) != cudaSuccess) {
+            cudaGetLastError();
+            return READER_ERR_CUDA;
         }
+        return READER_OK;
     }
     p.n_ctas = n_sm;
     launch_q4_attn_status(p, st);
@@ -880,6 +884,13 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
 }  // namespace
 
 void launch_q4_attn_status(const Q4AttnParams &p, cudaStream_t st) { launch_pdl(q4_attn_status_kernel, dim3(1), dim3(1024), 0, st, p.status, p.B); }
+
+bool q4_attn_rows_faster(const Q4AttnParams &p, int n_sm) {
+    if (p.T * p.G <= kQ4FewRows) return true;
+    // With many rows the form of one launch saves two, and its workers need longer for a tile: for calls that leave two thirds of the GPU idle either way.
+    const int64_t units = (int64_t)p.B * p.Hkv * ((p.T * p.G + 15) / 16);
+    return 3 * units <= n_sm && alone_split<2>(p, n_sm, kAloneTilesManyRows) != 0;
+}
 
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st) {
     const bool few = p.T * p.G <= 8;

@@ -705,3 +705,108 @@ def test_infinite_values_of_nodes_reach_the_rows_that_see_them_alone(rd, d, T, g
             else:
                 assert (torch.isnan(out[hit]) if np.isnan(value) else out[hit] == value).all()
             assert ((out.double() - want[0]).abs() <= want[2])[~hit].all()
+
+
+# ---------------------------------------------------------------------------------------------- forms of the calls
+@pytest.mark.parametrize("store", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_bf16_pools_on_any_16_byte_border(rd, store, d):
+    """Blocks of 32 bytes are moved whole only where they lie on such a border."""
+    b = binding()
+    rng = np.random.default_rng(41)
+    lens = [0, 77, 130]
+    both = Both(rng, [max(x, 1) for x in lens], 2, d)
+    first, last = i32([0, 5, 0]), i32(lens)
+
+    def shifted(t):
+        room = torch.empty(t.numel() + 8, dtype=t.dtype, device="cuda")
+        out = room[8:].view(t.shape)
+        assert out.data_ptr() % 32 == 16
+        return out.copy_(t)
+
+    if store:
+        rd.q4_store([both.wide], [both.narrow], first, last)
+        want = both.k4.clone(), both.v4.clone()
+        moved = b.KvCache(shifted(both.k), shifted(both.v), both.wide.page_table, both.wide.seq_lens)
+        for pool in (both.k4, both.v4):
+            pool.random_(0, 256)
+        assert rd.q4_store([moved], [both.narrow], first, last).tolist() == [0] * 3
+        rd.q4_load([both.narrow], [both.out], first, last)
+        again = both.out.k_pool.clone(), both.out.v_pool.clone()
+        both.k4.copy_(want[0])
+        both.v4.copy_(want[1])
+        rd.q4_load([both.narrow], [both.out], first, last)
+        assert torch.equal(again[0], both.out.k_pool) and torch.equal(again[1], both.out.v_pool)
+    else:
+        rd.q4_store([both.wide], [both.narrow], first, last)
+        rd.q4_load([both.narrow], [both.out], first, last)
+        moved = b.KvCache(shifted(torch.full_like(both.k, 3.0)), shifted(torch.full_like(both.v, 3.0)), both.wide.page_table, both.wide.seq_lens)
+        assert rd.q4_load([both.narrow], [moved], first, last).tolist() == [0] * 3
+        assert torch.equal(moved.k_pool, both.out.k_pool) and torch.equal(moved.v_pool, both.out.v_pool)
+
+
+def widened(cache, columns):
+    """The same cache with more columns in its page table (a call's form goes by their number)."""
+    b = binding()
+    t = torch.full((cache.page_table.shape[0], columns), -1, dtype=torch.int32, device="cuda")
+    t[:, :cache.page_table.shape[1]] = cache.page_table
+    return b.Q4Cache(cache.k_pool, cache.v_pool, t, cache.seq_lens)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,group,T", [
+    (1, 1, 1), (2, 4, 2), (1, 1, 17), (1, 2, 64), (1, 1, 128), (2, 3, 43), (1, 8, 17), (1, 2, 100), (1, 2, 128), (1, 3, 100), (1, 4, 97), (1, 3, 128), (1, 5, 128), (3, 5, 26)])
+@pytest.mark.parametrize("lens", [[517, 0, 1], [64, 127, 128, 129], [3000]])
+def test_attention_with_wide_page_tables(rd, d, heads, group, T, lens):
+    """Lists of work whatever the call's size: units of up to 128 rows, of more, both (257 to 384 rows of a head), ends inside a tile."""
+    rng = np.random.default_rng(d + heads + 10 * group + T + sum(lens))
+    both, cache, q, kt, vt, parent = make(rng, lens, T, heads, group, d)
+    want = plain_attn(both, lens, q, kt, vt, parent, 0.09)
+    got = attend(rd, widened(cache, 700), q, kt, vt, parent, 0.09)
+    assert got[2] == [0] * len(lens)
+    within(got[:2], want)
+
+
+@pytest.mark.parametrize("d,heads,group,T,L", [(128, 1, 2, 128, 20000), (128, 1, 4, 32, 30000), (64, 1, 4, 4, 40000), (128, 1, 1, 1, 50000), (64, 2, 3, 100, 9000)])
+def test_units_that_many_ranges_share(rd, d, heads, group, T, L):
+    rng = np.random.default_rng(L)
+    both, cache, q, kt, vt, parent = make(rng, [L], T, heads, group, d)
+    got = attend(rd, cache, q, kt, vt, parent, 0.09)
+    assert got[2] == [0]
+    within(got[:2], plain_attn(both, [L], q, kt, vt, parent, 0.09))
+
+
+@pytest.mark.parametrize("T,group", [(1, 4), (4, 4), (40, 3), (100, 4)])
+def test_many_calls_in_a_row_do_not_give_up(rd, T, group):
+    """Calls overlap at their ends (the next one is set up while one is under way); all of them answer the same."""
+    rng = np.random.default_rng(43)
+    lens = rng.integers(0, 1500, 24).tolist()
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, group, 128)
+    want = attend(rd, cache, q, kt, vt, parent, 0.1)
+    assert want[2] == [0] * 24
+    q, kt, vt, parent = q.cuda(), kt.cuda(), vt.cuda(), i32(parent)
+    outs = [torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    status = torch.full((300, 24), 9, dtype=torch.int32, device="cuda")
+    for i in range(300):
+        rd.q4_verify_attn(q, kt, vt, cache, parent, 0.1, out=outs[i % 4], status=status[i])
+    assert not status.any()
+    assert all(torch.equal(x.cpu(), want[0]) for x in outs)
+
+
+@pytest.mark.parametrize("T", [1, 40, 100])
+def test_statuses_with_wide_page_tables(rd, T):
+    """Lengths that cannot be, pages that are not there and parents that are no tree, each in a sequence of its own among good ones."""
+    b = binding()
+    rng = np.random.default_rng(45)
+    lens = [300, 200, 500, 64, 0]
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, 3, 64)
+    wide = widened(cache, 900)
+    want = plain_attn(both, lens, q, kt, vt, parent, 0.1)
+    wide.seq_lens = i32([300, -1, 500, 900 * PAGE + 1, 0])
+    wide.page_table[2, 3] = both.k4.shape[0]
+    parent = parent.copy()
+    parent[4][0] = 0
+    out, lse, st = attend(rd, wide, q, kt, vt, parent, 0.1)
+    assert st == [0, b.ERR_CAPACITY, b.ERR_BAD_PAGE, b.ERR_CAPACITY, b.ERR_BAD_TREE]
+    within((out[:1], lse[:1]), [x[:1] for x in want])   # (where the list is cut goes by all lengths: not the bits of another batch)
+    assert not out[1:].any() and not lse[1:].any()
