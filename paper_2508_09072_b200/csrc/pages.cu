@@ -65,19 +65,37 @@ __device__ __forceinline__ int block_rank(int x, int &total) {
     return __shfl_sync(0xffffffffu, wi - w, warp) + incl - x;
 }
 
-// Marks each row that the requests name with the first request that names it: two steps, each followed by the cluster's barrier.
-__device__ __forceinline__ void mark_rows(int32_t *mark, const int32_t *rows, int n, int n_rows) {
-    for (int i = gthread(); i < n; i += kBlocks * kThreads) {
-        const int r = rows[i];
-        if (r >= 0 && r < n_rows) mark[r] = INT_MAX;
+// Which request is the first that names a row.  Up to kNamed requests: by looking through those before it, in shared memory.  More: each row is marked with
+// its first request, two steps in global memory, each followed by the cluster's barrier (2 us more of a call's 5).
+constexpr int kNamed = 512;
+struct Named {
+    int32_t *mark;
+    const int *names;   // null: the marks
+    __device__ __forceinline__ Named(int32_t *mark_, int *room, const int32_t *rows, int n, int n_rows) : mark(mark_), names(n <= kNamed ? room : nullptr) {
+        if (names) {
+            for (int i = threadIdx.x; i < n; i += kThreads) room[i] = rows[i];
+            __syncthreads();
+            return;
+        }
+        for (int i = gthread(); i < n; i += kBlocks * kThreads) {
+            const int r = rows[i];
+            if (r >= 0 && r < n_rows) mark[r] = INT_MAX;
+        }
+        cluster_sync();
+        for (int i = gthread(); i < n; i += kBlocks * kThreads) {
+            const int r = rows[i];
+            if (r >= 0 && r < n_rows) atomicMin(mark + r, i);
+        }
+        cluster_sync();
     }
-    cluster_sync();
-    for (int i = gthread(); i < n; i += kBlocks * kThreads) {
-        const int r = rows[i];
-        if (r >= 0 && r < n_rows) atomicMin(mark + r, i);
+    // Of request i, which names a row that there is.  Warp-collective.
+    __device__ __forceinline__ bool first(int i, int row) const {
+        if (!names) return __ldcg(mark + row) == i;
+        bool before = false;
+        for (int j = threadIdx.x & 31; j < i; j += 32) before |= names[j] == row;
+        return !__any_sync(0xffffffffu, before);
     }
-    cluster_sync();
-}
+};
 
 // ---- fork
 __global__ void __cluster_dims__(kBlocks, 1, 1) __launch_bounds__(kThreads)
@@ -85,12 +103,13 @@ pages_fork_kernel(const PagesView p, const int32_t *__restrict__ src, const int3
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
-    mark_rows(ws.mark, dst, n, p.rows);
+    __shared__ int room[kNamed];
+    const Named named(ws.mark, room, dst, n, p.rows);
     // all sources are read (and their pages counted once more) ...
     for (int i = gwarp(); i < n; i += kWarps) {
         const int from = src[i], to = dst[i];
         int st = READER_OK, length = -1;
-        if (from < 0 || from >= p.rows || to < 0 || to >= p.rows || __ldcg(ws.mark + to) != i) {
+        if (from < 0 || from >= p.rows || to < 0 || to >= p.rows || !named.first(i, to)) {
             st = READER_ERR_INVALID_ARG;
         } else {
             length = p.lens[from];
@@ -156,12 +175,13 @@ pages_reserve_kernel(const PagesView p, const int32_t *__restrict__ rows, const 
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, block = blockIdx.x;
-    mark_rows(ws.mark, rows, n, p.rows);
+    __shared__ int room[kNamed];
+    const Named named(ws.mark, room, rows, n, p.rows);
     // 1. what each request needs
     for (int i = gwarp(); i < n; i += kWarps) {
         const int row = rows[i], t = tokens[i];
         int st = READER_OK, demand = 0;
-        if (row < 0 || row >= p.rows || t < 0 || __ldcg(ws.mark + row) != i) {
+        if (row < 0 || row >= p.rows || t < 0 || !named.first(i, row)) {
             st = READER_ERR_INVALID_ARG;
         } else if (p.lens[row] < 0 || (int64_t)p.lens[row] + t > (int64_t)p.width * kPage) {
             st = READER_ERR_CAPACITY;
