@@ -12,6 +12,7 @@ namespace reader {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kCommitThreads = 512;
 
 // A block of 16 elements in bf16: 32 bytes, by one instruction where the pools lie on such a border (two of 16 bytes each ask for every 32-byte sector
 // twice), streamed past the caches' other users.
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p,
 
 // Block (b, l) commits sequence b into layer l: the accepted nodes' rows to the positions seq_lens[b] + k.
 template <int D>
-__global__ void __launch_bounds__(kThreads) q4_commit_kernel(const Q4Commit p, const __grid_constant__ Q4Layers layers) {
+__global__ void __launch_bounds__(kCommitThreads) q4_commit_kernel(const Q4Commit p, const __grid_constant__ Q4Layers layers) {
     pdl_wait();
     pdl_launch_dependents();
     constexpr int kBlocks = D / q4::kBlock;
@@ -168,14 +169,14 @@ __global__ void __launch_bounds__(kThreads) q4_commit_kernel(const Q4Commit p, c
     int32_t *slots = p.slots && l == 0 ? p.slots + (size_t)b * p.max_path : nullptr;
     bool bad = n > 0 && (n > p.max_path || L < 0 || L < p.shared_prefix_len || (int64_t)L + n > (int64_t)p.max_pages * kPage);
     if (!bad)
-        for (int k = tid; k < n; k += kThreads) {
+        for (int k = tid; k < n; k += kCommitThreads) {
             const int page = table[(L + k) / kPage], node = path[k];
             bad |= page < 0 || page >= p.num_pages || node < 0 || node >= p.T;
         }
     bad = __syncthreads_or(bad);
     if (tid == 0 && p.status && l == 0) p.status[b] = bad ? READER_ERR_CAPACITY : READER_OK;
     if (slots)
-        for (int k = tid; k < p.max_path; k += kThreads)
+        for (int k = tid; k < p.max_path; k += kCommitThreads)
             slots[k] = !bad && k < n ? table[(L + k) / kPage] * kPage + (L + k) % kPage : -1;
     if (bad || n <= 0) return;
     auto row = [&](const void *tree, int k, int h, int u) {
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) q4_commit_kernel(const Q4Commit p, c
     };
     const int per_pos = p.Hkv * kBlocks, key_tasks = n * per_pos;
     const int pair0 = L / 2, value_tasks = ((L + n - 1) / 2 - pair0 + 1) * per_pos;
-    for (int i = tid; i < key_tasks + value_tasks; i += kThreads) {
+    for (int i = tid; i < key_tasks + value_tasks; i += kCommitThreads) {
         if (i < key_tasks) {
             const int k = i / per_pos, h = (i - k * per_pos) / kBlocks, u = i % kBlocks;
             const uint4 *src = row(layers.k_from[l], k, h, u);
@@ -245,7 +246,7 @@ void launch_q4_commit(Q4Commit p, const Q4Layers *chunks, int n_layers, bool upd
         const int layers = n_layers - l0 < kQ4LayersPerLaunch ? n_layers - l0 : kQ4LayersPerLaunch;
         p.status = l0 == 0 ? status : nullptr;
         p.slots = l0 == 0 ? slots : nullptr;
-        launch_pdl(p.D == 128 ? q4_commit_kernel<128> : q4_commit_kernel<64>, dim3((unsigned)p.B, (unsigned)layers), dim3(kThreads), 0, st, p,
+        launch_pdl(p.D == 128 ? q4_commit_kernel<128> : q4_commit_kernel<64>, dim3((unsigned)p.B, (unsigned)layers), dim3(kCommitThreads), 0, st, p,
                    chunks[l0 / kQ4LayersPerLaunch]);
     }
     if (update_seq_lens && n_layers > 1)
