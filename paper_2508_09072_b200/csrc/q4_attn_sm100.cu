@@ -47,7 +47,9 @@ static_assert(2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsRest <= 5 * 96 && kRegsS
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
 constexpr int kUnitCost = 4;       // entries that stand for a unit's start and end (6: 32 x 32 nodes 82 instead of 80 us)
 constexpr int kMinEntries = kUnitCost + 2;   // of a range: so every one of them holds a tile
-constexpr int kRawSlots = 3;       // of the ring: keys or values of a tile's pages each
+// Slots of the ring, keys or values of a tile's pages each: three, and three more in a call without wide units, in the half of the queries' place that it does
+// not need (with three the narrow units' tiles came too late: 32 x 32 nodes 80 us).
+constexpr int kRawSlots = 3;
 constexpr int kAhead = 8;          // units in the ring
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
 
@@ -70,7 +72,8 @@ struct Cfg {
     static constexpr int kOffTable = kOffSwap + 2 * 256 * 4;
     static constexpr int kOffBars = kOffTable + kPrefix * 8;
     static constexpr int kSmem = kOffBars + 1024;
-    static_assert(kSmem <= 227 * 1024, "shared memory");
+    static_assert(kSmem <= 227 * 1024 && kRawSlots * kRawBytes <= kQBytes, "shared memory");
+    static __device__ __forceinline__ uint32_t raw_at(int s) { return s * kRawBytes + (s < kRawSlots ? kOffRaw : kOffQ + kQBytes - kRawSlots * kRawBytes); }
 };
 
 // A unit as the roles see it: its tiles t0 .. t0 + tiles - 1 are this block's.
@@ -85,12 +88,21 @@ struct Piece {
     __device__ __forceinline__ int steps() const { return wide ? 2 * tiles : tiles; }
     __device__ __forceinline__ int tile_of(int step) const { return wide ? step >> 1 : step; }
 };
+// The n-th use of the ring: its slot, and the parity of the slot's use.
+struct Place {
+    int s, parity;
+    __device__ __forceinline__ Place(int n, bool six) {
+        const int q = (unsigned)n / kRawSlots, r = n - q * kRawSlots;
+        s = six ? r + (q & 1) * kRawSlots : r;
+        parity = (six ? q >> 1 : q) & 1;
+    }
+};
 struct Bars {
-    uint64_t raw_full[kRawSlots], raw_empty[kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], pv_done, o_full, piece_full[kAhead], piece_empty[kAhead];
+    uint64_t raw_full[2 * kRawSlots], raw_empty[2 * kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
+    uint64_t q_full, q_empty, s_full[2], p_full[2], pv_done, o_full, piece_full[kAhead], piece_empty[kAhead];
     uint32_t tmem_base;
     int32_t abort;
-    int32_t raw_bad[kRawSlots];   // a page outside the pool among the slot's
+    int32_t raw_bad[2 * kRawSlots];   // a page outside the pool among the slot's
     int32_t flags[kAhead];        // what is wrong with unit i mod kAhead
     int32_t poison[kAhead];       // its tree has infinities or NaN among the values
     int32_t warp_sum[kThreads / 32];
@@ -284,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     volatile int32_t *abort_s = &m->abort;
     auto bar = [&](const uint64_t *b) { return smem_u32(b); };
     if (tid == 0) {
-        for (int i = 0; i < kRawSlots; ++i) {
+        for (int i = 0; i < 2 * kRawSlots; ++i) {
             mbar_init(bar(&m->raw_full[i]), 1);
             mbar_init(bar(&m->raw_empty[i]), kUnpackWarps);
         }
@@ -293,12 +305,12 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             mbar_init(bar(&m->k_empty[i]), 1);
             mbar_init(bar(&m->v_full[i]), kUnpackWarps);
             mbar_init(bar(&m->v_empty[i]), 1);
-            mbar_init(bar(&m->q_full[i]), 1);
-            mbar_init(bar(&m->q_empty[i]), 1);
             mbar_init(bar(&m->s_full[i]), 1);
             mbar_init(bar(&m->p_full[i]), kSoftmaxThreads / 32);
         }
         m->task.first = -1;
+        mbar_init(bar(&m->q_full), 1);
+        mbar_init(bar(&m->q_empty), 1);
         mbar_init(bar(&m->pv_done), 1);
         mbar_init(bar(&m->o_full), 1);
         for (int i = 0; i < kAhead; ++i) {
@@ -334,6 +346,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     __syncthreads();
     list.per_block = 1;
     list.cut(max(1, min(p.n_ctas, list.W / kMinEntries)));
+    const bool six = list.n_wide == 0;   // slots of the ring
 
     if (warp >= kLoadWarp) {
         regs_dec<kRegsRest>();
@@ -410,11 +423,11 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     const bool streamed = once && page0 >= p.shared_prefix_pages;
 #pragma unroll 1
                     for (int kv = 0; kv < 2; ++kv, ++n) {
-                        const int s = n % kRawSlots;
-                        if (!wait(bar(&m->raw_empty[s]), ((n / kRawSlots) & 1) ^ 1, abort_s)) break;
+                        const Place slot(n, six);
+                        if (!wait(bar(&m->raw_empty[slot.s]), slot.parity ^ 1, abort_s)) break;
                         if (lane == 0) {
-                            m->raw_bad[s] = !(ok0 && ok1);
-                            const uint32_t full = bar(&m->raw_full[s]), dst = base + C::kOffRaw + s * C::kRawBytes;
+                            m->raw_bad[slot.s] = !(ok0 && ok1);
+                            const uint32_t full = bar(&m->raw_full[slot.s]), dst = base + C::raw_at(slot.s);
                             const unsigned char *pool = kv ? p.v_pool : p.k_pool;
                             const int bytes = (ok0 ? C::kPageBytes : 0) + (count == 2 && ok1 ? C::kPageBytes : 0);
                             mbar_arrive_expect_tx(full, bytes);   // (a page outside the pool is not read; what the slot holds is never shown)
@@ -427,25 +440,24 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             }
             if (gone(abort_s)) {   // the block does not end under its own copies
                 const uint64_t t0 = globaltimer_ns();
-                for (int i = max(0, n - kRawSlots); i < n; ++i)
-                    while (!mbar_try_wait(bar(&m->raw_full[i % kRawSlots]), (i / kRawSlots) & 1) && globaltimer_ns() - t0 < 20000000ull) {
+                for (int i = max(0, n - (six ? 2 : 1) * kRawSlots); i < n; ++i) {
+                    const Place at(i, six);
+                    while (!mbar_try_wait(bar(&m->raw_full[at.s]), at.parity) && globaltimer_ns() - t0 < 20000000ull) {
                     }
+                }
             }
         } else if (warp == kQueryWarp) {
             // ------------------------------------------------------------------ queries
-            // A wide unit's rows fill both halves of the place, and it has them when the unit before is done with its own; narrow ones have the
-            // halves in turn, so that one's queries come while the one before is worked on.
+            // A wide unit's rows fill both halves of the place, a narrow one's the first.  A unit has it when the one before is done with its last scores: while
+            // that one's last probabilities and results are under way.
             constexpr int kChunks = D / 8, kRowsAtOnce = 32 / kChunks;
             const int ch = lane % kChunks, r0 = lane / kChunks;
-            bool wide_before = false;
             Piece x;
             for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
-                const int after = x.wide || wide_before ? 1 : 2;   // the unit that was there before: that many before this
-                if (seg >= after) wait(bar(&m->q_empty[(seg - after) & 1]), ((seg - after) >> 1) & 1, abort_s);
-                wide_before = x.wide;
+                if (seg > 0) wait(bar(&m->q_empty), (seg - 1) & 1, abort_s);
                 // row r of the head: of node g / G, (j Hq + h G + g - j G) D elements behind the sequence's first
                 const __nv_bfloat16 *src = p.q + ((size_t)x.b * p.T * p.Hq + x.h * p.G) * D + ch * 8;
-                uint32_t dst = base + C::kOffQ + (x.wide ? 0 : (seg & 1) * C::kQBytes) + (ch >> 3) * C::kBlock + r0 * 128;
+                uint32_t dst = base + C::kOffQ + (ch >> 3) * C::kBlock + r0 * 128;
                 for (int r = r0; r < (x.wide ? 256 : 128); r += 8, dst += 8 * 128) {
                     if (r == 128 + r0) dst += C::kQBytes - C::kBlock;
 #pragma unroll
@@ -459,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&m->q_full[seg & 1]));
+                if (lane == 0) mbar_arrive(bar(&m->q_full));
             }
         } else {
             // ------------------------------------------------------------------ products
@@ -470,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             uint32_t p_parity = 0;       // bit `slot`
             Piece x;
             for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
-                wait(bar(&m->q_full[seg & 1]), (seg >> 1) & 1, abort_s);
+                wait(bar(&m->q_full), seg & 1, abort_s);
                 const int steps = x.steps();
                 auto score = [&](int i) {
                     const int slot = i & 1;
@@ -481,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     tc_fence_after();
                     if (elect_one()) {
                         const int buf = (nk - 1) & 1;
-                        const uint64_t kd = descK + (uint64_t)((buf * C::kKBytes) >> 4), qd = descQ + (uint64_t)(((x.wide ? slot : seg & 1) * C::kQBytes) >> 4);
+                        const uint64_t kd = descK + (uint64_t)((buf * C::kKBytes) >> 4), qd = descQ + (uint64_t)(((x.wide ? slot : 0) * C::kQBytes) >> 4);
                         const uint32_t tS = tmem + kTmemS + slot * 128;
 #pragma unroll
                         for (int hf = 0; hf < C::kHalves; ++hf)
@@ -490,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                                 mma_bf16_ss(tS, qd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kd + (uint64_t)((hf * C::kBlock + kk * 32) >> 4), kIdescQK, (hf | kk) != 0);
                         mma_commit(bar(&m->s_full[slot]));
                         if (!x.wide || slot == 1) mma_commit(bar(&m->k_empty[buf]));
-                        if (i == steps - 1) mma_commit(bar(&m->q_empty[seg & 1]));
+                        if (i == steps - 1) mma_commit(bar(&m->q_empty));
                     }
                     __syncwarp();
                 };
@@ -543,7 +555,6 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 const uint32_t free = (((n + i) >> 1) & 1) ^ 1;
                 const bool tree = has_tree && i == x.tiles - 1;
                 const int valid = x.valid(p.T, i);
-                int s = (raw + 2 * i) % kRawSlots, full = ((raw + 2 * i) / kRawSlots) & 1;
                 // keys
                 if (!wait(bar(&m->k_empty[group]), free, abort_s)) break;
                 if (tree) {
@@ -555,15 +566,14 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     }
                     copy_tree_keys<D>(p, x.b, x.h, kt, t);
                 } else {
-                    if (!wait(bar(&m->raw_full[s]), full, abort_s)) break;
-                    const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
-                    if (m->raw_bad[s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
+                    const Place at(raw + 2 * i, six);
+                    if (!wait(bar(&m->raw_full[at.s]), at.parity, abort_s)) break;
+                    const uint32_t src = base + C::raw_at(at.s);
+                    if (m->raw_bad[at.s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
-                    full ^= s == kRawSlots - 1;
-                    s = s == kRawSlots - 1 ? 0 : s + 1;
+                    if (lane == 0) mbar_arrive(bar(&m->raw_empty[at.s]));
                 }
                 fence_proxy_async();
                 __syncwarp();
@@ -573,13 +583,14 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                 if (tree) {
                     if (copy_tree_values<D>(p, x.b, x.h, vt, t)) atomicOr(&m->poison[seg & (kAhead - 1)], 1);
                 } else {
-                    if (!wait(bar(&m->raw_full[s]), full, abort_s)) break;
-                    const uint32_t src = base + C::kOffRaw + s * C::kRawBytes;
+                    const Place at(raw + 2 * i + 1, six);
+                    if (!wait(bar(&m->raw_full[at.s]), at.parity, abort_s)) break;
+                    const uint32_t src = base + C::raw_at(at.s);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page)
                         unpack_values<D>(src + page * C::kPageBytes, vt + page * C::kVPage, min(valid - page * kPage, kPage), t, sixteen);
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(&m->raw_empty[s]));
+                    if (lane == 0) mbar_arrive(bar(&m->raw_empty[at.s]));
                 }
                 fence_proxy_async();
                 __syncwarp();
