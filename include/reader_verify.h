@@ -21,7 +21,10 @@
  *   measured against the paged one), reader_accept_noalloc;
  *   and what comes before it: reader_prompt_append (head norms, position rotation and cache write of a prompt),
  *   reader_prompt_attn (its causal attention over the paged cache) and reader_tree_rotate (the same norms and rotation
- *   for draft nodes).
+ *   for draft nodes);
+ *   and the cache itself: held in 4 bits, reader_q4_store / reader_q4_load / reader_q4_commit and reader_q4_verify_attn (the attention
+ *   over it, draft trees and single tokens); its pages, reader_pages_fork / reader_pages_reserve / reader_pages_free / reader_pages_compact /
+ *   reader_pages_copy.
  *
  * Conventions common to every call
  *   - Every pointer named below is a DEVICE pointer owned by the caller unless it says "host".

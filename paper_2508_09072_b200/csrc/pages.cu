@@ -9,7 +9,8 @@
 // is the k-th free one).  One thread-block cluster does it: eight blocks of 1024 threads and its hardware barrier (0.3 us)
 // between the steps, in one launch; a prefix sum over several kernels would cost a launch per step.  Data move in a second
 // launch (2 x page_bytes per page and pool, 16 KB of a page to a thread block with all its loads in flight at once), which is
-// bound by the copy bandwidth.
+// bound by the copy bandwidth.  Measured: four rows released, forked from one of 700 positions and given pages 17.9 us (1.7, 4.5 and the rest), 128 rows of
+// 32 with 16 pools of 36 KB 33 us, 23 of them the pages' bytes; a pool of 4096 pages compacted (8 pools of 36 KB) 108 us, 98 of them bytes.
 #include <climits>
 
 #include "pages.cuh"
