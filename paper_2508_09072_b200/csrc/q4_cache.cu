@@ -82,6 +82,28 @@ __device__ __forceinline__ void store_tile(const __nv_bfloat16 *k, const __nv_bf
         q4::put_value_blocks<D>(v4, t, u, has[0], q4::quantise<false>(y[0][0], y[0][1]), has[1], q4::quantise<false>(y[1][0], y[1][1]));
 }
 
+// A position pair's words and codes of block u, and the pair's values from them.
+template <int D>
+__device__ __forceinline__ void read_pair(const unsigned char *v4, int t, int u, uint4 &words, int &codes) {
+    constexpr int kChunkWords = D / 32;
+    words = *reinterpret_cast<const uint4 *>(v4 + t * D + q4::v_chunk<D>(t, u * (4 / kChunkWords)) * kChunkWords * 4);
+    codes = *reinterpret_cast<const uint16_t *>(v4 + q4::scales_at(D) + q4::v_scale_at<D>(2 * t, u));
+}
+template <int D>
+__device__ __forceinline__ void write_pair(const uint4 &words, int codes, __nv_bfloat16 *v, int t, int u, const bool (&has)[2], bool whole) {
+    constexpr int kBlocks = D / q4::kBlock;
+    const uint32_t w[4] = {q4::plain_of(words.x), q4::plain_of(words.y), q4::plain_of(words.z), q4::plain_of(words.w)};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if (!has[e]) continue;
+        const float s = q4::scale_of((codes >> (8 * e)) & 255);
+        const int sh = 16 * e;
+        store_block(reinterpret_cast<uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2, whole,
+                    q4::values_of(((w[0] >> sh) & 0xffffu) | (((w[1] >> sh) & 0xffffu) << 16), s),
+                    q4::values_of(((w[2] >> sh) & 0xffffu) | (((w[3] >> sh) & 0xffffu) << 16), s));
+    }
+}
+
 // The other way.
 template <int D>
 __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigned char *v4, __nv_bfloat16 *k, __nv_bfloat16 *v, int lo, int hi, bool whole) {
@@ -100,11 +122,7 @@ __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigne
     const bool has[2] = {tid < kPairs && 2 * t >= lo && 2 * t < hi, tid < kPairs && 2 * t + 1 >= lo && 2 * t + 1 < hi};
     uint4 vw = make_uint4(0, 0, 0, 0);
     int vc = 0;
-    if (has[0] || has[1]) {
-        constexpr int kChunkWords = D / 32;
-        vw = *reinterpret_cast<const uint4 *>(v4 + t * D + q4::v_chunk<D>(t, u * (4 / kChunkWords)) * kChunkWords * 4);
-        vc = *reinterpret_cast<const uint16_t *>(v4 + q4::scales_at(D) + q4::v_scale_at<D>(2 * t, u));
-    }
+    if (has[0] || has[1]) read_pair<D>(v4, t, u, vw, vc);
 #pragma unroll
     for (int i = 0; i < kKeyTasks; ++i) {
         const int task = i * kThreads + tid, r = task / kBlocks;
@@ -113,29 +131,76 @@ __device__ __forceinline__ void load_tile(const unsigned char *k4, const unsigne
         store_block(reinterpret_cast<uint4 *>(k) + task * 2, whole, q4::values_of(q4::in_order(q4::plain_of(kw[i].x)), s),
                     q4::values_of(q4::in_order(q4::plain_of(kw[i].y)), s));
     }
-    const uint32_t w[4] = {q4::plain_of(vw.x), q4::plain_of(vw.y), q4::plain_of(vw.z), q4::plain_of(vw.w)};
+    write_pair<D>(vw, vc, v, t, u, has, whole);
+}
+
+// A few rows of a tile, by a warp: a block of keys, or of a position pair of values, to a lane at a time.
+constexpr int kFewPositions = 16;
+template <int D, bool kStore>
+__device__ __forceinline__ void few_rows(const void *k_from, const void *v_from, void *k_to, void *v_to, int lo, int hi, bool whole) {
+    constexpr int kBlocks = D / q4::kBlock;
+    const int t0 = lo / 2, keys = (hi - lo) * kBlocks, pairs = ((hi - 1) / 2 - t0 + 1) * kBlocks;
+    for (int i = threadIdx.x & 31; i < keys + pairs; i += 32) {
+        if (i < keys) {
+            const int r = lo + i / kBlocks, u = i % kBlocks, task = r * kBlocks + u;
+            if (kStore) {
+                uint4 x[2];
+                load_block(static_cast<const uint4 *>(k_from) + task * 2, whole, x);
+                q4::put_key_block<D>(static_cast<unsigned char *>(k_to), r, u, q4::quantise<true>(x[0], x[1]));
+            } else {
+                const unsigned char *k4 = static_cast<const unsigned char *>(k_from);
+                const uint2 w = *reinterpret_cast<const uint2 *>(k4 + task * 8);
+                const float s = q4::scale_of(k4[q4::scales_at(D) + q4::k_scale_at<D>(r, u)]);
+                store_block(static_cast<uint4 *>(k_to) + task * 2, whole, q4::values_of(q4::in_order(q4::plain_of(w.x)), s),
+                            q4::values_of(q4::in_order(q4::plain_of(w.y)), s));
+            }
+        } else {
+            const int t = t0 + (i - keys) / kBlocks, u = (i - keys) % kBlocks;
+            const bool has[2] = {2 * t >= lo, 2 * t + 1 < hi};
+            if (kStore) {
+                uint4 y[2][2] = {};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (!has[e]) continue;
-        const float s = q4::scale_of((vc >> (8 * e)) & 255);
-        const int sh = 16 * e;
-        store_block(reinterpret_cast<uint4 *>(v) + ((2 * t + e) * kBlocks + u) * 2, whole,
-                    q4::values_of(((w[0] >> sh) & 0xffffu) | (((w[1] >> sh) & 0xffffu) << 16), s),
-                    q4::values_of(((w[2] >> sh) & 0xffffu) | (((w[3] >> sh) & 0xffffu) << 16), s));
+                for (int e = 0; e < 2; ++e)
+                    if (has[e]) load_block(static_cast<const uint4 *>(v_from) + ((2 * t + e) * kBlocks + u) * 2, whole, y[e]);
+                q4::put_value_blocks<D>(static_cast<unsigned char *>(v_to), t, u, has[0], q4::quantise<false>(y[0][0], y[0][1]), has[1],
+                                        q4::quantise<false>(y[1][0], y[1][1]));
+            } else {
+                uint4 words;
+                int codes;
+                read_pair<D>(static_cast<const unsigned char *>(v_from), t, u, words, codes);
+                write_pair<D>(words, codes, static_cast<__nv_bfloat16 *>(v_to), t, u, has, whole);
+            }
+        }
     }
 }
 
-// Blocks b * per_seq .. + per_seq - 1 walk the tiles (layer, page, head) of sequence b, heads fastest.
+// Blocks b * per_seq .. + per_seq - 1 walk the tiles (layer, page, head) of sequence b, heads fastest; a warp to a tile where a sequence
+// may have more tiles than blocks and the range has few positions (8 of 16 sequences in 16 layers loaded in 7.2 us, by whole blocks in 10.2; one sequence's in one layer 3.1
+// and 2.5).
 template <int D, bool kStore>
 __global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p, const __grid_constant__ Q4Layers layers) {
     pdl_wait();
     pdl_launch_dependents();
     const int b = blockIdx.x / p.per_seq, x = blockIdx.x - b * p.per_seq;
     const int first = p.first[b], last = p.last[b];
+    const bool few = p.crowded && last > first && (unsigned)last - (unsigned)first <= kFewPositions;
+    constexpr int kWarps = kThreads / 32;
+    if (few && x > 0 && x * kWarps >= ((last - 1) / kPage - first / kPage + 1) * p.Hkv * p.layers) return;   // (the first block looks at everything)
     const int st = convert_status(p, b, first, last);
     if (x == 0 && threadIdx.x == 0 && p.status) p.status[b] = st;
     if (st != READER_OK || last <= first) return;
     const int page0 = first / kPage, n_pages = (last - 1) / kPage - page0 + 1;
+    constexpr size_t kWide = (size_t)kPage * D * sizeof(__nv_bfloat16), kNarrow = q4::tile_bytes(D), kFrom = kStore ? kWide : kNarrow, kTo = kStore ? kNarrow : kWide;
+    if (few) {
+        for (int i = x * kWarps + (threadIdx.x >> 5); i < n_pages * p.Hkv * p.layers; i += p.per_seq * kWarps) {
+            const int h = i % p.Hkv, j = i / p.Hkv, l = j / n_pages, page = page0 + j - l * n_pages;
+            const size_t from = (size_t)p.from_table[(size_t)b * p.from_width + page] * p.Hkv + h, to = (size_t)p.to_table[(size_t)b * p.to_width + page] * p.Hkv + h;
+            few_rows<D, kStore>(static_cast<const unsigned char *>(layers.k_from[l]) + from * kFrom, static_cast<const unsigned char *>(layers.v_from[l]) + from * kFrom,
+                                static_cast<unsigned char *>(layers.k_to[l]) + to * kTo, static_cast<unsigned char *>(layers.v_to[l]) + to * kTo,
+                                max(0, first - page * kPage), min(kPage, last - page * kPage), p.whole);
+        }
+        return;
+    }
     // item (l, page, h) number x + k per_seq, by carrying (a division each time costs as much as an eighth of the tile)
     const int q = x / p.Hkv, dq = p.per_seq / p.Hkv, dh = p.per_seq - dq * p.Hkv, dl = dq / n_pages, dj = dq - dl * n_pages;
     int h = x - q * p.Hkv, l = q / n_pages, j = q - l * n_pages;
@@ -144,13 +209,10 @@ __global__ void __launch_bounds__(kThreads) q4_convert_kernel(const Q4Convert p,
         const int lo = max(0, first - page * kPage), hi = min(kPage, last - page * kPage);
         const size_t from = (size_t)p.from_table[(size_t)b * p.from_width + page] * p.Hkv + h;
         const size_t to = (size_t)p.to_table[(size_t)b * p.to_width + page] * p.Hkv + h;
-        constexpr size_t kWide = (size_t)kPage * D, kNarrow = q4::tile_bytes(D);
-        if (kStore)
-            store_tile<D>(static_cast<const __nv_bfloat16 *>(layers.k_from[l]) + from * kWide, static_cast<const __nv_bfloat16 *>(layers.v_from[l]) + from * kWide,
-                          static_cast<unsigned char *>(layers.k_to[l]) + to * kNarrow, static_cast<unsigned char *>(layers.v_to[l]) + to * kNarrow, lo, hi, p.whole);
-        else
-            load_tile<D>(static_cast<const unsigned char *>(layers.k_from[l]) + from * kNarrow, static_cast<const unsigned char *>(layers.v_from[l]) + from * kNarrow,
-                         static_cast<__nv_bfloat16 *>(layers.k_to[l]) + to * kWide, static_cast<__nv_bfloat16 *>(layers.v_to[l]) + to * kWide, lo, hi, p.whole);
+        const unsigned char *k = static_cast<const unsigned char *>(layers.k_from[l]) + from * kFrom, *v = static_cast<const unsigned char *>(layers.v_from[l]) + from * kFrom;
+        unsigned char *k_to = static_cast<unsigned char *>(layers.k_to[l]) + to * kTo, *v_to = static_cast<unsigned char *>(layers.v_to[l]) + to * kTo;
+        if (kStore) store_tile<D>(reinterpret_cast<const __nv_bfloat16 *>(k), reinterpret_cast<const __nv_bfloat16 *>(v), k_to, v_to, lo, hi, p.whole);
+        else load_tile<D>(k, v, reinterpret_cast<__nv_bfloat16 *>(k_to), reinterpret_cast<__nv_bfloat16 *>(v_to), lo, hi, p.whole);
         h += dh;
         j += dj;
         l += dl;
@@ -228,6 +290,7 @@ void launch_q4_convert(bool store, Q4Convert p, const Q4Layers *chunks, int n_la
         const int64_t tiles = (int64_t)(p.from_width < p.to_width ? p.from_width : p.to_width) * p.Hkv * p.layers;
         const int64_t share = (16 * (int64_t)n_sm + p.B - 1) / p.B;
         p.per_seq = (int)(tiles < share ? tiles : share);
+        p.crowded = tiles > share;
         p.status = l0 == 0 ? const_cast<int32_t *>(status) : nullptr;
         const Q4Layers &c = chunks[l0 / kQ4LayersPerLaunch];
         uintptr_t places = 0;

@@ -19,6 +19,7 @@ struct Q4Convert {
     int Hkv, D, B, layers;
     int per_seq;                           // thread blocks of a sequence
     bool whole;                            // the bf16 pools lie on 32-byte borders
+    bool crowded;                          // a sequence may have more tiles than thread blocks
     int32_t *status;                       // null: not reported (layers behind the first launch)
 };
 void launch_q4_convert(bool store, Q4Convert p, const Q4Layers *chunks, int n_layers, int n_sm, cudaStream_t st);

@@ -810,3 +810,32 @@ def test_statuses_with_wide_page_tables(rd, T):
     assert st == [0, b.ERR_CAPACITY, b.ERR_BAD_PAGE, b.ERR_CAPACITY, b.ERR_BAD_TREE]
     within((out[:1], lse[:1]), [x[:1] for x in want])   # (where the list is cut goes by all lengths: not the bits of another batch)
     assert not out[1:].any() and not lse[1:].any()
+
+
+@pytest.mark.parametrize("heads,d", [(1, 64), (8, 64), (3, 128), (8, 128)])
+@pytest.mark.parametrize("columns", [4, 900])
+def test_ranges_of_few_positions(rd, heads, d, columns):
+    """One to seventeen positions (up to sixteen take another form behind a wide page table), at both ends of pages and over them; several layers at once."""
+    b = binding()
+    rng = np.random.default_rng(47)
+    ranges = [(a, a + n) for n in (1, 2, 3, 8, 15, 16, 17) for a in (0, 1, 47, 48, 49, 62, 63, 64, 120)]
+    both = [Both(rng, [x for _, x in ranges], heads, d) for _ in range(3)]
+    for x in both[1:]:   # (the layers of a call have their tables in common)
+        x.t16, x.t4 = both[0].t16, both[0].t4
+    tables = [torch.full((len(ranges), columns), -1, dtype=torch.int32, device="cuda") for _ in range(2)]
+    for t, now in zip(tables, (both[0].wide.page_table, both[0].narrow.page_table)):
+        t[:, :now.shape[1]] = now
+    for x in both:
+        x.wide.page_table, x.narrow.page_table, x.out.page_table = tables[0], tables[1], tables[0]
+    first, last = i32([a for a, _ in ranges]), i32([x for _, x in ranges])
+    assert not rd.q4_store([x.wide for x in both], [x.narrow for x in both], first, last).any()
+    assert not rd.q4_load([x.narrow for x in both], [x.out for x in both], first, last).any()
+    for x in both:
+        for src, out in ((x.k, x.out.k_pool), (x.v, x.out.v_pool)):
+            want = torch.full(src.shape, 3.0, dtype=torch.float64)
+            for s, (lo, hi) in enumerate(ranges):
+                pos = np.arange(lo, hi)
+                page = torch.from_numpy(x.t16[s][pos // PAGE].astype(np.int64))
+                want[page, :, torch.from_numpy(pos % PAGE)] = held(rows_of(src, x.t16, s, lo, hi))
+            assert torch.equal(out.cpu().double(), want)
+    assert b.ERR_CAPACITY in rd.q4_store([both[0].wide], [both[0].narrow], first - 1, last).tolist()
