@@ -6,11 +6,11 @@
 // change by integer atomics whose intermediate values nobody looks at.
 //
 // The bookkeeping of fork, reserve and compact needs answers over the whole batch or the whole pool between its steps (which page
-// is the k-th free one).  One thread-block cluster does it: eight blocks of 1024 threads and its hardware barrier (0.3 us)
-// between the steps, in one launch; a prefix sum over several kernels would cost a launch per step.  Data move in a second
-// launch (2 x page_bytes per page and pool, 16 KB of a page to a thread block with all its loads in flight at once), which is
-// bound by the copy bandwidth.  Measured: four rows released, forked from one of 700 positions and given pages 17.9 us (1.7, 4.5 and the rest), 128 rows of
-// 32 with 16 pools of 36 KB 33 us, 23 of them the pages' bytes; a pool of 4096 pages compacted (8 pools of 36 KB) 108 us, 98 of them bytes.
+// is the k-th free one).  One launch does it, between whose steps all threads wait for one another: a thread block where requests and pool are few, else a cluster
+// of eight (four rows released, forked and given pages: 14.1 us by one block, 17.8 by a cluster; 128 rows of 32: 41 and 33); a prefix sum over several kernels
+// would cost a launch per step.  Data move in a second launch (2 x page_bytes per page and pool, 16 KB of a page to a thread block with all its loads
+// in flight at once), which is bound by the copy bandwidth.  Measured: four rows released (1.8 us), forked from one of 700 positions (4.0) and given pages
+// 14.1 us; 128 rows of 32 with 16 pools of 36 KB 33 us, 23 of them the pages' bytes; a pool of 4096 pages compacted (8 pools of 36 KB) 107 us, 91 of them bytes.
 #include <climits>
 
 #include "pages.cuh"
@@ -19,16 +19,22 @@
 namespace reader {
 namespace {
 
-constexpr int kBlocks = 8;        // of the cluster
+constexpr int kCluster = 8;       // thread blocks of the cluster
+constexpr int kMoves = 2 * kCluster;   // of PagesWs::counts: pages that a compaction moves
 constexpr int kThreads = 1024;
-constexpr int kWarps = kBlocks * kThreads / 32;
 constexpr int kCopyThreads = 256;
 constexpr int kCopyUnroll = 4;
 constexpr int kCopyPart = kCopyThreads * kCopyUnroll * 16;   // bytes of a page that one thread block moves
 
-__device__ __forceinline__ void cluster_sync() {
-    ptx::cluster_arrive_release();
-    ptx::cluster_wait_acquire();
+// All threads of the call's kBlocks blocks: a cluster, or one block.
+template <int kBlocks>
+__device__ __forceinline__ void all_sync() {
+    if (kBlocks == 1) {
+        __syncthreads();
+    } else {
+        ptx::cluster_arrive_release();
+        ptx::cluster_wait_acquire();
+    }
 }
 __device__ __forceinline__ int gthread() { return blockIdx.x * kThreads + threadIdx.x; }
 __device__ __forceinline__ int gwarp() { return gthread() >> 5; }
@@ -69,6 +75,7 @@ __device__ __forceinline__ int block_rank(int x, int &total) {
 // Which request is the first that names a row.  Up to kNamed requests: by looking through those before it, in shared memory.  More: each row is marked with
 // its first request, two steps in global memory, each followed by the cluster's barrier (2 us more of a call's 5).
 constexpr int kNamed = 512;
+template <int kBlocks>
 struct Named {
     int32_t *mark;
     const int *names;   // null: the marks
@@ -82,12 +89,12 @@ struct Named {
             const int r = rows[i];
             if (r >= 0 && r < n_rows) mark[r] = INT_MAX;
         }
-        cluster_sync();
+        all_sync<kBlocks>();
         for (int i = gthread(); i < n; i += kBlocks * kThreads) {
             const int r = rows[i];
             if (r >= 0 && r < n_rows) atomicMin(mark + r, i);
         }
-        cluster_sync();
+        all_sync<kBlocks>();
     }
     // Of request i, which names a row that there is.  Warp-collective.
     __device__ __forceinline__ bool first(int i, int row) const {
@@ -99,15 +106,16 @@ struct Named {
 };
 
 // ---- fork
+template <int kBlocks>
 __global__ void __cluster_dims__(kBlocks, 1, 1) __launch_bounds__(kThreads)
 pages_fork_kernel(const PagesView p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int n, const PagesWs ws, int32_t *__restrict__ status) {
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
     __shared__ int room[kNamed];
-    const Named named(ws.mark, room, dst, n, p.rows);
+    const Named<kBlocks> named(ws.mark, room, dst, n, p.rows);
     // all sources are read (and their pages counted once more) ...
-    for (int i = gwarp(); i < n; i += kWarps) {
+    for (int i = gwarp(); i < n; i += kBlocks * kThreads / 32) {
         const int from = src[i], to = dst[i];
         int st = READER_OK, length = -1;
         if (from < 0 || from >= p.rows || to < 0 || to >= p.rows || !named.first(i, to)) {
@@ -140,9 +148,9 @@ pages_fork_kernel(const PagesView p, const int32_t *__restrict__ src, const int3
             ws.length[i] = st == READER_OK ? length : -1;
         }
     }
-    cluster_sync();
+    all_sync<kBlocks>();
     // ... before any destination is released and written
-    for (int i = gwarp(); i < n; i += kWarps) {
+    for (int i = gwarp(); i < n; i += kBlocks * kThreads / 32) {
         const int length = __ldcg(ws.length + i);
         if (length < 0) continue;
         int32_t *row = p.table + (size_t)dst[i] * p.width;
@@ -171,15 +179,16 @@ __device__ __forceinline__ Wanted wanted(const PagesView &p, int row, int tokens
     return w;
 }
 
+template <int kBlocks>
 __global__ void __cluster_dims__(kBlocks, 1, 1) __launch_bounds__(kThreads)
 pages_reserve_kernel(const PagesView p, const int32_t *__restrict__ rows, const int32_t *__restrict__ tokens, int n, const PagesWs ws, int32_t *__restrict__ status) {
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, block = blockIdx.x;
     __shared__ int room[kNamed];
-    const Named named(ws.mark, room, rows, n, p.rows);
+    const Named<kBlocks> named(ws.mark, room, rows, n, p.rows);
     // 1. what each request needs
-    for (int i = gwarp(); i < n; i += kWarps) {
+    for (int i = gwarp(); i < n; i += kBlocks * kThreads / 32) {
         const int row = rows[i], t = tokens[i];
         int st = READER_OK, demand = 0;
         if (row < 0 || row >= p.rows || t < 0 || !named.first(i, row)) {
@@ -215,7 +224,7 @@ pages_reserve_kernel(const PagesView p, const int32_t *__restrict__ rows, const 
     for (int i = page0 + threadIdx.x; i < page1; i += kThreads) mine += p.refs[i] == 0;
     mine = block_sum(mine);
     if (threadIdx.x == 0) ws.counts[block] = mine;
-    cluster_sync();
+    all_sync<kBlocks>();
     int free_before = 0, free_all = 0;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
@@ -261,7 +270,7 @@ pages_reserve_kernel(const PagesView p, const int32_t *__restrict__ rows, const 
     if (threadIdx.x == 0) ws.counts[kBlocks + block] = 0;
     __syncthreads();
     if (lane == 0) atomicMax(ws.counts + kBlocks + block, granted);
-    cluster_sync();
+    all_sync<kBlocks>();
     int handed = 0;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) handed = max(handed, __ldcg(ws.counts + kBlocks + c));
@@ -285,7 +294,7 @@ pages_reserve_kernel(const PagesView p, const int32_t *__restrict__ rows, const 
         }
         rank0 += total;
     }
-    cluster_sync();
+    all_sync<kBlocks>();
     // 5. the pages that were replaced lose a holder (only now: a page must not look free while others still look for free ones)
     for (int k = gthread(); k < handed; k += kBlocks * kThreads) {
         const int old = __ldcg(ws.slots + k).x;
@@ -363,6 +372,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
 }
 
 // ---- compact
+template <int kBlocks>
 __global__ void __cluster_dims__(kBlocks, 1, 1) __launch_bounds__(kThreads)
 pages_plan_kernel(const PagesView p, int32_t *__restrict__ n_used, const PagesWs ws) {
     pdl_wait();
@@ -375,7 +385,7 @@ pages_plan_kernel(const PagesView p, int32_t *__restrict__ n_used, const PagesWs
     for (int i = page0 + threadIdx.x; i < page1; i += kThreads) held += p.refs[i] != 0;
     held = block_sum(held);
     if (threadIdx.x == 0) ws.counts[block] = held;
-    cluster_sync();
+    all_sync<kBlocks>();
     int used = 0, held_before = 0;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
@@ -390,7 +400,7 @@ pages_plan_kernel(const PagesView p, int32_t *__restrict__ n_used, const PagesWs
     for (int i = page0 + threadIdx.x; i < min(page1, used); i += kThreads) low += p.refs[i] != 0;
     low = block_sum(low);
     if (threadIdx.x == 0) ws.counts[kBlocks + block] = low;
-    cluster_sync();
+    all_sync<kBlocks>();
     int low_before = 0, low_all = 0;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
@@ -411,10 +421,10 @@ pages_plan_kernel(const PagesView p, int32_t *__restrict__ n_used, const PagesWs
         holes += total & 0xffff;
         movers += total >> 16;
     }
-    cluster_sync();
+    all_sync<kBlocks>();
     // 3. the k-th of the ones to the k-th of the others
     const int count = used - low_all;
-    if (block == 0 && threadIdx.x == 0) ws.counts[2 * kBlocks] = count;
+    if (block == 0 && threadIdx.x == 0) ws.counts[kMoves] = count;
     for (int k = gthread(); k < count; k += kBlocks * kThreads) {
         const int to = __ldcg(ws.holes + k), from = __ldcg(&ws.moves[k].x);
         ws.moves[k].y = to;
@@ -429,7 +439,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_compact_kernel(const Pages
                                                                      int rename) {
     pdl_wait();
     pdl_launch_dependents();
-    const int count = ws.counts[2 * kBlocks], used = *n_used;
+    const int count = ws.counts[kMoves], used = *n_used;
     const int64_t items = (int64_t)count * n_pools * parts;
     for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
         const int part = (int)(i % parts);
@@ -452,13 +462,18 @@ unsigned moves_of(int n) { return (unsigned)(n < 65535 ? n : 65535); }
 
 }  // namespace
 
+// Up to here a call is one thread block's.
+constexpr int kOneBlockRequests = 32, kOneBlockPages = 4096;
+
 void launch_pages_fork(const PagesView &p, const int32_t *src, const int32_t *dst, int n, const PagesWs &ws, int32_t *status, cudaStream_t st) {
-    launch_pdl(pages_fork_kernel, dim3(kBlocks), dim3(kThreads), 0, st, p, src, dst, n, ws, status);
+    const bool one = n <= kOneBlockRequests;
+    launch_pdl(one ? pages_fork_kernel<1> : pages_fork_kernel<kCluster>, dim3(one ? 1 : kCluster), dim3(kThreads), 0, st, p, src, dst, n, ws, status);
 }
 
 void launch_pages_reserve(const PagesView &p, const int32_t *rows, const int32_t *tokens, int n, const PagesWs &ws, const PoolList *pools, int n_pools,
                           size_t page_bytes, int32_t *status, cudaStream_t st) {
-    launch_pdl(pages_reserve_kernel, dim3(kBlocks), dim3(kThreads), 0, st, p, rows, tokens, n, ws, status);
+    const bool one = n <= kOneBlockRequests && p.num_pages <= kOneBlockPages;
+    launch_pdl(one ? pages_reserve_kernel<1> : pages_reserve_kernel<kCluster>, dim3(one ? 1 : kCluster), dim3(kThreads), 0, st, p, rows, tokens, n, ws, status);
     const int parts = parts_of(page_bytes);
     for (int at = 0; at < n_pools; at += kPoolsPerLaunch)
         launch_pdl(pages_move_kernel, dim3((unsigned)(pools_of(n_pools, at) * parts), moves_of(n)), dim3(kCopyThreads), 0, st, pools[at / kPoolsPerLaunch],
@@ -471,7 +486,8 @@ void launch_pages_free(const PagesView &p, const int32_t *rows, const int32_t *k
 
 void launch_pages_compact(const PagesView &p, int32_t *n_used, const PagesWs &ws, const PoolList *pools, int n_pools, size_t page_bytes, int n_sm,
                           cudaStream_t st) {
-    launch_pdl(pages_plan_kernel, dim3(kBlocks), dim3(kThreads), 0, st, p, n_used, ws);
+    const bool one = p.num_pages <= kOneBlockPages;
+    launch_pdl(one ? pages_plan_kernel<1> : pages_plan_kernel<kCluster>, dim3(one ? 1 : kCluster), dim3(kThreads), 0, st, p, n_used, ws);
     for (int at = 0; at < n_pools; at += kPoolsPerLaunch)
         launch_pdl(pages_compact_kernel, dim3((unsigned)(8 * n_sm)), dim3(kCopyThreads), 0, st, p, static_cast<const int32_t *>(n_used), ws,
                    pools[at / kPoolsPerLaunch], pools_of(n_pools, at), parts_of(page_bytes), page_bytes, at == 0 ? 1 : 0);

@@ -348,3 +348,36 @@ def test_more_rows_than_threads(rd):
     assert rd.pages_free(p, i32(r[::2]), None).tolist() == m.free(r[::2])
     assert rd.pages_compact(p).tolist() == [m.compact()]
     m.same(p)
+
+
+@pytest.mark.parametrize("num_pages", [300, 6000])
+@pytest.mark.parametrize("n", [2, 31, 32, 33, 512, 513, 1500])
+def test_rows_named_more_than_once(rd, n, num_pages):
+    """The first request that names a row is the one that counts, however many there are."""
+    rng = np.random.default_rng(n)
+    rows, width = 700, 6
+    m = Model(rng, num_pages, rows, width, 1, 16)
+    p = m.device()
+    r = rng.integers(-2, rows + 2, n).tolist()
+    r[n - 1] = r[0] = 5
+    t = rng.integers(0, 2 * PAGE, n).tolist()
+    assert rd.pages_reserve(p, i32(r), i32(t)).tolist() == m.reserve(r, t)
+    m.same(p)
+    for row in range(rows):
+        m.lens[row] = next((e for e in range(width) if m.table[row][e] < 0), width) * PAGE
+    p.seq_lens.copy_(i32(m.lens))
+    src = rng.integers(0, rows, n).tolist()
+    assert rd.pages_fork(p, i32(src), i32(r)).tolist() == m.fork(src, r)
+    m.same(p)
+
+
+@pytest.mark.parametrize("held", [0, 1, 4999, 5000])
+def test_compaction_of_large_pools(rd, held):
+    rng = np.random.default_rng(36)
+    m = Model(rng, 5000, 100, 50, 1, 32)
+    for i, page in enumerate(rng.permutation(5000)[:held].tolist()):
+        m.table[i // 50][i % 50] = page
+        m.refs[page] = 1
+    p = m.device()
+    assert rd.pages_compact(p).tolist() == [m.compact()] == [held]
+    m.same(p)
