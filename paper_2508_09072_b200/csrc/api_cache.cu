@@ -270,7 +270,8 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
     p.partial_o = reinterpret_cast<float *>(ws + w.partial_o);
     p.tasks = reinterpret_cast<ShareTask *>(ws + w.tasks);
     p.inv_G = (unsigned)((((uint64_t)1 << 32) + p.G - 1) / p.G);
-    const bool few = q4_attn_rows_faster(p, ctx->n_sm);
+    bool few;
+    if (reader_status s = q4_attn_rows_faster(&ctx->q4_attr, p, ctx->n_sm, &few)) return s;
     if (reader_status s = (few ? launch_q4_attn_rows : launch_q4_attn_sm100)(&ctx->q4_attr, p, ctx->n_sm, (cudaStream_t)stream)) return s;
     return launch_status();
 }

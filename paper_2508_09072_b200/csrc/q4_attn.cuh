@@ -39,14 +39,20 @@ struct Q4AttnParams {
     int split;                 // thread blocks of a unit (alone)
 };
 
-// Which kernels have their attributes set.
+// Which kernels have their attributes set, and what was asked about them then.
+constexpr int kQ4MaxCluster = 16;
+struct Q4RowsKernels {
+    bool set;
+    int16_t clusters[kQ4MaxCluster + 1];   // of so many thread blocks that the GPU holds at a time
+};
 struct Q4AttrSet {
-    bool rows[4], sm100[2];
+    Q4RowsKernels rows[4];   // head_dim 64, 128 (2); 8, 16 rows (1)
+    bool sm100[2];
 };
 // Few query rows of a KV head (q4_attn_rows.cu), many (q4_attn_sm100.cu).  The former, too, for some small calls
 // with more rows, in their form of one launch: 32 rows and 8 heads on 512 positions 9 against 15 us, 4 x 80 rows and 2 heads 12 against 18, 256 rows on 1400
 // 21 against 26; but 8 x 128 rows on 1000, half a GPU full, 27 against 21, and they stay with the latter.
-bool q4_attn_rows_faster(const Q4AttnParams &p, int n_sm);
+reader_status q4_attn_rows_faster(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, bool *yes);
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
 reader_status launch_q4_attn_sm100(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st);
 // The status words before a kernel raises some.

@@ -42,7 +42,6 @@ struct Shape {
 };
 constexpr int kUnitCost = 2;       // entries that stand for a unit's start and end
 constexpr int kMinEntries = kUnitCost + 1;   // of a range: so every one of them holds a tile
-constexpr int kMaxCluster = 16;
 
 template <int D, int NT>
 struct Cfg {
@@ -825,34 +824,62 @@ __global__ void __launch_bounds__(1024) q4_attn_status_kernel(int32_t *status, i
     for (int b = threadIdx.x; b < B; b += 1024) status[b] = READER_OK;
 }
 
-// Thread blocks of a unit in the alone form, 0 if the call is not one for it: the units of a sequence have to fit a cluster, the clusters the GPU, and,
+// Thread blocks of a unit in the alone form, 0 if the call is not one for it: the units of a sequence have to fit a cluster, the clusters the GPU all at once (8
+// single tokens on 2048, 32/8/128: eight clusters of 16 blocks in two turns 20.8 us, of 8 in one 13.9; 4 of them 11.2 and 13.5), and,
 // going by the page table's width, a worker gets at most `most` tiles.
 constexpr int kAloneTiles = 6, kAloneTilesManyRows = 2;
 template <int NT>
-int alone_split(const Q4AttnParams &p, int n_sm, int most) {
+int alone_split(const Q4AttnParams &p, const Q4RowsKernels &k, int most) {
     using S = Shape<NT>;
     const int64_t units = (int64_t)p.Hkv * ((p.T * p.G + S::kRows - 1) / S::kRows), tiles = p.max_pages + (p.T + kPage - 1) / kPage;
-    if (units > kMaxCluster) return 0;
+    auto fits = [&](int64_t blocks) { return blocks <= kQ4MaxCluster && p.B <= k.clusters[blocks]; };
+    if (!fits(units)) return 0;
     int split = 1;
-    while (2 * split * units <= kMaxCluster && 2 * split * units * p.B <= n_sm && tiles > split * S::kWarps) split *= 2;
-    return units * split * p.B <= n_sm && tiles <= (int64_t)most * split * S::kWarps ? split : 0;
+    while (fits(2 * split * units) && tiles > split * S::kWarps) split *= 2;
+    return tiles <= (int64_t)most * split * S::kWarps ? split : 0;
 }
 
 template <int D, int NT>
-reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) {
+reader_status set_up(Q4RowsKernels *k) {
     using S = Shape<NT>;
     using C = Cfg<D, NT>;
-    if (!*attr_set) {
+    if (!k->set) {
         if (cudaFuncSetAttribute(q4_attn_list_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess ||
             cudaFuncSetAttribute(q4_attn_alone_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess ||
             cudaFuncSetAttribute(q4_attn_alone_kernel<D, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
             cudaGetLastError();
             return READER_ERR_CUDA;
         }
-        *attr_set = true;
+        for (int blocks = 1; blocks <= kQ4MaxCluster; ++blocks) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)blocks);
+            cfg.blockDim = dim3(S::kThreads);
+            cfg.dynamicSmemBytes = C::kSmem;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = (unsigned)blocks;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, q4_attn_alone_kernel<D, NT>, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                return READER_ERR_CUDA;
+            }
+            k->clusters[blocks] = (int16_t)n;
+        }
+        k->set = true;
     }
+    return READER_OK;
+}
+
+template <int D, int NT>
+reader_status launch(Q4RowsKernels *k, Q4AttnParams p, int n_sm, cudaStream_t st) {
+    using S = Shape<NT>;
+    using C = Cfg<D, NT>;
+    if (reader_status e = set_up<D, NT>(k)) return e;
     p.n_rt = (p.T * p.G + S::kRows - 1) / S::kRows;
-    p.split = alone_split<NT>(p, n_sm, kAloneTiles);
+    p.split = alone_split<NT>(p, *k, kAloneTiles);
     if (p.split) {
         const int blocks = p.Hkv * p.n_rt * p.split;   // of a sequence
         cudaLaunchConfig_t cfg = {};
@@ -887,17 +914,22 @@ reader_status launch(bool *attr_set, Q4AttnParams p, int n_sm, cudaStream_t st) 
 
 void launch_q4_attn_status(const Q4AttnParams &p, cudaStream_t st) { launch_pdl(q4_attn_status_kernel, dim3(1), dim3(1024), 0, st, p.status, p.B); }
 
-bool q4_attn_rows_faster(const Q4AttnParams &p, int n_sm) {
-    if (p.T * p.G <= kQ4FewRows) return true;
+reader_status q4_attn_rows_faster(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, bool *yes) {
+    *yes = p.T * p.G <= kQ4FewRows;
+    if (*yes) return READER_OK;
     // With many rows the form of one launch saves two, and its workers need longer for a tile: for calls that leave two thirds of the GPU idle either way.
     const int64_t units = (int64_t)p.B * p.Hkv * ((p.T * p.G + 15) / 16);
-    return 3 * units <= n_sm && alone_split<2>(p, n_sm, kAloneTilesManyRows) != 0;
+    if (3 * units > n_sm) return READER_OK;
+    Q4RowsKernels *k = &attr->rows[p.D == 128 ? 3 : 1];
+    if (reader_status e = p.D == 128 ? set_up<128, 2>(k) : set_up<64, 2>(k)) return e;
+    *yes = alone_split<2>(p, *k, kAloneTilesManyRows) != 0;
+    return READER_OK;
 }
 
 reader_status launch_q4_attn_rows(Q4AttrSet *attr, const Q4AttnParams &p, int n_sm, cudaStream_t st) {
     const bool few = p.T * p.G <= 8;
-    if (p.D == 128) return few ? launch<128, 1>(&attr->rows[0], p, n_sm, st) : launch<128, 2>(&attr->rows[1], p, n_sm, st);
-    return few ? launch<64, 1>(&attr->rows[2], p, n_sm, st) : launch<64, 2>(&attr->rows[3], p, n_sm, st);
+    if (p.D == 128) return few ? launch<128, 1>(&attr->rows[2], p, n_sm, st) : launch<128, 2>(&attr->rows[3], p, n_sm, st);
+    return few ? launch<64, 1>(&attr->rows[0], p, n_sm, st) : launch<64, 2>(&attr->rows[1], p, n_sm, st);
 }
 
 }  // namespace reader

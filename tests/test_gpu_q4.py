@@ -839,3 +839,26 @@ def test_ranges_of_few_positions(rd, heads, d, columns):
                 want[page, :, torch.from_numpy(pos % PAGE)] = held(rows_of(src, x.t16, s, lo, hi))
             assert torch.equal(out.cpu().double(), want)
     assert b.ERR_CAPACITY in rd.q4_store([both[0].wide], [both[0].narrow], first - 1, last).tolist()
+
+
+@pytest.mark.parametrize("B,T,group", [(65536, 1, 1), (65536, 1, 12), (9000, 20, 2)])
+def test_the_largest_batches(rd, B, T, group):
+    """As many sequences as a call may have, with empty ones and ones of a few pages; one page for all that are short."""
+    b = binding()
+    rng = np.random.default_rng(B + T)
+    lens = np.where(rng.random(B) < 0.2, 0, rng.integers(1, PAGE, B))
+    long_ones = [3, 64, B // 2, B - 2]
+    lens[long_ones] = 200
+    both = Both(rng, [200], 1, 64)
+    assert not rd.q4_store([both.wide], [both.narrow], i32([0]), i32([200])).any()
+    table = np.tile(both.t4[0][:4], (B, 1))
+    cache = b.Q4Cache(both.k4, both.v4, i32(table), i32(lens))
+    q, kt, vt = bf16(rng, B, T, group, 64), bf16(rng, B, T, 1, 64), bf16(rng, B, T, 1, 64)
+    parent = random_parents(rng, B, T)
+    got = attend(rd, cache, q, kt, vt, parent, 0.125)
+    assert not any(got[2])
+    some = long_ones + [0, 1, 31, 32, 255, 256, 257, B - 1] + rng.integers(0, B, 20).tolist()
+    pick = lambda x: x[torch.tensor(some)]  # noqa: E731
+    sub = Both.__new__(Both)
+    sub.k, sub.v, sub.t16 = both.k, both.v, np.tile(both.t16[0][:4], (len(some), 1))
+    within((pick(got[0]), pick(got[1])), plain_attn(sub, [int(lens[i]) for i in some], pick(q), pick(kt), pick(vt), parent[some], 0.125))
