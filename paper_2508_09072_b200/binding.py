@@ -253,6 +253,7 @@ class Reader:
         self._prompt_ws: Optional[torch.Tensor] = None
         self._q4_ws: Optional[torch.Tensor] = None
         self._pages_ws: list = []
+        self._pages_need = {}   # bytes, by sizes
 
     @functools.cached_property
     def _native(self):
@@ -708,9 +709,15 @@ class Reader:
     def pages_workspace(self, pages: Pages, n: int = 0) -> torch.Tensor:
         """A cached device buffer for page calls of n requests.  A larger one is made when it is needed; those before it live as long
         as the reader (a captured call may use them)."""
-        need = int(self.lib.reader_pages_workspace_bytes(pages.refs.shape[0], *pages.page_table.shape, n))
-        if need == 0:
-            raise ReaderError(ERR_INVALID_ARG, "reader_pages_workspace_bytes")
+        sizes = (pages.refs.shape[0], *pages.page_table.shape, n)
+        need = self._pages_need.get(sizes)   # (asking the library costs as much as a third of the call)
+        if need is None:
+            need = int(self.lib.reader_pages_workspace_bytes(*sizes))
+            if need == 0:
+                raise ReaderError(ERR_INVALID_ARG, "reader_pages_workspace_bytes")
+            if len(self._pages_need) >= 64:
+                self._pages_need.clear()
+            self._pages_need[sizes] = need
         if not self._pages_ws or self._pages_ws[-1].numel() < need:
             self._pages_ws.append(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
         return self._pages_ws[-1]
