@@ -104,7 +104,7 @@ struct Bars {
     uint64_t q_full, q_empty, s_full[2], p_full[2], pv_done, o_full, piece_full[kAhead], piece_empty[kAhead];
     uint32_t tmem_base;
     int32_t abort;
-    int32_t raw_bad[2 * kRawSlots];   // a page outside the pool among the slot's
+    int32_t raw_use[2 * kRawSlots];   // which use of the slot its barrier is at, times two; odd: a page outside the pool among its pages
     int32_t flags[kAhead];        // what is wrong with unit i mod kAhead
     int32_t poison[kAhead];       // its tree has infinities or NaN among the values
     int32_t warp_sum[kThreads / 32];
@@ -125,6 +125,25 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
         if (gone(abort_s)) return false;
         if (globaltimer_ns() - t0 > kWaitLimitNs) *abort_s = 1;
     }
+}
+// Wait for the n-th use of the ring, whose place is `at`.  The groups of unpacking warps have a slot's uses in turns, so neither sees all phases of its barrier,
+// and a parity tells a phase only from the one before: where the use before this one is still on its way (a later copy may come first), the wait would
+// be over at once.  So the slot has to be at this use first.
+__device__ __forceinline__ bool arrived(Bars *m, const Place &at, int n, volatile int32_t *abort_s, bool &bad) {
+    volatile int32_t *use = m->raw_use + at.s;
+    const uint32_t bar = smem_u32(m->raw_full + at.s);
+    int now = *use;   // (before the wait: what it says after one may have come between)
+    const bool ok = mbar_try_wait(bar, at.parity);
+    if (!__all_sync(0xffffffffu, ok && now >> 1 == n)) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!__all_sync(0xffffffffu, (now = *use) >> 1 == n)) {
+            if (gone(abort_s)) return false;
+            if (globaltimer_ns() - t0 > kWaitLimitNs) *abort_s = 1;
+        }
+        if (!wait(bar, at.parity, abort_s)) return false;
+    }
+    bad = now & 1;
+    return true;
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -299,6 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     auto bar = [&](const uint64_t *b) { return smem_u32(b); };
     if (tid == 0) {
         for (int i = 0; i < 2 * kRawSlots; ++i) {
+            m->raw_use[i] = -1;
             mbar_init(bar(&m->raw_full[i]), 1);
             mbar_init(bar(&m->raw_empty[i]), kUnpackWarps);
         }
@@ -428,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         const Place slot(n, six);
                         if (!wait(bar(&m->raw_empty[slot.s]), slot.parity ^ 1, abort_s)) break;
                         if (lane == 0) {
-                            m->raw_bad[slot.s] = !(ok0 && ok1);
+                            *(volatile int32_t *)&m->raw_use[slot.s] = 2 * n + !(ok0 && ok1);
                             const uint32_t full = bar(&m->raw_full[slot.s]), dst = base + C::raw_at(slot.s);
                             const unsigned char *pool = kv ? p.v_pool : p.k_pool;
                             const int bytes = (ok0 ? C::kPageBytes : 0) + (count == 2 && ok1 ? C::kPageBytes : 0);
@@ -569,9 +589,10 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     copy_tree_keys<D>(p, x.b, x.h, kt, t);
                 } else {
                     const Place at(raw + 2 * i, six);
-                    if (!wait(bar(&m->raw_full[at.s]), at.parity, abort_s)) break;
+                    bool bad;
+                    if (!arrived(m, at, raw + 2 * i, abort_s, bad)) break;
                     const uint32_t src = base + C::raw_at(at.s);
-                    if (m->raw_bad[at.s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
+                    if (bad && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
@@ -586,7 +607,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     if (copy_tree_values<D>(p, x.b, x.h, vt, t)) atomicOr(&m->poison[seg & (kAhead - 1)], 1);
                 } else {
                     const Place at(raw + 2 * i + 1, six);
-                    if (!wait(bar(&m->raw_full[at.s]), at.parity, abort_s)) break;
+                    bool bad;
+                    if (!arrived(m, at, raw + 2 * i + 1, abort_s, bad)) break;
                     const uint32_t src = base + C::raw_at(at.s);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page)

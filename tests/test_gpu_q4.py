@@ -862,3 +862,21 @@ def test_the_largest_batches(rd, B, T, group):
     sub = Both.__new__(Both)
     sub.k, sub.v, sub.t16 = both.k, both.v, np.tile(both.t16[0][:4], (len(some), 1))
     within((pick(got[0]), pick(got[1])), plain_attn(sub, [int(lens[i]) for i in some], pick(q), pick(kt), pick(vt), parent[some], 0.125))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,group", [(77, 5), (100, 3), (32, 4)])
+def test_the_same_bits_behind_other_work(rd, T, group, d):
+    """Calls that begin with cold caches, whose first pages come late and in any order: one call in some hundreds once took values before they were there."""
+    rng = np.random.default_rng(49)
+    lens = rng.integers(379, 610, 31).tolist()
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, group, d)
+    want = attend(rd, cache, q, kt, vt, parent, d ** -0.5)
+    within(want[:2], plain_attn(both, lens, q, kt, vt, parent, d ** -0.5))
+    q, kt, vt, parent, expect = q.cuda(), kt.cuda(), vt.cuda(), i32(parent), want[0].cuda()
+    out, wide, differ = torch.empty_like(expect), expect.double(), 0
+    for i in range(1500):
+        rd.q4_verify_attn(q, kt, vt, cache, parent, d ** -0.5, out=out)
+        off = (out.double() - wide).norm(dim=-1) / wide.norm(dim=-1)
+        differ += len((off != 0).nonzero())
+    assert differ == 0
