@@ -128,22 +128,20 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
 }
 // Wait for the n-th use of the ring, whose place is `at`.  The groups of unpacking warps have a slot's uses in turns, so neither sees all phases of its barrier,
 // and a parity tells a phase only from the one before: where the use before this one is still on its way (a later copy may come first), the wait would
-// be over at once.  So the slot has to be at this use first.
-__device__ __forceinline__ bool arrived(Bars *m, const Place &at, int n, volatile int32_t *abort_s, bool &bad) {
-    volatile int32_t *use = m->raw_use + at.s;
-    const uint32_t bar = smem_u32(m->raw_full + at.s);
-    int now = *use;   // (before the wait: what it says after one may have come between)
-    const bool ok = mbar_try_wait(bar, at.parity);
-    if (!__all_sync(0xffffffffu, ok && now >> 1 == n)) {
-        const uint64_t t0 = globaltimer_ns();
-        while (!__all_sync(0xffffffffu, (now = *use) >> 1 == n)) {
-            if (gone(abort_s)) return false;
-            if (globaltimer_ns() - t0 > kWaitLimitNs) *abort_s = 1;
+// be over at once.  So of three slots this one has to be at this use first.  (Of six, the use before is three tiles or more back: its tile has been multiplied before
+// this one's place among the operands is free.)
+__device__ __forceinline__ bool arrived(Bars *m, const Place &at, int n, bool six, volatile int32_t *abort_s) {
+    if (!six) {
+        volatile int32_t *use = m->raw_use + at.s;
+        if (!__all_sync(0xffffffffu, *use >> 1 == n)) {
+            const uint64_t t0 = globaltimer_ns();
+            while (!__all_sync(0xffffffffu, *use >> 1 == n)) {
+                if (gone(abort_s)) return false;
+                if (globaltimer_ns() - t0 > kWaitLimitNs) *abort_s = 1;
+            }
         }
-        if (!wait(bar, at.parity, abort_s)) return false;
     }
-    bad = now & 1;
-    return true;
+    return wait(smem_u32(m->raw_full + at.s), at.parity, abort_s);
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -589,10 +587,9 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     copy_tree_keys<D>(p, x.b, x.h, kt, t);
                 } else {
                     const Place at(raw + 2 * i, six);
-                    bool bad;
-                    if (!arrived(m, at, raw + 2 * i, abort_s, bad)) break;
+                    if (!arrived(m, at, raw + 2 * i, six, abort_s)) break;
                     const uint32_t src = base + C::raw_at(at.s);
-                    if (bad && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
+                    if ((m->raw_use[at.s] & 1) && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
@@ -607,8 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     if (copy_tree_values<D>(p, x.b, x.h, vt, t)) atomicOr(&m->poison[seg & (kAhead - 1)], 1);
                 } else {
                     const Place at(raw + 2 * i + 1, six);
-                    bool bad;
-                    if (!arrived(m, at, raw + 2 * i + 1, abort_s, bad)) break;
+                    if (!arrived(m, at, raw + 2 * i + 1, six, abort_s)) break;
                     const uint32_t src = base + C::raw_at(at.s);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page)
