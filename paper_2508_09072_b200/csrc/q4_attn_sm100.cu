@@ -100,11 +100,13 @@ struct Place {
     }
 };
 struct Bars {
-    uint64_t raw_full[2 * kRawSlots], raw_empty[2 * kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
+    // A slot has a barrier for each group of unpacking warps.  (The groups have its uses in turns, and a parity tells a phase only from the one before: at a common barrier a
+    // group would take a use of the other's that is still on its way for its own.  Copies need not come in order.)
+    uint64_t raw_full[2][2 * kRawSlots], raw_empty[2 * kRawSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t q_full, q_empty, s_full[2], p_full[2], pv_done, o_full, piece_full[kAhead], piece_empty[kAhead];
     uint32_t tmem_base;
     int32_t abort;
-    int32_t raw_use[2 * kRawSlots];   // which use of the slot its barrier is at, times two; odd: a page outside the pool among its pages
+    int32_t raw_bad[2 * kRawSlots];   // a page outside the pool among the slot's
     int32_t flags[kAhead];        // what is wrong with unit i mod kAhead
     int32_t poison[kAhead];       // its tree has infinities or NaN among the values
     int32_t warp_sum[kThreads / 32];
@@ -125,23 +127,6 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
         if (gone(abort_s)) return false;
         if (globaltimer_ns() - t0 > kWaitLimitNs) *abort_s = 1;
     }
-}
-// Wait for the n-th use of the ring, whose place is `at`.  The groups of unpacking warps have a slot's uses in turns, so neither sees all phases of its barrier,
-// and a parity tells a phase only from the one before: where the use before this one is still on its way (a later copy may come first), the wait would
-// be over at once.  So of three slots this one has to be at this use first.  (Of six, the use before is three tiles or more back: its tile has been multiplied before
-// this one's place among the operands is free.)
-__device__ __forceinline__ bool arrived(Bars *m, const Place &at, int n, bool six, volatile int32_t *abort_s) {
-    if (!six) {
-        volatile int32_t *use = m->raw_use + at.s;
-        if (!__all_sync(0xffffffffu, *use >> 1 == n)) {
-            const uint64_t t0 = globaltimer_ns();
-            while (!__all_sync(0xffffffffu, *use >> 1 == n)) {
-                if (gone(abort_s)) return false;
-                if (globaltimer_ns() - t0 > kWaitLimitNs) *abort_s = 1;
-            }
-        }
-    }
-    return wait(smem_u32(m->raw_full + at.s), at.parity, abort_s);
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -316,8 +301,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
     auto bar = [&](const uint64_t *b) { return smem_u32(b); };
     if (tid == 0) {
         for (int i = 0; i < 2 * kRawSlots; ++i) {
-            m->raw_use[i] = -1;
-            mbar_init(bar(&m->raw_full[i]), 1);
+            mbar_init(bar(&m->raw_full[0][i]), 1);
+            mbar_init(bar(&m->raw_full[1][i]), 1);
             mbar_init(bar(&m->raw_empty[i]), kUnpackWarps);
         }
         for (int i = 0; i < 2; ++i) {
@@ -425,7 +410,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             // ------------------------------------------------------------------ pages
             const uint64_t policy = l2_policy_evict_first();
             const bool once = list.n_wide + list.narrow == 1;   // no other unit reads these pages
-            int n = 0;   // slots of the ring so far
+            int n = 0, tiles = 0;                // slots of the ring, tiles so far
+            uint32_t parity = 0, of_group = 0;   // bit slot + 8 group: of the next use; bit slot: whose the last use is
             Piece x;
             for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
                 const int pages_end = min(x.npages, 2 * (x.t0 + x.tiles));
@@ -446,8 +432,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         const Place slot(n, six);
                         if (!wait(bar(&m->raw_empty[slot.s]), slot.parity ^ 1, abort_s)) break;
                         if (lane == 0) {
-                            *(volatile int32_t *)&m->raw_use[slot.s] = 2 * n + !(ok0 && ok1);
-                            const uint32_t full = bar(&m->raw_full[slot.s]), dst = base + C::raw_at(slot.s);
+                            m->raw_bad[slot.s] = !(ok0 && ok1);
+                            const uint32_t full = bar(&m->raw_full[(tiles + t) & 1][slot.s]), dst = base + C::raw_at(slot.s);
                             const unsigned char *pool = kv ? p.v_pool : p.k_pool;
                             const int bytes = (ok0 ? C::kPageBytes : 0) + (count == 2 && ok1 ? C::kPageBytes : 0);
                             mbar_arrive_expect_tx(full, bytes);   // (a page outside the pool is not read; what the slot holds is never shown)
@@ -455,14 +441,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                             if (count == 2 && ok1) bulk_load(dst + C::kPageBytes, pool + ((size_t)id1 * p.Hkv + x.h) * C::kPageBytes, C::kPageBytes, full, policy, streamed);
                         }
                         __syncwarp();
+                        parity ^= 1u << (slot.s + 8 * ((tiles + t) & 1));
+                        of_group = (of_group & ~(1u << slot.s)) | ((tiles + t) & 1u) << slot.s;
                     }
                 }
+                tiles += x.tiles;
             }
             if (gone(abort_s)) {   // the block does not end under its own copies
                 const uint64_t t0 = globaltimer_ns();
                 for (int i = max(0, n - (six ? 2 : 1) * kRawSlots); i < n; ++i) {
-                    const Place at(i, six);
-                    while (!mbar_try_wait(bar(&m->raw_full[at.s]), at.parity) && globaltimer_ns() - t0 < 20000000ull) {
+                    const int s = Place(i, six).s, group = (of_group >> s) & 1;
+                    while (!mbar_try_wait(bar(&m->raw_full[group][s]), ((parity >> (s + 8 * group)) & 1) ^ 1) && globaltimer_ns() - t0 < 20000000ull) {
                     }
                 }
             }
@@ -567,6 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         const uint32_t sixteen = *word;
         asm volatile("bar.sync 2, 256;" ::: "memory");
         int n = 0, raw = 0, trees = 0;   // tiles, slots of the ring, trees so far
+        uint32_t parity = 0;             // bit slot: of the group's next use
         Piece x;
         for (int seg = 0; next_piece(m, x, seg, lane, abort_s); ++seg) {
             const bool has_tree = x.is_tree(x.tiles - 1);
@@ -587,9 +577,10 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     copy_tree_keys<D>(p, x.b, x.h, kt, t);
                 } else {
                     const Place at(raw + 2 * i, six);
-                    if (!arrived(m, at, raw + 2 * i, six, abort_s)) break;
+                    if (!wait(bar(&m->raw_full[group][at.s]), (parity >> at.s) & 1, abort_s)) break;
+                    parity ^= 1u << at.s;
                     const uint32_t src = base + C::raw_at(at.s);
-                    if ((m->raw_use[at.s] & 1) && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
+                    if (m->raw_bad[at.s] && t == 0) atomicOr(&m->flags[seg & (kAhead - 1)], kBadPage);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page) unpack_keys<D>(src + page * C::kPageBytes, kt, page * kPage, t, sixteen);
                     __syncwarp();
@@ -604,7 +595,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     if (copy_tree_values<D>(p, x.b, x.h, vt, t)) atomicOr(&m->poison[seg & (kAhead - 1)], 1);
                 } else {
                     const Place at(raw + 2 * i + 1, six);
-                    if (!arrived(m, at, raw + 2 * i + 1, six, abort_s)) break;
+                    if (!wait(bar(&m->raw_full[group][at.s]), (parity >> at.s) & 1, abort_s)) break;
+                    parity ^= 1u << at.s;
                     const uint32_t src = base + C::raw_at(at.s);
 #pragma unroll 1
                     for (int page = 0; page * kPage < valid && page < 2; ++page)
