@@ -2,7 +2,7 @@
 //
 // Bound: the tensor pipe and the exponentials, 2048 cycles each for 256 query rows and 128 keys; what 4 bits add is turning
 // numbers into bf16 operands, 16384 of them for each, once for all rows that share them.  Measured (32 query heads, 8 KV heads, head_dim 128): four trees of 128
-// nodes on 32768 positions 316 us, 0.87 PF/s; 32 trees of 32 nodes on 1024-4096 79 us.  Either way a step of 128 rows and 128 keys is 1.4 to 1.7 us,
+// nodes on 32768 positions 316 us, 0.87 PF/s; 32 trees of 32 nodes on 1024-4096 80 us.  Either way a step of 128 rows and 128 keys is 1.4 to 1.7 us,
 // the softmax warps' 0.3 for the maximum and 0.85 to 1.05 for 8192 exponentials (0.54 if nothing else ran) and hardly a wait.  So a thread block (one per SM) has up to
 // 256 rows of one KV head, two slots of 128, and eight warps of it do nothing but unpack: a tile of 128 keys (two pages) becomes
 // the rows of K, and its values the rows of V^T (position pairs are neighbours in the pages, so a pair of numbers is a
