@@ -741,6 +741,7 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_alone_kernel(c
     k.init(smem, warp);
     __shared__ int flags;
     if (tid == 0) flags = 0;
+    __syncthreads();   // before any warp raises one
     pdl_wait();
     pdl_launch_dependents();
     const int size = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
