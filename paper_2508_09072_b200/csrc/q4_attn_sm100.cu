@@ -786,28 +786,37 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
             const uint32_t tO = tmem + kTmemO + (x.wide ? half * D : 0) + lane_base;
             int flag = *(volatile int32_t *)&m->flags[seg % kAhead];
             if (*abort_s || (int)blockIdx.x == p.give_up) flag |= kGaveUp;
-            if (has_tree && *(volatile int32_t *)&m->poison[seg % kAhead] && warp_live) {
-                // infinities and NaN were left out of the product: the rows that see them get them
+            if (has_tree && *(volatile int32_t *)&m->poison[seg % kAhead] && warp_live && !(flag & kBadTree)) {
+                // Infinities and NaN were left out of the product: the rows that see them get them.  All nodes' before the columns are stored again: a store to tensor
+                // memory is not there for the next load until it has been waited for.
+                uint64_t sees0 = 0, sees1 = 0;
+                if (live && p.anc) {
+                    sees0 = p.anc[((size_t)x.b * p.T + node) * 2];
+                    sees1 = p.anc[((size_t)x.b * p.T + node) * 2 + 1];
+                } else if (live) {
+                    for (int i = node; i >= 0; i = p.parent[(size_t)x.b * p.T + i]) {
+                        if (i < 64) sees0 |= 1ull << i;
+                        else sees1 |= 1ull << (i - 64);
+                    }
+                }
+                const uint32_t *val = reinterpret_cast<const uint32_t *>(p.v_tree + ((size_t)x.b * p.T * p.Hkv + x.h) * D);
 #pragma unroll 1
-                for (int n = 0; n < p.T && !(flag & kBadTree); ++n) {
-                    bool sees = false;
-                    if (live && p.anc) sees = (p.anc[((size_t)x.b * p.T + node) * 2 + (n >> 6)] >> (n & 63)) & 1;
-                    if (live && !p.anc)
-                        for (int i = node; i >= n; i = p.parent[(size_t)x.b * p.T + i]) sees |= i == n;
-                    const uint32_t *val = reinterpret_cast<const uint32_t *>(p.v_tree + (((size_t)x.b * p.T + n) * p.Hkv + x.h) * D);
+                for (int c = col0; c < col1; c += 16) {
+                    uint32_t o[16];
+                    tmem_ld16(tO + c, o);
+                    tmem_wait_ld();
 #pragma unroll 1
-                    for (int c = col0; c < col1; c += 16) {
-                        uint32_t o[16];
-                        tmem_ld16(tO + c, o);
-                        tmem_wait_ld();
+                    for (int n = 0; n < p.T; ++n) {
+                        if (!(((n < 64 ? sees0 : sees1) >> (n & 63)) & 1)) continue;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const uint32_t w = val[c / 2 + i];
-                            if (sees && nonfinite(w << 16)) o[2 * i] = __float_as_uint(__uint_as_float(o[2 * i]) + bf16lo(w));
-                            if (sees && nonfinite(w)) o[2 * i + 1] = __float_as_uint(__uint_as_float(o[2 * i + 1]) + bf16hi(w));
+                            const uint32_t w = val[(size_t)n * p.Hkv * (D / 2) + c / 2 + i];
+                            if (nonfinite(w << 16)) o[2 * i] = __float_as_uint(__uint_as_float(o[2 * i]) + bf16lo(w));
+                            if (nonfinite(w)) o[2 * i + 1] = __float_as_uint(__uint_as_float(o[2 * i + 1]) + bf16hi(w));
                         }
-                        tmem_st16(tO + c, o);
                     }
+                    __syncwarp();
+                    tmem_st16(tO + c, o);
                 }
                 tmem_wait_st();
             }

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_q4 import attend, binding, i32, make, rd  # noqa: F401 (rd: a fixture)
+from test_gpu_q4 import attend, binding, i32, make, plain_attn, rd, sees_of  # noqa: F401 (rd: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +27,34 @@ def test_every_bad_page_is_reported_on_every_call(rd, T, group, d):
     for i in range(500):
         rd.q4_verify_attn(q, kt, vt, cache, parent, 0.1, out=out, status=status[i])
     assert (status == b.ERR_BAD_PAGE).all() and not out.any()
+
+
+# ---------------------------------------------------------------------------------------------- infinite values
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,group", [(5, 1), (16, 1), (40, 4), (100, 3), (128, 2)])
+@pytest.mark.parametrize("masks", [False, True])
+def test_infinite_values_of_several_nodes_add_up(rd, d, T, group, masks):
+    """A column has what all the nodes that a row sees add to it: their sum in fp32, infinite or NaN (of +inf and -inf), in one column or in many."""
+    rng = np.random.default_rng(61)
+    lens = [70, 0, 200]
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, group, d)
+    for s in range(3):   # (a path down half of the nodes, so that rows see several)
+        parent[s, 1:T // 2] = np.arange(T // 2 - 1)
+    want = plain_attn(both, lens, q, kt, vt, parent, 0.1)
+    x = vt.clone()
+    for s in range(3):
+        for h in range(2):
+            for n in rng.permutation(T)[:max(3, T // 4)]:
+                for e in rng.permutation(d)[:3].tolist() + [1, d - 1]:
+                    x[s, n, h, e] = float(rng.choice([np.inf, -np.inf, np.inf, np.nan] if s == 1 else [np.inf, -np.inf] if s == 0 else [np.inf]))
+    kw = {"anc_mask": rd.tree_encode(i32(parent))[0]} if masks else {}
+    out, lse, st = attend(rd, cache, q, kt, x, parent, 0.1, **kw)
+    assert st == [0] * 3
+    seen = torch.from_numpy(np.stack([sees_of(p) for p in parent]))                       # [b, rows, nodes]
+    count = lambda which: torch.einsum("btn,bnhd->bthd", seen.double(), which(x.double()).double()).repeat_interleave(group, 2)  # noqa: E731
+    plus, minus, nan = count(lambda y: y == np.inf), count(lambda y: y == -np.inf), count(torch.isnan)
+    assert (plus > 1).any() and ((plus > 0) & (minus > 0)).any()
+    is_nan, is_plus, is_minus = (nan > 0) | (plus > 0) & (minus > 0), (plus > 0) & (minus == 0) & (nan == 0), (minus > 0) & (plus == 0) & (nan == 0)
+    assert torch.isnan(out[is_nan]).all() and (out[is_plus] == np.inf).all() and (out[is_minus] == -np.inf).all()
+    rest = ~(is_nan | is_plus | is_minus)
+    assert ((out.double() - want[0]).abs() <= want[2])[rest].all() and ((lse.double() - want[1]).abs() <= want[3]).all()
