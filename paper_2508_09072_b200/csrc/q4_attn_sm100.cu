@@ -30,6 +30,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "ancestors.cuh"
 #include "prompt_ptx.cuh"
 #include "q4_attn_common.cuh"
 
@@ -659,8 +660,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                                 sees = p.anc[((size_t)x.b * p.T + node) * 2 + half];
                             } else if (live && !(*(volatile int32_t *)&m->flags[seg % kAhead] & kBadTree)) {
                                 const unsigned char *parents = smem + C::kOffParents + (trees & (kAhead / 2 - 1)) * kMaxNodes;
-                                for (int n = node; n != 255; n = parents[n])   // (strictly falling on a valid tree)
-                                    if ((n >> 6) == half) sees |= 1ull << (n & 63);
+                                sees = ancestors(parents, node, half);
                             }
                         }
                         if (valid < 64) sees &= valid <= 0 ? 0 : (1ull << valid) - 1;
@@ -794,10 +794,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                     sees0 = p.anc[((size_t)x.b * p.T + node) * 2];
                     sees1 = p.anc[((size_t)x.b * p.T + node) * 2 + 1];
                 } else if (live) {
-                    for (int i = node; i >= 0; i = p.parent[(size_t)x.b * p.T + i]) {
-                        if (i < 64) sees0 |= 1ull << i;
-                        else sees1 |= 1ull << (i - 64);
-                    }
+                    sees0 = ancestors(p.parent + (size_t)x.b * p.T, node, 0);
+                    sees1 = ancestors(p.parent + (size_t)x.b * p.T, node, 1);
                 }
                 const uint32_t *val = reinterpret_cast<const uint32_t *>(p.v_tree + ((size_t)x.b * p.T * p.Hkv + x.h) * D);
 #pragma unroll 1
