@@ -724,9 +724,10 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                         }
                     }
                     // 2^((s - max) scale) by one multiplication and addition.  The maximum times the scale is rounded, by the same for all keys of a
-                    // row: it cancels, but where it is so large that its rounding is not small against 1 the difference is taken first.
+                    // row: it cancels, but where it is so large that its rounding is not small against 1, or beyond fp32, the difference is taken first.  (A row
+                    // without a query, and one with an infinite score, has an infinite maximum: no difference helps.)
                     float from = mx == -INFINITY ? 0.f : -mx * p.scale_log2;
-                    if (__any_sync(0xffffffffu, fabsf(from) > 65536.f && fabsf(from) < INFINITY)) {
+                    if (__any_sync(0xffffffffu, fabsf(from) > 65536.f && fabsf(mx) < INFINITY)) {
 #pragma unroll 1
                         for (int c = 0; c < 64; c += 16) {
                             uint32_t y[16];

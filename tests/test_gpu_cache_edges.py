@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_q4 import attend, binding, i32, make, plain_attn, rd, sees_of  # noqa: F401 (rd: a fixture)
+from test_gpu_q4 import attend, binding, held, i32, make, plain_attn, rd, rows_of, sees_of, widened  # noqa: F401 (rd: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,54 @@ def test_infinite_values_of_several_nodes_add_up(rd, d, T, group, masks):
     assert torch.isnan(out[is_nan]).all() and (out[is_plus] == np.inf).all() and (out[is_minus] == -np.inf).all()
     rest = ~(is_nan | is_plus | is_minus)
     assert ((out.double() - want[0]).abs() <= want[2])[rest].all() and ((lse.double() - want[1]).abs() <= want[3]).all()
+
+
+# ---------------------------------------------------------------------------------------------- scores and scales at the ends of fp32
+FP32_MAX = torch.finfo(torch.float32).max
+
+
+def one_hot(rng, shape, value):
+    """Queries with one element that is not 0: a score is that times an element of a key, which fp32 holds exactly."""
+    q = torch.zeros(shape, dtype=torch.bfloat16)
+    at = torch.from_numpy(rng.integers(0, shape[-1], shape[:-1]))
+    return q.scatter_(-1, at[..., None], torch.full((*shape[:-1], 1), value, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("columns", [None, 700])
+@pytest.mark.parametrize("T", [1, 4, 40])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("size,scale", [(2.0 ** 100, 2.0 ** 30), (2.0 ** 118, 64.0), (1.0, 1.9e38)])
+def test_scaled_scores_beyond_fp32(rd, size, scale, sign, T, columns):
+    """Finite scores whose products with the scale are not: a row's largest keys share it, whatever the largest score's sign.  Scores are exact and differ by 0 or by
+    far more than 2^10 scaled, so that weights are exact, too: what is left are the roundings to bf16 of 1 / n (its sum: n terms in fp32) and of the output."""
+    rng = np.random.default_rng(50)
+    lens = [300, 65, 2000]
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, 2, 64, scale=16.0)
+    if sign < 0:   # keys below 0 alone, far enough that none is held as 0
+        both.k.copy_(-both.k.abs() - 16)
+        rd.q4_store([both.wide], [both.narrow], torch.zeros(3, dtype=torch.int32, device="cuda"), cache.seq_lens)
+        kt = -kt.abs() - 16
+    q = one_hot(rng, tuple(q.shape), size)
+    out, lse, st = attend(rd, cache if columns is None else widened(cache, columns), q, kt, vt, parent, scale)
+    assert st == [0] * 3
+    o, z, mag = plain_rows(both, lens, q, kt, vt, parent, scale)
+    far = z.abs() > FP32_MAX
+    assert far.any() and (lse[far] == torch.where(z[far] > 0, torch.inf, -torch.inf)).all()
+    assert ((lse.double() - z).abs() <= z.abs() * 2.0 ** -22)[z.abs() < FP32_MAX / 2].all()
+    assert ((out.double() - o).abs() <= 2.0 ** -8 * (mag + o.abs()) * 1.01 + 1e-30).all()
+
+
+def plain_rows(both, lens, q, kt, vt, parent, scale):
+    """out, lse and the sums of weights times magnitudes in 64 bits, the maximum taken off before the exponentials (beside scores of 2^128 a logarithm is lost in 64 bits, too)."""
+    out, mag, lse = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape[:3], dtype=torch.float64)
+    group = q.shape[2] // kt.shape[2]
+    for b, n in enumerate(lens):
+        k = torch.cat([held(rows_of(both.k, both.t16, b, 0, n)), kt[b].double()])
+        v = torch.cat([held(rows_of(both.v, both.t16, b, 0, n)), vt[b].double()])
+        mask = torch.ones(q.shape[1], len(k), dtype=torch.bool)
+        mask[:, n:] = torch.from_numpy(sees_of(parent[b]))
+        for h in range(q.shape[2]):
+            s = (q[b, :, h].double() @ k[:, h // group].T * scale).masked_fill(~mask, -torch.inf)
+            p = s.softmax(-1)
+            out[b, :, h], mag[b, :, h], lse[b, :, h] = p @ v[:, h // group], p @ v[:, h // group].abs(), s.logsumexp(-1)
+    return out, lse, mag
