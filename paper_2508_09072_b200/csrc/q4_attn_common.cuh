@@ -1,5 +1,7 @@
 // What the kernels of the attention over a 4-bit cache share: copies, the numbers' way to bf16, the list of their work, the merge of shares.
 #pragma once
+#include <cfloat>
+
 #include "ptx_sm100.cuh"
 #include "q4_attn.cuh"
 #include "q4_format.cuh"
@@ -10,6 +12,8 @@ namespace q4 {
 using namespace ptx;
 
 constexpr float kRaiseBy = 8.f;    // log2 units by which a score may exceed the maximum in use
+// The same as a difference of scores; finite whatever the scale (infinity and -inf, the maximum before the first score, have no sum).
+__device__ __forceinline__ float raise_by(const Q4AttnParams &p) { return fminf(kRaiseBy / p.scale_log2, FLT_MAX); }
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr int kBadTree = 1, kBadLength = 2, kBadPage = 4, kGaveUp = 8;   // what is wrong with a share
 

@@ -209,7 +209,7 @@ struct Worker {
         float top[NT][2];
         bool rises = false;
         // the maximum in use is raised only when a score exceeds it by 2^8: the vote needs no exchange
-        const float by = kRaiseBy / p.scale_log2;
+        const float by = raise_by(p);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -621,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         constexpr uint32_t kNegInf = 0xff800000u;
         float *top_s = reinterpret_cast<float *>(smem + C::kOffSwap), *sum_s = top_s + 256;
-        const float by = kRaiseBy / p.scale_log2;
+        const float by = raise_by(p);
         auto pair_barrier = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(5 + (warp & 3)) : "memory"); };
         uint32_t s_parity = 0;   // bit `slot`
         uint32_t narrow_steps = 0;

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_q4 import attend, binding, held, i32, make, plain_attn, rd, rows_of, sees_of, widened  # noqa: F401 (rd: a fixture)
+from test_gpu_q4 import attend, binding, held, i32, make, plain_attn, rd, rows_of, sees_of, widened, within  # noqa: F401 (rd: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +109,19 @@ def plain_rows(both, lens, q, kt, vt, parent, scale):
             p = s.softmax(-1)
             out[b, :, h], mag[b, :, h], lse[b, :, h] = p @ v[:, h // group], p @ v[:, h // group].abs(), s.logsumexp(-1)
     return out, lse, mag
+
+
+@pytest.mark.parametrize("columns", [None, 700])
+@pytest.mark.parametrize("T", [1, 4, 40])
+@pytest.mark.parametrize("size,scale", [(2.0 ** 118, 1e-38), (2.0 ** 118, 1e-39), (1.0, 1.5e-38), (1.0, 1e-45)])
+def test_the_smallest_scales(rd, size, scale, T, columns):
+    """Scales down to the smallest number: weights go by the scaled scores, 0.1 to 1 where the scores are near the end of fp32."""
+    rng = np.random.default_rng(51)
+    lens = [300, 65, 4000]
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 2, 2, 64, scale=16.0)
+    q = one_hot(rng, tuple(q.shape), size)
+    out, lse, st = attend(rd, cache if columns is None else widened(cache, columns), q, kt, vt, parent, scale)
+    assert st == [0] * 3
+    o, z, tol, ltol = plain_attn(both, lens, q, kt, vt, parent, float(np.float32(scale)))
+    # (a subnormal scale times log2 e is off by half of 2^-149, a score is below 2^125 by far: an exponent by 2^-24 at most)
+    within((out, lse), (o, z, tol + 2.0 ** -23 * 8, ltol + 2.0 ** -23))
