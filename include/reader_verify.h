@@ -615,10 +615,10 @@ reader_status reader_pages_fork(reader_ctx *ctx, const reader_pages *pages, cons
  * free one, entries whose page other entries name too get a free one in its place, and where such a page holds positions
  * below seq_lens[r] its data are copied, in all pools.  Whether a page is shared goes by refs before the call: two rows that share a
  * page and are both among the requests get a page each, and the shared one is released.
- *   status_out  READER_ERR_INVALID_ARG: a row outside the table or named by an earlier request, tokens[i] < 0; READER_ERR_BAD_PAGE: an
- *               entry outside the pool, or no page where positions are committed; READER_ERR_CAPACITY: the row is too short for the
- *               new length, or too few pages are free: requests are served in order, and from the first that does not find enough
- *               on none that needs a page is
+ *   status_out  READER_ERR_INVALID_ARG: a row outside the table or named by an earlier request, tokens[i] < 0; READER_ERR_BAD_PAGE
+ *               (tokens[i] > 0): an entry outside the pool among those to write to, or no page where positions are committed;
+ *               READER_ERR_CAPACITY: the row is too short for the new length, or too few pages are free: requests are served in
+ *               order, and from the first that does not find enough on none that needs a page is
  * workspace as for reader_pages_fork.
  */
 reader_status reader_pages_reserve(reader_ctx *ctx, const reader_pages *pages, const int32_t *rows, const int32_t *tokens, int32_t n,

@@ -203,8 +203,8 @@ pages_reserve_kernel(const PagesView p, const int32_t *__restrict__ rows, const 
                 if (page >= p.num_pages) bad = true;
                 else if (page < 0 || p.refs[page] > 1) ++demand;
             }
-            // a page that is begun has to be there
-            if (w.length % kPage != 0 && p.table[(size_t)row * p.width + w.first] < 0) bad = true;
+            // committed positions have pages
+            for (int e = lane; e < (w.length + kPage - 1) / kPage; e += 32) bad |= p.table[(size_t)row * p.width + e] < 0;
             demand = __reduce_add_sync(0xffffffffu, demand);
             if (__any_sync(0xffffffffu, bad)) {
                 st = READER_ERR_BAD_PAGE;

@@ -5,6 +5,8 @@ import torch
 
 from test_gpu_q4 import attend, binding, held, i32, make, plain_attn, rd, rows_of, sees_of, widened, within  # noqa: F401 (rd: a fixture)
 
+from test_gpu_pages import Model, pages
+
 pytestmark = pytest.mark.gpu
 
 
@@ -125,3 +127,41 @@ def test_the_smallest_scales(rd, size, scale, T, columns):
     o, z, tol, ltol = plain_attn(both, lens, q, kt, vt, parent, float(np.float32(scale)))
     # (a subnormal scale times log2 e is off by half of 2^-149, a score is below 2^125 by far: an exponent by 2^-24 at most)
     within((out, lse), (o, z, tol + 2.0 ** -23 * 8, ltol + 2.0 ** -23))
+
+
+# ---------------------------------------------------------------------------------------------- pages
+@pytest.mark.parametrize("rows", [7, 70])
+def test_rows_without_a_committed_page_get_none(rd, rows):
+    """Wherever the missing page is; other requests are served, and pages that nothing is written to need not be in the pool."""
+    b = binding()
+    rng = np.random.default_rng(62)
+    m = Model(rng, 60 * rows, rows, 50, 1, 16)
+    free = rng.permutation(60 * rows).tolist()
+    for r in range(rows):
+        m.lens[r] = [64 * 40, 64 * 40 + 1, 1, 64, 0, 64 * 33 + 7, 64 * 40][r % 7]
+        for e in range(pages(m.lens[r])):
+            m.table[r][e] = free.pop()
+            m.refs[m.table[r][e]] = 1
+    want = []
+    for r in range(rows):
+        hole = [0, 39, None, 0, None, 32, 35][r % 7]
+        if hole is not None:
+            m.refs[m.table[r][hole]] = 0
+            m.table[r][hole] = -1
+        want.append(0 if hole is None else b.ERR_BAD_PAGE)
+    m.table[2][49] = -7
+    p = m.device()
+    before = [list(x) for x in m.table]
+    assert rd.pages_reserve(p, i32(range(rows)), i32([0] * rows)).tolist() == [0] * rows
+    assert rd.pages_reserve(p, i32(range(rows)), i32([70] * rows)).tolist() == want
+    table, refs = p.page_table.tolist(), p.refs.tolist()
+    served = [r for r in range(rows) if want[r] == 0]
+    fresh = [table[r][e] for r in served for e in range(m.lens[r] // 64, pages(m.lens[r] + 70)) if before[r][e] < 0]
+    assert fresh == [page for page, n in enumerate(m.refs) if n == 0][:len(fresh)] and all(refs[page] == 1 for page in fresh)
+    for r in range(rows):
+        if r in served:
+            n = pages(m.lens[r])
+            assert table[r][:n] == before[r][:n]
+        else:
+            assert table[r] == before[r]
+    assert sum(refs) == sum(m.refs) + len(fresh) and p.seq_lens.tolist() == m.lens
