@@ -573,11 +573,13 @@ reader_status reader_set_q4_give_up(reader_ctx *ctx, int32_t worker);
  * Which page of the pools holds what is the caller's affair in the calls above: they follow page_table.  The calls below look
  * after the table on the device, without a host that waits for lengths, for caches of either kind.
  *   refs         i32 [num_pages]: how many entries of the page table name a page; 0 = the page is free.  The caller sets it up
- *                (all zero for an empty cache); pages that are not to be handed out get a count of their own
+ *                (all zero for an empty cache); pages that are not to be handed out get a count of their own (a compaction moves
+ *                them as it moves others: new_ids tells where to)
  *   page_table   i32 [rows][max_pages_per_seq], -1 = no page (as for reader_kv_cache: one table for all layers of a model)
  *   seq_lens     i32 [rows]
  *   pools        HOST array [n_pools] of device pointers, 16-byte aligned: every pool whose pages the table names (keys and
  *                values of all layers), each num_pages * page_bytes bytes; page_bytes is a multiple of 16
+ *   new_ids      i32 [num_pages] or NULL, written by reader_pages_compact alone
  * Row numbers, counts and lengths live on the device; requests come as arrays [n], answers as status_out[n].  A request with a
  * status other than READER_OK changes nothing, unless it says so, and does not disturb the others.
  * Free pages are handed out lowest number first, in the order of the requests: the same inputs give the same pages.
@@ -592,6 +594,7 @@ typedef struct {
     void *const *pools;
     int32_t n_pools;
     size_t page_bytes;
+    int32_t *new_ids;
 } reader_pages;
 
 /* Bytes of device scratch that reader_pages_fork, reader_pages_reserve (of at most n requests) and reader_pages_compact need.
@@ -637,7 +640,10 @@ reader_status reader_pages_free(reader_ctx *ctx, const reader_pages *pages, cons
 /*
  * Moves the pages in use to the front of the pools: with n of them, those numbered n and above move, in ascending order, to the
  * free numbers below n, in ascending order; page_table and refs follow, the data of all pools move.  As few pages move as can.
+ * Pages with a count of the caller's own move like the others, and so do those that another table over the same pools names:
+ * who keeps numbers anywhere but in page_table needs new_ids.
  *   n_used_out  i32 [1]: pages in use; pages from that number on are free afterwards
+ *   pages->new_ids  each page's new number, its own if it stays, -1 if it was free
  * workspace as for reader_pages_fork (any n).
  */
 reader_status reader_pages_compact(reader_ctx *ctx, const reader_pages *pages, int32_t *n_used_out, void *workspace,

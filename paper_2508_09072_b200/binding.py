@@ -750,10 +750,12 @@ class Reader:
             raise ReaderError(st, "reader_pages_free")
         return status
 
-    def pages_compact(self, pages: Pages, n_used: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """The pages in use move to the front of the pools.  Returns their number (i32 [1], on the device)."""
+    def pages_compact(self, pages: Pages, n_used: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      new_ids: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The pages in use move to the front of the pools.  Returns their number (i32 [1], on the device).  new_ids (i32 [num_pages]) is
+        filled with each page's new number, -1 if it was free: for whoever keeps numbers outside the page table."""
         ws = workspace if workspace is not None else self.pages_workspace(pages)
-        st, n_used = self._native.pages_compact(self._handle(), self.device, pages, ws, n_used)
+        st, n_used = self._native.pages_compact(self._handle(), self.device, pages, ws, n_used, new_ids)
         if st != OK:
             raise ReaderError(st, "reader_pages_compact")
         return n_used

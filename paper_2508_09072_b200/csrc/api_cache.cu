@@ -139,7 +139,7 @@ reader_status check_pages(const reader_pages *p, bool with_pools) {
         if (!p->pools[i] || !aligned16(p->pools[i])) return READER_ERR_INVALID_ARG;
     return READER_OK;
 }
-PagesView view(const reader_pages *p) { return {p->refs, p->num_pages, p->page_table, p->rows, p->max_pages_per_seq, p->seq_lens}; }
+PagesView view(const reader_pages *p) { return {p->refs, p->num_pages, p->page_table, p->rows, p->max_pages_per_seq, p->seq_lens, p->new_ids}; }
 
 reader_status pool_chunks(const void *const *from, void *const *to, int n, std::vector<PoolList> &chunks) {
     try {

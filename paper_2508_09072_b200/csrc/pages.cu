@@ -418,6 +418,7 @@ pages_plan_kernel(const PagesView p, int32_t *__restrict__ n_used, const PagesWs
         if (hole) ws.holes[holes + (rank & 0xffff)] = i;
         if (mover) ws.moves[movers + (rank >> 16)].x = i;
         if (in && i >= used && !mover) ws.name[i] = i;
+        if (in && !mover && p.new_ids) p.new_ids[i] = is_held ? i : -1;
         holes += total & 0xffff;
         movers += total >> 16;
     }
@@ -429,6 +430,7 @@ pages_plan_kernel(const PagesView p, int32_t *__restrict__ n_used, const PagesWs
         const int to = __ldcg(ws.holes + k), from = __ldcg(&ws.moves[k].x);
         ws.moves[k].y = to;
         ws.name[from] = to;
+        if (p.new_ids) p.new_ids[from] = to;
         p.refs[to] = p.refs[from];
         p.refs[from] = 0;
     }

@@ -10,6 +10,7 @@ struct PagesView {
     int32_t *table;   // [rows][width], -1: no page
     int rows, width;
     int32_t *lens;    // [rows]
+    int32_t *new_ids;   // nullable: [num_pages] what a compaction makes of a page's number
 };
 
 // Pools whose pages are moved, passed to the kernels by value.

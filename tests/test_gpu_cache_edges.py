@@ -165,3 +165,39 @@ def test_rows_without_a_committed_page_get_none(rd, rows):
         else:
             assert table[r] == before[r]
     assert sum(refs) == sum(m.refs) + len(fresh) and p.seq_lens.tolist() == m.lens
+
+
+@pytest.mark.parametrize("num_pages", [60, 4096, 4097, 9000])
+@pytest.mark.parametrize("share", [0.0, 0.3, 0.9, 1.0])
+def test_a_compaction_tells_where_pages_went(rd, num_pages, share):
+    """Pages that no entry names (a count of the caller's own) and a second table over the same pools are found again."""
+    rng = np.random.default_rng(63)
+    m = Model(rng, num_pages, 10, 20, 2, 16)
+    used = rng.permutation(num_pages)[:int(num_pages * share)].tolist()
+    for i, page in enumerate(used):
+        m.refs[page] = 1
+        if i < 150:
+            m.table[i // 20][i % 20] = page
+    p = m.device()
+    data = [x.clone() for x in p.pools]
+    new_ids = torch.full((num_pages,), 7, dtype=torch.int32, device="cuda")
+    assert rd.pages_compact(p, new_ids=new_ids).tolist() == [m.compact()] == [len(used)]
+    m.same(p)
+    ids = new_ids.cpu().long()
+    held = torch.zeros(num_pages, dtype=torch.bool)
+    held[used] = True
+    assert (ids[~held] == -1).all() and sorted(ids[held].tolist()) == list(range(len(used)))
+    for was, now in zip(data, p.pools):
+        assert torch.equal(now[ids[held].cuda()], was[held.cuda()])
+    again = torch.empty_like(new_ids)   # nothing moves a second time
+    rd.pages_compact(p, new_ids=again)
+    assert again.tolist() == list(range(len(used))) + [-1] * (num_pages - len(used))
+
+
+def test_new_ids_that_cannot_be(rd):
+    m = Model(np.random.default_rng(64), 20, 2, 4, 1, 16)
+    p = m.device()
+    for wrong, error in ((torch.zeros(19, dtype=torch.int32, device="cuda"), ValueError), (torch.zeros(20, dtype=torch.int64, device="cuda"), TypeError),
+                         (torch.zeros(20, dtype=torch.int32), TypeError), (torch.zeros(40, dtype=torch.int32, device="cuda")[::2], TypeError)):
+        with pytest.raises(error, match="new_ids"):
+            rd.pages_compact(p, new_ids=wrong)
