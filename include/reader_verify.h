@@ -530,7 +530,8 @@ reader_status reader_set_prompt_give_up(reader_ctx *ctx, int32_t cta);
  *   first, last  i32 [batch]
  *   status_out   i32 [batch]: READER_ERR_CAPACITY when first[b] < 0, first[b] < shared_prefix_len of `to` or a page table is too
  *                short, READER_ERR_BAD_PAGE when a page of either is outside its pool: nothing of that sequence is written
- * Positions outside the range keep what they hold.  Sequences must not share a page that the call writes to.  head_dim 64 or 128.
+ * Positions outside the range keep what they hold.  Sequences must not share a page that the call writes to.  head_dim 64 or 128, at most
+ * 2^30 sequences.
  */
 reader_status reader_q4_store(reader_ctx *ctx, const reader_kv_cache *from, const reader_kv_cache *to, int32_t n_layers, int32_t batch,
                               const int32_t *first, const int32_t *last, int32_t *status_out, void *stream);
@@ -584,6 +585,7 @@ reader_status reader_set_q4_give_up(reader_ctx *ctx, int32_t worker);
  * status other than READER_OK changes nothing, unless it says so, and does not disturb the others.
  * Free pages are handed out lowest number first, in the order of the requests: the same inputs give the same pages.
  * Pages that a call takes out of the table are free for the next call.
+ * READER_ERR_UNSUPPORTED: more than 2^30 pages or requests, pages of 2^31 bytes or more, rows of 2^31 positions or more.
  */
 typedef struct {
     int32_t *refs;

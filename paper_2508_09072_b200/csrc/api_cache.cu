@@ -13,6 +13,7 @@ namespace {
 using namespace reader;
 
 constexpr size_t kAlign = 256;
+constexpr int kMost = 1 << 30;   // pages, requests, sequences of a call: the kernels count them in steps, in 32 bits
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -47,6 +48,7 @@ reader_status convert(bool store, reader_ctx *ctx, const reader_kv_cache *from, 
     if (!ctx) return READER_ERR_INVALID_ARG;
     if (batch == 0) return READER_OK;
     if (!from || !to || n_layers < 1 || batch < 0 || !first || !last || !status_out) return READER_ERR_INVALID_ARG;
+    if (batch > kMost) return READER_ERR_UNSUPPORTED;
     if (reader_status st = check_layers(from, n_layers)) return st;
     if (reader_status st = check_layers(to, n_layers)) return st;
     if (from[0].n_kv_heads != to[0].n_kv_heads || from[0].head_dim != to[0].head_dim) return READER_ERR_INVALID_ARG;
@@ -131,7 +133,7 @@ PagesWs carve(const PagesLayout &w, void *workspace) {
 }
 reader_status check_pages(const reader_pages *p, bool with_pools) {
     if (!p || !p->refs || !p->page_table || !p->seq_lens || p->num_pages < 1 || p->rows < 1 || p->max_pages_per_seq < 1) return READER_ERR_INVALID_ARG;
-    if ((int64_t)p->max_pages_per_seq * kPage >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
+    if ((int64_t)p->max_pages_per_seq * kPage >= (int64_t)1 << 31 || p->num_pages > kMost) return READER_ERR_UNSUPPORTED;
     if (!with_pools) return READER_OK;
     if (!p->pools || p->n_pools < 1 || p->page_bytes == 0 || p->page_bytes % 16 != 0) return READER_ERR_INVALID_ARG;
     if (p->page_bytes >= (size_t)1 << 31) return READER_ERR_UNSUPPORTED;
@@ -157,7 +159,7 @@ reader_status pool_chunks(const void *const *from, void *const *to, int n, std::
 // What fork, reserve and compact share: the workspace, and sums of at most n * width pages in 32 bits.
 reader_status check_requests(const reader_pages *p, int n, const void *workspace, size_t workspace_bytes) {
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return READER_ERR_INVALID_ARG;
-    if ((int64_t)n * p->max_pages_per_seq >= (int64_t)1 << 31) return READER_ERR_UNSUPPORTED;
+    if ((int64_t)n * p->max_pages_per_seq >= (int64_t)1 << 31 || n > kMost) return READER_ERR_UNSUPPORTED;
     if (workspace_bytes < pages_layout(p->num_pages, p->rows, p->max_pages_per_seq, n).total) return READER_ERR_WORKSPACE;
     return READER_OK;
 }
@@ -184,6 +186,7 @@ reader_status reader_q4_commit(reader_ctx *ctx, const reader_kv_cache *caches, c
     if (!caches || !k_trees || !v_trees || n_layers < 1 || batch < 0 || n_nodes < 1 || n_nodes > kMaxNodes || max_path < 1 || !path || !n_acc ||
         !slots_out || !status_out)
         return READER_ERR_INVALID_ARG;
+    if (batch > kMost) return READER_ERR_UNSUPPORTED;
     if (reader_status st = check_layers(caches, n_layers)) return st;
     for (int i = 0; i < n_layers; ++i)
         if (!caches[i].seq_lens || caches[i].seq_lens != caches[0].seq_lens || !k_trees[i] || !v_trees[i] || !aligned16(k_trees[i]) || !aligned16(v_trees[i]))
@@ -277,7 +280,7 @@ reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_
 }
 
 size_t reader_pages_workspace_bytes(int32_t num_pages, int32_t rows, int32_t max_pages_per_seq, int32_t n) {
-    if (num_pages < 1 || rows < 1 || max_pages_per_seq < 1 || n < 0 || (int64_t)n * max_pages_per_seq >= (int64_t)1 << 31) return 0;
+    if (num_pages < 1 || num_pages > kMost || rows < 1 || max_pages_per_seq < 1 || n < 0 || n > kMost || (int64_t)n * max_pages_per_seq >= (int64_t)1 << 31) return 0;
     return pages_layout(num_pages, rows, max_pages_per_seq, n).total;
 }
 
@@ -316,6 +319,7 @@ reader_status reader_pages_free(reader_ctx *ctx, const reader_pages *pages, cons
     if (n == 0) return READER_OK;
     if (reader_status st = check_pages(pages, false)) return st;
     if (n < 0 || !rows || !status_out) return READER_ERR_INVALID_ARG;
+    if (n > kMost) return READER_ERR_UNSUPPORTED;
     if (reader_status st = check_device(ctx)) return st;
     launch_pages_free(view(pages), rows, keep, n, status_out, (cudaStream_t)stream);
     return launch_status();
@@ -343,7 +347,7 @@ reader_status reader_pages_copy(reader_ctx *ctx, const void *const *from_pools, 
     if (!from_pools || !to_pools || from_pages < 0 || to_pages < 0 || n_pools < 1 || page_bytes == 0 || page_bytes % 16 != 0 || n < 0 || !from_ids ||
         !to_ids || !status_out)
         return READER_ERR_INVALID_ARG;
-    if (page_bytes >= (size_t)1 << 31) return READER_ERR_UNSUPPORTED;
+    if (page_bytes >= (size_t)1 << 31 || n > kMost) return READER_ERR_UNSUPPORTED;
     for (int i = 0; i < n_pools; ++i)
         if (!from_pools[i] || !to_pools[i] || !aligned16(from_pools[i]) || !aligned16(to_pools[i])) return READER_ERR_INVALID_ARG;
     if (reader_status st = check_device(ctx)) return st;

@@ -1,4 +1,5 @@
 """The 4-bit cache and the page calls without a GPU: what their code does on the host, and device functions that are plain C++ run there."""
+import ctypes
 import os
 import subprocess
 
@@ -83,3 +84,43 @@ def test_the_walk_ends_whatever_the_parents_are(walk):
             for j in range(128):   # the node itself, and none above it
                 word = got[:, j, 0].astype(object) + (got[:, j, 1].astype(object) << 64)
                 assert all((w >> j) == 1 for w in word)
+
+
+# ---------------------------------------------------------------------------------------------- refusals
+class Pages(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("rows", ctypes.c_int32),
+                ("max_pages_per_seq", ctypes.c_int32), ("seq_lens", ctypes.c_void_p), ("pools", ctypes.c_void_p), ("n_pools", ctypes.c_int32),
+                ("page_bytes", ctypes.c_size_t), ("new_ids", ctypes.c_void_p)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("max_pages_per_seq", ctypes.c_int32),
+                ("seq_lens", ctypes.c_void_p), ("shared_prefix_len", ctypes.c_int32)]
+
+
+@pytest.mark.parametrize("many", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_counts_that_32_bit_loops_cannot_pass_are_refused(many):
+    """Before anything is launched, and before anything behind an address is looked at (here none is one)."""
+    from paper_2508_09072_b200 import binding
+    lib = binding.load_library()
+    at, i, size, no, bad = ctypes.c_void_p(1 << 20), ctypes.c_int32, ctypes.c_size_t, ctypes.c_void_p(None), binding.ERR_UNSUPPORTED
+    pool = (ctypes.c_void_p * 1)(1 << 20)
+    pools = ctypes.cast(pool, ctypes.c_void_p)
+
+    def pages(num_pages):
+        return ctypes.byref(Pages(1 << 20, num_pages, 1 << 20, 8, 1, 1 << 20, pools, 1, 16, None))
+    few, huge = pages(100), pages(many)
+    ws, room, n = ctypes.c_void_p(1 << 20), size(1 << 50), i(many)
+    for p, count in ((huge, i(1)), (few, n)):
+        assert lib.reader_pages_fork(at, p, at, at, count, ws, room, at, no) == bad
+        assert lib.reader_pages_reserve(at, p, at, at, count, ws, room, at, no) == bad
+        assert lib.reader_pages_free(at, p, at, at, count, at, no) == bad
+    assert lib.reader_pages_compact(at, huge, at, ws, room, no) == bad
+    assert lib.reader_pages_copy(at, pools, i(9), pools, i(9), i(1), size(16), at, at, n, at, no) == bad
+    need = lib.reader_pages_workspace_bytes
+    assert need(many, 8, 1, 1) == 0 and need(100, 8, 1, many) == 0 and need(2 ** 30, 8, 1, 2 ** 30) > 0
+    wide, narrow = (Cache(1 << 20, 1 << 20, 4, 64, 2, 64, 1 << 20, 1, 1 << 20, 0) for _ in range(2))
+    assert lib.reader_q4_store(at, ctypes.byref(wide), ctypes.byref(narrow), i(1), n, at, at, at, no) == bad
+    assert lib.reader_q4_load(at, ctypes.byref(narrow), ctypes.byref(wide), i(1), n, at, at, at, no) == bad
+    assert lib.reader_q4_commit(at, ctypes.byref(narrow), pools, pools, i(1), n, i(4), at, at, i(4), i(1), at, at, no) == bad
