@@ -707,8 +707,8 @@ class Reader:
 
     # ---- the pages of a cache
     def pages_workspace(self, pages: Pages, n: int = 0) -> torch.Tensor:
-        """A cached device buffer for page calls of n requests.  A larger one is made when it is needed; those before it live as long
-        as the reader (a captured call may use them)."""
+        """A cached device buffer for page calls of n requests.  A larger one, of twice the size at least, is made when it is needed; those
+        before it live as long as the reader (a captured call may use them), and are no larger than it together."""
         sizes = (pages.refs.shape[0], *pages.page_table.shape, n)
         need = self._pages_need.get(sizes)   # (asking the library costs as much as a third of the call)
         if need is None:
@@ -719,7 +719,8 @@ class Reader:
                 self._pages_need.clear()
             self._pages_need[sizes] = need
         if not self._pages_ws or self._pages_ws[-1].numel() < need:
-            self._pages_ws.append(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
+            room = max(need, 2 * self._pages_ws[-1].numel()) if self._pages_ws else need
+            self._pages_ws.append(torch.empty(room, dtype=torch.uint8, device=f"cuda:{self.device}"))
         return self._pages_ws[-1]
 
     def pages_fork(self, pages: Pages, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None,

@@ -201,3 +201,16 @@ def test_new_ids_that_cannot_be(rd):
                          (torch.zeros(20, dtype=torch.int32), TypeError), (torch.zeros(40, dtype=torch.int32, device="cuda")[::2], TypeError)):
         with pytest.raises(error, match="new_ids"):
             rd.pages_compact(p, new_ids=wrong)
+
+
+def test_workspaces_of_growing_calls_take_little_room():
+    """Calls that have a few requests more each time: all the buffers together are less than twice what the largest call may be given."""
+    from paper_2508_09072_b200 import binding as b
+    reader = b.Reader(0)
+    p = Model(np.random.default_rng(65), 20, 4, 4000, 1, 16).device()
+    for n in range(1, 400, 3):
+        ws = reader.pages_workspace(p, n)
+        need = reader.lib.reader_pages_workspace_bytes(20, 4, 4000, n)
+        assert need <= ws.numel() <= max(2 * need, reader._pages_ws[0].numel())
+        assert sum(x.numel() for x in reader._pages_ws) <= 2 * ws.numel()
+    reader.close()
