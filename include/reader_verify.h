@@ -559,7 +559,8 @@ size_t reader_q4_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  * n_kv_heads * (n_nodes * n_q_heads / n_kv_heads / 16 + 1) * (max_pages_per_seq + 4) below 2^31.
  * Bytes at positions that are not committed have no influence, whatever they are.  A row that sees nothing (an anc_mask without the
  * node itself, on an empty cache) is zero, its lse -inf.
- * Arithmetic: fp32 accumulation and softmax, probabilities rounded to bf16 before the value product, bf16 (nearest-even) output.
+ * Arithmetic: fp32 accumulation and softmax (an exponent, in log2 units, to 2^-23 of the row's largest scaled score), probabilities
+ * rounded to bf16 before the value product, bf16 (nearest-even) output.
  */
 reader_status reader_q4_verify_attn(reader_ctx *ctx, const void *q, int32_t n_q_heads, const void *k_tree, const void *v_tree,
                                     const reader_kv_cache *cache, const reader_tree *tree, float softmax_scale, void *out,

@@ -723,9 +723,11 @@ __global__ void __launch_bounds__(kThreads, 1) q4_attn_sm100_kernel(const __grid
                             }
                         }
                     }
-                    // 2^((s - max) scale) by one multiplication and addition.  The maximum times the scale is rounded, by the same for all keys of a
-                    // row: it cancels, but where it is so large that its rounding is not small against 1, or beyond fp32, the difference is taken first.  (A row
-                    // without a query, and one with an infinite score, has an infinite maximum: no difference helps.)
+                    // 2^((s - max) scale) by one multiplication and addition.  The maximum times the scale is rounded, by the same for all keys that are weighed with
+                    // this maximum, among which that cancels; between steps and shares with other maxima it does not, and is 2^-24 of the scaled maximum at most, as
+                    // fp32 scores of that size themselves are: up to 65536, 2^-9 or 0.14 % of a weight, a third of what a probability's rounding to bf16 may be.
+                    // Beyond that, or beyond fp32, the difference is taken first.  (A row without a query, and one with an infinite score, has an infinite maximum: no
+                    // difference helps.)
                     float from = mx == -INFINITY ? 0.f : -mx * p.scale_log2;
                     if (__any_sync(0xffffffffu, fabsf(from) > 65536.f && fabsf(mx) < INFINITY)) {
 #pragma unroll 1

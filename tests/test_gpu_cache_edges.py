@@ -129,6 +129,34 @@ def test_the_smallest_scales(rd, size, scale, T, columns):
     within((out, lse), (o, z, tol + 2.0 ** -23 * 8, ltol + 2.0 ** -23))
 
 
+@pytest.mark.parametrize("T,group", [(1, 4), (40, 2), (100, 3)])
+@pytest.mark.parametrize("big", [2048.0, 4096.0, 6144.0, 8192.0, 65536.0])
+def test_shares_with_large_maxima_of_their_own(rd, big, T, group):
+    """One long sequence cut into many shares whose largest scores differ by a few units beside 2^14 to 2^19 (scaled, in log2 units).  Scores have two terms and are rounded
+    once at most: what counts is the exponents' 2^-23 of the largest scaled score, and 2^-8 for the roundings to bf16 of a probability and of the output."""
+    rng = np.random.default_rng(66)
+    L, d = 9000, 64
+    both, cache, q, kt, vt, parent = make(rng, [L], T, 1, group, d)
+    pos = torch.arange(L)
+    page, at = torch.from_numpy(both.t16[0])[pos // 64].long().cuda(), (pos % 64).cuda()
+    level = torch.from_numpy(rng.integers(-3, 4, L // 512 + 1)).repeat_interleave(512)[:L] + torch.from_numpy(rng.integers(-4, 1, L))
+    both.k.zero_()
+    both.k[page, 0, at, 3] = 7.0                                        # (7 of a scale of 1)
+    both.k[page, 0, at, 20] = (level / 4).to(torch.bfloat16).cuda()     # (whole numbers up to 7 of a scale of 1 / 4 or less)
+    rd.q4_store([both.wide], [both.narrow], i32([0]), i32([L]))
+    kt = torch.zeros_like(kt)
+    kt[..., 3], kt[..., 20] = 7.0, 0.25
+    q = torch.zeros_like(q)
+    q[..., 3], q[..., 20] = big, 2.0
+    out, lse, st = attend(rd, cache, q, kt, vt, parent, 1.0)
+    assert st == [0]
+    o, z, mag = plain_rows(both, [L], q, kt, vt, parent, 1.0)
+    off = 2.0 ** -23 * 7 * big * 1.4427 * 2 * np.log(2)     # of a weight, and of the sum that it is divided by
+    off += (L + T) * 2.0 ** -23
+    assert ((out.double() - o).abs() <= 2.0 ** -8 * (mag + o.abs()) * 1.01 + mag * off).all()
+    assert ((lse.double() - z).abs() <= off + z * 2.0 ** -23).all()
+
+
 # ---------------------------------------------------------------------------------------------- pages
 @pytest.mark.parametrize("rows", [7, 70])
 def test_rows_without_a_committed_page_get_none(rd, rows):
