@@ -129,6 +129,40 @@ def test_the_smallest_scales(rd, size, scale, T, columns):
     within((out, lse), (o, z, tol + 2.0 ** -23 * 8, ltol + 2.0 ** -23))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,group,columns", [(1, 4, None), (1, 4, 700), (4, 4, None), (4, 4, 700), (40, 2, None), (100, 3, None)])
+def test_a_readers_first_call_may_be_captured(T, group, columns, d):
+    """What a context asks about its kernels once, it may ask while a graph is captured."""
+    from paper_2508_09072_b200 import binding as b
+    rng = np.random.default_rng(67)
+    lens = [300, 5]
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 1, group, d)
+    if columns:
+        cache = widened(cache, columns)
+    args = q.cuda(), kt.cuda(), vt.cuda(), cache, i32(parent), 0.1
+    out, status = torch.empty_like(args[0]), torch.full((2,), 7, dtype=torch.int32, device="cuda")
+    reader = b.Reader(0)
+    ws = torch.empty_like(reader.q4_workspace())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        reader.q4_verify_attn(*args, out=out, status=status, workspace=ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    o, _, tol, _ = plain_attn(both, lens, q, kt, vt, parent, 0.1)
+    assert status.tolist() == [0, 0] and ((out.cpu().double() - o).abs() <= tol).all()
+    del graph
+    reader.close()
+
+
+@pytest.mark.parametrize("d,group,T,lens", [(64, 4096, 1, [70]), (64, 4095, 7, [0, 200]), (128, 4093, 33, [130]), (64, 4095, 128, [64]), (128, 257, 1, [1000, 3])])
+def test_the_widest_groups(rd, d, group, T, lens):
+    rng = np.random.default_rng(group + T)
+    both, cache, q, kt, vt, parent = make(rng, lens, T, 1, group, d)
+    got = attend(rd, cache, q, kt, vt, parent, 0.1)
+    assert got[2] == [0] * len(lens)
+    within(got[:2], plain_attn(both, lens, q, kt, vt, parent, 0.1))
+
+
 @pytest.mark.parametrize("T,group", [(1, 4), (40, 2), (100, 3)])
 @pytest.mark.parametrize("big", [2048.0, 4096.0, 6144.0, 8192.0, 65536.0])
 def test_shares_with_large_maxima_of_their_own(rd, big, T, group):
