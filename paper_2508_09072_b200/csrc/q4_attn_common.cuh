@@ -107,8 +107,7 @@ struct Unit {
     int w0;                  // flat index of the unit's first entry
     int entries;             // of the flat list that this range has of the unit
     bool any;
-    // the flat entries of the first and the last tile
-    __device__ __forceinline__ int first_entry(int cost) const { return w0 + cost; }
+    // the flat entry of the last tile
     __device__ __forceinline__ int last_entry(int cost) const { return w0 + cost + weight * (ntiles - 1); }
 };
 
