@@ -557,6 +557,8 @@ size_t reader_q4_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  * READER_ERR_UNSUPPORTED unless: softmax_scale > 0 and at most 2e38; n_q_heads a multiple of n_kv_heads, at most 4096
  * times it; batch at most 65536; and batch *
  * n_kv_heads * (n_nodes * n_q_heads / n_kv_heads / 16 + 1) * (max_pages_per_seq + 4) below 2^31.
+ * Small calls run as one launch, which goes by the page table's width: a token on 511 positions (32 query and 8 KV heads of 128) takes 7 to
+ * 9 us, 13 behind a table of more than 191 pages; eight of them 8 us, 18 behind more than 95.
  * Bytes at positions that are not committed have no influence, whatever they are.  A row that sees nothing (an anc_mask without the
  * node itself, on an empty cache) is zero, its lse -inf.
  * Arithmetic: fp32 accumulation and softmax (an exponent, in log2 units, to 2^-23 of the row's largest scaled score), probabilities

@@ -7,10 +7,10 @@
 //
 // The bookkeeping of fork, reserve and compact needs answers over the whole batch or the whole pool between its steps (which page
 // is the k-th free one).  One launch does it, between whose steps all threads wait for one another: a thread block where requests and pool are few, else a cluster
-// of eight (four rows released, forked and given pages: 14.1 us by one block, 17.8 by a cluster; 128 rows of 32: 41 and 33); a prefix sum over several kernels
+// of eight (four rows released, forked and given pages: 12.4 us by one block, 16.4 by a cluster; 128 rows of 32: 42.7 and 34.5); a prefix sum over several kernels
 // would cost a launch per step.  Data move in a second launch (2 x page_bytes per page and pool, 16 KB of a page to a thread block with all its loads
-// in flight at once), which is bound by the copy bandwidth.  Measured: four rows released (1.8 us), forked from one of 700 positions (4.0) and given pages
-// 14.1 us; 128 rows of 32 with 16 pools of 36 KB 33 us, 23 of them the pages' bytes; a pool of 4096 pages compacted (8 pools of 36 KB) 107 us, 91 of them bytes.
+// in flight at once), which is bound by the copy bandwidth.  Measured: four rows released, forked from one of 700 positions and given pages
+// 12.4 us; 128 rows of 32 with 16 pools of 36 KB 34.5 us, 23 of them the pages' bytes; a pool of 4096 pages compacted (8 pools of 36 KB) 109 us, 91 of them bytes.
 #include <climits>
 
 #include "pages.cuh"
@@ -73,7 +73,8 @@ __device__ __forceinline__ int block_rank(int x, int &total) {
 }
 
 // Which request is the first that names a row.  Up to kNamed requests: by looking through those before it, in shared memory.  More: each row is marked with
-// its first request, two steps in global memory, each followed by the cluster's barrier (2 us more of a call's 5).
+// its first request, two steps in global memory, each followed by the cluster's barrier (rows forked, looked through and marked: 64 4.7 and 6.1 us, 512 7.6 and 8.6, 1024 13.9 and
+// 13.0 to 14.8, 2000 26.5 and 23.6).
 constexpr int kNamed = 512;
 template <int kBlocks>
 struct Named {
@@ -464,7 +465,8 @@ unsigned moves_of(int n) { return (unsigned)(n < 65535 ? n : 65535); }
 
 }  // namespace
 
-// Up to here a call is one thread block's.
+// Up to here a call is one thread block's.  Requests, by one block and by a cluster: 32 rows forked in 3.7 and 4.5 us, 33 in 5.5 and 4.6; 32 given pages and released again 8.4 and
+// 11.8, 64 10 and 12, 128 13.4 and 12.3.  Pages, the books of a compaction: 4096 8.8 and 10.2, 6000 11.8 and 11.1, 16384 22.5 and 15.4.
 constexpr int kOneBlockRequests = 32, kOneBlockPages = 4096;
 
 void launch_pages_fork(const PagesView &p, const int32_t *src, const int32_t *dst, int n, const PagesWs &ws, int32_t *status, cudaStream_t st) {

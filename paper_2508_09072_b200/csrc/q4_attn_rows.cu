@@ -7,8 +7,8 @@
 // nothing that is not its own.  The A fragments are unpacked in registers, two bf16 in 2.75 instructions; the pages are laid
 // out so that a lane's words, and their scales, are one or two 16-byte loads.  (Feeding tcgen05.mma instead means writing every
 // tile in bf16 to shared memory and reading it back: worth it once many rows share it, not for 4 or 16.)  Measured (32 query heads, 8 KV heads, head_dim 128):
-// single tokens on 32 contexts of 1024-4096 33 us, 0.43 of the copy bandwidth, 25 to 28 of them the walk; on 64 of 2048-8192 87 us, 0.68;
-// one token on 511 (8 heads, head_dim 64) 5.7 us.  A product's inner order
+// single tokens on 32 contexts of 1024-4096 34 us, 0.44 of the copy bandwidth, 25 to 28 of them the walk; on 64 of 2048-8192 87 us, 0.68;
+// one token on 511 (8 heads, head_dim 64) 6.1 us.  A product's inner order
 // is free as long as both operands agree: of the elements, lane (g, c) = (lane / 4, lane % 4) has D/4 consecutive ones of a key,
 // and D/8 consecutive ones of a pair of values, with one or two scales; P^T gets from the score product's result to the value
 // product's operand by one transposing move per 8 x 8 block.
@@ -34,7 +34,9 @@ namespace {
 
 using namespace q4;
 
-// Workers of a thread block, and their ring's slots (a tile of keys or of values each): what registers and shared memory allow.
+// Workers of a thread block, and their ring's slots (a tile of keys or of values each): what registers and shared memory allow.  At head_dim 128 registers do not
+// quite: of 128 to a thread the list form's kernel for 8 rows spills 36 bytes (64 read back), of 168 that for 16 rows 208 (272); the form of one launch 8 (16) and
+// 88 (152).
 template <int NT>
 struct Shape {
     static constexpr int kWarps = NT == 1 ? 16 : 12, kSlots = NT == 1 ? 3 : 4;
@@ -693,7 +695,8 @@ __global__ void __launch_bounds__(Shape<NT>::kThreads, 1) q4_attn_list_kernel(co
 
 // Units that several workers have shares of: those that the workers of block blockIdx.x of the attention begin, some rows of each, a thread to four
 // elements of a row.  Four groups of threads take a unit each; a long one (at most one of a block's workers begins a unit that goes on behind
-// the block) is all groups' at once.  (By a group alone the 300 shares of each unit of a single token on 32768 took 30 us.)
+// the block) is all groups' at once.  (Single tokens, 32/8/128, by all groups and by one: one on 32768, 300 shares a unit, 28.4 and 44.9 us; 16 on 4096, 18 shares, 27.5
+// and 28.7.  Fewer than 17 may be several in a block.)
 constexpr int kGroup = 128, kGroups = 4, kLongTask = 16;
 template <int D, int NT>
 __global__ void __launch_bounds__(kGroup *kGroups) q4_attn_list_merge_kernel(const __grid_constant__ Q4AttnParams p) {
@@ -827,7 +830,11 @@ __global__ void __launch_bounds__(1024) q4_attn_status_kernel(int32_t *status, i
 
 // Thread blocks of a unit in the alone form, 0 if the call is not one for it: the units of a sequence have to fit a cluster, the clusters the GPU all at once (8
 // single tokens on 2048, 32/8/128: eight clusters of 16 blocks in two turns 20.8 us, of 8 in one 13.9; 4 of them 11.2 and 13.5), and,
-// going by the page table's width, a worker gets at most `most` tiles.
+// going by the page table's width, a worker gets at most `most` tiles.  Few rows: six.  The width is what a sequence may grow to, and short ones gain: 511 positions
+// (32/8/128) behind a table of any allowed width take 7.2 to 9.0 us instead of the list form's 12.8, of eight sequences 8.3 instead of 18.0.  Those that fill their table gain
+// up to two tiles a worker (4032 positions 14.2 instead of 15.6, eight of 1984 13.3 instead of 16.8; one KV head's 98240, six tiles, 31.9 instead of 33.2), eight
+// up to four (4032 positions 21.9 instead of 22.9), and lose at six (12224 positions 30.8 instead of 17.6, eight of 6080 30.3 instead of 27.2); at seven the alone form
+// would lose by as much or more (34.9 instead of 17.6, 34.5 instead of 27.7).
 constexpr int kAloneTiles = 6, kAloneTilesManyRows = 2;
 template <int NT>
 int alone_split(const Q4AttnParams &p, const Q4RowsKernels &k, int most) {

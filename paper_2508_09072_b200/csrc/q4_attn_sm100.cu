@@ -2,8 +2,8 @@
 //
 // Bound: the tensor pipe and the exponentials, 2048 cycles each for 256 query rows and 128 keys; what 4 bits add is turning
 // numbers into bf16 operands, 16384 of them for each, once for all rows that share them.  Measured (32 query heads, 8 KV heads, head_dim 128): four trees of 128
-// nodes on 32768 positions 316 us, 0.87 PF/s; 32 trees of 32 nodes on 1024-4096 80 us.  Either way a step of 128 rows and 128 keys is 1.4 to 1.7 us,
-// the softmax warps' 0.3 for the maximum and 0.85 to 1.05 for 8192 exponentials (0.54 if nothing else ran) and hardly a wait.  So a thread block (one per SM) has up to
+// nodes on 32768 positions 314 us, 0.88 PF/s; 32 trees of 32 nodes on 1024-4096 83 us.  Either way a step of 128 rows and 128 keys is 1.4 to 1.7 us,
+// the softmax warps' 0.3 for the maximum and 0.85 to 1.05 for 16384 exponentials (0.54 if nothing else ran) and hardly a wait.  So a thread block (one per SM) has up to
 // 256 rows of one KV head, two slots of 128, and eight warps of it do nothing but unpack: a tile of 128 keys (two pages) becomes
 // the rows of K, and its values the rows of V^T (position pairs are neighbours in the pages, so a pair of numbers is a
 // pair of bf16 along the value product's inner axis as it stands), in the 128-byte swizzle of the matrix instructions.
@@ -44,14 +44,15 @@ constexpr int kSoftmaxThreads = 256;
 constexpr int kUnpackWarp = 8, kLoadWarp = 16, kMmaWarp = 17, kQueryWarp = 18, kListWarp = 19;
 constexpr int kUnpackThreads = 128, kUnpackWarps = 4;   // of a tile
 constexpr int kReaders = 19;       // warps that read the ring of units: all but kListWarp
-// Registers of a thread: softmax, unpacking, the rest: 256 x 112 + 256 x 96 + 128 x 64 = the 640 x 96 that the block is launched with.
+// Registers of a thread: softmax, unpacking, the rest: 256 x 112 + 256 x 96 + 128 x 64 = the 640 x 96 that the block is launched with.  (24 bytes are spilled, 28 read
+// back; at head_dim 64 20 and 24.)
 constexpr int kRegsSoftmax = 112, kRegsUnpack = 96, kRegsRest = 64;
 static_assert(2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsRest <= 5 * 96 && kRegsSoftmax >= 96 && kRegsUnpack <= 96 && kRegsRest <= 96, "what a block is launched with");
 constexpr int kTileKeys = 128;     // keys of a tile: two pages
-constexpr int kUnitCost = 4;       // entries that stand for a unit's start and end (6: 32 x 32 nodes 82 instead of 80 us)
+constexpr int kUnitCost = 4;       // entries that stand for a unit's start and end (32 x 32 nodes, 4 x 128 on 32768: 82.8, 314 us; 2: 82.7, 316; 6: 84.8, 314)
 constexpr int kMinEntries = kUnitCost + 2;   // of a range: so every one of them holds a tile
 // Slots of the ring, keys or values of a tile's pages each: three, and three more in a call without wide units, in the half of the queries' place that it does
-// not need (with three the narrow units' tiles came too late: 32 x 32 nodes 80 us).
+// not need (with three the narrow units' tiles come too late: 32 x 32 nodes 84.7 us, with six 82.9).
 constexpr int kRawSlots = 3;
 constexpr int kAhead = 8;          // units in the ring
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;
