@@ -560,7 +560,8 @@ size_t reader_q4_workspace_bytes(const reader_ctx *ctx, int32_t head_dim);
  * Small calls run as one launch, which goes by the page table's width: a token on 511 positions (32 query and 8 KV heads of 128) takes 7 to
  * 9 us, 13 behind a table of more than 191 pages; eight of them 8 us, 18 behind more than 95.
  * Bytes at positions that are not committed have no influence, whatever they are.  A row that sees nothing (an anc_mask without the
- * node itself, on an empty cache) is zero, its lse -inf.
+ * node itself, on an empty cache) is zero, its lse -inf.  Infinite or NaN values of a node reach the rows that see it, and no others; where
+ * an infinite one's weight is 0 in fp32, as infinity or as NaN.
  * Arithmetic: fp32 accumulation and softmax (an exponent, in log2 units, to 2^-23 of the row's largest scaled score), probabilities
  * rounded to bf16 before the value product, bf16 (nearest-even) output.
  */
