@@ -23,8 +23,8 @@
  *   reader_prompt_attn (its causal attention over the paged cache) and reader_tree_rotate (the same norms and rotation
  *   for draft nodes);
  *   and the cache itself: held in 4 bits, reader_q4_store / reader_q4_load / reader_q4_commit and reader_q4_verify_attn (the attention
- *   over it, draft trees and single tokens); its pages, reader_pages_fork / reader_pages_reserve / reader_pages_free / reader_pages_compact /
- *   reader_pages_copy.
+ *   over it, draft trees and single tokens); its pages, reader_pages_fork / reader_pages_reserve / reader_pages_free / reader_pages_compact
+ *   (reader_pages_compact_map) / reader_pages_copy.
  *
  * Conventions common to every call
  *   - Every pointer named below is a DEVICE pointer owned by the caller unless it says "host".
@@ -579,12 +579,11 @@ reader_status reader_set_q4_give_up(reader_ctx *ctx, int32_t worker);
  * after the table on the device, without a host that waits for lengths, for caches of either kind.
  *   refs         i32 [num_pages]: how many entries of the page table name a page; 0 = the page is free.  The caller sets it up
  *                (all zero for an empty cache); pages that are not to be handed out get a count of their own (a compaction moves
- *                them as it moves others: new_ids tells where to)
+ *                them as it moves others: reader_pages_compact_map tells where to)
  *   page_table   i32 [rows][max_pages_per_seq], -1 = no page (as for reader_kv_cache: one table for all layers of a model)
  *   seq_lens     i32 [rows]
  *   pools        HOST array [n_pools] of device pointers, 16-byte aligned: every pool whose pages the table names (keys and
  *                values of all layers), each num_pages * page_bytes bytes; page_bytes is a multiple of 16
- *   new_ids      i32 [num_pages] or NULL, written by reader_pages_compact alone
  * Row numbers, counts and lengths live on the device; requests come as arrays [n], answers as status_out[n].  A request with a
  * status other than READER_OK changes nothing, unless it says so, and does not disturb the others.
  * Free pages are handed out lowest number first, in the order of the requests: the same inputs give the same pages.
@@ -600,7 +599,6 @@ typedef struct {
     void *const *pools;
     int32_t n_pools;
     size_t page_bytes;
-    int32_t *new_ids;
 } reader_pages;
 
 /* Bytes of device scratch that reader_pages_fork, reader_pages_reserve (of at most n requests) and reader_pages_compact need.
@@ -647,13 +645,17 @@ reader_status reader_pages_free(reader_ctx *ctx, const reader_pages *pages, cons
  * Moves the pages in use to the front of the pools: with n of them, those numbered n and above move, in ascending order, to the
  * free numbers below n, in ascending order; page_table and refs follow, the data of all pools move.  As few pages move as can.
  * Pages with a count of the caller's own move like the others, and so do those that another table over the same pools names:
- * who keeps numbers anywhere but in page_table needs new_ids.
+ * who keeps numbers anywhere but in page_table needs reader_pages_compact_map.
  *   n_used_out  i32 [1]: pages in use; pages from that number on are free afterwards
- *   pages->new_ids  each page's new number, its own if it stays, -1 if it was free
  * workspace as for reader_pages_fork (any n).
  */
 reader_status reader_pages_compact(reader_ctx *ctx, const reader_pages *pages, int32_t *n_used_out, void *workspace,
                                    size_t workspace_bytes, void *stream);
+
+/* reader_pages_compact that tells where pages went.
+ *   new_ids_out  i32 [num_pages] (NULL: not told): each page's new number, its own if it stays, -1 if it was free */
+reader_status reader_pages_compact_map(reader_ctx *ctx, const reader_pages *pages, int32_t *n_used_out, int32_t *new_ids_out,
+                                       void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Copies page from_ids[i] of from_pools[j] to page to_ids[i] of to_pools[j], for all i < n and j < n_pools: within pools or to others

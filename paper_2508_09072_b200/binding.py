@@ -33,7 +33,7 @@ EXPORTS = ("reader_create", "reader_destroy", "reader_status_string", "reader_se
            "reader_set_prompt_give_up",
            "reader_q4_store", "reader_q4_load", "reader_q4_commit", "reader_q4_workspace_bytes", "reader_q4_verify_attn",
            "reader_set_q4_give_up", "reader_pages_workspace_bytes", "reader_pages_fork", "reader_pages_reserve", "reader_pages_free",
-           "reader_pages_compact", "reader_pages_copy")
+           "reader_pages_compact", "reader_pages_compact_map", "reader_pages_copy")
 
 
 class ReaderError(RuntimeError):

@@ -141,7 +141,7 @@ reader_status check_pages(const reader_pages *p, bool with_pools) {
         if (!p->pools[i] || !aligned16(p->pools[i])) return READER_ERR_INVALID_ARG;
     return READER_OK;
 }
-PagesView view(const reader_pages *p) { return {p->refs, p->num_pages, p->page_table, p->rows, p->max_pages_per_seq, p->seq_lens, p->new_ids}; }
+PagesView view(const reader_pages *p) { return {p->refs, p->num_pages, p->page_table, p->rows, p->max_pages_per_seq, p->seq_lens, nullptr}; }
 
 reader_status pool_chunks(const void *const *from, void *const *to, int n, std::vector<PoolList> &chunks) {
     try {
@@ -326,6 +326,11 @@ reader_status reader_pages_free(reader_ctx *ctx, const reader_pages *pages, cons
 }
 
 reader_status reader_pages_compact(reader_ctx *ctx, const reader_pages *pages, int32_t *n_used_out, void *workspace, size_t workspace_bytes, void *stream) {
+    return reader_pages_compact_map(ctx, pages, n_used_out, nullptr, workspace, workspace_bytes, stream);
+}
+
+reader_status reader_pages_compact_map(reader_ctx *ctx, const reader_pages *pages, int32_t *n_used_out, int32_t *new_ids_out, void *workspace,
+                                       size_t workspace_bytes, void *stream) {
     if (!ctx) return READER_ERR_INVALID_ARG;
     if (reader_status st = check_pages(pages, true)) return st;
     if (!n_used_out) return READER_ERR_INVALID_ARG;
@@ -333,7 +338,8 @@ reader_status reader_pages_compact(reader_ctx *ctx, const reader_pages *pages, i
     if (reader_status st = check_device(ctx)) return st;
     std::vector<PoolList> chunks;
     if (reader_status st = pool_chunks(pages->pools, pages->pools, pages->n_pools, chunks)) return st;
-    const PagesView v = view(pages);
+    PagesView v = view(pages);
+    v.new_ids = new_ids_out;
     launch_pages_compact(v, n_used_out, carve(pages_layout(v.num_pages, v.rows, v.width, 0), workspace), chunks.data(), pages->n_pools, pages->page_bytes,
                          ctx->n_sm, (cudaStream_t)stream);
     return launch_status();

@@ -519,8 +519,9 @@ PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
         pages_of(a[2], device, true, p);
         const at::Tensor &ws = dense(a[3], at::kByte, 1, device, "workspace");
         const at::Tensor used = output(a[4], {1}, at::kInt, device, "n_used");
-        if (n == 6 && a[5] != Py_None) p.p.new_ids = const_cast<int32_t *>(ints(a[5], p.p.num_pages, device, "new_ids"));
-        const reader_status st = reader_pages_compact(context(a[0]), &p.p, static_cast<int32_t *>(address(used)), address(ws), (size_t)ws.numel(), stream());
+        int32_t *new_ids = n == 6 && a[5] != Py_None ? const_cast<int32_t *>(ints(a[5], p.p.num_pages, device, "new_ids")) : nullptr;
+        const reader_status st =
+            reader_pages_compact_map(context(a[0]), &p.p, static_cast<int32_t *>(address(used)), new_ids, address(ws), (size_t)ws.numel(), stream());
         return results(st, {given_back(a[4], used)});
     });
 }

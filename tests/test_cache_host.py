@@ -90,7 +90,7 @@ def test_the_walk_ends_whatever_the_parents_are(walk):
 class Pages(ctypes.Structure):
     _fields_ = [("refs", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("rows", ctypes.c_int32),
                 ("max_pages_per_seq", ctypes.c_int32), ("seq_lens", ctypes.c_void_p), ("pools", ctypes.c_void_p), ("n_pools", ctypes.c_int32),
-                ("page_bytes", ctypes.c_size_t), ("new_ids", ctypes.c_void_p)]
+                ("page_bytes", ctypes.c_size_t)]
 
 
 class Cache(ctypes.Structure):
@@ -109,14 +109,14 @@ def test_counts_that_32_bit_loops_cannot_pass_are_refused(many):
     pools = ctypes.cast(pool, ctypes.c_void_p)
 
     def pages(num_pages):
-        return ctypes.byref(Pages(1 << 20, num_pages, 1 << 20, 8, 1, 1 << 20, pools, 1, 16, None))
+        return ctypes.byref(Pages(1 << 20, num_pages, 1 << 20, 8, 1, 1 << 20, pools, 1, 16))
     few, huge = pages(100), pages(many)
     ws, room, n = ctypes.c_void_p(1 << 20), size(1 << 50), i(many)
     for p, count in ((huge, i(1)), (few, n)):
         assert lib.reader_pages_fork(at, p, at, at, count, ws, room, at, no) == bad
         assert lib.reader_pages_reserve(at, p, at, at, count, ws, room, at, no) == bad
         assert lib.reader_pages_free(at, p, at, at, count, at, no) == bad
-    assert lib.reader_pages_compact(at, huge, at, ws, room, no) == bad
+    assert lib.reader_pages_compact(at, huge, at, ws, room, no) == lib.reader_pages_compact_map(at, huge, at, at, ws, room, no) == bad
     assert lib.reader_pages_copy(at, pools, i(9), pools, i(9), i(1), size(16), at, at, n, at, no) == bad
     need = lib.reader_pages_workspace_bytes
     assert need(many, 8, 1, 1) == 0 and need(100, 8, 1, many) == 0 and need(2 ** 30, 8, 1, 2 ** 30) > 0
